@@ -332,10 +332,13 @@ def _append_one(cache, lens, k, v):
     """One token for every sequence."""
     B, Hkv = k.shape[:2]
     b, at = torch.arange(B, device=k.device), (lens % BLOCK).long()
-    cache["kt"][b, :, at] = k[:, :, 0]
-    cache["vt"][b, :, :, at] = v[:, :, 0]
+    kt, vt, full = cache["kt"].clone(), cache["vt"].clone(), at == BLOCK - 1
+    kt[b, :, at] = k[:, :, 0]
+    vt[b, :, :, at] = v[:, :, 0]
     pages = torch.gather(cache["table"].long(), 2, (lens // BLOCK).long().view(B, 1, 1).expand(B, Hkv, 1))[..., 0]
-    _store(cache, pages, (at == BLOCK - 1).unsqueeze(1).expand(B, Hkv), cache["kt"].float(), cache["vt"].float().transpose(-1, -2))
+    _store(cache, pages, full.unsqueeze(1).expand(B, Hkv), kt.float(), vt.float().transpose(-1, -2))
+    for x, t in ((kt, "kt"), (vt, "vt")):   # (a block that is whole leaves nothing behind here)
+        cache[t].copy_(torch.where(full.view(B, 1, 1, 1), cache[t], x))
 
 
 def _append_prompts(cache, counts, k, v):
