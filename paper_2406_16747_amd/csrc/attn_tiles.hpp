@@ -286,6 +286,65 @@ __device__ __forceinline__ WaveRuns wave_runs(bool wave_live, int nkl, int nkc, 
     return r;
 }
 
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2v __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
+typedef float f32x4v __attribute__((ext_vector_type(4)));
+// two floats rounded to bf16 (nearest even), the first in the low half
+__device__ __forceinline__ unsigned pack_bf16x2(float a, float b)
+{
+    f32x2v f = {a, b};
+    return __builtin_bit_cast(unsigned, __builtin_convertvector(f, bf16x2v));
+}
+
+// A tile of 64 rows (Q or dO) in LDS serves 16-byte row reads (A operand of the contractions over the head dimension) and
+// transposing 8-byte reads (A operand of the contractions over the queries).  Every row lands once, in groups of 1 KB (a
+// wave-load) padded by 16 bytes; which rows share a group is chosen so that both kinds of reads touch every bank once per
+// pass: 16 consecutive rows differ in (group, slot) modulo the 16 chunks of 256 bytes, and 4 consecutive ones by multiples
+// of 4 chunks.  Unlike a permutation of the chunks inside a row this leaves every operand of a tile at a constant distance
+// from one address per lane (two in all, one for each kind of read), so tiles can sit in a ring without code of their own.
+template <int D>
+struct RowTile {
+    static constexpr int RB = D * 2, RPL = 1024 / RB, NL = KT / RPL;   // bytes per row, rows per group, groups
+    static constexpr int GS = 1024 + 16, BYTES = NL * GS;
+    // tile row r sits in group g(r), slot s(r)
+    __device__ static constexpr int group(int r) { return D == 128 ? 4 * (r & 3) + ((r >> 2) & 3) : 4 * (r & 1) + ((r >> 2) & 3); }
+    __device__ static constexpr int slot(int r) { return D == 128 ? r >> 4 : ((r >> 1) & 1) + 2 * (r >> 4); }
+    __device__ static constexpr int row(int g, int s)   // the inverse
+    {
+        return D == 128 ? (g >> 2) + 4 * (g & 3) + 16 * s : (g >> 2) + 2 * (s & 1) + 4 * (g & 3) + 16 * (s >> 1);
+    }
+    __device__ static constexpr int offset(int r) { return group(r) * GS + slot(r) * RB; }
+    static constexpr int R16 = 16 / (D == 128 ? 16 : 8) * RB;   // 16 rows on: the same group, so many bytes on
+    static constexpr int R8 = 2 * GS;                           // 8 rows on, from a row of 0 .. 7 modulo 16
+};
+
+typedef const unsigned char __attribute__((address_space(3)))* lds_bytes_t;
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(lds_void_t*)p; }
+// The operands of a RowTile: a row read (16 bytes of one row), and a transposing read (8 + 8 bytes, rows 8 apart).
+__device__ __forceinline__ bf16x8 row_operand(uint32_t at)
+{
+    return *(const bf16x8 __attribute__((address_space(3)))*)(lds_bytes_t)(uintptr_t)at;
+}
+template <int D>
+__device__ __forceinline__ bf16x8 transposed_operand(uint32_t at)
+{
+    const i16x4 lo4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((i16x4 __attribute__((address_space(3)))*)(uintptr_t)at);
+    const i16x4 hi4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((i16x4 __attribute__((address_space(3)))*)(uintptr_t)(at + RowTile<D>::R8));
+    const bf16x4 lo = __builtin_bit_cast(bf16x4, lo4), hi = __builtin_bit_cast(bf16x4, hi4);
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+// Where in a tile a lane's operands start: row reads of rows 0 .. 31, chunk lane / 32 (+ 2 per step); transposing reads of rows
+// 4 (lane / 32) + r16 / 4 (+ 8, + 16 per step), 8 bytes at column 16 grp2 + 4 (r16 % 4) (+ 32 per step).
+template <int D>
+__device__ __forceinline__ uint32_t row_lane(int lane) { return RowTile<D>::offset(lane & 31) + 16 * (lane >> 5); }
+template <int D>
+__device__ __forceinline__ uint32_t transposed_lane(int lane)
+{
+    const int half = lane >> 5, r16 = lane & 15, grp2 = (lane >> 4) & 1;
+    return RowTile<D>::offset(4 * half + (r16 >> 2)) + (16 * grp2 + 4 * (r16 & 3)) * 2;
+}
+
 // Compile-time loop: f(integral_constant<int, I>) for I = 0 .. N-1.
 template <int I, int N, typename F>
 __device__ __forceinline__ void static_for(F&& f)
