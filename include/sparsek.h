@@ -261,6 +261,102 @@ int sparsek_chunk_to_decode(const sparsek_chunk_cfg *cfg, void *state, size_t st
 int sparsek_chunk_status(const sparsek_chunk_cfg *cfg, const void *state, int32_t *host_counts,
                          int32_t *host_flags, void *stream);
 
+/* ---- attention over blocks of tokens that a cheap score selects for each query ----
+ * For models without a trained scorer: what is selected are blocks of SPARSEK_BLOCK_TOKENS = 64 consecutive keys, by the keys
+ * themselves.  Block j = positions 64 j .. 64 j + 63.  Query i attends its own block up to itself, and the blocks that idx names for it,
+ * all of them behind its own.  Query head h belongs to key/value head h / (H / Hkv); the heads of such a group share a selection.
+ *
+ * sparsek_block_select fills idx [B,Hkv,n,top] int32: for every query the (up to) `top` blocks behind its own with the largest scores, in
+ * ascending order, padded with -1; of equal scores the older block wins.
+ *     mean_j  = mean of the block's keys (summed in fp64, rounded to fp32)
+ *     m8_j    = rint(mean_j * (127 / max|mean_j|)), ms_j = max|mean_j| / 127         (0 where the maximum is below 2^-100)
+ *     p8_i    = the same rounding of the sum of the group's queries at position i
+ *     score   = float(p8_i . m8_j) * ms_j                                            (the product is exact)
+ * A selection from anywhere else will do for the attention too: entries that are no block behind the query's own (-1 among them) and
+ * repeated ones are left out.
+ *
+ * q, o, dO, dq in/out [B,H,n,d], k, v, dk, dv [B,Hkv,n,d] of `dtype`, lse [B,H,n] fp32 (natural logarithm), all contiguous.
+ * mass out [B,Hkv,ceil(n/64)] fp32, may be NULL: the attention weight that each block's keys got from all queries and heads of the group,
+ * added up (what sparsek_cache8_evict goes by).
+ * The backward takes the forward's o and lse and gives the gradients of L = sum(dO * o) with the selection held fixed.
+ * SPARSEK_BF16, d = 64 or 128, Hkv dividing H, n <= 2^20, top <= 64 (UNSUPPORTED otherwise); idx may be NULL where top == 0.
+ * Results do not depend on timing: no sum's order is left to atomics. */
+#define SPARSEK_BLOCK_TOKENS 64
+typedef struct {
+    int32_t B, H, Hkv, n, d;
+    int32_t top;           /* selected blocks per query, 0 .. 64 */
+    int32_t dtype;         /* SPARSEK_BF16 */
+    float softmax_scale;   /* finite and > 0 */
+} sparsek_block_cfg;
+size_t sparsek_block_select_workspace_bytes(const sparsek_block_cfg *cfg);
+int sparsek_block_select(const sparsek_block_cfg *cfg, const void *q, const void *k, int32_t *idx, void *ws, size_t ws_bytes,
+                         void *stream);
+size_t sparsek_block_attn_fwd_workspace_bytes(const sparsek_block_cfg *cfg);
+int sparsek_block_attn_fwd(const sparsek_block_cfg *cfg, const void *q, const void *k, const void *v, const int32_t *idx, void *o,
+                           float *lse, float *mass, void *ws, size_t ws_bytes, void *stream);
+size_t sparsek_block_attn_bwd_workspace_bytes(const sparsek_block_cfg *cfg);
+int sparsek_block_attn_bwd(const sparsek_block_cfg *cfg, const void *q, const void *k, const void *v, const int32_t *idx,
+                           const void *o, const float *lse, const void *dO, void *dq, void *dk, void *dv, void *ws, size_t ws_bytes,
+                           void *stream);
+
+/* ---- a key/value cache in blocks of 64 tokens held in 8 bits, its attention, and eviction by accumulated weight ----
+ * The cache is tensors of the caller's.  A page holds one block of one key/value head; the pool has `pages` of them, which any
+ * sequence and head may name (two may name the same one, as for a common prefix).
+ *     k8 [pages,64,d], v8 [pages,d,64] (transposed)   codes: SPARSEK_I8 int8, rint(x * (127 / max)); SPARSEK_E4M3 OCP e4m3, x * (448 / max)
+ *     ks, vs [pages] fp32                             what a code of 1 stands for: max / 127 or max / 448, max = the block's largest |x|;
+ *                                                     a block with max < 2^-100 is held as zeros with scale 0
+ *     km [pages,d] int8, kms [pages] fp32             the block's mean key, as m8 and ms of sparsek_block_select
+ *     kt [B,Hkv,64,d], vt [B,Hkv,d,64] of `dtype`     the tokens of the last, unfinished block
+ *     table [B,Hkv,cap] int32                         a head's pages, oldest first; behind its blocks the pages for the next ones
+ *     mass [B,Hkv,cap] fp32                           accumulated attention weight of the block at each place of the table (of the
+ *                                                     unfinished one at the next place); zero it for a new sequence
+ *     lens [B] int32                                  tokens in the cache: lens / 64 whole blocks and lens % 64 unfinished tokens; at
+ *                                                     most 64 cap + 63, larger values count as that, negative ones as 0
+ * lens is an argument of every call and only sparsek_cache8_evict gives new ones: after an append the caller adds what it appended.
+ * Pages outside 0 .. pages-1 are never touched: what would go there is dropped, and such a block is attended by nobody.
+ *
+ * append: the first counts[b] (NULL: all) of c new tokens k, v [B,Hkv,c,d] of every sequence join the lens[b] that are there.  Blocks
+ *     that become whole are rounded from the original values and leave the unfinished block's tensors as they are; rows behind a
+ *     sequence's last token are not written.  Tokens beyond 64 cap + 63 are dropped.  Pages that blocks become whole in must not be shared.
+ * select: idx [B,Hkv,top] out, for the query q [B,H,d] at position lens - 1: the (up to) `top` whole blocks behind the query's own
+ *     (the one that token lens - 1 lies in) with the largest scores, as sparsek_block_select.
+ * attn:  o out [B,H,d], lse out [B,H] fp32: the query attends all tokens (idx NULL), or its own block and the whole blocks of idx
+ *     [B,Hkv,top] (places in the table; places of no whole block behind its own, and repeated ones, are left out).  A sequence without
+ *     tokens gets o = 0 and lse = -inf.  accumulate != 0: the weights are added to mass.
+ * evict: sequences with more than `budget` whole blocks keep the first `sink`, the last `recent` and of the others those with the largest
+ *     mass (of equal ones the older), `budget` in all, by age.  table_out and mass_out [B,Hkv,cap], lens_out [B] out: the kept pages
+ *     first, then those that went (free for new blocks), then the rest; masses move along, the unfinished block's with it, what lies
+ *     behind becomes 0.  The outputs must not overlap the inputs (INVALID_ARG).
+ * SPARSEK_BF16, d = 64 or 128, Hkv dividing H, cap <= 8192, pages <= 2^24 (UNSUPPORTED otherwise). */
+#define SPARSEK_I8 2
+#define SPARSEK_E4M3 3
+typedef struct {
+    int32_t B, H, Hkv, d, cap, pages;
+    int32_t format;        /* of the codes: SPARSEK_I8 or SPARSEK_E4M3 */
+    int32_t dtype;         /* of q, k, v, o and the unfinished blocks: SPARSEK_BF16 */
+    float softmax_scale;   /* finite and > 0 */
+} sparsek_cache8_cfg;
+typedef struct {
+    void *k8, *v8;
+    float *ks, *vs;
+    int8_t *km;
+    float *kms;
+    void *kt, *vt;
+    int32_t *table;
+    float *mass;
+} sparsek_cache8;
+int sparsek_cache8_append(const sparsek_cache8_cfg *cfg, const sparsek_cache8 *cache, const int32_t *lens, const int32_t *counts,
+                          int32_t c, const void *k, const void *v, void *stream);
+int sparsek_cache8_select(const sparsek_cache8_cfg *cfg, const sparsek_cache8 *cache, const int32_t *lens, const void *q, int32_t top,
+                          int32_t *idx, void *stream);
+/* top: of idx; 0 with idx NULL */
+size_t sparsek_cache8_attn_workspace_bytes(const sparsek_cache8_cfg *cfg, int32_t top);
+int sparsek_cache8_attn(const sparsek_cache8_cfg *cfg, const sparsek_cache8 *cache, const int32_t *lens, const void *q,
+                        const int32_t *idx, int32_t top, int32_t accumulate, void *o, float *lse, void *ws, size_t ws_bytes,
+                        void *stream);
+int sparsek_cache8_evict(const sparsek_cache8_cfg *cfg, const sparsek_cache8 *cache, const int32_t *lens, int32_t budget,
+                         int32_t sink, int32_t recent, int32_t *table_out, float *mass_out, int32_t *lens_out, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -2,6 +2,8 @@
 #include "common.hpp"
 #include "mask_ranges.hpp"
 
+#include <initializer_list>
+
 using namespace spk;
 
 namespace {
@@ -409,3 +411,188 @@ int sparsek_chunk_status(const sparsek_chunk_cfg* cfg, const void* state, int32_
 
 }  // extern "C"
 
+// ---- attention over blocks of tokens (block_select.hip, block_attn.hip, block_attn_bwd.hip) and the cache in 8 bits (cache8.hip) ----
+namespace spk {
+size_t block_select_ws_bytes(const sparsek_block_cfg& c);
+int launch_block_select(const sparsek_block_cfg& c, const void* q, const void* k, int32_t* idx, void* ws, hipStream_t st);
+size_t block_fwd_ws_bytes(const sparsek_block_cfg& c);
+int launch_block_fwd(const sparsek_block_cfg& c, const void* q, const void* k, const void* v, const int32_t* idx, void* o, float* lse,
+                     float* mass, void* ws, hipStream_t st);
+size_t block_bwd_ws_bytes(const sparsek_block_cfg& c);
+int launch_block_bwd(const sparsek_block_cfg& c, const void* q, const void* k, const void* v, const int32_t* idx, const void* o,
+                     const float* lse, const void* dO, void* dq, void* dk, void* dv, void* ws, hipStream_t st);
+int launch_cache8_append(const sparsek_cache8_cfg& c, const sparsek_cache8& t, const int32_t* lens, const int32_t* counts, int count,
+                         const void* k, const void* v, hipStream_t st);
+int launch_cache8_select(const sparsek_cache8_cfg& c, const sparsek_cache8& t, const int32_t* lens, const void* q, int top, int32_t* idx,
+                         hipStream_t st);
+size_t cache8_attn_ws_bytes(const sparsek_cache8_cfg& c, int top);
+int launch_cache8_attn(const sparsek_cache8_cfg& c, const sparsek_cache8& t, const int32_t* lens, const void* q, const int32_t* idx,
+                       int top, int accumulate, void* o, float* lse, void* ws, hipStream_t st);
+int launch_cache8_evict(const sparsek_cache8_cfg& c, const sparsek_cache8& t, const int32_t* lens, int budget, int sink, int recent,
+                        int32_t* table, float* mass, int32_t* lens_out, hipStream_t st);
+}  // namespace spk
+
+namespace {
+
+constexpr int MAX_BLOCK_TOP = 64, MAX_CACHE_BLOCKS = 8192;
+
+int check_heads(int B, int H, int Hkv, int d, int dtype, float scale)
+{
+    if (B < 1 || H < 1 || Hkv < 1 || H % Hkv != 0) return SPARSEK_ERR_INVALID_ARG;
+    if (!(scale > 0.0f) || !(scale < INFINITY)) return SPARSEK_ERR_INVALID_ARG;
+    if (dtype != SPARSEK_BF16 || (d != 64 && d != 128)) return SPARSEK_ERR_UNSUPPORTED;
+    if ((long long)B * H > 65535) return SPARSEK_ERR_UNSUPPORTED;
+    return SPARSEK_OK;
+}
+
+int check_block(const sparsek_block_cfg* c)
+{
+    if (!c || c->n < 1 || c->top < 0) return SPARSEK_ERR_INVALID_ARG;
+    int rc = check_heads(c->B, c->H, c->Hkv, c->d, c->dtype, c->softmax_scale);
+    if (rc) return rc;
+    if (c->n > (1 << 20) || c->top > MAX_BLOCK_TOP) return SPARSEK_ERR_UNSUPPORTED;
+    if ((long long)c->n * (c->H / c->Hkv) > (1 << 28)) return SPARSEK_ERR_UNSUPPORTED;   // rows of one block's list
+    return SPARSEK_OK;
+}
+
+int check_cache8(const sparsek_cache8_cfg* c, const sparsek_cache8* t)
+{
+    if (!c || c->cap < 1 || c->pages < 1) return SPARSEK_ERR_INVALID_ARG;
+    int rc = check_heads(c->B, c->H, c->Hkv, c->d, c->dtype, c->softmax_scale);
+    if (rc) return rc;
+    if (c->format != SPARSEK_I8 && c->format != SPARSEK_E4M3) return SPARSEK_ERR_UNSUPPORTED;
+    if (c->cap > MAX_CACHE_BLOCKS || c->pages > (1 << 24)) return SPARSEK_ERR_UNSUPPORTED;
+    if (t && (!t->k8 || !t->v8 || !t->ks || !t->vs || !t->km || !t->kms || !t->kt || !t->vt || !t->table || !t->mass)) return SPARSEK_ERR_INVALID_ARG;
+    return SPARSEK_OK;
+}
+
+// What is read or written 16 bytes at a time.
+bool aligned(std::initializer_list<const void*> ps)
+{
+    for (const void* p : ps)
+        if ((uintptr_t)p & 15) return false;
+    return true;
+}
+bool aligned(const sparsek_cache8& t) { return aligned({t.k8, t.v8, t.km, t.kt, t.vt}); }
+
+bool overlap(const void* a, size_t na, const void* b, size_t nb)
+{
+    return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t sparsek_block_select_workspace_bytes(const sparsek_block_cfg* cfg)
+{
+    if (check_block(cfg)) return 0;
+    return spk::block_select_ws_bytes(*cfg);
+}
+
+int sparsek_block_select(const sparsek_block_cfg* cfg, const void* q, const void* k, int32_t* idx, void* ws, size_t ws_bytes, void* stream)
+{
+    int rc = check_block(cfg);
+    if (rc) return rc;
+    if (!q || !k || (!idx && cfg->top) || !ws || !aligned({q, k, ws})) return SPARSEK_ERR_INVALID_ARG;
+    if (ws_bytes < spk::block_select_ws_bytes(*cfg)) return SPARSEK_ERR_WORKSPACE;
+    return spk::launch_block_select(*cfg, q, k, idx, ws, (hipStream_t)stream);
+}
+
+size_t sparsek_block_attn_fwd_workspace_bytes(const sparsek_block_cfg* cfg)
+{
+    if (check_block(cfg)) return 0;
+    return spk::block_fwd_ws_bytes(*cfg);
+}
+
+int sparsek_block_attn_fwd(const sparsek_block_cfg* cfg, const void* q, const void* k, const void* v, const int32_t* idx, void* o,
+                           float* lse, float* mass, void* ws, size_t ws_bytes, void* stream)
+{
+    int rc = check_block(cfg);
+    if (rc) return rc;
+    if (!q || !k || !v || (!idx && cfg->top) || !o || !lse || !ws || !aligned({q, k, v, o, ws})) return SPARSEK_ERR_INVALID_ARG;
+    if (ws_bytes < spk::block_fwd_ws_bytes(*cfg)) return SPARSEK_ERR_WORKSPACE;
+    return spk::launch_block_fwd(*cfg, q, k, v, idx, o, lse, mass, ws, (hipStream_t)stream);
+}
+
+size_t sparsek_block_attn_bwd_workspace_bytes(const sparsek_block_cfg* cfg)
+{
+    if (check_block(cfg)) return 0;
+    return spk::block_bwd_ws_bytes(*cfg);
+}
+
+int sparsek_block_attn_bwd(const sparsek_block_cfg* cfg, const void* q, const void* k, const void* v, const int32_t* idx,
+                           const void* o, const float* lse, const void* dO, void* dq, void* dk, void* dv, void* ws, size_t ws_bytes,
+                           void* stream)
+{
+    int rc = check_block(cfg);
+    if (rc) return rc;
+    if (!q || !k || !v || (!idx && cfg->top) || !o || !lse || !dO || !dq || !dk || !dv || !ws) return SPARSEK_ERR_INVALID_ARG;
+    if (!aligned({q, k, v, o, dO, dq, dk, dv, ws})) return SPARSEK_ERR_INVALID_ARG;
+    if (ws_bytes < spk::block_bwd_ws_bytes(*cfg)) return SPARSEK_ERR_WORKSPACE;
+    return spk::launch_block_bwd(*cfg, q, k, v, idx, o, lse, dO, dq, dk, dv, ws, (hipStream_t)stream);
+}
+
+int sparsek_cache8_append(const sparsek_cache8_cfg* cfg, const sparsek_cache8* cache, const int32_t* lens, const int32_t* counts,
+                          int32_t c, const void* k, const void* v, void* stream)
+{
+    if (!cache) return SPARSEK_ERR_INVALID_ARG;
+    int rc = check_cache8(cfg, cache);
+    if (rc) return rc;
+    if (!lens || !k || !v || c < 1 || !aligned(*cache) || !aligned({k, v})) return SPARSEK_ERR_INVALID_ARG;
+    if (c > (1 << 24)) return SPARSEK_ERR_UNSUPPORTED;
+    return spk::launch_cache8_append(*cfg, *cache, lens, counts, c, k, v, (hipStream_t)stream);
+}
+
+int sparsek_cache8_select(const sparsek_cache8_cfg* cfg, const sparsek_cache8* cache, const int32_t* lens, const void* q, int32_t top,
+                          int32_t* idx, void* stream)
+{
+    if (!cache) return SPARSEK_ERR_INVALID_ARG;
+    int rc = check_cache8(cfg, cache);
+    if (rc) return rc;
+    if (!lens || !q || !idx || top < 1 || !aligned(*cache) || !aligned({q})) return SPARSEK_ERR_INVALID_ARG;
+    if (top > MAX_CACHE_BLOCKS) return SPARSEK_ERR_UNSUPPORTED;
+    return spk::launch_cache8_select(*cfg, *cache, lens, q, top, idx, (hipStream_t)stream);
+}
+
+size_t sparsek_cache8_attn_workspace_bytes(const sparsek_cache8_cfg* cfg, int32_t top)
+{
+    if (check_cache8(cfg, nullptr) || top < 0 || top > MAX_CACHE_BLOCKS) return 0;
+    return spk::cache8_attn_ws_bytes(*cfg, top);
+}
+
+int sparsek_cache8_attn(const sparsek_cache8_cfg* cfg, const sparsek_cache8* cache, const int32_t* lens, const void* q,
+                        const int32_t* idx, int32_t top, int32_t accumulate, void* o, float* lse, void* ws, size_t ws_bytes,
+                        void* stream)
+{
+    if (!cache) return SPARSEK_ERR_INVALID_ARG;
+    int rc = check_cache8(cfg, cache);
+    if (rc) return rc;
+    if (!lens || !q || !o || !lse || !ws || (idx ? top < 1 : top != 0)) return SPARSEK_ERR_INVALID_ARG;
+    if (!aligned(*cache) || !aligned({q, o, ws})) return SPARSEK_ERR_INVALID_ARG;
+    if (top > MAX_CACHE_BLOCKS) return SPARSEK_ERR_UNSUPPORTED;
+    if (ws_bytes < spk::cache8_attn_ws_bytes(*cfg, top)) return SPARSEK_ERR_WORKSPACE;
+    return spk::launch_cache8_attn(*cfg, *cache, lens, q, idx, top, accumulate != 0, o, lse, ws, (hipStream_t)stream);
+}
+
+int sparsek_cache8_evict(const sparsek_cache8_cfg* cfg, const sparsek_cache8* cache, const int32_t* lens, int32_t budget, int32_t sink,
+                         int32_t recent, int32_t* table_out, float* mass_out, int32_t* lens_out, void* stream)
+{
+    if (!cache) return SPARSEK_ERR_INVALID_ARG;
+    int rc = check_cache8(cfg, cache);
+    if (rc) return rc;
+    if (!lens || !table_out || !mass_out || !lens_out) return SPARSEK_ERR_INVALID_ARG;
+    if (budget < 0 || sink < 0 || recent < 0 || (long long)sink + recent > budget) return SPARSEK_ERR_INVALID_ARG;
+    const size_t nt = (size_t)cfg->B * cfg->Hkv * cfg->cap * 4, nl = (size_t)cfg->B * 4;
+    const void* in[] = {cache->table, cache->mass, lens};
+    const size_t nin[] = {nt, nt, nl};
+    void* out[] = {table_out, mass_out, lens_out};
+    for (int x = 0; x < 3; x++)
+        for (int y = 0; y < 3; y++) {
+            if (overlap(in[x], nin[x], out[y], nin[y])) return SPARSEK_ERR_INVALID_ARG;
+            if (x < y && overlap(out[x], nin[x], out[y], nin[y])) return SPARSEK_ERR_INVALID_ARG;
+        }
+    return spk::launch_cache8_evict(*cfg, *cache, lens, budget, sink, recent, table_out, mass_out, lens_out, (hipStream_t)stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,377 @@
+// Attention over selected blocks of 64 tokens, backward: with p_ij = exp(s_ij - lse_i), delta_i = dO_i.o_i and
+// ds_ij = p_ij (dO_i.v_j - delta_i) scale:  dq_i = sum_j ds_ij k_j,  dk_j = sum_i ds_ij q_i,  dv_j = sum_i p_ij dO_i.
+//
+// By key block, like the forward (see block_attn.hip).  block_bwd_tiles_kernel holds a block's K and V in LDS and walks the
+// rows that selected it, 64 at a time: S = Q.K^T and dP = dO.V^T with a lane per key, so that P and dS are the operands of
+// dV^T += dO^T.P and dK^T += Q^T.dS as they stand (sums stay in registers for a whole unit of rows, then go out once); dS
+// passes through LDS for dQ^T = K^T.dS^T, whose partial results go out in list order.  block_bwd_join_kernel does the
+// queries' own block in the same way, and adds the partial results of dq, dk and dv to it.
+#include "block_parts.hpp"
+
+namespace spk {
+
+struct BlockBwd {
+    BlockArgs a;
+    uint16_t *dq, *dk, *dv;
+    float2* rows;       // [B,H,n]: lse * log2(e), dO.o
+    _Float16* part;     // partial dq: [entry rows][half of D][lane / 32][D / 4]
+    float2* meta;       // what the halves of each half of D stand for
+    float* kvpart;      // [units][2 halves of the keys][dV, dK][D / 32][4][64 lanes][4]
+};
+
+// dO.o and the logarithm of the denominator, a wave per 64 / (D / 8) rows.
+template <int D>
+__global__ __launch_bounds__(256) void block_delta_kernel(BlockBwd f, size_t nrows)
+{
+    constexpr int LPR = D / 8;
+    const size_t row = (blockIdx.x * (size_t)256 + threadIdx.x) / LPR;
+    const int c = threadIdx.x % LPR;
+    float s = 0.0f;
+    if (row < nrows) {
+        const u32x4 x = *(const u32x4*)(f.a.o + row * D + 8 * c), y = *(const u32x4*)(f.a.dO + row * D + 8 * c);
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            s = fmaf(__uint_as_float(x[e] << 16), __uint_as_float(y[e] << 16), s);
+            s = fmaf(__uint_as_float(x[e] & 0xFFFF0000u), __uint_as_float(y[e] & 0xFFFF0000u), s);
+        }
+    }
+#pragma unroll
+    for (int d = 1; d < LPR; d <<= 1) s += __shfl_xor(s, d, 64);
+    if (row < nrows && c == 0) f.rows[row] = make_float2(f.a.lse[row] * 1.4426950408889634f, s);
+}
+
+template <int D>
+struct BwdBlockSmem {
+    unsigned char k[RowTile<D>::BYTES], v[RowTile<D>::BYTES], q[RowTile<D>::BYTES], g[RowTile<D>::BYTES];   // g: dO
+    unsigned char ds[RowTile<64>::BYTES];   // [key][row]
+    float lse2[BT], delta[BT];
+    long long at[BT];                       // the row's place in [B,H,n], -1: none
+};
+static_assert(sizeof(BwdBlockSmem<128>) <= 80 * 1024, "two workgroups per CU");
+
+// The rows named by sm.at go to the q and g tiles; rows that do not exist become zeros.
+template <int D>
+__device__ __forceinline__ void load_query_rows(BwdBlockSmem<D>& sm, const uint16_t* q, const uint16_t* dO, int tid)
+{
+    constexpr int CPR = D / 8;
+#pragma unroll
+    for (int t = 0; t < BT * CPR / 256; t++) {
+        const int id = tid + 256 * t, r = id / CPR, c = id % CPR;
+        const long long at = sm.at[r];
+        u32x4 x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
+        if (at >= 0) {
+            x = *(const u32x4*)(q + (size_t)at * D + 8 * c);
+            y = *(const u32x4*)(dO + (size_t)at * D + 8 * c);
+        }
+        *(u32x4*)(sm.q + RowTile<D>::offset(r) + 16 * c) = x;
+        *(u32x4*)(sm.g + RowTile<D>::offset(r) + 16 * c) = y;
+    }
+}
+
+// 64 rows against 64 keys.  Wave (kb = wv & 1, rb = wv >> 1): keys 32 kb .. and rows 32 rb .. of S and dP; its share of dV^T and
+// dK^T (those keys, those rows) joins acc_v, acc_k; then dQ^T of rows 32 rb .. and the D/2 columns of half kb, into acc_q.
+template <int D, bool CAUSAL>
+__device__ __forceinline__ void bwd_block_tile(BwdBlockSmem<D>& sm, int lane, int wv, float c2, float scale, f32x16 (&acc_v)[D / 32],
+                                               f32x16 (&acc_k)[D / 32], f32x16 (&acc_q)[D / 64])
+{
+    using S = RowTile<D>;
+    constexpr int DS = D / 16, DB = D / 32;
+    const int kb = wv & 1, rb = wv >> 1, col = lane & 31, half = lane >> 5;
+    const uint32_t rk = lds_address(sm.k) + row_lane<D>(lane) + 2 * kb * S::R16, rv = lds_address(sm.v) + row_lane<D>(lane) + 2 * kb * S::R16;
+    const uint32_t rq = lds_address(sm.q) + row_lane<D>(lane) + 2 * rb * S::R16, rg = lds_address(sm.g) + row_lane<D>(lane) + 2 * rb * S::R16;
+    f32x16 s = {0}, dp = {0};
+#pragma unroll
+    for (int x = 0; x < DS; x++) {
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_operand(rq + 32 * x), row_operand(rk + 32 * x), s, 0, 0, 0);
+        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_operand(rg + 32 * x), row_operand(rv + 32 * x), dp, 0, 0, 0);
+    }
+    bf16x8 pb[2], db[2];   // as operands: 2^-9 of every weight and every score gradient
+#pragma unroll
+    for (int g4 = 0; g4 < 4; g4++) {
+        const int r0 = 32 * rb + 8 * g4 + 4 * half;
+        const float4 L4 = *(const float4*)&sm.lse2[r0], D4 = *(const float4*)&sm.delta[r0];
+        const float ll[4] = {L4.x, L4.y, L4.z, L4.w}, dd[4] = {D4.x, D4.y, D4.z, D4.w};
+        float ds[4];
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const int r = 4 * g4 + e;
+            float p = __builtin_amdgcn_exp2f(fmaf(s[r], c2, -ll[e]));
+            if (CAUSAL && 32 * kb + col > r0 + e) p = 0.0f;
+            ds[e] = p * (dp[r] - dd[e]);
+            if (CAUSAL && 32 * kb + col > r0 + e) ds[e] = 0.0f;
+            pb[r >> 3][r & 7] = (__bf16)p;
+            db[r >> 3][r & 7] = (__bf16)ds[e];
+        }
+        *(uint2*)(sm.ds + RowTile<64>::offset(32 * kb + col) + 2 * r0) = make_uint2(pack_bf16x2(ds[0], ds[1]), pack_bf16x2(ds[2], ds[3]));
+    }
+    const uint32_t tq = lds_address(sm.q) + transposed_lane<D>(lane) + 2 * rb * S::R16, tg = lds_address(sm.g) + transposed_lane<D>(lane) + 2 * rb * S::R16;
+#pragma unroll
+    for (int g = 0; g < 2; g++)
+#pragma unroll
+        for (int x = 0; x < DB; x++) {
+            acc_v[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_operand<D>(tg + g * S::R16 + 64 * x), pb[g], acc_v[x], 0, 0, 0);
+            acc_k[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_operand<D>(tq + g * S::R16 + 64 * x), db[g], acc_k[x], 0, 0, 0);
+        }
+    __syncthreads();   // dS is there
+    const uint32_t tk = lds_address(sm.k) + transposed_lane<D>(lane) + 64 * (DB / 2) * kb, td = lds_address(sm.ds) + transposed_lane<64>(lane) + 64 * rb;
+#pragma unroll
+    for (int x = 0; x < DB / 2; x++) acc_q[x] = f32x16{0};
+#pragma unroll
+    for (int g = 0; g < 4; g++) {
+        const bf16x8 d8 = transposed_operand<64>(td + g * RowTile<64>::R16);
+#pragma unroll
+        for (int x = 0; x < DB / 2; x++)
+            acc_q[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_operand<D>(tk + g * S::R16 + 64 * x), d8, acc_q[x], 0, 0, 0);
+    }
+#pragma unroll
+    for (int x = 0; x < DB / 2; x++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) acc_q[x][r] *= scale;
+}
+
+// The two row halves' shares of dV^T and dK^T are added up in LDS (over the q, g tiles and what follows); waves 0 and 1 have the sums.
+template <int D>
+__device__ __forceinline__ void add_row_halves(BwdBlockSmem<D>& sm, int lane, int wv, f32x16 (&acc_v)[D / 32], f32x16 (&acc_k)[D / 32])
+{
+    float4* buf = (float4*)&sm + (wv & 1) * (2 * (D / 32) * 4 * 64);
+    __syncthreads();
+    if (wv >= 2) {
+#pragma unroll
+        for (int x = 0; x < D / 32; x++)
+#pragma unroll
+            for (int y = 0; y < 4; y++) {
+                buf[(x * 4 + y) * 64 + lane] = make_float4(acc_v[x][4 * y], acc_v[x][4 * y + 1], acc_v[x][4 * y + 2], acc_v[x][4 * y + 3]);
+                buf[((D / 32 + x) * 4 + y) * 64 + lane] = make_float4(acc_k[x][4 * y], acc_k[x][4 * y + 1], acc_k[x][4 * y + 2], acc_k[x][4 * y + 3]);
+            }
+    }
+    __syncthreads();
+    if (wv < 2) {
+#pragma unroll
+        for (int x = 0; x < D / 32; x++)
+#pragma unroll
+            for (int y = 0; y < 4; y++) {
+                const float4 a = buf[(x * 4 + y) * 64 + lane], b = buf[((D / 32 + x) * 4 + y) * 64 + lane];
+                acc_v[x][4 * y] += a.x; acc_v[x][4 * y + 1] += a.y; acc_v[x][4 * y + 2] += a.z; acc_v[x][4 * y + 3] += a.w;
+                acc_k[x][4 * y] += b.x; acc_k[x][4 * y + 1] += b.y; acc_k[x][4 * y + 2] += b.z; acc_k[x][4 * y + 3] += b.w;
+            }
+    }
+}
+static_assert(2 * 2 * 4 * 4 * 64 * 16 <= sizeof(BwdBlockSmem<128>) && 2 * 2 * 2 * 4 * 64 * 16 <= sizeof(BwdBlockSmem<64>), "room for the sums");
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void block_bwd_tiles_kernel(BlockBwd f)
+{
+    __shared__ __attribute__((aligned(16))) BwdBlockSmem<D> sm;
+    constexpr int DB = D / 32;
+    const BlockLists& l = f.a.l;
+    const int bg = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, col = lane & 31, half = lane >> 5;
+    if ((int)blockIdx.x >= l.nunits[bg]) return;
+    const size_t un = (size_t)bg * l.maxu + blockIdx.x;
+    const int2 u = l.units[un];
+    const int j = u.x, first = u.y, G = l.G, b = bg / l.Hkv, g = bg % l.Hkv;
+    const int base = l.base[(size_t)bg * l.nb + j];
+    const int end = min(l.total[(size_t)bg * l.nb + j] * G, first + l.unit);
+    const size_t kv = ((size_t)bg * l.n + (size_t)j * BT) * D;
+    load_rows<D>(sm.k, f.a.k + kv, BT - 1, tid);
+    load_rows<D>(sm.v, f.a.v + kv, BT - 1, tid);
+    const int32_t* list = l.list + (size_t)bg * l.pairs + base;
+    const size_t row0 = ((size_t)bg * l.pairs + base) * G;
+    f32x16 acc_v[DB], acc_k[DB], acc_q[DB / 2];
+#pragma unroll
+    for (int x = 0; x < DB; x++) acc_v[x] = acc_k[x] = f32x16{0};
+    for (int r0 = first; r0 < end; r0 += BT) {
+        __syncthreads();   // everybody is done with the rows before
+        if (tid < BT) {
+            const int r = r0 + tid;
+            long long at = -1;
+            float2 m = make_float2(INFINITY, 0.0f);   // p = 0
+            if (r < end) {
+                at = ((long long)b * l.H + g * G + r % G) * l.n + list[r / G];
+                m = f.rows[at];
+            }
+            sm.at[tid] = at;
+            sm.lse2[tid] = m.x;
+            sm.delta[tid] = m.y;
+        }
+        __syncthreads();
+        load_query_rows<D>(sm, f.a.q, f.a.dO, tid);
+        __syncthreads();
+        bwd_block_tile<D, false>(sm, lane, wv, f.a.c2, f.a.scale, acc_v, acc_k, acc_q);
+        // the partial dq of rows 32 rb + col, columns of half kb
+        const int kb = wv & 1, r = r0 + 32 * (wv >> 1) + col;
+        float top = 0.0f;
+#pragma unroll
+        for (int x = 0; x < DB / 2; x++)
+#pragma unroll
+            for (int e = 0; e < 16; e++) top = fmaxf(top, fabsf(acc_q[x][e]));
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+        const int E = scale_exp(max((unsigned)sw[0], (unsigned)sw[1]));
+        const float down = __uint_as_float((unsigned)(254 - E) << 23), up = __uint_as_float((unsigned)E << 23);
+        if (r < end) {
+            _Float16* pr = f.part + (row0 + r) * D + kb * (D / 2) + half * (D / 4);
+#pragma unroll
+            for (int x = 0; x < DB / 2; x++)
+#pragma unroll
+                for (int y = 0; y < 2; y++) {
+                    f16x8 v;
+#pragma unroll
+                    for (int e = 0; e < 8; e++) v[e] = (_Float16)(acc_q[x][8 * y + e] * down);
+                    *(f16x8*)(pr + 16 * x + 8 * y) = v;
+                }
+            if (half == 0) ((float*)(f.meta + row0 + r))[kb] = up;
+        }
+    }
+    add_row_halves<D>(sm, lane, wv, acc_v, acc_k);
+    if (wv < 2) {
+        float4* out = (float4*)f.kvpart + (un * 2 + wv) * (2 * DB * 4 * 64);
+#pragma unroll
+        for (int x = 0; x < DB; x++)
+#pragma unroll
+            for (int y = 0; y < 4; y++) {
+                out[(x * 4 + y) * 64 + lane] = make_float4(acc_v[x][4 * y], acc_v[x][4 * y + 1], acc_v[x][4 * y + 2], acc_v[x][4 * y + 3]);
+                out[((DB + x) * 4 + y) * 64 + lane] = make_float4(acc_k[x][4 * y], acc_k[x][4 * y + 1], acc_k[x][4 * y + 2], acc_k[x][4 * y + 3]);
+            }
+    }
+}
+
+// The own block of 64 queries, every head of the group in turn, and the sums with the partial results.
+template <int D>
+__global__ __launch_bounds__(256, 2) void block_bwd_join_kernel(BlockBwd f)
+{
+    __shared__ __attribute__((aligned(16))) BwdBlockSmem<D> sm;
+    constexpr int DB = D / 32;
+    const BlockLists& l = f.a.l;
+    const int bg = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, col = lane & 31, half = lane >> 5;
+    const int qb = blockIdx.x, G = l.G, b = bg / l.Hkv, g = bg % l.Hkv, kb = wv & 1;
+    const size_t kv = ((size_t)bg * l.n + (size_t)qb * BT) * D;
+    const int last = l.n - 1 - qb * BT;
+    load_rows<D>(sm.k, f.a.k + kv, last, tid);
+    load_rows<D>(sm.v, f.a.v + kv, last, tid);
+    const int i = qb * BT + 32 * (wv >> 1) + col;
+    const int32_t* pos = l.pos + ((size_t)bg * l.n + min(i, l.n - 1)) * l.top;
+    f32x16 acc_v[DB], acc_k[DB], acc_q[DB / 2];
+#pragma unroll
+    for (int x = 0; x < DB; x++) acc_v[x] = acc_k[x] = f32x16{0};
+    for (int gh = 0; gh < G; gh++) {
+        const long long head = ((long long)b * l.H + g * G + gh) * l.n;
+        __syncthreads();
+        if (tid < BT) {
+            const int y = qb * BT + tid;
+            float2 m = make_float2(INFINITY, 0.0f);
+            if (y < l.n) m = f.rows[head + y];
+            sm.at[tid] = y < l.n ? head + y : -1;
+            sm.lse2[tid] = m.x;
+            sm.delta[tid] = m.y;
+        }
+        __syncthreads();
+        load_query_rows<D>(sm, f.a.q, f.a.dO, tid);
+        __syncthreads();
+        bwd_block_tile<D, true>(sm, lane, wv, f.a.c2, f.a.scale, acc_v, acc_k, acc_q);
+        if (i < l.n) {
+            for (int s = 0; s < l.top; s++) {
+                const int p = pos[s];
+                if (p < 0) continue;
+                const size_t pr = (size_t)bg * l.pairs * G + (size_t)p * G + gh;
+                const float up = ((const float*)(f.meta + pr))[kb];
+                const _Float16* src = f.part + pr * D + kb * (D / 2) + half * (D / 4);
+#pragma unroll
+                for (int x = 0; x < DB / 2; x++)
+#pragma unroll
+                    for (int y = 0; y < 2; y++) {
+                        const f16x8 v = *(const f16x8*)(src + 16 * x + 8 * y);
+#pragma unroll
+                        for (int e = 0; e < 8; e++) acc_q[x][8 * y + e] = fmaf(up, (float)v[e], acc_q[x][8 * y + e]);
+                    }
+            }
+            uint16_t* out = f.dq + (head + i) * D + kb * (D / 2) + 4 * half;
+#pragma unroll
+            for (int x = 0; x < DB / 2; x++)
+#pragma unroll
+                for (int y = 0; y < 4; y++)
+                    *(uint2*)(out + 32 * x + 8 * y) = make_uint2(pack_bf16x2(acc_q[x][4 * y], acc_q[x][4 * y + 1]), pack_bf16x2(acc_q[x][4 * y + 2], acc_q[x][4 * y + 3]));
+        }
+    }
+    add_row_halves<D>(sm, lane, wv, acc_v, acc_k);
+    if (wv < 2) {
+        // the block's units follow one another
+        const int rows = l.pairs ? l.total[(size_t)bg * l.nb + qb] * G : 0;
+        const int units = (int)(((long long)rows + l.unit - 1) / l.unit);
+        const int u0 = units ? l.first_unit[(size_t)bg * l.nb + qb] : 0;
+        for (int u = 0; u < units; u++) {
+            const float4* in = (const float4*)f.kvpart + (((size_t)bg * l.maxu + u0 + u) * 2 + wv) * (2 * DB * 4 * 64);
+#pragma unroll
+            for (int x = 0; x < DB; x++)
+#pragma unroll
+                for (int y = 0; y < 4; y++) {
+                    const float4 v = in[(x * 4 + y) * 64 + lane], w = in[((DB + x) * 4 + y) * 64 + lane];
+                    acc_v[x][4 * y] += v.x; acc_v[x][4 * y + 1] += v.y; acc_v[x][4 * y + 2] += v.z; acc_v[x][4 * y + 3] += v.w;
+                    acc_k[x][4 * y] += w.x; acc_k[x][4 * y + 1] += w.y; acc_k[x][4 * y + 2] += w.z; acc_k[x][4 * y + 3] += w.w;
+                }
+        }
+        const int key = 32 * wv + col;
+        if (key <= last) {
+            uint16_t *ok = f.dk + kv + (size_t)key * D + 4 * half, *ov = f.dv + kv + (size_t)key * D + 4 * half;
+            const float c = f.a.scale;
+#pragma unroll
+            for (int x = 0; x < DB; x++)
+#pragma unroll
+                for (int y = 0; y < 4; y++) {
+                    *(uint2*)(ov + 32 * x + 8 * y) = make_uint2(pack_bf16x2(acc_v[x][4 * y], acc_v[x][4 * y + 1]), pack_bf16x2(acc_v[x][4 * y + 2], acc_v[x][4 * y + 3]));
+                    *(uint2*)(ok + 32 * x + 8 * y) = make_uint2(pack_bf16x2(acc_k[x][4 * y] * c, acc_k[x][4 * y + 1] * c), pack_bf16x2(acc_k[x][4 * y + 2] * c, acc_k[x][4 * y + 3] * c));
+                }
+        }
+    }
+}
+
+constexpr int BWD_UNIT = 512;   // rows whose dK and dV are summed in registers
+
+struct BwdLayout {
+    BlockLayout y;
+    size_t rows, part, meta, kvpart, bytes;
+};
+static BwdLayout bwd_layout(const sparsek_block_cfg& c, void* ws)
+{
+    BwdLayout f;
+    f.y = block_lists_layout(c, BWD_UNIT, ws);
+    const size_t BG = (size_t)c.B * c.Hkv, rows = BG * f.y.l.pairs * f.y.l.G;
+    f.rows = f.y.bytes;
+    f.part = align_up(f.rows + (size_t)c.B * c.H * c.n * 8, 256);
+    f.meta = align_up(f.part + rows * c.d * 2, 256);
+    f.kvpart = align_up(f.meta + rows * 8, 256);
+    f.bytes = align_up(f.kvpart + BG * f.y.l.maxu * (size_t)BT * c.d * 8, 256);
+    return f;
+}
+
+size_t block_bwd_ws_bytes(const sparsek_block_cfg& c) { return bwd_layout(c, nullptr).bytes; }
+
+int launch_block_bwd(const sparsek_block_cfg& c, const void* q, const void* k, const void* v, const int32_t* idx, const void* o,
+                     const float* lse, const void* dO, void* dq, void* dk, void* dv, void* ws, hipStream_t st)
+{
+    const BwdLayout y = bwd_layout(c, ws);
+    BlockBwd f;
+    f.a.l = y.y.l;
+    f.a.q = (const uint16_t*)q; f.a.k = (const uint16_t*)k; f.a.v = (const uint16_t*)v;
+    f.a.o = (const uint16_t*)o; f.a.dO = (const uint16_t*)dO; f.a.lse = lse;
+    f.a.scale = c.softmax_scale;
+    f.a.c2 = c.softmax_scale * 1.4426950408889634f;
+    f.dq = (uint16_t*)dq; f.dk = (uint16_t*)dk; f.dv = (uint16_t*)dv;
+    f.rows = (float2*)((char*)ws + y.rows);
+    f.part = (_Float16*)((char*)ws + y.part); f.meta = (float2*)((char*)ws + y.meta); f.kvpart = (float*)((char*)ws + y.kvpart);
+    const BlockLists& l = f.a.l;
+    const int BG = c.B * c.Hkv;
+    if (int rc = launch_block_lists(l, idx, st)) return rc;
+    const size_t nrows = (size_t)c.B * c.H * c.n;
+#define BWD(D)                                                                                                                                   \
+    hipLaunchKernelGGL((block_delta_kernel<D>), dim3((unsigned)((nrows * (D / 8) + 255) / 256)), dim3(256), 0, st, f, nrows);                     \
+    if (l.maxu) hipLaunchKernelGGL((block_bwd_tiles_kernel<D>), dim3(l.maxu, BG), dim3(256), 0, st, f);                                          \
+    hipLaunchKernelGGL((block_bwd_join_kernel<D>), dim3(l.nb, BG), dim3(256), 0, st, f)
+    if (c.d == 128) {
+        BWD(128);
+    } else {
+        BWD(64);
+    }
+#undef BWD
+    return launch_status();
+}
+
+}  // namespace spk

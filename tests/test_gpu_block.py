@@ -1,0 +1,235 @@
+"""Attention over selected blocks of 64 tokens: selection, forward and backward against their definitions in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import block_ref as ref
+import paper_2406_16747_amd as spk
+from gpu_util import require_gpu, say
+
+pytestmark = pytest.mark.gpu
+
+# B, H, Hkv, n, d, top: lengths of one token, around a block's and a chunk's ends and beyond; groups of 1 to 25 heads
+SHAPES = [
+    (1, 1, 1, 1, 64, 2), (2, 2, 1, 63, 128, 1), (1, 2, 2, 64, 64, 4), (1, 3, 1, 65, 128, 3), (1, 2, 2, 129, 128, 1), (2, 4, 2, 300, 64, 2),
+    (1, 8, 1, 517, 128, 3), (1, 25, 1, 200, 64, 64), (1, 16, 1, 385, 128, 0), (1, 3, 3, 1000, 64, 5), (1, 4, 2, 1030, 128, 9),
+]
+
+
+def draw(seed, B, H, Hkv, n, d, qk=1.5):
+    g = torch.Generator().manual_seed(seed)
+    r = lambda *s: torch.randn(*s, generator=g)  # noqa: E731
+    q, k, v, dO = r(B, H, n, d) * qk, r(B, Hkv, n, d) + 0.7 * r(B, 1, -(-n // 64), d).repeat_interleave(64, 2)[:, :, :n], r(B, Hkv, n, d), r(B, H, n, d)
+    return [x.bfloat16().cuda() for x in (q, k, v, dO)]
+
+
+def within(got, want, bound, what):
+    err = (ref.f64(got) - want).abs()
+    bad = ~(err <= bound)
+    assert not bad.any(), "%s: %d of %d beyond their bound, worst %.3g of it (err %.3g)" % (
+        what, int(bad.sum()), bad.numel(), float((err / bound).max()), float(err.max()))
+
+
+def check_all(q, k, v, dO, idx, scale):
+    o, lse, mass = spk.sparsek_block_attn_fwd(q, k, v, idx, scale, mass=True)
+    torch.cuda.synchronize()
+    ro, rl, rm, ob, lb = ref.attn(q, k, v, idx, scale)
+    within(o, ro, ob, "o")
+    within(lse, rl, lb, "lse")
+    within(mass, rm, 2 ** -12 * rm + 1e-9, "mass")   # (a logit below 2^5 is off by 128 products of 2^-24 at most)
+    o, lse = ro.bfloat16().cuda(), rl.float().cuda()
+    got = spk.sparsek_block_attn_bwd(q, k, v, idx, o, lse, dO, scale)
+    torch.cuda.synchronize()
+    want, bound = ref.attn_bwd(q, k, v, idx, o, lse, dO, scale)
+    for name, x, y, z in zip(("dq", "dk", "dv"), got, want, bound):
+        within(x, y, z, name)
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+def test_selection_is_the_definitions(shape):
+    require_gpu()
+    B, H, Hkv, n, d, top = shape
+    say("block select", shape)
+    q, k, _, _ = draw(11, B, H, Hkv, n, d)
+    idx = spk.sparsek_block_select(q, k, top)
+    torch.cuda.synchronize()
+    assert torch.equal(idx.cpu(), ref.select(q, k, top))
+
+
+def test_selection_of_many_blocks():
+    """More blocks than a wave takes at a time, top of 1, 17 and 64; scores that differ in their last bits only."""
+    require_gpu()
+    say("block select, many blocks")
+    q, k, _, _ = draw(12, 1, 2, 1, 9000, 64)
+    k = (k * 0.001 + torch.randn(64, generator=torch.Generator().manual_seed(1)).cuda()).bfloat16()
+    for top in (1, 17, 64):
+        idx = spk.sparsek_block_select(q, k, top).cpu()
+        rows = list(range(0, 9000, 777)) + [8999]
+        want = ref.select(q, k, top) if top == 17 else None
+        if want is not None:
+            assert torch.equal(idx, want)
+        for i in rows:
+            got = [j for j in idx[0, 0, i].tolist() if j >= 0]
+            assert got == sorted(set(got)) and len(got) == min(top, i // 64) and all(j < i // 64 for j in got)
+
+
+@pytest.mark.parametrize("kind", ["equal keys", "zeros", "tiny", "huge", "one sign"])
+def test_selection_of_equal_and_extreme_scores(kind):
+    require_gpu()
+    say("block select", kind)
+    q, k, _, _ = draw(13, 1, 2, 1, 700, 64)
+    if kind == "equal keys":
+        k[:] = k[:, :, :1]
+    elif kind == "zeros":
+        q.zero_()
+    elif kind == "tiny":
+        k.mul_(2.0 ** -120)
+    elif kind == "huge":
+        k.mul_(2.0 ** 100)
+        q.mul_(2.0 ** 100)
+    else:
+        k.abs_()
+        q.copy_(-q.abs())
+    assert torch.equal(spk.sparsek_block_select(q, k, 3).cpu(), ref.select(q, k, 3))
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+def test_attention_and_gradients(shape):
+    require_gpu()
+    B, H, Hkv, n, d, top = shape
+    say("block attention", shape)
+    q, k, v, dO = draw(21, B, H, Hkv, n, d)
+    idx = spk.sparsek_block_select(q, k, top)
+    check_all(q, k, v, dO, idx, 1 / math.sqrt(d))
+
+
+@pytest.mark.parametrize("kind", ["none", "all", "one block", "repeated", "out of range", "any order"])
+@pytest.mark.parametrize("d,H,Hkv", [(64, 2, 2), (128, 6, 2)])
+def test_selections_of_the_callers_own(kind, d, H, Hkv):
+    """Rows that select nothing, everything, the same block all of them, a block twice, blocks that do not exist or are not behind the
+    query, in any order."""
+    require_gpu()
+    say("block attention, selection", kind, d, H, Hkv)
+    n, top = 460, 8
+    g = torch.Generator().manual_seed(5)
+    idx = torch.randint(-3, n // 64 + 3, (1, Hkv, n, top), generator=g, dtype=torch.int32)
+    if kind == "none":
+        idx.fill_(-1)
+    elif kind == "all":
+        idx[:] = torch.arange(top, dtype=torch.int32)
+    elif kind == "one block":
+        idx.fill_(-1)
+        idx[..., 3] = 0
+    elif kind == "repeated":
+        idx[:] = torch.randint(0, 2, idx.shape, generator=g, dtype=torch.int32)
+    elif kind == "out of range":
+        idx[:] = torch.where(torch.rand(idx.shape, generator=g) < 0.5, idx, torch.tensor(2 ** 31 - 1, dtype=torch.int32))
+        idx[:, :, ::3, 0] = -2 ** 31
+        idx[:, :, 1::3, 1] = 2 ** 30
+    q, k, v, dO = draw(31, 1, H, Hkv, n, d)
+    check_all(q, k, v, dO, idx.cuda(), 1 / math.sqrt(d))
+
+
+@pytest.mark.parametrize("kind", ["v zero", "v large", "v small", "peaked", "flat"])
+def test_values_of_all_sizes(kind):
+    """Partial results are held relative to their block's largest value: of any size; and softmaxes of one key and of all."""
+    require_gpu()
+    say("block attention,", kind)
+    q, k, v, dO = draw(41, 1, 4, 2, 400, 64, qk={"peaked": 4.0, "flat": 0.0}.get(kind, 1.5))
+    if kind == "v zero":
+        v[:, :, 64:256] = 0
+    elif kind == "v large":
+        v.mul_(2.0 ** 40)
+        dO.mul_(2.0 ** -40)
+    elif kind == "v small":
+        v.mul_(2.0 ** -60)
+    idx = spk.sparsek_block_select(q, k, 3)
+    check_all(q, k, v, dO, idx, 1 / 8)
+
+
+def test_many_rows_select_one_block():
+    """A block that everybody selects: its rows span many units."""
+    require_gpu()
+    say("block attention, a popular block")
+    n, H, Hkv, d = 900, 8, 2, 128
+    q, k, v, dO = draw(51, 1, H, Hkv, n, d)
+    idx = torch.full((1, Hkv, n, 2), -1, dtype=torch.int32)
+    idx[:, 0, :, 0] = 1
+    idx[:, 1, :, 1] = 0
+    check_all(q, k, v, dO, idx.cuda(), 1 / math.sqrt(d))
+
+
+def test_a_long_document_row_by_row():
+    """30000 tokens: rows picked all over it against a definition of their own."""
+    require_gpu()
+    say("block attention, 30000 tokens")
+    n, H, Hkv, d, top = 30000, 4, 1, 128, 16
+    q, k, v, dO = draw(61, 1, H, Hkv, n, d)
+    scale = 1 / math.sqrt(d)
+    idx = spk.sparsek_block_select(q, k, top)
+    o, lse, mass = spk.sparsek_block_attn_fwd(q, k, v, idx, scale, mass=True)
+    dq, dk, dv = spk.sparsek_block_attn_bwd(q, k, v, idx, o, lse, dO, scale)
+    torch.cuda.synchronize()
+    assert abs(float(mass.double().sum()) / (n * H) - 1) < 1e-5      # every row hands out a weight of 1
+    K, V = ref.f64(k[0, 0]), ref.f64(v[0, 0])
+    for i in list(range(0, n, 1777)) + [n - 1]:
+        at = torch.cat([torch.arange(64) + 64 * j for j in idx[0, 0, i].tolist() if j >= 0] + [torch.arange(i // 64 * 64, i + 1)])
+        s = ref.f64(q[0, :, i]) @ K[at].T * scale
+        p = torch.softmax(s, 1)
+        A = p @ V[at].abs()
+        want = p @ V[at]
+        within(o[0, :, i], want, 2 ** -8 * want.abs() + (2 ** -8 + 2 ** -11 + 2 ** -14) * A + 2 ** -22 * V.abs().max(), "o of row %d" % i)
+        g, oo = ref.f64(dO[0, :, i]), ref.f64(o[0, :, i])
+        delta = (g * oo).sum(1, keepdim=True)
+        ds = p * (g @ V[at].T - delta) * scale
+        e = (2 ** -8 + 2 ** -11 + 2 ** -14) * ds.abs() + 2 ** -17 * p * (g.abs() @ V[at].abs().T + (g * oo).abs().sum(1, keepdim=True)) * scale
+        want = ds @ K[at]
+        within(dq[0, :, i], want, 2 ** -8 * want.abs() + e @ K[at].abs() + 2 ** -22 * (ds.abs() @ K[at].abs()).amax(1, keepdim=True), "dq of row %d" % i)
+    assert torch.isfinite(dk).all() and torch.isfinite(dv).all()
+
+
+def test_results_do_not_depend_on_timing():
+    require_gpu()
+    say("block attention, twice")
+    q, k, v, dO = draw(71, 2, 8, 2, 2500, 128)
+    runs = []
+    for _ in range(2):
+        idx = spk.sparsek_block_select(q, k, 6)
+        o, lse, mass = spk.sparsek_block_attn_fwd(q, k, v, idx, 0.1, mass=True)
+        runs.append((idx, o, lse, mass) + spk.sparsek_block_attn_bwd(q, k, v, idx, o, lse, dO, 0.1))
+    torch.cuda.synchronize()
+    for a, b in zip(*runs):
+        assert torch.equal(a, b)
+
+
+def test_training_step_replays_as_a_graph():
+    """Selection, forward and backward captured once, replayed on new inputs with eager work in between, and on a side stream."""
+    require_gpu()
+    say("block attention as a graph")
+    shape = (1, 4, 2, 700, 64)
+    q, k, v, dO = draw(81, *shape)
+
+    def step(q, k, v, dO):
+        idx = spk.sparsek_block_select(q, k, 4)
+        o, lse, mass = spk.sparsek_block_attn_fwd(q, k, v, idx, 0.125, mass=True)
+        return (idx, o, lse, mass) + spk.sparsek_block_attn_bwd(q, k, v, idx, o, lse, dO, 0.125)
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step(q, k, v, dO)
+    torch.cuda.current_stream().wait_stream(s)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = step(q, k, v, dO)
+    for rep in range(4):
+        new = draw(90 + rep, *shape)
+        for a, b in zip((q, k, v, dO), new):
+            a.copy_(b)
+        g.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, step(*new)):
+            assert torch.equal(a, b), rep
+        torch.cuda.synchronize()
