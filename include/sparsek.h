@@ -269,7 +269,8 @@ int sparsek_chunk_status(const sparsek_chunk_cfg *cfg, const void *state, int32_
  * sparsek_block_select fills idx [B,Hkv,n,top] int32: for every query the (up to) `top` blocks behind its own with the largest scores, in
  * ascending order, padded with -1; of equal scores the older block wins.
  *     mean_j  = mean of the block's keys (summed in fp64, rounded to fp32)
- *     m8_j    = rint(mean_j * (127 / max|mean_j|)), ms_j = max|mean_j| / 127         (0 where the maximum is below 2^-100)
+ *     m8_j    = rint(mean_j * (1 / max|mean_j| * 127)), ms_j = max|mean_j| * (1/127)   (0 where the maximum is below 2^-100; every
+ *               operation rounded to fp32)
  *     p8_i    = the same rounding of the sum of the group's queries at position i
  *     score   = float(p8_i . m8_j) * ms_j                                            (the product is exact)
  * A selection from anywhere else will do for the attention too: entries that are no block behind the query's own (-1 among them) and
@@ -302,8 +303,8 @@ int sparsek_block_attn_bwd(const sparsek_block_cfg *cfg, const void *q, const vo
 /* ---- a key/value cache in blocks of 64 tokens held in 8 bits, its attention, and eviction by accumulated weight ----
  * The cache is tensors of the caller's.  A page holds one block of one key/value head; the pool has `pages` of them, which any
  * sequence and head may name (two may name the same one, as for a common prefix).
- *     k8 [pages,64,d], v8 [pages,d,64] (transposed)   codes: SPARSEK_I8 int8, rint(x * (127 / max)); SPARSEK_E4M3 OCP e4m3, x * (448 / max)
- *     ks, vs [pages] fp32                             what a code of 1 stands for: max / 127 or max / 448, max = the block's largest |x|;
+ *     k8 [pages,64,d], v8 [pages,d,64] (transposed)   codes: SPARSEK_I8 int8, rint(x * (1 / max * 127)); SPARSEK_E4M3 OCP e4m3, x * (1 / max * 448)
+ *     ks, vs [pages] fp32                             what a code of 1 stands for: max * (1/127) or max * (1/448), max = the block's largest |x|;
  *                                                     a block with max < 2^-100 is held as zeros with scale 0
  *     km [pages,d] int8, kms [pages] fp32             the block's mean key, as m8 and ms of sparsek_block_select
  *     kt [B,Hkv,64,d], vt [B,Hkv,d,64] of `dtype`     the tokens of the last, unfinished block

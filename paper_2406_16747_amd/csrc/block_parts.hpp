@@ -93,9 +93,11 @@ __device__ __forceinline__ void load_rows(unsigned char* tile, const uint16_t* s
     }
 }
 
-// Rounds to whole numbers of at most 127: the mean key of a block, the pooled query, a block held in 8 bits.  The factor is
-// one division, the product is rounded once and then to the nearest whole number (even on ties): the same in every kernel.
-__device__ __forceinline__ float code_factor(float top, float most) { return top >= TINY_MAX ? most / top : 0.0f; }
+// Rounds to whole numbers of at most 127: the mean key of a block, the pooled query, a block held in 8 bits.  The factor is the
+// reciprocal of the largest magnitude, rounded, times 127 (or 448), rounded; the product with it is rounded once and then to the
+// nearest whole number (even on ties): the same in every kernel.  What a code of 1 stands for: the magnitude times 1/127 (1/448).
+__device__ __forceinline__ float code_factor(float top, float most) { return top >= TINY_MAX ? (1.0f / top) * most : 0.0f; }
+__device__ __forceinline__ float code_scale(float top, float most) { return top >= TINY_MAX ? top * (1.0f / most) : 0.0f; }
 __device__ __forceinline__ int code_i8(float x, float f)
 {
     const float y = rintf(x * f);

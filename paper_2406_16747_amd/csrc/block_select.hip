@@ -40,7 +40,7 @@ __global__ __launch_bounds__(256) void block_means_kernel(const uint16_t* __rest
     }
     const float top = __uint_as_float(block_max_bits(__float_as_uint(fabsf(mean)), red, tid));
     if (tid < D) km[(bg * nbw + j) * D + tid] = (int8_t)code_i8(mean, code_factor(top, 127.0f));
-    if (tid == 0) kms[bg * nbw + j] = top >= TINY_MAX ? top / 127.0f : 0.0f;
+    if (tid == 0) kms[bg * nbw + j] = code_scale(top, 127.0f);
 }
 
 // One workgroup of 4 waves per (64 queries, batch and head), a wave per 16 queries.  The `top` largest of up to thousands of

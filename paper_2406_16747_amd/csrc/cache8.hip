@@ -99,9 +99,9 @@ __device__ __forceinline__ void store_block(AppendSmem<D>& sm, const CacheArgs& 
     const float topm = __uint_as_float(block_max_bits(__float_as_uint(fabsf(mean)), sm.red, tid));
     if (tid < D) a.t.km[(size_t)page * D + tid] = (int8_t)code_i8(mean, code_factor(topm, 127.0f));
     if (tid == 0) {
-        a.t.ks[page] = topk >= TINY_MAX ? topk / most : 0.0f;
-        a.t.vs[page] = topv >= TINY_MAX ? topv / most : 0.0f;
-        a.t.kms[page] = topm >= TINY_MAX ? topm / 127.0f : 0.0f;
+        a.t.ks[page] = code_scale(topk, most);
+        a.t.vs[page] = code_scale(topv, most);
+        a.t.kms[page] = code_scale(topm, 127.0f);
     }
 }
 

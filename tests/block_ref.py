@@ -20,8 +20,8 @@ def codes_i8(x):
     x = x.float()
     top = x.abs().amax(-1, keepdim=True)
     some = top >= TINY
-    f = torch.where(some, torch.tensor(127.0) / torch.where(some, top, torch.ones(())), torch.zeros(()))
-    return torch.round(x * f).clamp(-127, 127), torch.where(some, top / 127.0, torch.zeros(()))[..., 0]
+    f = torch.where(some, torch.ones(()) / torch.where(some, top, torch.ones(())) * torch.tensor(127.0), torch.zeros(()))
+    return torch.round(x * f).clamp(-127, 127), torch.where(some, top * (torch.ones(()) / torch.tensor(127.0)), torch.zeros(()))[..., 0]
 
 
 def mean_codes(blocks):
@@ -115,10 +115,10 @@ def block_codes(x, fmt):
     x = x.detach().cpu().float()
     top = x.abs().amax((-1, -2), keepdim=True)
     some = top >= TINY
-    f = torch.where(some, torch.tensor(most) / torch.where(some, top, torch.ones(())), torch.zeros(()))
+    f = torch.where(some, torch.ones(()) / torch.where(some, top, torch.ones(())) * torch.tensor(most), torch.zeros(()))
     y = (x * f).clamp(-most, most)
     y = torch.round(y) if fmt == torch.int8 else y.to(torch.float8_e4m3fn).float()
-    return y, torch.where(some, top / most, torch.zeros(()))[..., 0, 0]
+    return y, torch.where(some, top * (torch.ones(()) / torch.tensor(most)), torch.zeros(()))[..., 0, 0]
 
 
 def values(t):
