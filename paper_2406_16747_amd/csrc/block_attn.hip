@@ -2,68 +2,88 @@
 //
 // Queries that lie side by side select different blocks, so a tile of queries against the union of their blocks would do
 // several times the work.  The kernels go by key block instead: block_tiles_kernel takes a block's K and V into LDS once and
-// walks the queries that selected it, 32 rows (query, head of the group) to a wave: S^T = K.Q^T, the softmax of these 64 keys alone,
-// O^T = V^T.P^T, and leaves the normalised partial result, with the log of its denominator, in list order.  block_join_kernel takes
-// 64 queries at a time, does their own block (causal) in the same way and adds the partial results with their weights.
-// What bounds it is memory: a selected (row, block) pair moves D halves out and in again and a row of q in, for 4*64*D flops.
+// walks the queries that attend it, 32 rows (query, head of the group) to a wave: S^T = K.Q^T, the softmax of these 64 keys alone,
+// O^T = V^T.P^T, and leaves the normalised partial result, with the log of its denominator, in list order.  block_join_kernel adds up
+// the partial results of every row with their weights.
+// What bounds it is memory: a (row, block) pair moves a row of q in and D halves out and in again, for 4*64*D flops.
 #include "block_parts.hpp"
+
+#include <cmath>
 
 namespace spk {
 
 // ---- the lists ----
 
-__global__ __launch_bounds__(256) void block_masks_zero_kernel(u32x4* p, size_t n16)
+// The chunk's 64 queries as bits, for the key blocks j0 .. j0 + MASK_BLOCKS - 1.
+constexpr int MASK_BLOCKS = 4096;
+__device__ __forceinline__ void chunk_masks(unsigned long long* masks, const BlockLists& l, const int32_t* idx, int bg, int c, int j0, int tid)
 {
-    for (size_t x = blockIdx.x * (size_t)256 + threadIdx.x; x < n16; x += (size_t)gridDim.x * 256) p[x] = u32x4{0, 0, 0, 0};
+    const int jn = min(MASK_BLOCKS, c - j0), rows = min(BT, l.n - c * BT);
+    for (int x = tid; x < jn; x += 256) masks[x] = 0;
+    __syncthreads();
+    const int32_t* row = idx + ((size_t)bg * l.n + (size_t)c * BT) * l.top;
+    for (int x = tid; x < rows * l.top; x += 256) {
+        const int j = row[x] - j0;
+        if (row[x] >= j0 && j < jn) atomicOr(&masks[j], 1ull << (x / l.top));
+    }
+    __syncthreads();
 }
 
-__global__ __launch_bounds__(256) void block_masks_kernel(BlockLists l, const int32_t* __restrict__ idx)
+// counts: a workgroup per (chunk, batch and head).
+__global__ __launch_bounds__(256) void block_counts_kernel(BlockLists l, const int32_t* __restrict__ idx)
 {
-    const int bg = blockIdx.y;
-    const size_t x = blockIdx.x * (size_t)256 + threadIdx.x;
-    if (x >= (size_t)l.n * l.top) return;
-    const int i = (int)(x / l.top), c = i / BT, j = idx[(size_t)bg * l.n * l.top + x];
-    if (j >= 0 && j < c) atomicOr(&l.masks[((size_t)bg * l.nb + c) * l.nb + j], 1ull << (i % BT));
+    __shared__ unsigned long long masks[MASK_BLOCKS];
+    const int c = blockIdx.x, bg = blockIdx.y, tid = threadIdx.x;
+    for (int j0 = 0; j0 < c; j0 += MASK_BLOCKS) {
+        chunk_masks(masks, l, idx, bg, c, j0, tid);
+        for (int x = tid; x < min(MASK_BLOCKS, c - j0); x += 256) l.counts[((size_t)bg * l.nb + c) * l.nb + j0 + x] = (uint8_t)__popcll(masks[x]);
+        __syncthreads();
+    }
 }
 
-// off and total: a workgroup of 1024 per 64 blocks, its 16 waves share the chunks.
+// off and total: a workgroup of 1024 per (64 blocks, stretch, batch and head), its 16 waves share the stretch's chunks.
 __global__ __launch_bounds__(1024) void block_offsets_kernel(BlockLists l)
 {
     __shared__ int part[16][64];
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, j = blockIdx.x * 64 + lane, bg = blockIdx.y;
-    const int jc = min(j, l.nb - 1);
-    const int per = (l.nb + 15) / 16, c0 = wv * per, c1 = min(l.nb, c0 + per);
-    const unsigned long long* m = l.masks + (size_t)bg * l.nb * l.nb + jc;
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, j = blockIdx.x * 64 + lane, bg = blockIdx.z;
+    const int first = (int)blockIdx.y * (l.cq / BT), count = min(l.cq / BT, l.nb - first);
+    if ((int)blockIdx.x * 64 >= first + count) return;   // nobody sees these blocks yet
+    const int per = (count + 15) / 16, c1 = l.top ? first + min(count, wv * per + per) : 0;
+    const int c0 = max(first + wv * per, j + 1);         // (a chunk selects blocks behind its own only)
+    const uint8_t* m = l.counts + (size_t)bg * l.nb * l.nb + j;
     int sum = 0;
 #pragma unroll 8
-    for (int c = c0; c < c1; c++) sum += __popcll(m[(size_t)c * l.nb]);
+    for (int c = c0; c < c1; c++) sum += m[(size_t)c * l.nb];
     part[wv][lane] = sum;
     __syncthreads();
-    int run = 0, all = 0;
+    const int own = j >= first && j < first + count ? min(BT, l.n - j * BT) : 0;
+    int run = own, all = own;
 #pragma unroll
     for (int w = 0; w < 16; w++) {
         run += w < wv ? part[w][lane] : 0;
         all += part[w][lane];
     }
-    if (j >= l.nb) return;
+    if (j >= first + count) return;
     int32_t* off = l.off + (size_t)bg * l.nb * l.nb + j;
 #pragma unroll 8
     for (int c = c0; c < c1; c++) {
         off[(size_t)c * l.nb] = run;
-        run += __popcll(m[(size_t)c * l.nb]);
+        run += m[(size_t)c * l.nb];
     }
-    if (wv == 0) l.total[(size_t)bg * l.nb + j] = all;
+    if (wv == 0) l.total[l.cbg(blockIdx.y, bg) * l.nb + j] = all;
 }
 
-// base and units: a workgroup of 1024 per (batch, head).
+// base and units: a workgroup of 1024 per (stretch, batch and head).
 __global__ __launch_bounds__(1024) void block_units_kernel(BlockLists l)
 {
     __shared__ int2 wsum[16];
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, bg = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    const size_t cbg = l.cbg(blockIdx.x, blockIdx.y);
+    const int seen = min(l.nb, ((int)blockIdx.x + 1) * (l.cq / BT));   // blocks that the stretch's queries can see
     int2 done = make_int2(0, 0);   // list entries and units ahead of this round of 1024 blocks
-    for (int j0 = 0; j0 < l.nb; j0 += 1024) {
+    for (int j0 = 0; j0 < seen; j0 += 1024) {
         const int j = j0 + tid;
-        const int mine = j < l.nb ? l.total[(size_t)bg * l.nb + j] : 0;
+        const int mine = j < seen ? l.total[cbg * l.nb + j] : 0;
         const int units = (int)(((long long)mine * l.G + l.unit - 1) / l.unit);
         int2 s = make_int2(mine, units);
 #pragma unroll
@@ -80,289 +100,379 @@ __global__ __launch_bounds__(1024) void block_units_kernel(BlockLists l)
             all.x += wsum[w].x;
             all.y += wsum[w].y;
         }
-        if (j < l.nb) {
-            l.base[(size_t)bg * l.nb + j] = before.x + s.x - mine;
+        if (j < seen) {
+            l.base[cbg * l.nb + j] = before.x + s.x - mine;
             const int u0 = before.y + s.y - units;
-            l.first_unit[(size_t)bg * l.nb + j] = u0;
+            l.first_unit[cbg * l.nb + j] = u0;
             for (int u = 0; u < units; u++)
-                if (u0 + u < l.maxu) l.units[(size_t)bg * l.maxu + u0 + u] = make_int2(j, u * l.unit);
+                if (u0 + u < l.maxu) l.units[cbg * l.maxu + u0 + u] = make_int2(j, u * l.unit);
         }
         done.x += all.x;
         done.y += all.y;
         __syncthreads();
     }
-    if (tid == 0) l.nunits[bg] = min(done.y, l.maxu);
+    if (tid == 0) l.nunits[cbg] = min(done.y, l.maxu);
 }
 
+// list and pos: a workgroup per (chunk, batch and head).
 __global__ __launch_bounds__(256) void block_place_kernel(BlockLists l, const int32_t* __restrict__ idx)
 {
-    const int bg = blockIdx.y;
-    const size_t x = blockIdx.x * (size_t)256 + threadIdx.x;
-    if (x >= (size_t)l.n * l.top) return;
-    const int i = (int)(x / l.top), s = (int)(x % l.top), c = i / BT;
-    const int32_t* row = idx + ((size_t)bg * l.n + i) * l.top;
-    const int j = row[s];
-    bool ok = j >= 0 && j < c;
-    for (int y = 0; y < s; y++) ok &= row[y] != j;   // (a repeated block counts once)
-    int p = -1;
-    if (ok) {
-        const size_t cj = ((size_t)bg * l.nb + c) * l.nb + j;
-        p = l.base[(size_t)bg * l.nb + j] + l.off[cj] + __popcll(l.masks[cj] & ((1ull << (i % BT)) - 1));
-        l.list[(size_t)bg * l.pairs + p] = i;
+    __shared__ unsigned long long masks[MASK_BLOCKS];
+    const int c = blockIdx.x, bg = blockIdx.y, tid = threadIdx.x, rows = min(BT, l.n - c * BT);
+    const size_t cbg = l.cbg(c * BT / l.cq, bg);
+    int32_t *list = l.list + cbg * l.entries, *pos = l.pos + ((size_t)bg * l.n + (size_t)c * BT) * l.slots;
+    const int32_t* base = l.base + cbg * l.nb;
+    if (tid < rows) {
+        list[base[c] + tid] = c * BT + tid;
+        pos[(size_t)tid * l.slots] = base[c] + tid;
     }
-    l.pos[(size_t)bg * l.n * l.top + x] = p;
+    const int32_t *row = idx + ((size_t)bg * l.n + (size_t)c * BT) * l.top, *off = l.off + ((size_t)bg * l.nb + c) * l.nb;
+    for (int j0 = 0; j0 == 0 || j0 < c; j0 += MASK_BLOCKS) {
+        if (c) chunk_masks(masks, l, idx, bg, c, j0, tid);
+        for (int x = tid; x < rows * l.top; x += 256) {
+            const int r = x / l.top, s = x % l.top, j = row[x];
+            if (j < 0 || j >= c) {
+                if (j0 == 0) pos[(size_t)r * l.slots + 1 + s] = -1;
+                continue;
+            }
+            if (j < j0 || j >= j0 + MASK_BLOCKS) continue;
+            int p = base[j] + off[j] + __popcll(masks[j - j0] & ((1ull << r) - 1));
+            for (int y = 0; y < s; y++) p = row[x - s + y] == j ? -1 : p;   // (a repeated block counts once)
+            if (p >= 0) list[p] = c * BT + r;
+            pos[(size_t)r * l.slots + 1 + s] = p;
+        }
+        __syncthreads();
+    }
 }
 
 int launch_block_lists(const BlockLists& l, const int32_t* idx, hipStream_t st)
 {
-    if (!l.pairs) {   // nobody has a block behind it to select, but the slots are read
-        if (l.top) hipLaunchKernelGGL(block_place_kernel, dim3((unsigned)(((size_t)l.n * l.top + 255) / 256), l.B * l.Hkv), dim3(256), 0, st, l, idx);
-        return launch_status();
-    }
     const int BG = l.B * l.Hkv;
-    const size_t n16 = align_up((size_t)BG * l.nb * l.nb * 8, 256) / 16;
-    hipLaunchKernelGGL(block_masks_zero_kernel, dim3((unsigned)std::min<size_t>(2048, (n16 + 255) / 256)), dim3(256), 0, st, (u32x4*)l.masks, n16);
-    const dim3 pairs((unsigned)(((size_t)l.n * l.top + 255) / 256), BG);
-    hipLaunchKernelGGL(block_masks_kernel, pairs, dim3(256), 0, st, l, idx);
-    hipLaunchKernelGGL(block_offsets_kernel, dim3((l.nb + 63) / 64, BG), dim3(1024), 0, st, l);
-    hipLaunchKernelGGL(block_units_kernel, dim3(BG), dim3(1024), 0, st, l);
-    hipLaunchKernelGGL(block_place_kernel, pairs, dim3(256), 0, st, l, idx);
+    if (l.top) hipLaunchKernelGGL(block_counts_kernel, dim3(l.nb, BG), dim3(256), 0, st, l, idx);
+    hipLaunchKernelGGL(block_offsets_kernel, dim3((l.nb + 63) / 64, l.nc, BG), dim3(1024), 0, st, l);
+    hipLaunchKernelGGL(block_units_kernel, dim3(l.nc, BG), dim3(1024), 0, st, l);
+    hipLaunchKernelGGL(block_place_kernel, dim3(l.nb, BG), dim3(256), 0, st, l, idx);
     return launch_status();
 }
 
 // ---- the forward ----
 
+constexpr double FWD_STRETCH_BYTES = 8e9;
+
 struct BlockFwd {
     BlockArgs a;
     uint16_t* o;
     float* lse;
-    _Float16* part;    // [entry rows][D], a row as the two lanes of its column hold it: [lane / 32][D / 2]
-    float2* meta;      // log2 of the denominator, and the factor that the halves stand for
-    float* own;        // the same log2 for every query's own block [B,H,n]
+    _Float16* part;    // [nbg][entry rows of a stretch][D]
+    float2* meta;      // log2 of the row's denominator, and the factor that the halves stand for
     float* mass;       // [B,Hkv,nb] or null
+    int c, bg0, nbg;   // the stretch, the first of the heads (of all batches) and their number
 };
 
-// One tile of 32 rows against the block's keys: S^T = K.Q^T for NKH halves of 32 keys, softmax, O^T = V^T.P^T.  A lane has one
-// column (row of q).  causal >= 0: the column sees keys 0 .. causal of the block.
-template <int D, int NKH, bool CAUSAL>
-__device__ __forceinline__ void block_column(uint32_t rk, uint32_t tv, const bf16x8 (&qf)[D / 16], float c2, int causal, int half,
-                                             f32x16 (&acc)[D / 32], float& m, float& l)
+template <int D>
+__device__ __forceinline__ f16x8 transposed_half(uint32_t at) { return __builtin_bit_cast(f16x8, transposed_operand<D>(at)); }
+
+// The softmax of one tile of 32 rows against the block's 64 keys: S^T = K.Q^T, and P^T as the operand of O^T = V^T.P^T.  A lane has one
+// column (row of q); with `own` it sees keys 0 .. limit of the block.  V is in fp16, relative to the block's largest value, and so
+// are the weights (times 2^15): a weight is rounded to 2^-11 where bf16 would keep 2^-8, at the same rate.
+template <int D>
+__device__ __forceinline__ void block_weights(uint32_t rk, const bf16x8 (&qf)[D / 16], float c2, bool own, int limit, int half, f16x8 (&pb)[4],
+                                              float& m, float& den)
 {
     using S = RowTile<D>;
-    constexpr int DS = D / 16, DB = D / 32;
-    f32x16 s[NKH];
+    constexpr int DS = D / 16;
+    f32x16 s[2];
 #pragma unroll
-    for (int kh = 0; kh < NKH; kh++) {
+    for (int kh = 0; kh < 2; kh++) {
+        bf16x8 ka[DS];   // (all of them on their way before the first product waits for one)
+#pragma unroll
+        for (int x = 0; x < DS; x++) ka[x] = row_operand(rk + 2 * kh * S::R16 + 32 * x);
+        __builtin_amdgcn_sched_barrier(0);
         s[kh] = f32x16{0};
 #pragma unroll
-        for (int x = 0; x < DS; x++) s[kh] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_operand(rk + 2 * kh * S::R16 + 32 * x), qf[x], s[kh], 0, 0, 0);
+        for (int x = 0; x < DS; x++) s[kh] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[x], qf[x], s[kh], 0, 0, 0);
     }
+    if (own)
+#pragma unroll
+        for (int kh = 0; kh < 2; kh++)
+#pragma unroll
+            for (int r = 0; r < 16; r++) s[kh][r] = 32 * kh + 8 * (r / 4) + 4 * half + r % 4 > limit ? -INFINITY : s[kh][r];
     m = -INFINITY;
 #pragma unroll
-    for (int kh = 0; kh < NKH; kh++)
+    for (int kh = 0; kh < 2; kh++)
 #pragma unroll
-        for (int r = 0; r < 16; r++) {
-            if (CAUSAL && 32 * kh + 8 * (r / 4) + 4 * half + r % 4 > causal) s[kh][r] = -INFINITY;
-            m = fmaxf(m, s[kh][r]);
-        }
+        for (int r = 0; r < 16; r++) m = fmaxf(m, s[kh][r]);
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
     m = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * c2;
-    const float ref = m == -INFINITY ? 0.0f : m;
-    l = 0.0f;
-    bf16x8 pb[NKH][2];
+    const float ref = (m == -INFINITY ? 0.0f : m) - 15.0f;
+    den = 0.0f;
 #pragma unroll
-    for (int kh = 0; kh < NKH; kh++)
+    for (int kh = 0; kh < 2; kh++)
 #pragma unroll
         for (int r = 0; r < 16; r++) {
             const float p = __builtin_amdgcn_exp2f(fmaf(s[kh][r], c2, -ref));
-            l += p;
-            pb[kh][r >> 3][r & 7] = (__bf16)p;   // the operand of the second product: 2^-9 of every weight, as in the other attention kernels
+            den += p;
+            pb[2 * kh + (r >> 3)][r & 7] = (_Float16)p;
         }
-    const auto sl = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
-    l = __uint_as_float(sl[0]) + __uint_as_float(sl[1]);
-#pragma unroll
-    for (int x = 0; x < DB; x++) acc[x] = f32x16{0};
-#pragma unroll
-    for (int g = 0; g < 2 * NKH; g++)
-#pragma unroll
-        for (int x = 0; x < DB; x++)
-            acc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_operand<D>(tv + g * S::R16 + 64 * x), pb[g >> 1][g & 1], acc[x], 0, 0, 0);
+    const auto sl = __builtin_amdgcn_permlane32_swap(__float_as_uint(den), __float_as_uint(den), false, false);
+    den = __uint_as_float(sl[0]) + __uint_as_float(sl[1]);
 }
 
 template <int D>
 struct FwdBlockSmem {
+    static constexpr int RS = 128 + 16;     // bytes between rows: half a row of 128 columns
     unsigned char k[RowTile<D>::BYTES], v[RowTile<D>::BYTES];
+    unsigned char rows[4][32 * RS];         // a wave's rows on their way in and its results on their way out
     unsigned red[4];
 };
+static_assert(sizeof(FwdBlockSmem<128>) <= 160 * 1024 / 3, "three workgroups per CU");
 
 template <int D>
-__global__ __launch_bounds__(256, 2) void block_tiles_kernel(BlockFwd f)
+__global__ __launch_bounds__(256, 3) void block_tiles_kernel(BlockFwd f)
 {
     __shared__ __attribute__((aligned(16))) FwdBlockSmem<D> sm;
+    constexpr int CPR = D / 8;
     const BlockLists& l = f.a.l;
-    const int bg = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, col = lane & 31, half = lane >> 5;
-    if ((int)blockIdx.x >= l.nunits[bg]) return;
-    const int2 u = l.units[(size_t)bg * l.maxu + blockIdx.x];
+    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
+    int bg, un;
+    deal_head(blockIdx.x, l.maxu, f.nbg, bg, un);
+    bg += f.bg0;
+    const size_t cbg = l.cbg(f.c, bg);
+    if (un >= l.nunits[cbg]) return;
+    const int2 u = l.units[cbg * l.maxu + un];
     const int j = u.x, first = u.y, G = l.G;
-    const int base = l.base[(size_t)bg * l.nb + j];
-    const int end = min(l.total[(size_t)bg * l.nb + j] * G, first + l.unit);
+    const int base = l.base[cbg * l.nb + j];
+    const int end = min(l.total[cbg * l.nb + j] * G, first + l.unit);
     const size_t kv = ((size_t)bg * l.n + (size_t)j * BT) * D;
-    load_rows<D>(sm.k, f.a.k + kv, BT - 1, tid);
-    load_rows<D>(sm.v, f.a.v + kv, BT - 1, tid);
-    // the largest |v| of the block scales its partial results
+    const int last = l.n - 1 - j * BT;
+    load_rows<D>(sm.k, f.a.k + kv, last, tid);
+    // V goes to fp16 relative to its largest magnitude
+    u32x4 vr[BT * CPR / 256];
     unsigned top = 0;
-    for (int x = tid; x < BT * D / 8; x += 256) {
-        const u32x4 y = *(const u32x4*)(f.a.v + kv + 8 * x);
 #pragma unroll
-        for (int e = 0; e < 4; e++) top = max(top, max(y[e] << 16 & 0x7FFFFFFFu, y[e] & 0x7FFF0000u));
+    for (int t = 0; t < BT * CPR / 256; t++) {
+        const int id = tid + 256 * t;
+        vr[t] = *(const u32x4*)(f.a.v + kv + (size_t)min(id / CPR, last) * D + 8 * (id % CPR));
+#pragma unroll
+        for (int e = 0; e < 4; e++) top = max(top, max(vr[t][e] << 16 & 0x7FFFFFFFu, vr[t][e] & 0x7FFF0000u));
     }
     const int E = scale_exp(block_max_bits(top, sm.red, tid));
-    const float down = __uint_as_float((unsigned)(254 - E) << 23), up = __uint_as_float((unsigned)E << 23);
+    const float down = scale_down(E), up = scale_up(E);
+#pragma unroll
+    for (int t = 0; t < BT * CPR / 256; t++) {
+        const int id = tid + 256 * t;
+        f16x8 y;
+#pragma unroll
+        for (int e = 0; e < 8; e++) y[e] = (_Float16)(__uint_as_float(e & 1 ? vr[t][e / 2] & 0xFFFF0000u : vr[t][e / 2] << 16) * down);
+        *(f16x8*)(sm.v + RowTile<D>::offset(id / CPR) + 16 * (id % CPR)) = y;
+    }
+    __syncthreads();
     const uint32_t rk = lds_address(sm.k) + row_lane<D>(lane), tv = lds_address(sm.v) + transposed_lane<D>(lane);
     const int b = bg / l.Hkv, g = bg % l.Hkv;
-    const int32_t* list = l.list + (size_t)bg * l.pairs + base;
-    const size_t row0 = ((size_t)bg * l.pairs + base) * G;
-    for (int r0 = first + 32 * wv; r0 < end; r0 += 128) {
-        const int r = r0 + col, rc = min(r, end - 1);
-        const int i = list[rc / G], h = g * G + rc % G;
-        const uint16_t* qr = f.a.q + (((size_t)b * l.H + h) * l.n + i) * D + 8 * half;
-        bf16x8 qf[D / 16];
+    const int32_t* list = l.list + cbg * l.entries + base;
+    const size_t row0 = ((size_t)(bg - f.bg0) * l.entries + base) * G;
+    constexpr int RS = FwdBlockSmem<D>::RS, NH = D / 64;
+    unsigned char* rows = sm.rows[wv];
+    const int own_end = j >= f.c * (l.cq / BT) && j < (f.c + 1) * (l.cq / BT) ? min(BT, last + 1) * G : 0;
+    // Rows come and go in whole lines, 8 lanes to 64 columns of a row, and change places with the operands' layout in LDS, 64 columns
+    // at a time.  The rows of the next tile and the queries of the one behind it are on their way while a tile is computed.
+    const int lrow = lane >> 3, lcol = 8 * (lane & 7);
+    const uint16_t* q0 = f.a.q + ((size_t)b * l.H + g * G) * l.n * D + lcol;
+    auto entry = [&](int r) { return list[min(r, end - 1) / G]; };
+    auto load_q = [&](int r, int i, u32x4 (&to)[4 * NH]) {   // r, i: of the lane's column
+        const int at = min(r, end - 1) % G * l.n + i;
 #pragma unroll
-        for (int x = 0; x < D / 16; x++) qf[x] = *(const bf16x8*)(qr + 16 * x);
-        f32x16 acc[D / 32];
-        float m, den;
-        block_column<D, 2, false>(rk, tv, qf, f.a.c2, 0, half, acc, m, den);
-        if (r < end) {
-            const float inv = den > 0.0f ? down / den : den;   // (nothing but -inf: weight 0 in the sum)
-            _Float16* pr = f.part + (row0 + r) * D + half * (D / 2);
+        for (int t = 0; t < 4; t++) {
+            const uint16_t* row = q0 + (size_t)__shfl(at, 8 * t + lrow, 64) * D;
 #pragma unroll
-            for (int x = 0; x < D / 32; x++)
-#pragma unroll
-                for (int y = 0; y < 2; y++) {
-                    f16x8 v;
-#pragma unroll
-                    for (int e = 0; e < 8; e++) v[e] = (_Float16)(acc[x][8 * y + e] * inv);
-                    *(f16x8*)(pr + 16 * x + 8 * y) = v;
-                }
-            if (half == 0) f.meta[row0 + r] = make_float2(m + log2f(den), up);
+            for (int h = 0; h < NH; h++) to[4 * h + t] = *(const u32x4*)(row + 64 * h);
         }
+    };
+    bf16x8 qf[D / 16];
+    auto take_q = [&](const u32x4 (&from)[4 * NH]) {
+#pragma unroll
+        for (int h = 0; h < NH; h++) {
+#pragma unroll
+            for (int t = 0; t < 4; t++) *(u32x4*)(rows + (8 * t + lrow) * RS + 2 * lcol) = from[4 * h + t];
+            wave_lds_order();
+#pragma unroll
+            for (int x = 0; x < 4; x++) qf[4 * h + x] = *(const bf16x8*)(rows + col * RS + 32 * x + 16 * half);
+            wave_lds_order();
+        }
+    };
+    int r0 = first + 32 * wv;
+    if (r0 >= end) return;
+    int i = entry(r0 + col), i_next = entry(r0 + 128 + col);
+    u32x4 next[4 * NH];
+    load_q(r0 + col, i, next);
+    take_q(next);
+    for (; r0 < end; r0 += 128) {
+        const int r = r0 + col;
+        const int i_then = entry(r + 256);
+        load_q(r + 128, i_next, next);
+        f16x8 pb[4];
+        float m, den;
+        block_weights<D>(rk, qf, f.a.c2, r0 < own_end, i - j * BT, half, pb, m, den);
+        const float inv = den > 0.0f ? 1.0f / den : den;   // (nothing but -inf: weight 0 in the sum)
+        // (rows behind the last one, and the upper lanes' copy of the logarithms, lie outside the buffers and are dropped)
+        const int count = min(32, end - r0);
+        const auto dst = buffer_of(f.part + (row0 + r0) * D, 2 * D * count);
+        store_words(buffer_of(f.meta + row0 + r0, 8 * count), half ? 0x7FFFFFF0 : 8 * col, u32x2{__float_as_uint(m + log2f(den * 0x1p-15f)), __float_as_uint(up)});
+#pragma unroll
+        for (int h = 0; h < NH; h++) {
+            f32x16 acc[2];
+#pragma unroll
+            for (int x = 0; x < 2; x++) acc[x] = f32x16{0};
+#pragma unroll
+            for (int y = 0; y < 4; y++)
+#pragma unroll
+                for (int x = 0; x < 2; x++)
+                    acc[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(transposed_half<D>(tv + y * RowTile<D>::R16 + 64 * (2 * h + x)), pb[y], acc[x], 0, 0, 0);
+#pragma unroll
+            for (int x = 0; x < 2; x++)
+#pragma unroll
+                for (int y = 0; y < 4; y += 2) {
+                    // columns 8 y .. 8 y + 7 from both halves of the wave to its lower lanes, the next 8 to its upper lanes
+                    u32x4 w;
+#pragma unroll
+                    for (int e = 0; e < 2; e++) {
+                        const f16x2v a = {(_Float16)(acc[x][4 * y + 2 * e] * inv), (_Float16)(acc[x][4 * y + 2 * e + 1] * inv)};
+                        const f16x2v c = {(_Float16)(acc[x][4 * y + 4 + 2 * e] * inv), (_Float16)(acc[x][4 * y + 5 + 2 * e] * inv)};
+                        const auto sw = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, c), false, false);
+                        w[e] = sw[0];
+                        w[2 + e] = sw[1];
+                    }
+                    *(u32x4*)(rows + col * RS + 64 * x + 16 * (y + half)) = w;
+                }
+            wave_lds_order();
+#pragma unroll
+            for (int t = 0; t < 4; t++) store_words(dst, 2 * D * (8 * t + lrow) + 128 * h + 2 * lcol, *(const u32x4*)(rows + (8 * t + lrow) * RS + 2 * lcol));
+            wave_lds_order();
+        }
+        take_q(next);   // (here and not ahead of the loop's next round: the wait for these loads leaves the stores under way)
+        i = i_next;
+        i_next = i_then;
     }
 }
 
-// 64 queries of a key/value head's group per workgroup: wave wv takes 32 of them (wv & 1) and every second head.
+// D / 8 lanes per row (query, head of the group): the weights of its slots, then the sum of the partial results.
 template <int D>
-__global__ __launch_bounds__(256, 2) void block_join_kernel(BlockFwd f)
+__global__ __launch_bounds__(256) void block_join_kernel(BlockFwd f, int rows_per_head)
 {
-    __shared__ __attribute__((aligned(16))) FwdBlockSmem<D> sm;
+    constexpr int LPR = D / 8;
     const BlockLists& l = f.a.l;
-    const int bg = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, col = lane & 31, half = lane >> 5;
-    const int qb = gridDim.x - 1 - blockIdx.x, G = l.G, b = bg / l.Hkv, g = bg % l.Hkv, qh = wv & 1;
-    const size_t kv = ((size_t)bg * l.n + (size_t)qb * BT) * D;
-    const int last = l.n - 1 - qb * BT;
-    load_rows<D>(sm.k, f.a.k + kv, last, tid);
-    load_rows<D>(sm.v, f.a.v + kv, last, tid);
-    __syncthreads();
-    const int i = qb * BT + 32 * qh + col, ic = min(i, l.n - 1);
-    const uint32_t rk = lds_address(sm.k) + row_lane<D>(lane), tv = lds_address(sm.v) + transposed_lane<D>(lane);
-    const int32_t* pos = l.pos + ((size_t)bg * l.n + ic) * l.top;
-    for (int gh = wv >> 1; gh < G; gh += 2) {
-        const size_t row = ((size_t)b * l.H + g * G + gh) * l.n + ic;
-        const uint16_t* qr = f.a.q + row * D + 8 * half;
-        bf16x8 qf[D / 16];
+    const int G = l.G, tid = threadIdx.x, t = tid % LPR, lane0 = (tid & 63) - t;
+    int bg, item;
+    deal_head(blockIdx.x, rows_per_head, f.nbg, bg, item);
+    bg += f.bg0;
+    const int q0 = f.c * l.cq, nq = min(l.cq, l.n - q0);
+    const int rr = item * (256 / LPR) + tid / LPR;
+    const int row = min(rr, nq * G - 1);          // (lanes without a row follow the last one, and store nothing)
+    const int i = q0 + row / G, gh = row % G, b = bg / l.Hkv, g = bg % l.Hkv;
+    const int32_t* pos = l.pos + ((size_t)bg * l.n + i) * l.slots;
+    const size_t rows0 = (size_t)(bg - f.bg0) * l.entries * G + gh;
+    float M = -INFINITY;
+    for (int s = t; s < l.slots; s += LPR) {
+        const int p = pos[s];
+        if (p >= 0) M = fmaxf(M, f.meta[rows0 + (size_t)p * G].x);
+    }
 #pragma unroll
-        for (int x = 0; x < D / 16; x++) qf[x] = *(const bf16x8*)(qr + 16 * x);
-        f32x16 acc[D / 32];
-        float m, den;
-        if (qh == 0) block_column<D, 1, true>(rk, tv, qf, f.a.c2, col, half, acc, m, den);
-        else block_column<D, 2, true>(rk, tv, qf, f.a.c2, 32 + col, half, acc, m, den);
-        const size_t rows0 = (size_t)bg * l.pairs * G + gh;
-        float M = m;
-        if (i < l.n && half == 0) f.own[row] = m + log2f(den);
-        for (int s = 0; s < l.top; s++) {
-            const int p = pos[s];
-            if (p >= 0) M = fmaxf(M, f.meta[rows0 + (size_t)p * G].x);
+    for (int d = 1; d < LPR; d <<= 1) M = fmaxf(M, __shfl_xor(M, d, 64));
+    const float ref = M == -INFINITY ? 0.0f : M;
+    float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0}, L = 0.0f;
+    for (int s0 = 0; s0 < l.slots; s0 += LPR) {
+        const int p = s0 + t < l.slots ? pos[s0 + t] : -1;
+        float w = 0.0f, ws = 0.0f;
+        if (p >= 0) {
+            const float2 mt = f.meta[rows0 + (size_t)p * G];
+            w = __builtin_amdgcn_exp2f(mt.x - ref);
+            ws = w * mt.y;
         }
-        const float w0 = __builtin_amdgcn_exp2f(m - M);
-        float L = den * w0;
+        L += w;
+        const int count = min(LPR, l.slots - s0);
+#pragma unroll 4
+        for (int s = 0; s < count; s++) {
+            const int ps = __shfl(p, lane0 + s, 64);
+            const float wss = __shfl(ws, lane0 + s, 64);
+            if (ps < 0) continue;
+            const f16x8 v = *(const f16x8*)(f.part + (rows0 + (size_t)ps * G) * D + 8 * t);
 #pragma unroll
-        for (int x = 0; x < D / 32; x++)
-#pragma unroll
-            for (int r = 0; r < 16; r++) acc[x][r] *= w0;
-        for (int s = 0; s < l.top; s++) {
-            const int p = pos[s];
-            if (p < 0) continue;
-            const size_t pr = rows0 + (size_t)p * G;
-            const float2 mt = f.meta[pr];
-            const float w = __builtin_amdgcn_exp2f(mt.x - M), ws = w * mt.y;
-            L += w;
-            const _Float16* src = f.part + pr * D + half * (D / 2);
-#pragma unroll
-            for (int x = 0; x < D / 32; x++)
-#pragma unroll
-                for (int y = 0; y < 2; y++) {
-                    const f16x8 v = *(const f16x8*)(src + 16 * x + 8 * y);
-#pragma unroll
-                    for (int e = 0; e < 8; e++) acc[x][8 * y + e] = fmaf(ws, (float)v[e], acc[x][8 * y + e]);
-                }
-        }
-        if (i < l.n) {
-            const float inv = 1.0f / L;
-            uint16_t* orow = f.o + row * D + 4 * half;
-#pragma unroll
-            for (int x = 0; x < D / 32; x++)
-#pragma unroll
-                for (int y = 0; y < 4; y++) {
-                    const uint2 v = make_uint2(pack_bf16x2(acc[x][4 * y] * inv, acc[x][4 * y + 1] * inv), pack_bf16x2(acc[x][4 * y + 2] * inv, acc[x][4 * y + 3] * inv));
-                    *(uint2*)(orow + 32 * x + 8 * y) = v;
-                }
-            if (half == 0) f.lse[row] = (M + log2f(L)) * 0.6931471805599453f;
+            for (int e = 0; e < 8; e++) acc[e] = fmaf(wss, (float)v[e], acc[e]);
         }
     }
+#pragma unroll
+    for (int d = 1; d < LPR; d <<= 1) L += __shfl_xor(L, d, 64);
+    if (rr >= nq * G) return;
+    const float inv = 1.0f / L;
+    const size_t at = ((size_t)b * l.H + g * G + gh) * l.n + i;
+    u32x4 out;
+#pragma unroll
+    for (int e = 0; e < 4; e++) out[e] = pack_bf16x2(acc[2 * e] * inv, acc[2 * e + 1] * inv);
+    *(u32x4*)(f.o + at * D + 8 * t) = out;
+    if (t == 0) f.lse[at] = (ref + log2f(L)) * 0.6931471805599453f;
 }
 
-// mass_j = the weights that the block's keys got from all queries and heads of the group.  A workgroup per block; the order of
-// the sum is fixed.
+// mass_j: the weights that the block's keys got from the stretch's queries and the heads of the group join what earlier stretches gave.
+// A workgroup per block; the order of the sum is fixed.
 __global__ __launch_bounds__(256) void block_mass_kernel(BlockFwd f)
 {
     __shared__ float red[4];
     const BlockLists& l = f.a.l;
-    const int j = blockIdx.x, bg = blockIdx.y, tid = threadIdx.x, G = l.G, b = bg / l.Hkv, g = bg % l.Hkv;
-    const float LOG2E = 1.4426950408889634f;
-    const size_t h0 = (size_t)b * l.H + g * G;
+    const int j = blockIdx.x, bg = f.bg0 + blockIdx.y, tid = threadIdx.x, G = l.G, b = bg / l.Hkv, g = bg % l.Hkv;
+    const size_t cbg = l.cbg(f.c, bg), h0 = (size_t)b * l.H + g * G;
+    const int rows = l.total[cbg * l.nb + j] * G, base = l.base[cbg * l.nb + j];
+    const int32_t* list = l.list + cbg * l.entries + base;
+    const float2* meta = f.meta + ((size_t)blockIdx.y * l.entries + base) * G;
     float sum = 0.0f;
-    const int own = min(BT, l.n - j * BT) * G;
-    for (int r = tid; r < own; r += 256) {
-        const size_t row = (h0 + r % G) * l.n + j * BT + r / G;
-        sum += __builtin_amdgcn_exp2f(f.own[row] - f.lse[row] * LOG2E);
-    }
-    const int rows = l.pairs ? l.total[(size_t)bg * l.nb + j] * G : 0;
-    if (rows) {
-        const int base = l.base[(size_t)bg * l.nb + j];
-        const int32_t* list = l.list + (size_t)bg * l.pairs + base;
-        const float2* meta = f.meta + ((size_t)bg * l.pairs + base) * G;
-        for (int r = tid; r < rows; r += 256) sum += __builtin_amdgcn_exp2f(meta[r].x - f.lse[(h0 + r % G) * l.n + list[r / G]] * LOG2E);
-    }
+    for (int r = tid; r < rows; r += 256) sum += __builtin_amdgcn_exp2f(meta[r].x - f.lse[(h0 + r % G) * l.n + list[r / G]] * 1.4426950408889634f);
     sum = wave_sum_f32(sum);
     if ((tid & 63) == 0) red[tid >> 6] = sum;
     __syncthreads();
-    if (tid == 0) f.mass[(size_t)bg * l.nb + j] = (red[0] + red[1]) + (red[2] + red[3]);
+    if (tid == 0) {
+        sum = (red[0] + red[1]) + (red[2] + red[3]);
+        float* m = f.mass + (size_t)bg * l.nb + j;
+        *m = j < f.c * (l.cq / BT) ? *m + sum : sum;   // (a block's first stretch is the one it lies in)
+    }
 }
 
-constexpr int FWD_UNIT = 256;   // rows that share a block's K and V in LDS
+// Queries per stretch and heads per launch: what they leave behind is at most FWD_STRETCH_BYTES of workspace.  As many queries as fit
+// come first, because all the rows that a stretch has for a block share one load of K and V.  (Stretches whose results would stay in
+// the chip's last cache, of 256 MB, do not pay: 32 heads of 32768, 16 blocks: 3.56 ms with 128 MB and 3.26 with 256 against 3.00 in one.
+// The join reads 4 to 15 % faster then, but the launches' ends cost the tiles more.)
+static int fwd_stretch(const sparsek_block_cfg& c)
+{
+    const double per_query = (double)(c.H / c.Hkv) * (c.top + 1) * c.d * 2, blocks = block_count(c.n);
+    const double stretches = std::ceil(blocks / std::max(1.0, std::floor(FWD_STRETCH_BYTES / per_query / BT)));
+    return (int)std::ceil(blocks / stretches) * BT;
+}
+static int fwd_heads(const sparsek_block_cfg& c, int cq)
+{
+    const double per_head = (double)std::min(cq, c.n) * (c.H / c.Hkv) * (c.top + 1) * c.d * 2;
+    return (int)std::max(1.0, std::min((double)c.B * c.Hkv, std::floor(FWD_STRETCH_BYTES / per_head)));
+}
+
+// Rows that share a block's K and V in LDS: more of them where that leaves three workgroups for every compute unit.
+static int fwd_unit(const sparsek_block_cfg& c)
+{
+    const double rows = (double)c.B * c.H * c.n * (c.top + 1);
+    return rows >= 768 * 512.0 ? 512 : rows >= 768 * 256.0 ? 256 : 128;
+}
 
 struct FwdLayout {
     BlockLayout y;
-    size_t part, meta, own, bytes;
+    int heads;
+    size_t part, meta, bytes;
 };
 static FwdLayout fwd_layout(const sparsek_block_cfg& c, void* ws)
 {
     FwdLayout f;
-    f.y = block_lists_layout(c, FWD_UNIT, ws);
-    const size_t rows = (size_t)c.B * c.Hkv * f.y.l.pairs * f.y.l.G;
+    const int cq = fwd_stretch(c);
+    f.y = block_lists_layout(c, cq, fwd_unit(c), ws);
+    f.heads = fwd_heads(c, cq);
+    const size_t rows = (size_t)f.heads * f.y.l.entries * f.y.l.G;
     f.part = f.y.bytes;
     f.meta = align_up(f.part + rows * c.d * 2, 256);
-    f.own = align_up(f.meta + rows * 8, 256);
-    f.bytes = align_up(f.own + (size_t)c.B * c.H * c.n * 4, 256);
+    f.bytes = align_up(f.meta + rows * 8, 256);
     return f;
 }
 
@@ -378,20 +488,26 @@ int launch_block_fwd(const sparsek_block_cfg& c, const void* q, const void* k, c
     f.a.scale = c.softmax_scale;
     f.a.c2 = c.softmax_scale * 1.4426950408889634f;
     f.o = (uint16_t*)o; f.lse = lse; f.mass = mass;
-    f.part = (_Float16*)((char*)ws + y.part); f.meta = (float2*)((char*)ws + y.meta); f.own = (float*)((char*)ws + y.own);
+    f.part = (_Float16*)((char*)ws + y.part); f.meta = (float2*)((char*)ws + y.meta);
     const BlockLists& l = f.a.l;
     const int BG = c.B * c.Hkv;
     if (int rc = launch_block_lists(l, idx, st)) return rc;
-#define FWD(D)                                                                                                \
-    if (l.maxu) hipLaunchKernelGGL((block_tiles_kernel<D>), dim3(l.maxu, BG), dim3(256), 0, st, f);           \
-    hipLaunchKernelGGL((block_join_kernel<D>), dim3(l.nb, BG), dim3(256), 0, st, f)
-    if (c.d == 128) {
-        FWD(128);
-    } else {
-        FWD(64);
-    }
+    for (f.bg0 = 0; f.bg0 < BG; f.bg0 += y.heads)
+        for (f.c = 0; f.c < l.nc; f.c++) {
+            f.nbg = std::min(y.heads, BG - f.bg0);
+            const int nq = std::min(l.cq, c.n - f.c * l.cq), seen = std::min(l.nb, (f.c + 1) * (l.cq / BT));
+            const int items = (int)(((long long)nq * l.G * (c.d / 8) + 255) / 256);
+#define FWD(D)                                                                                                   \
+    hipLaunchKernelGGL((block_tiles_kernel<D>), dim3((unsigned)l.maxu * f.nbg), dim3(256), 0, st, f);            \
+    hipLaunchKernelGGL((block_join_kernel<D>), dim3((unsigned)items * f.nbg), dim3(256), 0, st, f, items)
+            if (c.d == 128) {
+                FWD(128);
+            } else {
+                FWD(64);
+            }
 #undef FWD
-    if (mass) hipLaunchKernelGGL(block_mass_kernel, dim3(l.nb, BG), dim3(256), 0, st, f);
+            if (mass) hipLaunchKernelGGL(block_mass_kernel, dim3(seen, f.nbg), dim3(256), 0, st, f);
+        }
     return launch_status();
 }
 

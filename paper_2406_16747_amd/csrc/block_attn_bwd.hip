@@ -2,10 +2,10 @@
 // ds_ij = p_ij (dO_i.v_j - delta_i) scale:  dq_i = sum_j ds_ij k_j,  dk_j = sum_i ds_ij q_i,  dv_j = sum_i p_ij dO_i.
 //
 // By key block, like the forward (see block_attn.hip).  block_bwd_tiles_kernel holds a block's K and V in LDS and walks the
-// rows that selected it, 64 at a time: S = Q.K^T and dP = dO.V^T with a lane per key, so that P and dS are the operands of
-// dV^T += dO^T.P and dK^T += Q^T.dS as they stand (sums stay in registers for a whole unit of rows, then go out once); dS
-// passes through LDS for dQ^T = K^T.dS^T, whose partial results go out in list order.  block_bwd_join_kernel does the
-// queries' own block in the same way, and adds the partial results of dq, dk and dv to it.
+// rows that attend it, 64 at a time: S = Q.K^T and dP = dO.V^T with a lane per key, so that P and dS are the operands of
+// dV^T += dO^T.P and dK^T += Q^T.dS as they stand (sums stay in registers for a whole unit of rows); dS passes through LDS for
+// dQ^T = K^T.dS^T, whose partial results go out in list order.  A block whose rows are one unit is finished there; the sums of
+// the others go out and block_kv_join_kernel adds them up.  block_dq_join_kernel adds up the partial dq of every row.
 #include "block_parts.hpp"
 
 namespace spk {
@@ -14,9 +14,9 @@ struct BlockBwd {
     BlockArgs a;
     uint16_t *dq, *dk, *dv;
     float2* rows;       // [B,H,n]: lse * log2(e), dO.o
-    _Float16* part;     // partial dq: [entry rows][half of D][lane / 32][D / 4]
+    _Float16* part;     // partial dq: [B,Hkv][entry rows][D]
     float2* meta;       // what the halves of each half of D stand for
-    float* kvpart;      // [units][2 halves of the keys][dV, dK][D / 32][4][64 lanes][4]
+    float* kvpart;      // [B,Hkv][units][2 halves of the keys][dV, dK][D / 32][4][64 lanes][4]
 };
 
 // dO.o and the logarithm of the denominator, a wave per 64 / (D / 8) rows.
@@ -45,6 +45,7 @@ struct BwdBlockSmem {
     unsigned char k[RowTile<D>::BYTES], v[RowTile<D>::BYTES], q[RowTile<D>::BYTES], g[RowTile<D>::BYTES];   // g: dO
     unsigned char ds[RowTile<64>::BYTES];   // [key][row]
     float lse2[BT], delta[BT];
+    int limit[BT];                          // keys 0 .. limit are attended
     long long at[BT];                       // the row's place in [B,H,n], -1: none
 };
 static_assert(sizeof(BwdBlockSmem<128>) <= 80 * 1024, "two workgroups per CU");
@@ -70,8 +71,8 @@ __device__ __forceinline__ void load_query_rows(BwdBlockSmem<D>& sm, const uint1
 
 // 64 rows against 64 keys.  Wave (kb = wv & 1, rb = wv >> 1): keys 32 kb .. and rows 32 rb .. of S and dP; its share of dV^T and
 // dK^T (those keys, those rows) joins acc_v, acc_k; then dQ^T of rows 32 rb .. and the D/2 columns of half kb, into acc_q.
-template <int D, bool CAUSAL>
-__device__ __forceinline__ void bwd_block_tile(BwdBlockSmem<D>& sm, int lane, int wv, float c2, float scale, f32x16 (&acc_v)[D / 32],
+template <int D>
+__device__ __forceinline__ void bwd_block_tile(BwdBlockSmem<D>& sm, int lane, int wv, bool own, float c2, float scale, f32x16 (&acc_v)[D / 32],
                                                f32x16 (&acc_k)[D / 32], f32x16 (&acc_q)[D / 64])
 {
     using S = RowTile<D>;
@@ -85,6 +86,14 @@ __device__ __forceinline__ void bwd_block_tile(BwdBlockSmem<D>& sm, int lane, in
         s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_operand(rq + 32 * x), row_operand(rk + 32 * x), s, 0, 0, 0);
         dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_operand(rg + 32 * x), row_operand(rv + 32 * x), dp, 0, 0, 0);
     }
+    if (own)   // (some of the rows are the block's own queries)
+#pragma unroll
+        for (int g4 = 0; g4 < 4; g4++) {
+            const int4 L4 = *(const int4*)&sm.limit[32 * rb + 8 * g4 + 4 * half];
+            const int ll[4] = {L4.x, L4.y, L4.z, L4.w};
+#pragma unroll
+            for (int e = 0; e < 4; e++) s[4 * g4 + e] = 32 * kb + col > ll[e] ? -INFINITY : s[4 * g4 + e];
+        }
     bf16x8 pb[2], db[2];   // as operands: 2^-9 of every weight and every score gradient
 #pragma unroll
     for (int g4 = 0; g4 < 4; g4++) {
@@ -95,10 +104,8 @@ __device__ __forceinline__ void bwd_block_tile(BwdBlockSmem<D>& sm, int lane, in
 #pragma unroll
         for (int e = 0; e < 4; e++) {
             const int r = 4 * g4 + e;
-            float p = __builtin_amdgcn_exp2f(fmaf(s[r], c2, -ll[e]));
-            if (CAUSAL && 32 * kb + col > r0 + e) p = 0.0f;
+            const float p = __builtin_amdgcn_exp2f(fmaf(s[r], c2, -ll[e]));
             ds[e] = p * (dp[r] - dd[e]);
-            if (CAUSAL && 32 * kb + col > r0 + e) ds[e] = 0.0f;
             pb[r >> 3][r & 7] = (__bf16)p;
             db[r >> 3][r & 7] = (__bf16)ds[e];
         }
@@ -158,24 +165,42 @@ __device__ __forceinline__ void add_row_halves(BwdBlockSmem<D>& sm, int lane, in
 }
 static_assert(2 * 2 * 4 * 4 * 64 * 16 <= sizeof(BwdBlockSmem<128>) && 2 * 2 * 2 * 4 * 64 * 16 <= sizeof(BwdBlockSmem<64>), "room for the sums");
 
+// dV and dK of 32 keys, as the lanes of waves 0 and 1 hold them, to their rows.
+template <int D>
+__device__ __forceinline__ void store_kv(const BlockBwd& f, size_t kv, int key, int last, int half, const f32x16 (&acc_v)[D / 32], const f32x16 (&acc_k)[D / 32])
+{
+    if (key > last) return;
+    uint16_t *ok = f.dk + kv + (size_t)key * D + 4 * half, *ov = f.dv + kv + (size_t)key * D + 4 * half;
+    const float c = f.a.scale;
+#pragma unroll
+    for (int x = 0; x < D / 32; x++)
+#pragma unroll
+        for (int y = 0; y < 4; y++) {
+            *(uint2*)(ov + 32 * x + 8 * y) = make_uint2(pack_bf16x2(acc_v[x][4 * y], acc_v[x][4 * y + 1]), pack_bf16x2(acc_v[x][4 * y + 2], acc_v[x][4 * y + 3]));
+            *(uint2*)(ok + 32 * x + 8 * y) = make_uint2(pack_bf16x2(acc_k[x][4 * y] * c, acc_k[x][4 * y + 1] * c), pack_bf16x2(acc_k[x][4 * y + 2] * c, acc_k[x][4 * y + 3] * c));
+        }
+}
+
 template <int D>
 __global__ __launch_bounds__(256, 2) void block_bwd_tiles_kernel(BlockBwd f)
 {
     __shared__ __attribute__((aligned(16))) BwdBlockSmem<D> sm;
     constexpr int DB = D / 32;
     const BlockLists& l = f.a.l;
-    const int bg = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, col = lane & 31, half = lane >> 5;
-    if ((int)blockIdx.x >= l.nunits[bg]) return;
-    const size_t un = (size_t)bg * l.maxu + blockIdx.x;
-    const int2 u = l.units[un];
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, col = lane & 31, half = lane >> 5;
+    int bg, un;
+    deal_head(blockIdx.x, l.maxu, l.B * l.Hkv, bg, un);
+    if (un >= l.nunits[bg]) return;
+    const int2 u = l.units[(size_t)bg * l.maxu + un];
     const int j = u.x, first = u.y, G = l.G, b = bg / l.Hkv, g = bg % l.Hkv;
-    const int base = l.base[(size_t)bg * l.nb + j];
-    const int end = min(l.total[(size_t)bg * l.nb + j] * G, first + l.unit);
+    const int base = l.base[(size_t)bg * l.nb + j], rows = l.total[(size_t)bg * l.nb + j] * G, end = min(rows, first + l.unit);
     const size_t kv = ((size_t)bg * l.n + (size_t)j * BT) * D;
-    load_rows<D>(sm.k, f.a.k + kv, BT - 1, tid);
-    load_rows<D>(sm.v, f.a.v + kv, BT - 1, tid);
-    const int32_t* list = l.list + (size_t)bg * l.pairs + base;
-    const size_t row0 = ((size_t)bg * l.pairs + base) * G;
+    const int last = l.n - 1 - j * BT;
+    load_rows<D>(sm.k, f.a.k + kv, last, tid);
+    load_rows<D>(sm.v, f.a.v + kv, last, tid);
+    const int32_t* list = l.list + (size_t)bg * l.entries + base;
+    const size_t row0 = ((size_t)bg * l.entries + base) * G;
+    const int own_end = min(BT, last + 1) * G;
     f32x16 acc_v[DB], acc_k[DB], acc_q[DB / 2];
 #pragma unroll
     for (int x = 0; x < DB; x++) acc_v[x] = acc_k[x] = f32x16{0};
@@ -184,21 +209,25 @@ __global__ __launch_bounds__(256, 2) void block_bwd_tiles_kernel(BlockBwd f)
         if (tid < BT) {
             const int r = r0 + tid;
             long long at = -1;
+            int limit = BT - 1;
             float2 m = make_float2(INFINITY, 0.0f);   // p = 0
             if (r < end) {
-                at = ((long long)b * l.H + g * G + r % G) * l.n + list[r / G];
+                const int i = list[r / G];
+                at = ((long long)b * l.H + g * G + r % G) * l.n + i;
+                limit = min(limit, i - j * BT);
                 m = f.rows[at];
             }
             sm.at[tid] = at;
+            sm.limit[tid] = limit;
             sm.lse2[tid] = m.x;
             sm.delta[tid] = m.y;
         }
         __syncthreads();
         load_query_rows<D>(sm, f.a.q, f.a.dO, tid);
         __syncthreads();
-        bwd_block_tile<D, false>(sm, lane, wv, f.a.c2, f.a.scale, acc_v, acc_k, acc_q);
-        // the partial dq of rows 32 rb + col, columns of half kb
-        const int kb = wv & 1, r = r0 + 32 * (wv >> 1) + col;
+        bwd_block_tile<D>(sm, lane, wv, r0 < own_end, f.a.c2, f.a.scale, acc_v, acc_k, acc_q);
+        // the partial dq of rows 32 rb + col, columns of half kb, relative to the largest of them
+        const int kb = wv & 1, rt = 32 * (wv >> 1) + col, r = r0 + rt;
         float top = 0.0f;
 #pragma unroll
         for (int x = 0; x < DB / 2; x++)
@@ -206,124 +235,109 @@ __global__ __launch_bounds__(256, 2) void block_bwd_tiles_kernel(BlockBwd f)
             for (int e = 0; e < 16; e++) top = fmaxf(top, fabsf(acc_q[x][e]));
         const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
         const int E = scale_exp(max((unsigned)sw[0], (unsigned)sw[1]));
-        const float down = __uint_as_float((unsigned)(254 - E) << 23), up = __uint_as_float((unsigned)E << 23);
-        if (r < end) {
-            _Float16* pr = f.part + (row0 + r) * D + kb * (D / 2) + half * (D / 4);
+        const float down = scale_down(E);
+        if (r < end && half == 0) ((float*)(f.meta + row0 + r))[kb] = scale_up(E);
+        __syncthreads();   // (the rows of q are not needed any more)
 #pragma unroll
-            for (int x = 0; x < DB / 2; x++)
-#pragma unroll
-                for (int y = 0; y < 2; y++) {
-                    f16x8 v;
-#pragma unroll
-                    for (int e = 0; e < 8; e++) v[e] = (_Float16)(acc_q[x][8 * y + e] * down);
-                    *(f16x8*)(pr + 16 * x + 8 * y) = v;
-                }
-            if (half == 0) ((float*)(f.meta + row0 + r))[kb] = up;
-        }
-    }
-    add_row_halves<D>(sm, lane, wv, acc_v, acc_k);
-    if (wv < 2) {
-        float4* out = (float4*)f.kvpart + (un * 2 + wv) * (2 * DB * 4 * 64);
-#pragma unroll
-        for (int x = 0; x < DB; x++)
+        for (int x = 0; x < DB / 2; x++)
 #pragma unroll
             for (int y = 0; y < 4; y++) {
-                out[(x * 4 + y) * 64 + lane] = make_float4(acc_v[x][4 * y], acc_v[x][4 * y + 1], acc_v[x][4 * y + 2], acc_v[x][4 * y + 3]);
-                out[((DB + x) * 4 + y) * 64 + lane] = make_float4(acc_k[x][4 * y], acc_k[x][4 * y + 1], acc_k[x][4 * y + 2], acc_k[x][4 * y + 3]);
+                f16x4 v;
+#pragma unroll
+                for (int e = 0; e < 4; e++) v[e] = (_Float16)(acc_q[x][4 * y + e] * down);
+                *(f16x4*)(sm.q + rt * (2 * D + 16) + D * kb + 64 * x + 16 * y + 8 * half) = v;
             }
-    }
-}
-
-// The own block of 64 queries, every head of the group in turn, and the sums with the partial results.
-template <int D>
-__global__ __launch_bounds__(256, 2) void block_bwd_join_kernel(BlockBwd f)
-{
-    __shared__ __attribute__((aligned(16))) BwdBlockSmem<D> sm;
-    constexpr int DB = D / 32;
-    const BlockLists& l = f.a.l;
-    const int bg = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, col = lane & 31, half = lane >> 5;
-    const int qb = blockIdx.x, G = l.G, b = bg / l.Hkv, g = bg % l.Hkv, kb = wv & 1;
-    const size_t kv = ((size_t)bg * l.n + (size_t)qb * BT) * D;
-    const int last = l.n - 1 - qb * BT;
-    load_rows<D>(sm.k, f.a.k + kv, last, tid);
-    load_rows<D>(sm.v, f.a.v + kv, last, tid);
-    const int i = qb * BT + 32 * (wv >> 1) + col;
-    const int32_t* pos = l.pos + ((size_t)bg * l.n + min(i, l.n - 1)) * l.top;
-    f32x16 acc_v[DB], acc_k[DB], acc_q[DB / 2];
-#pragma unroll
-    for (int x = 0; x < DB; x++) acc_v[x] = acc_k[x] = f32x16{0};
-    for (int gh = 0; gh < G; gh++) {
-        const long long head = ((long long)b * l.H + g * G + gh) * l.n;
         __syncthreads();
-        if (tid < BT) {
-            const int y = qb * BT + tid;
-            float2 m = make_float2(INFINITY, 0.0f);
-            if (y < l.n) m = f.rows[head + y];
-            sm.at[tid] = y < l.n ? head + y : -1;
-            sm.lse2[tid] = m.x;
-            sm.delta[tid] = m.y;
-        }
-        __syncthreads();
-        load_query_rows<D>(sm, f.a.q, f.a.dO, tid);
-        __syncthreads();
-        bwd_block_tile<D, true>(sm, lane, wv, f.a.c2, f.a.scale, acc_v, acc_k, acc_q);
-        if (i < l.n) {
-            for (int s = 0; s < l.top; s++) {
-                const int p = pos[s];
-                if (p < 0) continue;
-                const size_t pr = (size_t)bg * l.pairs * G + (size_t)p * G + gh;
-                const float up = ((const float*)(f.meta + pr))[kb];
-                const _Float16* src = f.part + pr * D + kb * (D / 2) + half * (D / 4);
+        unsigned char* dst = (unsigned char*)(f.part + (row0 + r0) * D);
+        const int bytes = min(BT, end - r0) * 2 * D;
 #pragma unroll
-                for (int x = 0; x < DB / 2; x++)
-#pragma unroll
-                    for (int y = 0; y < 2; y++) {
-                        const f16x8 v = *(const f16x8*)(src + 16 * x + 8 * y);
-#pragma unroll
-                        for (int e = 0; e < 8; e++) acc_q[x][8 * y + e] = fmaf(up, (float)v[e], acc_q[x][8 * y + e]);
-                    }
-            }
-            uint16_t* out = f.dq + (head + i) * D + kb * (D / 2) + 4 * half;
-#pragma unroll
-            for (int x = 0; x < DB / 2; x++)
-#pragma unroll
-                for (int y = 0; y < 4; y++)
-                    *(uint2*)(out + 32 * x + 8 * y) = make_uint2(pack_bf16x2(acc_q[x][4 * y], acc_q[x][4 * y + 1]), pack_bf16x2(acc_q[x][4 * y + 2], acc_q[x][4 * y + 3]));
+        for (int t = 0; t < BT * (D / 8) / 256; t++) {
+            const int id = tid + 256 * t;
+            const u32x4 v = *(const u32x4*)(sm.q + id / (D / 8) * (2 * D + 16) + 16 * (id % (D / 8)));
+            if (16 * id < bytes) *(u32x4*)(dst + 16 * id) = v;
         }
     }
     add_row_halves<D>(sm, lane, wv, acc_v, acc_k);
-    if (wv < 2) {
-        // the block's units follow one another
-        const int rows = l.pairs ? l.total[(size_t)bg * l.nb + qb] * G : 0;
-        const int units = (int)(((long long)rows + l.unit - 1) / l.unit);
-        const int u0 = units ? l.first_unit[(size_t)bg * l.nb + qb] : 0;
-        for (int u = 0; u < units; u++) {
-            const float4* in = (const float4*)f.kvpart + (((size_t)bg * l.maxu + u0 + u) * 2 + wv) * (2 * DB * 4 * 64);
-#pragma unroll
-            for (int x = 0; x < DB; x++)
-#pragma unroll
-                for (int y = 0; y < 4; y++) {
-                    const float4 v = in[(x * 4 + y) * 64 + lane], w = in[((DB + x) * 4 + y) * 64 + lane];
-                    acc_v[x][4 * y] += v.x; acc_v[x][4 * y + 1] += v.y; acc_v[x][4 * y + 2] += v.z; acc_v[x][4 * y + 3] += v.w;
-                    acc_k[x][4 * y] += w.x; acc_k[x][4 * y + 1] += w.y; acc_k[x][4 * y + 2] += w.z; acc_k[x][4 * y + 3] += w.w;
-                }
-        }
-        const int key = 32 * wv + col;
-        if (key <= last) {
-            uint16_t *ok = f.dk + kv + (size_t)key * D + 4 * half, *ov = f.dv + kv + (size_t)key * D + 4 * half;
-            const float c = f.a.scale;
-#pragma unroll
-            for (int x = 0; x < DB; x++)
-#pragma unroll
-                for (int y = 0; y < 4; y++) {
-                    *(uint2*)(ov + 32 * x + 8 * y) = make_uint2(pack_bf16x2(acc_v[x][4 * y], acc_v[x][4 * y + 1]), pack_bf16x2(acc_v[x][4 * y + 2], acc_v[x][4 * y + 3]));
-                    *(uint2*)(ok + 32 * x + 8 * y) = make_uint2(pack_bf16x2(acc_k[x][4 * y] * c, acc_k[x][4 * y + 1] * c), pack_bf16x2(acc_k[x][4 * y + 2] * c, acc_k[x][4 * y + 3] * c));
-                }
-        }
+    if (wv >= 2) return;
+    if (rows <= l.unit) {
+        store_kv<D>(f, kv, 32 * wv + col, last, half, acc_v, acc_k);
+        return;
     }
+    float4* out = (float4*)f.kvpart + (((size_t)bg * l.maxu + un) * 2 + wv) * (2 * DB * 4 * 64);
+#pragma unroll
+    for (int x = 0; x < DB; x++)
+#pragma unroll
+        for (int y = 0; y < 4; y++) {
+            out[(x * 4 + y) * 64 + lane] = make_float4(acc_v[x][4 * y], acc_v[x][4 * y + 1], acc_v[x][4 * y + 2], acc_v[x][4 * y + 3]);
+            out[((DB + x) * 4 + y) * 64 + lane] = make_float4(acc_k[x][4 * y], acc_k[x][4 * y + 1], acc_k[x][4 * y + 2], acc_k[x][4 * y + 3]);
+        }
 }
 
-constexpr int BWD_UNIT = 512;   // rows whose dK and dV are summed in registers
+// dK and dV of the blocks with several units: a workgroup per (block and 32 of its columns, batch and head), its first two waves dV and its last two
+// dK, of 32 keys each.
+template <int D>
+__global__ __launch_bounds__(256) void block_kv_join_kernel(BlockBwd f)
+{
+    constexpr int DB = D / 32;
+    const BlockLists& l = f.a.l;
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, j = blockIdx.x / DB, x = blockIdx.x % DB, bg = blockIdx.y;
+    const int rows = l.total[(size_t)bg * l.nb + j] * l.G;
+    if (rows <= l.unit) return;
+    const int units = (int)(((long long)rows + l.unit - 1) / l.unit), u0 = l.first_unit[(size_t)bg * l.nb + j];
+    const float4* in = (const float4*)f.kvpart + (((size_t)bg * l.maxu + u0) * 2 + (wv & 1)) * (2 * DB * 4 * 64) + (((wv >> 1) * DB + x) * 4) * 64 + lane;
+    float4 s[4];
+#pragma unroll
+    for (int y = 0; y < 4; y++) s[y] = make_float4(0, 0, 0, 0);
+#pragma unroll 4
+    for (int u = 0; u < units; u++)
+#pragma unroll
+        for (int y = 0; y < 4; y++) {
+            const float4 v = in[(size_t)u * (4 * DB * 4 * 64) + y * 64];
+            s[y].x += v.x; s[y].y += v.y; s[y].z += v.z; s[y].w += v.w;
+        }
+    const int key = 32 * (wv & 1) + (lane & 31);
+    if (j * BT + key >= l.n) return;
+    const float c = wv >> 1 ? f.a.scale : 1.0f;
+    uint16_t* out = (wv >> 1 ? f.dk : f.dv) + ((size_t)bg * l.n + (size_t)j * BT + key) * D + 32 * x + 4 * (lane >> 5);
+#pragma unroll
+    for (int y = 0; y < 4; y++) *(uint2*)(out + 8 * y) = make_uint2(pack_bf16x2(s[y].x * c, s[y].y * c), pack_bf16x2(s[y].z * c, s[y].w * c));
+}
+
+// D / 8 lanes per row (query, head of the group).
+template <int D>
+__global__ __launch_bounds__(256) void block_dq_join_kernel(BlockBwd f, int items)
+{
+    constexpr int LPR = D / 8;
+    const BlockLists& l = f.a.l;
+    const int G = l.G, tid = threadIdx.x, t = tid % LPR, lane0 = (tid & 63) - t;
+    int bg, item;
+    deal_head(blockIdx.x, items, l.B * l.Hkv, bg, item);
+    const int rr = item * (256 / LPR) + tid / LPR, row = min(rr, l.n * G - 1);
+    const int i = row / G, gh = row % G, b = bg / l.Hkv, g = bg % l.Hkv;
+    const int32_t* pos = l.pos + ((size_t)bg * l.n + i) * l.slots;
+    const size_t rows0 = (size_t)bg * l.entries * G + gh;
+    float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (int s0 = 0; s0 < l.slots; s0 += LPR) {
+        const int p = s0 + t < l.slots ? pos[s0 + t] : -1, count = min(LPR, l.slots - s0);
+#pragma unroll 4
+        for (int s = 0; s < count; s++) {
+            const int ps = __shfl(p, lane0 + s, 64);
+            if (ps < 0) continue;
+            const size_t pr = rows0 + (size_t)ps * G;
+            const float up = ((const float*)(f.meta + pr))[2 * t / LPR];
+            const f16x8 v = *(const f16x8*)(f.part + pr * D + 8 * t);
+#pragma unroll
+            for (int e = 0; e < 8; e++) acc[e] = fmaf(up, (float)v[e], acc[e]);
+        }
+    }
+    if (rr >= l.n * G) return;
+    u32x4 out;
+#pragma unroll
+    for (int e = 0; e < 4; e++) out[e] = pack_bf16x2(acc[2 * e], acc[2 * e + 1]);
+    *(u32x4*)(f.dq + (((size_t)b * l.H + g * G + gh) * l.n + i) * D + 8 * t) = out;
+}
+
+constexpr int BWD_UNIT = 1024;   // rows whose dK and dV are summed in registers
 
 struct BwdLayout {
     BlockLayout y;
@@ -332,8 +346,8 @@ struct BwdLayout {
 static BwdLayout bwd_layout(const sparsek_block_cfg& c, void* ws)
 {
     BwdLayout f;
-    f.y = block_lists_layout(c, BWD_UNIT, ws);
-    const size_t BG = (size_t)c.B * c.Hkv, rows = BG * f.y.l.pairs * f.y.l.G;
+    f.y = block_lists_layout(c, block_count(c.n) * BT, BWD_UNIT, ws);
+    const size_t BG = (size_t)c.B * c.Hkv, rows = BG * f.y.l.entries * f.y.l.G;
     f.rows = f.y.bytes;
     f.part = align_up(f.rows + (size_t)c.B * c.H * c.n * 8, 256);
     f.meta = align_up(f.part + rows * c.d * 2, 256);
@@ -363,8 +377,10 @@ int launch_block_bwd(const sparsek_block_cfg& c, const void* q, const void* k, c
     const size_t nrows = (size_t)c.B * c.H * c.n;
 #define BWD(D)                                                                                                                                   \
     hipLaunchKernelGGL((block_delta_kernel<D>), dim3((unsigned)((nrows * (D / 8) + 255) / 256)), dim3(256), 0, st, f, nrows);                     \
-    if (l.maxu) hipLaunchKernelGGL((block_bwd_tiles_kernel<D>), dim3(l.maxu, BG), dim3(256), 0, st, f);                                          \
-    hipLaunchKernelGGL((block_bwd_join_kernel<D>), dim3(l.nb, BG), dim3(256), 0, st, f)
+    hipLaunchKernelGGL((block_bwd_tiles_kernel<D>), dim3((unsigned)l.maxu * BG), dim3(256), 0, st, f);                                           \
+    hipLaunchKernelGGL((block_kv_join_kernel<D>), dim3(l.nb * (D / 32), BG), dim3(256), 0, st, f);                                               \
+    const int items = (int)(((long long)c.n * l.G * (D / 8) + 255) / 256);                                                                       \
+    hipLaunchKernelGGL((block_dq_join_kernel<D>), dim3((unsigned)items * BG), dim3(256), 0, st, f, items)
     if (c.d == 128) {
         BWD(128);
     } else {

@@ -12,28 +12,26 @@ constexpr float TINY_MAX = 0x1p-100f;
 
 inline int block_count(int n) { return (n + BT - 1) / BT; }
 
-// Selected (query, block) pairs of one key/value head at most: query i has i / 64 blocks behind it.
-inline long long block_pairs(int n, int top)
-{
-    const long long nb = n / BT, rest = n % BT, full = std::min<long long>(nb, top);   // blocks 0 .. full-1 have fewer than top behind them
-    return BT * (full * (full - 1) / 2 + (nb - full) * top) + rest * std::min<long long>(nb, top);
-}
-
-// The lists that the attention kernels walk: for every key block the queries that selected it, ascending.  Everything per
-// (batch, key/value head); rows are (list entry, query head of the group), entry-major.
-//   masks[chunk][block]  which of the chunk's 64 queries selected the block
-//   off[chunk][block]    list entries of the block that come from earlier chunks
-//   total, base[block]   length and start of the block's list
-//   list[entry]          the query;  pos[query][slot]: the entry of the query's slot, -1 where the slot is empty
-//   units[]              (block, first row) of every piece of at most `unit` rows, block by block; nunits; first_unit[block]
+// The lists that the attention kernels walk: for every key block the queries that attend it -- its own ones first, then those that
+// selected it, ascending.  They are made for stretches of `cq` queries (a multiple of 64): what a stretch's queries leave behind per
+// block is joined before the next one's, in the same memory.  Everything per (batch, key/value head); rows are (list entry, query head
+// of the group), entry-major.  Stretch c, block j:
+//   counts[chunk][block]   how many of the chunk's 64 queries selected the block
+//   off[chunk][block]      list entries of the block that come from earlier chunks of the stretch
+//   total, base[c][block]  length and start of the block's list
+//   list[c][entry]         the query;  pos[query][slot]: the entry of the query's own block (slot 0) and of its selected ones, -1: none
+//   units[c][]             (block, first row) of every piece of at most `unit` rows, block by block; nunits[c]; first_unit[c][block]
 // A counting sort whose result depends on nothing but idx.
 struct BlockLists {
-    unsigned long long* masks;
+    uint8_t* counts;
     int32_t *off, *total, *base, *first_unit, *list, *pos, *nunits;
     int2* units;
     int B, H, Hkv, G, n, nb, top;
-    int unit, maxu;          // rows per unit, units at most
-    long long pairs;
+    int cq, nc, unit, maxu;  // queries per stretch, stretches, rows per unit, units of a stretch at most
+    int slots;               // top + 1
+    size_t entries;          // of a stretch at most
+
+    __host__ __device__ size_t cbg(int c, int bg) const { return (size_t)c * B * Hkv + bg; }
 };
 
 struct BlockLayout {
@@ -41,7 +39,7 @@ struct BlockLayout {
     size_t bytes;
 };
 // Carves the lists out of ws (null: sizes only).
-inline BlockLayout block_lists_layout(const sparsek_block_cfg& c, int unit, void* ws)
+inline BlockLayout block_lists_layout(const sparsek_block_cfg& c, int cq, int unit, void* ws)
 {
     BlockLayout y;
     BlockLists& l = y.l;
@@ -52,19 +50,22 @@ inline BlockLayout block_lists_layout(const sparsek_block_cfg& c, int unit, void
         return (void*)p;
     };
     l.B = c.B; l.H = c.H; l.Hkv = c.Hkv; l.G = c.H / c.Hkv; l.n = c.n; l.nb = block_count(c.n); l.top = c.top;
+    l.cq = cq;
+    l.nc = (c.n + cq - 1) / cq;
     l.unit = unit;
-    l.pairs = block_pairs(c.n, c.top);
-    l.maxu = (int)(l.pairs * l.G / unit + (l.pairs ? l.nb : 0));
-    const size_t BG = (size_t)c.B * c.Hkv, nb = l.nb;
-    l.masks = (unsigned long long*)take(BG * nb * nb * 8);
+    l.slots = c.top + 1;
+    l.entries = (size_t)std::min(cq, c.n) * l.slots;
+    l.maxu = (int)(l.entries * l.G / unit + std::min<size_t>(l.nb, l.entries));
+    const size_t BG = (size_t)c.B * c.Hkv, nb = l.nb, S = BG * l.nc;
+    l.counts = (uint8_t*)take(BG * nb * nb);
     l.off = (int32_t*)take(BG * nb * nb * 4);
-    l.total = (int32_t*)take(BG * nb * 4);
-    l.base = (int32_t*)take(BG * nb * 4);
-    l.first_unit = (int32_t*)take(BG * nb * 4);
-    l.list = (int32_t*)take(BG * l.pairs * 4);
-    l.pos = (int32_t*)take(BG * c.n * c.top * 4);
-    l.nunits = (int32_t*)take(BG * 4);
-    l.units = (int2*)take(BG * l.maxu * 8);
+    l.total = (int32_t*)take(S * nb * 4);
+    l.base = (int32_t*)take(S * nb * 4);
+    l.first_unit = (int32_t*)take(S * nb * 4);
+    l.list = (int32_t*)take(S * l.entries * 4);
+    l.pos = (int32_t*)take(BG * c.n * l.slots * 4);
+    l.nunits = (int32_t*)take(S * 4);
+    l.units = (int2*)take(S * l.maxu * 8);
     y.bytes = at;
     return y;
 }
@@ -108,11 +109,50 @@ __device__ __forceinline__ unsigned pack4(int a, int b, int c, int d)
     return (a & 255) | (b & 255) << 8 | (c & 255) << 16 | (unsigned)d << 24;
 }
 
-// fp16 holds a partial result relative to the largest value of its block: h = x * 2^(127 - E) with E the biased exponent
-// of that value, so |h| < 4, and 2^-12 relative is lost where bf16 would lose 2^-9.
-__device__ __forceinline__ int scale_exp(unsigned top_bits) { return min(max((int)(top_bits >> 23) & 255, 1), 253); }
+// fp16 holds values relative to the largest of their block, with biased exponent E: x * 2^(140 - E), so that the largest lies in
+// [2^13, 2^14) and only what is below 2^-27 of it loses bits that fp16's normal numbers have: 2^-11 relative, where bf16 has 2^-8.
+__device__ __forceinline__ int scale_exp(unsigned top_bits) { return min(max((int)(top_bits >> 23) & 255, 14), 253); }
+__device__ __forceinline__ float scale_down(int E) { return __uint_as_float((unsigned)(267 - E) << 23); }   // 2^(140 - E)
+__device__ __forceinline__ float scale_up(int E) { return __uint_as_float((unsigned)(E - 13) << 23); }      // 2^(E - 140)
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x2v __attribute__((ext_vector_type(2)));
+
+// Orders a wave's own LDS accesses across its lanes (the hardware keeps a wave's LDS operations in order).
+__device__ __forceinline__ void wave_lds_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// Stores through a buffer of `bytes` bytes at p (both the same for the whole wave): what lies outside is dropped.  A condition on the
+// store itself is a branch around it, behind which the compiler waits for everything that the wave has under way.
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef __amdgpu_buffer_rsrc_t buffer_t;
+__device__ __forceinline__ buffer_t buffer_of(const void* p, int bytes)
+{
+    const uint64_t at = (uint64_t)p;
+    void* base = (void*)((uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(at >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)at));
+    return __builtin_amdgcn_make_buffer_rsrc(base, 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+}
+__device__ __forceinline__ void store_words(buffer_t b, int offset, u32x4 v) { __builtin_amdgcn_raw_buffer_store_b128(v, b, offset, 0, 0); }
+__device__ __forceinline__ void store_words(buffer_t b, int offset, u32x2 v) { __builtin_amdgcn_raw_buffer_store_b64(v, b, offset, 0, 0); }
+
+// Workgroup id -> (batch and head, item): workgroups go to the chip's 8 partitions in turn; of every 8 heads each partition gets
+// one, so that what a head's workgroups share stays in one L2.  Those of up to 7 heads that are left over go to all of them.
+__device__ __forceinline__ void deal_head(unsigned id, int items, int BG, int& bg, int& item)
+{
+    const unsigned whole = BG & ~7;
+    if (id < whole * items) {
+        const unsigned slot = id >> 3;
+        bg = (int)(slot / items * 8 + (id & 7));
+        item = (int)(slot % items);
+    } else {
+        const unsigned rest = id - whole * items;
+        bg = (int)(whole + rest / items);
+        item = (int)(rest % items);
+    }
+}
 
 // The largest of a workgroup's 256 values (>= 0, as bits); red: 4 words of LDS.  Two barriers.
 __device__ __forceinline__ unsigned block_max_bits(unsigned x, unsigned* red, int tid)

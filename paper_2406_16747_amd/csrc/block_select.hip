@@ -43,22 +43,33 @@ __global__ __launch_bounds__(256) void block_means_kernel(const uint16_t* __rest
     if (tid == 0) kms[bg * nbw + j] = code_scale(top, 127.0f);
 }
 
-// One workgroup of 4 waves per (64 queries, batch and head), a wave per 16 queries.  The `top` largest of up to thousands of
-// scores by radix: four passes over the scores, 8 bits of their order-preserving image a pass, in counters per query; a
-// pass forms the scores again (the matrix instructions cost less than keeping them).  A last pass writes what is above the
-// threshold and, of those equal to it, the first ones, in ascending order.
-template <int D>
-struct SelectSmem {
-    unsigned hist[4][16][257];
-    unsigned q8[64][D / 4 + 1];
-};
+// The sum and the largest over the four lanes col, col + 16, col + 32, col + 48.
+__device__ __forceinline__ unsigned groups_sum(unsigned x)
+{
+    const auto a = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    const unsigned y = (unsigned)a[0] + (unsigned)a[1];
+    const auto b = __builtin_amdgcn_permlane16_swap(y, y, false, false);
+    return (unsigned)b[0] + (unsigned)b[1];
+}
+__device__ __forceinline__ unsigned groups_max(unsigned x)
+{
+    const auto a = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    const unsigned y = max((unsigned)a[0], (unsigned)a[1]);
+    const auto b = __builtin_amdgcn_permlane16_swap(y, y, false, false);
+    return max((unsigned)b[0], (unsigned)b[1]);
+}
 
-template <int D>
+// One workgroup of 4 waves per (64 queries, batch and head), a wave per 16 queries: a lane holds the order-preserving images of
+// the scores of every fourth group of 4 blocks for one query.  A threshold with exactly `top` scores at or above it is
+// found by bisection, first halfway between values, then between images; where equal scores leave no such threshold the first of
+// those that share the last place are taken.  Counting a score costs two instructions; a radix pass in LDS counters
+// cost 4 to 8 times as much.  NT: tiles of 16 blocks whose images stay in registers; 0: any number, formed again for every count.
+template <int D, int NT>
 __global__ __launch_bounds__(256) void block_select_kernel(const uint16_t* __restrict__ q, int H, int Hkv, int n, int nbw, int top,
                                                            const int8_t* __restrict__ km, const float* __restrict__ kms,
                                                            int32_t* __restrict__ idx)
 {
-    __shared__ SelectSmem<D> sm;
+    __shared__ unsigned q8[64][D / 4 + 1];
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     const int nbp = gridDim.x - 1 - blockIdx.x;   // blocks behind the chunk's own; long chunks first
     const int bg = blockIdx.y, b = bg / Hkv, g = bg % Hkv, G = H / Hkv;
@@ -93,19 +104,21 @@ __global__ __launch_bounds__(256) void block_select_kernel(const uint16_t* __res
         const float f = code_factor(most, 127.0f);
 #pragma unroll
         for (int c = 0; c < DP / 4; c++)
-            sm.q8[r][DP / 4 * part + c] = pack4(code_i8(x[4 * c], f), code_i8(x[4 * c + 1], f), code_i8(x[4 * c + 2], f), code_i8(x[4 * c + 3], f));
+            q8[r][DP / 4 * part + c] = pack4(code_i8(x[4 * c], f), code_i8(x[4 * c + 1], f), code_i8(x[4 * c + 2], f), code_i8(x[4 * c + 3], f));
     }
     __syncthreads();
+    if (16 * wv >= rows) return;
     const int col = lane & 15, grp = lane >> 4;   // query of the wave, 16-byte piece of the operands / row group of the result
     i32x4 qf[D / 64];
 #pragma unroll
     for (int s = 0; s < D / 64; s++)
 #pragma unroll
-        for (int e = 0; e < 4; e++) qf[s][e] = (int)sm.q8[16 * wv + col][16 * s + 4 * grp + e];
+        for (int e = 0; e < 4; e++) qf[s][e] = (int)q8[16 * wv + col][16 * s + 4 * grp + e];
     const int8_t* kmr = km + (size_t)bg * nbw * D;
     const float* msr = kms + (size_t)bg * nbw;
+    typedef unsigned keys4 __attribute__((ext_vector_type(4)));
     // the images of blocks 16 t + 4 grp .. + 3 for query col; 0 (below every score) beyond the last block
-    auto keys = [&](int t, unsigned (&key)[4]) {
+    auto form = [&](int t) -> keys4 {
         const int row = min(16 * t + col, nbp - 1);
         i32x4 acc = {0, 0, 0, 0};
 #pragma unroll
@@ -113,84 +126,93 @@ __global__ __launch_bounds__(256) void block_select_kernel(const uint16_t* __res
             const i32x4 a = *(const i32x4*)(kmr + (size_t)row * D + 64 * s + 16 * grp);
             acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, qf[s], acc, 0, 0, 0);
         }
+        keys4 key;
 #pragma unroll
         for (int r = 0; r < 4; r++) {
             const int j = 16 * t + 4 * grp + r;
-            key[r] = j < nbp ? max(score_key((float)acc[r] * msr[min(j, nbp - 1)]), 1u) : 0u;
+            key[r] = j < nbp ? min(max(score_key((float)acc[r] * msr[min(j, nbp - 1)]), 1u), 0xFFFFFFFEu) : 0u;
         }
+        return key;
     };
     const int nt = (nbp + 15) / 16;
-    unsigned(*hist)[257] = sm.hist[wv];
-    unsigned prefix = 0, need = top;   // the threshold's upper bits, and how many of the scores that share them are wanted
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int x = lane; x < 16 * 257; x += 64) (&hist[0][0])[x] = 0;
-        __builtin_amdgcn_wave_barrier();
-        for (int t = 0; t < nt; t++) {
-            unsigned key[4];
-            keys(t, key);
+    keys4 kept[NT ? NT : 1];
+    // f(t, images) for every tile, the numbers of tiles known to the compiler where they stay in registers
+    auto each = [&](auto&& f) {
+        if constexpr (NT > 0) {
+            static_for<0, NT>([&](auto t) {
+                if (t < nt) f((int)t, kept[t]);
+            });
+        } else {
+            for (int t = 0; t < nt; t++) f(t, form(t));
+        }
+    };
+    if constexpr (NT > 0)
+        static_for<0, NT>([&](auto t) {
+            if (t < nt) kept[t] = form(t);
+        });
+    unsigned most = 0, least = ~0u;
+    each([&](int t, const keys4& k) {
 #pragma unroll
-            for (int r = 0; r < 4; r++)
-                if (shift == 24 || key[r] >> (shift + 8) == prefix) atomicAdd(&hist[col][key[r] >> shift & 255], 1u);
+        for (int r = 0; r < 4; r++) {
+            most = max(most, k[r]);
+            least = min(least, k[r] ? k[r] : ~0u);
         }
-        __builtin_amdgcn_wave_barrier();
-        // lane (col, grp) adds up digits 64 grp .. 64 grp + 63; the threshold's digit is where the sum from the top reaches `need`
-        unsigned mine = 0;
-        for (int x = 0; x < 64; x++) mine += hist[col][64 * grp + x];
-        unsigned above = 0;
+    });
+    // at least `top` images are >= lo, fewer are >= hi
+    unsigned lo = ~groups_max(~least), hi = groups_max(most) + 1, above = 0;
+    bool done = false;
+    for (int it = 0; __any(!done); it++) {
+        unsigned mid = lo + (hi - lo) / 2;
+        if (it < 20) {   // halfway between the values: scores of one size are found apart in about ten steps
+            const unsigned m = score_key(0.5f * __uint_as_float(score_key_inv(lo)) + 0.5f * __uint_as_float(score_key_inv(hi - 1)));
+            mid = m > lo && m < hi ? m : mid;
+        }
+        unsigned c = 0;
+        each([&](int t, const keys4& k) {
 #pragma unroll
-        for (int y = 1; y < 4; y++) {
-            const unsigned other = (unsigned)__shfl((int)mine, (col + 16 * (grp + y)) & 63, 64);
-            if (grp + y < 4) above += other;
+            for (int r = 0; r < 4; r++) c += k[r] >= mid ? 1u : 0u;
+        });
+        c = groups_sum(c);
+        if (!done) {
+            if (mid == lo) done = true;              // hi == lo + 1: what is equal to lo shares the last places
+            else if (c >= (unsigned)top) lo = mid;
+            else { hi = mid; above = c; }
+            if (!done && c == (unsigned)top) { hi = lo; above = c; done = true; }
         }
-        unsigned digit = 0, left = 0;
-        const bool here = above < need && above + mine >= need;
-        if (here) {
-            unsigned sum = above;
-            for (int x = 63; x >= 0; x--) {
-                const unsigned c = hist[col][64 * grp + x];
-                if (sum + c >= need) {
-                    digit = 64 * grp + x;
-                    left = need - sum;
-                    break;
-                }
-                sum += c;
-            }
-        }
-        // (one of a query's four lanes has found it)
-        digit |= (unsigned)__shfl_xor((int)digit, 16, 64);
-        left |= (unsigned)__shfl_xor((int)left, 16, 64);
-        digit |= (unsigned)__shfl_xor((int)digit, 32, 64);
-        left |= (unsigned)__shfl_xor((int)left, 32, 64);
-        prefix = prefix << 8 | digit;
-        need = left;
-        __builtin_amdgcn_wave_barrier();
     }
-    unsigned written = 0, equal = 0;   // so far, of this query
+    unsigned need = (unsigned)top - above, written = 0;   // places left for images equal to lo; written so far
     const bool live = 16 * wv + col < rows;
     int32_t* mine = out + (size_t)(16 * wv + col) * top;
-    for (int t = 0; t < nt; t++) {
-        unsigned key[4];
-        keys(t, key);
-        unsigned gt = 0, eq = 0;   // bit 4 grp + r
+    const unsigned long long all = 0x0001000100010001ull << col, lower = all & ((1ull << (16 * grp)) - 1);
+    const bool ties = __any(need > 0);
+    each([&](int t, const keys4& k) {
+        bool in[4];
+#pragma unroll
+        for (int r = 0; r < 4; r++) in[r] = k[r] >= hi;
+        if (ties) {
+            unsigned eq = 0;
+#pragma unroll
+            for (int r = 0; r < 4; r++) eq |= (need > 0 && k[r] == lo ? 1u : 0u) << (4 * grp + r);
+            eq = groups_sum(eq);   // (each bit is one lane's)
+            unsigned take = 0;
+            for (; eq && need; eq &= eq - 1, need--) take |= eq & -eq;
+#pragma unroll
+            for (int r = 0; r < 4; r++) in[r] |= take >> (4 * grp + r) & 1;
+        }
+        unsigned place = written;
 #pragma unroll
         for (int r = 0; r < 4; r++) {
-            gt |= (key[r] > prefix ? 1u : 0u) << (4 * grp + r);
-            eq |= (key[r] == prefix ? 1u : 0u) << (4 * grp + r);
+            const unsigned long long m = __ballot(in[r]);
+            place += __popcll(m & lower);
+            written += __popcll(m & all);
         }
-        unsigned both = gt | eq << 16;
-        both |= (unsigned)__shfl_xor((int)both, 16, 64);
-        both |= (unsigned)__shfl_xor((int)both, 32, 64);
-        gt = both & 0xFFFFu;
-        eq = both >> 16;
-        unsigned take = gt;
-        for (unsigned e = eq; e && equal < need; e &= e - 1, equal++) take |= e & -e;
 #pragma unroll
-        for (int r = 0; r < 4; r++) {
-            const unsigned bit = 1u << (4 * grp + r);
-            if (live && (take & bit)) mine[written + __popc(take & (bit - 1))] = 16 * t + 4 * grp + r;
-        }
-        written += __popc(take);
-    }
+        for (int r = 0; r < 4; r++)
+            if (in[r]) {
+                if (live) mine[place] = 16 * t + 4 * grp + r;
+                place++;
+            }
+    });
 }
 
 size_t block_select_ws_bytes(const sparsek_block_cfg& c)
@@ -206,14 +228,21 @@ int launch_block_select(const sparsek_block_cfg& c, const void* q, const void* k
     int8_t* km = (int8_t*)ws;
     float* kms = (float*)((char*)ws + align_up((size_t)BG * nbw * c.d, 256));
     const dim3 all(block_count(c.n), BG);
-#define SELECT(D)                                                                                                                  \
-    if (nbw > c.top) hipLaunchKernelGGL((block_means_kernel<D>), dim3(nbw, BG), dim3(256), 0, st, (const uint16_t*)k, c.n, nbw, km, kms); \
-    hipLaunchKernelGGL((block_select_kernel<D>), all, dim3(256), 0, st, (const uint16_t*)q, c.H, c.Hkv, c.n, nbw, c.top, km, kms, idx)
-    if (c.d == 128) {
-        SELECT(128);
-    } else {
-        SELECT(64);
+    if (nbw > c.top) {
+        if (c.d == 128) hipLaunchKernelGGL((block_means_kernel<128>), dim3(nbw, BG), dim3(256), 0, st, (const uint16_t*)k, c.n, nbw, km, kms);
+        else hipLaunchKernelGGL((block_means_kernel<64>), dim3(nbw, BG), dim3(256), 0, st, (const uint16_t*)k, c.n, nbw, km, kms);
     }
+#define SELECT(D, NT) hipLaunchKernelGGL((block_select_kernel<D, NT>), all, dim3(256), 0, st, (const uint16_t*)q, c.H, c.Hkv, c.n, nbw, c.top, km, kms, idx)
+#define BY_LENGTH(D)                          \
+    if (nbw <= 128) { SELECT(D, 8); }         \
+    else if (nbw <= 512) { SELECT(D, 32); }   \
+    else { SELECT(D, 0); }
+    if (c.d == 128) {
+        BY_LENGTH(128)
+    } else {
+        BY_LENGTH(64)
+    }
+#undef BY_LENGTH
 #undef SELECT
     return launch_status();
 }

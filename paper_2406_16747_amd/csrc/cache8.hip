@@ -9,7 +9,6 @@
 namespace spk {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 
 struct CacheArgs {
     sparsek_cache8 t;

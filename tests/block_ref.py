@@ -1,9 +1,9 @@
 """Attention over selected blocks of 64 tokens and the cache in 8 bits from their definitions, in 64 bits on the CPU, with bounds
 on how far a kernel's results may be from them.
 
-A value rounded to bf16 is off by at most 2^-8 of itself (half a step).  The kernels round every weight p, every score
-gradient ds and every output once to bf16, and partial results to fp16 relative to the largest value of their block (2^-11);
-sums are fp32 (d products of 2^-24 each; 2^-14 covers them and the exponentials with room, for logits below 2^5)."""
+A value rounded to bf16 is off by at most 2^-8 of itself (half a step), one rounded to fp16 by 2^-11.  The kernels round every
+output once to bf16; the weights p to fp16 in the forward and to bf16 in the backward and over the cache, the score gradients ds to bf16, and
+partial results to fp16 relative to the largest value of their block; sums are fp32 (d products of 2^-24 each; 2^-14 covers them and the exponentials with room, for logits below 2^5)."""
 import numpy as np
 import torch
 
@@ -76,7 +76,7 @@ def attn(q, k, v, idx, scale):
                 lse[b, h] = torch.logsumexp(s, 1)
                 p = torch.exp(s - lse[b, h][:, None])
                 o[b, h] = p @ v[b, g]
-                ob[b, h] = 2 ** -8 * o[b, h].abs() + (2 ** -8 + 2 ** -11 + 2 ** -14) * (p @ v[b, g].abs()) + 2 ** -22 * v[b, g].abs().max()
+                ob[b, h] = 2 ** -8 * o[b, h].abs() + (2 ** -11 + 2 ** -11 + 2 ** -14) * (p @ v[b, g].abs()) + 2 ** -22 * v[b, g].abs().max()
                 lb[b, h] = 2 ** -17 * (q[b, h].abs() @ k[b, g].abs().T * scale).masked_fill(~see, 0).amax(1) + 2 ** -20
                 mass[b, g] += torch.nn.functional.pad(p.sum(0), (0, nb * T - n)).view(nb, T).sum(1)
     return o, lse, mass, ob, lb

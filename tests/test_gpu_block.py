@@ -160,6 +160,25 @@ def test_many_rows_select_one_block():
     check_all(q, k, v, dO, idx.cuda(), 1 / math.sqrt(d))
 
 
+def check_rows(q, k, v, dO, idx, o, dq, scale, heads, rows):
+    """Single rows of every kind of long input against a definition of their own."""
+    G = q.shape[1] // k.shape[1]
+    for h in heads:
+        K, V = ref.f64(k[0, h // G]), ref.f64(v[0, h // G])
+        for i in rows:
+            at = torch.cat([torch.arange(64) + 64 * j for j in idx[0, h // G, i].tolist() if j >= 0] + [torch.arange(i // 64 * 64, i + 1)])
+            p = torch.softmax(K[at] @ ref.f64(q[0, h, i]) * scale, 0)
+            want = p @ V[at]
+            within(o[0, h, i], want, 2 ** -8 * want.abs() + (2 ** -11 + 2 ** -11 + 2 ** -14) * (p @ V[at].abs()) + 2 ** -22 * V.abs().max(), "o of row %d" % i)
+            if dq is None:
+                continue
+            g, oo = ref.f64(dO[0, h, i]), ref.f64(o[0, h, i])
+            ds = p * (V[at] @ g - (g * oo).sum()) * scale
+            e = (2 ** -8 + 2 ** -11 + 2 ** -14) * ds.abs() + 2 ** -17 * p * (V[at].abs() @ g.abs() + (g * oo).abs().sum()) * scale
+            want = ds @ K[at]
+            within(dq[0, h, i], want, 2 ** -8 * want.abs() + e @ K[at].abs() + 2 ** -22 * (ds.abs() @ K[at].abs()).max(), "dq of row %d" % i)
+
+
 def test_a_long_document_row_by_row():
     """30000 tokens: rows picked all over it against a definition of their own."""
     require_gpu()
@@ -172,21 +191,24 @@ def test_a_long_document_row_by_row():
     dq, dk, dv = spk.sparsek_block_attn_bwd(q, k, v, idx, o, lse, dO, scale)
     torch.cuda.synchronize()
     assert abs(float(mass.double().sum()) / (n * H) - 1) < 1e-5      # every row hands out a weight of 1
-    K, V = ref.f64(k[0, 0]), ref.f64(v[0, 0])
-    for i in list(range(0, n, 1777)) + [n - 1]:
-        at = torch.cat([torch.arange(64) + 64 * j for j in idx[0, 0, i].tolist() if j >= 0] + [torch.arange(i // 64 * 64, i + 1)])
-        s = ref.f64(q[0, :, i]) @ K[at].T * scale
-        p = torch.softmax(s, 1)
-        A = p @ V[at].abs()
-        want = p @ V[at]
-        within(o[0, :, i], want, 2 ** -8 * want.abs() + (2 ** -8 + 2 ** -11 + 2 ** -14) * A + 2 ** -22 * V.abs().max(), "o of row %d" % i)
-        g, oo = ref.f64(dO[0, :, i]), ref.f64(o[0, :, i])
-        delta = (g * oo).sum(1, keepdim=True)
-        ds = p * (g @ V[at].T - delta) * scale
-        e = (2 ** -8 + 2 ** -11 + 2 ** -14) * ds.abs() + 2 ** -17 * p * (g.abs() @ V[at].abs().T + (g * oo).abs().sum(1, keepdim=True)) * scale
-        want = ds @ K[at]
-        within(dq[0, :, i], want, 2 ** -8 * want.abs() + e @ K[at].abs() + 2 ** -22 * (ds.abs() @ K[at].abs()).amax(1, keepdim=True), "dq of row %d" % i)
+    check_rows(q, k, v, dO, idx, o, dq, scale, range(H), list(range(0, n, 1777)) + [n - 1])
     assert torch.isfinite(dk).all() and torch.isfinite(dv).all()
+
+
+@pytest.mark.parametrize("H,Hkv,n,top", [(16, 2, 131000, 32), (20, 10, 100000, 16)])
+def test_documents_of_several_stretches(H, Hkv, n, top):
+    """More than the forward's workspace holds at a time: the queries, or the heads, go through it in parts (17.7 and 8.7 GB of partial
+    results); the masses of a block come from all of them."""
+    require_gpu()
+    say("block attention, several stretches", H, Hkv, n, top)
+    d, scale = 128, 1 / math.sqrt(128)
+    g = torch.Generator(device="cuda").manual_seed(7)
+    q, k, v = (torch.randn(1, h, n, d, device="cuda", generator=g).bfloat16() for h in (H, Hkv, Hkv))
+    idx = spk.sparsek_block_select(q, k, top)
+    o, lse, mass = spk.sparsek_block_attn_fwd(q, k, v, idx, scale, mass=True)
+    torch.cuda.synchronize()
+    assert ((mass.double().sum(2) / (n * (H // Hkv)) - 1).abs() < 1e-5).all()
+    check_rows(q, k, v, None, idx, o, None, scale, (0, H // 2, H - 1), list(range(0, n, n // 9)) + [n - 1])
 
 
 def test_results_do_not_depend_on_timing():
