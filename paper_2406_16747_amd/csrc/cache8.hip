@@ -24,7 +24,6 @@ __device__ __forceinline__ int clamp_len(int len, int cap) { return min(max(len,
 template <int D>
 struct BlockRegs {
     static constexpr int CPR = D / 8, RG = 256 / CPR, NT = BT / RG;
-    u32x4 k[NT], v[NT];
 };
 
 __device__ __forceinline__ float half_of(u32x4 x, int e) { return __uint_as_float(e & 1 ? x[e / 2] & 0xFFFF0000u : x[e / 2] << 16); }
@@ -44,50 +43,73 @@ __device__ __forceinline__ unsigned codes4(float a, float b, float c, float d, f
 
 template <int D>
 struct AppendSmem {
+    static constexpr int VS = BT + 8;                                       // bf16 values between the columns of vt
     double sums[256 / (D / 8)][D];
-    unsigned char vt[D][BT + 16];
-    unsigned red[4];
+    __attribute__((aligned(16))) uint16_t vt[D * VS];                       // the block's values, transposed
+    unsigned red[8];
 };
 
-// A whole block goes to its page: codes, scales and the mean key.
+// The largest of a workgroup's 256 values (>= 0, as bits) in two of them at once.  Two barriers.
+__device__ __forceinline__ void block_max_bits2(unsigned& x, unsigned& y, unsigned* red, int tid)
+{
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+        x = max(x, (unsigned)__shfl_xor((int)x, s, 64));
+        y = max(y, (unsigned)__shfl_xor((int)y, s, 64));
+    }
+    __syncthreads();
+    if ((tid & 63) == 0) {
+        red[tid >> 6] = x;
+        red[4 + (tid >> 6)] = y;
+    }
+    __syncthreads();
+    x = max(max(red[0], red[1]), max(red[2], red[3]));
+    y = max(max(red[4], red[5]), max(red[6], red[7]));
+}
+
+// A whole block goes to its page: codes, scales and the mean key.  The keys are in registers, the values (transposed) in sm.vt; every
+// thread has seen the end of what was written there.
 template <int D, int FORMAT>
-__device__ __forceinline__ void store_block(AppendSmem<D>& sm, const CacheArgs& a, int page, const BlockRegs<D>& r, int tid)
+__device__ __forceinline__ void store_block(AppendSmem<D>& sm, const CacheArgs& a, int page, const u32x4 (&kr)[BlockRegs<D>::NT], unsigned tv, int tid)
 {
     using R = BlockRegs<D>;
     const float most = FORMAT == SPARSEK_I8 ? 127.0f : 448.0f;
     const int tok = tid / R::CPR, c = tid % R::CPR;
-    unsigned tk = 0, tv = 0;
+    unsigned tk = 0;
     double s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
     for (int t = 0; t < R::NT; t++)
 #pragma unroll
         for (int e = 0; e < 8; e++) {
-            const float k = half_of(r.k[t], e);
+            const float k = half_of(kr[t], e);
             s[e] += (double)k;
             tk = max(tk, __float_as_uint(fabsf(k)));
-            tv = max(tv, __float_as_uint(fabsf(half_of(r.v[t], e))));
         }
-    const float topk = __uint_as_float(block_max_bits(tk, sm.red, tid)), topv = __uint_as_float(block_max_bits(tv, sm.red, tid));
-    const float fk = code_factor(topk, most), fv = code_factor(topv, most);
 #pragma unroll
     for (int e = 0; e < 8; e++) sm.sums[tok][8 * c + e] = s[e];
+    block_max_bits2(tk, tv, sm.red, tid);   // (and the sums and values are there)
+    const float topk = __uint_as_float(tk), topv = __uint_as_float(tv);
+    const float fk = code_factor(topk, most), fv = code_factor(topv, most);
     unsigned char* kp = (unsigned char*)a.t.k8 + (size_t)page * BT * D;
 #pragma unroll
     for (int t = 0; t < R::NT; t++) {
         u32x2 w;
-        w[0] = codes4<FORMAT>(half_of(r.k[t], 0), half_of(r.k[t], 1), half_of(r.k[t], 2), half_of(r.k[t], 3), fk);
-        w[1] = codes4<FORMAT>(half_of(r.k[t], 4), half_of(r.k[t], 5), half_of(r.k[t], 6), half_of(r.k[t], 7), fk);
+        w[0] = codes4<FORMAT>(half_of(kr[t], 0), half_of(kr[t], 1), half_of(kr[t], 2), half_of(kr[t], 3), fk);
+        w[1] = codes4<FORMAT>(half_of(kr[t], 4), half_of(kr[t], 5), half_of(kr[t], 6), half_of(kr[t], 7), fk);
         *(u32x2*)(kp + (tok + R::RG * t) * D + 8 * c) = w;
-#pragma unroll
-        for (int h = 0; h < 2; h++) {
-            const unsigned x = codes4<FORMAT>(half_of(r.v[t], 4 * h), half_of(r.v[t], 4 * h + 1), half_of(r.v[t], 4 * h + 2), half_of(r.v[t], 4 * h + 3), fv);
-#pragma unroll
-            for (int e = 0; e < 4; e++) sm.vt[8 * c + 4 * h + e][tok + R::RG * t] = (unsigned char)(x >> (8 * e));
-        }
     }
-    __syncthreads();
     unsigned char* vp = (unsigned char*)a.t.v8 + (size_t)page * BT * D;
-    for (int x = tid; x < D * (BT / 16); x += 256) *(u32x4*)(vp + 16 * x) = *(const u32x4*)&sm.vt[x / 4][16 * (x % 4)];
+#pragma unroll
+    for (int t = 0; t < BT * D / 16 / 256; t++) {
+        const int x = tid + 256 * t;
+        const u32x4 lo = *(const u32x4*)&sm.vt[x / 4 * AppendSmem<D>::VS + 16 * (x % 4)], hi = *(const u32x4*)&sm.vt[x / 4 * AppendSmem<D>::VS + 16 * (x % 4) + 8];
+        u32x4 w;
+        w[0] = codes4<FORMAT>(half_of(lo, 0), half_of(lo, 1), half_of(lo, 2), half_of(lo, 3), fv);
+        w[1] = codes4<FORMAT>(half_of(lo, 4), half_of(lo, 5), half_of(lo, 6), half_of(lo, 7), fv);
+        w[2] = codes4<FORMAT>(half_of(hi, 0), half_of(hi, 1), half_of(hi, 2), half_of(hi, 3), fv);
+        w[3] = codes4<FORMAT>(half_of(hi, 4), half_of(hi, 5), half_of(hi, 6), half_of(hi, 7), fv);
+        *(u32x4*)(vp + 16 * x) = w;
+    }
     float mean = 0.0f;
     if (tid < D) {
         double y = 0;
@@ -111,7 +133,7 @@ __global__ __launch_bounds__(256) void cache8_append_kernel(CacheArgs a, const i
                                                             const uint16_t* __restrict__ v)
 {
     using R = BlockRegs<D>;
-    __shared__ __attribute__((aligned(16))) AppendSmem<D> sm;
+    __shared__ AppendSmem<D> sm;
     const int tid = threadIdx.x, bg = blockIdx.y, b = bg / a.Hkv;
     const int len = clamp_len(a.lens[b], a.cap);
     const int count = min(counts ? min(max(counts[b], 0), c) : c, a.cap * BT + BT - 1 - len);   // (what does not fit is dropped)
@@ -120,26 +142,45 @@ __global__ __launch_bounds__(256) void cache8_append_kernel(CacheArgs a, const i
     if (j * BT >= after) return;
     const uint16_t *kn = k + (size_t)bg * c * D, *vn = v + (size_t)bg * c * D;
     uint16_t *kt = (uint16_t*)a.t.kt + (size_t)bg * BT * D, *vt = (uint16_t*)a.t.vt + (size_t)bg * BT * D;
-    if ((j + 1) * BT <= after) {
-        R r;
-        const int page = a.t.table[(size_t)bg * a.cap + j];
+    const int page = (j + 1) * BT <= after ? a.t.table[(size_t)bg * a.cap + j] : -1;
+    if (page >= 0 && page < a.pages) {
+        u32x4 kr[R::NT];
+        unsigned tv = 0;
+        const int old = max(0, len - j * BT);   // tokens of the block that are there already (in the first one only)
 #pragma unroll
         for (int t = 0; t < R::NT; t++) {
-            const int tok = j * BT + tid / R::CPR + R::RG * t, col = 8 * (tid % R::CPR);
-            if (tok >= len) {
-                r.k[t] = *(const u32x4*)(kn + (size_t)(tok - len) * D + col);
-                r.v[t] = *(const u32x4*)(vn + (size_t)(tok - len) * D + col);
-            } else {
-                r.k[t] = *(const u32x4*)(kt + (tok % BT) * D + col);
+            const int x = tid / R::CPR + R::RG * t, col = 8 * (tid % R::CPR), tok = j * BT + x;
+            if (x >= old) {
+                kr[t] = *(const u32x4*)(kn + (size_t)(tok - len) * D + col);
+                const u32x4 vr = *(const u32x4*)(vn + (size_t)(tok - len) * D + col);
 #pragma unroll
-                for (int e = 0; e < 4; e++) r.v[t][e] = (unsigned)vt[(col + 2 * e) * BT + tok % BT] | (unsigned)vt[(col + 2 * e + 1) * BT + tok % BT] << 16;
+                for (int e = 0; e < 8; e++) {
+                    const unsigned y = e & 1 ? vr[e / 2] >> 16 : vr[e / 2] & 0xFFFFu;
+                    tv = max(tv, (y & 0x7FFFu) << 16);
+                    sm.vt[(col + e) * AppendSmem<D>::VS + x] = (uint16_t)y;
+                }
+            } else {
+                kr[t] = *(const u32x4*)(kt + x * D + col);
             }
         }
-        if (page >= 0 && page < a.pages) store_block<D, FORMAT>(sm, a, page, r, tid);
+        if (old)   // (8 tokens of a column at a time, the last of them perhaps in part)
+            for (int x = tid; x < D * 8; x += 256) {
+                const int col = x >> 3, t0 = 8 * (x & 7);
+                if (t0 >= old) continue;
+                const u32x4 vr = *(const u32x4*)(vt + col * BT + t0);
+#pragma unroll
+                for (int e = 0; e < 8; e++)
+                    if (t0 + e < old) {
+                        const unsigned y = e & 1 ? vr[e / 2] >> 16 : vr[e / 2] & 0xFFFFu;
+                        tv = max(tv, (y & 0x7FFFu) << 16);
+                        sm.vt[col * AppendSmem<D>::VS + t0 + e] = (uint16_t)y;
+                    }
+            }
+        store_block<D, FORMAT>(sm, a, page, kr, tv, tid);
     }
-    const int whole = after / BT;   // the block that stays unfinished, if it has tokens
     if (blockIdx.x != 0) return;
     __syncthreads();                // everybody has read what is overwritten now
+    const int whole = after / BT;   // the block that stays unfinished, if it has tokens
     const int t0 = max(len, whole * BT);
     for (int x = tid; x < (after - t0) * D; x += 256) {
         const int tok = t0 + x / D, col = x % D;
@@ -148,94 +189,95 @@ __global__ __launch_bounds__(256) void cache8_append_kernel(CacheArgs a, const i
     }
 }
 
-// ---- the `top` largest of n keys in LDS, by radix: four passes of 8 bits ----
-
-// What a workgroup of 1024 keeps in LDS beside the keys.
-struct TopSmem {
-    unsigned hist[256], digit, left;
-    int wsum[16][2];
+// ---- the `need` largest of n keys in LDS, by a workgroup of NT ----
+// Radix: four passes of 8 bits over the keys, counters in LDS that every wave adds up for itself: one barrier a pass.  (A wave that
+// bisects takes 35 us for 512 rows of 2048, 16 waves with a bound each 46, passes with a barrier ahead of and behind the sum 17.)
+struct TopBounds {
+    unsigned thr, left;   // keys above thr, and `left` of those equal to it
 };
-
-// The threshold of the `need` largest (need <= n, need >= 1) and how many of those equal to it belong to them.
-__device__ __forceinline__ void top_threshold(TopSmem& sm, const unsigned* keys, int n, unsigned need, unsigned& thr, unsigned& equal)
+template <int NT>
+struct TopSmem {
+    unsigned hist[3][256];
+    int wsum[NT / 64][2];
+};
+template <int NT>
+__device__ __forceinline__ TopBounds wg_top(TopSmem<NT>& sm, const unsigned* keys, int n, unsigned need)
 {
     const int tid = threadIdx.x, lane = tid & 63;
     unsigned prefix = 0;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (tid < 256) sm.hist[tid] = 0;
-        __syncthreads();
-        for (int x = tid; x < n; x += 1024)
-            if (shift == 24 || keys[x] >> (shift + 8) == prefix) atomicAdd(&sm.hist[keys[x] >> shift & 255], 1u);
-        __syncthreads();
-        if (tid < 64) {   // lane: digits 255 - 4 lane .. 252 - 4 lane
-            unsigned c[4], mine = 0;
-#pragma unroll
-            for (int e = 0; e < 4; e++) mine += c[e] = sm.hist[255 - 4 * lane - e];
-            unsigned sum = mine;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const unsigned y = (unsigned)__shfl_up((int)sum, d, 64);
-                if (lane >= d) sum += y;
-            }
-            unsigned above = sum - mine;
-            if (above < need && sum >= need) {
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    if (above < need && above + c[e] >= need) {
-                        sm.digit = 255 - 4 * lane - e;
-                        sm.left = need - above;
-                    }
-                    above += c[e];
-                }
-            }
-        }
-        __syncthreads();
-        prefix = prefix << 8 | sm.digit;
-        need = sm.left;
-    }
-    thr = prefix;
-    equal = need;
+    if (tid < 256) sm.hist[0][tid] = 0;
     __syncthreads();
+#pragma unroll
+    for (int pass = 0; pass < 4; pass++) {
+        const int shift = 24 - 8 * pass;
+        unsigned* hist = sm.hist[pass % 3];
+        for (int x = tid; x < n; x += NT)
+            if (pass == 0 || keys[x] >> (shift + 8) == prefix) atomicAdd(&hist[keys[x] >> shift & 255], 1u);
+        if (tid < 256) sm.hist[(pass + 1) % 3][tid] = 0;   // (read in the pass before the last one: everybody is past that)
+        __syncthreads();
+        // lane: digits 255 - 4 lane .. 252 - 4 lane; the threshold's digit is where the sum from the top reaches `need`
+        const u32x4 c = *(const u32x4*)&hist[252 - 4 * lane];
+        const unsigned mine = c[0] + c[1] + c[2] + c[3];
+        unsigned sum = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const unsigned y = (unsigned)__shfl_up((int)sum, d, 64);
+            if (lane >= d) sum += y;
+        }
+        unsigned above = sum - mine, digit = 0, left = 0;
+#pragma unroll
+        for (int e = 3; e >= 0; e--) {
+            if (above < need && above + c[e] >= need) {
+                digit = 252 - 4 * lane + e;
+                left = need - above;
+            }
+            above += c[e];
+        }
+        const unsigned long long found = __ballot(left > 0);
+        const int at = __ffsll(found) - 1;
+        prefix = prefix << 8 | (unsigned)__builtin_amdgcn_readlane((int)digit, at);
+        need = (unsigned)__builtin_amdgcn_readlane((int)left, at);
+    }
+    return TopBounds{prefix, need};
 }
 
-// emit(x, kept, place): every x < n in order, whether it belongs to the `need` largest (of equal ones the first), and its place
-// among the kept ones or among the others.
-template <typename F>
-__device__ __forceinline__ void top_emit(TopSmem& sm, const unsigned* keys, int n, unsigned thr, unsigned equal, F&& emit)
+// order[place] = x for every x < n: those that belong to the largest (of equal ones the first) ahead of the others, both in order.
+// Thread t has the keys t R .. t R + R - 1.  Ends with a barrier.
+template <int NT>
+__device__ __forceinline__ void wg_order(TopSmem<NT>& sm, const unsigned* keys, int n, TopBounds t, int budget, int* order)
 {
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    const unsigned long long below = (1ull << lane) - 1;
-    int kept = 0, eqs = 0;
-    for (int x0 = 0; x0 < n; x0 += 1024) {
-        const int x = x0 + tid;
-        const unsigned key = x < n ? keys[x] : 0;
-        const bool gt = x < n && key > thr, eq = x < n && key == thr;
-        const unsigned long long mg = __ballot(gt), me = __ballot(eq);
-        if (lane == 0) {
-            sm.wsum[wv][0] = __popcll(mg);
-            sm.wsum[wv][1] = __popcll(me);
-        }
-        __syncthreads();
-        int g = kept, e = eqs, ga = 0, ea = 0;
-#pragma unroll
-        for (int w = 0; w < 16; w++) {
-            const int a = sm.wsum[w][0], c = sm.wsum[w][1];
-            if (w < wv) { g += a; e += c; }
-            ga += a;
-            ea += c;
-        }
-        // kept so far = those above the threshold + the first `equal` of those at it
-        g += __popcll(mg & below);
-        e += __popcll(me & below);
-        const int before = g + min(e, (int)equal);
-        if (x < n) {
-            const bool in = gt || (eq && e < (int)equal);
-            emit(x, in, in ? before : x - before);
-        }
-        kept += ga;
-        eqs += ea;
-        __syncthreads();
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, R = (n + NT - 1) / NT, x0 = min(n, tid * R), x1 = min(n, x0 + R);
+    int g = 0, e = 0;
+    for (int x = x0; x < x1; x++) {
+        g += keys[x] > t.thr;
+        e += keys[x] == t.thr;
     }
+    int gs = g, es = e;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int y = __shfl_up(gs, d, 64), z = __shfl_up(es, d, 64);
+        if (lane >= d) { gs += y; es += z; }
+    }
+    if (lane == 63) {
+        sm.wsum[wv][0] = gs;
+        sm.wsum[wv][1] = es;
+    }
+    __syncthreads();
+    gs -= g;
+    es -= e;
+    for (int w = 0; w < wv; w++) {
+        gs += sm.wsum[w][0];
+        es += sm.wsum[w][1];
+    }
+    int kept = gs + min(es, (int)t.left);
+    for (int x = x0; x < x1; x++) {
+        const unsigned k = keys[x];
+        const bool in = k > t.thr || (k == t.thr && es < (int)t.left);
+        order[in ? kept : budget + x - kept] = x;
+        es += k == t.thr;
+        kept += in;
+    }
+    __syncthreads();
 }
 
 // ---- selection of blocks for a single query ----
@@ -243,10 +285,11 @@ __device__ __forceinline__ void top_emit(TopSmem& sm, const unsigned* keys, int 
 template <int D>
 __global__ __launch_bounds__(1024) void cache8_select_kernel(CacheArgs a, const uint16_t* __restrict__ q, int top, int32_t* __restrict__ idx)
 {
-    extern __shared__ unsigned keys[];
-    __shared__ TopSmem sm;
+    extern __shared__ unsigned keys[];   // [cap], and the pages, then the order [cap]
+    int* at = (int*)(keys + a.cap);
+    __shared__ __attribute__((aligned(16))) TopSmem<1024> sm;
     __shared__ unsigned q8[D / 4];
-    constexpr int LPB = D / 16;   // lanes per block: 16 bytes each
+    constexpr int LPB = D / 16, BPR = 1024 / LPB;   // lanes per block (16 bytes each), blocks per round
     const int tid = threadIdx.x, bg = blockIdx.x, b = bg / a.Hkv, g = bg % a.Hkv;
     const int len = clamp_len(a.lens[b], a.cap);
     const int nb = len > 0 ? (len - 1) / BT : 0;   // blocks behind the query's own
@@ -255,15 +298,21 @@ __global__ __launch_bounds__(1024) void cache8_select_kernel(CacheArgs a, const 
         for (int x = tid; x < top; x += 1024) out[x] = x < nb ? x : -1;
         return;
     }
+    for (int x = tid; x < nb; x += 1024) at[x] = a.t.table[(size_t)bg * a.cap + x];
     if (tid < 64) {   // the group's queries, added up and rounded
         constexpr int PL = D / 64;
         float x[PL];
         float most = 0.0f;
+        double s[PL];
+#pragma unroll
+        for (int e = 0; e < PL; e++) s[e] = 0;
+#pragma unroll 4
+        for (int h = 0; h < a.G; h++)
+#pragma unroll
+            for (int e = 0; e < PL; e++) s[e] += (double)bf16_to_f32(q[((size_t)b * a.H + g * a.G + h) * D + PL * tid + e]);
 #pragma unroll
         for (int e = 0; e < PL; e++) {
-            double s = 0;
-            for (int h = 0; h < a.G; h++) s += (double)bf16_to_f32(q[((size_t)b * a.H + g * a.G + h) * D + PL * tid + e]);
-            x[e] = (float)s;
+            x[e] = (float)s[e];
             most = fmaxf(most, fabsf(x[e]));
         }
         const float f = code_factor(wave_max_f32(most), 127.0f);
@@ -275,68 +324,82 @@ __global__ __launch_bounds__(1024) void cache8_select_kernel(CacheArgs a, const 
     i32x4 qv;
 #pragma unroll
     for (int e = 0; e < 4; e++) qv[e] = (int)q8[4 * c + e];
-    for (int x0 = 0; x0 < nb; x0 += 1024 / LPB) {
-        const int x = x0 + tid / LPB;
-        const int page = a.t.table[(size_t)bg * a.cap + min(x, nb - 1)];
-        const bool ok = page >= 0 && page < a.pages;
-        const i32x4 m = *(const i32x4*)(a.t.km + (size_t)(ok ? page : 0) * D + 16 * c);
-        int s = 0;
+    constexpr int UNR = 4;   // rounds whose loads are under way together
+    for (int x0 = tid / LPB; x0 < nb; x0 += UNR * BPR) {
+        i32x4 m[UNR];
+        float ms[UNR];
 #pragma unroll
-        for (int e = 0; e < 4; e++) s = __builtin_amdgcn_sdot4(m[e], qv[e], s, false);
+        for (int u = 0; u < UNR; u++) {
+            const int page = at[min(x0 + u * BPR, nb - 1)], p = page >= 0 && page < a.pages ? page : 0;
+            m[u] = *(const i32x4*)(a.t.km + (size_t)p * D + 16 * c);
+            ms[u] = a.t.kms[p];
+        }
 #pragma unroll
-        for (int d = 1; d < LPB; d <<= 1) s += __shfl_xor(s, d, 64);
-        if (c == 0 && x < nb) keys[x] = ok ? max(score_key((float)s * a.t.kms[page]), 1u) : 0u;
+        for (int u = 0; u < UNR; u++) {
+            const int x = x0 + u * BPR, page = at[min(x, nb - 1)];
+            int s = 0;
+#pragma unroll
+            for (int e = 0; e < 4; e++) s = __builtin_amdgcn_sdot4(m[u][e], qv[e], s, false);
+#pragma unroll
+            for (int d = 1; d < LPB; d <<= 1) s += __shfl_xor(s, d, 64);
+            if (c == 0 && x < nb) keys[x] = page >= 0 && page < a.pages ? min(max(score_key((float)s * ms[u]), 2u), 0xFFFFFFFEu) : 1u;
+        }
     }
     __syncthreads();
-    unsigned thr, equal;
-    top_threshold(sm, keys, nb, top, thr, equal);
-    top_emit(sm, keys, nb, thr, equal, [&](int x, bool in, int place) {
-        if (in) out[place] = x;
-    });
+    wg_order(sm, keys, nb, wg_top(sm, keys, nb, (unsigned)top), top, at);
+    for (int x = tid; x < top; x += 1024) out[x] = at[x];
 }
 
 // ---- attention of a single query per sequence ----
 
 // A workgroup has 4 waves, and a wave takes whole blocks: S = K.Q^T (64 tokens by 16 heads), the running softmax, O^T += V^T.P^T.
 // The pieces of a block go from memory to the matrix instructions without LDS or lane exchange: row m of S's tile t is token
-// 16 (m / 4) + 4 t + m % 4, so a lane's 16 weights are those of the 16 tokens whose values it loads for every column.
+// 16 (m / 4) + 4 t + m % 4, so a lane's 16 weights are those of the 16 tokens whose values it loads for every column.  Codes of 8
+// bits are exact in fp16; so is q relative to its largest value (what fp16 drops lies 2^-27 below it), and weights lose 2^-11
+// where bf16 would lose 2^-8.  What bounds it is memory: a wave has the keys of one block and the values of another on
+// their way while it computes.
 struct AttnArgs {
     CacheArgs c;
     const uint16_t* q;
     const int32_t* idx;    // [B,Hkv,top] or null: all blocks
-    int top, splits;
+    int top, splits, upw;  // parts of a row, units per wave
     float c2;
-    float *part_o, *part_m, *part_l;   // [B,Hkv,row groups,splits][16][D], [..][16]
-    float* weight;                     // [B,H,units]: log2 of a unit's share before the division; null: no masses
-    int units;                         // units per row at most
+    float* part_o;         // [B,H,splits][D]
+    float2* part_ml;       // [B,H,splits]: the largest logit (times log2 e), the sum
+    float* weight;         // [B,H,units]: log2 of a unit's share before the division; null: no masses
+    int units;             // units per row at most
     uint16_t* o;
     float* lse;
 };
 
+// 8 codes as fp16
 template <int FORMAT>
-__device__ __forceinline__ bf16x8 widen(unsigned lo, unsigned hi)
+__device__ __forceinline__ f16x8 widen(unsigned lo, unsigned hi)
 {
-    bf16x8 r;
     const unsigned w[2] = {lo, hi};
+    u32x4 r;
 #pragma unroll
     for (int x = 0; x < 2; x++) {
         if constexpr (FORMAT == SPARSEK_I8) {
-#pragma unroll
-            for (int e = 0; e < 4; e++) r[4 * x + e] = (__bf16)(float)((int)(w[x] << (24 - 8 * e)) >> 24);
+            // 0x6400 | b is 1024 + b for a byte b = code + 128
+            const unsigned y = w[x] ^ 0x80808080u;
+            const f16x2v off = {(_Float16)-1152.0f, (_Float16)-1152.0f};
+            r[2 * x] = __builtin_bit_cast(unsigned, __builtin_bit_cast(f16x2v, __builtin_amdgcn_perm(0x64646464u, y, 0x04010400u)) + off);
+            r[2 * x + 1] = __builtin_bit_cast(unsigned, __builtin_bit_cast(f16x2v, __builtin_amdgcn_perm(0x64646464u, y, 0x04030402u)) + off);
         } else {
-            const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[x], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[x], true);
-            r[4 * x] = (__bf16)a[0]; r[4 * x + 1] = (__bf16)a[1]; r[4 * x + 2] = (__bf16)b[0]; r[4 * x + 3] = (__bf16)b[1];
+            r[2 * x] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[x], 1.0f, false));
+            r[2 * x + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[x], 1.0f, true));
         }
     }
-    return r;
+    return __builtin_bit_cast(f16x8, r);
 }
 
 typedef float f32x4m __attribute__((ext_vector_type(4)));
 
-// What unit u of a row is: the place in the table, or -1 (no such block, one named before, a page outside the pool); the
-// unfinished block is the unit behind the others.
+// The units of a row: the whole blocks, or those that idx names and the one the query ends, if it does; and the unfinished block
+// behind them.
 struct RowUnits {
-    int whole, tail, nsel;   // whole blocks, tokens of the unfinished one, units that idx names (or whole)
+    int whole, tail, nsel;   // whole blocks, tokens of the unfinished one, units ahead of it
     int own;                 // with idx: the whole block that the query ends, -1: none
 };
 __device__ __forceinline__ RowUnits row_units(const AttnArgs& a, int b)
@@ -349,21 +412,55 @@ __device__ __forceinline__ RowUnits row_units(const AttnArgs& a, int b)
     r.nsel = a.idx ? a.top + (r.own >= 0 ? 1 : 0) : r.whole;
     return r;
 }
-// (wave-uniform u; all lanes)
-__device__ __forceinline__ int unit_block(const AttnArgs& a, const RowUnits& r, size_t bg, int u, int lane)
+// The place in the table of unit u < nsel, -1: none (no whole block behind the query's own, or one named before).
+__device__ __forceinline__ int unit_block(const AttnArgs& a, const RowUnits& r, size_t bg, int u)
 {
     if (!a.idx) return u;
     if (u == a.top) return r.own;
     const int32_t* row = a.idx + bg * a.top;
     const int x = row[u];
-    if (x < 0 || x >= (r.own >= 0 ? r.own : r.whole)) return -1;
-    bool seen = false;
-    for (int s = lane; s < u; s += 64) seen |= row[s] == x;
-    return __any(seen) ? -1 : x;
+    bool ok = x >= 0 && x < (r.own >= 0 ? r.own : r.whole);
+    for (int s = 0; s < u; s++) ok &= row[s] != x;
+    return ok ? x : -1;
+}
+
+// The running softmax over a unit's logits (in s, times log2 e): weights as the operand of the second product (times 2^15).
+struct SoftRow {
+    float m, l;
+};
+__device__ __forceinline__ float soft_unit(const f32x4m (&s)[4], SoftRow& row, f16x8 (&pb)[2], float& corr)
+{
+    float top = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 4; t++)
+#pragma unroll
+        for (int r = 0; r < 4; r++) top = fmaxf(top, s[t][r]);
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+    top = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto c = __builtin_amdgcn_permlane16_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+    top = fmaxf(__uint_as_float(c[0]), __uint_as_float(c[1]));
+    const float mx = fmaxf(row.m, top), ref = mx == -INFINITY ? 0.0f : mx;
+    corr = __builtin_amdgcn_exp2f(row.m - ref);
+    row.m = mx;
+    float sum = 0.0f;
+#pragma unroll
+    for (int t = 0; t < 4; t++)
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+            const float p = __builtin_amdgcn_exp2f(s[t][r] - (ref - 15.0f));
+            sum += p;
+            pb[t >> 1][4 * (t & 1) + r] = (_Float16)p;
+        }
+    const auto d = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
+    sum = __uint_as_float(d[0]) + __uint_as_float(d[1]);
+    const auto e = __builtin_amdgcn_permlane16_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
+    sum = __uint_as_float(e[0]) + __uint_as_float(e[1]);
+    row.l = fmaf(row.l, corr, sum);
+    return ref + log2f(sum * 0x1p-15f);   // log2 of the unit's share
 }
 
 template <int D, int FORMAT>
-__global__ __launch_bounds__(256, 2) void cache8_attn_kernel(AttnArgs a)
+__global__ __launch_bounds__(256, 3) void cache8_attn_kernel(AttnArgs a)
 {
     constexpr int KH = D / 64, NX = D / 16;
     __shared__ float so[4][16][D + 4], sm_[4][16], sl[4][16];
@@ -373,117 +470,170 @@ __global__ __launch_bounds__(256, 2) void cache8_attn_kernel(AttnArgs a)
     const size_t bg = (size_t)b * a.c.Hkv + g;
     const RowUnits ru = row_units(a, b);
     const int nu = ru.nsel + (ru.tail ? 1 : 0);
-    const int head = g * a.c.G + rg * 16 + col;
-    const bool live = rg * 16 + col < a.c.G;
-    const size_t prow = (bg * groups + rg) * a.splits + split;
-    // Q^T: head col, columns 64 half + 16 grp + 8 sub ..
-    bf16x8 qf[KH][2];
-    const uint16_t* qr = a.q + ((size_t)b * a.c.H + (live ? head : g * a.c.G)) * D;
+    if (split * 4 * a.upw >= nu) return;   // (the join leaves such parts out)
+    const int live = min(16, a.c.G - rg * 16);
+    const size_t head0 = (size_t)b * a.c.H + g * a.c.G + rg * 16;
+    // the wave's units, one to a lane: page (of any unit that has one where there is none), scales
+    const int u0 = split * 4 * a.upw + wv * a.upw, count = max(0, min(a.upw, ru.nsel - u0));
+    int page = -1;
+    if (lane < count) {
+        const int j = unit_block(a, ru, bg, u0 + lane);
+        if (j >= 0) page = a.c.t.table[bg * a.c.cap + j];
+        if (page >= a.c.pages) page = -1;
+    }
+    const unsigned long long have = __ballot(page >= 0);
+    const int some = have ? __builtin_amdgcn_readlane(page, __ffsll(have) - 1) : 0;
+    if (page < 0) page = some;
+    float ks = 0.0f, vs = 0.0f;
+    if (lane < count && have) {
+        ks = a.c.t.ks[page];
+        vs = a.c.t.vs[page];
+    }
+    // Q^T: head col, columns 64 half + 16 grp + 8 sub .., relative to the head's largest value
+    const uint16_t* qr = a.q + (head0 + min(col, live - 1)) * D + 16 * grp;
+    u32x4 qw[KH][2];
+    unsigned top = 0;
 #pragma unroll
     for (int h = 0; h < KH; h++)
 #pragma unroll
-        for (int s = 0; s < 2; s++) qf[h][s] = *(const bf16x8*)(qr + 64 * h + 16 * grp + 8 * s);
+        for (int s = 0; s < 2; s++) {
+            qw[h][s] = *(const u32x4*)(qr + 64 * h + 8 * s);
+#pragma unroll
+            for (int e = 0; e < 4; e++) top = max(top, max(qw[h][s][e] << 16 & 0x7FFFFFFFu, qw[h][s][e] & 0x7FFF0000u));
+        }
+    top = max(top, (unsigned)__shfl_xor((int)top, 16, 64));
+    top = max(top, (unsigned)__shfl_xor((int)top, 32, 64));
+    const int E = scale_exp(top);
+    const float down = scale_down(E), c2q = a.c2 * scale_up(E);
+    f16x8 qf[KH][2];
+#pragma unroll
+    for (int h = 0; h < KH; h++)
+#pragma unroll
+        for (int s = 0; s < 2; s++)
+#pragma unroll
+            for (int e = 0; e < 8; e++) qf[h][s][e] = (_Float16)(half_of(qw[h][s], e) * down);
     f32x4m acc[NX];
 #pragma unroll
     for (int x = 0; x < NX; x++) acc[x] = f32x4m{0, 0, 0, 0};
-    float m = -INFINITY, l = 0.0f;
-    for (int u = split * 4 + wv; u < nu; u += a.splits * 4) {
-        f32x4m s[4];
-        float vscale = 1.0f;
-        const bool tail = u == ru.nsel;
-        const unsigned char* vp = nullptr;
-        bool skip = false;
-        if (!tail) {
-            const int j = unit_block(a, ru, bg, u, lane);
-            const int page = j >= 0 ? a.c.t.table[bg * a.c.cap + j] : -1;
-            skip = page < 0 || page >= a.c.pages;
-            if (!skip) {
-                const unsigned char* kp = (const unsigned char*)a.c.t.k8 + (size_t)page * BT * D + (16 * (col >> 2) + (col & 3)) * D + 16 * grp;
-                const float ks = a.c.t.ks[page] * a.c2;
-                vscale = a.c.t.vs[page];
-                vp = (const unsigned char*)a.c.t.v8 + (size_t)page * BT * D + col * BT + 16 * grp;
+    SoftRow row = {-INFINITY, 0.0f};
+    // the weights of the live heads' units; the other lanes' lie outside the buffer
+    const buffer_t wbuf = buffer_of(a.weight ? a.weight + head0 * a.units : nullptr, a.weight ? live * a.units * 4 : 0);
+    const int wat = grp == 0 && col < live ? col * a.units * 4 : 0x7FFFFF00;
+    if (have) {
+        const int kat = (16 * (col >> 2) + (col & 3)) * D + 16 * grp, vat = col * BT + 16 * grp;
+        u32x4 kw[4][KH], vw[NX];
+        auto load_k = [&](int i) {
+            const unsigned char* kp = (const unsigned char*)a.c.t.k8 + (size_t)__builtin_amdgcn_readlane(page, i) * (BT * D) + kat;
 #pragma unroll
-                for (int t = 0; t < 4; t++) {
-                    s[t] = f32x4m{0, 0, 0, 0};
+            for (int t = 0; t < 4; t++)
 #pragma unroll
-                    for (int h = 0; h < KH; h++) {
-                        const u32x4 w = *(const u32x4*)(kp + 4 * t * D + 64 * h);
-                        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen<FORMAT>(w[0], w[1]), qf[h][0], s[t], 0, 0, 0);
-                        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen<FORMAT>(w[2], w[3]), qf[h][1], s[t], 0, 0, 0);
-                    }
-                    s[t] *= ks;
-                }
-            }
-        } else {
-            const uint16_t* kp = (const uint16_t*)a.c.t.kt + bg * BT * D;
+                for (int h = 0; h < KH; h++) kw[t][h] = *(const u32x4*)(kp + 4 * t * D + 64 * h);
+        };
+        auto load_v = [&](int i) {
+            const unsigned char* vp = (const unsigned char*)a.c.t.v8 + (size_t)__builtin_amdgcn_readlane(page, i) * (BT * D) + vat;
+#pragma unroll
+            for (int x = 0; x < NX; x++) vw[x] = *(const u32x4*)(vp + 16 * x * BT);
+        };
+        load_k(0);
+        load_v(0);
+        for (int i = 0; i < count; i++) {
+            const float f = readlane_f32(ks, i) * c2q, vscale = readlane_f32(vs, i);
+            const bool there = have >> i & 1;
+            f32x4m s[4];
 #pragma unroll
             for (int t = 0; t < 4; t++) {
                 s[t] = f32x4m{0, 0, 0, 0};
-                const int tok = min(16 * (col >> 2) + 4 * t + (col & 3), ru.tail - 1);
 #pragma unroll
-                for (int h = 0; h < KH; h++)
-#pragma unroll
-                    for (int x = 0; x < 2; x++)
-                        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8*)(kp + tok * D + 64 * h + 16 * grp + 8 * x), qf[h][x], s[t], 0, 0, 0);
-#pragma unroll
-                for (int r = 0; r < 4; r++) s[t][r] = 16 * grp + 4 * t + r < ru.tail ? s[t][r] * a.c2 : -INFINITY;
-            }
-        }
-        if (skip) {
-            if (a.weight && live && grp == 0) a.weight[((size_t)b * a.c.H + head) * a.units + u] = -INFINITY;
-            continue;
-        }
-        float top = -INFINITY;
-#pragma unroll
-        for (int t = 0; t < 4; t++)
-#pragma unroll
-            for (int r = 0; r < 4; r++) top = fmaxf(top, s[t][r]);
-        top = fmaxf(top, __shfl_xor(top, 16, 64));
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
-        const float mx = fmaxf(m, top), mn = mx == -INFINITY ? 0.0f : mx, corr = __builtin_amdgcn_exp2f(m - mn);
-        m = mx;
-        float sum = 0.0f;
-        bf16x8 pb[2];
-#pragma unroll
-        for (int t = 0; t < 4; t++)
-#pragma unroll
-            for (int r = 0; r < 4; r++) {
-                const float p = __builtin_amdgcn_exp2f(s[t][r] - mn);
-                sum += p;
-                pb[t >> 1][4 * (t & 1) + r] = (__bf16)(p * vscale);   // the operand of the second product: 2^-9 of every weight
-            }
-        sum += __shfl_xor(sum, 16, 64);
-        sum += __shfl_xor(sum, 32, 64);
-        if (a.weight && live && grp == 0) a.weight[((size_t)b * a.c.H + head) * a.units + u] = mn + log2f(sum);
-        l = l * corr + sum;
-#pragma unroll
-        for (int x = 0; x < NX; x++) {
-            acc[x] *= corr;
-            if (!tail) {
-                const u32x4 w = *(const u32x4*)(vp + 16 * x * BT);
-                acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen<FORMAT>(w[0], w[1]), pb[0], acc[x], 0, 0, 0);
-                acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen<FORMAT>(w[2], w[3]), pb[1], acc[x], 0, 0, 0);
-            } else {
-                const uint16_t* vr = (const uint16_t*)a.c.t.vt + (bg * D + 16 * x + col) * BT + 16 * grp;
-#pragma unroll
-                for (int y = 0; y < 2; y++) {
-                    u32x4 w = *(const u32x4*)(vr + 8 * y);
-#pragma unroll
-                    for (int e = 0; e < 4; e++) {   // what lies behind the last token may be anything
-                        const int tok = 16 * grp + 8 * y + 2 * e;
-                        w[e] = tok + 1 < ru.tail ? w[e] : tok < ru.tail ? w[e] & 0xFFFFu : 0u;
-                    }
-                    acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), pb[y], acc[x], 0, 0, 0);
+                for (int h = 0; h < KH; h++) {
+                    s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen<FORMAT>(kw[t][h][0], kw[t][h][1]), qf[h][0], s[t], 0, 0, 0);
+                    s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen<FORMAT>(kw[t][h][2], kw[t][h][3]), qf[h][1], s[t], 0, 0, 0);
                 }
             }
+            load_k(min(i + 1, count - 1));
+#pragma unroll
+            for (int t = 0; t < 4; t++)
+#pragma unroll
+                for (int r = 0; r < 4; r++) s[t][r] = there ? s[t][r] * f : -INFINITY;
+            f16x8 pb[2];
+            float corr;
+            const float share = soft_unit(s, row, pb, corr);
+            __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(share), wbuf, wat + 4 * (u0 + i), 0, 0);
+#pragma unroll
+            for (int x = 0; x < NX; x++) {
+                f32x4m y = {0, 0, 0, 0};
+                y = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen<FORMAT>(vw[x][0], vw[x][1]), pb[0], y, 0, 0, 0);
+                y = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen<FORMAT>(vw[x][2], vw[x][3]), pb[1], y, 0, 0, 0);
+#pragma unroll
+                for (int r = 0; r < 4; r++) acc[x][r] = fmaf(acc[x][r], corr, vscale * y[r]);
+            }
+            load_v(min(i + 1, count - 1));
+        }
+    } else {   // nothing to attend: the units have no share
+        for (int i = 0; i < count; i++) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(-INFINITY), wbuf, wat + 4 * (u0 + i), 0, 0);
+    }
+    if (ru.tail && ru.nsel >= u0 && ru.nsel < u0 + a.upw) {   // the unfinished block, in bf16
+        const uint16_t *kp = (const uint16_t*)a.c.t.kt + bg * BT * D, *vp = (const uint16_t*)a.c.t.vt + (bg * D + col) * BT + 16 * grp;
+        f32x4m s[4];
+#pragma unroll
+        for (int t = 0; t < 4; t++) {
+            s[t] = f32x4m{0, 0, 0, 0};
+            const int tok = min(16 * (col >> 2) + 4 * t + (col & 3), ru.tail - 1);
+#pragma unroll
+            for (int h = 0; h < KH; h++)
+#pragma unroll
+                for (int x = 0; x < 2; x++)
+                    s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8*)(kp + tok * D + 64 * h + 16 * grp + 8 * x), *(const bf16x8*)(qr + 64 * h + 8 * x), s[t], 0, 0, 0);
+#pragma unroll
+            for (int r = 0; r < 4; r++) s[t][r] = 16 * grp + 4 * t + r < ru.tail ? s[t][r] * a.c2 : -INFINITY;
+        }
+        // values to fp16, relative to the largest of them; what lies behind the last token may be anything and becomes 0
+        auto values = [&](int x, int y) {
+            u32x4 w = *(const u32x4*)(vp + 16 * x * BT + 8 * y);
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const int tok = 16 * grp + 8 * y + 2 * e;
+                w[e] = tok + 1 < ru.tail ? w[e] : tok < ru.tail ? w[e] & 0xFFFFu : 0u;
+            }
+            return w;
+        };
+        unsigned most = 0;
+#pragma unroll
+        for (int x = 0; x < NX; x++)
+#pragma unroll
+            for (int y = 0; y < 2; y++) {
+                const u32x4 w = values(x, y);
+#pragma unroll
+                for (int e = 0; e < 4; e++) most = max(most, max(w[e] << 16 & 0x7FFFFFFFu, w[e] & 0x7FFF0000u));
+            }
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) most = max(most, (unsigned)__shfl_xor((int)most, d, 64));
+        const int F = scale_exp(most);
+        const float vdown = scale_down(F), vup = scale_up(F);
+        f16x8 pb[2];
+        float corr;
+        const float share = soft_unit(s, row, pb, corr);
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(share), wbuf, wat + 4 * ru.nsel, 0, 0);
+#pragma unroll
+        for (int x = 0; x < NX; x++) {
+            f32x4m y = {0, 0, 0, 0};
+#pragma unroll
+            for (int z = 0; z < 2; z++) {
+                const u32x4 w = values(x, z);
+                f16x8 v;
+#pragma unroll
+                for (int e = 0; e < 8; e++) v[e] = (_Float16)(half_of(w, e) * vdown);
+                y = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pb[z], y, 0, 0, 0);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; r++) acc[x][r] = fmaf(acc[x][r], corr, vup * y[r]);
         }
     }
     // the four waves' results are joined; rows 4 grp + r of tile x are columns of the head
-    if (grp == 0) { sm_[wv][col] = m; sl[wv][col] = l; }
+    if (grp == 0) { sm_[wv][col] = row.m; sl[wv][col] = row.l; }
 #pragma unroll
     for (int x = 0; x < NX; x++) *(f32x4m*)&so[wv][col][16 * x + 4 * grp] = acc[x];
     __syncthreads();
-    for (int x = tid; x < 16 * D; x += 256) {
+    for (int x = tid; x < live * D; x += 256) {
         const int h = x / D, d = x % D;
         const float M = fmaxf(fmaxf(sm_[0][h], sm_[1][h]), fmaxf(sm_[2][h], sm_[3][h]));
         float sum = 0.0f, den = 0.0f;
@@ -493,57 +643,105 @@ __global__ __launch_bounds__(256, 2) void cache8_attn_kernel(AttnArgs a)
             sum += f * so[w][h][d];
             den += f * sl[w][h];
         }
-        a.part_o[prow * 16 * D + x] = sum;
-        if (d == 0) {
-            a.part_m[prow * 16 + h] = M;
-            a.part_l[prow * 16 + h] = den;
-        }
+        const size_t at = (head0 + h) * a.splits + split;
+        a.part_o[at * D + d] = sum;
+        if (d == 0) a.part_ml[at] = make_float2(M, den);
     }
 }
 
-// The splits of a head are joined (workgroups 0 .. H-1 of a sequence), and the shares of its blocks join the masses (the others).
+// The parts of a head are joined (workgroups 0 .. H-1 of a sequence), and the shares of its blocks join the masses (the others).
 template <int D>
 __global__ __launch_bounds__(256) void cache8_join_kernel(AttnArgs a, int mass_wgs)
 {
-    const int tid = threadIdx.x, b = blockIdx.y, G = a.c.G, groups = (G + 15) / 16;
-    auto total = [&](int h, float& M, float& L) {   // of head h
-        const int g = h / G, r = h % G;
-        const size_t p0 = (((size_t)b * a.c.Hkv + g) * groups + r / 16) * a.splits;
-        M = -INFINITY;
-        for (int s = 0; s < a.splits; s++) M = fmaxf(M, a.part_m[(p0 + s) * 16 + r % 16]);
-        L = 0.0f;
-        if (M > -INFINITY)
-            for (int s = 0; s < a.splits; s++) L += a.part_l[(p0 + s) * 16 + r % 16] * __builtin_amdgcn_exp2f(a.part_m[(p0 + s) * 16 + r % 16] - M);
-    };
-    if ((int)blockIdx.x < a.c.H) {
-        const int h = blockIdx.x, g = h / G, r = h % G;
-        const size_t p0 = (((size_t)b * a.c.Hkv + g) * groups + r / 16) * a.splits;
-        float M, L;
-        total(h, M, L);
-        if (tid < D) {
-            float sum = 0.0f;
-            if (M > -INFINITY)
-                for (int s = 0; s < a.splits; s++) {
-                    const float m = a.part_m[(p0 + s) * 16 + r % 16];
-                    if (m > -INFINITY) sum += a.part_o[((p0 + s) * 16 + r % 16) * D + tid] * __builtin_amdgcn_exp2f(m - M);
-                }
-            a.o[((size_t)b * a.c.H + h) * D + tid] = f32_to_bf16(L > 0.0f ? sum / L : M > -INFINITY ? sum : 0.0f);
+    constexpr int EPL = D / 64, UNR = 8;   // columns per lane
+    __shared__ float red[4][D], ms[4], ls[4], logs[4];
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, b = blockIdx.y, G = a.c.G;
+    const RowUnits ru = row_units(a, b);
+    const int nu = ru.nsel + (ru.tail ? 1 : 0), splits = (nu + 4 * a.upw - 1) / (4 * a.upw);
+    if ((int)blockIdx.x < a.c.H) {   // a wave takes every fourth part, 8 of them under way together
+        const size_t row = (size_t)b * a.c.H + blockIdx.x;
+        const float2* ml = a.part_ml + row * a.splits;
+        const float* po = a.part_o + row * a.splits * D + EPL * lane;
+        float M = -INFINITY, L = 0.0f, sum[EPL];
+#pragma unroll
+        for (int e = 0; e < EPL; e++) sum[e] = 0.0f;
+        for (int s0 = wv; s0 < splits; s0 += 4 * UNR) {
+            float2 p[UNR];
+            float x[UNR][EPL];
+#pragma unroll
+            for (int u = 0; u < UNR; u++) {
+                const int s = min(s0 + 4 * u, splits - 1);
+                p[u] = ml[s];
+#pragma unroll
+                for (int e = 0; e < EPL; e++) x[u][e] = po[(size_t)s * D + e];
+            }
+            float top = M;
+#pragma unroll
+            for (int u = 0; u < UNR; u++) {
+                if (s0 + 4 * u >= splits) p[u].x = -INFINITY;
+                top = fmaxf(top, p[u].x);
+            }
+            if (top == -INFINITY) continue;
+            const float corr = __builtin_amdgcn_exp2f(M - top);
+            M = top;
+            L *= corr;
+#pragma unroll
+            for (int e = 0; e < EPL; e++) sum[e] *= corr;
+#pragma unroll
+            for (int u = 0; u < UNR; u++) {
+                if (p[u].x == -INFINITY) continue;   // (a part without keys)
+                const float w = __builtin_amdgcn_exp2f(p[u].x - top);
+                L = fmaf(w, p[u].y, L);
+#pragma unroll
+                for (int e = 0; e < EPL; e++) sum[e] = fmaf(w, x[u][e], sum[e]);
+            }
         }
-        if (tid == 0) a.lse[(size_t)b * a.c.H + h] = M > -INFINITY ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+        if (lane == 0) { ms[wv] = M; ls[wv] = L; }
+#pragma unroll
+        for (int e = 0; e < EPL; e++) red[wv][EPL * lane + e] = sum[e];
+        __syncthreads();
+        const float top = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3]));
+        float all = 0.0f, y = 0.0f;
+        if (top > -INFINITY)
+#pragma unroll
+            for (int w = 0; w < 4; w++) {
+                const float f = __builtin_amdgcn_exp2f(ms[w] - top);
+                all = fmaf(f, ls[w], all);
+                if (tid < D) y = fmaf(f, red[w][tid], y);
+            }
+        if (tid < D) a.o[row * D + tid] = f32_to_bf16(top > -INFINITY ? y / all : 0.0f);
+        if (tid == 0) a.lse[row] = top > -INFINITY ? (top + log2f(all * 0x1p-15f)) * 0.6931471805599453f : -INFINITY;
         return;
     }
+    auto total = [&](int h, float& M, float& L) {   // of head h, by a wave
+        const float2* p = a.part_ml + ((size_t)b * a.c.H + h) * a.splits;
+        M = -INFINITY;
+        L = 0.0f;
+        for (int s = lane; s < splits; s += 64) M = fmaxf(M, p[s].x);
+        M = wave_max_f32(M);
+        for (int s = lane; s < splits; s += 64) L += M > -INFINITY ? p[s].y * __builtin_amdgcn_exp2f(p[s].x - M) : 0.0f;
+        L = wave_sum_f32(L);
+    };
     const int g = (blockIdx.x - a.c.H) / mass_wgs, part = (blockIdx.x - a.c.H) % mass_wgs;
-    const size_t bg = (size_t)b * a.c.Hkv + g;
-    const RowUnits ru = row_units(a, b);
-    const int nu = ru.nsel + (ru.tail ? 1 : 0);
     if (part * 256 >= nu) return;
+    const size_t bg = (size_t)b * a.c.Hkv + g;
     const int u = part * 256 + tid;
     float sum = 0.0f;
-    for (int r = 0; r < G; r++) {
-        float M, L;
-        total(g * G + r, M, L);
-        const float w = u < nu ? a.weight[((size_t)b * a.c.H + g * G + r) * a.units + u] : -INFINITY;
-        if (w > -INFINITY) sum += __builtin_amdgcn_exp2f(w - (M + log2f(L)));
+    for (int r0 = 0; r0 < G; r0 += 4) {   // a wave per head
+        __syncthreads();
+        if (r0 + wv < G) {
+            float M, L;
+            total(g * G + r0 + wv, M, L);
+            if (lane == 0) logs[wv] = M + log2f(L * 0x1p-15f);
+        }
+        __syncthreads();
+        if (u < nu)
+#pragma unroll
+            for (int x = 0; x < 4; x++)
+                if (r0 + x < G) {
+                    const float w = a.weight[((size_t)b * a.c.H + g * G + r0 + x) * a.units + u];
+                    if (w > -INFINITY) sum += __builtin_amdgcn_exp2f(w - logs[x]);
+                }
     }
     if (u < nu) {
         const int j = u == ru.nsel ? ru.whole : !a.idx ? u : u == a.top ? ru.own : a.idx[bg * a.top + u];
@@ -554,37 +752,39 @@ __global__ __launch_bounds__(256) void cache8_join_kernel(AttnArgs a, int mass_w
 
 // ---- eviction ----
 
-__global__ __launch_bounds__(1024) void cache8_evict_kernel(CacheArgs a, int budget, int sink, int recent, int32_t* table, float* mass, int32_t* lens)
+__global__ __launch_bounds__(256) void cache8_evict_kernel(CacheArgs a, int budget, int sink, int recent, int32_t* __restrict__ table,
+                                                           float* __restrict__ mass, int32_t* __restrict__ lens)
 {
-    extern __shared__ unsigned keys[];
-    __shared__ TopSmem sm;
+    extern __shared__ unsigned keys[];   // [cap], and the order [cap]
+    int* order = (int*)(keys + a.cap);
+    __shared__ __attribute__((aligned(16))) TopSmem<256> sm;
     const int tid = threadIdx.x, bg = blockIdx.x, b = bg / a.Hkv, cap = a.cap;
     const int len = clamp_len(a.lens[b], cap), nb = len / BT;
     const size_t row = (size_t)bg * cap;
+    const int32_t* table_in = a.t.table + row;
+    const float* mass_in = a.t.mass + row;
+    if (bg % a.Hkv == 0 && tid == 0) lens[b] = min(nb, budget) * BT + len % BT;
     if (nb <= budget) {
-        for (int x = tid; x < cap; x += 1024) {
-            table[row + x] = a.t.table[row + x];
-            mass[row + x] = a.t.mass[row + x];
+        for (int x = tid; x < cap; x += 256) {
+            table[row + x] = table_in[x];
+            mass[row + x] = mass_in[x];
         }
-        if (bg % a.Hkv == 0 && tid == 0) lens[b] = len;
         return;
     }
-    const float tail = nb < cap ? a.t.mass[row + nb] : 0.0f;
-    for (int x = tid; x < nb; x += 1024)
-        keys[x] = x < sink || x >= nb - recent ? 0xFFFFFFFFu : min(score_key(a.t.mass[row + x]), 0xFFFFFFFEu);
-    __syncthreads();
-    unsigned thr, equal;
-    if (budget > 0) top_threshold(sm, keys, nb, budget, thr, equal);
-    else { thr = 0xFFFFFFFFu; equal = 0; }
-    top_emit(sm, keys, nb, thr, equal, [&](int x, bool in, int place) {
-        table[row + (in ? place : budget + place)] = a.t.table[row + x];
-        if (in) mass[row + place] = a.t.mass[row + x];
-    });
-    for (int x = budget + tid; x < cap; x += 1024) {
-        mass[row + x] = x == budget ? tail : 0.0f;
-        if (x >= nb) table[row + x] = a.t.table[row + x];
+#pragma unroll 8
+    for (int x = tid; x < nb; x += 256) {
+        const float m = mass_in[x];
+        keys[x] = x < sink || x >= nb - recent ? 0xFFFFFFFFu : min(max(score_key(m), 1u), 0xFFFFFFFEu);
     }
-    if (bg % a.Hkv == 0 && tid == 0) lens[b] = budget * BT + len % BT;
+    __syncthreads();
+    const TopBounds t = budget > 0 ? wg_top(sm, keys, nb, (unsigned)budget) : TopBounds{0xFFFFFFFFu, 0u};
+    wg_order(sm, keys, nb, t, budget, order);
+#pragma unroll 4
+    for (int x = tid; x < cap; x += 256) {
+        const int y = x < nb ? order[x] : x;
+        table[row + x] = table_in[y];
+        mass[row + x] = x < budget ? mass_in[y] : x == budget && nb < cap ? mass_in[nb] : 0.0f;   // (the unfinished block's goes along)
+    }
 }
 
 // ---- launches ----
@@ -614,29 +814,30 @@ int launch_cache8_append(const sparsek_cache8_cfg& c, const sparsek_cache8& t, c
 int launch_cache8_select(const sparsek_cache8_cfg& c, const sparsek_cache8& t, const int32_t* lens, const void* q, int top, int32_t* idx, hipStream_t st)
 {
     const CacheArgs a = cache_args(c, t, lens);
-    const size_t lds = (size_t)c.cap * 4;
+    const size_t lds = (size_t)c.cap * 8;
     if (c.d == 128) hipLaunchKernelGGL((cache8_select_kernel<128>), dim3(c.B * c.Hkv), dim3(1024), lds, st, a, (const uint16_t*)q, top, idx);
     else hipLaunchKernelGGL((cache8_select_kernel<64>), dim3(c.B * c.Hkv), dim3(1024), lds, st, a, (const uint16_t*)q, top, idx);
     return launch_status();
 }
 
 struct Cache8Layout {
-    int units, splits, groups;
-    size_t part_o, part_m, part_l, weight, bytes;
+    int units, splits, upw, groups;
+    size_t part_o, part_ml, weight, bytes;
 };
 static Cache8Layout cache8_layout(const sparsek_cache8_cfg& c, int top)
 {
     Cache8Layout y;
     y.units = (top ? top : c.cap) + 1;   // and the query's own block
     y.groups = (c.H / c.Hkv + 15) / 16;
-    // enough workgroups for two on each of 256 compute units, and at least one unit for every wave
-    const long long rows = (long long)c.B * c.Hkv * y.groups;
-    y.splits = (int)std::max<long long>(1, std::min<long long>((512 + rows - 1) / rows, (y.units + 3) / 4));
-    const size_t parts = (size_t)rows * y.splits * 16;
+    // Units per wave: as many as leave 8 waves for each of 256 compute units, 4 at most (sequences are shorter than the longest, and
+    // the waves that they leave idle weigh less the fewer units each has: 64 sequences of up to 8192 159 us with 16, 155 with 4).
+    const long long all = (long long)c.B * c.Hkv * y.groups * y.units;
+    y.upw = (int)std::max<long long>(1, std::min<long long>(4, all / 2048));
+    y.splits = (y.units + 4 * y.upw - 1) / (4 * y.upw);
+    const size_t parts = (size_t)c.B * c.H * y.splits;
     y.part_o = 0;
-    y.part_m = align_up(parts * c.d * 4, 256);
-    y.part_l = y.part_m + align_up(parts * 4, 256);
-    y.weight = y.part_l + align_up(parts * 4, 256);
+    y.part_ml = align_up(parts * c.d * 4, 256);
+    y.weight = y.part_ml + align_up(parts * 8, 256);
     y.bytes = y.weight + align_up((size_t)c.B * c.H * y.units * 4, 256);
     return y;
 }
@@ -652,9 +853,10 @@ int launch_cache8_attn(const sparsek_cache8_cfg& c, const sparsek_cache8& t, con
     a.idx = idx;
     a.top = idx ? top : 0;
     a.splits = y.splits;
+    a.upw = y.upw;
     a.c2 = c.softmax_scale * 1.4426950408889634f;
     char* w = (char*)ws;
-    a.part_o = (float*)(w + y.part_o); a.part_m = (float*)(w + y.part_m); a.part_l = (float*)(w + y.part_l);
+    a.part_o = (float*)(w + y.part_o); a.part_ml = (float2*)(w + y.part_ml);
     a.weight = accumulate ? (float*)(w + y.weight) : nullptr;
     a.units = y.units;
     a.o = (uint16_t*)o;
@@ -673,7 +875,7 @@ int launch_cache8_evict(const sparsek_cache8_cfg& c, const sparsek_cache8& t, co
                         int32_t* table, float* mass, int32_t* lens_out, hipStream_t st)
 {
     const CacheArgs a = cache_args(c, t, lens);
-    hipLaunchKernelGGL(cache8_evict_kernel, dim3(c.B * c.Hkv), dim3(1024), (size_t)c.cap * 4, st, a, budget, sink, recent, table, mass, lens_out);
+hipLaunchKernelGGL(cache8_evict_kernel, dim3(c.B * c.Hkv), dim3(256), (size_t)c.cap * 8, st, a, budget, sink, recent, table, mass, lens_out);
     return launch_status();
 }
 

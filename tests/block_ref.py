@@ -2,7 +2,7 @@
 on how far a kernel's results may be from them.
 
 A value rounded to bf16 is off by at most 2^-8 of itself (half a step), one rounded to fp16 by 2^-11.  The kernels round every
-output once to bf16; the weights p to fp16 in the forward and to bf16 in the backward and over the cache, the score gradients ds to bf16, and
+output once to bf16; the weights p to fp16 in the forward and over the cache and to bf16 in the backward, the score gradients ds to bf16, and
 partial results to fp16 relative to the largest value of their block; sums are fp32 (d products of 2^-24 each; 2^-14 covers them and the exponentials with room, for logits below 2^5)."""
 import numpy as np
 import torch
@@ -166,7 +166,7 @@ def cache_attn(cache, lens, q, idx=None):
                 lse[b, h] = torch.logsumexp(s, 0)
                 p = torch.exp(s - lse[b, h])
                 o[b, h] = p @ V
-                ob[b, h] = 2 ** -8 * o[b, h].abs() + (2 ** -8 + 2 ** -14) * (p @ V.abs()) + 1e-30
+                ob[b, h] = 2 ** -8 * o[b, h].abs() + (2 ** -11 + 2 ** -14) * (p @ V.abs()) + 1e-30
                 mass[b, g].index_add_(0, at, p)
     return o, lse, mass[:, :, :cache.cap], ob
 
