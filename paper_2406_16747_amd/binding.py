@@ -481,29 +481,24 @@ def sparsek_decode_status(state):
 
 # ---- attention over blocks of 64 tokens that a cheap score selects ----
 
-def _same(tensors, dtype, shape, device):
-    """Every named tensor is contiguous, of that type and shape, and on that device."""
-    for name, t in tensors:
-        if t.dtype is not dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_contiguous():
-            raise ValueError("%s must be a contiguous %s tensor of shape %s on %s, got %s %s on %s%s" % (
-                name, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device, "" if t.is_contiguous() else " (strided)"))
+def _same(name, t, dtype, shape, device):
+    """The tensor is contiguous, of that type and shape, and on that device."""
+    if t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of shape %s on %s, got %s %s on %s%s" % (
+            name, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device, "" if t.is_contiguous() else " (strided)"))
 
 
-class _On:
-    """Calls made for the device that the tensors are on, on its current stream."""
-
-    def __init__(self, device):
-        if device.type != "cuda":
-            raise ValueError("the tensors must be on the GPU, got %s" % device)
-        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
-
-    def __enter__(self):
-        if self.guard:
-            self.guard.__enter__()
-
-    def __exit__(self, *a):
-        if self.guard:
-            self.guard.__exit__(*a)
+def _on(device, f, *args):
+    """f(*args, stream) for the device that the tensors are on, on its current stream."""
+    if device.type != "cuda":
+        raise ValueError("the tensors must be on the GPU, got %s" % device)
+    if device.index == torch.cuda.current_device():
+        rc = f(*args, _raw_stream())
+    else:
+        with torch.cuda.device(device):
+            rc = f(*args, _raw_stream())
+    if rc:
+        check(rc)
 
 
 def _make_block_cfg(B, H, Hkv, n, d, top, dtype, scale):
@@ -514,8 +509,8 @@ def _block_kept(q, k, top, scale):
     if q.dim() != 4 or k.dim() != 4:
         raise ValueError("q is [B,H,n,d] and k, v are [B,Hkv,n,d]")
     B, H, n, d = q.shape
-    _same([("q", q)], torch.bfloat16, (B, H, n, d), q.device)
-    _same([("k", k)], torch.bfloat16, (B, k.shape[1], n, d), q.device)
+    _same("q", q, torch.bfloat16, (B, H, n, d), q.device)
+    _same("k", k, torch.bfloat16, (B, k.shape[1], n, d), q.device)
     return _kept("block", (B, H, k.shape[1], n, d, int(top), BF16, float(scale)), _make_block_cfg)
 
 
@@ -533,17 +528,17 @@ def sparsek_block_select(q, k, top, ws=None):
     the largest cheap scores, ascending, padded with -1; the query heads of a key/value head share them."""
     torch = _torch()
     cfg = _block_kept(q, k, top, 1.0)
-    with _On(q.device):
-        idx = torch.empty(q.shape[0], k.shape[1], q.shape[2], max(int(top), 0), dtype=torch.int32, device=q.device)
-        ws, nbytes = _block_ws(cfg, "sparsek_block_select_workspace_bytes", ws, q.device)
-        check(lib().sparsek_block_select(cfg[0], q.data_ptr(), k.data_ptr(), idx.data_ptr(), ws.data_ptr(), nbytes, _raw_stream()))
+    idx = torch.empty(q.shape[0], k.shape[1], q.shape[2], max(int(top), 0), dtype=torch.int32, device=q.device)
+    ws, nbytes = _block_ws(cfg, "sparsek_block_select_workspace_bytes", ws, q.device)
+    _on(q.device, lib().sparsek_block_select, cfg[0], q.data_ptr(), k.data_ptr(), idx.data_ptr(), ws.data_ptr(), nbytes)
     return idx
 
 
-def _block_idx(idx, q, k):
+def _block_rest(q, k, v, idx):
     if idx.dim() != 4:
         raise ValueError("idx is [B,Hkv,n,top]")
-    _same([("idx", idx)], torch.int32, (q.shape[0], k.shape[1], q.shape[2], idx.shape[3]), q.device)
+    _same("idx", idx, torch.int32, (q.shape[0], k.shape[1], q.shape[2], idx.shape[3]), q.device)
+    _same("v", v, torch.bfloat16, k.shape, q.device)
 
 
 def sparsek_block_attn_fwd(q, k, v, idx, scale, mass=False, ws=None):
@@ -551,15 +546,13 @@ def sparsek_block_attn_fwd(q, k, v, idx, scale, mass=False, ws=None):
     mass=True also the weight that each block got, [B,Hkv,ceil(n/64)] fp32."""
     torch = _torch()
     cfg = _block_kept(q, k, idx.shape[-1], scale)
-    _block_idx(idx, q, k)
-    _same([("v", v)], torch.bfloat16, k.shape, q.device)
-    with _On(q.device):
-        o = torch.empty_like(q)
-        lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device)
-        m = torch.empty(k.shape[0], k.shape[1], -(-k.shape[2] // BLOCK_TOKENS), dtype=torch.float32, device=q.device) if mass else None
-        ws, nbytes = _block_ws(cfg, "sparsek_block_attn_fwd_workspace_bytes", ws, q.device)
-        check(lib().sparsek_block_attn_fwd(cfg[0], q.data_ptr(), k.data_ptr(), v.data_ptr(), idx.data_ptr(), o.data_ptr(),
-                                           lse.data_ptr(), _ptr(m), ws.data_ptr(), nbytes, _raw_stream()))
+    _block_rest(q, k, v, idx)
+    o = torch.empty_like(q)
+    lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device)
+    m = torch.empty(k.shape[0], k.shape[1], -(-k.shape[2] // BLOCK_TOKENS), dtype=torch.float32, device=q.device) if mass else None
+    ws, nbytes = _block_ws(cfg, "sparsek_block_attn_fwd_workspace_bytes", ws, q.device)
+    _on(q.device, lib().sparsek_block_attn_fwd, cfg[0], q.data_ptr(), k.data_ptr(), v.data_ptr(), idx.data_ptr(), o.data_ptr(),
+        lse.data_ptr(), _ptr(m), ws.data_ptr(), nbytes)
     return (o, lse, m) if mass else (o, lse)
 
 
@@ -567,16 +560,14 @@ def sparsek_block_attn_bwd(q, k, v, idx, o, lse, dO, scale, ws=None):
     """dq [B,H,n,d], dk, dv [B,Hkv,n,d]: gradients of sum(dO*o) for the outputs o, lse of sparsek_block_attn_fwd, the selection held fixed."""
     torch = _torch()
     cfg = _block_kept(q, k, idx.shape[-1], scale)
-    _block_idx(idx, q, k)
-    _same([("v", v)], torch.bfloat16, k.shape, q.device)
-    _same([("o", o), ("dO", dO)], torch.bfloat16, q.shape, q.device)
-    _same([("lse", lse)], torch.float32, q.shape[:3], q.device)
-    with _On(q.device):
-        dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
-        ws, nbytes = _block_ws(cfg, "sparsek_block_attn_bwd_workspace_bytes", ws, q.device)
-        check(lib().sparsek_block_attn_bwd(cfg[0], q.data_ptr(), k.data_ptr(), v.data_ptr(), idx.data_ptr(), o.data_ptr(),
-                                           lse.data_ptr(), dO.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
-                                           ws.data_ptr(), nbytes, _raw_stream()))
+    _block_rest(q, k, v, idx)
+    _same("o", o, torch.bfloat16, q.shape, q.device)
+    _same("dO", dO, torch.bfloat16, q.shape, q.device)
+    _same("lse", lse, torch.float32, q.shape[:3], q.device)
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    ws, nbytes = _block_ws(cfg, "sparsek_block_attn_bwd_workspace_bytes", ws, q.device)
+    _on(q.device, lib().sparsek_block_attn_bwd, cfg[0], q.data_ptr(), k.data_ptr(), v.data_ptr(), idx.data_ptr(), o.data_ptr(),
+        lse.data_ptr(), dO.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ws.data_ptr(), nbytes)
     return dq, dk, dv
 
 
@@ -596,16 +587,18 @@ class Cache8:
         if k8.dtype not in formats:
             raise ValueError("k8 must be int8 or float8_e4m3fn, got %s" % k8.dtype)
         dev = k8.device
-        for names, dtype, shape in (((("k8", k8),), k8.dtype, (pages, BLOCK_TOKENS, d)), ((("v8", v8),), k8.dtype, (pages, d, BLOCK_TOKENS)),
-                                    ((("ks", ks), ("vs", vs), ("kms", kms)), torch.float32, (pages,)), ((("km", km),), torch.int8, (pages, d)),
-                                    ((("kt", kt),), torch.bfloat16, (B, Hkv, BLOCK_TOKENS, d)), ((("vt", vt),), torch.bfloat16, (B, Hkv, d, BLOCK_TOKENS)),
-                                    ((("table", table),), torch.int32, (B, Hkv, cap)), ((("mass", mass),), torch.float32, (B, Hkv, cap))):
-            _same(names, dtype, shape, dev)
+        for name, t, dtype, shape in (
+                ("k8", k8, k8.dtype, (pages, BLOCK_TOKENS, d)), ("v8", v8, k8.dtype, (pages, d, BLOCK_TOKENS)), ("ks", ks, torch.float32, (pages,)),
+                ("vs", vs, torch.float32, (pages,)), ("km", km, torch.int8, (pages, d)), ("kms", kms, torch.float32, (pages,)),
+                ("kt", kt, torch.bfloat16, (B, Hkv, BLOCK_TOKENS, d)), ("vt", vt, torch.bfloat16, (B, Hkv, d, BLOCK_TOKENS)),
+                ("table", table, torch.int32, (B, Hkv, cap)), ("mass", mass, torch.float32, (B, Hkv, cap))):
+            _same(name, t, dtype, shape, dev)
         self.k8, self.v8, self.ks, self.vs, self.km, self.kms, self.kt, self.vt = k8, v8, ks, vs, km, kms, kt, vt
         self.table, self.mass = table, mass
         self.B, self.H, self.Hkv, self.d, self.cap, self.device = B, int(H), Hkv, d, cap, dev
         self.cfg = SparsekCache8Cfg(B=B, H=int(H), Hkv=Hkv, d=d, cap=cap, pages=pages, format=formats[k8.dtype], dtype=BF16,
                                     softmax_scale=float(scale))
+        self.q_shape, self.lens_shape, self.bytes = (B, int(H), d), (B,), {}
         if not lib().sparsek_cache8_attn_workspace_bytes(self.cfg, 0):
             raise ValueError("unsupported cache configuration")
         self._ref()
@@ -630,8 +623,8 @@ class Cache8:
 
     def adopt(self, table, mass):
         """From now on with this table and these masses (those that sparsek_cache8_evict gave)."""
-        _same([("table", table)], torch.int32, (self.B, self.Hkv, self.cap), self.device)
-        _same([("mass", mass)], torch.float32, (self.B, self.Hkv, self.cap), self.device)
+        _same("table", table, torch.int32, (self.B, self.Hkv, self.cap), self.device)
+        _same("mass", mass, torch.float32, (self.B, self.Hkv, self.cap), self.device)
         self.table, self.mass = table, mass
         self._ref()
 
@@ -640,47 +633,48 @@ def sparsek_cache8_append(cache, lens, k, v, counts=None):
     """The first counts[b] (None: all) of the new tokens k, v [B,Hkv,c,d] join the lens[b] (int32 [B]) that sequence b has; lens itself is
     the caller's to move on."""
     torch = _torch()
-    c = k.shape[2] if k.dim() == 4 else 0
-    _same([("k", k), ("v", v)], torch.bfloat16, (cache.B, cache.Hkv, c, cache.d), cache.device)
-    _same([("lens", lens)] + ([] if counts is None else [("counts", counts)]), torch.int32, (cache.B,), cache.device)
-    with _On(cache.device):
-        check(lib().sparsek_cache8_append(cache.ref, cache.cref, lens.data_ptr(), _ptr(counts), c, k.data_ptr(), v.data_ptr(), _raw_stream()))
+    shape = (cache.B, cache.Hkv, k.shape[2] if k.dim() == 4 else 0, cache.d)
+    _same("k", k, torch.bfloat16, shape, cache.device)
+    _same("v", v, torch.bfloat16, shape, cache.device)
+    _same("lens", lens, torch.int32, cache.lens_shape, cache.device)
+    if counts is not None:
+        _same("counts", counts, torch.int32, cache.lens_shape, cache.device)
+    _on(cache.device, lib().sparsek_cache8_append, cache.ref, cache.cref, lens.data_ptr(), _ptr(counts), shape[2], k.data_ptr(), v.data_ptr())
 
 
 def sparsek_cache8_select(cache, lens, q, top):
     """idx [B,Hkv,top] int32: the places in the table of the `top` whole blocks behind the own block of the query q [B,H,d] at position
     lens - 1 with the largest cheap scores, ascending, padded with -1."""
     torch = _torch()
-    _same([("q", q)], torch.bfloat16, (cache.B, cache.H, cache.d), cache.device)
-    _same([("lens", lens)], torch.int32, (cache.B,), cache.device)
-    with _On(cache.device):
-        idx = torch.empty(cache.B, cache.Hkv, max(int(top), 0), dtype=torch.int32, device=cache.device)
-        check(lib().sparsek_cache8_select(cache.ref, cache.cref, lens.data_ptr(), q.data_ptr(), int(top), idx.data_ptr(), _raw_stream()))
+    _same("q", q, torch.bfloat16, cache.q_shape, cache.device)
+    _same("lens", lens, torch.int32, cache.lens_shape, cache.device)
+    idx = torch.empty(cache.B, cache.Hkv, max(int(top), 0), dtype=torch.int32, device=cache.device)
+    _on(cache.device, lib().sparsek_cache8_select, cache.ref, cache.cref, lens.data_ptr(), q.data_ptr(), int(top), idx.data_ptr())
     return idx
 
 
 def sparsek_cache8_attn(cache, lens, q, idx=None, accumulate=False, ws=None):
     """o [B,H,d] and lse [B,H] fp32 of the query q [B,H,d] at position lens - 1 over all tokens, or over its own block and those of
     idx [B,Hkv,top]; accumulate=True adds the weights to cache.mass."""
-    torch = _torch()
-    _same([("q", q)], torch.bfloat16, (cache.B, cache.H, cache.d), cache.device)
-    _same([("lens", lens)], torch.int32, (cache.B,), cache.device)
-    top = 0
+    torch, L, top = _torch(), lib(), 0
+    _same("q", q, torch.bfloat16, cache.q_shape, cache.device)
+    _same("lens", lens, torch.int32, cache.lens_shape, cache.device)
     if idx is not None:
         top = idx.shape[-1]
-        _same([("idx", idx)], torch.int32, (cache.B, cache.Hkv, top), cache.device)
-    L = lib()
-    with _On(cache.device):
-        o = torch.empty_like(q)
-        lse = torch.empty(cache.B, cache.H, dtype=torch.float32, device=cache.device)
-        if ws is None:
-            nbytes = L.sparsek_cache8_attn_workspace_bytes(cache.ref, top)
-            ws = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=cache.device)
-        elif ws.device != cache.device or not ws.is_contiguous():
+        _same("idx", idx, torch.int32, (cache.B, cache.Hkv, top), cache.device)
+    o = torch.empty_like(q)
+    lse = torch.empty(cache.B, cache.H, dtype=torch.float32, device=cache.device)
+    if ws is None:
+        nbytes = cache.bytes.get(top)
+        if nbytes is None:
+            nbytes = cache.bytes[top] = max(L.sparsek_cache8_attn_workspace_bytes(cache.ref, top), 256)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=cache.device)
+    else:
+        if ws.device != cache.device or not ws.is_contiguous():
             raise ValueError("ws must be contiguous and on %s" % cache.device)
         nbytes = ws.numel() * ws.element_size()
-        check(L.sparsek_cache8_attn(cache.ref, cache.cref, lens.data_ptr(), q.data_ptr(), _ptr(idx), top, int(bool(accumulate)), o.data_ptr(),
-                                    lse.data_ptr(), ws.data_ptr(), nbytes, _raw_stream()))
+    _on(cache.device, L.sparsek_cache8_attn, cache.ref, cache.cref, lens.data_ptr(), q.data_ptr(), _ptr(idx), top, 1 if accumulate else 0,
+        o.data_ptr(), lse.data_ptr(), ws.data_ptr(), nbytes)
     return o, lse
 
 
@@ -688,13 +682,13 @@ def sparsek_cache8_evict(cache, lens, budget, sink=1, recent=1, out=None):
     """Sequences with more than `budget` whole blocks keep the first `sink`, the last `recent` and the heaviest of the others.  Returns
     dict(table, mass, lens), new tensors or those of `out`; cache.adopt(table, mass) makes the cache go on with them."""
     torch = _torch()
-    _same([("lens", lens)], torch.int32, (cache.B,), cache.device)
-    with _On(cache.device):
-        if out is None:
-            out = dict(table=torch.empty_like(cache.table), mass=torch.empty_like(cache.mass), lens=torch.empty_like(lens))
-        _same([("out table", out["table"])], torch.int32, cache.table.shape, cache.device)
-        _same([("out mass", out["mass"])], torch.float32, cache.mass.shape, cache.device)
-        _same([("out lens", out["lens"])], torch.int32, lens.shape, cache.device)
-        check(lib().sparsek_cache8_evict(cache.ref, cache.cref, lens.data_ptr(), int(budget), int(sink), int(recent),
-                                         out["table"].data_ptr(), out["mass"].data_ptr(), out["lens"].data_ptr(), _raw_stream()))
+    _same("lens", lens, torch.int32, cache.lens_shape, cache.device)
+    if out is None:
+        out = dict(table=torch.empty_like(cache.table), mass=torch.empty_like(cache.mass), lens=torch.empty_like(lens))
+    table, mass, after = out["table"], out["mass"], out["lens"]
+    _same("out table", table, torch.int32, cache.table.shape, cache.device)
+    _same("out mass", mass, torch.float32, cache.mass.shape, cache.device)
+    _same("out lens", after, torch.int32, cache.lens_shape, cache.device)
+    _on(cache.device, lib().sparsek_cache8_evict, cache.ref, cache.cref, lens.data_ptr(), int(budget), int(sink), int(recent),
+        table.data_ptr(), mass.data_ptr(), after.data_ptr())
     return out

@@ -43,6 +43,16 @@ __device__ __forceinline__ void async_load_lds16(const void* gbase, uint32_t vof
                  : "memory", "m0");
 }
 
+// The same with an address per lane: for rows of arrays that 32-bit offsets do not span.
+__device__ __forceinline__ void async_load_lds16_from(const void* at, const void* lds_dst)
+{
+    const uint32_t m0v = (uint32_t)(uintptr_t)(lds_void_t*)lds_dst;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                 :
+                 : "s"(m0v), "v"(at)
+                 : "memory", "m0");
+}
+
 constexpr int KT = 64;     // keys per tile
 constexpr int SEG = 1088;  // keys whose metadata is staged in LDS at a time (17 tiles)
 

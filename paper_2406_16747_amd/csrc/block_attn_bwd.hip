@@ -44,36 +44,35 @@ template <int D>
 struct BwdBlockSmem {
     unsigned char k[RowTile<D>::BYTES], v[RowTile<D>::BYTES], q[RowTile<D>::BYTES], g[RowTile<D>::BYTES];   // g: dO
     unsigned char ds[RowTile<64>::BYTES];   // [key][row]
-    float lse2[BT], delta[BT];
-    int limit[BT];                          // keys 0 .. limit are attended
-    long long at[BT];                       // the row's place in [B,H,n], -1: none
+    struct Rows {                           // of one tile
+        float lse2[BT], delta[BT];
+        int limit[BT];                      // keys 0 .. limit are attended
+        int at[BT];                         // the row's place in [G,n]
+    } rows[2];                              // the tile in use and the next one
 };
 static_assert(sizeof(BwdBlockSmem<128>) <= 80 * 1024, "two workgroups per CU");
 
-// The rows named by sm.at go to the q and g tiles; rows that do not exist become zeros.
+// The rows of a tile on their way to the q and g tiles: untracked direct-to-LDS loads, a wave-load per group of rows.
 template <int D>
-__device__ __forceinline__ void load_query_rows(BwdBlockSmem<D>& sm, const uint16_t* q, const uint16_t* dO, int tid)
+__device__ __forceinline__ void issue_query_rows(BwdBlockSmem<D>& sm, const typename BwdBlockSmem<D>::Rows& rows, const uint16_t* q, const uint16_t* dO,
+                                                 int wv, int lane)
 {
-    constexpr int CPR = D / 8;
+    using S = RowTile<D>;
+    constexpr int LPR = D / 8;
 #pragma unroll
-    for (int t = 0; t < BT * CPR / 256; t++) {
-        const int id = tid + 256 * t, r = id / CPR, c = id % CPR;
-        const long long at = sm.at[r];
-        u32x4 x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
-        if (at >= 0) {
-            x = *(const u32x4*)(q + (size_t)at * D + 8 * c);
-            y = *(const u32x4*)(dO + (size_t)at * D + 8 * c);
-        }
-        *(u32x4*)(sm.q + RowTile<D>::offset(r) + 16 * c) = x;
-        *(u32x4*)(sm.g + RowTile<D>::offset(r) + 16 * c) = y;
+    for (int x = 0; x < S::NL / 4; x++) {
+        const int L = wv + 4 * x;
+        const size_t off = (size_t)rows.at[S::row(L, lane / LPR)] * D + 8 * (lane % LPR);
+        async_load_lds16_from(q + off, sm.q + L * S::GS);
+        async_load_lds16_from(dO + off, sm.g + L * S::GS);
     }
 }
 
 // 64 rows against 64 keys.  Wave (kb = wv & 1, rb = wv >> 1): keys 32 kb .. and rows 32 rb .. of S and dP; its share of dV^T and
-// dK^T (those keys, those rows) joins acc_v, acc_k; then dQ^T of rows 32 rb .. and the D/2 columns of half kb, into acc_q.
+// dK^T (those keys, those rows) joins acc_v, acc_k; dS goes to LDS.
 template <int D>
-__device__ __forceinline__ void bwd_block_tile(BwdBlockSmem<D>& sm, int lane, int wv, bool own, float c2, float scale, f32x16 (&acc_v)[D / 32],
-                                               f32x16 (&acc_k)[D / 32], f32x16 (&acc_q)[D / 64])
+__device__ __forceinline__ void bwd_block_tile(BwdBlockSmem<D>& sm, const typename BwdBlockSmem<D>::Rows& rows, int lane, int wv, bool own, float c2,
+                                               f32x16 (&acc_v)[D / 32], f32x16 (&acc_k)[D / 32])
 {
     using S = RowTile<D>;
     constexpr int DS = D / 16, DB = D / 32;
@@ -89,16 +88,16 @@ __device__ __forceinline__ void bwd_block_tile(BwdBlockSmem<D>& sm, int lane, in
     if (own)   // (some of the rows are the block's own queries)
 #pragma unroll
         for (int g4 = 0; g4 < 4; g4++) {
-            const int4 L4 = *(const int4*)&sm.limit[32 * rb + 8 * g4 + 4 * half];
+            const int4 L4 = *(const int4*)&rows.limit[32 * rb + 8 * g4 + 4 * half];
             const int ll[4] = {L4.x, L4.y, L4.z, L4.w};
 #pragma unroll
             for (int e = 0; e < 4; e++) s[4 * g4 + e] = 32 * kb + col > ll[e] ? -INFINITY : s[4 * g4 + e];
         }
-    bf16x8 pb[2], db[2];   // as operands: 2^-9 of every weight and every score gradient
+    bf16x8 pb[2], db[2];   // as operands: 2^-8 of every weight and every score gradient
 #pragma unroll
     for (int g4 = 0; g4 < 4; g4++) {
         const int r0 = 32 * rb + 8 * g4 + 4 * half;
-        const float4 L4 = *(const float4*)&sm.lse2[r0], D4 = *(const float4*)&sm.delta[r0];
+        const float4 L4 = *(const float4*)&rows.lse2[r0], D4 = *(const float4*)&rows.delta[r0];
         const float ll[4] = {L4.x, L4.y, L4.z, L4.w}, dd[4] = {D4.x, D4.y, D4.z, D4.w};
         float ds[4];
 #pragma unroll
@@ -119,7 +118,14 @@ __device__ __forceinline__ void bwd_block_tile(BwdBlockSmem<D>& sm, int lane, in
             acc_v[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_operand<D>(tg + g * S::R16 + 64 * x), pb[g], acc_v[x], 0, 0, 0);
             acc_k[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_operand<D>(tq + g * S::R16 + 64 * x), db[g], acc_k[x], 0, 0, 0);
         }
-    __syncthreads();   // dS is there
+}
+
+// dQ^T of rows 32 rb .. and the D/2 columns of half kb, from the dS in LDS.
+template <int D>
+__device__ __forceinline__ void bwd_block_dq(BwdBlockSmem<D>& sm, int lane, int wv, float scale, f32x16 (&acc_q)[D / 64])
+{
+    constexpr int DB = D / 32;
+    const int kb = wv & 1, rb = wv >> 1;
     const uint32_t tk = lds_address(sm.k) + transposed_lane<D>(lane) + 64 * (DB / 2) * kb, td = lds_address(sm.ds) + transposed_lane<64>(lane) + 64 * rb;
 #pragma unroll
     for (int x = 0; x < DB / 2; x++) acc_q[x] = f32x16{0};
@@ -128,7 +134,7 @@ __device__ __forceinline__ void bwd_block_tile(BwdBlockSmem<D>& sm, int lane, in
         const bf16x8 d8 = transposed_operand<64>(td + g * RowTile<64>::R16);
 #pragma unroll
         for (int x = 0; x < DB / 2; x++)
-            acc_q[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_operand<D>(tk + g * S::R16 + 64 * x), d8, acc_q[x], 0, 0, 0);
+            acc_q[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_operand<D>(tk + g * RowTile<D>::R16 + 64 * x), d8, acc_q[x], 0, 0, 0);
     }
 #pragma unroll
     for (int x = 0; x < DB / 2; x++)
@@ -187,7 +193,7 @@ __global__ __launch_bounds__(256, 2) void block_bwd_tiles_kernel(BlockBwd f)
     __shared__ __attribute__((aligned(16))) BwdBlockSmem<D> sm;
     constexpr int DB = D / 32;
     const BlockLists& l = f.a.l;
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, col = lane & 31, half = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
     int bg, un;
     deal_head(blockIdx.x, l.maxu, l.B * l.Hkv, bg, un);
     if (un >= l.nunits[bg]) return;
@@ -199,35 +205,51 @@ __global__ __launch_bounds__(256, 2) void block_bwd_tiles_kernel(BlockBwd f)
     load_rows<D>(sm.k, f.a.k + kv, last, tid);
     load_rows<D>(sm.v, f.a.v + kv, last, tid);
     const int32_t* list = l.list + (size_t)bg * l.entries + base;
-    const size_t row0 = ((size_t)bg * l.entries + base) * G;
-    const int own_end = min(BT, last + 1) * G;
-    f32x16 acc_v[DB], acc_k[DB], acc_q[DB / 2];
+    const size_t row0 = ((size_t)bg * l.entries + base) * G, head0 = (size_t)b * l.H + g * G;
+    const uint16_t *q0 = f.a.q + head0 * l.n * D, *g0 = f.a.dO + head0 * l.n * D;
+    const float2* meta_in = f.rows + head0 * l.n;
+    const int own_end = min(BT, last + 1) * G, kb = wv & 1, rt = 32 * (wv >> 1) + col;
+    // A tile's rows are on their way while the dQ of the tile before is formed; what is known of them (by the first wave, a row to a
+    // lane) two tiles ahead (the query) and one (its logarithm and dO.o).
+    auto entry = [&](int r) { return list[min(r, end - 1) / G]; };
+    auto place = [&](int r, int i) { return min(r, end - 1) % G * l.n + i; };
+    auto put = [&](typename BwdBlockSmem<D>::Rows& rows, int r, int i, float2 m) {
+        rows.lse2[lane] = r < end ? m.x : INFINITY;   // (a row that does not exist: p = 0)
+        rows.delta[lane] = r < end ? m.y : 0.0f;
+        rows.limit[lane] = min(BT - 1, i - j * BT);
+        rows.at[lane] = place(r, i);
+    };
+    int i_next = 0;
+    if (wv == 0) {
+        const int i = entry(first + lane);
+        i_next = entry(first + BT + lane);
+        put(sm.rows[0], first + lane, i, meta_in[place(first + lane, i)]);
+    }
+    f32x16 acc_v[DB], acc_k[DB];
 #pragma unroll
     for (int x = 0; x < DB; x++) acc_v[x] = acc_k[x] = f32x16{0};
-    for (int r0 = first; r0 < end; r0 += BT) {
-        __syncthreads();   // everybody is done with the rows before
-        if (tid < BT) {
-            const int r = r0 + tid;
-            long long at = -1;
-            int limit = BT - 1;
-            float2 m = make_float2(INFINITY, 0.0f);   // p = 0
-            if (r < end) {
-                const int i = list[r / G];
-                at = ((long long)b * l.H + g * G + r % G) * l.n + i;
-                limit = min(limit, i - j * BT);
-                m = f.rows[at];
-            }
-            sm.at[tid] = at;
-            sm.limit[tid] = limit;
-            sm.lse2[tid] = m.x;
-            sm.delta[tid] = m.y;
+    __syncthreads();
+    issue_query_rows<D>(sm, sm.rows[0], q0, g0, wv, lane);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    int buf = 0;
+    for (int r0 = first; r0 < end; r0 += BT, buf ^= 1) {
+        __syncthreads();   // the tile's rows have landed
+        float2 m = make_float2(0.0f, 0.0f);
+        int i_then = 0;
+        if (wv == 0) {
+            m = meta_in[place(r0 + BT + lane, i_next)];
+            i_then = entry(r0 + 2 * BT + lane);
         }
-        __syncthreads();
-        load_query_rows<D>(sm, f.a.q, f.a.dO, tid);
-        __syncthreads();
-        bwd_block_tile<D>(sm, lane, wv, r0 < own_end, f.a.c2, f.a.scale, acc_v, acc_k, acc_q);
+        bwd_block_tile<D>(sm, sm.rows[buf], lane, wv, r0 < own_end, f.a.c2, acc_v, acc_k);
+        if (wv == 0) {
+            put(sm.rows[buf ^ 1], r0 + BT + lane, i_next, m);
+            i_next = i_then;
+        }
+        __syncthreads();   // dS is there, and nobody reads the rows any more
+        if (r0 + BT < end) issue_query_rows<D>(sm, sm.rows[buf ^ 1], q0, g0, wv, lane);
+        f32x16 acc_q[DB / 2];
+        bwd_block_dq<D>(sm, lane, wv, f.a.scale, acc_q);
         // the partial dq of rows 32 rb + col, columns of half kb, relative to the largest of them
-        const int kb = wv & 1, rt = 32 * (wv >> 1) + col, r = r0 + rt;
         float top = 0.0f;
 #pragma unroll
         for (int x = 0; x < DB / 2; x++)
@@ -236,26 +258,27 @@ __global__ __launch_bounds__(256, 2) void block_bwd_tiles_kernel(BlockBwd f)
         const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
         const int E = scale_exp(max((unsigned)sw[0], (unsigned)sw[1]));
         const float down = scale_down(E);
-        if (r < end && half == 0) ((float*)(f.meta + row0 + r))[kb] = scale_up(E);
-        __syncthreads();   // (the rows of q are not needed any more)
+        const int count = min(BT, end - r0);
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(scale_up(E)), buffer_of(f.meta + row0 + r0, 8 * count), half ? 0x7FFFFFF0 : 8 * rt + 4 * kb, 0, 0);
+        const auto dst = buffer_of(f.part + (row0 + r0) * D, 2 * D * count);
 #pragma unroll
         for (int x = 0; x < DB / 2; x++)
 #pragma unroll
-            for (int y = 0; y < 4; y++) {
-                f16x4 v;
+            for (int y = 0; y < 4; y += 2) {
+                // columns 8 y .. 8 y + 7 from both halves of the wave to its lower lanes, the next 8 to its upper lanes
+                u32x4 w;
 #pragma unroll
-                for (int e = 0; e < 4; e++) v[e] = (_Float16)(acc_q[x][4 * y + e] * down);
-                *(f16x4*)(sm.q + rt * (2 * D + 16) + D * kb + 64 * x + 16 * y + 8 * half) = v;
+                for (int e = 0; e < 2; e++) {
+                    const f16x2v a = {(_Float16)(acc_q[x][4 * y + 2 * e] * down), (_Float16)(acc_q[x][4 * y + 2 * e + 1] * down)};
+                    const f16x2v c = {(_Float16)(acc_q[x][4 * y + 4 + 2 * e] * down), (_Float16)(acc_q[x][4 * y + 5 + 2 * e] * down)};
+                    const auto sx = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, c), false, false);
+                    w[e] = sx[0];
+                    w[2 + e] = sx[1];
+                }
+                store_words(dst, rt * 2 * D + D * kb + 64 * x + 16 * (y + half), w);
             }
-        __syncthreads();
-        unsigned char* dst = (unsigned char*)(f.part + (row0 + r0) * D);
-        const int bytes = min(BT, end - r0) * 2 * D;
-#pragma unroll
-        for (int t = 0; t < BT * (D / 8) / 256; t++) {
-            const int id = tid + 256 * t;
-            const u32x4 v = *(const u32x4*)(sm.q + id / (D / 8) * (2 * D + 16) + 16 * (id % (D / 8)));
-            if (16 * id < bytes) *(u32x4*)(dst + 16 * id) = v;
-        }
+        // the next rows are there when no more than this tile's stores are under way (memory operations end in order)
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(DB + 1) : "memory");
     }
     add_row_halves<D>(sm, lane, wv, acc_v, acc_k);
     if (wv >= 2) return;

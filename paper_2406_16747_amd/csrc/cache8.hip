@@ -358,6 +358,7 @@ __global__ __launch_bounds__(1024) void cache8_select_kernel(CacheArgs a, const 
 // bits are exact in fp16; so is q relative to its largest value (what fp16 drops lies 2^-27 below it), and weights lose 2^-11
 // where bf16 would lose 2^-8.  What bounds it is memory: a wave has the keys of one block and the values of another on
 // their way while it computes.
+constexpr int MAX_UPW = 5;
 struct AttnArgs {
     CacheArgs c;
     const uint16_t* q;
@@ -366,8 +367,9 @@ struct AttnArgs {
     float c2;
     float* part_o;         // [B,H,splits][D]
     float2* part_ml;       // [B,H,splits]: the largest logit (times log2 e), the sum
-    float* weight;         // [B,H,units]: log2 of a unit's share before the division; null: no masses
+    float* weight;         // [B,H,units]: log2 of a unit's share before the division
     int units;             // units per row at most
+    bool accumulate;
     uint16_t* o;
     float* lse;
 };
@@ -424,6 +426,13 @@ __device__ __forceinline__ int unit_block(const AttnArgs& a, const RowUnits& r, 
     return ok ? x : -1;
 }
 
+// Unit u's weights join the mass of its place in the table.  (One that was left out has none and may name any place.)
+__device__ __forceinline__ void add_mass(const AttnArgs& a, const RowUnits& ru, size_t bg, int u, float sum)
+{
+    const int j = u == ru.nsel ? ru.whole : !a.idx ? u : u == a.top ? ru.own : a.idx[bg * a.top + u];
+    if (j >= 0 && j < a.c.cap && sum != 0.0f) a.c.t.mass[bg * a.c.cap + j] += sum;
+}
+
 // The running softmax over a unit's logits (in s, times log2 e): weights as the operand of the second product (times 2^15).
 struct SoftRow {
     float m, l;
@@ -463,14 +472,15 @@ template <int D, int FORMAT>
 __global__ __launch_bounds__(256, 3) void cache8_attn_kernel(AttnArgs a)
 {
     constexpr int KH = D / 64, NX = D / 16;
-    __shared__ float so[4][16][D + 4], sm_[4][16], sl[4][16];
+    __shared__ float so[4][16][D + 4], sm_[4][16], sl[4][16], shares[4 * MAX_UPW + 1][16];
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, grp = lane >> 4;
     const int groups = (a.c.G + 15) / 16;
     const int split = blockIdx.x, g = blockIdx.y / groups, rg = blockIdx.y % groups, b = blockIdx.z;
     const size_t bg = (size_t)b * a.c.Hkv + g;
     const RowUnits ru = row_units(a, b);
     const int nu = ru.nsel + (ru.tail ? 1 : 0);
-    if (split * 4 * a.upw >= nu) return;   // (the join leaves such parts out)
+    const bool alone = a.splits == 1 && groups == 1;   // the workgroup has all units of all heads of the group
+    if (split * 4 * a.upw >= nu && !alone) return;   // (the join leaves such parts out)
     const int live = min(16, a.c.G - rg * 16);
     const size_t head0 = (size_t)b * a.c.H + g * a.c.G + rg * 16;
     // the wave's units, one to a lane: page (of any unit that has one where there is none), scales
@@ -517,7 +527,8 @@ __global__ __launch_bounds__(256, 3) void cache8_attn_kernel(AttnArgs a)
     for (int x = 0; x < NX; x++) acc[x] = f32x4m{0, 0, 0, 0};
     SoftRow row = {-INFINITY, 0.0f};
     // the weights of the live heads' units; the other lanes' lie outside the buffer
-    const buffer_t wbuf = buffer_of(a.weight ? a.weight + head0 * a.units : nullptr, a.weight ? live * a.units * 4 : 0);
+    const bool weighs = a.accumulate && !alone;
+    const buffer_t wbuf = buffer_of(weighs ? a.weight + head0 * a.units : nullptr, weighs ? live * a.units * 4 : 0);
     const int wat = grp == 0 && col < live ? col * a.units * 4 : 0x7FFFFF00;
     if (have) {
         const int kat = (16 * (col >> 2) + (col & 3)) * D + 16 * grp, vat = col * BT + 16 * grp;
@@ -557,7 +568,8 @@ __global__ __launch_bounds__(256, 3) void cache8_attn_kernel(AttnArgs a)
             f16x8 pb[2];
             float corr;
             const float share = soft_unit(s, row, pb, corr);
-            __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(share), wbuf, wat + 4 * (u0 + i), 0, 0);
+            if (alone) shares[u0 + i][col] = share;
+            else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(share), wbuf, wat + 4 * (u0 + i), 0, 0);
 #pragma unroll
             for (int x = 0; x < NX; x++) {
                 f32x4m y = {0, 0, 0, 0};
@@ -569,7 +581,10 @@ __global__ __launch_bounds__(256, 3) void cache8_attn_kernel(AttnArgs a)
             load_v(min(i + 1, count - 1));
         }
     } else {   // nothing to attend: the units have no share
-        for (int i = 0; i < count; i++) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(-INFINITY), wbuf, wat + 4 * (u0 + i), 0, 0);
+        for (int i = 0; i < count; i++) {
+            if (alone) shares[u0 + i][col] = -INFINITY;
+            else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(-INFINITY), wbuf, wat + 4 * (u0 + i), 0, 0);
+        }
     }
     if (ru.tail && ru.nsel >= u0 && ru.nsel < u0 + a.upw) {   // the unfinished block, in bf16
         const uint16_t *kp = (const uint16_t*)a.c.t.kt + bg * BT * D, *vp = (const uint16_t*)a.c.t.vt + (bg * D + col) * BT + 16 * grp;
@@ -612,7 +627,8 @@ __global__ __launch_bounds__(256, 3) void cache8_attn_kernel(AttnArgs a)
         f16x8 pb[2];
         float corr;
         const float share = soft_unit(s, row, pb, corr);
-        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(share), wbuf, wat + 4 * ru.nsel, 0, 0);
+        if (alone) shares[ru.nsel][col] = share;
+        else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(share), wbuf, wat + 4 * ru.nsel, 0, 0);
 #pragma unroll
         for (int x = 0; x < NX; x++) {
             f32x4m y = {0, 0, 0, 0};
@@ -643,9 +659,27 @@ __global__ __launch_bounds__(256, 3) void cache8_attn_kernel(AttnArgs a)
             sum += f * so[w][h][d];
             den += f * sl[w][h];
         }
+        if (alone) {
+            const bool some_key = M > -INFINITY;
+            a.o[(head0 + h) * D + d] = f32_to_bf16(some_key ? sum / den : 0.0f);
+            if (d == 0) a.lse[head0 + h] = some_key ? (M + log2f(den * 0x1p-15f)) * 0.6931471805599453f : -INFINITY;
+            continue;
+        }
         const size_t at = (head0 + h) * a.splits + split;
         a.part_o[at * D + d] = sum;
         if (d == 0) a.part_ml[at] = make_float2(M, den);
+    }
+    if (alone && a.accumulate && tid < nu) {   // (one group of heads: nobody else adds to these masses)
+        float sum = 0.0f;
+        for (int h = 0; h < live; h++) {
+            const float M = fmaxf(fmaxf(sm_[0][h], sm_[1][h]), fmaxf(sm_[2][h], sm_[3][h]));
+            if (M == -INFINITY) continue;
+            float den = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 4; w++) den += sm_[w][h] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm_[w][h] - M) * sl[w][h];
+            if (shares[tid][h] > -INFINITY) sum += __builtin_amdgcn_exp2f(shares[tid][h] - (M + log2f(den * 0x1p-15f)));
+        }
+        add_mass(a, ru, bg, tid, sum);
     }
 }
 
@@ -743,11 +777,7 @@ __global__ __launch_bounds__(256) void cache8_join_kernel(AttnArgs a, int mass_w
                     if (w > -INFINITY) sum += __builtin_amdgcn_exp2f(w - logs[x]);
                 }
     }
-    if (u < nu) {
-        const int j = u == ru.nsel ? ru.whole : !a.idx ? u : u == a.top ? ru.own : a.idx[bg * a.top + u];
-        // (a unit that was left out has weight 0 and may name any place)
-        if (j >= 0 && j < a.c.cap && sum != 0.0f) a.c.t.mass[bg * a.c.cap + j] += sum;
-    }
+    if (u < nu) add_mass(a, ru, bg, u, sum);
 }
 
 // ---- eviction ----
@@ -829,10 +859,12 @@ static Cache8Layout cache8_layout(const sparsek_cache8_cfg& c, int top)
     Cache8Layout y;
     y.units = (top ? top : c.cap) + 1;   // and the query's own block
     y.groups = (c.H / c.Hkv + 15) / 16;
-    // Units per wave: as many as leave 8 waves for each of 256 compute units, 4 at most (sequences are shorter than the longest, and
-    // the waves that they leave idle weigh less the fewer units each has: 64 sequences of up to 8192 159 us with 16, 155 with 4).
+    // Units per wave.  Up to 20 units and 16 heads of a group are one workgroup's, which needs no second launch.  Beyond that
+    // as many as leave 8 waves for each of 256 compute units, 4 at most (sequences are shorter than the longest, and the waves that
+    // they leave idle weigh less the fewer units each has: 64 sequences of up to 8192 159 us with 16, 155 with 4).
     const long long all = (long long)c.B * c.Hkv * y.groups * y.units;
-    y.upw = (int)std::max<long long>(1, std::min<long long>(4, all / 2048));
+    if (y.units <= 4 * MAX_UPW && y.groups == 1) y.upw = (y.units + 3) / 4;
+    else y.upw = (int)std::max<long long>(1, std::min<long long>(4, all / 2048));
     y.splits = (y.units + 4 * y.upw - 1) / (4 * y.upw);
     const size_t parts = (size_t)c.B * c.H * y.splits;
     y.part_o = 0;
@@ -857,7 +889,8 @@ int launch_cache8_attn(const sparsek_cache8_cfg& c, const sparsek_cache8& t, con
     a.c2 = c.softmax_scale * 1.4426950408889634f;
     char* w = (char*)ws;
     a.part_o = (float*)(w + y.part_o); a.part_ml = (float2*)(w + y.part_ml);
-    a.weight = accumulate ? (float*)(w + y.weight) : nullptr;
+    a.weight = (float*)(w + y.weight);
+    a.accumulate = accumulate;
     a.units = y.units;
     a.o = (uint16_t*)o;
     a.lse = lse;
@@ -865,6 +898,7 @@ int launch_cache8_attn(const sparsek_cache8_cfg& c, const sparsek_cache8& t, con
 #define ATTN(D, F) hipLaunchKernelGGL((cache8_attn_kernel<D, F>), dim3(y.splits, c.Hkv * y.groups, c.B), dim3(256), 0, st, a)
     BY_FORMAT(c, ATTN)
 #undef ATTN
+    if (y.splits == 1 && y.groups == 1) return launch_status();
     const dim3 join(c.H + c.Hkv * mass_wgs, c.B);
     if (c.d == 128) hipLaunchKernelGGL((cache8_join_kernel<128>), join, dim3(256), 0, st, a, std::max(mass_wgs, 1));
     else hipLaunchKernelGGL((cache8_join_kernel<64>), join, dim3(256), 0, st, a, std::max(mass_wgs, 1));
