@@ -14,17 +14,30 @@ namespace spk {
 
 // ---- the lists ----
 
-// The chunk's 64 queries as bits, for the key blocks j0 .. j0 + MASK_BLOCKS - 1.
+// A chunk's selection [64][top] and its 64 queries as bits, for the key blocks j0 .. j0 + MASK_BLOCKS - 1.  LDS: masks, then the selection.
 constexpr int MASK_BLOCKS = 4096;
-__device__ __forceinline__ void chunk_masks(unsigned long long* masks, const BlockLists& l, const int32_t* idx, int bg, int c, int j0, int tid)
+inline size_t chunk_lds(const BlockLists& l) { return (size_t)std::min(MASK_BLOCKS, l.nb) * 8 + (size_t)BT * l.top * 4; }
+struct ChunkLds {
+    unsigned long long* masks;
+    int* sel;
+};
+__device__ __forceinline__ ChunkLds chunk_lds_at(unsigned char* lds, const BlockLists& l)
 {
-    const int jn = min(MASK_BLOCKS, c - j0), rows = min(BT, l.n - c * BT);
-    for (int x = tid; x < jn; x += 256) masks[x] = 0;
+    return ChunkLds{(unsigned long long*)lds, (int*)(lds + (size_t)min(MASK_BLOCKS, l.nb) * 8)};
+}
+__device__ __forceinline__ void chunk_masks(ChunkLds m, const BlockLists& l, const int32_t* idx, int bg, int c, int j0, int tid)
+{
+    const int jn = min(MASK_BLOCKS, c - j0), count = min(BT, l.n - c * BT) * l.top;
+    for (int x = tid; x < jn; x += 256) m.masks[x] = 0;
+    if (j0 == 0) {
+        const int32_t* row = idx + ((size_t)bg * l.n + (size_t)c * BT) * l.top;
+#pragma unroll 4
+        for (int x = tid; x < count; x += 256) m.sel[x] = row[x];
+    }
     __syncthreads();
-    const int32_t* row = idx + ((size_t)bg * l.n + (size_t)c * BT) * l.top;
-    for (int x = tid; x < rows * l.top; x += 256) {
-        const int j = row[x] - j0;
-        if (row[x] >= j0 && j < jn) atomicOr(&masks[j], 1ull << (x / l.top));
+    for (int x = tid; x < count; x += 256) {
+        const int j = m.sel[x];
+        if (j >= j0 && j - j0 < jn) atomicOr(&m.masks[j - j0], 1ull << (x / l.top));
     }
     __syncthreads();
 }
@@ -32,11 +45,12 @@ __device__ __forceinline__ void chunk_masks(unsigned long long* masks, const Blo
 // counts: a workgroup per (chunk, batch and head).
 __global__ __launch_bounds__(256) void block_counts_kernel(BlockLists l, const int32_t* __restrict__ idx)
 {
-    __shared__ unsigned long long masks[MASK_BLOCKS];
+    extern __shared__ unsigned char lds[];
+    const ChunkLds m = chunk_lds_at(lds, l);
     const int c = blockIdx.x, bg = blockIdx.y, tid = threadIdx.x;
     for (int j0 = 0; j0 < c; j0 += MASK_BLOCKS) {
-        chunk_masks(masks, l, idx, bg, c, j0, tid);
-        for (int x = tid; x < min(MASK_BLOCKS, c - j0); x += 256) l.counts[((size_t)bg * l.nb + c) * l.nb + j0 + x] = (uint8_t)__popcll(masks[x]);
+        chunk_masks(m, l, idx, bg, c, j0, tid);
+        for (int x = tid; x < min(MASK_BLOCKS, c - j0); x += 256) l.counts[((size_t)bg * l.nb + c) * l.nb + j0 + x] = (uint8_t)__popcll(m.masks[x]);
         __syncthreads();
     }
 }
@@ -117,27 +131,27 @@ __global__ __launch_bounds__(1024) void block_units_kernel(BlockLists l)
 // list and pos: a workgroup per (chunk, batch and head).
 __global__ __launch_bounds__(256) void block_place_kernel(BlockLists l, const int32_t* __restrict__ idx)
 {
-    __shared__ unsigned long long masks[MASK_BLOCKS];
+    extern __shared__ unsigned char lds[];
+    const ChunkLds m = chunk_lds_at(lds, l);
     const int c = blockIdx.x, bg = blockIdx.y, tid = threadIdx.x, rows = min(BT, l.n - c * BT);
     const size_t cbg = l.cbg(c * BT / l.cq, bg);
     int32_t *list = l.list + cbg * l.entries, *pos = l.pos + ((size_t)bg * l.n + (size_t)c * BT) * l.slots;
-    const int32_t* base = l.base + cbg * l.nb;
+    const int32_t *base = l.base + cbg * l.nb, *off = l.off + ((size_t)bg * l.nb + c) * l.nb;
     if (tid < rows) {
         list[base[c] + tid] = c * BT + tid;
         pos[(size_t)tid * l.slots] = base[c] + tid;
     }
-    const int32_t *row = idx + ((size_t)bg * l.n + (size_t)c * BT) * l.top, *off = l.off + ((size_t)bg * l.nb + c) * l.nb;
     for (int j0 = 0; j0 == 0 || j0 < c; j0 += MASK_BLOCKS) {
-        if (c) chunk_masks(masks, l, idx, bg, c, j0, tid);
+        chunk_masks(m, l, idx, bg, c, j0, tid);
         for (int x = tid; x < rows * l.top; x += 256) {
-            const int r = x / l.top, s = x % l.top, j = row[x];
+            const int r = x / l.top, s = x - r * l.top, j = m.sel[x];
             if (j < 0 || j >= c) {
                 if (j0 == 0) pos[(size_t)r * l.slots + 1 + s] = -1;
                 continue;
             }
             if (j < j0 || j >= j0 + MASK_BLOCKS) continue;
-            int p = base[j] + off[j] + __popcll(masks[j - j0] & ((1ull << r) - 1));
-            for (int y = 0; y < s; y++) p = row[x - s + y] == j ? -1 : p;   // (a repeated block counts once)
+            int p = base[j] + off[j] + __popcll(m.masks[j - j0] & ((1ull << r) - 1));
+            for (int y = 0; y < s; y++) p = m.sel[x - s + y] == j ? -1 : p;   // (a repeated block counts once)
             if (p >= 0) list[p] = c * BT + r;
             pos[(size_t)r * l.slots + 1 + s] = p;
         }
@@ -145,13 +159,81 @@ __global__ __launch_bounds__(256) void block_place_kernel(BlockLists l, const in
     }
 }
 
+// All of it in one launch where a (batch, head) has few blocks and pairs: a workgroup of 1024 each, counts and offsets in LDS.  Four
+// launches of 3 us each are most of a short sequence's lists.
+constexpr int FEW_BLOCKS = 64, FEW_PAIRS = 16384;
+__global__ __launch_bounds__(1024) void block_short_lists_kernel(BlockLists l, const int32_t* __restrict__ idx)
+{
+    __shared__ unsigned long long masks[FEW_BLOCKS][FEW_BLOCKS];   // [chunk][block]
+    __shared__ uint16_t off[FEW_BLOCKS][FEW_BLOCKS];
+    __shared__ int base[FEW_BLOCKS];
+    const int bg = blockIdx.x, tid = threadIdx.x, nb = l.nb, pairs = l.n * l.top;
+    const int32_t* row = idx + (size_t)bg * pairs;
+    for (int x = tid; x < nb * FEW_BLOCKS; x += 1024) masks[x / FEW_BLOCKS][x % FEW_BLOCKS] = 0;
+    __syncthreads();
+#pragma unroll 4
+    for (int x = tid; x < pairs; x += 1024) {
+        const int j = row[x], i = x / l.top, c = i / BT;
+        if (j >= 0 && j < c) atomicOr(&masks[c][j], 1ull << (i % BT));
+    }
+    __syncthreads();
+    if (tid < 64) {   // a lane per block
+        const int j = tid, own = j < nb ? min(BT, l.n - j * BT) : 0;
+        int run = own;
+        for (int c = j + 1; c < nb; c++) {
+            off[c][j] = (uint16_t)run;
+            run += __popcll(masks[c][j]);
+        }
+        const int units = (int)(((long long)run * l.G + l.unit - 1) / l.unit);
+        int2 s = make_int2(run, units);
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int x = __shfl_up(s.x, d, 64), y = __shfl_up(s.y, d, 64);
+            if (j >= d) { s.x += x; s.y += y; }
+        }
+        base[j] = s.x - run;
+        if (j < nb) {
+            l.total[(size_t)bg * nb + j] = run;
+            l.base[(size_t)bg * nb + j] = s.x - run;
+            const int u0 = s.y - units;
+            l.first_unit[(size_t)bg * nb + j] = u0;
+            for (int u = 0; u < units; u++)
+                if (u0 + u < l.maxu) l.units[(size_t)bg * l.maxu + u0 + u] = make_int2(j, u * l.unit);
+        }
+        if (j == 63) l.nunits[bg] = min(s.y, l.maxu);
+    }
+    __syncthreads();
+    int32_t *list = l.list + (size_t)bg * l.entries, *pos = l.pos + (size_t)bg * l.n * l.slots;
+    for (int i = tid; i < l.n; i += 1024) {
+        const int p = base[i / BT] + i % BT;
+        list[p] = i;
+        pos[(size_t)i * l.slots] = p;
+    }
+#pragma unroll 4
+    for (int x = tid; x < pairs; x += 1024) {
+        const int j = row[x], i = x / l.top, s = x - i * l.top, c = i / BT;
+        int p = -1;
+        if (j >= 0 && j < c) {
+            p = base[j] + off[c][j] + __popcll(masks[c][j] & ((1ull << (i % BT)) - 1));
+            for (int y = 0; y < s; y++) p = row[x - s + y] == j ? -1 : p;   // (a repeated block counts once)
+            if (p >= 0) list[p] = i;
+        }
+        pos[(size_t)i * l.slots + 1 + s] = p;
+    }
+}
+
 int launch_block_lists(const BlockLists& l, const int32_t* idx, hipStream_t st)
 {
     const int BG = l.B * l.Hkv;
-    if (l.top) hipLaunchKernelGGL(block_counts_kernel, dim3(l.nb, BG), dim3(256), 0, st, l, idx);
+    if (l.nb <= FEW_BLOCKS && l.nc == 1 && (long long)l.n * l.top <= FEW_PAIRS) {
+        hipLaunchKernelGGL(block_short_lists_kernel, dim3(BG), dim3(1024), 0, st, l, idx);
+        return launch_status();
+    }
+    const size_t lds = chunk_lds(l);
+    if (l.top) hipLaunchKernelGGL(block_counts_kernel, dim3(l.nb, BG), dim3(256), lds, st, l, idx);
     hipLaunchKernelGGL(block_offsets_kernel, dim3((l.nb + 63) / 64, l.nc, BG), dim3(1024), 0, st, l);
     hipLaunchKernelGGL(block_units_kernel, dim3(l.nc, BG), dim3(1024), 0, st, l);
-    hipLaunchKernelGGL(block_place_kernel, dim3(l.nb, BG), dim3(256), 0, st, l, idx);
+    hipLaunchKernelGGL(block_place_kernel, dim3(l.nb, BG), dim3(256), lds, st, l, idx);
     return launch_status();
 }
 

@@ -296,34 +296,38 @@ __global__ __launch_bounds__(256, 2) void block_bwd_tiles_kernel(BlockBwd f)
         }
 }
 
-// dK and dV of the blocks with several units: a workgroup per (block and 32 of its columns, batch and head), its first two waves dV and its last two
-// dK, of 32 keys each.
+// dK and dV of the blocks with several units: a workgroup per (every KV_JOIN-th block and 32 of its columns, batch and head), its first two
+// waves dV and its last two dK, of 32 keys each.  (Most blocks have one unit: a workgroup for each of them takes 76 us for 64 heads of
+// 128 blocks, most of it to start workgroups that find nothing.)
+constexpr int KV_JOIN = 16;
 template <int D>
 __global__ __launch_bounds__(256) void block_kv_join_kernel(BlockBwd f)
 {
     constexpr int DB = D / 32;
     const BlockLists& l = f.a.l;
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, j = blockIdx.x / DB, x = blockIdx.x % DB, bg = blockIdx.y;
-    const int rows = l.total[(size_t)bg * l.nb + j] * l.G;
-    if (rows <= l.unit) return;
-    const int units = (int)(((long long)rows + l.unit - 1) / l.unit), u0 = l.first_unit[(size_t)bg * l.nb + j];
-    const float4* in = (const float4*)f.kvpart + (((size_t)bg * l.maxu + u0) * 2 + (wv & 1)) * (2 * DB * 4 * 64) + (((wv >> 1) * DB + x) * 4) * 64 + lane;
-    float4 s[4];
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, x = blockIdx.x % DB, bg = blockIdx.y;
+    for (int j = blockIdx.x / DB; j < l.nb; j += KV_JOIN) {
+        const int rows = l.total[(size_t)bg * l.nb + j] * l.G;
+        if (rows <= l.unit) continue;
+        const int units = (int)(((long long)rows + l.unit - 1) / l.unit), u0 = l.first_unit[(size_t)bg * l.nb + j];
+        const float4* in = (const float4*)f.kvpart + (((size_t)bg * l.maxu + u0) * 2 + (wv & 1)) * (2 * DB * 4 * 64) + (((wv >> 1) * DB + x) * 4) * 64 + lane;
+        float4 s[4];
 #pragma unroll
-    for (int y = 0; y < 4; y++) s[y] = make_float4(0, 0, 0, 0);
+        for (int y = 0; y < 4; y++) s[y] = make_float4(0, 0, 0, 0);
 #pragma unroll 4
-    for (int u = 0; u < units; u++)
+        for (int u = 0; u < units; u++)
 #pragma unroll
-        for (int y = 0; y < 4; y++) {
-            const float4 v = in[(size_t)u * (4 * DB * 4 * 64) + y * 64];
-            s[y].x += v.x; s[y].y += v.y; s[y].z += v.z; s[y].w += v.w;
-        }
-    const int key = 32 * (wv & 1) + (lane & 31);
-    if (j * BT + key >= l.n) return;
-    const float c = wv >> 1 ? f.a.scale : 1.0f;
-    uint16_t* out = (wv >> 1 ? f.dk : f.dv) + ((size_t)bg * l.n + (size_t)j * BT + key) * D + 32 * x + 4 * (lane >> 5);
+            for (int y = 0; y < 4; y++) {
+                const float4 v = in[(size_t)u * (4 * DB * 4 * 64) + y * 64];
+                s[y].x += v.x; s[y].y += v.y; s[y].z += v.z; s[y].w += v.w;
+            }
+        const int key = 32 * (wv & 1) + (lane & 31);
+        if (j * BT + key >= l.n) continue;
+        const float c = wv >> 1 ? f.a.scale : 1.0f;
+        uint16_t* out = (wv >> 1 ? f.dk : f.dv) + ((size_t)bg * l.n + (size_t)j * BT + key) * D + 32 * x + 4 * (lane >> 5);
 #pragma unroll
-    for (int y = 0; y < 4; y++) *(uint2*)(out + 8 * y) = make_uint2(pack_bf16x2(s[y].x * c, s[y].y * c), pack_bf16x2(s[y].z * c, s[y].w * c));
+        for (int y = 0; y < 4; y++) *(uint2*)(out + 8 * y) = make_uint2(pack_bf16x2(s[y].x * c, s[y].y * c), pack_bf16x2(s[y].z * c, s[y].w * c));
+    }
 }
 
 // D / 8 lanes per row (query, head of the group).
@@ -360,7 +364,14 @@ __global__ __launch_bounds__(256) void block_dq_join_kernel(BlockBwd f, int item
     *(u32x4*)(f.dq + (((size_t)b * l.H + g * G + gh) * l.n + i) * D + 8 * t) = out;
 }
 
-constexpr int BWD_UNIT = 1024;   // rows whose dK and dV are summed in registers
+// Rows whose dK and dV are summed in registers: most blocks have fewer and are finished by one workgroup (4 x 16 heads of 8192:
+// 2245, 2075, 1968 and 1962 us with 512, 1024, 2048 and 4096); where there are few rows altogether, a popular block's are
+// shared out to more of the chip.
+static int bwd_unit(const sparsek_block_cfg& c)
+{
+    const double rows = (double)c.B * c.H * c.n * (c.top + 1);
+    return rows >= 512 * 1024.0 ? 2048 : rows >= 256 * 1024.0 ? 1024 : 512;
+}
 
 struct BwdLayout {
     BlockLayout y;
@@ -369,7 +380,7 @@ struct BwdLayout {
 static BwdLayout bwd_layout(const sparsek_block_cfg& c, void* ws)
 {
     BwdLayout f;
-    f.y = block_lists_layout(c, block_count(c.n) * BT, BWD_UNIT, ws);
+    f.y = block_lists_layout(c, block_count(c.n) * BT, bwd_unit(c), ws);
     const size_t BG = (size_t)c.B * c.Hkv, rows = BG * f.y.l.entries * f.y.l.G;
     f.rows = f.y.bytes;
     f.part = align_up(f.rows + (size_t)c.B * c.H * c.n * 8, 256);
@@ -401,7 +412,7 @@ int launch_block_bwd(const sparsek_block_cfg& c, const void* q, const void* k, c
 #define BWD(D)                                                                                                                                   \
     hipLaunchKernelGGL((block_delta_kernel<D>), dim3((unsigned)((nrows * (D / 8) + 255) / 256)), dim3(256), 0, st, f, nrows);                     \
     hipLaunchKernelGGL((block_bwd_tiles_kernel<D>), dim3((unsigned)l.maxu * BG), dim3(256), 0, st, f);                                           \
-    hipLaunchKernelGGL((block_kv_join_kernel<D>), dim3(l.nb * (D / 32), BG), dim3(256), 0, st, f);                                               \
+    hipLaunchKernelGGL((block_kv_join_kernel<D>), dim3(std::min(l.nb, KV_JOIN) * (D / 32), BG), dim3(256), 0, st, f);                                               \
     const int items = (int)(((long long)c.n * l.G * (D / 8) + 255) / 256);                                                                       \
     hipLaunchKernelGGL((block_dq_join_kernel<D>), dim3((unsigned)items * BG), dim3(256), 0, st, f, items)
     if (c.d == 128) {

@@ -10,6 +10,9 @@ namespace spk {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
+// Scales of a head: whole tiles of 16.
+__host__ __device__ inline size_t scale_row(int nbw) { return (size_t)(nbw + 15) / 16 * 16; }
+
 // One workgroup of 256 per (whole block, batch and head): m8 and ms.
 template <int D>
 __global__ __launch_bounds__(256) void block_means_kernel(const uint16_t* __restrict__ k, int n, int nbw, int8_t* __restrict__ km,
@@ -40,7 +43,7 @@ __global__ __launch_bounds__(256) void block_means_kernel(const uint16_t* __rest
     }
     const float top = __uint_as_float(block_max_bits(__float_as_uint(fabsf(mean)), red, tid));
     if (tid < D) km[(bg * nbw + j) * D + tid] = (int8_t)code_i8(mean, code_factor(top, 127.0f));
-    if (tid == 0) kms[bg * nbw + j] = code_scale(top, 127.0f);
+    if (tid == 0) kms[bg * scale_row(nbw) + j] = code_scale(top, 127.0f);
 }
 
 // The sum and the largest over the four lanes col, col + 16, col + 32, col + 48.
@@ -62,7 +65,8 @@ __device__ __forceinline__ unsigned groups_max(unsigned x)
 // One workgroup of 4 waves per (64 queries, batch and head), a wave per 16 queries: a lane holds the order-preserving images of
 // the scores of every fourth group of 4 blocks for one query.  A threshold with exactly `top` scores at or above it is
 // found by bisection, first halfway between values, then between images; where equal scores leave no such threshold the first of
-// those that share the last place are taken.  Counting a score costs two instructions; a radix pass in LDS counters
+// those that share the last place are taken.  (Between the logarithms of the counts instead: 10 % slower, the logarithms cost more than
+// the steps they save.)  Counting a score costs two instructions; a radix pass in LDS counters
 // cost 4 to 8 times as much.  NT: tiles of 16 blocks whose images stay in registers; 0: any number, formed again for every count.
 template <int D, int NT>
 __global__ __launch_bounds__(256) void block_select_kernel(const uint16_t* __restrict__ q, int H, int Hkv, int n, int nbw, int top,
@@ -115,7 +119,8 @@ __global__ __launch_bounds__(256) void block_select_kernel(const uint16_t* __res
 #pragma unroll
         for (int e = 0; e < 4; e++) qf[s][e] = (int)q8[16 * wv + col][16 * s + 4 * grp + e];
     const int8_t* kmr = km + (size_t)bg * nbw * D;
-    const float* msr = kms + (size_t)bg * nbw;
+    const float* msr = kms + (size_t)bg * scale_row(nbw);
+    const int nt = (nbp + 15) / 16;
     typedef unsigned keys4 __attribute__((ext_vector_type(4)));
     // the images of blocks 16 t + 4 grp .. + 3 for query col; 0 (below every score) beyond the last block
     auto form = [&](int t) -> keys4 {
@@ -126,15 +131,18 @@ __global__ __launch_bounds__(256) void block_select_kernel(const uint16_t* __res
             const i32x4 a = *(const i32x4*)(kmr + (size_t)row * D + 64 * s + 16 * grp);
             acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, qf[s], acc, 0, 0, 0);
         }
+        const f32x4v ms = *(const f32x4v*)(msr + 16 * t + 4 * grp);   // (the scales' rows are whole tiles long)
         keys4 key;
 #pragma unroll
         for (int r = 0; r < 4; r++) {
-            const int j = 16 * t + 4 * grp + r;
-            key[r] = j < nbp ? min(max(score_key((float)acc[r] * msr[min(j, nbp - 1)]), 1u), 0xFFFFFFFEu) : 0u;
+            const unsigned b = __float_as_uint((float)acc[r] * ms[r] + 0.0f);   // (as score_key; 1 at least, and below the largest)
+            key[r] = min(max(b ^ ((unsigned)((int)b >> 31) | 0x80000000u), 1u), 0xFFFFFFFEu);
         }
+        if (t == nt - 1)
+#pragma unroll
+            for (int r = 0; r < 4; r++) key[r] = 16 * t + 4 * grp + r < nbp ? key[r] : 0u;
         return key;
     };
-    const int nt = (nbp + 15) / 16;
     keys4 kept[NT ? NT : 1];
     // f(t, images) for every tile, the numbers of tiles known to the compiler where they stay in registers
     auto each = [&](auto&& f) {
@@ -217,8 +225,8 @@ __global__ __launch_bounds__(256) void block_select_kernel(const uint16_t* __res
 
 size_t block_select_ws_bytes(const sparsek_block_cfg& c)
 {
-    const size_t rows = (size_t)c.B * c.Hkv * (c.n / BT);
-    return align_up(rows * c.d, 256) + align_up(rows * sizeof(float), 256);
+    const size_t BG = (size_t)c.B * c.Hkv, nbw = c.n / BT;
+    return align_up(BG * nbw * c.d, 256) + align_up(BG * scale_row(nbw) * sizeof(float), 256);
 }
 
 int launch_block_select(const sparsek_block_cfg& c, const void* q, const void* k, int32_t* idx, void* ws, hipStream_t st)
