@@ -81,17 +81,22 @@ struct BlockArgs {
 };
 
 #ifdef __HIPCC__
-// 64 rows of D bf16 (contiguous rows at src, row r clamped to r_max) into a RowTile; 256 threads.
+// 64 rows of D bf16 (contiguous rows at src, row r clamped to r_max) into a RowTile; 256 threads.  Returns the largest magnitude that
+// the thread has seen, as bits.
 template <int D>
-__device__ __forceinline__ void load_rows(unsigned char* tile, const uint16_t* src, int r_max, int tid)
+__device__ __forceinline__ unsigned load_rows(unsigned char* tile, const uint16_t* src, int r_max, int tid)
 {
     constexpr int CPR = D / 8;   // 16-byte pieces per row
+    unsigned top = 0;
 #pragma unroll
     for (int t = 0; t < BT * CPR / 256; t++) {
         const int id = tid + 256 * t, r = id / CPR, c = id % CPR;
         const u32x4 x = *(const u32x4*)(src + (size_t)min(r, r_max) * D + 8 * c);
         *(u32x4*)(tile + RowTile<D>::offset(r) + 16 * c) = x;
+#pragma unroll
+        for (int e = 0; e < 4; e++) top = max(top, max(x[e] << 16 & 0x7FFFFFFFu, x[e] & 0x7FFF0000u));
     }
+    return top;
 }
 
 // Rounds to whole numbers of at most 127: the mean key of a block, the pooled query, a block held in 8 bits.  The factor is the
@@ -155,14 +160,34 @@ __device__ __forceinline__ void deal_head(unsigned id, int items, int BG, int& b
 }
 
 // The largest of a workgroup's 256 values (>= 0, as bits); red: 4 words of LDS.  Two barriers.
+__device__ __forceinline__ unsigned wave_max_bits(unsigned x)
+{
+    int y = (int)x;
+#pragma unroll
+    for (int s = 0; s < 4; s++) y = max(y, dpp_i32(y, s));
+    return (unsigned)max(max(__builtin_amdgcn_readlane(y, 15), __builtin_amdgcn_readlane(y, 31)), max(__builtin_amdgcn_readlane(y, 47), __builtin_amdgcn_readlane(y, 63)));
+}
 __device__ __forceinline__ unsigned block_max_bits(unsigned x, unsigned* red, int tid)
 {
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) x = max(x, (unsigned)__shfl_xor((int)x, s, 64));
+    x = wave_max_bits(x);
     __syncthreads();
     if ((tid & 63) == 0) red[tid >> 6] = x;
     __syncthreads();
     return max(max(red[0], red[1]), max(red[2], red[3]));
+}
+// The largest of a workgroup's 256 values (>= 0, as bits) twice; red: 8 words of LDS.  Two barriers.
+__device__ __forceinline__ void block_max_bits2(unsigned& x, unsigned& y, unsigned* red, int tid)
+{
+    x = wave_max_bits(x);
+    y = wave_max_bits(y);
+    __syncthreads();
+    if ((tid & 63) == 0) {
+        red[tid >> 6] = x;
+        red[4 + (tid >> 6)] = y;
+    }
+    __syncthreads();
+    x = max(max(red[0], red[1]), max(red[2], red[3]));
+    y = max(max(red[4], red[5]), max(red[6], red[7]));
 }
 #endif
 

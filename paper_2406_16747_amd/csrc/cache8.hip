@@ -49,24 +49,6 @@ struct AppendSmem {
     unsigned red[8];
 };
 
-// The largest of a workgroup's 256 values (>= 0, as bits) in two of them at once.  Two barriers.
-__device__ __forceinline__ void block_max_bits2(unsigned& x, unsigned& y, unsigned* red, int tid)
-{
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) {
-        x = max(x, (unsigned)__shfl_xor((int)x, s, 64));
-        y = max(y, (unsigned)__shfl_xor((int)y, s, 64));
-    }
-    __syncthreads();
-    if ((tid & 63) == 0) {
-        red[tid >> 6] = x;
-        red[4 + (tid >> 6)] = y;
-    }
-    __syncthreads();
-    x = max(max(red[0], red[1]), max(red[2], red[3]));
-    y = max(max(red[4], red[5]), max(red[6], red[7]));
-}
-
 // A whole block goes to its page: codes, scales and the mean key.  The keys are in registers, the values (transposed) in sm.vt; every
 // thread has seen the end of what was written there.
 template <int D, int FORMAT>
@@ -477,6 +459,9 @@ __global__ __launch_bounds__(256, 3) void cache8_attn_kernel(AttnArgs a)
     const int groups = (a.c.G + 15) / 16;
     const int split = blockIdx.x, g = blockIdx.y / groups, rg = blockIdx.y % groups, b = blockIdx.z;
     const size_t bg = (size_t)b * a.c.Hkv + g;
+    const int u0 = split * 4 * a.upw + wv * a.upw;
+    // (the pages are asked for ahead of the length, of which they depend in number only)
+    const int early = a.c.t.table[bg * a.c.cap + min(u0 + min(lane, a.upw - 1), a.c.cap - 1)];
     const RowUnits ru = row_units(a, b);
     const int nu = ru.nsel + (ru.tail ? 1 : 0);
     const bool alone = a.splits == 1 && groups == 1;   // the workgroup has all units of all heads of the group
@@ -484,11 +469,15 @@ __global__ __launch_bounds__(256, 3) void cache8_attn_kernel(AttnArgs a)
     const int live = min(16, a.c.G - rg * 16);
     const size_t head0 = (size_t)b * a.c.H + g * a.c.G + rg * 16;
     // the wave's units, one to a lane: page (of any unit that has one where there is none), scales
-    const int u0 = split * 4 * a.upw + wv * a.upw, count = max(0, min(a.upw, ru.nsel - u0));
+    const int count = max(0, min(a.upw, ru.nsel - u0));
     int page = -1;
     if (lane < count) {
-        const int j = unit_block(a, ru, bg, u0 + lane);
-        if (j >= 0) page = a.c.t.table[bg * a.c.cap + j];
+        if (a.idx) {
+            const int j = unit_block(a, ru, bg, u0 + lane);
+            if (j >= 0) page = a.c.t.table[bg * a.c.cap + j];
+        } else {
+            page = early;
+        }
         if (page >= a.c.pages) page = -1;
     }
     const unsigned long long have = __ballot(page >= 0);
@@ -747,14 +736,18 @@ __global__ __launch_bounds__(256) void cache8_join_kernel(AttnArgs a, int mass_w
         if (tid == 0) a.lse[row] = top > -INFINITY ? (top + log2f(all * 0x1p-15f)) * 0.6931471805599453f : -INFINITY;
         return;
     }
-    auto total = [&](int h, float& M, float& L) {   // of head h, by a wave
+    auto total = [&](int h) {   // log2 of head h's sum, by a wave
         const float2* p = a.part_ml + ((size_t)b * a.c.H + h) * a.splits;
-        M = -INFINITY;
-        L = 0.0f;
-        for (int s = lane; s < splits; s += 64) M = fmaxf(M, p[s].x);
-        M = wave_max_f32(M);
-        for (int s = lane; s < splits; s += 64) L += M > -INFINITY ? p[s].y * __builtin_amdgcn_exp2f(p[s].x - M) : 0.0f;
-        L = wave_sum_f32(L);
+        float M = -INFINITY, L = 0.0f;
+        for (int s = lane; s < splits; s += 64) {
+            const float2 x = p[s];
+            const float top = fmaxf(M, x.x);
+            if (x.x > -INFINITY) L = L * __builtin_amdgcn_exp2f(M - top) + x.y * __builtin_amdgcn_exp2f(x.x - top);
+            M = top;
+        }
+        const float top = wave_max_f32(M);
+        L = wave_sum_f32(M > -INFINITY ? L * __builtin_amdgcn_exp2f(M - top) : 0.0f);
+        return top + log2f(L * 0x1p-15f);
     };
     const int g = (blockIdx.x - a.c.H) / mass_wgs, part = (blockIdx.x - a.c.H) % mass_wgs;
     if (part * 256 >= nu) return;
@@ -762,20 +755,18 @@ __global__ __launch_bounds__(256) void cache8_join_kernel(AttnArgs a, int mass_w
     const int u = part * 256 + tid;
     float sum = 0.0f;
     for (int r0 = 0; r0 < G; r0 += 4) {   // a wave per head
-        __syncthreads();
+        float w[4];
+#pragma unroll
+        for (int x = 0; x < 4; x++) w[x] = u < nu && r0 + x < G ? a.weight[((size_t)b * a.c.H + g * G + r0 + x) * a.units + u] : -INFINITY;
         if (r0 + wv < G) {
-            float M, L;
-            total(g * G + r0 + wv, M, L);
-            if (lane == 0) logs[wv] = M + log2f(L * 0x1p-15f);
+            const float all = total(g * G + r0 + wv);
+            if (lane == 0) logs[wv] = all;
         }
         __syncthreads();
-        if (u < nu)
 #pragma unroll
-            for (int x = 0; x < 4; x++)
-                if (r0 + x < G) {
-                    const float w = a.weight[((size_t)b * a.c.H + g * G + r0 + x) * a.units + u];
-                    if (w > -INFINITY) sum += __builtin_amdgcn_exp2f(w - logs[x]);
-                }
+        for (int x = 0; x < 4; x++)
+            if (w[x] > -INFINITY) sum += __builtin_amdgcn_exp2f(w[x] - logs[x]);
+        __syncthreads();
     }
     if (u < nu) add_mass(a, ru, bg, u, sum);
 }

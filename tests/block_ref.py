@@ -2,8 +2,9 @@
 on how far a kernel's results may be from them.
 
 A value rounded to bf16 is off by at most 2^-8 of itself (half a step), one rounded to fp16 by 2^-11.  The kernels round every
-output once to bf16; the weights p to fp16 in the forward and over the cache and to bf16 in the backward, the score gradients ds to bf16, and
-partial results to fp16 relative to the largest value of their block; sums are fp32 (d products of 2^-24 each; 2^-14 covers them and the exponentials with room, for logits below 2^5)."""
+output once to bf16; the weights p to fp16 in the forward and over the cache and to bf16 in the backward; the score gradients ds to
+fp16 for dq and to the sum of two bf16 numbers for dk; partial results to fp16 relative to the largest value of their block.  Sums
+are fp32 (d products of 2^-24 each; 2^-14 covers them and the exponentials with room, for logits below 2^5)."""
 import numpy as np
 import torch
 
@@ -96,14 +97,14 @@ def attn_bwd(q, k, v, idx, o, lse, dO, scale):
                 p = torch.exp((q[b, h] @ k[b, g].T * scale).masked_fill(~see, -np.inf) - lse[b, h][:, None])
                 dp, delta = dO[b, h] @ v[b, g].T, (dO[b, h] * o[b, h]).sum(1, keepdim=True)
                 ds = p * (dp - delta) * scale
-                # what is rounded (ds), and what the sums behind it lose: of dp and delta, and of p
-                e = (2 ** -8 + 2 ** -11 + 2 ** -14) * ds.abs() + 2 ** -17 * p * (dO[b, h].abs() @ v[b, g].abs().T + (dO[b, h] * o[b, h]).abs().sum(1, keepdim=True)) * scale
+                # what the sums behind ds lose, of dp and delta, and of p; then ds is rounded, to two bf16 numbers for dk and to fp16 for dq
+                e = 2 ** -14 * ds.abs() + 2 ** -17 * p * (dO[b, h].abs() @ v[b, g].abs().T + (dO[b, h] * o[b, h]).abs().sum(1, keepdim=True)) * scale
                 dv[b, g] += p.T @ dO[b, h]
                 dk[b, g] += ds.T @ q[b, h]
                 dq[b, h] = ds @ k[b, g]
                 av[b, g] += (2 ** -8 + 2 ** -14) * p.T @ dO[b, h].abs()
-                ak[b, g] += e.T @ q[b, h].abs()
-                aq[b, h] = e @ k[b, g].abs() + 2 ** -22 * (ds.abs() @ k[b, g].abs()).amax(1, keepdim=True)
+                ak[b, g] += (e + 2 ** -16 * ds.abs()).T @ q[b, h].abs()
+                aq[b, h] = (e + (2 ** -11 + 2 ** -11) * ds.abs()) @ k[b, g].abs() + 2 ** -22 * (ds.abs() @ k[b, g].abs()).amax(1, keepdim=True)
     return (dq, dk, dv), tuple(2 ** -8 * x.abs() + a + 1e-30 for x, a in ((dq, aq), (dk, ak), (dv, av)))
 
 

@@ -174,7 +174,7 @@ def check_rows(q, k, v, dO, idx, o, dq, scale, heads, rows):
                 continue
             g, oo = ref.f64(dO[0, h, i]), ref.f64(o[0, h, i])
             ds = p * (V[at] @ g - (g * oo).sum()) * scale
-            e = (2 ** -8 + 2 ** -11 + 2 ** -14) * ds.abs() + 2 ** -17 * p * (V[at].abs() @ g.abs() + (g * oo).abs().sum()) * scale
+            e = (2 ** -11 + 2 ** -11 + 2 ** -14) * ds.abs() + 2 ** -17 * p * (V[at].abs() @ g.abs() + (g * oo).abs().sum()) * scale
             want = ds @ K[at]
             within(dq[0, h, i], want, 2 ** -8 * want.abs() + e @ K[at].abs() + 2 ** -22 * (ds.abs() @ K[at].abs()).max(), "dq of row %d" % i)
 
