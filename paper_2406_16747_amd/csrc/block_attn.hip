@@ -305,7 +305,7 @@ struct FwdBlockSmem {
     static constexpr int RS = 128 + 16;     // bytes between rows: half a row of 128 columns
     unsigned char k[RowTile<D>::BYTES], v[RowTile<D>::BYTES];
     unsigned char rows[4][32 * RS];         // a wave's rows on their way in and its results on their way out
-    unsigned red[4];
+    unsigned red[4], bad[2][2];             // bad: keys that are not finite, or have values that are not, as bits
 };
 static_assert(sizeof(FwdBlockSmem<128>) <= 160 * 1024 / 3, "three workgroups per CU");
 
@@ -327,18 +327,29 @@ __global__ __launch_bounds__(256, 3) void block_tiles_kernel(BlockFwd f)
     const int end = min(l.total[cbg * l.nb + j] * G, first + l.unit);
     const size_t kv = ((size_t)bg * l.n + (size_t)j * BT) * D;
     const int last = l.n - 1 - j * BT;
-    load_rows<D>(sm.k, f.a.k + kv, last, tid);
-    // V goes to fp16 relative to its largest magnitude
+    // V goes to fp16 relative to its largest magnitude.  What is not finite in a key or in its values is left out of that and of the
+    // products, and makes the rows that attend the key NaN.
     u32x4 vr[BT * CPR / 256];
-    unsigned top = 0;
+    unsigned top = 0, bad_k = 0, bad_v = 0;
 #pragma unroll
     for (int t = 0; t < BT * CPR / 256; t++) {
         const int id = tid + 256 * t;
         vr[t] = *(const u32x4*)(f.a.v + kv + (size_t)min(id / CPR, last) * D + 8 * (id % CPR));
-#pragma unroll
-        for (int e = 0; e < 4; e++) top = max(top, max(vr[t][e] << 16 & 0x7FFFFFFFu, vr[t][e] & 0x7FFF0000u));
     }
-    const int E = scale_exp(block_max_bits(top, sm.red, tid));
+    load_rows<D>(sm.k, f.a.k + kv, last, tid, bad_k);
+#pragma unroll
+    for (int t = 0; t < BT * CPR / 256; t++) {
+        const unsigned y = top_of_8(vr[t]);
+        if (y >= INF_BITS) {
+            vr[t] = u32x4{0, 0, 0, 0};
+            bad_v |= 1u << t;
+        }
+        top = max(top, y >= INF_BITS ? 0u : y);
+    }
+    if (tid < 4) (&sm.bad[0][0])[tid] = 0;
+    const int E = scale_exp(block_max_bits(top, sm.red, tid));   // (with a barrier inside)
+    note_rows<D>(sm.bad[0], bad_k, tid);
+    note_rows<D>(sm.bad[1], bad_v, tid);
     const float down = scale_down(E), up = scale_up(E);
 #pragma unroll
     for (int t = 0; t < BT * CPR / 256; t++) {
@@ -349,6 +360,7 @@ __global__ __launch_bounds__(256, 3) void block_tiles_kernel(BlockFwd f)
         *(f16x8*)(sm.v + RowTile<D>::offset(id / CPR) + 16 * (id % CPR)) = y;
     }
     __syncthreads();
+    const unsigned long long badk = (unsigned long long)sm.bad[0][1] << 32 | sm.bad[0][0], badv = (unsigned long long)sm.bad[1][1] << 32 | sm.bad[1][0];
     const uint32_t rk = lds_address(sm.k) + row_lane<D>(lane), tv = lds_address(sm.v) + transposed_lane<D>(lane);
     const int b = bg / l.Hkv, g = bg % l.Hkv;
     const int32_t* list = l.list + cbg * l.entries + base;
@@ -395,7 +407,12 @@ __global__ __launch_bounds__(256, 3) void block_tiles_kernel(BlockFwd f)
         f16x8 pb[4];
         float m, den;
         block_weights<D>(rk, qf, f.a.c2, r0 < own_end, i - j * BT, half, pb, m, den);
-        const float inv = den > 0.0f ? 1.0f / den : den;   // (nothing but -inf: weight 0 in the sum)
+        float inv = den > 0.0f ? 1.0f / den : den;   // (nothing but -inf: weight 0 in the sum)
+        if (badk | badv) {
+            const unsigned long long attended = (2ull << min(BT - 1, i - j * BT)) - 1;
+            inv = (badk | badv) & attended ? __uint_as_float(0x7FC00000u) : inv;
+            den = badk & attended ? __uint_as_float(0x7FC00000u) : den;
+        }
         // (rows behind the last one, and the upper lanes' copy of the logarithms, lie outside the buffers and are dropped)
         const int count = min(32, end - r0);
         const auto dst = buffer_of(f.part + (row0 + r0) * D, 2 * D * count);

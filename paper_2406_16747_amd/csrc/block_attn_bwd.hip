@@ -51,8 +51,9 @@ struct BwdBlockSmem {
     struct Rows {                           // of one tile
         float lse2[BT], delta[BT];
         float down[BT], up[BT];             // to and from the row's dS in fp16
-        int limit[BT];                      // keys 0 .. limit are attended
+        int limit[BT];                      // keys 0 .. limit are attended; BT more: one of the block's own rows that is not finite
         int at[BT];                         // the row's place in [G,n]
+        unsigned bad[2];                    // rows whose lse, o or dO is not finite, as bits
     } rows[2];                              // the tile in use and the next one
     unsigned red[8];
 };
@@ -97,7 +98,10 @@ __device__ __forceinline__ void bwd_block_tile(BwdBlockSmem<D>& sm, const typena
             const int4 L4 = *(const int4*)&rows.limit[32 * rb + 8 * g4 + 4 * half];
             const int ll[4] = {L4.x, L4.y, L4.z, L4.w};
 #pragma unroll
-            for (int e = 0; e < 4; e++) s[4 * g4 + e] = 32 * kb + col > ll[e] ? -INFINITY : s[4 * g4 + e];
+            for (int e = 0; e < 4; e++) {
+                const float x = ll[e] < BT ? s[4 * g4 + e] : __uint_as_float(0x7FC00000u);
+                s[4 * g4 + e] = 32 * kb + col > (ll[e] & BT - 1) ? -INFINITY : x;
+            }
         }
     // As operands: weights in bf16 (2^-8), for dV.  Score gradients cancel in their sums (a row's add up to 0), so they keep more: the sum
     // of two bf16 numbers for dK (two products; the error of dK falls from 1.5 times that of its own rounding to 1.1, for 2 % of a
@@ -216,7 +220,7 @@ __device__ __forceinline__ void store_kv(const BlockBwd& f, size_t kv, int key, 
 }
 
 template <int D>
-__global__ __launch_bounds__(256, 2) void block_bwd_tiles_kernel(BlockBwd f)
+__global__ __launch_bounds__(256, D == 128 ? 2 : 3) void block_bwd_tiles_kernel(BlockBwd f)
 {
     __shared__ __attribute__((aligned(16))) BwdBlockSmem<D> sm;
     constexpr int DB = D / 32;
@@ -230,7 +234,8 @@ __global__ __launch_bounds__(256, 2) void block_bwd_tiles_kernel(BlockBwd f)
     const int base = l.base[(size_t)bg * l.nb + j], rows = l.total[(size_t)bg * l.nb + j] * G, end = min(rows, first + l.unit);
     const size_t kv = ((size_t)bg * l.n + (size_t)j * BT) * D;
     const int last = l.n - 1 - j * BT;
-    unsigned topk = load_rows<D>(sm.k, f.a.k + kv, last, tid), topv = load_rows<D>(sm.v, f.a.v + kv, last, tid);
+    // (rows that attend a key which is not finite have an lse or an o that is not, and the others must not see it)
+    unsigned unused = 0, topk = load_rows<D>(sm.k, f.a.k + kv, last, tid, unused), topv = load_rows<D>(sm.v, f.a.v + kv, last, tid, unused);
     block_max_bits2(topk, topv, sm.red, tid);
     const int Ek = scale_exp(topk);
     const float kdown = scale_down(Ek), kup = scale_up(Ek), vmax = __uint_as_float(topv);
@@ -244,12 +249,17 @@ __global__ __launch_bounds__(256, 2) void block_bwd_tiles_kernel(BlockBwd f)
     auto entry = [&](int r) { return list[min(r, end - 1) / G]; };
     auto place = [&](int r, int i) { return min(r, end - 1) % G * l.n + i; };
     auto put = [&](typename BwdBlockSmem<D>::Rows& rows, int r, int i, float4 m) {
+        const bool bad = r < end && !(fabsf(m.x) < INFINITY && fabsf(m.y) < INFINITY && m.z < INFINITY);
+        const unsigned long long all = __ballot(bad);
+        if (lane < 2) rows.bad[lane] = (unsigned)(all >> (32 * lane));
+        // such a row: weights of NaN for the keys that it attends (all of a selected block, in the own block by `limit`), q and dO of 0
+        if (bad) m = make_float4(r < own_end ? 0.0f : __uint_as_float(0x7FC00000u), 0.0f, 0.0f, 0.0f);
         rows.lse2[lane] = r < end ? m.x : INFINITY;   // (a row that does not exist: p = 0)
         rows.delta[lane] = r < end ? m.y : 0.0f;
         const int E = scale_exp(__float_as_uint(fmaf(m.z, vmax, fabsf(m.y))));
         rows.down[lane] = scale_down(E);
         rows.up[lane] = scale_up(E) * f.a.scale;
-        rows.limit[lane] = min(BT - 1, i - j * BT);
+        rows.limit[lane] = min(BT - 1, i - j * BT) + (bad && r < own_end ? BT : 0);
         rows.at[lane] = place(r, i);
     };
     int i_next = 0;
@@ -265,8 +275,21 @@ __global__ __launch_bounds__(256, 2) void block_bwd_tiles_kernel(BlockBwd f)
     issue_query_rows<D>(sm, sm.rows[0], q0, g0, wv, lane);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     int buf = 0;
+    unsigned bad0 = sm.rows[0].bad[0], bad1 = sm.rows[0].bad[1];
     for (int r0 = first; r0 < end; r0 += BT, buf ^= 1) {
         __syncthreads();   // the tile's rows have landed
+        bad0 = __builtin_amdgcn_readfirstlane(bad0);
+        bad1 = __builtin_amdgcn_readfirstlane(bad1);
+        if (bad0 | bad1) {
+            for (int x = tid; x < BT * (D / 8); x += 256) {
+                const int r = x / (D / 8), c = x % (D / 8);
+                if ((r >> 5 ? bad1 : bad0) >> (r & 31) & 1) {
+                    *(u32x4*)(sm.q + RowTile<D>::offset(r) + 16 * c) = u32x4{0, 0, 0, 0};
+                    *(u32x4*)(sm.g + RowTile<D>::offset(r) + 16 * c) = u32x4{0, 0, 0, 0};
+                }
+            }
+            __syncthreads();
+        }
         float4 m = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         int i_then = 0;
         if (wv == 0) {
@@ -280,6 +303,8 @@ __global__ __launch_bounds__(256, 2) void block_bwd_tiles_kernel(BlockBwd f)
         }
         __syncthreads();   // dS is there, and nobody reads the rows any more
         if (r0 + BT < end) issue_query_rows<D>(sm, sm.rows[buf ^ 1], q0, g0, wv, lane);
+        bad0 = sm.rows[buf ^ 1].bad[0];
+        bad1 = sm.rows[buf ^ 1].bad[1];
         f32x16 acc_q[DB / 2];
         bwd_block_dq<D>(sm, lane, wv, kdown, sm.rows[buf].up[rt] * kup, acc_q);
         // the partial dq of rows 32 rb + col, columns of half kb, relative to the largest of them

@@ -81,20 +81,44 @@ struct BlockArgs {
 };
 
 #ifdef __HIPCC__
-// 64 rows of D bf16 (contiguous rows at src, row r clamped to r_max) into a RowTile; 256 threads.  Returns the largest magnitude that
-// the thread has seen, as bits.
+// Notes the rows of the pieces that load_rows (or a loop like it) found to be not finite in rows[2], as bits.
 template <int D>
-__device__ __forceinline__ unsigned load_rows(unsigned char* tile, const uint16_t* src, int r_max, int tid)
+__device__ __forceinline__ void note_rows(unsigned* rows, unsigned bad, int tid)
+{
+    for (; bad; bad &= bad - 1) {
+        const int r = (tid + 256 * (__ffs(bad) - 1)) / (D / 8);
+        atomicOr(&rows[r >> 5], 1u << (r & 31));
+    }
+}
+// The largest magnitude of 8 bf16 values, as bits of a float.
+__device__ __forceinline__ unsigned top_of_8(u32x4 x)
+{
+    unsigned top = 0;
+#pragma unroll
+    for (int e = 0; e < 4; e++) top = max(top, max(x[e] << 16 & 0x7FFFFFFFu, x[e] & 0x7FFF0000u));
+    return top;
+}
+constexpr unsigned INF_BITS = 0x7F800000u;
+
+// 64 rows of D bf16 (contiguous rows at src, row r clamped to r_max) into a RowTile; 256 threads.  Returns the largest finite magnitude
+// that the thread has seen, as bits.  Pieces with an infinity or a NaN become zeros (a weight of zero times one of those would reach
+// rows that do not attend the key), and are noted in `bad`, a bit each.
+template <int D>
+__device__ __forceinline__ unsigned load_rows(unsigned char* tile, const uint16_t* src, int r_max, int tid, unsigned& bad)
 {
     constexpr int CPR = D / 8;   // 16-byte pieces per row
     unsigned top = 0;
 #pragma unroll
     for (int t = 0; t < BT * CPR / 256; t++) {
         const int id = tid + 256 * t, r = id / CPR, c = id % CPR;
-        const u32x4 x = *(const u32x4*)(src + (size_t)min(r, r_max) * D + 8 * c);
+        u32x4 x = *(const u32x4*)(src + (size_t)min(r, r_max) * D + 8 * c);
+        const unsigned y = top_of_8(x);
+        if (y >= INF_BITS) {
+            x = u32x4{0, 0, 0, 0};
+            bad |= 1u << t;
+        }
+        top = max(top, y >= INF_BITS ? 0u : y);
         *(u32x4*)(tile + RowTile<D>::offset(r) + 16 * c) = x;
-#pragma unroll
-        for (int e = 0; e < 4; e++) top = max(top, max(x[e] << 16 & 0x7FFFFFFFu, x[e] & 0x7FFF0000u));
     }
     return top;
 }

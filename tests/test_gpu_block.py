@@ -57,21 +57,22 @@ def test_selection_is_the_definitions(shape):
     assert torch.equal(idx.cpu(), ref.select(q, k, top))
 
 
-def test_selection_of_many_blocks():
-    """More blocks than a wave takes at a time, top of 1, 17 and 64; scores that differ in their last bits only."""
+@pytest.mark.parametrize("n,d,tops", [(9000, 64, (1, 17, 64)), (40000, 128, (5,)), (300000, 64, (3,))])
+def test_selection_of_many_blocks(n, d, tops):
+    """More blocks than a wave keeps in registers (128 and 512 of them), more than 4096; scores that differ in their last bits only."""
     require_gpu()
-    say("block select, many blocks")
-    q, k, _, _ = draw(12, 1, 2, 1, 9000, 64)
-    k = (k * 0.001 + torch.randn(64, generator=torch.Generator().manual_seed(1)).cuda()).bfloat16()
-    for top in (1, 17, 64):
+    say("block select, many blocks", n, d, tops)
+    g = torch.Generator(device="cuda").manual_seed(12)
+    q, k = (torch.randn(1, h, n, d, device="cuda", generator=g) for h in (2, 1))
+    q, k = q.bfloat16(), (k * 0.001 + torch.randn(d, device="cuda", generator=g)).bfloat16()
+    nb = n // 64
+    m8, ms = ref.mean_codes(k[0, 0, :nb * 64].view(nb, 64, d))
+    for top in tops:
         idx = spk.sparsek_block_select(q, k, top).cpu()
-        rows = list(range(0, 9000, 777)) + [8999]
-        want = ref.select(q, k, top) if top == 17 else None
-        if want is not None:
-            assert torch.equal(idx, want)
-        for i in rows:
-            got = [j for j in idx[0, 0, i].tolist() if j >= 0]
-            assert got == sorted(set(got)) and len(got) == min(top, i // 64) and all(j < i // 64 for j in got)
+        for i in list(range(0, n, n // 11)) + [n - 1]:
+            p8, _ = ref.codes_i8(ref.f64(q[0, :, i]).sum(0).float())
+            score = (m8.double() @ p8.double()).float() * ms
+            assert idx[0, 0, i].tolist() == ref.top_of(score, [j < i // 64 for j in range(nb)], top), (top, i)
 
 
 @pytest.mark.parametrize("kind", ["equal keys", "zeros", "tiny", "huge", "one sign"])
@@ -209,6 +210,65 @@ def test_documents_of_several_stretches(H, Hkv, n, top):
     torch.cuda.synchronize()
     assert ((mass.double().sum(2) / (n * (H // Hkv)) - 1).abs() < 1e-5).all()
     check_rows(q, k, v, None, idx, o, None, scale, (0, H // 2, H - 1), list(range(0, n, n // 9)) + [n - 1])
+
+
+def test_more_blocks_than_one_pass_of_the_lists():
+    """300000 tokens have 4688 blocks; the lists take 4096 at a time."""
+    require_gpu()
+    say("block attention, 300000 tokens")
+    n, d, top = 300000, 64, 3
+    g = torch.Generator(device="cuda").manual_seed(8)
+    q, k, v, dO = (torch.randn(1, 1, n, d, device="cuda", generator=g).bfloat16() for _ in range(4))
+    idx = torch.randint(-1, n // 64, (1, 1, n, top), device="cuda", generator=g, dtype=torch.int32)
+    idx[:, :, :, 2] = idx[:, :, :, 0]       # (and every block twice)
+    o, lse, mass = spk.sparsek_block_attn_fwd(q, k, v, idx, 0.125, mass=True)
+    dq, dk, dv = spk.sparsek_block_attn_bwd(q, k, v, idx, o, lse, dO, 0.125)
+    torch.cuda.synchronize()
+    assert abs(float(mass.double().sum()) / n - 1) < 1e-5
+    seen = torch.where(idx < (torch.arange(n, device="cuda") // 64).view(1, 1, n, 1), idx, -1)
+    seen[..., 2] = -1
+    seen[..., 1] = torch.where(seen[..., 1] == seen[..., 0], -1, seen[..., 1])
+    check_rows(q, k, v, dO, seen.cpu(), o, dq, 0.125, (0,), list(range(0, n, 23456)) + [n - 1, n - 37856])
+    assert torch.isfinite(dk).all() and torch.isfinite(dv).all()
+
+
+@pytest.mark.parametrize("what", ["q", "k", "v", "dO"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("d", [64, 128])
+def test_values_that_are_not_finite_reach_who_attends_them(what, value, d):
+    """One such value, in a block that some rows attend and others do not, and in front of and behind queries of its own block: the
+    rows that do not attend its key (or, for q and dO, the keys that its row does not attend) have the results they have without it."""
+    require_gpu()
+    say("block attention,", what, value)
+    n, H, at, top = 500, 2, 150, 2
+    q, k, v, dO = draw(83, 1, H, 1, n, d)
+    idx = spk.sparsek_block_select(q, k, top)
+    x = dict(q=q, k=k, v=v, dO=dO)
+    runs = []
+    for spoil in (False, True):
+        if spoil:
+            x[what][0, 0, at, 7] = value
+        o, lse, mass = spk.sparsek_block_attn_fwd(q, k, v, idx, 0.125, mass=True)
+        runs.append((o, lse) + spk.sparsek_block_attn_bwd(q, k, v, idx, o, lse, dO, 0.125))
+    torch.cuda.synchronize()
+    (o, lse, dq, dk, dv), (o1, lse1, dq1, dk1, dv1) = runs
+    see = ref.seen(idx[0, 0].cpu().numpy(), n).cuda()          # [queries, keys]
+    if what in ("k", "v"):
+        rows = see[:, at]                                      # who attends the key
+        for h in range(H):
+            assert torch.equal(o[0, h][~rows], o1[0, h][~rows]) and torch.equal(dq[0, h][~rows], dq1[0, h][~rows])
+            assert torch.equal(lse[0, h][~rows], lse1[0, h][~rows])
+            bad = ~torch.isfinite(o1[0, h]).all(1)
+            assert torch.equal(bad[rows], torch.ones_like(bad[rows]))
+        keys = see[rows].any(0)                                # keys that those rows attend
+        assert torch.equal(dk[0, 0][~keys], dk1[0, 0][~keys]) and torch.equal(dv[0, 0][~keys], dv1[0, 0][~keys])
+    else:
+        rows = torch.arange(n, device="cuda") != at
+        assert torch.equal(o[0, 0][rows], o1[0, 0][rows]) and torch.equal(o[0, 1], o1[0, 1])
+        assert torch.equal(dq[0, 0][rows], dq1[0, 0][rows]) and torch.equal(dq[0, 1], dq1[0, 1])
+        keys = see[at]
+        assert torch.equal(dk[0, 0][~keys], dk1[0, 0][~keys]) and torch.equal(dv[0, 0][~keys], dv1[0, 0][~keys])
+        assert not torch.isfinite(dk1[0, 0][keys]).all(1).any()
 
 
 def test_results_do_not_depend_on_timing():
