@@ -40,8 +40,11 @@ class SparsekCache8Cfg(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("B", "H", "Hkv", "d", "cap", "pages", "format", "dtype")] + [("softmax_scale", C.c_float)]
 
 
+_CACHE8_TENSORS = ("k8", "v8", "ks", "vs", "km", "kms", "kt", "vt", "table", "mass")
+
+
 class SparsekCache8(C.Structure):
-    _fields_ = [(n, C.c_void_p) for n in ("k8", "v8", "ks", "vs", "km", "kms", "kt", "vt", "table", "mass")]
+    _fields_ = [(n, C.c_void_p) for n in _CACHE8_TENSORS]
 
 
 def lib_path():
@@ -603,9 +606,13 @@ class Cache8:
             raise ValueError("unsupported cache configuration")
         self._ref()
 
+    def __setattr__(self, name, value):
+        if name in _CACHE8_TENSORS and hasattr(self, "cref"):   # (the calls go by the addresses taken in the constructor)
+            raise AttributeError("the tensors of a Cache8 stay; adopt() takes another table and masses")
+        object.__setattr__(self, name, value)
+
     def _ref(self):
-        self.c = SparsekCache8(*(t.data_ptr() for t in (self.k8, self.v8, self.ks, self.vs, self.km, self.kms, self.kt, self.vt,
-                                                        self.table, self.mass)))
+        self.c = SparsekCache8(*(getattr(self, n).data_ptr() for n in _CACHE8_TENSORS))
         self.ref, self.cref = C.byref(self.cfg), C.byref(self.c)
 
     @classmethod
@@ -625,7 +632,8 @@ class Cache8:
         """From now on with this table and these masses (those that sparsek_cache8_evict gave)."""
         _same("table", table, torch.int32, (self.B, self.Hkv, self.cap), self.device)
         _same("mass", mass, torch.float32, (self.B, self.Hkv, self.cap), self.device)
-        self.table, self.mass = table, mass
+        object.__setattr__(self, "table", table)
+        object.__setattr__(self, "mass", mass)
         self._ref()
 
 

@@ -335,12 +335,13 @@ __global__ __launch_bounds__(1024) void cache8_select_kernel(CacheArgs a, const 
 // ---- attention of a single query per sequence ----
 
 // A workgroup has 4 waves, and a wave takes whole blocks: S = K.Q^T (64 tokens by 16 heads), the running softmax, O^T += V^T.P^T.
-// The pieces of a block go from memory to the matrix instructions without LDS or lane exchange: row m of S's tile t is token
-// 16 (m / 4) + 4 t + m % 4, so a lane's 16 weights are those of the 16 tokens whose values it loads for every column.  Codes of 8
+// A block goes through LDS, in loads of whole lines: loaded as the operands have it, 16 bytes of a row to a lane, every lane is a line of
+// its own to the cache, which takes four times as many cycles (a sequence of 32768 tokens 29.8 us then, 26.7 now; 64 of up to 8192 155 and 150).  Between S and O nothing is exchanged: row m of S's tile t is
+// token 16 (m / 4) + 4 t + m % 4, so a lane's 16 weights are those of the 16 tokens whose values it reads for every column.  Codes of 8
 // bits are exact in fp16; so is q relative to its largest value (what fp16 drops lies 2^-27 below it), and weights lose 2^-11
-// where bf16 would lose 2^-8.  What bounds it is memory: a wave has the keys of one block and the values of another on
+// where bf16 would lose 2^-8.  What bounds it is memory: a wave has the keys of one block or the values of another on
 // their way while it computes.
-constexpr int MAX_UPW = 5;
+constexpr int MAX_UPW = 5, MAX_CAP = 8192;   // units of a wave, blocks of a row at most
 struct AttnArgs {
     CacheArgs c;
     const uint16_t* q;
@@ -397,14 +398,16 @@ __device__ __forceinline__ RowUnits row_units(const AttnArgs& a, int b)
     return r;
 }
 // The place in the table of unit u < nsel, -1: none (no whole block behind the query's own, or one named before).
-__device__ __forceinline__ int unit_block(const AttnArgs& a, const RowUnits& r, size_t bg, int u)
+// seen: the blocks that units ahead of `first` name, as bits (first == 0: not read).
+__device__ __forceinline__ int unit_block(const AttnArgs& a, const RowUnits& r, size_t bg, int u, int first, const unsigned* seen)
 {
     if (!a.idx) return u;
     if (u == a.top) return r.own;
     const int32_t* row = a.idx + bg * a.top;
     const int x = row[u];
     bool ok = x >= 0 && x < (r.own >= 0 ? r.own : r.whole);
-    for (int s = 0; s < u; s++) ok &= row[s] != x;
+    if (ok && first) ok = !(seen[x >> 5] >> (x & 31) & 1);
+    for (int s = first; s < u; s++) ok &= row[s] != x;
     return ok ? x : -1;
 }
 
@@ -450,11 +453,35 @@ __device__ __forceinline__ float soft_unit(const f32x4m (&s)[4], SoftRow& row, f
     return ref + log2f(sum * 0x1p-15f);   // log2 of the unit's share
 }
 
+// A wave's block in LDS: 64 rows of D bytes of keys, D rows of 64 bytes of values.  The pieces (16 bytes) of a row change places so that the
+// 8 lanes that read at a time find them in different banks; a row's stay among each other, so the loads see whole lines.
+template <int D>
+struct CacheTile {
+    static constexpr int BYTES = BT * D, LOADS = BYTES / 1024;   // of the keys, and of the values; wave-loads of each
+    __device__ static int key_swap(int row) { return D == 128 ? (row & 3) | (row >> 4 & 1) << 2 : row >> 4 & 3; }
+    __device__ static int value_swap(int row) { return row >> 2 & 3; }
+    // where in the page the piece lies that wave-load x brings to the lane's place
+    __device__ static uint32_t key_at(int x, int lane)
+    {
+        const int row = x * (1024 / D) + lane / (D / 16);
+        return (uint32_t)(row * D + 16 * ((lane % (D / 16)) ^ key_swap(row)));
+    }
+    __device__ static uint32_t value_at(int x, int lane)
+    {
+        const int row = 16 * x + lane / 4;
+        return (uint32_t)(row * BT + 16 * ((lane & 3) ^ value_swap(row)));
+    }
+};
+
 template <int D, int FORMAT>
-__global__ __launch_bounds__(256, 3) void cache8_attn_kernel(AttnArgs a)
+__global__ __launch_bounds__(256, D == 128 ? 2 : 4) void cache8_attn_kernel(AttnArgs a)
 {
-    constexpr int KH = D / 64, NX = D / 16;
-    __shared__ float so[4][16][D + 4], sm_[4][16], sl[4][16], shares[4 * MAX_UPW + 1][16];
+    using T = CacheTile<D>;
+    constexpr int KH = D / 64, NX = D / 16, RO = D + 4;
+    __shared__ __attribute__((aligned(16))) unsigned char tiles[4][2 * T::BYTES];   // a wave's keys and values; its result at the end
+    __shared__ float sm_[4][16], sl[4][16], shares[4 * MAX_UPW + 1][16];
+    __shared__ unsigned seen[MAX_CAP / 32];
+    static_assert(16 * RO * 4 <= 2 * T::BYTES, "room for a wave's result");
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, grp = lane >> 4;
     const int groups = (a.c.G + 15) / 16;
     const int split = blockIdx.x, g = blockIdx.y / groups, rg = blockIdx.y % groups, b = blockIdx.z;
@@ -469,11 +496,20 @@ __global__ __launch_bounds__(256, 3) void cache8_attn_kernel(AttnArgs a)
     const int live = min(16, a.c.G - rg * 16);
     const size_t head0 = (size_t)b * a.c.H + g * a.c.G + rg * 16;
     // the wave's units, one to a lane: page (of any unit that has one where there is none), scales
-    const int count = max(0, min(a.upw, ru.nsel - u0));
+    const int count = max(0, min(a.upw, ru.nsel - u0)), first = split * 4 * a.upw;
     int page = -1;
+    if (a.idx && first) {   // (a selection longer than a workgroup's share: what the others name, for repeated blocks)
+        for (int x = tid; x < MAX_CAP / 32; x += 256) seen[x] = 0;
+        __syncthreads();
+        for (int x = tid; x < min(first, a.top); x += 256) {
+            const int j = a.idx[bg * a.top + x];
+            if (j >= 0 && j < MAX_CAP) atomicOr(&seen[j >> 5], 1u << (j & 31));
+        }
+        __syncthreads();
+    }
     if (lane < count) {
         if (a.idx) {
-            const int j = unit_block(a, ru, bg, u0 + lane);
+            const int j = unit_block(a, ru, bg, u0 + lane, first, seen);
             if (j >= 0) page = a.c.t.table[bg * a.c.cap + j];
         } else {
             page = early;
@@ -520,54 +556,65 @@ __global__ __launch_bounds__(256, 3) void cache8_attn_kernel(AttnArgs a)
     const buffer_t wbuf = buffer_of(weighs ? a.weight + head0 * a.units : nullptr, weighs ? live * a.units * 4 : 0);
     const int wat = grp == 0 && col < live ? col * a.units * 4 : 0x7FFFFF00;
     if (have) {
-        const int kat = (16 * (col >> 2) + (col & 3)) * D + 16 * grp, vat = col * BT + 16 * grp;
-        u32x4 kw[4][KH], vw[NX];
+        unsigned char *kt = tiles[wv], *vt = kt + T::BYTES;
         auto load_k = [&](int i) {
-            const unsigned char* kp = (const unsigned char*)a.c.t.k8 + (size_t)__builtin_amdgcn_readlane(page, i) * (BT * D) + kat;
+            const unsigned char* kp = (const unsigned char*)a.c.t.k8 + (size_t)__builtin_amdgcn_readlane(page, i) * T::BYTES;
 #pragma unroll
-            for (int t = 0; t < 4; t++)
-#pragma unroll
-                for (int h = 0; h < KH; h++) kw[t][h] = *(const u32x4*)(kp + 4 * t * D + 64 * h);
+            for (int x = 0; x < T::LOADS; x++) async_load_lds16(kp, T::key_at(x, lane), kt + 1024 * x);
         };
         auto load_v = [&](int i) {
-            const unsigned char* vp = (const unsigned char*)a.c.t.v8 + (size_t)__builtin_amdgcn_readlane(page, i) * (BT * D) + vat;
+            const unsigned char* vp = (const unsigned char*)a.c.t.v8 + (size_t)__builtin_amdgcn_readlane(page, i) * T::BYTES;
 #pragma unroll
-            for (int x = 0; x < NX; x++) vw[x] = *(const u32x4*)(vp + 16 * x * BT);
+            for (int x = 0; x < T::LOADS; x++) async_load_lds16(vp, T::value_at(x, lane), vt + 1024 * x);
         };
         load_k(0);
         load_v(0);
         for (int i = 0; i < count; i++) {
             const float f = readlane_f32(ks, i) * c2q, vscale = readlane_f32(vs, i);
             const bool there = have >> i & 1;
+            // the keys are there when no more than the values' loads are under way (memory operations end in order)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(T::LOADS) : "memory");
             f32x4m s[4];
 #pragma unroll
             for (int t = 0; t < 4; t++) {
                 s[t] = f32x4m{0, 0, 0, 0};
+                const int row = 16 * (col >> 2) + 4 * t + (col & 3);
 #pragma unroll
                 for (int h = 0; h < KH; h++) {
-                    s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen<FORMAT>(kw[t][h][0], kw[t][h][1]), qf[h][0], s[t], 0, 0, 0);
-                    s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen<FORMAT>(kw[t][h][2], kw[t][h][3]), qf[h][1], s[t], 0, 0, 0);
+                    const u32x4 w = *(const u32x4*)(kt + row * D + 16 * ((4 * h + grp) ^ T::key_swap(row)));
+                    s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen<FORMAT>(w[0], w[1]), qf[h][0], s[t], 0, 0, 0);
+                    s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen<FORMAT>(w[2], w[3]), qf[h][1], s[t], 0, 0, 0);
                 }
             }
-            load_k(min(i + 1, count - 1));
 #pragma unroll
             for (int t = 0; t < 4; t++)
 #pragma unroll
                 for (int r = 0; r < 4; r++) s[t][r] = there ? s[t][r] * f : -INFINITY;
+            // the next keys; the values are there when no more than those are under way
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (i + 1 < count) {
+                load_k(i + 1);
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(T::LOADS) : "memory");
+            } else {
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            }
             f16x8 pb[2];
             float corr;
             const float share = soft_unit(s, row, pb, corr);
-            if (alone) shares[u0 + i][col] = share;
-            else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(share), wbuf, wat + 4 * (u0 + i), 0, 0);
 #pragma unroll
             for (int x = 0; x < NX; x++) {
+                const int vr = 16 * x + col;
+                const u32x4 w = *(const u32x4*)(vt + vr * BT + 16 * (grp ^ T::value_swap(vr)));
                 f32x4m y = {0, 0, 0, 0};
-                y = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen<FORMAT>(vw[x][0], vw[x][1]), pb[0], y, 0, 0, 0);
-                y = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen<FORMAT>(vw[x][2], vw[x][3]), pb[1], y, 0, 0, 0);
+                y = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen<FORMAT>(w[0], w[1]), pb[0], y, 0, 0, 0);
+                y = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen<FORMAT>(w[2], w[3]), pb[1], y, 0, 0, 0);
 #pragma unroll
                 for (int r = 0; r < 4; r++) acc[x][r] = fmaf(acc[x][r], corr, vscale * y[r]);
             }
-            load_v(min(i + 1, count - 1));
+            if (alone) shares[u0 + i][col] = share;
+            else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(share), wbuf, wat + 4 * (u0 + i), 0, 0);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (i + 1 < count) load_v(i + 1);
         }
     } else {   // nothing to attend: the units have no share
         for (int i = 0; i < count; i++) {
@@ -636,7 +683,7 @@ __global__ __launch_bounds__(256, 3) void cache8_attn_kernel(AttnArgs a)
     // the four waves' results are joined; rows 4 grp + r of tile x are columns of the head
     if (grp == 0) { sm_[wv][col] = row.m; sl[wv][col] = row.l; }
 #pragma unroll
-    for (int x = 0; x < NX; x++) *(f32x4m*)&so[wv][col][16 * x + 4 * grp] = acc[x];
+    for (int x = 0; x < NX; x++) *(f32x4m*)((float*)tiles[wv] + col * RO + 16 * x + 4 * grp) = acc[x];   // (the wave's own blocks are read)
     __syncthreads();
     for (int x = tid; x < live * D; x += 256) {
         const int h = x / D, d = x % D;
@@ -645,7 +692,7 @@ __global__ __launch_bounds__(256, 3) void cache8_attn_kernel(AttnArgs a)
 #pragma unroll
         for (int w = 0; w < 4; w++) {
             const float f = sm_[w][h] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm_[w][h] - M);
-            sum += f * so[w][h][d];
+            sum += f * ((const float*)tiles[w])[h * RO + d];
             den += f * sl[w][h];
         }
         if (alone) {

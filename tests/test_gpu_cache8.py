@@ -226,6 +226,78 @@ def test_eviction(cap, lens, budget, sink, recent):
         assert torch.equal(got.cpu(), want)
 
 
+def test_the_longest_table():
+    """8192 blocks of a row that share 96 pages: selection, attention over all and over a selection longer than a workgroup's share
+    with repeated places, eviction."""
+    require_gpu()
+    say("cache of 8192 blocks")
+    B, H, d, cap = 2, 2, 64, 8192
+    cache = spk.Cache8.empty(B, H, 1, d, cap, torch.float8_e4m3fn, pages=96)
+    g = gen(81)
+    lens = torch.full((B,), 0, dtype=torch.int32).cuda()
+    spk.sparsek_cache8_append(cache, lens, rand(g, B, 1, 96 * 64, d), rand(g, B, 1, 96 * 64, d))
+    cache.table.copy_(torch.randint(0, 96, cache.table.shape, generator=g, dtype=torch.int32))
+    cache.kt.copy_(rand(g, *cache.kt.shape))
+    cache.vt.copy_(rand(g, *cache.vt.shape))
+    L = [cap * 64 + 63, 5000 * 64]
+    lens = torch.tensor(L, dtype=torch.int32).cuda()
+    q = rand(g, B, H, d)
+    idx = spk.sparsek_cache8_select(cache, lens, q, 100)
+    torch.cuda.synchronize()
+    p8, _ = ref.codes_i8(ref.f64(q).sum(1).float())
+    for b in range(B):
+        nb = (L[b] - 1) // 64
+        pages = cache.table[b, 0, :nb].cpu().long()
+        score = (cache.km.cpu()[pages].double() @ p8[b].double()).float() * cache.kms.cpu()[pages]
+        assert idx[b, 0].tolist() == ref.top_of(score, [True] * nb, 100)
+    many = torch.randint(-5, 5200, (B, 1, 300), generator=g, dtype=torch.int32)
+    many[:, :, 200:] = many[:, :, :100]
+    for x in (None, idx, many.cuda()):
+        cache.mass.zero_()
+        o, lse = spk.sparsek_cache8_attn(cache, lens, q, x, accumulate=True)
+        torch.cuda.synchronize()
+        ro, rl, rm, ob = ref.cache_attn(cache, L, q, None if x is None else x.cpu())
+        assert ((ref.f64(o) - ro).abs() <= ob).all()
+        assert ((lse.cpu().double() - rl).abs() <= 2e-4).all()
+        assert ((ref.f64(cache.mass) - rm).abs() <= 2 ** -12 * rm).all()
+    cache.mass.copy_(torch.randint(0, 50, cache.mass.shape, generator=g).float())     # many of one size
+    out = spk.sparsek_cache8_evict(cache, lens, 4000, 4, 100)
+    torch.cuda.synchronize()
+    for got, want in zip((out["table"], out["mass"], out["lens"]), ref.evict(cache.table, cache.mass, lens, 4000, 4, 100)):
+        assert torch.equal(got.cpu(), want)
+
+
+def test_the_handle_keeps_its_tensors():
+    require_gpu()
+    cache = spk.Cache8.empty(1, 2, 1, 64, 4)
+    with pytest.raises(AttributeError):
+        cache.mass = torch.zeros_like(cache.mass)
+    table, mass = cache.table.clone(), torch.ones_like(cache.mass)
+    cache.adopt(table, mass)
+    assert cache.mass is mass and cache.table is table
+
+
+def test_calls_on_streams_of_their_own():
+    """Two caches stepped on two streams at once give what they give one after the other."""
+    require_gpu()
+    say("cache steps on two streams")
+    made = [filled(90 + x, [700 + 60 * x, 90], 8, 2, 128, FORMATS[x], cap=14) for x in range(2)]
+    q = [rand(gen(95 + x), 2, 8, 128) for x in range(2)]
+    torch.cuda.synchronize()
+    want = [spk.sparsek_cache8_attn(c, L, y) for (c, L, _, _), y in zip(made, q)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(20):
+        for x in range(2):
+            with torch.cuda.stream(streams[x]):
+                got[x].append(spk.sparsek_cache8_attn(made[x][0], made[x][1], q[x]))
+    torch.cuda.synchronize()
+    for x in range(2):
+        for o, lse in got[x]:
+            assert torch.equal(o, want[x][0]) and torch.equal(lse, want[x][1])
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 def test_a_conversation(fmt):
     """Prefill over selected blocks, its keys, values and masses into the cache, then tokens one by one with eviction: every step
