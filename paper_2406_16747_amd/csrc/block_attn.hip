@@ -166,23 +166,37 @@ __global__ __launch_bounds__(1024) void block_short_lists_kernel(BlockLists l, c
 {
     __shared__ unsigned long long masks[FEW_BLOCKS][FEW_BLOCKS];   // [chunk][block]
     __shared__ uint16_t off[FEW_BLOCKS][FEW_BLOCKS];
-    __shared__ int base[FEW_BLOCKS];
+    __shared__ int base[FEW_BLOCKS], repeated;
+    __shared__ uint8_t sel[FEW_PAIRS];   // the pairs' blocks; 255: not one of them
     const int bg = blockIdx.x, tid = threadIdx.x, nb = l.nb, pairs = l.n * l.top;
     const int32_t* row = idx + (size_t)bg * pairs;
+    int first[4];   // (on their way while the masks are cleared)
+#pragma unroll
+    for (int y = 0; y < 4; y++) first[y] = tid + 1024 * y < pairs ? row[tid + 1024 * y] : -1;
+    if (tid == 0) repeated = 0;
     for (int x = tid; x < nb * FEW_BLOCKS; x += 1024) masks[x / FEW_BLOCKS][x % FEW_BLOCKS] = 0;
     __syncthreads();
+    auto take = [&](int x, int j) {
+        const int i = x / l.top, c = i / BT;
+        const bool ok = j >= 0 && j < c;
+        const unsigned long long bit = 1ull << (i % BT);
+        sel[x] = ok ? (uint8_t)j : 255;
+        if (ok && (atomicOr(&masks[c][j], bit) & bit)) repeated = 1;
+    };
+#pragma unroll
+    for (int y = 0; y < 4; y++)
+        if (tid + 1024 * y < pairs) take(tid + 1024 * y, first[y]);
 #pragma unroll 4
-    for (int x = tid; x < pairs; x += 1024) {
-        const int j = row[x], i = x / l.top, c = i / BT;
-        if (j >= 0 && j < c) atomicOr(&masks[c][j], 1ull << (i % BT));
-    }
+    for (int x = tid + 4096; x < pairs; x += 1024) take(x, row[x]);
     __syncthreads();
     if (tid < 64) {   // a lane per block
         const int j = tid, own = j < nb ? min(BT, l.n - j * BT) : 0;
         int run = own;
-        for (int c = j + 1; c < nb; c++) {
+#pragma unroll 8
+        for (int c = 0; c < nb; c++) {
+            const int count = __popcll(masks[c][j]);   // (0 where c <= j)
             off[c][j] = (uint16_t)run;
-            run += __popcll(masks[c][j]);
+            run += count;
         }
         const int units = (int)(((long long)run * l.G + l.unit - 1) / l.unit);
         int2 s = make_int2(run, units);
@@ -211,11 +225,12 @@ __global__ __launch_bounds__(1024) void block_short_lists_kernel(BlockLists l, c
     }
 #pragma unroll 4
     for (int x = tid; x < pairs; x += 1024) {
-        const int j = row[x], i = x / l.top, s = x - i * l.top, c = i / BT;
+        const int j = sel[x], i = x / l.top, s = x - i * l.top, c = i / BT;
         int p = -1;
-        if (j >= 0 && j < c) {
+        if (j < 255) {
             p = base[j] + off[c][j] + __popcll(masks[c][j] & ((1ull << (i % BT)) - 1));
-            for (int y = 0; y < s; y++) p = row[x - s + y] == j ? -1 : p;   // (a repeated block counts once)
+            if (repeated)
+                for (int y = 0; y < s; y++) p = sel[x - s + y] == j ? -1 : p;   // (a repeated block counts once)
             if (p >= 0) list[p] = i;
         }
         pos[(size_t)i * l.slots + 1 + s] = p;

@@ -46,7 +46,7 @@ struct AppendSmem {
     static constexpr int VS = BT + 8;                                       // bf16 values between the columns of vt
     double sums[256 / (D / 8)][D];
     __attribute__((aligned(16))) uint16_t vt[D * VS];                       // the block's values, transposed
-    unsigned red[8];
+    unsigned red[12];
 };
 
 // A whole block goes to its page: codes, scales and the mean key.  The keys are in registers, the values (transposed) in sm.vt; every
@@ -69,8 +69,25 @@ __device__ __forceinline__ void store_block(AppendSmem<D>& sm, const CacheArgs& 
         }
 #pragma unroll
     for (int e = 0; e < 8; e++) sm.sums[tok][8 * c + e] = s[e];
-    block_max_bits2(tk, tv, sm.red, tid);   // (and the sums and values are there)
-    const float topk = __uint_as_float(tk), topv = __uint_as_float(tv);
+    tk = wave_max_bits(tk);
+    tv = wave_max_bits(tv);
+    __syncthreads();   // the sums and values are there
+    float mean = 0.0f;
+    if (tid < D) {
+        double y = 0;
+#pragma unroll
+        for (int g = 0; g < R::RG; g++) y += sm.sums[g][tid];
+        mean = (float)(y / BT);
+    }
+    const unsigned tm = wave_max_bits(__float_as_uint(fabsf(mean)));
+    if ((tid & 63) == 0) {
+        sm.red[tid >> 6] = tk;
+        sm.red[4 + (tid >> 6)] = tv;
+        sm.red[8 + (tid >> 6)] = tm;
+    }
+    __syncthreads();
+    auto top_of = [&](int x) { return __uint_as_float(max(max(sm.red[x], sm.red[x + 1]), max(sm.red[x + 2], sm.red[x + 3]))); };
+    const float topk = top_of(0), topv = top_of(4), topm = top_of(8);
     const float fk = code_factor(topk, most), fv = code_factor(topv, most);
     unsigned char* kp = (unsigned char*)a.t.k8 + (size_t)page * BT * D;
 #pragma unroll
@@ -92,14 +109,6 @@ __device__ __forceinline__ void store_block(AppendSmem<D>& sm, const CacheArgs& 
         w[3] = codes4<FORMAT>(half_of(hi, 4), half_of(hi, 5), half_of(hi, 6), half_of(hi, 7), fv);
         *(u32x4*)(vp + 16 * x) = w;
     }
-    float mean = 0.0f;
-    if (tid < D) {
-        double y = 0;
-#pragma unroll
-        for (int g = 0; g < R::RG; g++) y += sm.sums[g][tid];
-        mean = (float)(y / BT);
-    }
-    const float topm = __uint_as_float(block_max_bits(__float_as_uint(fabsf(mean)), sm.red, tid));
     if (tid < D) a.t.km[(size_t)page * D + tid] = (int8_t)code_i8(mean, code_factor(topm, 127.0f));
     if (tid == 0) {
         a.t.ks[page] = code_scale(topk, most);
@@ -129,35 +138,40 @@ __global__ __launch_bounds__(256) void cache8_append_kernel(CacheArgs a, const i
         u32x4 kr[R::NT];
         unsigned tv = 0;
         const int old = max(0, len - j * BT);   // tokens of the block that are there already (in the first one only)
+        const int tok0 = tid / R::CPR, col = 8 * (tid % R::CPR);
 #pragma unroll
         for (int t = 0; t < R::NT; t++) {
-            const int x = tid / R::CPR + R::RG * t, col = 8 * (tid % R::CPR), tok = j * BT + x;
-            if (x >= old) {
-                kr[t] = *(const u32x4*)(kn + (size_t)(tok - len) * D + col);
-                const u32x4 vr = *(const u32x4*)(vn + (size_t)(tok - len) * D + col);
+            const int x = tok0 + R::RG * t;
+            const size_t at = (size_t)max(j * BT + x - len, 0) * D + col;
+            kr[t] = *(const u32x4*)(x >= old ? kn + at : kt + x * D + col);
+            if (x < old) continue;
+            const u32x4 vr = *(const u32x4*)(vn + at);
+            tv = max(tv, top_of_8(vr));
 #pragma unroll
-                for (int e = 0; e < 8; e++) {
-                    const unsigned y = e & 1 ? vr[e / 2] >> 16 : vr[e / 2] & 0xFFFFu;
-                    tv = max(tv, (y & 0x7FFFu) << 16);
-                    sm.vt[(col + e) * AppendSmem<D>::VS + x] = (uint16_t)y;
+            for (int e = 0; e < 8; e++) sm.vt[(col + e) * AppendSmem<D>::VS + x] = (uint16_t)(e & 1 ? vr[e / 2] >> 16 : vr[e / 2] & 0xFFFFu);
+        }
+        if (old) {   // (8 tokens of a column at a time, the last of them perhaps in part)
+            u32x4 vo[D * 8 / 256];
+#pragma unroll
+            for (int y = 0; y < D * 8 / 256; y++) vo[y] = *(const u32x4*)(vt + 8 * (tid + 256 * y));
+            const int t0 = 8 * (tid & 7);
+#pragma unroll
+            for (int y = 0; y < D * 8 / 256; y++) {
+                uint16_t* to = &sm.vt[(tid / 8 + 32 * y) * AppendSmem<D>::VS + t0];
+                if (t0 + 8 <= old) {
+                    *(u32x4*)to = vo[y];
+                    tv = max(tv, top_of_8(vo[y]));
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 7; e++)
+                        if (t0 + e < old) {
+                            const unsigned w = e & 1 ? vo[y][e / 2] >> 16 : vo[y][e / 2] & 0xFFFFu;
+                            tv = max(tv, (w & 0x7FFFu) << 16);
+                            to[e] = (uint16_t)w;
+                        }
                 }
-            } else {
-                kr[t] = *(const u32x4*)(kt + x * D + col);
             }
         }
-        if (old)   // (8 tokens of a column at a time, the last of them perhaps in part)
-            for (int x = tid; x < D * 8; x += 256) {
-                const int col = x >> 3, t0 = 8 * (x & 7);
-                if (t0 >= old) continue;
-                const u32x4 vr = *(const u32x4*)(vt + col * BT + t0);
-#pragma unroll
-                for (int e = 0; e < 8; e++)
-                    if (t0 + e < old) {
-                        const unsigned y = e & 1 ? vr[e / 2] >> 16 : vr[e / 2] & 0xFFFFu;
-                        tv = max(tv, (y & 0x7FFFu) << 16);
-                        sm.vt[col * AppendSmem<D>::VS + t0 + e] = (uint16_t)y;
-                    }
-            }
         store_block<D, FORMAT>(sm, a, page, kr, tv, tid);
     }
     if (blockIdx.x != 0) return;
