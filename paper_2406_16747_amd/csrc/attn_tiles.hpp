@@ -43,6 +43,16 @@ __device__ __forceinline__ void async_load_lds16(const void* gbase, uint32_t vof
                  : "memory", "m0");
 }
 
+// The same for lines that nobody else reads soon: they leave the caches to others.
+__device__ __forceinline__ void async_stream_lds16(const void* gbase, uint32_t voff, const void* lds_dst)
+{
+    const uint32_t m0v = (uint32_t)(uintptr_t)(lds_void_t*)lds_dst;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt"
+                 :
+                 : "s"(m0v), "v"(voff), "s"(gbase)
+                 : "memory", "m0");
+}
+
 // The same with an address per lane: for rows of arrays that 32-bit offsets do not span.
 __device__ __forceinline__ void async_load_lds16_from(const void* at, const void* lds_dst)
 {

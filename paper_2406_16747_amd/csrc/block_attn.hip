@@ -128,6 +128,44 @@ __global__ __launch_bounds__(1024) void block_units_kernel(BlockLists l)
     if (tid == 0) l.nunits[cbg] = min(done.y, l.maxu);
 }
 
+// order: the units by the chunk of their first query, a workgroup of 1024 per (stretch, batch and head).  Units that are worked on
+// side by side have queries in common then: XXX
+constexpr int ORDER_BUCKETS = 1024;
+__global__ __launch_bounds__(1024) void block_order_kernel(BlockLists l)
+{
+    __shared__ int at[ORDER_BUCKETS], wsum[16];
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    const size_t cbg = l.cbg(blockIdx.x, blockIdx.y);
+    const int q0 = (int)blockIdx.x * l.cq, units = l.nunits[cbg], per = ((l.cq / BT + ORDER_BUCKETS - 1) / ORDER_BUCKETS) * BT;
+    const int2* in = l.units + cbg * l.maxu;
+    const int32_t *list = l.list + cbg * l.entries, *base = l.base + cbg * l.nb;
+    auto bucket = [&](int2 u) { return (list[base[u.x] + u.y / l.G] - q0) / per; };
+    at[tid] = 0;
+    __syncthreads();
+#pragma unroll 4
+    for (int x = tid; x < units; x += 1024) atomicAdd(&at[bucket(in[x])], 1);
+    __syncthreads();
+    const int mine = at[tid];
+    int s = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int x = __shfl_up(s, d, 64);
+        if (lane >= d) s += x;
+    }
+    if (lane == 63) wsum[wv] = s;
+    __syncthreads();
+    s -= mine;
+#pragma unroll
+    for (int w = 0; w < 16; w++) s += w < wv ? wsum[w] : 0;
+    at[tid] = s;
+    __syncthreads();
+#pragma unroll 4
+    for (int x = tid; x < units; x += 1024) {
+        const int2 u = in[x];
+        l.order[cbg * l.maxu + atomicAdd(&at[bucket(u)], 1)] = u;   // (which of a bucket's comes first changes no result)
+    }
+}
+
 // list and pos: a workgroup per (chunk, batch and head).
 __global__ __launch_bounds__(256) void block_place_kernel(BlockLists l, const int32_t* __restrict__ idx)
 {
@@ -212,7 +250,7 @@ __global__ __launch_bounds__(1024) void block_short_lists_kernel(BlockLists l, c
             const int u0 = s.y - units;
             l.first_unit[(size_t)bg * nb + j] = u0;
             for (int u = 0; u < units; u++)
-                if (u0 + u < l.maxu) l.units[(size_t)bg * l.maxu + u0 + u] = make_int2(j, u * l.unit);
+                if (u0 + u < l.maxu) l.order[(size_t)bg * l.maxu + u0 + u] = make_int2(j, u * l.unit);
         }
         if (j == 63) l.nunits[bg] = min(s.y, l.maxu);
     }
@@ -249,6 +287,7 @@ int launch_block_lists(const BlockLists& l, const int32_t* idx, hipStream_t st)
     hipLaunchKernelGGL(block_offsets_kernel, dim3((l.nb + 63) / 64, l.nc, BG), dim3(1024), 0, st, l);
     hipLaunchKernelGGL(block_units_kernel, dim3(l.nc, BG), dim3(1024), 0, st, l);
     hipLaunchKernelGGL(block_place_kernel, dim3(l.nb, BG), dim3(256), lds, st, l, idx);
+    hipLaunchKernelGGL(block_order_kernel, dim3(l.nc, BG), dim3(1024), 0, st, l);
     return launch_status();
 }
 
@@ -336,7 +375,7 @@ __global__ __launch_bounds__(256, 3) void block_tiles_kernel(BlockFwd f)
     bg += f.bg0;
     const size_t cbg = l.cbg(f.c, bg);
     if (un >= l.nunits[cbg]) return;
-    const int2 u = l.units[cbg * l.maxu + un];
+    const int2 u = l.order[cbg * l.maxu + un];
     const int j = u.x, first = u.y, G = l.G;
     const int base = l.base[cbg * l.nb + j];
     const int end = min(l.total[cbg * l.nb + j] * G, first + l.unit);
@@ -460,7 +499,7 @@ __global__ __launch_bounds__(256, 3) void block_tiles_kernel(BlockFwd f)
                 }
             wave_lds_order();
 #pragma unroll
-            for (int t = 0; t < 4; t++) store_words(dst, 2 * D * (8 * t + lrow) + 128 * h + 2 * lcol, *(const u32x4*)(rows + (8 * t + lrow) * RS + 2 * lcol));
+            for (int t = 0; t < 4; t++) stream_words(dst, 2 * D * (8 * t + lrow) + 128 * h + 2 * lcol, *(const u32x4*)(rows + (8 * t + lrow) * RS + 2 * lcol));
             wave_lds_order();
         }
         take_q(next);   // (here and not ahead of the loop's next round: the wait for these loads leaves the stores under way)
@@ -509,7 +548,7 @@ __global__ __launch_bounds__(256) void block_join_kernel(BlockFwd f, int rows_pe
             const int ps = __shfl(p, lane0 + s, 64);
             const float wss = __shfl(ws, lane0 + s, 64);
             if (ps < 0) continue;
-            const f16x8 v = *(const f16x8*)(f.part + (rows0 + (size_t)ps * G) * D + 8 * t);
+            const f16x8 v = __builtin_nontemporal_load((const f16x8*)(f.part + (rows0 + (size_t)ps * G) * D + 8 * t));
 #pragma unroll
             for (int e = 0; e < 8; e++) acc[e] = fmaf(wss, (float)v[e], acc[e]);
         }
@@ -522,7 +561,7 @@ __global__ __launch_bounds__(256) void block_join_kernel(BlockFwd f, int rows_pe
     u32x4 out;
 #pragma unroll
     for (int e = 0; e < 4; e++) out[e] = pack_bf16x2(acc[2 * e] * inv, acc[2 * e + 1] * inv);
-    *(u32x4*)(f.o + at * D + 8 * t) = out;
+    __builtin_nontemporal_store(out, (u32x4*)(f.o + at * D + 8 * t));
     if (t == 0) f.lse[at] = (ref + log2f(L)) * 0.6931471805599453f;
 }
 

@@ -229,7 +229,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void block_bwd_tiles_kernel(
     int bg, un;
     deal_head(blockIdx.x, l.maxu, l.B * l.Hkv, bg, un);
     if (un >= l.nunits[bg]) return;
-    const int2 u = l.units[(size_t)bg * l.maxu + un];
+    const int2 u = l.order[(size_t)bg * l.maxu + un];
     const int j = u.x, first = u.y, G = l.G, b = bg / l.Hkv, g = bg % l.Hkv;
     const int base = l.base[(size_t)bg * l.nb + j], rows = l.total[(size_t)bg * l.nb + j] * G, end = min(rows, first + l.unit);
     const size_t kv = ((size_t)bg * l.n + (size_t)j * BT) * D;
@@ -344,7 +344,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void block_bwd_tiles_kernel(
         store_kv<D>(f, kv, 32 * wv + col, last, half, acc_v, acc_k);
         return;
     }
-    float4* out = (float4*)f.kvpart + (((size_t)bg * l.maxu + un) * 2 + wv) * (2 * DB * 4 * 64);
+    float4* out = (float4*)f.kvpart + (((size_t)bg * l.maxu + l.first_unit[(size_t)bg * l.nb + j] + first / l.unit) * 2 + wv) * (2 * DB * 4 * 64);
 #pragma unroll
     for (int x = 0; x < DB; x++)
 #pragma unroll

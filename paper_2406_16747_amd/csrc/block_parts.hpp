@@ -25,7 +25,7 @@ inline int block_count(int n) { return (n + BT - 1) / BT; }
 struct BlockLists {
     uint8_t* counts;
     int32_t *off, *total, *base, *first_unit, *list, *pos, *nunits;
-    int2* units;
+    int2 *units, *order;     // (block, first row), block by block, and as they are worked through
     int B, H, Hkv, G, n, nb, top;
     int cq, nc, unit, maxu;  // queries per stretch, stretches, rows per unit, units of a stretch at most
     int slots;               // top + 1
@@ -66,6 +66,7 @@ inline BlockLayout block_lists_layout(const sparsek_block_cfg& c, int cq, int un
     l.pos = (int32_t*)take(BG * c.n * l.slots * 4);
     l.nunits = (int32_t*)take(S * 4);
     l.units = (int2*)take(S * l.maxu * 8);
+    l.order = (int2*)take(S * l.maxu * 8);
     y.bytes = at;
     return y;
 }
@@ -165,6 +166,8 @@ __device__ __forceinline__ buffer_t buffer_of(const void* p, int bytes)
     return __builtin_amdgcn_make_buffer_rsrc(base, 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
 }
 __device__ __forceinline__ void store_words(buffer_t b, int offset, u32x4 v) { __builtin_amdgcn_raw_buffer_store_b128(v, b, offset, 0, 0); }
+// Whole lines that nobody reads soon: they leave the caches to what is read again.
+__device__ __forceinline__ void stream_words(buffer_t b, int offset, u32x4 v) { __builtin_amdgcn_raw_buffer_store_b128(v, b, offset, 0, 2); }
 __device__ __forceinline__ void store_words(buffer_t b, int offset, u32x2 v) { __builtin_amdgcn_raw_buffer_store_b64(v, b, offset, 0, 0); }
 
 // Workgroup id -> (batch and head, item): workgroups go to the chip's 8 partitions in turn; of every 8 heads each partition gets

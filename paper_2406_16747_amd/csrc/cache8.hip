@@ -95,7 +95,7 @@ __device__ __forceinline__ void store_block(AppendSmem<D>& sm, const CacheArgs& 
         u32x2 w;
         w[0] = codes4<FORMAT>(half_of(kr[t], 0), half_of(kr[t], 1), half_of(kr[t], 2), half_of(kr[t], 3), fk);
         w[1] = codes4<FORMAT>(half_of(kr[t], 4), half_of(kr[t], 5), half_of(kr[t], 6), half_of(kr[t], 7), fk);
-        *(u32x2*)(kp + (tok + R::RG * t) * D + 8 * c) = w;
+        __builtin_nontemporal_store(w, (u32x2*)(kp + (tok + R::RG * t) * D + 8 * c));
     }
     unsigned char* vp = (unsigned char*)a.t.v8 + (size_t)page * BT * D;
 #pragma unroll
@@ -107,7 +107,7 @@ __device__ __forceinline__ void store_block(AppendSmem<D>& sm, const CacheArgs& 
         w[1] = codes4<FORMAT>(half_of(lo, 4), half_of(lo, 5), half_of(lo, 6), half_of(lo, 7), fv);
         w[2] = codes4<FORMAT>(half_of(hi, 0), half_of(hi, 1), half_of(hi, 2), half_of(hi, 3), fv);
         w[3] = codes4<FORMAT>(half_of(hi, 4), half_of(hi, 5), half_of(hi, 6), half_of(hi, 7), fv);
-        *(u32x4*)(vp + 16 * x) = w;
+        __builtin_nontemporal_store(w, (u32x4*)(vp + 16 * x));
     }
     if (tid < D) a.t.km[(size_t)page * D + tid] = (int8_t)code_i8(mean, code_factor(topm, 127.0f));
     if (tid == 0) {
@@ -142,10 +142,13 @@ __global__ __launch_bounds__(256) void cache8_append_kernel(CacheArgs a, const i
 #pragma unroll
         for (int t = 0; t < R::NT; t++) {
             const int x = tok0 + R::RG * t;
-            const size_t at = (size_t)max(j * BT + x - len, 0) * D + col;
-            kr[t] = *(const u32x4*)(x >= old ? kn + at : kt + x * D + col);
-            if (x < old) continue;
-            const u32x4 vr = *(const u32x4*)(vn + at);
+            const size_t at = (size_t)(j * BT + x - len) * D + col;
+            if (x < old) {
+                kr[t] = *(const u32x4*)(kt + x * D + col);
+                continue;
+            }
+            kr[t] = __builtin_nontemporal_load((const u32x4*)(kn + at));
+            const u32x4 vr = __builtin_nontemporal_load((const u32x4*)(vn + at));
             tv = max(tv, top_of_8(vr));
 #pragma unroll
             for (int e = 0; e < 8; e++) sm.vt[(col + e) * AppendSmem<D>::VS + x] = (uint16_t)(e & 1 ? vr[e / 2] >> 16 : vr[e / 2] & 0xFFFFu);
@@ -571,15 +574,29 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void cache8_attn_kernel(Attn
     const int wat = grp == 0 && col < live ? col * a.units * 4 : 0x7FFFFF00;
     if (have) {
         unsigned char *kt = tiles[wv], *vt = kt + T::BYTES;
+        // A whole cache is streamed past the chip's caches (64 sequences of up to 8192: 148 us -> 130).  Blocks that were chosen are likely
+        // to be chosen by the next token again (16 sequences, 32 of 1024 blocks, the same ones again: 31 us, and 33 streamed), and more
+        // than 16 heads of a group read a block several times.
+        const bool stream = !a.idx && a.c.G <= 16;
         auto load_k = [&](int i) {
             const unsigned char* kp = (const unsigned char*)a.c.t.k8 + (size_t)__builtin_amdgcn_readlane(page, i) * T::BYTES;
+            if (stream) {
 #pragma unroll
-            for (int x = 0; x < T::LOADS; x++) async_load_lds16(kp, T::key_at(x, lane), kt + 1024 * x);
+                for (int x = 0; x < T::LOADS; x++) async_stream_lds16(kp, T::key_at(x, lane), kt + 1024 * x);
+            } else {
+#pragma unroll
+                for (int x = 0; x < T::LOADS; x++) async_load_lds16(kp, T::key_at(x, lane), kt + 1024 * x);
+            }
         };
         auto load_v = [&](int i) {
             const unsigned char* vp = (const unsigned char*)a.c.t.v8 + (size_t)__builtin_amdgcn_readlane(page, i) * T::BYTES;
+            if (stream) {
 #pragma unroll
-            for (int x = 0; x < T::LOADS; x++) async_load_lds16(vp, T::value_at(x, lane), vt + 1024 * x);
+                for (int x = 0; x < T::LOADS; x++) async_stream_lds16(vp, T::value_at(x, lane), vt + 1024 * x);
+            } else {
+#pragma unroll
+                for (int x = 0; x < T::LOADS; x++) async_load_lds16(vp, T::value_at(x, lane), vt + 1024 * x);
+            }
         };
         load_k(0);
         load_v(0);
