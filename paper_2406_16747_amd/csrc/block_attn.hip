@@ -129,7 +129,8 @@ __global__ __launch_bounds__(1024) void block_units_kernel(BlockLists l)
 }
 
 // order: the units by the chunk of their first query, a workgroup of 1024 per (stretch, batch and head).  Units that are worked on
-// side by side have queries in common then: XXX
+// side by side find query rows that their neighbours have read in the caches then, which is worth more than a block's own K and V
+// (32 heads of 32768: 2712 us, 2778 block by block; 17 us of it are this kernel's).
 constexpr int ORDER_BUCKETS = 1024;
 __global__ __launch_bounds__(1024) void block_order_kernel(BlockLists l)
 {
@@ -590,8 +591,7 @@ __global__ __launch_bounds__(256) void block_mass_kernel(BlockFwd f)
 
 // Queries per stretch and heads per launch: what they leave behind is at most FWD_STRETCH_BYTES of workspace.  As many queries as fit
 // come first, because all the rows that a stretch has for a block share one load of K and V.  (Stretches whose results would stay in
-// the chip's last cache, of 256 MB, do not pay: 32 heads of 32768, 16 blocks: 3.56 ms with 128 MB and 3.26 with 256 against 3.00 in one.
-// The join reads 4 to 15 % faster then, but the launches' ends cost the tiles more.)
+// the chip's last cache, of 256 MB, do not pay: 32 heads of 32768, 16 blocks: 3.28 ms with 256 MB and 2.94 with 1 GB against 2.70 in one.)
 static int fwd_stretch(const sparsek_block_cfg& c)
 {
     const double per_query = (double)(c.H / c.Hkv) * (c.top + 1) * c.d * 2, blocks = block_count(c.n);
@@ -604,11 +604,13 @@ static int fwd_heads(const sparsek_block_cfg& c, int cq)
     return (int)std::max(1.0, std::min((double)c.B * c.Hkv, std::floor(FWD_STRETCH_BYTES / per_head)));
 }
 
-// Rows that share a block's K and V in LDS: more of them where that leaves three workgroups for every compute unit.
+// Rows that share a block's K and V in LDS: more of them where that leaves three workgroups for every compute unit, and beyond 512 four
+// rounds of those (32 heads of 32768, 16 blocks: 2695 us with 512, 2631 with 1024, 2597 with 2048, 2591 with 4096; two prompts of 16
+// heads of 5003: 299.5 with 512, 301 with 1024).
 static int fwd_unit(const sparsek_block_cfg& c)
 {
     const double rows = (double)c.B * c.H * c.n * (c.top + 1);
-    return rows >= 768 * 512.0 ? 512 : rows >= 768 * 256.0 ? 256 : 128;
+    return rows >= 768 * 8192.0 ? 2048 : rows >= 768 * 4096.0 ? 1024 : rows >= 768 * 512.0 ? 512 : rows >= 768 * 256.0 ? 256 : 128;
 }
 
 struct FwdLayout {

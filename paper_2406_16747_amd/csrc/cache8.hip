@@ -352,9 +352,9 @@ __global__ __launch_bounds__(1024) void cache8_select_kernel(CacheArgs a, const 
 // ---- attention of a single query per sequence ----
 
 // A workgroup has 4 waves, and a wave takes whole blocks: S = K.Q^T (64 tokens by 16 heads), the running softmax, O^T += V^T.P^T.
-// A block goes through LDS, in loads of whole lines: loaded as the operands have it, 16 bytes of a row to a lane, every lane is a line of
-// its own to the cache, which takes four times as many cycles (a sequence of 32768 tokens 29.8 us then, 26.7 now; 64 of up to 8192 155 and 150).  Between S and O nothing is exchanged: row m of S's tile t is
-// token 16 (m / 4) + 4 t + m % 4, so a lane's 16 weights are those of the 16 tokens whose values it reads for every column.  Codes of 8
+// A block goes through LDS, in loads of whole lines: loaded as the operands have it, 16 bytes of a row to a lane, every lane is a line
+// of its own to the cache, which takes four times as many cycles (a sequence of 32768 tokens 29.8 us so, 26.7 through LDS; 64 of up to
+// 8192 155 and 150).  Between S and O nothing is exchanged: row m of S's tile t is token 16 (m / 4) + 4 t + m % 4, so a lane's 16 weights are those of the 16 tokens whose values it reads for every column.  Codes of 8
 // bits are exact in fp16; so is q relative to its largest value (what fp16 drops lies 2^-27 below it), and weights lose 2^-11
 // where bf16 would lose 2^-8.  What bounds it is memory: a wave has the keys of one block or the values of another on
 // their way while it computes.
@@ -929,11 +929,11 @@ static Cache8Layout cache8_layout(const sparsek_cache8_cfg& c, int top)
     y.units = (top ? top : c.cap) + 1;   // and the query's own block
     y.groups = (c.H / c.Hkv + 15) / 16;
     // Units per wave.  Up to 20 units and 16 heads of a group are one workgroup's, which needs no second launch.  Beyond that
-    // as many as leave 8 waves for each of 256 compute units, 4 at most (sequences are shorter than the longest, and the waves that
-    // they leave idle weigh less the fewer units each has: 64 sequences of up to 8192 159 us with 16, 155 with 4).
+    // as many as leave 8 waves for each of 256 compute units, 5 at most (sequences are shorter than the longest, and the waves that
+    // they leave idle weigh less the fewer units each has: 64 sequences of up to 8192 127.5 us with 5, 128.3 with 4, 130 with 3, 136 with 2).
     const long long all = (long long)c.B * c.Hkv * y.groups * y.units;
     if (y.units <= 4 * MAX_UPW && y.groups == 1) y.upw = (y.units + 3) / 4;
-    else y.upw = (int)std::max<long long>(1, std::min<long long>(4, all / 2048));
+    else y.upw = (int)std::max<long long>(1, std::min<long long>(MAX_UPW, all / 2048));
     y.splits = (y.units + 4 * y.upw - 1) / (4 * y.upw);
     const size_t parts = (size_t)c.B * c.H * y.splits;
     y.part_o = 0;
