@@ -9,6 +9,7 @@
 #include "block_parts.hpp"
 
 #include <cmath>
+#include <type_traits>
 
 namespace spk {
 
@@ -304,6 +305,7 @@ struct BlockFwd {
     float2* meta;      // log2 of the row's denominator, and the factor that the halves stand for
     float* mass;       // [B,Hkv,nb] or null
     int c, bg0, nbg;   // the stretch, the first of the heads (of all batches) and their number
+    bool stream;       // the partial results are more than the chip's last cache holds
 };
 
 template <int D>
@@ -500,7 +502,11 @@ __global__ __launch_bounds__(256, 3) void block_tiles_kernel(BlockFwd f)
                 }
             wave_lds_order();
 #pragma unroll
-            for (int t = 0; t < 4; t++) stream_words(dst, 2 * D * (8 * t + lrow) + 128 * h + 2 * lcol, *(const u32x4*)(rows + (8 * t + lrow) * RS + 2 * lcol));
+            for (int t = 0; t < 4; t++) {
+                const u32x4 w = *(const u32x4*)(rows + (8 * t + lrow) * RS + 2 * lcol);
+                if (f.stream) stream_words(dst, 2 * D * (8 * t + lrow) + 128 * h + 2 * lcol, w);
+                else store_words(dst, 2 * D * (8 * t + lrow) + 128 * h + 2 * lcol, w);
+            }
             wave_lds_order();
         }
         take_q(next);   // (here and not ahead of the loop's next round: the wait for these loads leaves the stores under way)
@@ -534,7 +540,7 @@ __global__ __launch_bounds__(256) void block_join_kernel(BlockFwd f, int rows_pe
     for (int d = 1; d < LPR; d <<= 1) M = fmaxf(M, __shfl_xor(M, d, 64));
     const float ref = M == -INFINITY ? 0.0f : M;
     float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0}, L = 0.0f;
-    for (int s0 = 0; s0 < l.slots; s0 += LPR) {
+    auto add = [&](auto stream, int s0) {
         const int p = s0 + t < l.slots ? pos[s0 + t] : -1;
         float w = 0.0f, ws = 0.0f;
         if (p >= 0) {
@@ -549,11 +555,18 @@ __global__ __launch_bounds__(256) void block_join_kernel(BlockFwd f, int rows_pe
             const int ps = __shfl(p, lane0 + s, 64);
             const float wss = __shfl(ws, lane0 + s, 64);
             if (ps < 0) continue;
-            const f16x8 v = __builtin_nontemporal_load((const f16x8*)(f.part + (rows0 + (size_t)ps * G) * D + 8 * t));
+            const f16x8* at = (const f16x8*)(f.part + (rows0 + (size_t)ps * G) * D + 8 * t);
+            f16x8 v;
+            if constexpr (stream) v = __builtin_nontemporal_load(at);
+            else v = *at;
 #pragma unroll
             for (int e = 0; e < 8; e++) acc[e] = fmaf(wss, (float)v[e], acc[e]);
         }
-    }
+    };
+    if (f.stream)
+        for (int s0 = 0; s0 < l.slots; s0 += LPR) add(std::true_type{}, s0);
+    else
+        for (int s0 = 0; s0 < l.slots; s0 += LPR) add(std::false_type{}, s0);
 #pragma unroll
     for (int d = 1; d < LPR; d <<= 1) L += __shfl_xor(L, d, 64);
     if (rr >= nq * G) return;
@@ -650,6 +663,8 @@ int launch_block_fwd(const sparsek_block_cfg& c, const void* q, const void* k, c
     for (f.bg0 = 0; f.bg0 < BG; f.bg0 += y.heads)
         for (f.c = 0; f.c < l.nc; f.c++) {
             f.nbg = std::min(y.heads, BG - f.bg0);
+            // (two prompts of 16 heads of 5003, 533 MB: 370 us as they are, 296 streamed; 48 heads of 2000, 61 MB: the join alone 14.5 and 18.4)
+            f.stream = (double)f.nbg * l.entries * l.G * c.d * 2 > 256e6;
             const int nq = std::min(l.cq, c.n - f.c * l.cq), seen = std::min(l.nb, (f.c + 1) * (l.cq / BT));
             const int items = (int)(((long long)nq * l.G * (c.d / 8) + 255) / 256);
 #define FWD(D)                                                                                                   \

@@ -44,10 +44,30 @@ __device__ __forceinline__ unsigned codes4(float a, float b, float c, float d, f
 template <int D>
 struct AppendSmem {
     static constexpr int VS = BT + 8;                                       // bf16 values between the columns of vt
-    double sums[256 / (D / 8)][D];
+    double sums[4][D];                                                      // of a wave's tokens
     __attribute__((aligned(16))) uint16_t vt[D * VS];                       // the block's values, transposed
     unsigned red[12];
+    // Token x of a column.  Its groups of 8 tokens change places from 16 columns to the next: a token's columns, 8 to a lane, go to banks
+    // of their own (as they lie, to two; four prompts of 8192 into the cache 42 us then).
+    static __device__ __forceinline__ int at(int col, int x) { return col * VS + ((x >> 3 ^ (col >> 4 & 7)) << 3) + (x & 7); }
 };
+
+template <class F>
+__device__ __forceinline__ double both_words(double x, F f)
+{
+    const unsigned long long b = __builtin_bit_cast(unsigned long long, x);
+    const auto lo = f((unsigned)b), hi = f((unsigned)(b >> 32));
+    return __builtin_bit_cast(double, (unsigned long long)hi[0] << 32 | lo[0]) + __builtin_bit_cast(double, (unsigned long long)hi[1] << 32 | lo[1]);
+}
+// The sum over a wave's lanes that have the same place among CPR = 8 or 16 neighbours.
+template <int CPR>
+__device__ __forceinline__ double sum_columns(double x)
+{
+    if constexpr (CPR == 8)
+        x = both_words(x, [](unsigned y) { return u32x2{y, (unsigned)__builtin_amdgcn_mov_dpp((int)y, 0x128, 0xF, 0xF, true)}; });   // (8 lanes on, of 16)
+    x = both_words(x, [](unsigned y) { const auto s = __builtin_amdgcn_permlane16_swap(y, y, false, false); return u32x2{(unsigned)s[0], (unsigned)s[1]}; });
+    return both_words(x, [](unsigned y) { const auto s = __builtin_amdgcn_permlane32_swap(y, y, false, false); return u32x2{(unsigned)s[0], (unsigned)s[1]}; });
+}
 
 // A whole block goes to its page: codes, scales and the mean key.  The keys are in registers, the values (transposed) in sm.vt; every
 // thread has seen the end of what was written there.
@@ -68,7 +88,10 @@ __device__ __forceinline__ void store_block(AppendSmem<D>& sm, const CacheArgs& 
             tk = max(tk, __float_as_uint(fabsf(k)));
         }
 #pragma unroll
-    for (int e = 0; e < 8; e++) sm.sums[tok][8 * c + e] = s[e];
+    for (int e = 0; e < 8; e++) s[e] = sum_columns<R::CPR>(s[e]);
+    if ((tid & 63) < R::CPR)
+#pragma unroll
+        for (int e = 0; e < 8; e++) sm.sums[tid >> 6][8 * c + e] = s[e];
     tk = wave_max_bits(tk);
     tv = wave_max_bits(tv);
     __syncthreads();   // the sums and values are there
@@ -76,7 +99,7 @@ __device__ __forceinline__ void store_block(AppendSmem<D>& sm, const CacheArgs& 
     if (tid < D) {
         double y = 0;
 #pragma unroll
-        for (int g = 0; g < R::RG; g++) y += sm.sums[g][tid];
+        for (int g = 0; g < 4; g++) y += sm.sums[g][tid];
         mean = (float)(y / BT);
     }
     const unsigned tm = wave_max_bits(__float_as_uint(fabsf(mean)));
@@ -101,7 +124,7 @@ __device__ __forceinline__ void store_block(AppendSmem<D>& sm, const CacheArgs& 
 #pragma unroll
     for (int t = 0; t < BT * D / 16 / 256; t++) {
         const int x = tid + 256 * t;
-        const u32x4 lo = *(const u32x4*)&sm.vt[x / 4 * AppendSmem<D>::VS + 16 * (x % 4)], hi = *(const u32x4*)&sm.vt[x / 4 * AppendSmem<D>::VS + 16 * (x % 4) + 8];
+        const u32x4 lo = *(const u32x4*)&sm.vt[AppendSmem<D>::at(x / 4, 16 * (x % 4))], hi = *(const u32x4*)&sm.vt[AppendSmem<D>::at(x / 4, 16 * (x % 4) + 8)];
         u32x4 w;
         w[0] = codes4<FORMAT>(half_of(lo, 0), half_of(lo, 1), half_of(lo, 2), half_of(lo, 3), fv);
         w[1] = codes4<FORMAT>(half_of(lo, 4), half_of(lo, 5), half_of(lo, 6), half_of(lo, 7), fv);
@@ -151,7 +174,7 @@ __global__ __launch_bounds__(256) void cache8_append_kernel(CacheArgs a, const i
             const u32x4 vr = __builtin_nontemporal_load((const u32x4*)(vn + at));
             tv = max(tv, top_of_8(vr));
 #pragma unroll
-            for (int e = 0; e < 8; e++) sm.vt[(col + e) * AppendSmem<D>::VS + x] = (uint16_t)(e & 1 ? vr[e / 2] >> 16 : vr[e / 2] & 0xFFFFu);
+            for (int e = 0; e < 8; e++) sm.vt[AppendSmem<D>::at(col + e, x)] = (uint16_t)(e & 1 ? vr[e / 2] >> 16 : vr[e / 2] & 0xFFFFu);
         }
         if (old) {   // (8 tokens of a column at a time, the last of them perhaps in part)
             u32x4 vo[D * 8 / 256];
@@ -160,7 +183,7 @@ __global__ __launch_bounds__(256) void cache8_append_kernel(CacheArgs a, const i
             const int t0 = 8 * (tid & 7);
 #pragma unroll
             for (int y = 0; y < D * 8 / 256; y++) {
-                uint16_t* to = &sm.vt[(tid / 8 + 32 * y) * AppendSmem<D>::VS + t0];
+                uint16_t* to = &sm.vt[AppendSmem<D>::at(tid / 8 + 32 * y, t0)];
                 if (t0 + 8 <= old) {
                     *(u32x4*)to = vo[y];
                     tv = max(tv, top_of_8(vo[y]));
