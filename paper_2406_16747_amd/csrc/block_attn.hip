@@ -591,6 +591,7 @@ __global__ __launch_bounds__(256) void block_mass_kernel(BlockFwd f)
     const int32_t* list = l.list + cbg * l.entries + base;
     const float2* meta = f.meta + ((size_t)blockIdx.y * l.entries + base) * G;
     float sum = 0.0f;
+#pragma unroll 4
     for (int r = tid; r < rows; r += 256) sum += __builtin_amdgcn_exp2f(meta[r].x - f.lse[(h0 + r % G) * l.n + list[r / G]] * 1.4426950408889634f);
     sum = wave_sum_f32(sum);
     if ((tid & 63) == 0) red[tid >> 6] = sum;
