@@ -308,7 +308,8 @@ int sparsek_block_attn_bwd(const sparsek_block_cfg *cfg, const void *q, const vo
  * sequence and head may name (two may name the same one, as for a common prefix).
  *     k8 [pages,64,d], v8 [pages,d,64] (transposed)   codes: SPARSEK_I8 int8, rint(x * (1 / max * 127)); SPARSEK_E4M3 OCP e4m3, x * (1 / max * 448)
  *     ks, vs [pages] fp32                             what a code of 1 stands for: max * (1/127) or max * (1/448), max = the block's largest |x|;
- *                                                     a block with max < 2^-100 is held as zeros with scale 0
+ *                                                     a block with max < 2^-100 is held as zeros with scale 0; one with a value that
+ *                                                     is not finite gets a scale of NaN, and NaN is what a query gets that attends it
  *     km [pages,d] int8, kms [pages] fp32             the block's mean key, as m8 and ms of sparsek_block_select
  *     kt [B,Hkv,64,d], vt [B,Hkv,d,64] of `dtype`     the tokens of the last, unfinished block
  *     table [B,Hkv,cap] int32                         a head's pages, oldest first; behind its blocks the pages for the next ones

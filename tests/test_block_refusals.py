@@ -1,5 +1,7 @@
 """Arguments that the block attention and the cache in 8 bits refuse, on the CPU: nothing is launched."""
 import ctypes
+import os
+import re
 
 import pytest
 import torch
@@ -144,3 +146,11 @@ def test_reference_gradients_against_differences():
             L.append(float((ref.attn(*args, idx, scale)[0] * dO).sum()))
         want = (L[0] - L[1]) / 2e-5
         assert abs(float((grads[which] * step).sum()) - want) <= 1e-7 * (abs(want) + 1)
+
+
+def test_every_entry_point_of_the_header_is_there():
+    header = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "sparsek.h")).read()
+    names = set(re.findall(r"^(?:int|size_t) (sparsek_(?:block|cache8)_\w+)\(", header, re.M))
+    assert len(names) == 11
+    for name in names:
+        assert getattr(spk.lib(), name), name

@@ -390,3 +390,38 @@ def test_decode_step_replays_as_a_graph():
     for _, cache, lens, _, _ in graphs:
         assert torch.equal(cache.mass, ec.mass) and torch.equal(lens, el)
         assert torch.equal(cache.k8.view(torch.uint8), ec.k8.view(torch.uint8)) and torch.equal(cache.kt, ec.kt)
+
+
+@pytest.mark.parametrize("cap", [4, 40])   # one workgroup has all of it, or several
+@pytest.mark.parametrize("where", ["key", "value", "last token's key", "last token's value"])
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_values_that_are_not_finite_reach_who_attends_them(fmt, bad, where, cap):
+    """One value of a head, in its second block of three and a half, or of its last token (in bf16, where a value of infinity is one of the
+    result's column): nothing finite for that head's queries unless they leave the block out, and the same bits as ever for everybody else."""
+    B, H, Hkv, d, n = 2, 4, 2, 64, 220
+    g = gen(5)
+    k, v, q = rand(g, B, Hkv, n, d), rand(g, B, Hkv, n, d), rand(g, B, H, d)
+    q[1, 2:, 9] = q[1, 2:, 9].abs() + 1   # (a logit of +inf or NaN, or -inf where `bad` is that)
+    zero, L = torch.zeros(B, dtype=torch.int32).cuda(), torch.full((B,), n, dtype=torch.int32).cuda()
+    last = where.startswith("last")
+
+    def run(k, v):
+        cache = shuffled(spk.Cache8.empty(B, H, Hkv, d, cap, fmt), 5)
+        spk.sparsek_cache8_append(cache, zero, k, v)
+        without = torch.tensor([0, 2], dtype=torch.int32).cuda().expand(B, Hkv, 2).contiguous()
+        return spk.sparsek_cache8_attn(cache, L, q, accumulate=True) + spk.sparsek_cache8_attn(cache, L, q, without)
+
+    clean = run(k, v)
+    (k if "key" in where else v)[1, 1, n - 1 if last else 100, 9] = bad
+    for x, (got, want) in enumerate(zip(run(k, v), clean)):
+        mine = got[1, 2:]
+        if where == "last token's key" and bad == float("-inf"):   # (a weight of 0)
+            assert torch.isfinite(mine).all()
+        elif last and "value" in where and x in (0, 2):
+            assert not torch.isfinite(mine[:, 9]).any(), x
+        elif x == 0 or last and x == 2:
+            assert torch.isnan(mine).all(), x
+        elif x == 2:   # (without the second block)
+            assert torch.equal(mine, want[1, 2:])
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1, :2], want[1, :2]), x
