@@ -1,5 +1,6 @@
 """Arguments that the block attention and the cache in 8 bits refuse, on the CPU: nothing is launched."""
 import ctypes
+import json
 import os
 import re
 
@@ -154,3 +155,13 @@ def test_every_entry_point_of_the_header_is_there():
     assert len(names) == 11
     for name in names:
         assert getattr(spk.lib(), name), name
+
+
+def test_hand_written_m0_is_checked():
+    """The kernels whose direct-to-LDS loads set M0 by hand (like those that test_abi.py lists) went through the build's check."""
+    from paper_2406_16747_amd import build
+
+    if not os.path.exists(build.SIDECAR) or os.path.getmtime(build.SIDECAR) < os.path.getmtime(spk.lib_path()) - 60:
+        build.build()
+    rec = json.load(open(build.SIDECAR))
+    assert rec["m0_check"] == "ok" and set(rec["untracked_direct_to_lds_loads_of_blocks"]) == {"block_attn_bwd.hip", "cache8.hip"}
