@@ -6,8 +6,8 @@
 // O^T = V^T.P^T, and leaves the normalised partial result, with the log of its denominator, in list order.  block_join_kernel adds up
 // the partial results of every row with their weights.
 // What bounds it is memory, then the vector ALU: a (row, block) pair moves a row of q in and D halves out and in again, for 4*64*D
-// flops.  32 heads of 128 (8 of keys), 32768 tokens, 16 blocks: 2580 us, of which the tiles take 1320 (4.6 GB written; matrix pipes 22 %,
-// vector ALU 39 %, LDS 33 % of the time; 1160 with the partial results written to one place), the join 920 (4.9 TB/s), the selection 280.
+// flops.  32 heads of 128 (8 of keys), 32768 tokens, 16 blocks: 2580 us, of which the tiles take 1320 to 1350 (4.6 GB written; matrix pipes 22 %,
+// vector ALU 39 %, LDS 33 % of the time; 1150 with the partial results written to one place), the join 920 (4.9 TB/s), the selection 280.
 #include "block_parts.hpp"
 
 #include <cmath>

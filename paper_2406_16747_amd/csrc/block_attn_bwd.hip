@@ -427,7 +427,7 @@ __global__ __launch_bounds__(256) void block_dq_join_kernel(BlockBwd f, int item
 }
 
 // Rows whose dK and dV are summed in registers: most blocks have fewer and are finished by one workgroup (4 x 16 heads of 8192:
-// 2245, 2075, 1968 and 1962 us with 512, 1024, 2048 and 4096); where there are few rows altogether, a popular block's are
+// 2224, 2069, 1992 and 1994 us with 512, 1024, 2048 and 4096); where there are few rows altogether, a popular block's are
 // shared out to more of the chip.
 static int bwd_unit(const sparsek_block_cfg& c)
 {
