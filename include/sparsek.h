@@ -311,7 +311,8 @@ int sparsek_block_attn_bwd(const sparsek_block_cfg *cfg, const void *q, const vo
  *                                                     a block with max < 2^-100 is held as zeros with scale 0; one with a value that
  *                                                     is not finite gets a scale of NaN, and NaN is what a query gets that attends it
  *     km [pages,d] int8, kms [pages] fp32             the block's mean key, as m8 and ms of sparsek_block_select
- *     kt [B,Hkv,64,d], vt [B,Hkv,d,64] of `dtype`     the tokens of the last, unfinished block
+ *     kt [B,Hkv,64,d], vt [B,Hkv,d,64] of `dtype`     the tokens of the last, unfinished block, as they were given: a value that is not
+ *                                                     finite is one of its column of o only
  *     table [B,Hkv,cap] int32                         a head's pages, oldest first; behind its blocks the pages for the next ones
  *     mass [B,Hkv,cap] fp32                           accumulated attention weight of the block at each place of the table (of the
  *                                                     unfinished one at the next place); zero it for a new sequence

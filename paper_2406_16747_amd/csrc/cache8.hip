@@ -426,6 +426,17 @@ __device__ __forceinline__ f16x8 widen(unsigned lo, unsigned hi)
 
 typedef float f32x4m __attribute__((ext_vector_type(4)));
 
+// 8 bf16 values, 0 where one is not finite.
+__device__ __forceinline__ u32x4 finite_halves(u32x4 w)
+{
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+        const unsigned bad = ((w[e] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;   // (an exponent of ones carries into the sign's place)
+        w[e] &= ~(bad | (bad - (bad >> 15)));
+    }
+    return w;
+}
+
 // The units of a row: the whole blocks, or those that idx names and the one the query ends, if it does; and the unfinished block
 // behind them.
 struct RowUnits {
@@ -463,11 +474,12 @@ __device__ __forceinline__ void add_mass(const AttnArgs& a, const RowUnits& ru, 
     if (j >= 0 && j < a.c.cap && sum != 0.0f) a.c.t.mass[bg * a.c.cap + j] += sum;
 }
 
-// The running softmax over a unit's logits (in s, times log2 e): weights as the operand of the second product (times 2^15).
+// The running softmax over a unit's logits (in s, times log2 e); put(t, r, p) takes the weight of s[t][r], times 2^15.
 struct SoftRow {
     float m, l;
 };
-__device__ __forceinline__ float soft_unit(const f32x4m (&s)[4], SoftRow& row, f16x8 (&pb)[2], float& corr)
+template <class Put>
+__device__ __forceinline__ float soft_unit(const f32x4m (&s)[4], SoftRow& row, float& corr, Put put)
 {
     float top = -INFINITY;
 #pragma unroll
@@ -488,7 +500,7 @@ __device__ __forceinline__ float soft_unit(const f32x4m (&s)[4], SoftRow& row, f
         for (int r = 0; r < 4; r++) {
             const float p = __builtin_amdgcn_exp2f(s[t][r] - (ref - 15.0f));
             sum += p;
-            pb[t >> 1][4 * (t & 1) + r] = (_Float16)p;
+            put(t, r, p);
         }
     const auto d = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
     sum = __uint_as_float(d[0]) + __uint_as_float(d[1]);
@@ -659,7 +671,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void cache8_attn_kernel(Attn
             }
             f16x8 pb[2];
             float corr;
-            const float share = soft_unit(s, row, pb, corr);
+            const float share = soft_unit(s, row, corr, [&](int t, int r, float p) { pb[t >> 1][4 * (t & 1) + r] = (_Float16)p; });
 #pragma unroll
             for (int x = 0; x < NX; x++) {
                 const int vr = 16 * x + col;
@@ -696,7 +708,9 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void cache8_attn_kernel(Attn
 #pragma unroll
             for (int r = 0; r < 4; r++) s[t][r] = 16 * grp + 4 * t + r < ru.tail ? s[t][r] * a.c2 : -INFINITY;
         }
-        // values to fp16, relative to the largest of them; what lies behind the last token may be anything and becomes 0
+        // Values as they lie, in bf16, and weights as the sum of two bf16 numbers (2^-16): a column knows nothing of the others' sizes, and
+        // an infinity or a NaN in one stays there (the second products leave it out: 0 times infinity).  What lies behind the last token may be
+        // anything and becomes 0.
         auto values = [&](int x, int y) {
             u32x4 w = *(const u32x4*)(vp + 16 * x * BT + 8 * y);
 #pragma unroll
@@ -706,22 +720,13 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void cache8_attn_kernel(Attn
             }
             return w;
         };
-        unsigned most = 0;
-#pragma unroll
-        for (int x = 0; x < NX; x++)
-#pragma unroll
-            for (int y = 0; y < 2; y++) {
-                const u32x4 w = values(x, y);
-#pragma unroll
-                for (int e = 0; e < 4; e++) most = max(most, max(w[e] << 16 & 0x7FFFFFFFu, w[e] & 0x7FFF0000u));
-            }
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) most = max(most, (unsigned)__shfl_xor((int)most, d, 64));
-        const int F = scale_exp(most);
-        const float vdown = scale_down(F), vup = scale_up(F);
-        f16x8 pb[2];
+        bf16x8 ph[2], pl[2];
         float corr;
-        const float share = soft_unit(s, row, pb, corr);
+        const float share = soft_unit(s, row, corr, [&](int t, int r, float p) {
+            const __bf16 hi = (__bf16)p;
+            ph[t >> 1][4 * (t & 1) + r] = hi;
+            pl[t >> 1][4 * (t & 1) + r] = (__bf16)(p - (float)hi);
+        });
         if (alone) shares[ru.nsel][col] = share;
         else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(share), wbuf, wat + 4 * ru.nsel, 0, 0);
 #pragma unroll
@@ -730,13 +735,11 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void cache8_attn_kernel(Attn
 #pragma unroll
             for (int z = 0; z < 2; z++) {
                 const u32x4 w = values(x, z);
-                f16x8 v;
-#pragma unroll
-                for (int e = 0; e < 8; e++) v[e] = (_Float16)(half_of(w, e) * vdown);
-                y = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pb[z], y, 0, 0, 0);
+                y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), ph[z], y, 0, 0, 0);
+                y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, finite_halves(w)), pl[z], y, 0, 0, 0);
             }
 #pragma unroll
-            for (int r = 0; r < 4; r++) acc[x][r] = fmaf(acc[x][r], corr, vup * y[r]);
+            for (int r = 0; r < 4; r++) acc[x][r] = fmaf(acc[x][r], corr, y[r]);
         }
     }
     // the four waves' results are joined; rows 4 grp + r of tile x are columns of the head

@@ -1,0 +1,59 @@
+"""The cache in 8 bits at its edges: values of no ordinary size in the unfinished block, queries that are not finite, selections
+without a place, pools smaller than the table."""
+import pytest
+import torch
+
+import block_ref as ref
+import paper_2406_16747_amd as spk
+from gpu_util import require_gpu, say
+
+pytestmark = pytest.mark.gpu
+FORMATS = [torch.int8, torch.float8_e4m3fn]
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def rand(g, *s):
+    return torch.randn(*s, generator=g).bfloat16().cuda()
+
+
+def filled(k, v, H, cap, fmt, scale=None):
+    """A cache of its own with all of k, v [B,Hkv,n,d] in it, and its lengths."""
+    B, Hkv, n, d = k.shape
+    cache = spk.Cache8.empty(B, H, Hkv, d, cap, fmt, scale=scale)
+    spk.sparsek_cache8_append(cache, torch.zeros(B, dtype=torch.int32).cuda(), k, v)
+    return cache, torch.full((B,), n, dtype=torch.int32).cuda()
+
+
+@pytest.mark.parametrize("d,cap,n", [(64, 4, 220), (128, 40, 220), (64, 40, 129), (128, 4, 40)])   # one workgroup has all of it, or several
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan"), 1e30])
+def test_a_value_of_the_unfinished_block_stays_in_its_column(bad, d, cap, n):
+    """One value of the last token: its column is what the definition says, all other columns, the logarithms and the masses have the bits
+    they have without it."""
+    require_gpu()
+    say("cache attention, unfinished block", bad, d, cap, n)
+    B, H, Hkv = 2, 4, 2
+    g = gen(5)
+    k, v, q = rand(g, B, Hkv, n, d), rand(g, B, Hkv, n, d), rand(g, B, H, d)
+    own = torch.full((B, Hkv, 2), -1, dtype=torch.int32).cuda()
+    runs = []
+    for spoil in (False, True):
+        if spoil:
+            v[1, 1, n - 1, 9] = bad
+        cache, L = filled(k, v, H, cap, torch.int8)
+        runs.append([])
+        for idx in (None, own):
+            cache.mass.zero_()
+            runs[-1].append(spk.sparsek_cache8_attn(cache, L, q, idx, accumulate=True) + (cache.mass.clone(),))
+    torch.cuda.synchronize()
+    for (o, lse, mass), (o1, lse1, mass1), idx in zip(*runs, (None, own)):
+        want = ref.cache_attn(cache, [n] * B, q, idx)[0][1, 2:, 9]      # (infinite or NaN, or within 2^-8)
+        got = ref.f64(o1[1, 2:, 9])
+        assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.isinf(got), torch.isinf(want))
+        some = torch.isfinite(want)
+        assert torch.equal(got[torch.isinf(want)], want[torch.isinf(want)])
+        assert ((got - want)[some].abs() <= (2 ** -8 + 2 ** -13) * want[some].abs()).all()
+        o1[1, 2:, 9] = o[1, 2:, 9]
+        assert torch.equal(o, o1) and torch.equal(lse, lse1) and torch.equal(mass, mass1)
