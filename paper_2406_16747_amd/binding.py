@@ -662,14 +662,16 @@ def sparsek_cache8_select(cache, lens, q, top):
 
 
 def sparsek_cache8_attn(cache, lens, q, idx=None, accumulate=False, ws=None):
-    """o [B,H,d] and lse [B,H] fp32 of the query q [B,H,d] at position lens - 1 over all tokens, or over its own block and those of
-    idx [B,Hkv,top]; accumulate=True adds the weights to cache.mass."""
+    """o [B,H,d] and lse [B,H] fp32 of the query q [B,H,d] at position lens - 1 over all tokens (idx None), or over its own block and
+    those of idx [B,Hkv,top] (top 0: its own block only); accumulate=True adds the weights to cache.mass."""
     torch, L, top = _torch(), lib(), 0
     _same("q", q, torch.bfloat16, cache.q_shape, cache.device)
     _same("lens", lens, torch.int32, cache.lens_shape, cache.device)
     if idx is not None:
         top = idx.shape[-1]
         _same("idx", idx, torch.int32, (cache.B, cache.Hkv, top), cache.device)
+        if top == 0:   # (a tensor without elements has no address, which would stand for all tokens: one place that names no block)
+            idx, top = torch.full((cache.B, cache.Hkv, 1), -1, dtype=torch.int32, device=cache.device), 1
     o = torch.empty_like(q)
     lse = torch.empty(cache.B, cache.H, dtype=torch.float32, device=cache.device)
     if ws is None:

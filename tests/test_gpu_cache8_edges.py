@@ -57,3 +57,24 @@ def test_a_value_of_the_unfinished_block_stays_in_its_column(bad, d, cap, n):
         assert ((got - want)[some].abs() <= (2 ** -8 + 2 ** -13) * want[some].abs()).all()
         o1[1, 2:, 9] = o[1, 2:, 9]
         assert torch.equal(o, o1) and torch.equal(lse, lse1) and torch.equal(mass, mass1)
+
+
+@pytest.mark.parametrize("cap,n", [(4, 220), (40, 220), (40, 128), (4, 5)])
+def test_a_selection_of_no_places_is_the_own_block(cap, n):
+    """top = 0 is what a column of -1 is, masses included, and not all tokens."""
+    require_gpu()
+    say("cache attention, empty selection", cap, n)
+    B, H, Hkv, d = 2, 4, 2, 64
+    g = gen(15)
+    cache, L = filled(rand(g, B, Hkv, n, d), rand(g, B, Hkv, n, d), H, cap, torch.int8)
+    q, none = rand(g, B, H, d), torch.full((B, Hkv, 1), -1, dtype=torch.int32).cuda()
+    runs = []
+    for idx in (none, none[..., :0], torch.empty(B, Hkv, 0, dtype=torch.int32).cuda()):
+        cache.mass.zero_()
+        runs.append(spk.sparsek_cache8_attn(cache, L, q, idx, accumulate=True) + (cache.mass.clone(),))
+    torch.cuda.synchronize()
+    ro, rl, rm, ob = ref.cache_attn(cache, [n] * B, q, none)
+    assert ((ref.f64(runs[0][0]) - ro).abs() <= ob).all()
+    for run in runs[1:]:
+        for a, b in zip(run, runs[0]):
+            assert torch.equal(a, b)
