@@ -578,7 +578,7 @@ def sparsek_block_attn_bwd(q, k, v, idx, o, lse, dO, scale, ws=None):
 
 class Cache8:
     """The tensors of a cache (see include/sparsek.h), checked once.  The constructor takes the caller's own; Cache8.empty makes
-    them: a pool of `pages` pages that the rows of the table share out in order."""
+    them: a pool of `pages` pages, of which every row of the table (a sequence's key/value head) has an equal share, in order."""
 
     def __init__(self, k8, v8, ks, vs, km, kms, kt, vt, table, mass, H, scale):
         torch = _torch()
@@ -617,13 +617,18 @@ class Cache8:
 
     @classmethod
     def empty(cls, B, H, Hkv, d, cap, format=None, scale=None, pages=None, device="cuda"):
-        """A cache without tokens; format torch.int8 (default) or torch.float8_e4m3fn, scale d ** -0.5 by default."""
+        """A cache without tokens; format torch.int8 (default) or torch.float8_e4m3fn, scale d ** -0.5 by default.  `pages` (default:
+        one for every place of the table) may be fewer: places beyond a row's pages // (B * Hkv) hold -1, and blocks that become whole
+        there are dropped, until the caller writes pages of their own into the table (those beyond the shares are in nobody's)."""
         torch = _torch()
         format = torch.int8 if format is None else format
         pages = B * Hkv * cap if pages is None else int(pages)
         z = lambda *s, dtype=torch.float32: torch.zeros(*s, dtype=dtype, device=device)  # noqa: E731
         codes = lambda *s: z(*s, dtype=torch.uint8).view(format)                          # noqa: E731
-        table = (torch.arange(B * Hkv * cap, device=device) % pages).to(torch.int32).view(B, Hkv, cap)
+        # (no page in two places: an append writes whole pages, and two of one page would mix their tokens)
+        share = min(pages // (B * Hkv), cap) if B * Hkv > 0 else 0
+        place, row = torch.arange(cap, device=device), torch.arange(B * Hkv, device=device).view(B, Hkv, 1)
+        table = torch.where(place < share, row * share + place, -1).to(torch.int32)
         return cls(codes(pages, BLOCK_TOKENS, d), codes(pages, d, BLOCK_TOKENS), z(pages), z(pages), z(pages, d, dtype=torch.int8), z(pages),
                    z(B, Hkv, BLOCK_TOKENS, d, dtype=torch.bfloat16), z(B, Hkv, d, BLOCK_TOKENS, dtype=torch.bfloat16), table,
                    z(B, Hkv, cap), H, d ** -0.5 if scale is None else scale)

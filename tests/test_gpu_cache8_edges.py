@@ -78,3 +78,30 @@ def test_a_selection_of_no_places_is_the_own_block(cap, n):
     for run in runs[1:]:
         for a, b in zip(run, runs[0]):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_sequences_of_a_small_pool_keep_apart(fmt):
+    """A pool of half the table: what goes in at once lies in pages of its own, codes and scales of one block together; blocks beyond a
+    row's share are dropped and attended by nobody."""
+    require_gpu()
+    say("cache of a small pool", fmt)
+    B, H, Hkv, d, cap, n = 3, 4, 2, 64, 8, 6 * 64 + 9
+    g = gen(25)
+    k, v, q = rand(g, B, Hkv, n, d), rand(g, B, Hkv, n, d), rand(g, B, H, d)
+    cache = spk.Cache8.empty(B, H, Hkv, d, cap, fmt, pages=B * Hkv * cap // 2)
+    L = torch.full((B,), n, dtype=torch.int32).cuda()
+    spk.sparsek_cache8_append(cache, torch.zeros_like(L), k, v)
+    o, lse = spk.sparsek_cache8_attn(cache, L, q, accumulate=True)
+    torch.cuda.synchronize()
+    K8, V8 = ref.values(cache.k8), ref.values(cache.v8)
+    for b in range(B):
+        for h in range(Hkv):
+            for j in range(cap // 2):
+                page = int(cache.table[b, h, j])
+                for x, codes, scale in ((k, K8[page], cache.ks[page]), (v, V8[page].T, cache.vs[page])):
+                    y, s = ref.block_codes(x[b, h, 64 * j:64 * j + 64], fmt)
+                    assert torch.equal(codes, y) and float(scale) == float(s), (b, h, j)
+    ro, rl, rm, ob = ref.cache_attn(cache, [n] * B, q)
+    assert ((ref.f64(o) - ro).abs() <= ob).all()
+    assert ((ref.f64(cache.mass) - rm).abs() <= 2 ** -12 * rm).all() and (cache.mass[..., cap // 2:6] == 0).all()
