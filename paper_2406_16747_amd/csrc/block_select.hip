@@ -227,7 +227,8 @@ __global__ __launch_bounds__(256) void block_select_kernel(const uint16_t* __res
 size_t block_select_ws_bytes(const sparsek_block_cfg& c)
 {
     const size_t BG = (size_t)c.B * c.Hkv, nbw = c.n / BT;
-    return align_up(BG * nbw * c.d, 256) + align_up(BG * scale_row(nbw) * sizeof(float), 256);
+    // (0 is what the size query says of a configuration that is refused; without a whole block there is nothing to keep)
+    return std::max<size_t>(256, align_up(BG * nbw * c.d, 256) + align_up(BG * scale_row(nbw) * sizeof(float), 256));
 }
 
 int launch_block_select(const sparsek_block_cfg& c, const void* q, const void* k, int32_t* idx, void* ws, hipStream_t st)

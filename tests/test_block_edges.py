@@ -22,3 +22,12 @@ def test_a_new_cache_has_no_page_in_two_places(B, Hkv, cap, pages):
 def test_a_new_cache_of_nothing_is_refused(kw):
     with pytest.raises((ValueError, RuntimeError)):
         spk.Cache8.empty(**{**dict(B=1, H=4, Hkv=2, d=64, cap=4, device="cpu"), **kw})
+
+
+@pytest.mark.parametrize("n", [1, 63, 64, 65])
+@pytest.mark.parametrize("top", [0, 1, 64])
+def test_every_configuration_that_is_served_has_a_workspace(n, top):
+    """0 stands for a configuration that is refused."""
+    c = spk.SparsekBlockCfg(B=1, H=2, Hkv=1, n=n, d=64, top=top, dtype=spk.BF16, softmax_scale=1.0)
+    for name in ("select", "attn_fwd", "attn_bwd"):
+        assert getattr(spk.lib(), "sparsek_block_%s_workspace_bytes" % name)(c) > 0, name
