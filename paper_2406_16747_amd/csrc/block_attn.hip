@@ -578,7 +578,8 @@ __global__ __launch_bounds__(256) void block_join_kernel(BlockFwd f, int rows_pe
 #pragma unroll
     for (int e = 0; e < 4; e++) out[e] = pack_bf16x2(acc[2 * e] * inv, acc[2 * e + 1] * inv);
     __builtin_nontemporal_store(out, (u32x4*)(f.o + at * D + 8 * t));
-    if (t == 0) f.lse[at] = (ref + log2f(L)) * 0.6931471805599453f;
+    // (L = 0: logits of -inf alone, of a query that is not finite; any other row has a weight of 1 among its blocks)
+    if (t == 0) f.lse[at] = L == 0.0f ? __uint_as_float(0x7FC00000u) : (ref + log2f(L)) * 0.6931471805599453f;
 }
 
 // mass_j: the weights that the block's keys got from the stretch's queries and the heads of the group join what earlier stretches gave.
