@@ -328,7 +328,7 @@ int sparsek_block_attn_bwd(const sparsek_block_cfg *cfg, const void *q, const vo
  *     (the one that token lens - 1 lies in) with the largest scores, as sparsek_block_select.
  * attn:  o out [B,H,d], lse out [B,H] fp32: the query attends all tokens (idx NULL), or its own block and the whole blocks of idx
  *     [B,Hkv,top] (places in the table; places of no whole block behind its own, and repeated ones, are left out).  A sequence without
- *     tokens gets o = 0 and lse = -inf.  accumulate != 0: the weights are added to mass.
+ *     tokens gets o = 0 and lse = -inf, a query that is not finite NaN for both.  accumulate != 0: the weights are added to mass.
  * evict: sequences with more than `budget` whole blocks keep the first `sink`, the last `recent` and of the others those with the largest
  *     mass (of equal ones the older), `budget` in all, by age.  table_out and mass_out [B,Hkv,cap], lens_out [B] out: the kept pages
  *     first, then those that went (free for new blocks), then the rest; masses move along, the unfinished block's with it, what lies

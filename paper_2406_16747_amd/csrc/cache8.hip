@@ -510,6 +510,15 @@ __device__ __forceinline__ float soft_unit(const f32x4m (&s)[4], SoftRow& row, f
     return ref + log2f(sum * 0x1p-15f);   // log2 of the unit's share
 }
 
+// The largest logit of keys that were attended but have none above -inf: they are infinite themselves, or their query is, or their scale
+// is NaN.  Below every logit, and still not the -inf of no keys at all: what remains of such a row alone is 0 / 0.
+constexpr float NO_LOGIT = -3.0e38f;
+__device__ __forceinline__ float log_of(float top, float sum)   // a row's lse; sum: times 2^15
+{
+    if (top == -INFINITY) return -INFINITY;
+    return sum == 0.0f ? __uint_as_float(0x7FC00000u) : (top + log2f(sum * 0x1p-15f)) * 0.6931471805599453f;
+}
+
 // A wave's block in LDS: 64 rows of D bytes of keys, D rows of 64 bytes of values.  The pieces (16 bytes) of a row change places so that the
 // 8 lanes that read at a time find them in different banks; a row's stay among each other, so the loads see whole lines.
 template <int D>
@@ -744,7 +753,8 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void cache8_attn_kernel(Attn
     }
     // the four waves' results are joined; rows 4 grp + r of tile x are columns of the head
     if (grp == 0) {
-        sm_[wv][col] = row.m == -INFINITY && row.l != row.l ? 0.0f : row.m;   // (keys there were, but with a scale of NaN)
+        const bool some = have || (ru.tail && ru.nsel >= u0 && ru.nsel < u0 + a.upw);
+        sm_[wv][col] = row.m == -INFINITY && some ? NO_LOGIT : row.m;
         sl[wv][col] = row.l;
     }
 #pragma unroll
@@ -763,7 +773,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void cache8_attn_kernel(Attn
         if (alone) {
             const bool some_key = M > -INFINITY;
             a.o[(head0 + h) * D + d] = f32_to_bf16(some_key ? sum / den : 0.0f);
-            if (d == 0) a.lse[head0 + h] = some_key ? (M + log2f(den * 0x1p-15f)) * 0.6931471805599453f : -INFINITY;
+            if (d == 0) a.lse[head0 + h] = log_of(M, den);
             continue;
         }
         const size_t at = (head0 + h) * a.splits + split;
@@ -845,7 +855,7 @@ __global__ __launch_bounds__(256) void cache8_join_kernel(AttnArgs a, int mass_w
                 if (tid < D) y = fmaf(f, red[w][tid], y);
             }
         if (tid < D) a.o[row * D + tid] = f32_to_bf16(top > -INFINITY ? y / all : 0.0f);
-        if (tid == 0) a.lse[row] = top > -INFINITY ? (top + log2f(all * 0x1p-15f)) * 0.6931471805599453f : -INFINITY;
+        if (tid == 0) a.lse[row] = log_of(top, all);
         return;
     }
     auto total = [&](int h) {   // log2 of head h's sum, by a wave

@@ -105,3 +105,54 @@ def test_sequences_of_a_small_pool_keep_apart(fmt):
     ro, rl, rm, ob = ref.cache_attn(cache, [n] * B, q)
     assert ((ref.f64(o) - ro).abs() <= ob).all()
     assert ((ref.f64(cache.mass) - rm).abs() <= 2 ** -12 * rm).all() and (cache.mass[..., cap // 2:6] == 0).all()
+
+
+@pytest.mark.parametrize("cap,n", [(4, 220), (40, 220), (40, 128), (4, 30)])
+@pytest.mark.parametrize("value", [float("inf"), -float("inf"), float("nan")])
+@pytest.mark.parametrize("H", [4, 40])
+def test_a_query_that_is_not_finite_gets_nan(value, cap, n, H):
+    """Whatever the sign of its products: with keys of one sign in its column they are all +inf or all -inf, and the latter are not a
+    sequence without tokens.  Other heads have the bits they have without it; a sequence without tokens gives it 0 and -inf."""
+    require_gpu()
+    say("cache attention, a query of", value, cap, n, H)
+    B, Hkv, d = 3, 2, 64
+    g = gen(35)
+    k, v, q = rand(g, B, Hkv, n, d), rand(g, B, Hkv, n, d), rand(g, B, H, d)
+    k[..., 7] = 4.0     # (no code of 0 in the column)
+    cache, L = filled(k, v, H, cap, torch.int8)
+    L[2] = 0
+    own = torch.full((B, Hkv, 1), -1, dtype=torch.int32).cuda()
+    for idx in (None, own):
+        runs = []
+        for x in (q[1, 1, 7].item(), value):
+            q[1:, 1, 7] = x
+            runs.append(spk.sparsek_cache8_attn(cache, L, q, idx))
+        torch.cuda.synchronize()
+        (o, lse), (o1, lse1) = runs
+        assert torch.isnan(o1[1, 1]).all() and torch.isnan(lse1[1, 1])
+        assert (o1[2] == 0).all() and (lse1[2] == float("-inf")).all()
+        o1[1, 1], lse1[1, 1] = o[1, 1], lse[1, 1]
+        assert torch.equal(o, o1) and torch.equal(lse, lse1)
+        q[1:, 1, 7] = 0.5
+
+
+@pytest.mark.parametrize("cap", [4, 40])
+def test_keys_of_minus_infinity_alone_are_not_no_keys(cap):
+    """A sequence whose only token has a logit of -inf: 0 / 0, and not what a sequence without tokens has; with others it has weight 0."""
+    require_gpu()
+    say("cache attention, only logits of -inf", cap)
+    g = gen(45)
+    k, v, q = rand(g, 2, 1, 3, 64), rand(g, 2, 1, 3, 64), rand(g, 2, 2, 64).abs()
+    k[:, :, 2, 9] = float("-inf")
+    cache, L = filled(k[:, :, 2:].contiguous(), v[:, :, 2:].contiguous(), 2, cap, torch.int8)
+    L[1] = 0
+    o, lse = spk.sparsek_cache8_attn(cache, L, q, accumulate=True)
+    torch.cuda.synchronize()
+    assert torch.isnan(o[0]).all() and torch.isnan(lse[0]).all()
+    assert (o[1] == 0).all() and (lse[1] == float("-inf")).all() and (cache.mass[1] == 0).all()
+    cache, L = filled(k, v, 2, cap, torch.int8)
+    o, lse = spk.sparsek_cache8_attn(cache, L, q)
+    cache, L = filled(k[:, :, :2].contiguous(), v[:, :, :2].contiguous(), 2, cap, torch.int8)
+    o2, lse2 = spk.sparsek_cache8_attn(cache, L, q)
+    torch.cuda.synchronize()
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
