@@ -344,14 +344,26 @@ __device__ __forceinline__ void block_weights(uint32_t rk, const bf16x8 (&qf)[D 
 #pragma unroll
         for (int r = 0; r < 16; r++) m = fmaxf(m, s[kh][r]);
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
-    m = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * c2;
-    const float ref = (m == -INFINITY ? 0.0f : m) - 15.0f;
+    const float most = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+    m = most * c2;
+    const float at = m == -INFINITY ? 0.0f : m;
+    float ref = at - 15.0f, by = c2;
+    const bool large = fabsf(at) >= 0x1p22f;
+    if (__any(large)) {   // the roundings of m and m - 15 count: such a row's logits become distances from the largest first
+        const float off = fmaf(most, c2, -at);
+#pragma unroll
+        for (int kh = 0; kh < 2; kh++)
+#pragma unroll
+            for (int r = 0; r < 16; r++) s[kh][r] = large ? fmaf(s[kh][r], c2, -at) - off : s[kh][r];
+        by = large ? 1.0f : c2;
+        ref = large ? -15.0f : ref;
+    }
     den = 0.0f;
 #pragma unroll
     for (int kh = 0; kh < 2; kh++)
 #pragma unroll
         for (int r = 0; r < 16; r++) {
-            const float p = __builtin_amdgcn_exp2f(fmaf(s[kh][r], c2, -ref));
+            const float p = __builtin_amdgcn_exp2f(fmaf(s[kh][r], by, -ref));
             den += p;
             pb[2 * kh + (r >> 3)][r & 7] = (_Float16)p;
         }

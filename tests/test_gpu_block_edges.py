@@ -53,3 +53,29 @@ def test_a_query_that_is_not_finite_gets_nan(value, at, d):
     keys = ref.seen(idx[0, 0].cpu().numpy(), n)[at].cuda()
     assert torch.isnan(dk1[0, 0][keys]).all() and torch.isnan(dv1[0, 0][keys]).all()
     assert torch.equal(dk[0, 0][~keys], dk1[0, 0][~keys]) and torch.equal(dv[0, 0][~keys], dv1[0, 0][~keys])
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("e", [8, 20, 23, 24, 25, 26, 27, 30, 60, 100])
+def test_logits_of_all_sizes(e, sign):
+    """Logits up to 2^e, each of its own: the weight is the largest one's alone.  The products are exact here, so nothing but the size is
+    at stake."""
+    require_gpu()
+    say("block attention, logits of 2^%d" % e, sign)
+    n, d, top = 250, 64, 2
+    g = torch.Generator().manual_seed(91)
+    c = (torch.randperm(255, generator=g)[:n].float() + 1) / 256
+    q, k = torch.full((1, 2, n, d), float(sign)).bfloat16().cuda(), c.view(1, 1, n, 1).expand(1, 1, n, d).bfloat16().contiguous().cuda()
+    v = torch.randn(1, 1, n, d, generator=g).bfloat16().cuda()
+    scale = 0.7 * 2.0 ** e / d
+    idx = spk.sparsek_block_select(q, k, top)
+    o, lse, mass = spk.sparsek_block_attn_fwd(q, k, v, idx, scale, mass=True)
+    torch.cuda.synchronize()
+    ro, rl, rm, ob, _ = ref.attn(q, k, v, idx, scale)
+    if e >= 20:   # (the next logit is 2^-8 * 0.7 * 2^e behind, at least)
+        within(o, ro, 2 ** -8 * ro.abs() + 2 ** -11 * ro.abs() + 2 ** -24, "o")
+    else:
+        within(o, ro, ob + 2 ** -22 * 2 ** e * ro.abs().amax(), "o")     # (a logit of 2^e is off by 2^-23 of it, twice)
+    within(lse, rl, 2 ** -21 * rl.abs() + 2 ** -20, "lse")
+    if e == 8:    # masses go by the fp32 lse, whose own rounding is a factor of its size beyond that
+        within(mass, rm, 2 ** -12 * rm + 1e-9, "mass")
