@@ -498,7 +498,7 @@ __device__ __forceinline__ float soft_unit(const f32x4m (&s)[4], SoftRow& row, f
     for (int t = 0; t < 4; t++)
 #pragma unroll
         for (int r = 0; r < 4; r++) {
-            const float p = __builtin_amdgcn_exp2f(s[t][r] - (ref - 15.0f));
+            const float p = __builtin_amdgcn_exp2f(s[t][r] - ref + 15.0f);   // (ref - 15 would be rounded where it is large, past fp16's range)
             sum += p;
             put(t, r, p);
         }

@@ -156,3 +156,28 @@ def test_keys_of_minus_infinity_alone_are_not_no_keys(cap):
     o2, lse2 = spk.sparsek_cache8_attn(cache, L, q)
     torch.cuda.synchronize()
     assert torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("cap,n", [(4, 220), (40, 220), (40, 128)])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("e", [8, 20, 23, 24, 25, 26, 27, 30, 60])
+def test_logits_of_all_sizes(e, sign, cap, n):
+    """Logits up to 2^e, each block's and token's apart: the weight is the largest one's alone."""
+    require_gpu()
+    say("cache attention, logits of 2^%d" % e, sign, cap, n)
+    g = gen(55)
+    c = (torch.randperm(255, generator=g)[:n].float() + 1) / 256
+    k = c.view(1, 1, n, 1).expand(1, 1, n, 64).bfloat16().contiguous().cuda()
+    v, q = rand(g, 1, 1, n, 64), torch.full((1, 2, 64), float(sign)).bfloat16().cuda()
+    cache, L = filled(k, v, 2, cap, torch.int8, scale=0.7 * 2.0 ** e / 64)
+    o, lse = spk.sparsek_cache8_attn(cache, L, q)
+    torch.cuda.synchronize()
+    ro, rl, rm, ob = ref.cache_attn(cache, [n], q)
+    K = ref.row_tokens(cache, [n], 0, 0)[0][:, 0] * sign
+    first, second = torch.unique(K).topk(2).values.tolist()
+    if e >= 20:   # (codes of equal keys in one block share the weight; the next logit is far behind)
+        assert (first - second) * 0.7 * 2.0 ** e > 2.0 ** 10
+        assert ((ref.f64(o) - ro).abs() <= ob + 2 ** -11 * ro.abs()).all()
+    else:
+        assert ((ref.f64(o) - ro).abs() <= ob + 2 ** -22 * 2 ** e * ro.abs().amax()).all()
+    assert ((lse.cpu().double() - rl).abs() <= 2 ** -21 * rl.abs() + 2 ** -20).all()
