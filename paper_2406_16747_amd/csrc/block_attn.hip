@@ -313,12 +313,11 @@ struct BlockFwd {
 template <int D>
 __device__ __forceinline__ f16x8 transposed_half(uint32_t at) { return __builtin_bit_cast(f16x8, transposed_operand<D>(at)); }
 
-// The softmax of one tile of 32 rows against the block's 64 keys: S^T = K.Q^T, and P^T as the operand of O^T = V^T.P^T.  A lane has one
-// column (row of q); with `own` it sees keys 0 .. limit of the block.  V is in fp16, relative to the block's largest value, and so
-// are the weights (times 2^15): a weight is rounded to 2^-11 where bf16 would keep 2^-8, at the same rate.
-template <int D>
-__device__ __forceinline__ void block_weights(uint32_t rk, const bf16x8 (&qf)[D / 16], float c2, bool own, int limit, int half, f16x8 (&pb)[4],
-                                              float& m, float& den)
+// The softmax of one tile of 32 rows against the block's 64 keys: S^T = K.Q^T; put(x, p) takes the weights (times 2^UP), x in the order of
+// P^T as the operand of O^T = V^T.P^T.  A lane has one column (row of q); with `own` it sees keys 0 .. limit of the block.
+template <int D, int UP, class Put>
+__device__ __forceinline__ void block_weights(uint32_t rk, const bf16x8 (&qf)[D / 16], float c2, bool own, int limit, int half, float& m, float& den,
+                                              Put put)
 {
     using S = RowTile<D>;
     constexpr int DS = D / 16;
@@ -347,16 +346,16 @@ __device__ __forceinline__ void block_weights(uint32_t rk, const bf16x8 (&qf)[D 
     const float most = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
     m = most * c2;
     const float at = m == -INFINITY ? 0.0f : m;
-    float ref = at - 15.0f, by = c2;
+    float ref = at - UP, by = c2;
     const bool large = fabsf(at) >= 0x1p22f;
-    if (__any(large)) {   // the roundings of m and m - 15 count: such a row's logits become distances from the largest first
+    if (__any(large)) {   // the roundings of m and m - UP count: such a row's logits become distances from the largest first
         const float off = fmaf(most, c2, -at);
 #pragma unroll
         for (int kh = 0; kh < 2; kh++)
 #pragma unroll
             for (int r = 0; r < 16; r++) s[kh][r] = large ? fmaf(s[kh][r], c2, -at) - off : s[kh][r];
         by = large ? 1.0f : c2;
-        ref = large ? -15.0f : ref;
+        ref = large ? (float)-UP : ref;
     }
     den = 0.0f;
 #pragma unroll
@@ -365,7 +364,7 @@ __device__ __forceinline__ void block_weights(uint32_t rk, const bf16x8 (&qf)[D 
         for (int r = 0; r < 16; r++) {
             const float p = __builtin_amdgcn_exp2f(fmaf(s[kh][r], by, -ref));
             den += p;
-            pb[2 * kh + (r >> 3)][r & 7] = (_Float16)p;
+            put(16 * kh + r, p);
         }
     const auto sl = __builtin_amdgcn_permlane32_swap(__float_as_uint(den), __float_as_uint(den), false, false);
     den = __uint_as_float(sl[0]) + __uint_as_float(sl[1]);
@@ -376,7 +375,7 @@ struct FwdBlockSmem {
     static constexpr int RS = 128 + 16;     // bytes between rows: half a row of 128 columns
     unsigned char k[RowTile<D>::BYTES], v[RowTile<D>::BYTES];
     unsigned char rows[4][32 * RS];         // a wave's rows on their way in and its results on their way out
-    unsigned red[4], bad[2][2];             // bad: keys that are not finite, or have values that are not, as bits
+    unsigned red[8], bad[2][2];             // bad: keys that are not finite, or have values that are not, as bits
 };
 static_assert(sizeof(FwdBlockSmem<128>) <= 160 * 1024 / 3, "three workgroups per CU");
 
@@ -398,10 +397,12 @@ __global__ __launch_bounds__(256, 3) void block_tiles_kernel(BlockFwd f)
     const int end = min(l.total[cbg * l.nb + j] * G, first + l.unit);
     const size_t kv = ((size_t)bg * l.n + (size_t)j * BT) * D;
     const int last = l.n - 1 - j * BT;
-    // V goes to fp16 relative to its largest magnitude.  What is not finite in a key or in its values is left out of that and of the
-    // products, and makes the rows that attend the key NaN.
+    // V goes to fp16 relative to its largest magnitude, and so do the weights (times 2^15): a weight is rounded to 2^-11 where bf16
+    // would keep 2^-8, at the same rate.  What is not finite in a key or in its values is left out of that and of the products, and makes
+    // the rows that attend the key NaN.  A block is wide when some 8 values side by side (not all 0) lie more than 2^13 below the largest:
+    // its own rows see some of its tokens only, and one that they do not see must not push what they see out of fp16's range.
     u32x4 vr[BT * CPR / 256];
-    unsigned top = 0, bad_k = 0, bad_v = 0;
+    unsigned top = 0, low = 0, bad_k = 0, bad_v = 0;   // low: of the smallest pieces, inverted
 #pragma unroll
     for (int t = 0; t < BT * CPR / 256; t++) {
         const int id = tid + 256 * t;
@@ -416,9 +417,12 @@ __global__ __launch_bounds__(256, 3) void block_tiles_kernel(BlockFwd f)
             bad_v |= 1u << t;
         }
         top = max(top, y >= INF_BITS ? 0u : y);
+        low = max(low, y >= INF_BITS || y == 0 ? 0u : ~y);
     }
     if (tid < 4) (&sm.bad[0][0])[tid] = 0;
-    const int E = scale_exp(block_max_bits(top, sm.red, tid));   // (with a barrier inside)
+    block_max_bits2(top, low, sm.red, tid);   // (with a barrier inside)
+    const int E = scale_exp(top);
+    const bool wide = __builtin_amdgcn_readfirstlane((int)is_wide(top, low));
     note_rows<D>(sm.bad[0], bad_k, tid);
     note_rows<D>(sm.bad[1], bad_v, tid);
     const float down = scale_down(E), up = scale_up(E);
@@ -428,6 +432,7 @@ __global__ __launch_bounds__(256, 3) void block_tiles_kernel(BlockFwd f)
         f16x8 y;
 #pragma unroll
         for (int e = 0; e < 8; e++) y[e] = (_Float16)(__uint_as_float(e & 1 ? vr[t][e / 2] & 0xFFFF0000u : vr[t][e / 2] << 16) * down);
+        if (wide) y = __builtin_bit_cast(f16x8, vr[t]);   // (as they are, in bf16)
         *(f16x8*)(sm.v + RowTile<D>::offset(id / CPR) + 16 * (id % CPR)) = y;
     }
     __syncthreads();
@@ -465,67 +470,132 @@ __global__ __launch_bounds__(256, 3) void block_tiles_kernel(BlockFwd f)
             wave_lds_order();
         }
     };
-    int r0 = first + 32 * wv;
-    if (r0 >= end) return;
-    int i = entry(r0 + col), i_next = entry(r0 + 128 + col);
-    u32x4 next[4 * NH];
-    load_q(r0 + col, i, next);
-    take_q(next);
-    for (; r0 < end; r0 += 128) {
-        const int r = r0 + col;
-        const int i_then = entry(r + 256);
-        load_q(r + 128, i_next, next);
-        f16x8 pb[4];
-        float m, den;
-        block_weights<D>(rk, qf, f.a.c2, r0 < own_end, i - j * BT, half, pb, m, den);
+    // The factor of a row's result, NaN where it attends what is not finite, and its denominator likewise.
+    auto factor = [&](int i, float& den) {
         float inv = den > 0.0f ? 1.0f / den : den;   // (nothing but -inf: weight 0 in the sum)
         if (badk | badv) {
             const unsigned long long attended = (2ull << min(BT - 1, i - j * BT)) - 1;
             inv = (badk | badv) & attended ? __uint_as_float(0x7FC00000u) : inv;
             den = badk & attended ? __uint_as_float(0x7FC00000u) : den;
         }
-        // (rows behind the last one, and the upper lanes' copy of the logarithms, lie outside the buffers and are dropped)
-        const int count = min(32, end - r0);
-        const auto dst = buffer_of(f.part + (row0 + r0) * D, 2 * D * count);
-        store_words(buffer_of(f.meta + row0 + r0, 8 * count), half ? 0x7FFFFFF0 : 8 * col, u32x2{__float_as_uint(m + log2f(den * 0x1p-15f)), __float_as_uint(up)});
+        return inv;
+    };
+    // 64 columns of 32 rows' results, times `by`, go out.  (Rows behind the last one lie outside the buffer and are dropped.)
+    auto leave = [&](buffer_t dst, int h, const f32x16 (&acc)[2], float by) {
 #pragma unroll
-        for (int h = 0; h < NH; h++) {
+        for (int x = 0; x < 2; x++)
+#pragma unroll
+            for (int y = 0; y < 4; y += 2) {
+                // columns 8 y .. 8 y + 7 from both halves of the wave to its lower lanes, the next 8 to its upper lanes
+                u32x4 w;
+#pragma unroll
+                for (int e = 0; e < 2; e++) {
+                    const f16x2v a = {(_Float16)(acc[x][4 * y + 2 * e] * by), (_Float16)(acc[x][4 * y + 2 * e + 1] * by)};
+                    const f16x2v c = {(_Float16)(acc[x][4 * y + 4 + 2 * e] * by), (_Float16)(acc[x][4 * y + 5 + 2 * e] * by)};
+                    const auto sw = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, c), false, false);
+                    w[e] = sw[0];
+                    w[2 + e] = sw[1];
+                }
+                *(u32x4*)(rows + col * RS + 64 * x + 16 * (y + half)) = w;
+            }
+        wave_lds_order();
+#pragma unroll
+        for (int t = 0; t < 4; t++) {
+            const u32x4 w = *(const u32x4*)(rows + (8 * t + lrow) * RS + 2 * lcol);
+            if (f.stream) stream_words(dst, 2 * D * (8 * t + lrow) + 128 * h + 2 * lcol, w);
+            else store_words(dst, 2 * D * (8 * t + lrow) + 128 * h + 2 * lcol, w);
+        }
+        wave_lds_order();
+    };
+    // (the upper lanes' copy of the logarithms lies outside the buffer)
+    auto leave_meta = [&](int r0, int count, float logden, float up) {
+        store_words(buffer_of(f.meta + row0 + r0, 8 * count), half ? 0x7FFFFFF0 : 8 * col, u32x2{__float_as_uint(logden), __float_as_uint(up)});
+    };
+    int r0 = first + 32 * wv;
+    if (r0 >= end) return;
+    u32x4 next[4 * NH];
+    if (!wide) {
+        int i = entry(r0 + col), i_next = entry(r0 + 128 + col);
+        load_q(r0 + col, i, next);
+        take_q(next);
+        for (; r0 < end; r0 += 128) {
+            const int r = r0 + col;
+            const int i_then = entry(r + 256);
+            load_q(r + 128, i_next, next);
+            f16x8 pb[4];
+            float m, den;
+            block_weights<D, 15>(rk, qf, f.a.c2, r0 < own_end, i - j * BT, half, m, den, [&](int x, float p) { pb[x / 8][x % 8] = (_Float16)p; });
+            const float inv = factor(i, den);
+            const int count = min(32, end - r0);
+            const auto dst = buffer_of(f.part + (row0 + r0) * D, 2 * D * count);
+            leave_meta(r0, count, m + log2f(den * 0x1p-15f), up);
+#pragma unroll
+            for (int h = 0; h < NH; h++) {
+                f32x16 acc[2];
+#pragma unroll
+                for (int x = 0; x < 2; x++) acc[x] = f32x16{0};
+#pragma unroll
+                for (int y = 0; y < 4; y++)
+#pragma unroll
+                    for (int x = 0; x < 2; x++)
+                        acc[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(transposed_half<D>(tv + y * RowTile<D>::R16 + 64 * (2 * h + x)), pb[y], acc[x], 0, 0, 0);
+                leave(dst, h, acc, inv);
+            }
+            take_q(next);   // (here and not ahead of the loop's next round: the wait for these loads leaves the stores under way)
+            i = i_next;
+            i_next = i_then;
+        }
+    } else {
+        // Rare, and so without loads ahead: V in bf16, which holds any size, weights as the sum of two bf16 numbers (2^-16; at most 2^-7, so that
+        // no sum of products passes what fp32 holds), results relative to the row's own largest, for which the products are made twice (32 heads of 32768, 16
+        // blocks, every block wide: the attention 2608 us, 2336 as it is).
+        for (; r0 < end; r0 += 128) {
+            const int i = entry(r0 + col);
+            load_q(r0 + col, i, next);
+            take_q(next);
+            bf16x8 ph[4], pl[4];
+            float m, den;
+            block_weights<D, -7>(rk, qf, f.a.c2, r0 < own_end, i - j * BT, half, m, den, [&](int x, float p) {
+                const __bf16 hi = (__bf16)p;
+                ph[x / 8][x % 8] = hi;
+                pl[x / 8][x % 8] = (__bf16)(p - (float)hi);
+            });
+            const float inv = factor(i, den);
+            auto product = [&](int h, f32x16 (&acc)[2]) {
+#pragma unroll
+                for (int x = 0; x < 2; x++) {
+                    acc[x] = f32x16{0};
+#pragma unroll
+                    for (int y = 0; y < 4; y++) {
+                        const bf16x8 vt = transposed_operand<D>(tv + y * RowTile<D>::R16 + 64 * (2 * h + x));
+                        acc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, ph[y], acc[x], 0, 0, 0);
+                        acc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, pl[y], acc[x], 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; e++) acc[x][e] *= inv;
+                }
+            };
             f32x16 acc[2];
-#pragma unroll
-            for (int x = 0; x < 2; x++) acc[x] = f32x16{0};
-#pragma unroll
-            for (int y = 0; y < 4; y++)
+            float most = 0.0f;
+#pragma unroll 1
+            for (int h = 0; h < NH; h++) {
+                product(h, acc);
 #pragma unroll
                 for (int x = 0; x < 2; x++)
-                    acc[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(transposed_half<D>(tv + y * RowTile<D>::R16 + 64 * (2 * h + x)), pb[y], acc[x], 0, 0, 0);
 #pragma unroll
-            for (int x = 0; x < 2; x++)
-#pragma unroll
-                for (int y = 0; y < 4; y += 2) {
-                    // columns 8 y .. 8 y + 7 from both halves of the wave to its lower lanes, the next 8 to its upper lanes
-                    u32x4 w;
-#pragma unroll
-                    for (int e = 0; e < 2; e++) {
-                        const f16x2v a = {(_Float16)(acc[x][4 * y + 2 * e] * inv), (_Float16)(acc[x][4 * y + 2 * e + 1] * inv)};
-                        const f16x2v c = {(_Float16)(acc[x][4 * y + 4 + 2 * e] * inv), (_Float16)(acc[x][4 * y + 5 + 2 * e] * inv)};
-                        const auto sw = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, c), false, false);
-                        w[e] = sw[0];
-                        w[2 + e] = sw[1];
-                    }
-                    *(u32x4*)(rows + col * RS + 64 * x + 16 * (y + half)) = w;
-                }
-            wave_lds_order();
-#pragma unroll
-            for (int t = 0; t < 4; t++) {
-                const u32x4 w = *(const u32x4*)(rows + (8 * t + lrow) * RS + 2 * lcol);
-                if (f.stream) stream_words(dst, 2 * D * (8 * t + lrow) + 128 * h + 2 * lcol, w);
-                else store_words(dst, 2 * D * (8 * t + lrow) + 128 * h + 2 * lcol, w);
+                    for (int e = 0; e < 16; e++) most = fmaxf(most, fabsf(acc[x][e]));
             }
-            wave_lds_order();
+            const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false);
+            const int F = scale_exp(max((unsigned)sw[0], (unsigned)sw[1]));
+            const int count = min(32, end - r0);
+            const auto dst = buffer_of(f.part + (row0 + r0) * D, 2 * D * count);
+            leave_meta(r0, count, m + log2f(den * 0x1p7f), scale_up(F));
+#pragma unroll 1
+            for (int h = 0; h < NH; h++) {
+                product(h, acc);
+                leave(dst, h, acc, scale_down(F));
+            }
         }
-        take_q(next);   // (here and not ahead of the loop's next round: the wait for these loads leaves the stores under way)
-        i = i_next;
-        i_next = i_then;
     }
 }
 

@@ -100,6 +100,9 @@ __device__ __forceinline__ unsigned top_of_8(u32x4 x)
     return top;
 }
 constexpr unsigned INF_BITS = 0x7F800000u;
+// Whether the smallest of a block's pieces of 8 values (`low`, inverted; 0: none but zeros) lies more than 2^13 below its largest value:
+// relative to that, fp16 still has all its bits down to 2^-27.
+__device__ __forceinline__ bool is_wide(unsigned top, unsigned low) { return low && (top >> 23) > (~low >> 23) + 13; }
 
 // 64 rows of D bf16 (contiguous rows at src, row r clamped to r_max) into a RowTile; 256 threads.  Returns the largest finite magnitude
 // that the thread has seen, as bits.  Pieces with an infinity or a NaN become zeros (a weight of zero times one of those would reach

@@ -79,3 +79,73 @@ def test_logits_of_all_sizes(e, sign):
     within(lse, rl, 2 ** -21 * rl.abs() + 2 ** -20, "lse")
     if e == 8:    # masses go by the fp32 lse, whose own rounding is a factor of its size beyond that
         within(mass, rm, 2 ** -12 * rm + 1e-9, "mass")
+
+
+def behind(kind, g, shape):
+    """What may lie behind a sequence that is shorter than its batch: finite numbers of any size."""
+    if kind == "largest":
+        return torch.full(shape, torch.finfo(torch.bfloat16).max)
+    if kind == "lowest":
+        return torch.full(shape, torch.finfo(torch.bfloat16).min)
+    x = torch.randn(shape, generator=g)
+    return x * 2.0 ** 45 if kind == "large" else x * torch.exp2(torch.randint(-120, 100, shape, generator=g).float())
+
+
+PADDED = [(kind, d, real) for kind in ("large", "any", "largest", "lowest") for d in (64, 128)
+          for real in (200, 129, 191)]                             # in the middle of a block, one token and all but one of it
+
+
+def padded(kind, d, real):
+    n, H, Hkv, top = 300, 4, 2, 2
+    g = torch.Generator().manual_seed(7)
+    q, k, v, dO = draw(93, 1, H, Hkv, n, d)
+    dO[:, :, real:] = 0                                            # (no gradient comes from behind)
+    idx = spk.sparsek_block_select(q, k, top)
+    v[:, :, real:] = behind(kind, g, (1, Hkv, n - real, d)).bfloat16().cuda()
+    if kind in ("large", "any"):                                   # (products with the largest numbers are infinite, and NaN in a sum)
+        k[:, :, real:] = behind("large", g, (1, Hkv, n - real, d)).bfloat16().cuda()
+    return q, k, v, dO, idx, lambda x: x[:, :, :real].contiguous()
+
+
+@pytest.mark.parametrize("kind,d,real", PADDED)
+def test_what_lies_behind_a_padded_sequence_reaches_nobody(kind, d, real):
+    """Keys and values behind a sequence's end, in its last block and in further ones: what is ahead of them has the results of the
+    sequence alone."""
+    require_gpu()
+    say("block attention, behind a padded sequence", kind, d, real)
+    q, k, v, _, idx, cut = padded(kind, d, real)
+    o, lse = spk.sparsek_block_attn_fwd(q, k, v, idx, 0.125)
+    torch.cuda.synchronize()
+    ro, rl, _, ob, lb = ref.attn(cut(q), cut(k), cut(v), cut(idx), 0.125)
+    within(cut(o), ro, ob, "o")
+    within(cut(lse), rl, lb, "lse")
+
+
+@pytest.mark.parametrize("spread", [20, 40, 80])
+@pytest.mark.parametrize("d", [64, 128])
+def test_tokens_of_all_sizes_in_one_block(spread, d):
+    """Values whose tokens differ by up to 2^spread: every row is right relative to what it attends.  The queries look at single tokens,
+    so that the small ones' rows are small."""
+    require_gpu()
+    say("block attention, values of 2^%d" % spread, d)
+    n, top = 330, 2
+    g = torch.Generator().manual_seed(spread)
+    k, v = torch.randn(1, 1, n, d, generator=g), torch.randn(1, 1, n, d, generator=g)
+    target = (torch.arange(n) - torch.randint(0, 40, (n,), generator=g)).clamp(min=0)
+    target = torch.maximum(target, torch.arange(n) // 64 * 64)      # (in the own block)
+    q = (k / k.norm(dim=3, keepdim=True))[:, :, target].expand(1, 2, n, d) * 400
+    v = v * torch.exp2(torch.randint(-spread // 2, spread // 2 + 1, (1, 1, n, 1), generator=g).float())
+    q, k, v = (x.bfloat16().contiguous().cuda() for x in (q, k, v))
+    idx = spk.sparsek_block_select(q, k, top)
+    o, lse = spk.sparsek_block_attn_fwd(q, k, v, idx, 0.5)
+    torch.cuda.synchronize()
+    ro, rl, _, _, _ = ref.attn(q, k, v, idx, 0.5)
+    see = ref.seen(idx[0, 0].cpu().numpy(), n)
+    K, V = ref.f64(k[0, 0]), ref.f64(v[0, 0])
+    for h in range(2):
+        x = (ref.f64(q[0, h]) @ K.T * 0.5).masked_fill(~see, -math.inf)
+        p = torch.softmax(x, 1)
+        # outputs and weights rounded, a partial result relative to its row's largest, and logits up to 2^13 off by 2^-23 of their products
+        e = 2 ** -23 * 2 * (ref.f64(q[0, h]).abs() @ K.abs().T * 0.5).amax(1, keepdim=True) * 1.5
+        bound = (2 ** -8 + 2 ** -11) * ro[0, h].abs() + (2 ** -11 + 2 ** -14 + e) * (p @ V.abs()) + 2 ** -22 * (p @ V.abs()).amax(1, keepdim=True)
+        within(o[0, h], ro[0, h], bound, "o")
