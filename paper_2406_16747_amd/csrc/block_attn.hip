@@ -630,7 +630,7 @@ __global__ __launch_bounds__(256) void block_join_kernel(BlockFwd f, int rows_pe
         if (p >= 0) {
             const float2 mt = f.meta[rows0 + (size_t)p * G];
             w = __builtin_amdgcn_exp2f(mt.x - ref);
-            ws = w * mt.y;
+            ws = w * (mt.y * 0x1p-7f);   // (up to 65 results: their sum before the division stays in fp32's range whatever the values)
         }
         L += w;
         const int count = min(LPR, l.slots - s0);
@@ -654,7 +654,7 @@ __global__ __launch_bounds__(256) void block_join_kernel(BlockFwd f, int rows_pe
 #pragma unroll
     for (int d = 1; d < LPR; d <<= 1) L += __shfl_xor(L, d, 64);
     if (rr >= nq * G) return;
-    const float inv = 1.0f / L;
+    const float inv = 0x1p7f / L;
     const size_t at = ((size_t)b * l.H + g * G + gh) * l.n + i;
     u32x4 out;
 #pragma unroll

@@ -149,3 +149,20 @@ def test_tokens_of_all_sizes_in_one_block(spread, d):
         e = 2 ** -23 * 2 * (ref.f64(q[0, h]).abs() @ K.abs().T * 0.5).amax(1, keepdim=True) * 1.5
         bound = (2 ** -8 + 2 ** -11) * ro[0, h].abs() + (2 ** -11 + 2 ** -14 + e) * (p @ V.abs()) + 2 ** -22 * (p @ V.abs()).amax(1, keepdim=True)
         within(o[0, h], ro[0, h], bound, "o")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("exponent", [127, 100, -100, -120])
+def test_values_at_both_ends_of_the_range(exponent, d):
+    """A weighted mean of numbers is never larger than they are, up to the largest and down to the smallest ones with all their bits."""
+    require_gpu()
+    say("block attention, values of 2^%d" % exponent, d)
+    n, top = 700, 6
+    q, k, v, _ = draw(97, 1, 2, 1, n, d, qk=0.5)
+    v = (torch.sign(v.float()) * (1 + 0.99 * torch.rand(v.shape, generator=torch.Generator().manual_seed(1)).cuda()) * 2.0 ** exponent).bfloat16()
+    v[:, :, :400] = v[:, :, :400].abs()
+    idx = spk.sparsek_block_select(q, k, top)
+    o, lse = spk.sparsek_block_attn_fwd(q, k, v, idx, 0.125)
+    torch.cuda.synchronize()
+    ro, _, _, ob, _ = ref.attn(q, k, v, idx, 0.125)
+    within(o, ro, ob, "o")
