@@ -17,7 +17,7 @@ namespace spk {
 struct BlockBwd {
     BlockArgs a;
     uint16_t *dq, *dk, *dv;
-    float4* rows;       // [B,H,n]: lse * log2(e), dO.o, the sum of |dO|
+    float2* rows;       // [B,H,n]: lse * log2(e), dO.o
     _Float16* part;     // partial dq: [B,Hkv][entry rows][D]
     float2* meta;       // what the halves of each half of D stand for
     float* kvpart;      // [B,Hkv][units][2 halves of the keys][dV, dK][D / 32][4][64 lanes][4]
@@ -30,22 +30,18 @@ __global__ __launch_bounds__(256) void block_delta_kernel(BlockBwd f, size_t nro
     constexpr int LPR = D / 8;
     const size_t row = (blockIdx.x * (size_t)256 + threadIdx.x) / LPR;
     const int c = threadIdx.x % LPR;
-    float s = 0.0f, abs = 0.0f;
+    float s = 0.0f;
     if (row < nrows) {
         const u32x4 x = *(const u32x4*)(f.a.o + row * D + 8 * c), y = *(const u32x4*)(f.a.dO + row * D + 8 * c);
 #pragma unroll
         for (int e = 0; e < 4; e++) {
             s = fmaf(__uint_as_float(x[e] << 16), __uint_as_float(y[e] << 16), s);
             s = fmaf(__uint_as_float(x[e] & 0xFFFF0000u), __uint_as_float(y[e] & 0xFFFF0000u), s);
-            abs += fabsf(__uint_as_float(y[e] << 16)) + fabsf(__uint_as_float(y[e] & 0xFFFF0000u));
         }
     }
 #pragma unroll
-    for (int d = 1; d < LPR; d <<= 1) {
-        s += __shfl_xor(s, d, 64);
-        abs += __shfl_xor(abs, d, 64);
-    }
-    if (row < nrows && c == 0) f.rows[row] = make_float4(f.a.lse[row] * 1.4426950408889634f, s, abs, 0.0f);
+    for (int d = 1; d < LPR; d <<= 1) s += __shfl_xor(s, d, 64);
+    if (row < nrows && c == 0) f.rows[row] = make_float2(f.a.lse[row] * 1.4426950408889634f, s);
 }
 
 template <int D>
@@ -54,12 +50,10 @@ struct BwdBlockSmem {
     unsigned char ds[RowTile<64>::BYTES];   // [key][row]
     struct Rows {                           // of one tile
         float lse2[BT], delta[BT];
-        float down[BT], up[BT];             // to and from the row's dS in fp16
         int limit[BT];                      // keys 0 .. limit are attended; BT more: one of the block's own rows that is not finite
         int at[BT];                         // the row's place in [G,n]
-        unsigned bad[2];                    // rows whose lse, o or dO is not finite, as bits
+        unsigned bad[2];                    // rows whose lse or dO.o is not finite, as bits
     } rows[2];                              // the tile in use and the next one
-    unsigned red[8];
 };
 static_assert(sizeof(BwdBlockSmem<128>) <= 80 * 1024, "two workgroups per CU");
 
@@ -80,10 +74,13 @@ __device__ __forceinline__ void issue_query_rows(BwdBlockSmem<D>& sm, const type
 }
 
 // 64 rows against 64 keys.  Wave (kb = wv & 1, rb = wv >> 1): keys 32 kb .. and rows 32 rb .. of S and dP; its share of dV^T and
-// dK^T (those keys, those rows) joins acc_v, acc_k; dS goes to LDS.
+// dK^T (those keys, those rows) joins acc_v, acc_k.  Score gradients cancel in their sums (a row's add up to 0), so dS keeps more than bf16's
+// 2^-8: it is the sum of two bf16 numbers (2^-16, and of any size, as the keys and values of a block may be: fp16 relative to a bound of the
+// row's goes by values that the row may not attend, and takes as long, 4 x 16 heads of 8192 1953 us against 1942).  The first is in LDS then,
+// the second in dl.
 template <int D>
 __device__ __forceinline__ void bwd_block_tile(BwdBlockSmem<D>& sm, const typename BwdBlockSmem<D>::Rows& rows, int lane, int wv, bool own, float c2,
-                                               f32x16 (&acc_v)[D / 32], f32x16 (&acc_k)[D / 32])
+                                               f32x16 (&acc_v)[D / 32], f32x16 (&acc_k)[D / 32], bf16x8 (&dl)[2])
 {
     using S = RowTile<D>;
     constexpr int DS = D / 16, DB = D / 32;
@@ -104,31 +101,28 @@ __device__ __forceinline__ void bwd_block_tile(BwdBlockSmem<D>& sm, const typena
 #pragma unroll
             for (int e = 0; e < 4; e++) {
                 const float x = ll[e] < BT ? s[4 * g4 + e] : __uint_as_float(0x7FC00000u);
-                s[4 * g4 + e] = 32 * kb + col > (ll[e] & BT - 1) ? -INFINITY : x;
+                const bool behind = 32 * kb + col > (ll[e] & BT - 1);
+                s[4 * g4 + e] = behind ? -INFINITY : x;
+                dp[4 * g4 + e] = behind ? 0.0f : dp[4 * g4 + e];   // (infinite, perhaps: values that the row does not attend)
             }
         }
-    // As operands: weights in bf16 (2^-8), for dV.  Score gradients cancel in their sums (a row's add up to 0), so they keep more: the sum
-    // of two bf16 numbers for dK (two products; the error of dK falls from 1.5 times that of its own rounding to 1.1, for 2 % of a
-    // training step), and for dQ fp16 (2^-11), relative to a bound of the row's (|dO.v| is at most the sum of |dO| times the largest
-    // |v|), with the keys turned to fp16 as they are read (from 1.65 to 1.2, for 2.5 %).
-    bf16x8 pb[2], db[2], dl[2];
+    bf16x8 pb[2], db[2];   // (weights in bf16, 2^-8, for dV)
 #pragma unroll
     for (int g4 = 0; g4 < 4; g4++) {
         const int r0 = 32 * rb + 8 * g4 + 4 * half;
-        const float4 L4 = *(const float4*)&rows.lse2[r0], D4 = *(const float4*)&rows.delta[r0], F4 = *(const float4*)&rows.down[r0];
-        const float ll[4] = {L4.x, L4.y, L4.z, L4.w}, dd[4] = {D4.x, D4.y, D4.z, D4.w}, ff[4] = {F4.x, F4.y, F4.z, F4.w};
-        f16x4 half4;
+        const float4 L4 = *(const float4*)&rows.lse2[r0], D4 = *(const float4*)&rows.delta[r0];
+        const float ll[4] = {L4.x, L4.y, L4.z, L4.w}, dd[4] = {D4.x, D4.y, D4.z, D4.w};
+        bf16x4 first;
 #pragma unroll
         for (int e = 0; e < 4; e++) {
             const int r = 4 * g4 + e;
             const float p = __builtin_amdgcn_exp2f(fmaf(s[r], c2, -ll[e]));
             const float ds = p * (dp[r] - dd[e]);
             pb[r >> 3][r & 7] = (__bf16)p;
-            db[r >> 3][r & 7] = (__bf16)ds;
-            dl[r >> 3][r & 7] = (__bf16)(ds - (float)db[r >> 3][r & 7]);
-            half4[e] = (_Float16)(ds * ff[e]);
+            db[r >> 3][r & 7] = first[e] = (__bf16)ds;
+            dl[r >> 3][r & 7] = (__bf16)(ds - (float)first[e]);
         }
-        *(f16x4*)(sm.ds + RowTile<64>::offset(32 * kb + col) + 2 * r0) = half4;
+        *(bf16x4*)(sm.ds + RowTile<64>::offset(32 * kb + col) + 2 * r0) = first;
     }
     const uint32_t tq = lds_address(sm.q) + transposed_lane<D>(lane) + 2 * rb * S::R16, tg = lds_address(sm.g) + transposed_lane<D>(lane) + 2 * rb * S::R16;
 #pragma unroll
@@ -142,35 +136,35 @@ __device__ __forceinline__ void bwd_block_tile(BwdBlockSmem<D>& sm, const typena
         }
 }
 
-// 8 bf16 values times f, in fp16 (f brings them into its range: nothing is lost above 2^-27 of the block's largest).
-__device__ __forceinline__ f16x8 to_half(bf16x8 x, float f)
-{
-    const u32x4 w = __builtin_bit_cast(u32x4, x);
-    f16x8 y;
-#pragma unroll
-    for (int e = 0; e < 4; e++) {
-        y[2 * e] = (_Float16)(__uint_as_float(w[e] << 16) * f);
-        y[2 * e + 1] = (_Float16)(__uint_as_float(w[e] & 0xFFFF0000u) * f);
-    }
-    return y;
-}
-
-// dQ^T of rows 32 rb .. and the D/2 columns of half kb, from the dS in LDS.  kdown: what brings the block's keys into fp16's range (they
-// are exact there); scale: what undoes it and the column's own factor, and the softmax scale.
+// dQ^T of rows 32 rb .. and the D/2 columns of half kb: the two numbers of dS pass through LDS one after the other (two barriers).
 template <int D>
-__device__ __forceinline__ void bwd_block_dq(BwdBlockSmem<D>& sm, int lane, int wv, float kdown, float scale, f32x16 (&acc_q)[D / 64])
+__device__ __forceinline__ void bwd_block_dq(BwdBlockSmem<D>& sm, int lane, int wv, float scale, const bf16x8 (&dl)[2], f32x16 (&acc_q)[D / 64])
 {
     constexpr int DB = D / 32;
-    const int kb = wv & 1, rb = wv >> 1;
+    const int kb = wv & 1, rb = wv >> 1, col = lane & 31, half = lane >> 5;
     const uint32_t tk = lds_address(sm.k) + transposed_lane<D>(lane) + 64 * (DB / 2) * kb, td = lds_address(sm.ds) + transposed_lane<64>(lane) + 64 * rb;
 #pragma unroll
     for (int x = 0; x < DB / 2; x++) acc_q[x] = f32x16{0};
+#pragma unroll 1
+    for (int part = 0; part < 2; part++) {
+        if (part) {
+            __syncthreads();   // the first numbers have been read
 #pragma unroll
-    for (int g = 0; g < 4; g++) {
-        const f16x8 d8 = __builtin_bit_cast(f16x8, transposed_operand<64>(td + g * RowTile<64>::R16));
+            for (int g4 = 0; g4 < 4; g4++) {
+                bf16x4 w;
 #pragma unroll
-        for (int x = 0; x < DB / 2; x++)
-            acc_q[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(to_half(transposed_operand<D>(tk + g * RowTile<D>::R16 + 64 * x), kdown), d8, acc_q[x], 0, 0, 0);
+                for (int e = 0; e < 4; e++) w[e] = dl[g4 >> 1][4 * (g4 & 1) + e];
+                *(bf16x4*)(sm.ds + RowTile<64>::offset(32 * kb + col) + 2 * (32 * rb + 8 * g4 + 4 * half)) = w;
+            }
+            __syncthreads();
+        }
+#pragma unroll
+        for (int g = 0; g < 4; g++) {
+            const bf16x8 d8 = transposed_operand<64>(td + g * RowTile<64>::R16);
+#pragma unroll
+            for (int x = 0; x < DB / 2; x++)
+                acc_q[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_operand<D>(tk + g * RowTile<D>::R16 + 64 * x), d8, acc_q[x], 0, 0, 0);
+        }
     }
 #pragma unroll
     for (int x = 0; x < DB / 2; x++)
@@ -239,30 +233,26 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void block_bwd_tiles_kernel(
     const size_t kv = ((size_t)bg * l.n + (size_t)j * BT) * D;
     const int last = l.n - 1 - j * BT;
     // (rows that attend a key which is not finite have an lse or an o that is not, and the others must not see it)
-    unsigned unused = 0, topk = load_rows<D>(sm.k, f.a.k + kv, last, tid, unused), topv = load_rows<D>(sm.v, f.a.v + kv, last, tid, unused);
-    block_max_bits2(topk, topv, sm.red, tid);
-    const int Ek = scale_exp(topk);
-    const float kdown = scale_down(Ek), kup = scale_up(Ek), vmax = __uint_as_float(topv);
+    unsigned unused = 0;
+    load_rows<D>(sm.k, f.a.k + kv, last, tid, unused);
+    load_rows<D>(sm.v, f.a.v + kv, last, tid, unused);
     const int32_t* list = l.list + (size_t)bg * l.entries + base;
     const size_t row0 = ((size_t)bg * l.entries + base) * G, head0 = (size_t)b * l.H + g * G;
     const uint16_t *q0 = f.a.q + head0 * l.n * D, *g0 = f.a.dO + head0 * l.n * D;
-    const float4* meta_in = f.rows + head0 * l.n;
+    const float2* meta_in = f.rows + head0 * l.n;
     const int own_end = min(BT, last + 1) * G, kb = wv & 1, rt = 32 * (wv >> 1) + col;
     // A tile's rows are on their way while the dQ of the tile before is formed; what is known of them (by the first wave, a row to a
     // lane) two tiles ahead (the query) and one (its logarithm and dO.o).
     auto entry = [&](int r) { return list[min(r, end - 1) / G]; };
     auto place = [&](int r, int i) { return min(r, end - 1) % G * l.n + i; };
-    auto put = [&](typename BwdBlockSmem<D>::Rows& rows, int r, int i, float4 m) {
-        const bool bad = r < end && !(fabsf(m.x) < INFINITY && fabsf(m.y) < INFINITY && m.z < INFINITY);
+    auto put = [&](typename BwdBlockSmem<D>::Rows& rows, int r, int i, float2 m) {
+        const bool bad = r < end && !(fabsf(m.x) < INFINITY && fabsf(m.y) < INFINITY);   // (a dO that is not finite leaves no dO.o finite)
         const unsigned long long all = __ballot(bad);
         if (lane < 2) rows.bad[lane] = (unsigned)(all >> (32 * lane));
         // such a row: weights of NaN for the keys that it attends (all of a selected block, in the own block by `limit`), q and dO of 0
-        if (bad) m = make_float4(r < own_end ? 0.0f : __uint_as_float(0x7FC00000u), 0.0f, 0.0f, 0.0f);
+        if (bad) m = make_float2(r < own_end ? 0.0f : __uint_as_float(0x7FC00000u), 0.0f);
         rows.lse2[lane] = r < end ? m.x : INFINITY;   // (a row that does not exist: p = 0)
         rows.delta[lane] = r < end ? m.y : 0.0f;
-        const int E = scale_exp(__float_as_uint(fmaf(m.z, vmax, fabsf(m.y))));
-        rows.down[lane] = scale_down(E);
-        rows.up[lane] = scale_up(E) * f.a.scale;
         rows.limit[lane] = min(BT - 1, i - j * BT) + (bad && r < own_end ? BT : 0);
         rows.at[lane] = place(r, i);
     };
@@ -294,13 +284,14 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void block_bwd_tiles_kernel(
             }
             __syncthreads();
         }
-        float4 m = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        float2 m = make_float2(0.0f, 0.0f);
         int i_then = 0;
         if (wv == 0) {
             m = meta_in[place(r0 + BT + lane, i_next)];
             i_then = entry(r0 + 2 * BT + lane);
         }
-        bwd_block_tile<D>(sm, sm.rows[buf], lane, wv, r0 < own_end, f.a.c2, acc_v, acc_k);
+        bf16x8 dl[2];
+        bwd_block_tile<D>(sm, sm.rows[buf], lane, wv, r0 < own_end, f.a.c2, acc_v, acc_k, dl);
         if (wv == 0) {
             put(sm.rows[buf ^ 1], r0 + BT + lane, i_next, m);
             i_next = i_then;
@@ -310,7 +301,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void block_bwd_tiles_kernel(
         bad0 = sm.rows[buf ^ 1].bad[0];
         bad1 = sm.rows[buf ^ 1].bad[1];
         f32x16 acc_q[DB / 2];
-        bwd_block_dq<D>(sm, lane, wv, kdown, sm.rows[buf].up[rt] * kup, acc_q);
+        bwd_block_dq<D>(sm, lane, wv, f.a.scale, dl, acc_q);
         // the partial dq of rows 32 rb + col, columns of half kb, relative to the largest of them
         float top = 0.0f;
 #pragma unroll
@@ -445,7 +436,7 @@ static BwdLayout bwd_layout(const sparsek_block_cfg& c, void* ws)
     f.y = block_lists_layout(c, block_count(c.n) * BT, bwd_unit(c), ws);
     const size_t BG = (size_t)c.B * c.Hkv, rows = BG * f.y.l.entries * f.y.l.G;
     f.rows = f.y.bytes;
-    f.part = align_up(f.rows + (size_t)c.B * c.H * c.n * 16, 256);
+    f.part = align_up(f.rows + (size_t)c.B * c.H * c.n * 8, 256);
     f.meta = align_up(f.part + rows * c.d * 2, 256);
     f.kvpart = align_up(f.meta + rows * 8, 256);
     f.bytes = align_up(f.kvpart + BG * f.y.l.maxu * (size_t)BT * c.d * 8, 256);
@@ -465,7 +456,7 @@ int launch_block_bwd(const sparsek_block_cfg& c, const void* q, const void* k, c
     f.a.scale = c.softmax_scale;
     f.a.c2 = c.softmax_scale * 1.4426950408889634f;
     f.dq = (uint16_t*)dq; f.dk = (uint16_t*)dk; f.dv = (uint16_t*)dv;
-    f.rows = (float4*)((char*)ws + y.rows);
+    f.rows = (float2*)((char*)ws + y.rows);
     f.part = (_Float16*)((char*)ws + y.part); f.meta = (float2*)((char*)ws + y.meta); f.kvpart = (float*)((char*)ws + y.kvpart);
     const BlockLists& l = f.a.l;
     const int BG = c.B * c.Hkv;

@@ -166,3 +166,42 @@ def test_values_at_both_ends_of_the_range(exponent, d):
     torch.cuda.synchronize()
     ro, _, _, ob, _ = ref.attn(q, k, v, idx, 0.125)
     within(o, ro, ob, "o")
+
+
+@pytest.mark.parametrize("kind,d,real", PADDED)
+def test_gradients_of_a_padded_sequence(kind, d, real):
+    """The gradients of the sequence alone, whatever keys and values lie behind it."""
+    require_gpu()
+    say("block attention backward, behind a padded sequence", kind, d, real)
+    q, k, v, dO, idx, cut = padded(kind, d, real)
+    o, lse = spk.sparsek_block_attn_fwd(q, k, v, idx, 0.125)
+    got = spk.sparsek_block_attn_bwd(q, k, v, idx, o, lse, dO, 0.125)
+    torch.cuda.synchronize()
+    want, bound = ref.attn_bwd(*[cut(x) for x in (q, k, v, idx, o, lse, dO)], 0.125)
+    for name, x, y, z in zip(("dq", "dk", "dv"), got, want, bound):
+        # (ds is off by p times what o's rounding and lse's error make of delta: both are the same on both sides, and part of the bound)
+        within(cut(x), y, z, name)
+
+
+@pytest.mark.parametrize("which", ["k", "v"])
+@pytest.mark.parametrize("spread", [20, 40, 80])
+@pytest.mark.parametrize("d", [64, 128])
+def test_gradients_of_tokens_of_all_sizes_in_one_block(spread, d, which):
+    """Keys or values whose tokens differ by up to 2^spread, in a block's own rows: a row's dq is right relative to what it attends.  Sizes
+    grow along a block, so that its first rows see the small ones only."""
+    require_gpu()
+    say("block attention backward, %s of 2^%d" % (which, spread), d)
+    n = 192
+    q, k, v, dO = draw(spread, 1, 2, 1, n, d)
+    size = torch.exp2((torch.arange(n) % 64 * spread // 63 - spread).float()).view(1, 1, n, 1).cuda()
+    if which == "k":
+        k = (k.float() * size).bfloat16()
+    else:
+        v = (v.float() * size).bfloat16()
+    idx = torch.full((1, 1, n, 1), -1, dtype=torch.int32).cuda()
+    o, lse = spk.sparsek_block_attn_fwd(q, k, v, idx, 0.125)
+    got = spk.sparsek_block_attn_bwd(q, k, v, idx, o, lse, dO, 0.125)
+    torch.cuda.synchronize()
+    want, bound = ref.attn_bwd(q, k, v, idx, o, lse, dO, 0.125)
+    for name, x, y, z in zip(("dq", "dk", "dv"), got, want, bound):
+        within(x, y, z, name)
