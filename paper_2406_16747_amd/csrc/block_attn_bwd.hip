@@ -74,7 +74,8 @@ __device__ __forceinline__ void issue_query_rows(BwdBlockSmem<D>& sm, const type
 }
 
 // 64 rows against 64 keys.  Wave (kb = wv & 1, rb = wv >> 1): keys 32 kb .. and rows 32 rb .. of S and dP; its share of dV^T and
-// dK^T (those keys, those rows) joins acc_v, acc_k.  Score gradients cancel in their sums (a row's add up to 0), so dS keeps more than bf16's
+// dK^T (those keys, those rows) joins acc_v, acc_k.  Weights are the sum of two bf16 numbers (2^-16): as one, 2^-8, they leave dV 1.4 times the
+// error of its own rounding (two products a pair of 16 rows and 32 columns; 3 % of a training step).  Score gradients cancel in their sums (a row's add up to 0), so dS keeps more than bf16's
 // 2^-8: it is the sum of two bf16 numbers (2^-16, and of any size, as the keys and values of a block may be: fp16 relative to a bound of the
 // row's goes by values that the row may not attend, and takes as long, 4 x 16 heads of 8192 1953 us against 1942).  The first is in LDS then,
 // the second in dl.
@@ -106,7 +107,7 @@ __device__ __forceinline__ void bwd_block_tile(BwdBlockSmem<D>& sm, const typena
                 dp[4 * g4 + e] = behind ? 0.0f : dp[4 * g4 + e];   // (infinite, perhaps: values that the row does not attend)
             }
         }
-    bf16x8 pb[2], db[2];   // (weights in bf16, 2^-8, for dV)
+    bf16x8 pb[2], pl[2], db[2];
 #pragma unroll
     for (int g4 = 0; g4 < 4; g4++) {
         const int r0 = 32 * rb + 8 * g4 + 4 * half;
@@ -119,6 +120,7 @@ __device__ __forceinline__ void bwd_block_tile(BwdBlockSmem<D>& sm, const typena
             const float p = __builtin_amdgcn_exp2f(fmaf(s[r], c2, -ll[e]));
             const float ds = p * (dp[r] - dd[e]);
             pb[r >> 3][r & 7] = (__bf16)p;
+            pl[r >> 3][r & 7] = (__bf16)(p - (float)pb[r >> 3][r & 7]);
             db[r >> 3][r & 7] = first[e] = (__bf16)ds;
             dl[r >> 3][r & 7] = (__bf16)(ds - (float)first[e]);
         }
@@ -129,7 +131,9 @@ __device__ __forceinline__ void bwd_block_tile(BwdBlockSmem<D>& sm, const typena
     for (int g = 0; g < 2; g++)
 #pragma unroll
         for (int x = 0; x < DB; x++) {
-            acc_v[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_operand<D>(tg + g * S::R16 + 64 * x), pb[g], acc_v[x], 0, 0, 0);
+            const bf16x8 gt = transposed_operand<D>(tg + g * S::R16 + 64 * x);
+            acc_v[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(gt, pb[g], acc_v[x], 0, 0, 0);
+            acc_v[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(gt, pl[g], acc_v[x], 0, 0, 0);
             const bf16x8 qt = transposed_operand<D>(tq + g * S::R16 + 64 * x);
             acc_k[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qt, db[g], acc_k[x], 0, 0, 0);
             acc_k[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qt, dl[g], acc_k[x], 0, 0, 0);

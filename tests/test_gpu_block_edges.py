@@ -205,3 +205,22 @@ def test_gradients_of_tokens_of_all_sizes_in_one_block(spread, d, which):
     want, bound = ref.attn_bwd(q, k, v, idx, o, lse, dO, 0.125)
     for name, x, y, z in zip(("dq", "dk", "dv"), got, want, bound):
         within(x, y, z, name)
+
+
+@pytest.mark.parametrize("shape", [(1, 4, 2, 700, 64, 3), (1, 6, 2, 500, 128, 2), (2, 2, 2, 333, 128, 1)])
+def test_dv_is_rounded_once(shape):
+    """dv is off by its own rounding to bf16 (2^-8), weights as two bf16 numbers (2^-16) and fp32 sums and exponentials (2^-14, logits below
+    2^5): beyond that rounding by a 16th of what weights in bf16 would leave."""
+    require_gpu()
+    say("block attention, dv", shape)
+    B, H, Hkv, n, d, top = shape
+    q, k, v, dO = draw(101, B, H, Hkv, n, d)
+    scale = 1 / math.sqrt(d)
+    idx = spk.sparsek_block_select(q, k, top)
+    ro, rl = ref.attn(q, k, v, idx, scale)[:2]
+    o, lse = ro.bfloat16().cuda(), rl.float().cuda()
+    dv = spk.sparsek_block_attn_bwd(q, k, v, idx, o, lse, dO, scale)[2]
+    torch.cuda.synchronize()
+    (_, _, want), _ = ref.attn_bwd(q, k, v, idx, o, lse, dO, scale)
+    size = ref.attn_bwd(q, k, v, idx, o, lse, dO.abs(), scale)[0][2]       # p^T |dO|
+    within(dv, want, 2 ** -8 * want.abs() + (2 ** -16 + 2 ** -14) * size, "dv")
