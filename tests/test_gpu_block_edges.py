@@ -224,3 +224,60 @@ def test_dv_is_rounded_once(shape):
     (_, _, want), _ = ref.attn_bwd(q, k, v, idx, o, lse, dO, scale)
     size = ref.attn_bwd(q, k, v, idx, o, lse, dO.abs(), scale)[0][2]       # p^T |dO|
     within(dv, want, 2 ** -8 * want.abs() + (2 ** -16 + 2 ** -14) * size, "dv")
+
+
+def check_blocks(q, k, v, dO, idx, o, lse, dk, dv, scale, g, blocks):
+    """dk and dv of single blocks of long input, from all the rows that attend them, for the o and lse that the backward was given."""
+    n, G = q.shape[2], q.shape[1] // k.shape[1]
+    sel, i = idx[0, g].cpu(), torch.arange(n)
+    for j in blocks:
+        K, V = ref.f64(k[0, g, 64 * j:64 * j + 64]), ref.f64(v[0, g, 64 * j:64 * j + 64])
+        rows = i[((sel == j).any(1) & (i // 64 > j)) | (i // 64 == j)]
+        see = (64 * j + torch.arange(len(K))).view(1, -1) <= rows.view(-1, 1)
+        wk, wv, bk, bv = (torch.zeros_like(K) for _ in range(4))
+        for h in range(g * G, (g + 1) * G):
+            Q, D, O = (ref.f64(x[0, h])[rows] for x in (q, dO, o))
+            p = torch.exp((Q @ K.T * scale).masked_fill(~see, -math.inf) - ref.f64(lse[0, h])[rows].view(-1, 1))
+            ds = p * (D @ V.T - (D * O).sum(1, keepdim=True)) * scale
+            e = 2 ** -14 * ds.abs() + 2 ** -17 * p * (D.abs() @ V.abs().T + (D * O).abs().sum(1, keepdim=True)) * scale   # (as ref.attn_bwd)
+            wv += p.T @ D
+            wk += ds.T @ Q
+            bv += (2 ** -16 + 2 ** -14) * p.T @ D.abs()
+            bk += (e + 2 ** -16 * ds.abs()).T @ Q.abs()
+        at = slice(64 * j, 64 * j + len(K))
+        within(dv[0, g, at], wv, 2 ** -8 * wv.abs() + bv + 1e-30, "dv of block %d, %d rows" % (j, G * len(rows)))
+        within(dk[0, g, at], wk, 2 ** -8 * wk.abs() + bk + 1e-30, "dk of block %d, %d rows" % (j, G * len(rows)))
+
+
+@pytest.mark.parametrize("H,Hkv,n,d,top", [(8, 2, 10007, 128, 6), (4, 2, 9001, 64, 8), (6, 2, 5003, 128, 9), (4, 1, 30000, 128, 16)])
+def test_gradients_of_keys_at_the_sizes_of_training(H, Hkv, n, d, top):
+    """More blocks and pairs than one launch of the lists takes, units of 2048 and 1024 rows, blocks of one unit and of many (one that
+    everybody selects), the first, the last and ragged one, and blocks in every stride of the join."""
+    require_gpu()
+    say("block attention, gradients of keys", H, Hkv, n, d, top)
+    q, k, v, dO = draw(111, 1, H, Hkv, n, d)
+    scale = 1 / math.sqrt(d)
+    idx = spk.sparsek_block_select(q, k, top)
+    idx[:, 0, :, 0] = 1                                  # (in any order, perhaps twice: it counts once)
+    idx[:, -1, ::3, 1] = 17
+    o, lse = spk.sparsek_block_attn_fwd(q, k, v, idx, scale)
+    dq, dk, dv = spk.sparsek_block_attn_bwd(q, k, v, idx, o, lse, dO, scale)
+    torch.cuda.synchronize()
+    nb = -(-n // 64)
+    for g in range(Hkv):
+        check_blocks(q, k, v, dO, idx, o, lse, dk, dv, scale, g, [0, 1, 2, 15, 16, 17, 18, nb // 3, nb // 2, nb - 17, nb - 2, nb - 1])
+
+
+def test_gradients_of_keys_of_several_passes_of_the_lists():
+    """More than 4096 blocks."""
+    require_gpu()
+    say("block attention, gradients of keys, 300000 tokens")
+    n, d, top = 300000, 64, 2
+    g = torch.Generator(device="cuda").manual_seed(9)
+    q, k, v, dO = (torch.randn(1, 1, n, d, device="cuda", generator=g).bfloat16() for _ in range(4))
+    idx = torch.randint(-1, n // 64, (1, 1, n, top), device="cuda", generator=g, dtype=torch.int32)
+    idx[:, :, ::2, 0] = 4200
+    o, lse = spk.sparsek_block_attn_fwd(q, k, v, idx, 0.125)
+    dq, dk, dv = spk.sparsek_block_attn_bwd(q, k, v, idx, o, lse, dO, 0.125)
+    torch.cuda.synchronize()
+    check_blocks(q, k, v, dO, idx, o, lse, dk, dv, 0.125, 0, [0, 1, 4095, 4096, 4100, 4199, 4200, 4201, n // 64 - 1, n // 64])
