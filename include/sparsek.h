@@ -328,9 +328,10 @@ int sparsek_block_attn_bwd(const sparsek_block_cfg *cfg, const void *q, const vo
  *     (the one that token lens - 1 lies in) with the largest scores, as sparsek_block_select.
  * attn:  o out [B,H,d], lse out [B,H] fp32: the query attends all tokens (idx NULL), or its own block and the whole blocks of idx
  *     [B,Hkv,top] (places in the table; places of no whole block behind its own, and repeated ones, are left out).  A sequence without
- *     tokens gets o = 0 and lse = -inf, a query that is not finite NaN for both.  accumulate != 0: the weights are added to mass.
+ *     tokens gets o = 0 and lse = -inf, a query that is not finite NaN for both.  accumulate != 0: the weights are added to mass
+ *     (those of a query whose result is NaN are NaN for all blocks that it attends; one whose logits are all -inf has none).
  * evict: sequences with more than `budget` whole blocks keep the first `sink`, the last `recent` and of the others those with the largest
- *     mass (of equal ones the older), `budget` in all, by age.  table_out and mass_out [B,Hkv,cap], lens_out [B] out: the kept pages
+ *     mass (of equal ones the older; NaN counts as the largest), `budget` in all, by age.  table_out and mass_out [B,Hkv,cap], lens_out [B] out: the kept pages
  *     first, then those that went (free for new blocks), then the rest; masses move along, the unfinished block's with it, what lies
  *     behind becomes 0.  The outputs must not overlap the inputs (INVALID_ARG).
  * SPARSEK_BF16, d = 64 or 128, Hkv dividing H, cap <= 8192, pages <= 2^24 (UNSUPPORTED otherwise).  k8, v8, km, kt, vt, k, v, q, o and ws

@@ -788,7 +788,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void cache8_attn_kernel(Attn
             float den = 0.0f;
 #pragma unroll
             for (int w = 0; w < 4; w++) den += sm_[w][h] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm_[w][h] - M) * sl[w][h];
-            if (shares[tid][h] > -INFINITY) sum += __builtin_amdgcn_exp2f(shares[tid][h] - (M + log2f(den * 0x1p-15f)));
+            if (shares[tid][h] != -INFINITY) sum += __builtin_amdgcn_exp2f(shares[tid][h] - (M + log2f(den * 0x1p-15f)));
         }
         add_mass(a, ru, bg, tid, sum);
     }
@@ -887,7 +887,7 @@ __global__ __launch_bounds__(256) void cache8_join_kernel(AttnArgs a, int mass_w
         __syncthreads();
 #pragma unroll
         for (int x = 0; x < 4; x++)
-            if (w[x] > -INFINITY) sum += __builtin_amdgcn_exp2f(w[x] - logs[x]);
+            if (w[x] != -INFINITY) sum += __builtin_amdgcn_exp2f(w[x] - logs[x]);
         __syncthreads();
     }
     if (u < nu) add_mass(a, ru, bg, u, sum);
@@ -916,7 +916,7 @@ __global__ __launch_bounds__(256) void cache8_evict_kernel(CacheArgs a, int budg
     }
 #pragma unroll 8
     for (int x = tid; x < nb; x += 256) {
-        const float m = mass_in[x];
+        const float m = fabsf(mass_in[x]) <= INFINITY ? mass_in[x] : __uint_as_float(0x7FC00000u);   // (a NaN of either sign: the largest)
         keys[x] = x < sink || x >= nb - recent ? 0xFFFFFFFFu : min(max(score_key(m), 1u), 0xFFFFFFFEu);
     }
     __syncthreads();

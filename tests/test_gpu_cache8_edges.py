@@ -181,3 +181,31 @@ def test_logits_of_all_sizes(e, sign, cap, n):
     else:
         assert ((ref.f64(o) - ro).abs() <= ob + 2 ** -22 * 2 ** e * ro.abs().amax()).all()
     assert ((lse.cpu().double() - rl).abs() <= 2 ** -21 * rl.abs() + 2 ** -20).all()
+
+
+@pytest.mark.parametrize("cap", [6, 40])
+@pytest.mark.parametrize("who", ["query", "block"])
+def test_weights_that_are_nan_are_the_masses_of_all_that_is_attended(who, cap):
+    """A query that is NaN, or a block that makes it so: every block that it attends has a mass of NaN, the spoiled one too, and no other;
+    eviction keeps the older of those, whatever the NaN's sign."""
+    require_gpu()
+    say("cache attention, masses of NaN", who, cap)
+    H, n = 2, 300
+    g = gen(65)
+    k, v, q = rand(g, 2, 1, n, 64), rand(g, 2, 1, n, 64), rand(g, 2, H, 64)
+    if who == "block":
+        k[0, 0, 70, 3] = float("nan")
+    else:
+        q[0, 1, 3] = float("nan")
+    cache, L = filled(k, v, H, cap, torch.int8)
+    idx = torch.tensor([1, 3], dtype=torch.int32).cuda().expand(2, 1, 2).contiguous()
+    spk.sparsek_cache8_attn(cache, L, q, idx, accumulate=True)
+    torch.cuda.synchronize()
+    bad = torch.isnan(cache.mass[0, 0, :5])
+    assert bad.tolist() == [False, True, False, True, True] and (cache.mass[0, 0, [0, 2]] == 0).all()
+    assert torch.isfinite(cache.mass[1]).all() and float(cache.mass[1].sum()) > H - 1e-3
+    cache.mass[0, 0, :4] = torch.tensor([float("inf"), -float("nan"), 7.0, float("nan")])
+    cache.mass[0, 0, 1] = -cache.mass[0, 0, 3].abs()
+    out = spk.sparsek_cache8_evict(cache, L, 2, 0, 0)
+    torch.cuda.synchronize()
+    assert out["table"][0, 0, :4].tolist() == [int(cache.table[0, 0, x]) for x in (1, 3, 0, 2)]
