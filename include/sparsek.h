@@ -282,7 +282,10 @@ int sparsek_chunk_status(const sparsek_chunk_cfg *cfg, const void *state, int32_
  * The backward takes the forward's o and lse and gives the gradients of L = sum(dO * o) with the selection held fixed.
  * A query that attends a key which is not finite, or whose values are not, gets NaN, and so does its lse where the key or the query is
  * not; nobody else does.  Likewise backward: NaN for the keys that a row attends whose q, lse, o or dO is not finite, and for no other.
- * SPARSEK_BF16, d = 64 or 128, Hkv dividing H, n <= 2^20, top <= 64 (UNSUPPORTED otherwise); idx may be NULL where top == 0.
+ * Finite keys and values that a query does not attend have no part in its results, whatever their size.
+ * SPARSEK_BF16, d = 64 or 128, Hkv dividing H, B H <= 65535, n <= 2^20, n H / Hkv <= 2^28, top <= 64 (UNSUPPORTED otherwise); idx may be
+ * NULL where top == 0.  The forward's workspace holds 8 GB of partial results at most, the backward's 2 B H n (top + 1) d bytes of them; both
+ * 5 bytes for every pair of a block and a chunk of 64 queries of each key/value head.
  * q, k, v, o, dO, dq, dk, dv and ws begin at multiples of 16 bytes (INVALID_ARG otherwise); outputs overlap no inputs.
  * Results do not depend on timing: no sum's order is left to atomics. */
 #define SPARSEK_BLOCK_TOKENS 64
@@ -334,7 +337,9 @@ int sparsek_block_attn_bwd(const sparsek_block_cfg *cfg, const void *q, const vo
  *     mass (of equal ones the older; NaN counts as the largest), `budget` in all, by age.  table_out and mass_out [B,Hkv,cap], lens_out [B] out: the kept pages
  *     first, then those that went (free for new blocks), then the rest; masses move along, the unfinished block's with it, what lies
  *     behind becomes 0.  The outputs must not overlap the inputs (INVALID_ARG).
- * SPARSEK_BF16, d = 64 or 128, Hkv dividing H, cap <= 8192, pages <= 2^24 (UNSUPPORTED otherwise).  k8, v8, km, kt, vt, k, v, q, o and ws
+ * Values beyond 2^90 may give an infinite o.
+ * SPARSEK_BF16, d = 64 or 128, Hkv dividing H, B H <= 65535, cap <= 8192, top <= 8192 (of select: 1 at least), pages <= 2^24 (UNSUPPORTED
+ * otherwise).  k8, v8, km, kt, vt, k, v, q, o and ws
  * begin at multiples of 16 bytes (INVALID_ARG otherwise).  Calls on one cache must be ordered. */
 #define SPARSEK_I8 2
 #define SPARSEK_E4M3 3

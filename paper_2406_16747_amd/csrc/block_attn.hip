@@ -5,9 +5,10 @@
 // walks the queries that attend it, 32 rows (query, head of the group) to a wave: S^T = K.Q^T, the softmax of these 64 keys alone,
 // O^T = V^T.P^T, and leaves the normalised partial result, with the log of its denominator, in list order.  block_join_kernel adds up
 // the partial results of every row with their weights.
-// What bounds it is memory, then the vector ALU: a (row, block) pair moves a row of q in and D halves out and in again, for 4*64*D
-// flops.  32 heads of 128 (8 of keys), 32768 tokens, 16 blocks: 2580 us, of which the tiles take 1320 to 1350 (4.6 GB written; matrix pipes 22 %,
-// vector ALU 39 %, LDS 33 % of the time; 1150 with the partial results written to one place), the join 920 (4.9 TB/s), the selection 280.
+// A (row, block) pair moves a row of q in and D halves out and in again, for 4*64*D flops.  32 heads of 128 (8 of keys), 32768 tokens,
+// 16 blocks: 2550 to 2600 us, of which the tiles take 1350, the join 925 (4.9 TB/s: memory), the selection 285.  The tiles are bound by issue: matrix
+// pipes, vector ALU and LDS are busy 22, 40 and 33 % of the time and take turns rather than overlap (waves wait to issue half of their
+// cycles, for memory a quarter); with the 4.6 GB of partial results written to one place they took 1150 where 1350 is usual.
 #include "block_parts.hpp"
 
 #include <cmath>

@@ -7,9 +7,9 @@
 // dQ^T = K^T.dS^T, whose partial results go out in list order.  A block whose rows are one unit is finished there; the sums of
 // the others go out and block_kv_join_kernel adds them up.  block_dq_join_kernel adds up the partial dq of every row.
 //
-// The tiles are bound by issue and by waiting: two waves per SIMD (256 registers for d = 128) and five products a pair.  4 x 16 heads of
-// 128, 8192 tokens, 8 blocks: 870 to 1000 us (matrix pipes 26 %, vector ALU 43 %, LDS 28 % of the time); dO.o 53 us (5.1 TB/s), the join
-// of dq 279 (4.7 TB/s).
+// The tiles are bound by issue and by waiting: two waves per SIMD (256 registers for d = 128) and five products a pair, three of them in two
+// parts.  4 x 16 heads of 128, 8192 tokens, 8 blocks: 930 to 1000 us (matrix pipes 34 %, vector ALU 37 %, LDS 31 % of the time); dO.o 53 us
+// (5.1 TB/s), the join of dq 277 (4.7 TB/s).
 #include "block_parts.hpp"
 
 namespace spk {
