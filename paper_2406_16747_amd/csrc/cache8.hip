@@ -511,8 +511,8 @@ __device__ __forceinline__ float soft_unit(const f32x4m (&s)[4], SoftRow& row, f
 }
 
 // The largest logit of keys that were attended but have none above -inf: they are infinite themselves, or their query is, or their scale
-// is NaN.  Below every logit, and still not the -inf of no keys at all: what remains of such a row alone is 0 / 0.
-constexpr float NO_LOGIT = -3.0e38f;
+// is NaN.  No finite logit is below it, and still it is not the -inf of no keys at all: what remains of such a row alone is 0 / 0.
+constexpr float NO_LOGIT = -__FLT_MAX__;
 __device__ __forceinline__ float log_of(float top, float sum)   // a row's lse; sum: times 2^15
 {
     if (top == -INFINITY) return -INFINITY;

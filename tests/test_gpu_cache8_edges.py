@@ -209,3 +209,20 @@ def test_weights_that_are_nan_are_the_masses_of_all_that_is_attended(who, cap):
     out = spk.sparsek_cache8_evict(cache, L, 2, 0, 0)
     torch.cuda.synchronize()
     assert out["table"][0, 0, :4].tolist() == [int(cache.table[0, 0, x]) for x in (1, 3, 0, 2)]
+
+
+@pytest.mark.parametrize("cap", [4, 40])
+def test_the_lowest_finite_logits_are_above_minus_infinity(cap):
+    """Logits just above the lowest number, beside a last token of -inf: the weights are theirs."""
+    require_gpu()
+    say("cache attention, the lowest logits", cap)
+    g = gen(75)
+    k, v = torch.full((1, 1, 129, 64), -1.0).bfloat16().cuda(), rand(g, 1, 1, 129, 64)
+    k[:, :, 128, 5] = float("-inf")
+    q = torch.ones(1, 2, 64).bfloat16().cuda()
+    cache, L = filled(k, v, 2, cap, torch.int8, scale=3.35e38 / (64 * 1.4427))
+    o, lse = spk.sparsek_cache8_attn(cache, L, q)
+    torch.cuda.synchronize()
+    want = ref.row_tokens(cache, [128], 0, 0)[1].mean(0)
+    assert ((ref.f64(o[0]) - want).abs() <= 2 ** -8 * want.abs() + 2 ** -11).all()
+    assert ((lse.cpu().double() + 3.35e38 / 1.4427).abs() <= 2 ** -20 * 3.35e38).all()
