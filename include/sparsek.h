@@ -278,7 +278,7 @@ int sparsek_chunk_status(const sparsek_chunk_cfg *cfg, const void *state, int32_
  *
  * q, o, dO, dq in/out [B,H,n,d], k, v, dk, dv [B,Hkv,n,d] of `dtype`, lse [B,H,n] fp32 (natural logarithm), all contiguous.
  * mass out [B,Hkv,ceil(n/64)] fp32, may be NULL: the attention weight that each block's keys got from all queries and heads of the group,
- * added up (what sparsek_cache8_evict goes by).
+ * added up (what sparsek_cache8_evict goes by); NaN where one of the queries has an lse of NaN.
  * The backward takes the forward's o and lse and gives the gradients of L = sum(dO * o) with the selection held fixed.
  * A query that attends a key which is not finite, or whose values are not, gets NaN, and so does its lse where the key or the query is
  * not; nobody else does.  Likewise backward: NaN for the keys that a row attends whose q, lse, o or dO is not finite, and for no other.
