@@ -74,11 +74,10 @@ __device__ __forceinline__ void issue_query_rows(BwdBlockSmem<D>& sm, const type
 }
 
 // 64 rows against 64 keys.  Wave (kb = wv & 1, rb = wv >> 1): keys 32 kb .. and rows 32 rb .. of S and dP; its share of dV^T and
-// dK^T (those keys, those rows) joins acc_v, acc_k.  Weights are the sum of two bf16 numbers (2^-16): as one, 2^-8, they leave dV 1.4 times the
-// error of its own rounding (two products a pair of 16 rows and 32 columns; 3 % of a training step).  Score gradients cancel in their sums (a row's add up to 0), so dS keeps more than bf16's
-// 2^-8: it is the sum of two bf16 numbers (2^-16, and of any size, as the keys and values of a block may be: fp16 relative to a bound of the
-// row's goes by values that the row may not attend, and takes as long, 4 x 16 heads of 8192 1953 us against 1942).  The first is in LDS then,
-// the second in dl.
+// dK^T (those keys, those rows) joins acc_v, acc_k.  Weights are the sum of two bf16 numbers (2^-16): as one, 2^-8, they leave dV 1.4 times
+// the error of its own rounding (for 3 % of a training step).  Score gradients cancel in their sums (a row's add up to 0), so dS is two
+// bf16 numbers too, and of any size, as the keys and values of a block may be: fp16 relative to a bound of the row's goes by values that
+// the row may not attend, and takes as long (4 x 16 heads of 8192 1953 us against 1942).  The first is in LDS then, the second in dl.
 template <int D>
 __device__ __forceinline__ void bwd_block_tile(BwdBlockSmem<D>& sm, const typename BwdBlockSmem<D>::Rows& rows, int lane, int wv, bool own, float c2,
                                                f32x16 (&acc_v)[D / 32], f32x16 (&acc_k)[D / 32], bf16x8 (&dl)[2])
