@@ -370,6 +370,40 @@ int sparsek_cache8_attn(const sparsek_cache8_cfg *cfg, const sparsek_cache8 *cac
 int sparsek_cache8_evict(const sparsek_cache8_cfg *cfg, const sparsek_cache8 *cache, const int32_t *lens, int32_t budget,
                          int32_t sink, int32_t recent, int32_t *table_out, float *mass_out, int32_t *lens_out, void *stream);
 
+/* ---- norms of queries and keys for each head, with the rotation by position in the same pass ----
+ * What stands between a layer's projections and its attention: x [B,n,heads,d] in any strides (slices of a fused projection) goes to
+ * [B,heads,n,d] contiguous.  For every head of every token, of q and of k (Hkv = 0: no k, whose arguments may be NULL):
+ *     norm != 0:  y = x r w,  r = 1 / sqrt(mean(x^2) + eps);  w = qw or kw [d] fp32, the same for all heads, NULL: ones
+ *     norm == 0:  y = x
+ *     pair p of rot/2:  (y1, y2) -> (y1 cos a - y2 sin a, y2 cos a + y1 sin a),  a = pos[axis[p]][b][t] * freq[p]
+ *     interleaved == 0: y1, y2 are channels p and p + rot/2;  != 0: channels 2p and 2p + 1;  channels from rot on do not turn.
+ * pos [axes,B,n] int32 (axes: one, or time, height and width); freq [rot/2] fp32 (radians per position: any ladder and scaling); axis
+ * [rot/2] int32, which position turns the pair (values outside 0 .. axes-1 count as the nearest), NULL: 0.  pos, freq may be NULL where rot == 0.
+ * Angles are made in 64 bits, sums in fp32; the outputs are rounded once.  Squares that pass fp32's range overflow (values beyond 2^60).
+ * bwd: for L = sum(dqo * qo) + sum(dko * ko), dqo, dko contiguous as qo, ko: dq, dk in the strides cfg->dq, cfg->dk (places of one tensor must not
+ * coincide: INVALID_ARG), and dqw, dkw [d] fp32, NULL: not wanted (norm == 0: they must be NULL).  q and k are not read where norm == 0 and may be NULL.
+ * The sums behind dqw and dkw have an order of their own that does not depend on timing.
+ * SPARSEK_BF16 or SPARSEK_F32; d a multiple of 8, 8 .. 256; rot a multiple of 8, 0 .. d; axes 1 .. 4; H + Hkv <= 65535, B n < 2^31 (UNSUPPORTED
+ * otherwise).  Strides are in elements, not negative, multiples of 4, and the last row begins below 2^46; tensors and ws begin at multiples of 16 bytes; outputs overlap no
+ * inputs (INVALID_ARG otherwise). */
+typedef struct {
+    int64_t batch, token, head;   /* elements between neighbours; channels are contiguous */
+} sparsek_rope_strides;
+typedef struct {
+    int32_t B, H, Hkv, n, d;
+    int32_t rot, axes, interleaved, norm;
+    int32_t dtype;                /* of q, k, qo, ko and their gradients */
+    float eps;                    /* finite and > 0 where norm != 0 */
+    sparsek_rope_strides q, k;
+    sparsek_rope_strides dq, dk;  /* of the backward's outputs (not read by the forward) */
+} sparsek_rope_cfg;
+int sparsek_rope_fwd(const sparsek_rope_cfg *cfg, const void *q, const void *k, const int32_t *pos, const float *freq, const int32_t *axis,
+                     const float *qw, const float *kw, void *qo, void *ko, void *stream);
+size_t sparsek_rope_bwd_workspace_bytes(const sparsek_rope_cfg *cfg);
+int sparsek_rope_bwd(const sparsek_rope_cfg *cfg, const void *q, const void *k, const int32_t *pos, const float *freq, const int32_t *axis,
+                     const float *qw, const float *kw, const void *dqo, const void *dko, void *dq, void *dk, float *dqw, float *dkw,
+                     void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -40,6 +40,15 @@ class SparsekCache8Cfg(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("B", "H", "Hkv", "d", "cap", "pages", "format", "dtype")] + [("softmax_scale", C.c_float)]
 
 
+class SparsekRopeStrides(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("batch", "token", "head")]
+
+
+class SparsekRopeCfg(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("B", "H", "Hkv", "n", "d", "rot", "axes", "interleaved", "norm", "dtype")] + [
+        ("eps", C.c_float)] + [(n, SparsekRopeStrides) for n in ("q", "k", "dq", "dk")]
+
+
 _CACHE8_TENSORS = ("k8", "v8", "ks", "vs", "km", "kms", "kt", "vt", "table", "mass")
 
 
@@ -127,6 +136,12 @@ def lib():
         for name in ("sparsek_block_select", "sparsek_block_attn_fwd", "sparsek_block_attn_bwd", "sparsek_cache8_append",
                      "sparsek_cache8_select", "sparsek_cache8_attn", "sparsek_cache8_evict"):
             getattr(L, name).restype = C.c_int
+        rcfgp = C.POINTER(SparsekRopeCfg)
+        L.sparsek_rope_bwd_workspace_bytes.restype = sz
+        L.sparsek_rope_bwd_workspace_bytes.argtypes = [rcfgp]
+        L.sparsek_rope_fwd.argtypes = [rcfgp] + [vp] * 9 + [vp]
+        L.sparsek_rope_bwd.argtypes = [rcfgp] + [vp] * 13 + [vp, sz, vp]
+        L.sparsek_rope_fwd.restype = L.sparsek_rope_bwd.restype = C.c_int
         _lib = L
     return _lib
 
@@ -707,3 +722,95 @@ def sparsek_cache8_evict(cache, lens, budget, sink=1, recent=1, out=None):
     _on(cache.device, lib().sparsek_cache8_evict, cache.ref, cache.cref, lens.data_ptr(), int(budget), int(sink), int(recent),
         table.data_ptr(), mass.data_ptr(), after.data_ptr())
     return out
+
+
+# ---- norms of queries and keys with rotary positions ----
+
+def _make_rope_cfg(B, H, Hkv, n, d, rot, axes, interleaved, norm, dtype, eps, q, k, dq, dk):
+    return SparsekRopeCfg(B=B, H=H, Hkv=Hkv, n=n, d=d, rot=rot, axes=axes, interleaved=interleaved, norm=norm, dtype=dtype, eps=eps,
+                          **{name: SparsekRopeStrides(*s) for name, s in (("q", q), ("k", k), ("dq", dq), ("dk", dk))})
+
+
+def _heads_of(name, t, dtype, shape, device):
+    """The strides of batch, token and head of a tensor [B,n,heads,d] whose channels are contiguous (those of one place count as 0)."""
+    if t.dtype is not dtype or t.shape != shape or t.device != device:
+        raise ValueError("%s must be a %s tensor of shape %s on %s, got %s %s on %s" % (
+            name, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
+    if t.stride(3) != 1:
+        raise ValueError("the channels of %s must be contiguous" % name)
+    return tuple(t.stride(x) if t.shape[x] > 1 else 0 for x in range(3))
+
+
+def _rope_kept(q, k, pos, freq, axis, interleaved, norm, qw, kw, eps, grads=None):
+    torch = _torch()
+    if q.dim() != 4 or (k is not None and k.dim() != 4):
+        raise ValueError("q is [B,n,H,d] and k is [B,n,Hkv,d]")
+    B, n, H, d = q.shape
+    Hkv, dev = k.shape[2] if k is not None else 0, q.device
+    dtype = _dtype_code(q)
+    strides = [_heads_of("q", q, q.dtype, (B, n, H, d), dev), _heads_of("k", k, q.dtype, (B, n, Hkv, d), dev) if k is not None else (0, 0, 0)]
+    rot, axes = 2 * freq.shape[0] if freq is not None else 0, 1
+    if rot:
+        if pos is None or pos.dim() != 3:
+            raise ValueError("pos is [axes,B,n]")
+        axes = pos.shape[0]
+        _same("pos", pos, torch.int32, (axes, B, n), dev)
+        _same("freq", freq, torch.float32, (rot // 2,), dev)
+        if axis is not None:
+            _same("axis", axis, torch.int32, (rot // 2,), dev)
+    for name, w in (("qw", qw), ("kw", kw)):
+        if w is not None:
+            if not norm:
+                raise ValueError("%s without norm" % name)
+            _same(name, w, torch.float32, (d,), dev)
+    for name, t in (("dq", grads[0]), ("dk", grads[1])) if grads else ():
+        heads = H if name == "dq" else Hkv
+        strides.append(_heads_of(name, t, q.dtype, (B, n, heads, d), dev) if t is not None else (0, 0, 0))
+    strides += [(0, 0, 0)] * (4 - len(strides))
+    return _kept("rope", (B, H, Hkv, n, d, rot, axes, int(bool(interleaved)), int(bool(norm)), dtype, float(eps), *strides), _make_rope_cfg)
+
+
+def sparsek_rope_fwd(q, k, pos, freq, axis=None, interleaved=False, norm=False, qw=None, kw=None, eps=1e-6, out=None):
+    """Queries q [B,n,H,d] and keys k [B,n,Hkv,d] (any strides of batch, token and head; k None: queries alone) with each head's norm, if
+    norm, weighted by qw, kw [d] fp32, if given, and turned by their positions: pair p by pos[axis[p]] * freq[p] (pos [axes,B,n] int32, freq
+    [rot/2] fp32 or None, axis [rot/2] int32, None: the first).  Returns qo [B,H,n,d] and ko [B,Hkv,n,d] (None without k), new or those of `out`."""
+    torch = _torch()
+    cfg = _rope_kept(q, k, pos, freq, axis, interleaved, norm, qw, kw, eps)
+    B, n, H, d = q.shape
+    if out is None:
+        qo = torch.empty(B, H, n, d, dtype=q.dtype, device=q.device)
+        ko = torch.empty(B, k.shape[2], n, d, dtype=q.dtype, device=q.device) if k is not None else None
+    else:
+        qo, ko = out
+        _same("out q", qo, q.dtype, (B, H, n, d), q.device)
+        if k is not None:
+            _same("out k", ko, q.dtype, (B, k.shape[2], n, d), q.device)
+    _on(q.device, lib().sparsek_rope_fwd, cfg[0], q.data_ptr(), _ptr(k), _ptr(pos), _ptr(freq), _ptr(axis), _ptr(qw), _ptr(kw), qo.data_ptr(),
+        _ptr(ko) if k is not None else None)
+    return qo, ko
+
+
+def sparsek_rope_bwd(q, k, pos, freq, dqo, dko, axis=None, interleaved=False, norm=False, qw=None, kw=None, eps=1e-6, out=None, ws=None):
+    """dq [B,n,H,d], dk [B,n,Hkv,d], dqw, dkw [d] fp32 (None where there is no such weight): gradients of sum(dqo*qo) + sum(dko*ko) for the
+    outputs of sparsek_rope_fwd on the same arguments.  out: (dq, dk) to write to, in any strides (slices of a fused gradient)."""
+    torch = _torch()
+    B, n, H, d = q.shape
+    if out is None:
+        out = (torch.empty(q.shape, dtype=q.dtype, device=q.device), torch.empty(k.shape, dtype=q.dtype, device=q.device) if k is not None else None)
+    dq, dk = out
+    if (dk is None) != (k is None) or (dko is None) != (k is None):
+        raise ValueError("k, dko and dk go together")
+    cfg = _rope_kept(q, k, pos, freq, axis, interleaved, norm, qw, kw, eps, grads=(dq, dk))
+    _same("dqo", dqo, q.dtype, (B, H, n, d), q.device)
+    if k is not None:
+        _same("dko", dko, q.dtype, (B, k.shape[2], n, d), q.device)
+    dqw = torch.empty_like(qw) if qw is not None else None
+    dkw = torch.empty_like(kw) if kw is not None and k is not None else None
+    nbytes = 0
+    if dqw is not None or dkw is not None:
+        ws, nbytes = _block_ws(cfg, "sparsek_rope_bwd_workspace_bytes", ws, q.device)
+    else:
+        ws = None
+    _on(q.device, lib().sparsek_rope_bwd, cfg[0], q.data_ptr(), _ptr(k), _ptr(pos), _ptr(freq), _ptr(axis), _ptr(qw), _ptr(kw), dqo.data_ptr(),
+        _ptr(dko), dq.data_ptr(), _ptr(dk), _ptr(dqw), _ptr(dkw), _ptr(ws), nbytes)
+    return dq, dk, dqw, dkw

@@ -3,6 +3,7 @@
 #include "mask_ranges.hpp"
 
 #include <initializer_list>
+#include <utility>
 
 using namespace spk;
 
@@ -593,6 +594,118 @@ int sparsek_cache8_evict(const sparsek_cache8_cfg* cfg, const sparsek_cache8* ca
             if (x < y && overlap(out[x], nin[x], out[y], nin[y])) return SPARSEK_ERR_INVALID_ARG;
         }
     return spk::launch_cache8_evict(*cfg, *cache, lens, budget, sink, recent, table_out, mass_out, lens_out, (hipStream_t)stream);
+}
+
+}  // extern "C"
+
+// ---- norms of queries and keys with rotary positions (rope.hip) ----
+namespace spk {
+int launch_rope_fwd(const sparsek_rope_cfg& c, const void* q, const void* k, const int32_t* pos, const float* freq, const int32_t* axis,
+                    const float* qw, const float* kw, void* qo, void* ko, hipStream_t st);
+size_t rope_bwd_ws_bytes(const sparsek_rope_cfg& c);
+int launch_rope_bwd(const sparsek_rope_cfg& c, const void* q, const void* k, const int32_t* pos, const float* freq, const int32_t* axis,
+                    const float* qw, const float* kw, const void* dqo, const void* dko, void* dq, void* dk, float* dqw, float* dkw, void* ws,
+                    hipStream_t st);
+}  // namespace spk
+
+namespace {
+
+// Strides that the kernels can take: rows begin at multiples of 4 elements, and the last one below 2^46 of them.
+bool good(const sparsek_rope_cfg& c, const sparsek_rope_strides& s, int heads)
+{
+    for (int64_t x : {s.batch, s.token, s.head})
+        if (x < 0 || x > (1ll << 45) || x % 4) return false;
+    return (double)(c.B - 1) * s.batch + (double)(c.n - 1) * s.token + (double)(heads - 1) * s.head < 0x1p46;
+}
+
+// What a strided [B,n,heads,d] spans, in bytes.
+size_t span(const sparsek_rope_cfg& c, const sparsek_rope_strides& s, int heads)
+{
+    const int64_t last = (c.B - 1) * s.batch + (c.n - 1) * s.token + (heads - 1) * s.head + c.d;
+    return (size_t)last * (c.dtype == SPARSEK_BF16 ? 2 : 4);
+}
+
+// Whether every place of a strided output has an address of its own: each stride steps over all that the smaller ones reach.
+bool apart(const sparsek_rope_cfg& c, const sparsek_rope_strides& s, int heads)
+{
+    std::pair<int64_t, int64_t> dims[3] = {{s.batch, c.B}, {s.token, c.n}, {s.head, heads}};
+    std::sort(dims, dims + 3);
+    int64_t reach = c.d;
+    for (const auto& x : dims) {
+        if (x.second == 1) continue;
+        if (x.first < reach) return false;
+        reach += (x.second - 1) * x.first;
+    }
+    return true;
+}
+
+int check_rope(const sparsek_rope_cfg* c)
+{
+    if (!c || c->B < 1 || c->H < 1 || c->Hkv < 0 || c->n < 1 || c->d < 1 || c->rot < 0 || c->rot > c->d || c->axes < 1) return SPARSEK_ERR_INVALID_ARG;
+    if (c->norm && (!(c->eps > 0.0f) || !(c->eps < INFINITY))) return SPARSEK_ERR_INVALID_ARG;
+    if (c->dtype != SPARSEK_BF16 && c->dtype != SPARSEK_F32) return SPARSEK_ERR_UNSUPPORTED;
+    if (c->d % 8 || c->d > 256 || c->rot % 8 || c->axes > 4) return SPARSEK_ERR_UNSUPPORTED;
+    if ((long long)c->H + c->Hkv > 65535 || (long long)c->B * c->n >= (1ll << 31)) return SPARSEK_ERR_UNSUPPORTED;
+    if (!good(*c, c->q, c->H) || (c->Hkv && !good(*c, c->k, c->Hkv))) return SPARSEK_ERR_INVALID_ARG;
+    return SPARSEK_OK;
+}
+
+// Arguments that both directions share.  (x_read: q and k are read.)
+int check_rope_inputs(const sparsek_rope_cfg& c, bool x_read, const void* q, const void* k, const int32_t* pos, const float* freq)
+{
+    if (x_read && (!q || (c.Hkv && !k))) return SPARSEK_ERR_INVALID_ARG;
+    if (c.rot && (!pos || !freq)) return SPARSEK_ERR_INVALID_ARG;
+    return aligned({q, k}) ? SPARSEK_OK : SPARSEK_ERR_INVALID_ARG;
+}
+
+}  // namespace
+
+extern "C" {
+
+int sparsek_rope_fwd(const sparsek_rope_cfg* cfg, const void* q, const void* k, const int32_t* pos, const float* freq, const int32_t* axis,
+                     const float* qw, const float* kw, void* qo, void* ko, void* stream)
+{
+    int rc = check_rope(cfg);
+    if (rc) return rc;
+    const sparsek_rope_cfg& c = *cfg;
+    if ((rc = check_rope_inputs(c, true, q, k, pos, freq))) return rc;
+    if (!qo || (c.Hkv && !ko) || !aligned({qo, ko})) return SPARSEK_ERR_INVALID_ARG;
+    const size_t row = (size_t)c.B * c.n * c.d * (c.dtype == SPARSEK_BF16 ? 2 : 4), nq = span(c, c.q, c.H), nqo = row * c.H, nko = row * c.Hkv;
+    if (overlap(q, nq, qo, nqo)) return SPARSEK_ERR_INVALID_ARG;
+    if (c.Hkv) {
+        const size_t nk = span(c, c.k, c.Hkv);
+        if (overlap(q, nq, ko, nko) || overlap(k, nk, qo, nqo) || overlap(k, nk, ko, nko) || overlap(qo, nqo, ko, nko)) return SPARSEK_ERR_INVALID_ARG;
+    }
+    return spk::launch_rope_fwd(c, q, k, pos, freq, axis, qw, kw, qo, ko, (hipStream_t)stream);
+}
+
+size_t sparsek_rope_bwd_workspace_bytes(const sparsek_rope_cfg* cfg)
+{
+    if (check_rope(cfg)) return 0;
+    return spk::rope_bwd_ws_bytes(*cfg);
+}
+
+int sparsek_rope_bwd(const sparsek_rope_cfg* cfg, const void* q, const void* k, const int32_t* pos, const float* freq, const int32_t* axis,
+                     const float* qw, const float* kw, const void* dqo, const void* dko, void* dq, void* dk, float* dqw, float* dkw,
+                     void* ws, size_t ws_bytes, void* stream)
+{
+    int rc = check_rope(cfg);
+    if (rc) return rc;
+    const sparsek_rope_cfg& c = *cfg;
+    if ((rc = check_rope_inputs(c, c.norm, q, k, pos, freq))) return rc;
+    if (!dqo || !dq || (c.Hkv && (!dko || !dk)) || !aligned({dqo, dko, dq, dk, ws})) return SPARSEK_ERR_INVALID_ARG;
+    if ((dqw && !c.norm) || (dkw && (!c.norm || !c.Hkv)) || ((dqw || dkw) && !ws)) return SPARSEK_ERR_INVALID_ARG;
+    if (!good(c, c.dq, c.H) || !apart(c, c.dq, c.H) || (c.Hkv && (!good(c, c.dk, c.Hkv) || !apart(c, c.dk, c.Hkv)))) return SPARSEK_ERR_INVALID_ARG;
+    const size_t row = (size_t)c.B * c.n * c.d * (c.dtype == SPARSEK_BF16 ? 2 : 4);
+    const void* in[] = {c.norm ? q : nullptr, dqo, c.norm && c.Hkv ? k : nullptr, c.Hkv ? dko : nullptr};
+    const size_t nin[] = {span(c, c.q, c.H), row * c.H, c.Hkv ? span(c, c.k, c.Hkv) : 0, row * c.Hkv};
+    for (int x = 0; x < 4; x++) {
+        if (!in[x]) continue;
+        if (overlap(in[x], nin[x], dq, span(c, c.dq, c.H))) return SPARSEK_ERR_INVALID_ARG;
+        if (c.Hkv && overlap(in[x], nin[x], dk, span(c, c.dk, c.Hkv))) return SPARSEK_ERR_INVALID_ARG;
+    }
+    if ((dqw || dkw) && ws_bytes < spk::rope_bwd_ws_bytes(c)) return SPARSEK_ERR_WORKSPACE;
+    return spk::launch_rope_bwd(c, q, k, pos, freq, axis, qw, kw, dqo, dko, dq, dk, dqw, dkw, ws, (hipStream_t)stream);
 }
 
 }  // extern "C"
