@@ -345,7 +345,7 @@ int sparsek_block_attn_bwd(const sparsek_block_cfg *cfg, const void *q, const vo
 #define SPARSEK_E4M3 3
 typedef struct {
     int32_t B, H, Hkv, d, cap, pages;
-    int32_t format;        /* of the codes: SPARSEK_I8 or SPARSEK_E4M3 */
+    int32_t format;        /* of the codes: SPARSEK_I8 or SPARSEK_E4M3 (sparsek_cache4: SPARSEK_E2M1) */
     int32_t dtype;         /* of q, k, v, o and the unfinished blocks: SPARSEK_BF16 */
     float softmax_scale;   /* finite and > 0 */
 } sparsek_cache8_cfg;
@@ -368,6 +368,47 @@ int sparsek_cache8_attn(const sparsek_cache8_cfg *cfg, const sparsek_cache8 *cac
                         const int32_t *idx, int32_t top, int32_t accumulate, void *o, float *lse, void *ws, size_t ws_bytes,
                         void *stream);
 int sparsek_cache8_evict(const sparsek_cache8_cfg *cfg, const sparsek_cache8 *cache, const int32_t *lens, int32_t budget,
+                         int32_t sink, int32_t recent, int32_t *table_out, float *mass_out, int32_t *lens_out, void *stream);
+
+/* ---- the same cache in 4 bits ----
+ * As sparsek_cache8, with a code of 4 bits for a value and a power of two for 32 of them: of keys 32 channels of a token (channels 32 j ..), of
+ * values 32 tokens of a channel (the block's tokens 32 j ..).  A value is e2m1(code) * 2^(e-127): the magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6 for
+ * the codes 0 .. 7, negative with 8 added.  With max the group's largest |x|: e - 127 is the smallest whole number with max <= 6 * 2^(e-127), at
+ * most 125; a code is x / 2^(e-127) rounded to the nearest (halfway: to the even code), 6 at most; a group with max < 2^-100 is held as zeros with e = 0.
+ *     k4, v4 [pages,32 d] uint8   codes, two to a byte, the first in the low half.  With token s = 16 a + 4 t + r and channel c of the block
+ *                                 a key lies at [t][g][a][r][i] (g = c / (d/4), i = c % (d/4); d = 64: [t / 2][g][a][r][t % 2][i]), a value at
+ *                                 [c / 32][a][c % 16][c / 16 % 2][s % 16]
+ *     ke, ve [pages,2 d] uint8    e: of keys at [j][a][r][t], of values at [j][c % 16][c / 16]
+ *     ks, vs [pages] fp32         the page's largest 2^(e-127), times 1.5 where another that is not 0 lies more than 2^36 below it; 0: all zeros;
+ *                                 NaN: it holds a value that is not finite, and NaN is what a query gets that attends it
+ * The other tensors, lens, and what holds of pages are those of sparsek_cache8, and so are append, select, attn and evict; cfg.format is
+ * SPARSEK_E2M1.
+ * read: k, v [B,Hkv,n,d] out of `dtype`: tokens begin .. begin+n-1 of every sequence as they are attended (the unfinished block's as they were
+ *     given), NaN for all of a page that holds one which is not finite; zeros behind a sequence's end and for blocks whose page is outside the pool.
+ * begin >= 0, n >= 1 (INVALID_ARG), begin + n <= 2^28 (UNSUPPORTED).  k4, v4, ke, ve, km, kt, vt and all tensors of q, k, v, o and ws begin at multiples of 16
+ * bytes; outputs overlap no inputs. */
+#define SPARSEK_E2M1 4
+typedef struct {
+    void *k4, *v4;
+    uint8_t *ke, *ve;
+    float *ks, *vs;
+    int8_t *km;
+    float *kms;
+    void *kt, *vt;
+    int32_t *table;
+    float *mass;
+} sparsek_cache4;
+int sparsek_cache4_append(const sparsek_cache8_cfg *cfg, const sparsek_cache4 *cache, const int32_t *lens, const int32_t *counts,
+                          int32_t c, const void *k, const void *v, void *stream);
+int sparsek_cache4_read(const sparsek_cache8_cfg *cfg, const sparsek_cache4 *cache, const int32_t *lens, int32_t begin, int32_t n,
+                        void *k, void *v, void *stream);
+int sparsek_cache4_select(const sparsek_cache8_cfg *cfg, const sparsek_cache4 *cache, const int32_t *lens, const void *q, int32_t top,
+                          int32_t *idx, void *stream);
+size_t sparsek_cache4_attn_workspace_bytes(const sparsek_cache8_cfg *cfg, int32_t top);
+int sparsek_cache4_attn(const sparsek_cache8_cfg *cfg, const sparsek_cache4 *cache, const int32_t *lens, const void *q,
+                        const int32_t *idx, int32_t top, int32_t accumulate, void *o, float *lse, void *ws, size_t ws_bytes,
+                        void *stream);
+int sparsek_cache4_evict(const sparsek_cache8_cfg *cfg, const sparsek_cache4 *cache, const int32_t *lens, int32_t budget,
                          int32_t sink, int32_t recent, int32_t *table_out, float *mass_out, int32_t *lens_out, void *stream);
 
 /* ---- norms of queries and keys for each head, with the rotation by position in the same pass ----

@@ -6,7 +6,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libsparsek.so")
 _lib = None
 
-F32, BF16, I8, E4M3 = 0, 1, 2, 3
+F32, BF16, I8, E4M3, E2M1 = 0, 1, 2, 3, 4
 BLOCK_TOKENS = 64
 
 
@@ -54,6 +54,13 @@ _CACHE8_TENSORS = ("k8", "v8", "ks", "vs", "km", "kms", "kt", "vt", "table", "ma
 
 class SparsekCache8(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in _CACHE8_TENSORS]
+
+
+_CACHE4_TENSORS = ("k4", "v4", "ke", "ve") + _CACHE8_TENSORS[2:]
+
+
+class SparsekCache4(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in _CACHE4_TENSORS]
 
 
 def lib_path():
@@ -124,17 +131,19 @@ def lib():
                      "sparsek_block_attn_bwd_workspace_bytes"):
             getattr(L, name).restype = sz
             getattr(L, name).argtypes = [bcfgp]
-        L.sparsek_cache8_attn_workspace_bytes.restype = sz
-        L.sparsek_cache8_attn_workspace_bytes.argtypes = [c8cfgp, i32]
         L.sparsek_block_select.argtypes = [bcfgp, vp, vp, vp, vp, sz, vp]
         L.sparsek_block_attn_fwd.argtypes = [bcfgp] + [vp] * 7 + [vp, sz, vp]
         L.sparsek_block_attn_bwd.argtypes = [bcfgp] + [vp] * 10 + [vp, sz, vp]
-        L.sparsek_cache8_append.argtypes = [c8cfgp, c8p, vp, vp, i32, vp, vp, vp]
-        L.sparsek_cache8_select.argtypes = [c8cfgp, c8p, vp, vp, i32, vp, vp]
-        L.sparsek_cache8_attn.argtypes = [c8cfgp, c8p, vp, vp, vp, i32, i32, vp, vp, vp, sz, vp]
-        L.sparsek_cache8_evict.argtypes = [c8cfgp, c8p, vp, i32, i32, i32, vp, vp, vp, vp]
-        for name in ("sparsek_block_select", "sparsek_block_attn_fwd", "sparsek_block_attn_bwd", "sparsek_cache8_append",
-                     "sparsek_cache8_select", "sparsek_cache8_attn", "sparsek_cache8_evict"):
+        for cache, cp in (("sparsek_cache8_", c8p), ("sparsek_cache4_", C.POINTER(SparsekCache4))):
+            for name, types in (("append", [vp, vp, i32, vp, vp]), ("select", [vp, vp, i32, vp]), ("evict", [vp, i32, i32, i32, vp, vp, vp]),
+                                ("attn", [vp, vp, vp, i32, i32, vp, vp, vp, sz]), ("read", [vp, i32, i32, vp, vp])):
+                if name == "read" and cp is c8p:
+                    continue
+                getattr(L, cache + name).argtypes = [c8cfgp, cp] + types + [vp]
+                getattr(L, cache + name).restype = C.c_int
+            getattr(L, cache + "attn_workspace_bytes").restype = sz
+            getattr(L, cache + "attn_workspace_bytes").argtypes = [c8cfgp, i32]
+        for name in ("sparsek_block_select", "sparsek_block_attn_fwd", "sparsek_block_attn_bwd"):
             getattr(L, name).restype = C.c_int
         rcfgp = C.POINTER(SparsekRopeCfg)
         L.sparsek_rope_bwd_workspace_bytes.restype = sz
@@ -589,11 +598,61 @@ def sparsek_block_attn_bwd(q, k, v, idx, o, lse, dO, scale, ws=None):
     return dq, dk, dv
 
 
-# ---- a key/value cache in blocks of 64 tokens held in 8 bits ----
+# ---- a key/value cache in blocks of 64 tokens held in 8 bits, or in 4 ----
 
-class Cache8:
+class _Cache:
+    """What both caches are: tensors of the caller's that were checked once, and the addresses that the calls go by."""
+
+    def _keep(self, tensors, H, scale, format, pages, d):
+        B, Hkv, cap = tensors["table"].shape
+        for name in self._names:
+            setattr(self, name, tensors[name])
+        self.B, self.H, self.Hkv, self.d, self.cap, self.device = B, int(H), Hkv, d, cap, tensors["table"].device
+        self.cfg = SparsekCache8Cfg(B=B, H=int(H), Hkv=Hkv, d=d, cap=cap, pages=pages, format=format, dtype=BF16, softmax_scale=float(scale))
+        self.q_shape, self.lens_shape, self.bytes = (B, int(H), d), (B,), {}
+        if not lib().sparsek_cache8_attn_workspace_bytes(self.cfg, 0) and not lib().sparsek_cache4_attn_workspace_bytes(self.cfg, 0):
+            raise ValueError("unsupported cache configuration")
+        self._ref()
+
+    def __setattr__(self, name, value):
+        if name in self._names and hasattr(self, "cref"):   # (the calls go by the addresses taken in the constructor)
+            raise AttributeError("the tensors of a %s stay; adopt() takes another table and masses" % type(self).__name__)
+        object.__setattr__(self, name, value)
+
+    def _ref(self):
+        self.c = self._struct(*(getattr(self, n).data_ptr() for n in self._names))
+        self.ref, self.cref = C.byref(self.cfg), C.byref(self.c)
+
+    def adopt(self, table, mass):
+        """From now on with this table and these masses (those that sparsek_cache8_evict or sparsek_cache4_evict gave)."""
+        _same("table", table, torch.int32, (self.B, self.Hkv, self.cap), self.device)
+        _same("mass", mass, torch.float32, (self.B, self.Hkv, self.cap), self.device)
+        object.__setattr__(self, "table", table)
+        object.__setattr__(self, "mass", mass)
+        self._ref()
+
+
+def _common(B, Hkv, d, cap, pages):
+    """(name, type, shape) of the tensors that both caches have."""
+    return (("ks", torch.float32, (pages,)), ("vs", torch.float32, (pages,)), ("km", torch.int8, (pages, d)), ("kms", torch.float32, (pages,)),
+            ("kt", torch.bfloat16, (B, Hkv, BLOCK_TOKENS, d)), ("vt", torch.bfloat16, (B, Hkv, d, BLOCK_TOKENS)),
+            ("table", torch.int32, (B, Hkv, cap)), ("mass", torch.float32, (B, Hkv, cap)))
+
+
+def _empty_common(B, Hkv, d, cap, pages, device):
+    """Those tensors of a cache without tokens: every row of the table has an equal share of the pages, in order."""
+    got = {name: torch.zeros(*shape, dtype=dtype, device=device) for name, dtype, shape in _common(B, Hkv, d, cap, pages)}
+    # (no page in two places: an append writes whole pages, and two of one page would mix their tokens)
+    share = min(pages // (B * Hkv), cap) if B * Hkv > 0 else 0
+    place, row = torch.arange(cap, device=device), torch.arange(B * Hkv, device=device).view(B, Hkv, 1)
+    got["table"] = torch.where(place < share, row * share + place, -1).to(torch.int32)
+    return got
+
+
+class Cache8(_Cache):
     """The tensors of a cache (see include/sparsek.h), checked once.  The constructor takes the caller's own; Cache8.empty makes
     them: a pool of `pages` pages, of which every row of the table (a sequence's key/value head) has an equal share, in order."""
+    _names, _struct = _CACHE8_TENSORS, SparsekCache8
 
     def __init__(self, k8, v8, ks, vs, km, kms, kt, vt, table, mass, H, scale):
         torch = _torch()
@@ -605,30 +664,10 @@ class Cache8:
         if k8.dtype not in formats:
             raise ValueError("k8 must be int8 or float8_e4m3fn, got %s" % k8.dtype)
         dev = k8.device
-        for name, t, dtype, shape in (
-                ("k8", k8, k8.dtype, (pages, BLOCK_TOKENS, d)), ("v8", v8, k8.dtype, (pages, d, BLOCK_TOKENS)), ("ks", ks, torch.float32, (pages,)),
-                ("vs", vs, torch.float32, (pages,)), ("km", km, torch.int8, (pages, d)), ("kms", kms, torch.float32, (pages,)),
-                ("kt", kt, torch.bfloat16, (B, Hkv, BLOCK_TOKENS, d)), ("vt", vt, torch.bfloat16, (B, Hkv, d, BLOCK_TOKENS)),
-                ("table", table, torch.int32, (B, Hkv, cap)), ("mass", mass, torch.float32, (B, Hkv, cap))):
-            _same(name, t, dtype, shape, dev)
-        self.k8, self.v8, self.ks, self.vs, self.km, self.kms, self.kt, self.vt = k8, v8, ks, vs, km, kms, kt, vt
-        self.table, self.mass = table, mass
-        self.B, self.H, self.Hkv, self.d, self.cap, self.device = B, int(H), Hkv, d, cap, dev
-        self.cfg = SparsekCache8Cfg(B=B, H=int(H), Hkv=Hkv, d=d, cap=cap, pages=pages, format=formats[k8.dtype], dtype=BF16,
-                                    softmax_scale=float(scale))
-        self.q_shape, self.lens_shape, self.bytes = (B, int(H), d), (B,), {}
-        if not lib().sparsek_cache8_attn_workspace_bytes(self.cfg, 0):
-            raise ValueError("unsupported cache configuration")
-        self._ref()
-
-    def __setattr__(self, name, value):
-        if name in _CACHE8_TENSORS and hasattr(self, "cref"):   # (the calls go by the addresses taken in the constructor)
-            raise AttributeError("the tensors of a Cache8 stay; adopt() takes another table and masses")
-        object.__setattr__(self, name, value)
-
-    def _ref(self):
-        self.c = SparsekCache8(*(getattr(self, n).data_ptr() for n in _CACHE8_TENSORS))
-        self.ref, self.cref = C.byref(self.cfg), C.byref(self.c)
+        tensors = dict(k8=k8, v8=v8, ks=ks, vs=vs, km=km, kms=kms, kt=kt, vt=vt, table=table, mass=mass)
+        for name, dtype, shape in (("k8", k8.dtype, (pages, BLOCK_TOKENS, d)), ("v8", k8.dtype, (pages, d, BLOCK_TOKENS))) + _common(B, Hkv, d, cap, pages):
+            _same(name, tensors[name], dtype, shape, dev)
+        self._keep(tensors, H, scale, formats[k8.dtype], pages, d)
 
     @classmethod
     def empty(cls, B, H, Hkv, d, cap, format=None, scale=None, pages=None, device="cuda"):
@@ -638,53 +677,58 @@ class Cache8:
         torch = _torch()
         format = torch.int8 if format is None else format
         pages = B * Hkv * cap if pages is None else int(pages)
-        z = lambda *s, dtype=torch.float32: torch.zeros(*s, dtype=dtype, device=device)  # noqa: E731
-        codes = lambda *s: z(*s, dtype=torch.uint8).view(format)                          # noqa: E731
-        # (no page in two places: an append writes whole pages, and two of one page would mix their tokens)
-        share = min(pages // (B * Hkv), cap) if B * Hkv > 0 else 0
-        place, row = torch.arange(cap, device=device), torch.arange(B * Hkv, device=device).view(B, Hkv, 1)
-        table = torch.where(place < share, row * share + place, -1).to(torch.int32)
-        return cls(codes(pages, BLOCK_TOKENS, d), codes(pages, d, BLOCK_TOKENS), z(pages), z(pages), z(pages, d, dtype=torch.int8), z(pages),
-                   z(B, Hkv, BLOCK_TOKENS, d, dtype=torch.bfloat16), z(B, Hkv, d, BLOCK_TOKENS, dtype=torch.bfloat16), table,
-                   z(B, Hkv, cap), H, d ** -0.5 if scale is None else scale)
-
-    def adopt(self, table, mass):
-        """From now on with this table and these masses (those that sparsek_cache8_evict gave)."""
-        _same("table", table, torch.int32, (self.B, self.Hkv, self.cap), self.device)
-        _same("mass", mass, torch.float32, (self.B, self.Hkv, self.cap), self.device)
-        object.__setattr__(self, "table", table)
-        object.__setattr__(self, "mass", mass)
-        self._ref()
+        codes = lambda *s: torch.zeros(*s, dtype=torch.uint8, device=device).view(format)   # noqa: E731
+        return cls(codes(pages, BLOCK_TOKENS, d), codes(pages, d, BLOCK_TOKENS), **_empty_common(B, Hkv, d, cap, pages, device), H=H,
+                   scale=d ** -0.5 if scale is None else scale)
 
 
-def sparsek_cache8_append(cache, lens, k, v, counts=None):
-    """The first counts[b] (None: all) of the new tokens k, v [B,Hkv,c,d] join the lens[b] (int32 [B]) that sequence b has; lens itself is
-    the caller's to move on."""
-    torch = _torch()
+class Cache4(_Cache):
+    """The tensors of a cache in 4 bits (see include/sparsek.h), checked once.  The constructor takes the caller's own; Cache4.empty makes
+    them, as Cache8.empty does."""
+    _names, _struct = _CACHE4_TENSORS, SparsekCache4
+
+    def __init__(self, k4, v4, ke, ve, ks, vs, km, kms, kt, vt, table, mass, H, scale):
+        torch = _torch()
+        if km.dim() != 2 or table.dim() != 3:
+            raise ValueError("km is [pages,d] and table is [B,Hkv,cap]")
+        pages, d = km.shape
+        B, Hkv, cap = table.shape
+        tensors = dict(k4=k4, v4=v4, ke=ke, ve=ve, ks=ks, vs=vs, km=km, kms=kms, kt=kt, vt=vt, table=table, mass=mass)
+        u8 = torch.uint8
+        for name, dtype, shape in (("k4", u8, (pages, 32 * d)), ("v4", u8, (pages, 32 * d)), ("ke", u8, (pages, 2 * d)),
+                                   ("ve", u8, (pages, 2 * d))) + _common(B, Hkv, d, cap, pages):
+            _same(name, tensors[name], dtype, shape, k4.device)
+        self._keep(tensors, H, scale, E2M1, pages, d)
+
+    @classmethod
+    def empty(cls, B, H, Hkv, d, cap, scale=None, pages=None, device="cuda"):
+        """A cache without tokens; scale d ** -0.5 by default, pages as for Cache8.empty."""
+        torch = _torch()
+        pages = B * Hkv * cap if pages is None else int(pages)
+        z = lambda size: torch.zeros(pages, size, dtype=torch.uint8, device=device)   # noqa: E731
+        return cls(z(32 * d), z(32 * d), z(2 * d), z(2 * d), **_empty_common(B, Hkv, d, cap, pages, device), H=H, scale=d ** -0.5 if scale is None else scale)
+
+
+def _cache_append(f, cache, lens, k, v, counts):
     shape = (cache.B, cache.Hkv, k.shape[2] if k.dim() == 4 else 0, cache.d)
     _same("k", k, torch.bfloat16, shape, cache.device)
     _same("v", v, torch.bfloat16, shape, cache.device)
     _same("lens", lens, torch.int32, cache.lens_shape, cache.device)
     if counts is not None:
         _same("counts", counts, torch.int32, cache.lens_shape, cache.device)
-    _on(cache.device, lib().sparsek_cache8_append, cache.ref, cache.cref, lens.data_ptr(), _ptr(counts), shape[2], k.data_ptr(), v.data_ptr())
+    _on(cache.device, f, cache.ref, cache.cref, lens.data_ptr(), _ptr(counts), shape[2], k.data_ptr(), v.data_ptr())
 
 
-def sparsek_cache8_select(cache, lens, q, top):
-    """idx [B,Hkv,top] int32: the places in the table of the `top` whole blocks behind the own block of the query q [B,H,d] at position
-    lens - 1 with the largest cheap scores, ascending, padded with -1."""
-    torch = _torch()
+def _cache_select(f, cache, lens, q, top):
     _same("q", q, torch.bfloat16, cache.q_shape, cache.device)
     _same("lens", lens, torch.int32, cache.lens_shape, cache.device)
     idx = torch.empty(cache.B, cache.Hkv, max(int(top), 0), dtype=torch.int32, device=cache.device)
-    _on(cache.device, lib().sparsek_cache8_select, cache.ref, cache.cref, lens.data_ptr(), q.data_ptr(), int(top), idx.data_ptr())
+    _on(cache.device, f, cache.ref, cache.cref, lens.data_ptr(), q.data_ptr(), int(top), idx.data_ptr())
     return idx
 
 
-def sparsek_cache8_attn(cache, lens, q, idx=None, accumulate=False, ws=None):
-    """o [B,H,d] and lse [B,H] fp32 of the query q [B,H,d] at position lens - 1 over all tokens (idx None), or over its own block and
-    those of idx [B,Hkv,top] (top 0: its own block only); accumulate=True adds the weights to cache.mass."""
-    torch, L, top = _torch(), lib(), 0
+def _cache_attn(f, need, cache, lens, q, idx, accumulate, ws):
+    top = 0
     _same("q", q, torch.bfloat16, cache.q_shape, cache.device)
     _same("lens", lens, torch.int32, cache.lens_shape, cache.device)
     if idx is not None:
@@ -697,21 +741,18 @@ def sparsek_cache8_attn(cache, lens, q, idx=None, accumulate=False, ws=None):
     if ws is None:
         nbytes = cache.bytes.get(top)
         if nbytes is None:
-            nbytes = cache.bytes[top] = max(L.sparsek_cache8_attn_workspace_bytes(cache.ref, top), 256)
+            nbytes = cache.bytes[top] = max(need(cache.ref, top), 256)
         ws = torch.empty(nbytes, dtype=torch.uint8, device=cache.device)
     else:
         if ws.device != cache.device or not ws.is_contiguous():
             raise ValueError("ws must be contiguous and on %s" % cache.device)
         nbytes = ws.numel() * ws.element_size()
-    _on(cache.device, L.sparsek_cache8_attn, cache.ref, cache.cref, lens.data_ptr(), q.data_ptr(), _ptr(idx), top, 1 if accumulate else 0,
+    _on(cache.device, f, cache.ref, cache.cref, lens.data_ptr(), q.data_ptr(), _ptr(idx), top, 1 if accumulate else 0,
         o.data_ptr(), lse.data_ptr(), ws.data_ptr(), nbytes)
     return o, lse
 
 
-def sparsek_cache8_evict(cache, lens, budget, sink=1, recent=1, out=None):
-    """Sequences with more than `budget` whole blocks keep the first `sink`, the last `recent` and the heaviest of the others.  Returns
-    dict(table, mass, lens), new tensors or those of `out`; cache.adopt(table, mass) makes the cache go on with them."""
-    torch = _torch()
+def _cache_evict(f, cache, lens, budget, sink, recent, out):
     _same("lens", lens, torch.int32, cache.lens_shape, cache.device)
     if out is None:
         out = dict(table=torch.empty_like(cache.table), mass=torch.empty_like(cache.mass), lens=torch.empty_like(lens))
@@ -719,9 +760,68 @@ def sparsek_cache8_evict(cache, lens, budget, sink=1, recent=1, out=None):
     _same("out table", table, torch.int32, cache.table.shape, cache.device)
     _same("out mass", mass, torch.float32, cache.mass.shape, cache.device)
     _same("out lens", after, torch.int32, cache.lens_shape, cache.device)
-    _on(cache.device, lib().sparsek_cache8_evict, cache.ref, cache.cref, lens.data_ptr(), int(budget), int(sink), int(recent),
+    _on(cache.device, f, cache.ref, cache.cref, lens.data_ptr(), int(budget), int(sink), int(recent),
         table.data_ptr(), mass.data_ptr(), after.data_ptr())
     return out
+
+
+def sparsek_cache8_append(cache, lens, k, v, counts=None):
+    """The first counts[b] (None: all) of the new tokens k, v [B,Hkv,c,d] join the lens[b] (int32 [B]) that sequence b has; lens itself is
+    the caller's to move on."""
+    _cache_append(lib().sparsek_cache8_append, cache, lens, k, v, counts)
+
+
+def sparsek_cache8_select(cache, lens, q, top):
+    """idx [B,Hkv,top] int32: the places in the table of the `top` whole blocks behind the own block of the query q [B,H,d] at position
+    lens - 1 with the largest cheap scores, ascending, padded with -1."""
+    return _cache_select(lib().sparsek_cache8_select, cache, lens, q, top)
+
+
+def sparsek_cache8_attn(cache, lens, q, idx=None, accumulate=False, ws=None):
+    """o [B,H,d] and lse [B,H] fp32 of the query q [B,H,d] at position lens - 1 over all tokens (idx None), or over its own block and
+    those of idx [B,Hkv,top] (top 0: its own block only); accumulate=True adds the weights to cache.mass."""
+    return _cache_attn(lib().sparsek_cache8_attn, lib().sparsek_cache8_attn_workspace_bytes, cache, lens, q, idx, accumulate, ws)
+
+
+def sparsek_cache8_evict(cache, lens, budget, sink=1, recent=1, out=None):
+    """Sequences with more than `budget` whole blocks keep the first `sink`, the last `recent` and the heaviest of the others.  Returns
+    dict(table, mass, lens), new tensors or those of `out`; cache.adopt(table, mass) makes the cache go on with them."""
+    return _cache_evict(lib().sparsek_cache8_evict, cache, lens, budget, sink, recent, out)
+
+
+def sparsek_cache4_append(cache, lens, k, v, counts=None):
+    """As sparsek_cache8_append, into a Cache4."""
+    _cache_append(lib().sparsek_cache4_append, cache, lens, k, v, counts)
+
+
+def sparsek_cache4_select(cache, lens, q, top):
+    """As sparsek_cache8_select, from a Cache4."""
+    return _cache_select(lib().sparsek_cache4_select, cache, lens, q, top)
+
+
+def sparsek_cache4_attn(cache, lens, q, idx=None, accumulate=False, ws=None):
+    """As sparsek_cache8_attn, over a Cache4."""
+    return _cache_attn(lib().sparsek_cache4_attn, lib().sparsek_cache4_attn_workspace_bytes, cache, lens, q, idx, accumulate, ws)
+
+
+def sparsek_cache4_evict(cache, lens, budget, sink=1, recent=1, out=None):
+    """As sparsek_cache8_evict, from a Cache4."""
+    return _cache_evict(lib().sparsek_cache4_evict, cache, lens, budget, sink, recent, out)
+
+
+def sparsek_cache4_read(cache, lens, begin, n, out=None):
+    """k, v [B,Hkv,n,d] bf16: tokens begin .. begin + n - 1 of every sequence as they are attended, zeros behind its end; new tensors or those
+    of `out`."""
+    _same("lens", lens, torch.int32, cache.lens_shape, cache.device)
+    shape = (cache.B, cache.Hkv, int(n), cache.d)
+    if out is None:
+        out = tuple(torch.empty(cache.B, cache.Hkv, max(int(n), 0), cache.d, dtype=torch.bfloat16, device=cache.device) for _ in range(2))
+    else:
+        for name, t in zip(("out k", "out v"), out):
+            _same(name, t, torch.bfloat16, shape, cache.device)
+    k, v = out
+    _on(cache.device, lib().sparsek_cache4_read, cache.ref, cache.cref, lens.data_ptr(), int(begin), int(n), k.data_ptr(), v.data_ptr())
+    return k, v
 
 
 # ---- norms of queries and keys with rotary positions ----

@@ -412,7 +412,7 @@ int sparsek_chunk_status(const sparsek_chunk_cfg* cfg, const void* state, int32_
 
 }  // extern "C"
 
-// ---- attention over blocks of tokens (block_select.hip, block_attn.hip, block_attn_bwd.hip) and the cache in 8 bits (cache8.hip) ----
+// ---- attention over blocks of tokens (block_select.hip, block_attn.hip, block_attn_bwd.hip) and the caches in 8 and in 4 bits (cache8.hip, cache4.hip) ----
 namespace spk {
 size_t block_select_ws_bytes(const sparsek_block_cfg& c);
 int launch_block_select(const sparsek_block_cfg& c, const void* q, const void* k, int32_t* idx, void* ws, hipStream_t st);
@@ -430,6 +430,15 @@ size_t cache8_attn_ws_bytes(const sparsek_cache8_cfg& c, int top);
 int launch_cache8_attn(const sparsek_cache8_cfg& c, const sparsek_cache8& t, const int32_t* lens, const void* q, const int32_t* idx,
                        int top, int accumulate, void* o, float* lse, void* ws, hipStream_t st);
 int launch_cache8_evict(const sparsek_cache8_cfg& c, const sparsek_cache8& t, const int32_t* lens, int budget, int sink, int recent,
+                        int32_t* table, float* mass, int32_t* lens_out, hipStream_t st);
+int launch_cache4_append(const sparsek_cache8_cfg& c, const sparsek_cache4& t, const int32_t* lens, const int32_t* counts, int count,
+                         const void* k, const void* v, hipStream_t st);
+int launch_cache4_read(const sparsek_cache8_cfg& c, const sparsek_cache4& t, const int32_t* lens, int begin, int n, void* k, void* v, hipStream_t st);
+int launch_cache4_select(const sparsek_cache8_cfg& c, const sparsek_cache4& t, const int32_t* lens, const void* q, int top, int32_t* idx,
+                         hipStream_t st);
+int launch_cache4_attn(const sparsek_cache8_cfg& c, const sparsek_cache4& t, const int32_t* lens, const void* q, const int32_t* idx,
+                       int top, int accumulate, void* o, float* lse, void* ws, hipStream_t st);
+int launch_cache4_evict(const sparsek_cache8_cfg& c, const sparsek_cache4& t, const int32_t* lens, int budget, int sink, int recent,
                         int32_t* table, float* mass, int32_t* lens_out, hipStream_t st);
 }  // namespace spk
 
@@ -456,17 +465,6 @@ int check_block(const sparsek_block_cfg* c)
     return SPARSEK_OK;
 }
 
-int check_cache8(const sparsek_cache8_cfg* c, const sparsek_cache8* t)
-{
-    if (!c || c->cap < 1 || c->pages < 1) return SPARSEK_ERR_INVALID_ARG;
-    int rc = check_heads(c->B, c->H, c->Hkv, c->d, c->dtype, c->softmax_scale);
-    if (rc) return rc;
-    if (c->format != SPARSEK_I8 && c->format != SPARSEK_E4M3) return SPARSEK_ERR_UNSUPPORTED;
-    if (c->cap > MAX_CACHE_BLOCKS || c->pages > (1 << 24)) return SPARSEK_ERR_UNSUPPORTED;
-    if (t && (!t->k8 || !t->v8 || !t->ks || !t->vs || !t->km || !t->kms || !t->kt || !t->vt || !t->table || !t->mass)) return SPARSEK_ERR_INVALID_ARG;
-    return SPARSEK_OK;
-}
-
 // What is read or written 16 bytes at a time.
 bool aligned(std::initializer_list<const void*> ps)
 {
@@ -474,11 +472,111 @@ bool aligned(std::initializer_list<const void*> ps)
         if ((uintptr_t)p & 15) return false;
     return true;
 }
-bool aligned(const sparsek_cache8& t) { return aligned({t.k8, t.v8, t.km, t.kt, t.vt}); }
 
 bool overlap(const void* a, size_t na, const void* b, size_t nb)
 {
     return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
+
+// Both caches: the same checks, and the same launches.
+struct Of8 {
+    typedef sparsek_cache8 Cache;
+    static bool format(int f) { return f == SPARSEK_I8 || f == SPARSEK_E4M3; }
+    static bool whole(const Cache& t) { return t.k8 && t.v8 && t.ks && t.vs && t.km && t.kms && t.kt && t.vt && t.table && t.mass; }
+    static bool wide(const Cache& t) { return aligned({t.k8, t.v8, t.km, t.kt, t.vt}); }
+    static constexpr auto append = spk::launch_cache8_append;
+    static constexpr auto select = spk::launch_cache8_select;
+    static constexpr auto attn = spk::launch_cache8_attn;
+    static constexpr auto evict = spk::launch_cache8_evict;
+};
+struct Of4 {
+    typedef sparsek_cache4 Cache;
+    static bool format(int f) { return f == SPARSEK_E2M1; }
+    static bool whole(const Cache& t) { return t.k4 && t.v4 && t.ke && t.ve && t.ks && t.vs && t.km && t.kms && t.kt && t.vt && t.table && t.mass; }
+    static bool wide(const Cache& t) { return aligned({t.k4, t.v4, t.ke, t.ve, t.km, t.kt, t.vt}); }
+    static constexpr auto append = spk::launch_cache4_append;
+    static constexpr auto select = spk::launch_cache4_select;
+    static constexpr auto attn = spk::launch_cache4_attn;
+    static constexpr auto evict = spk::launch_cache4_evict;
+};
+
+template <class Of>
+int check_cache(const sparsek_cache8_cfg* c, const typename Of::Cache* t)
+{
+    if (!c || c->cap < 1 || c->pages < 1) return SPARSEK_ERR_INVALID_ARG;
+    int rc = check_heads(c->B, c->H, c->Hkv, c->d, c->dtype, c->softmax_scale);
+    if (rc) return rc;
+    if (!Of::format(c->format)) return SPARSEK_ERR_UNSUPPORTED;
+    if (c->cap > MAX_CACHE_BLOCKS || c->pages > (1 << 24)) return SPARSEK_ERR_UNSUPPORTED;
+    if (t && !Of::whole(*t)) return SPARSEK_ERR_INVALID_ARG;
+    return SPARSEK_OK;
+}
+
+template <class Of>
+int cache_append(const sparsek_cache8_cfg* cfg, const typename Of::Cache* cache, const int32_t* lens, const int32_t* counts,
+                 int32_t c, const void* k, const void* v, void* stream)
+{
+    if (!cache) return SPARSEK_ERR_INVALID_ARG;
+    int rc = check_cache<Of>(cfg, cache);
+    if (rc) return rc;
+    if (!lens || !k || !v || c < 1 || !Of::wide(*cache) || !aligned({k, v})) return SPARSEK_ERR_INVALID_ARG;
+    if (c > (1 << 24)) return SPARSEK_ERR_UNSUPPORTED;
+    return Of::append(*cfg, *cache, lens, counts, c, k, v, (hipStream_t)stream);
+}
+
+template <class Of>
+int cache_select(const sparsek_cache8_cfg* cfg, const typename Of::Cache* cache, const int32_t* lens, const void* q, int32_t top,
+                 int32_t* idx, void* stream)
+{
+    if (!cache) return SPARSEK_ERR_INVALID_ARG;
+    int rc = check_cache<Of>(cfg, cache);
+    if (rc) return rc;
+    if (!lens || !q || !idx || top < 1 || !Of::wide(*cache) || !aligned({q})) return SPARSEK_ERR_INVALID_ARG;
+    if (top > MAX_CACHE_BLOCKS) return SPARSEK_ERR_UNSUPPORTED;
+    return Of::select(*cfg, *cache, lens, q, top, idx, (hipStream_t)stream);
+}
+
+template <class Of>
+size_t cache_attn_workspace_bytes(const sparsek_cache8_cfg* cfg, int32_t top)
+{
+    if (check_cache<Of>(cfg, nullptr) || top < 0 || top > MAX_CACHE_BLOCKS) return 0;
+    return spk::cache8_attn_ws_bytes(*cfg, top);
+}
+
+template <class Of>
+int cache_attn(const sparsek_cache8_cfg* cfg, const typename Of::Cache* cache, const int32_t* lens, const void* q,
+               const int32_t* idx, int32_t top, int32_t accumulate, void* o, float* lse, void* ws, size_t ws_bytes,
+               void* stream)
+{
+    if (!cache) return SPARSEK_ERR_INVALID_ARG;
+    int rc = check_cache<Of>(cfg, cache);
+    if (rc) return rc;
+    if (!lens || !q || !o || !lse || !ws || (idx ? top < 1 : top != 0)) return SPARSEK_ERR_INVALID_ARG;
+    if (!Of::wide(*cache) || !aligned({q, o, ws})) return SPARSEK_ERR_INVALID_ARG;
+    if (top > MAX_CACHE_BLOCKS) return SPARSEK_ERR_UNSUPPORTED;
+    if (ws_bytes < spk::cache8_attn_ws_bytes(*cfg, top)) return SPARSEK_ERR_WORKSPACE;
+    return Of::attn(*cfg, *cache, lens, q, idx, top, accumulate != 0, o, lse, ws, (hipStream_t)stream);
+}
+
+template <class Of>
+int cache_evict(const sparsek_cache8_cfg* cfg, const typename Of::Cache* cache, const int32_t* lens, int32_t budget, int32_t sink,
+                int32_t recent, int32_t* table_out, float* mass_out, int32_t* lens_out, void* stream)
+{
+    if (!cache) return SPARSEK_ERR_INVALID_ARG;
+    int rc = check_cache<Of>(cfg, cache);
+    if (rc) return rc;
+    if (!lens || !table_out || !mass_out || !lens_out) return SPARSEK_ERR_INVALID_ARG;
+    if (budget < 0 || sink < 0 || recent < 0 || (long long)sink + recent > budget) return SPARSEK_ERR_INVALID_ARG;
+    const size_t nt = (size_t)cfg->B * cfg->Hkv * cfg->cap * 4, nl = (size_t)cfg->B * 4;
+    const void* in[] = {cache->table, cache->mass, lens};
+    const size_t nin[] = {nt, nt, nl};
+    void* out[] = {table_out, mass_out, lens_out};
+    for (int x = 0; x < 3; x++)
+        for (int y = 0; y < 3; y++) {
+            if (overlap(in[x], nin[x], out[y], nin[y])) return SPARSEK_ERR_INVALID_ARG;
+            if (x < y && overlap(out[x], nin[x], out[y], nin[y])) return SPARSEK_ERR_INVALID_ARG;
+        }
+    return Of::evict(*cfg, *cache, lens, budget, sink, recent, table_out, mass_out, lens_out, (hipStream_t)stream);
 }
 
 }  // namespace
@@ -537,63 +635,72 @@ int sparsek_block_attn_bwd(const sparsek_block_cfg* cfg, const void* q, const vo
 int sparsek_cache8_append(const sparsek_cache8_cfg* cfg, const sparsek_cache8* cache, const int32_t* lens, const int32_t* counts,
                           int32_t c, const void* k, const void* v, void* stream)
 {
-    if (!cache) return SPARSEK_ERR_INVALID_ARG;
-    int rc = check_cache8(cfg, cache);
-    if (rc) return rc;
-    if (!lens || !k || !v || c < 1 || !aligned(*cache) || !aligned({k, v})) return SPARSEK_ERR_INVALID_ARG;
-    if (c > (1 << 24)) return SPARSEK_ERR_UNSUPPORTED;
-    return spk::launch_cache8_append(*cfg, *cache, lens, counts, c, k, v, (hipStream_t)stream);
+    return cache_append<Of8>(cfg, cache, lens, counts, c, k, v, stream);
 }
 
 int sparsek_cache8_select(const sparsek_cache8_cfg* cfg, const sparsek_cache8* cache, const int32_t* lens, const void* q, int32_t top,
                           int32_t* idx, void* stream)
 {
-    if (!cache) return SPARSEK_ERR_INVALID_ARG;
-    int rc = check_cache8(cfg, cache);
-    if (rc) return rc;
-    if (!lens || !q || !idx || top < 1 || !aligned(*cache) || !aligned({q})) return SPARSEK_ERR_INVALID_ARG;
-    if (top > MAX_CACHE_BLOCKS) return SPARSEK_ERR_UNSUPPORTED;
-    return spk::launch_cache8_select(*cfg, *cache, lens, q, top, idx, (hipStream_t)stream);
+    return cache_select<Of8>(cfg, cache, lens, q, top, idx, stream);
 }
 
 size_t sparsek_cache8_attn_workspace_bytes(const sparsek_cache8_cfg* cfg, int32_t top)
 {
-    if (check_cache8(cfg, nullptr) || top < 0 || top > MAX_CACHE_BLOCKS) return 0;
-    return spk::cache8_attn_ws_bytes(*cfg, top);
+    return cache_attn_workspace_bytes<Of8>(cfg, top);
 }
 
 int sparsek_cache8_attn(const sparsek_cache8_cfg* cfg, const sparsek_cache8* cache, const int32_t* lens, const void* q,
                         const int32_t* idx, int32_t top, int32_t accumulate, void* o, float* lse, void* ws, size_t ws_bytes,
                         void* stream)
 {
-    if (!cache) return SPARSEK_ERR_INVALID_ARG;
-    int rc = check_cache8(cfg, cache);
-    if (rc) return rc;
-    if (!lens || !q || !o || !lse || !ws || (idx ? top < 1 : top != 0)) return SPARSEK_ERR_INVALID_ARG;
-    if (!aligned(*cache) || !aligned({q, o, ws})) return SPARSEK_ERR_INVALID_ARG;
-    if (top > MAX_CACHE_BLOCKS) return SPARSEK_ERR_UNSUPPORTED;
-    if (ws_bytes < spk::cache8_attn_ws_bytes(*cfg, top)) return SPARSEK_ERR_WORKSPACE;
-    return spk::launch_cache8_attn(*cfg, *cache, lens, q, idx, top, accumulate != 0, o, lse, ws, (hipStream_t)stream);
+    return cache_attn<Of8>(cfg, cache, lens, q, idx, top, accumulate, o, lse, ws, ws_bytes, stream);
 }
 
 int sparsek_cache8_evict(const sparsek_cache8_cfg* cfg, const sparsek_cache8* cache, const int32_t* lens, int32_t budget, int32_t sink,
                          int32_t recent, int32_t* table_out, float* mass_out, int32_t* lens_out, void* stream)
 {
+    return cache_evict<Of8>(cfg, cache, lens, budget, sink, recent, table_out, mass_out, lens_out, stream);
+}
+
+int sparsek_cache4_append(const sparsek_cache8_cfg* cfg, const sparsek_cache4* cache, const int32_t* lens, const int32_t* counts,
+                          int32_t c, const void* k, const void* v, void* stream)
+{
+    return cache_append<Of4>(cfg, cache, lens, counts, c, k, v, stream);
+}
+
+int sparsek_cache4_select(const sparsek_cache8_cfg* cfg, const sparsek_cache4* cache, const int32_t* lens, const void* q, int32_t top,
+                          int32_t* idx, void* stream)
+{
+    return cache_select<Of4>(cfg, cache, lens, q, top, idx, stream);
+}
+
+size_t sparsek_cache4_attn_workspace_bytes(const sparsek_cache8_cfg* cfg, int32_t top)
+{
+    return cache_attn_workspace_bytes<Of4>(cfg, top);
+}
+
+int sparsek_cache4_attn(const sparsek_cache8_cfg* cfg, const sparsek_cache4* cache, const int32_t* lens, const void* q,
+                        const int32_t* idx, int32_t top, int32_t accumulate, void* o, float* lse, void* ws, size_t ws_bytes,
+                        void* stream)
+{
+    return cache_attn<Of4>(cfg, cache, lens, q, idx, top, accumulate, o, lse, ws, ws_bytes, stream);
+}
+
+int sparsek_cache4_evict(const sparsek_cache8_cfg* cfg, const sparsek_cache4* cache, const int32_t* lens, int32_t budget, int32_t sink,
+                         int32_t recent, int32_t* table_out, float* mass_out, int32_t* lens_out, void* stream)
+{
+    return cache_evict<Of4>(cfg, cache, lens, budget, sink, recent, table_out, mass_out, lens_out, stream);
+}
+
+int sparsek_cache4_read(const sparsek_cache8_cfg* cfg, const sparsek_cache4* cache, const int32_t* lens, int32_t begin, int32_t n, void* k,
+                        void* v, void* stream)
+{
     if (!cache) return SPARSEK_ERR_INVALID_ARG;
-    int rc = check_cache8(cfg, cache);
+    int rc = check_cache<Of4>(cfg, cache);
     if (rc) return rc;
-    if (!lens || !table_out || !mass_out || !lens_out) return SPARSEK_ERR_INVALID_ARG;
-    if (budget < 0 || sink < 0 || recent < 0 || (long long)sink + recent > budget) return SPARSEK_ERR_INVALID_ARG;
-    const size_t nt = (size_t)cfg->B * cfg->Hkv * cfg->cap * 4, nl = (size_t)cfg->B * 4;
-    const void* in[] = {cache->table, cache->mass, lens};
-    const size_t nin[] = {nt, nt, nl};
-    void* out[] = {table_out, mass_out, lens_out};
-    for (int x = 0; x < 3; x++)
-        for (int y = 0; y < 3; y++) {
-            if (overlap(in[x], nin[x], out[y], nin[y])) return SPARSEK_ERR_INVALID_ARG;
-            if (x < y && overlap(out[x], nin[x], out[y], nin[y])) return SPARSEK_ERR_INVALID_ARG;
-        }
-    return spk::launch_cache8_evict(*cfg, *cache, lens, budget, sink, recent, table_out, mass_out, lens_out, (hipStream_t)stream);
+    if (!lens || !k || !v || begin < 0 || n < 1 || !Of4::wide(*cache) || !aligned({k, v})) return SPARSEK_ERR_INVALID_ARG;
+    if ((long long)begin + n > (1 << 28)) return SPARSEK_ERR_UNSUPPORTED;
+    return spk::launch_cache4_read(*cfg, *cache, lens, begin, n, k, v, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -1,0 +1,84 @@
+// The cache in 4 bits: what its append, its attention and its reading back share.
+//
+// A value is an e2m1 code (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign) times a power of two that 32 values share: of keys 32 channels of a token, of
+// values 32 tokens of a channel.  The power is the smallest with which none of the 32 passes 6, so a value is off by a sixth of the
+// largest at most, and scaling loses nothing.  Inside a page codes and scales lie as the lanes of the matrix instructions take them, 16
+// bytes of codes to a lane at a time: the attention's loads are whole lines, straight into registers.
+#pragma once
+#include "block_parts.hpp"
+
+namespace spk {
+
+constexpr int FORMAT_E2M1 = SPARSEK_E2M1;
+
+// Bytes of a page: codes, and scales (biased by 127, 0: a group of zeros), of keys as of values.
+template <int D>
+struct Page4 {
+    static constexpr int CODES = BT * D / 2, SCALES = BT * D / 32;
+    // 8 codes (4 bytes): keys of token s, channels 8 c8 ..; values of channel c, tokens 8 s8 ..
+    static __device__ __forceinline__ int key_at(int s, int c8)
+    {
+        const int t = s >> 2 & 3, row = (s >> 4) * 4 + (s & 3);
+        if constexpr (D == 128) return ((t * 4 + c8 / 4) * 16 + row) * 16 + c8 % 4 * 4;
+        else return ((t / 2 * 4 + c8 / 2) * 16 + row) * 16 + t % 2 * 8 + c8 % 2 * 4;
+    }
+    static __device__ __forceinline__ int value_at(int c, int s8) { return ((c / 32 * 4 + s8 / 2) * 16 + c % 16) * 16 + c / 16 % 2 * 8 + s8 % 2 * 4; }
+    // the scale of token s, channels 32 j ..; of channel c, tokens 32 j ..
+    static __device__ __forceinline__ int key_scale_at(int s, int j) { return (j * 16 + (s >> 4) * 4 + (s & 3)) * 4 + (s >> 2 & 3); }
+    static __device__ __forceinline__ int value_scale_at(int c, int j) { return (j * 16 + c % 16) * (D / 16) + c / 16; }
+};
+
+// The scale of a group whose largest magnitude has the bits `top`: the smallest power of two with top <= 6 of them, at most 2^125 (6 2^126
+// is no number any more), as its biased exponent.
+__device__ __forceinline__ unsigned scale_of_top(unsigned top) { return top >= __float_as_uint(TINY_MAX) ? min((top + 0x3FFFFFu >> 23) - 2u, 252u) : 0u; }
+
+typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
+
+// 8 bf16 values as codes; e: their scale.
+__device__ __forceinline__ unsigned codes_e2m1(u32x4 x, unsigned e)
+{
+    const float scale = __uint_as_float(e << 23);
+    const unsigned p[4] = {x[0], x[1], x[2], x[3]};   // (a bit cast of a vector's element takes the first one's bits)
+    unsigned w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2v, p[0]), scale, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2v, p[1]), scale, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2v, p[2]), scale, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2v, p[3]), scale, 3);
+    return e ? w : 0u;
+}
+
+// 8 codes as fp16, times 2^(e - 127).
+__device__ __forceinline__ f16x8 widen_e2m1(unsigned w, float scale)
+{
+    const f16x2v a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 1);
+    const f16x2v c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 3);
+    return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// A page's largest scale, which ks and vs hold: times 1.5 where its scales are `wide`, where one that is not 0 is less than 2^-36 of it.
+constexpr int WIDE = 36;
+__device__ __forceinline__ float page_scale(float top, int lowest)
+{
+    if (!(top < INFINITY)) return __uint_as_float(0x7FC00000u);
+    const int e = (int)scale_of_top(__float_as_uint(top));
+    return __uint_as_float((unsigned)e << 23 | (lowest < e - WIDE ? 0x400000u : 0u));
+}
+
+// In fp16 a page's values stand relative to its largest scale, which becomes 2^13 (6 times that is below fp16's largest number): all of them are
+// exact unless the page is wide, whose products are scaled in fp32 instead.
+struct Relative {
+    int add;      // to a scale's biased exponent
+    float unit;   // what 1 stands for in the products; NaN of a page with a value that is not finite
+    bool wide;
+    __device__ __forceinline__ explicit Relative(float largest)
+    {
+        const unsigned b = __float_as_uint(largest);
+        const int e = (int)(b >> 23) & 255;
+        add = 127 + 13 - e;
+        wide = (b & 0x7FFFFFu) && e < 255;
+        unit = largest * 0x1p-13f;
+    }
+    __device__ __forceinline__ float of(unsigned scales, int byte) const { return __uint_as_float((unsigned)max((int)(scales >> 8 * byte & 255) + add, 1) << 23); }
+};
+
+}  // namespace spk

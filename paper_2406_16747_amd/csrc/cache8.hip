@@ -1,4 +1,4 @@
-// A key/value cache in blocks of 64 tokens, held in 8 bits with a scale for each block and head.
+// A key/value cache in blocks of 64 tokens, held in 8 bits with a scale for each block and head, or in 4 with one for 32 values.
 //
 // A page holds one block of one key/value head: keys [64][D] and values transposed [D][64], so that both products of the
 // attention read their 8-bit operands as they lie (16 bytes a lane).  The table names a head's pages by age; the unfinished
@@ -8,7 +8,7 @@
 // What bounds the kernels is memory where there is much to move (four prompts of 8192 go in at 5.2 TB/s, 64 sequences of up to 8192 are
 // attended at 5.4 TB/s of the kernel's time) and the length of a chain of dependent steps where there is little: a token's append takes
 // 3 us, 6 to 8 where it ends a block; the choice among 1024 blocks 12; the attention of 200 tokens 8; an eviction from 129 blocks 6.
-#include "block_parts.hpp"
+#include "cache4_parts.hpp"
 
 namespace spk {
 
@@ -18,6 +18,7 @@ struct CacheArgs {
     sparsek_cache8 t;
     int B, H, Hkv, G, cap, pages;
     const int32_t* lens;
+    uint8_t *ke, *ve;   // the scales of the cache in 4 bits; its codes are t.k8 and t.v8, the largest scale of a page t.ks and t.vs
 };
 
 __device__ __forceinline__ int clamp_len(int len, int cap) { return min(max(len, 0), cap * BT + BT - 1); }
@@ -48,9 +49,10 @@ __device__ __forceinline__ unsigned codes4(float a, float b, float c, float d, f
 template <int D>
 struct AppendSmem {
     static constexpr int VS = BT + 8;                                       // bf16 values between the columns of vt
-    double sums[4][D];                                                      // of a wave's tokens
+    __attribute__((aligned(16))) double sums[4][D];                         // of a wave's tokens
     __attribute__((aligned(16))) uint16_t vt[D * VS];                       // the block's values, transposed
     unsigned red[12];
+    __attribute__((aligned(16))) unsigned char scales4[2][BT * D / 32];     // of a cache in 4 bits, the keys' and the values'
     // Token x of a column.  Its groups of 8 tokens change places from 16 columns to the next: a token's columns, 8 to a lane, go to banks
     // of their own (as they lie, to two; four prompts of 8192 into the cache 42 us then).
     static __device__ __forceinline__ int at(int col, int x) { return col * VS + ((x >> 3 ^ (col >> 4 & 7)) << 3) + (x & 7); }
@@ -71,6 +73,70 @@ __device__ __forceinline__ double sum_columns(double x)
         x = both_words(x, [](unsigned y) { return u32x2{y, (unsigned)__builtin_amdgcn_mov_dpp((int)y, 0x128, 0xF, 0xF, true)}; });   // (8 lanes on, of 16)
     x = both_words(x, [](unsigned y) { const auto s = __builtin_amdgcn_permlane16_swap(y, y, false, false); return u32x2{(unsigned)s[0], (unsigned)s[1]}; });
     return both_words(x, [](unsigned y) { const auto s = __builtin_amdgcn_permlane32_swap(y, y, false, false); return u32x2{(unsigned)s[0], (unsigned)s[1]}; });
+}
+
+// The codes and scales of a block in 4 bits.  A group of keys is four neighbouring lanes' (8 channels each), one of values a thread's.
+// Codes meet in LDS, the keys' where the sums were that nobody needs any more, the values' where the values were, so that whole lines leave.
+template <int D>
+__device__ __forceinline__ void store_codes4(AppendSmem<D>& sm, const CacheArgs& a, int page, const u32x4 (&kr)[BlockRegs<D>::NT], float topk, float topv, int tid)
+{
+    using R = BlockRegs<D>;
+    using P = Page4<D>;
+    unsigned char *k4 = (unsigned char*)sm.sums, *v4 = (unsigned char*)sm.vt;
+    static_assert(sizeof(sm.sums) >= P::CODES && sizeof(sm.vt) >= P::CODES, "room for a page's codes");
+    const int tok = tid / R::CPR, c = tid % R::CPR;
+    unsigned lowk = 0, lowv = 0;   // 255 less the smallest scale that is not 0
+#pragma unroll
+    for (int t = 0; t < R::NT; t++) {
+        int top = (int)top_of_8(kr[t]);
+        top = max(top, dpp_i32(top, 0));
+        top = max(top, dpp_i32(top, 1));
+        const unsigned e = scale_of_top((unsigned)top);
+        lowk = max(lowk, e ? 255u - e : 0u);
+        const int s = tok + R::RG * t;
+        *(unsigned*)&k4[P::key_at(s, c)] = codes_e2m1(kr[t], e);
+        if (c % 4 == 0) sm.scales4[0][P::key_scale_at(s, c / 4)] = (unsigned char)e;
+    }
+    u32x4 w = {0, 0, 0, 0};
+    const int col = tid / 2, j = tid % 2;
+    if (col < D) {
+        u32x4 x[4];
+        unsigned top = 0;
+#pragma unroll
+        for (int y = 0; y < 4; y++) {
+            x[y] = *(const u32x4*)&sm.vt[AppendSmem<D>::at(col, 32 * j + 8 * y)];
+            top = max(top, top_of_8(x[y]));
+        }
+        const unsigned e = scale_of_top(top);
+#pragma unroll
+        for (int y = 0; y < 4; y++) w[y] = codes_e2m1(x[y], e);
+        lowv = e ? 255u - e : 0u;
+        sm.scales4[1][P::value_scale_at(col, j)] = (unsigned char)e;
+    }
+    lowk = wave_max_bits(lowk);
+    lowv = wave_max_bits(lowv);
+    __syncthreads();   // the values are read, and so is sm.red
+    if ((tid & 63) == 0) {
+        sm.red[tid >> 6] = lowk;
+        sm.red[4 + (tid >> 6)] = lowv;
+    }
+    if (col < D) {
+        *(u32x2*)&v4[P::value_at(col, 4 * j)] = u32x2{w[0], w[1]};
+        *(u32x2*)&v4[P::value_at(col, 4 * j + 2)] = u32x2{w[2], w[3]};
+    }
+    __syncthreads();
+    if (tid < P::CODES / 16) {
+        __builtin_nontemporal_store(*(const u32x4*)&k4[16 * tid], (u32x4*)((unsigned char*)a.t.k8 + (size_t)page * P::CODES + 16 * tid));
+        __builtin_nontemporal_store(*(const u32x4*)&v4[16 * tid], (u32x4*)((unsigned char*)a.t.v8 + (size_t)page * P::CODES + 16 * tid));
+    }
+    if (tid < P::SCALES / 4) {
+        __builtin_nontemporal_store(*(const unsigned*)&sm.scales4[0][4 * tid], (unsigned*)(a.ke + (size_t)page * P::SCALES + 4 * tid));
+        __builtin_nontemporal_store(*(const unsigned*)&sm.scales4[1][4 * tid], (unsigned*)(a.ve + (size_t)page * P::SCALES + 4 * tid));
+    }
+    if (tid == 0) {
+        a.t.ks[page] = page_scale(topk, 255 - (int)max(max(sm.red[0], sm.red[1]), max(sm.red[2], sm.red[3])));
+        a.t.vs[page] = page_scale(topv, 255 - (int)max(max(sm.red[4], sm.red[5]), max(sm.red[6], sm.red[7])));
+    }
 }
 
 // A whole block goes to its page: codes, scales and the mean key.  The keys are in registers, the values (transposed) in sm.vt; every
@@ -115,6 +181,12 @@ __device__ __forceinline__ void store_block(AppendSmem<D>& sm, const CacheArgs& 
     __syncthreads();
     auto top_of = [&](int x) { return __uint_as_float(max(max(sm.red[x], sm.red[x + 1]), max(sm.red[x + 2], sm.red[x + 3]))); };
     const float topk = top_of(0), topv = top_of(4), topm = top_of(8);
+    if (tid < D) a.t.km[(size_t)page * D + tid] = (int8_t)code_i8(mean, code_factor(topm, 127.0f));
+    if constexpr (FORMAT == FORMAT_E2M1) {
+        if (tid == 0) a.t.kms[page] = code_scale(topm, 127.0f);
+        store_codes4<D>(sm, a, page, kr, topk, topv, tid);
+        return;
+    }
     const float fk = code_factor(topk, most), fv = code_factor(topv, most);
     unsigned char* kp = (unsigned char*)a.t.k8 + (size_t)page * BT * D;
 #pragma unroll
@@ -136,7 +208,6 @@ __device__ __forceinline__ void store_block(AppendSmem<D>& sm, const CacheArgs& 
         w[3] = codes4<FORMAT>(half_of(hi, 4), half_of(hi, 5), half_of(hi, 6), half_of(hi, 7), fv);
         __builtin_nontemporal_store(w, (u32x4*)(vp + 16 * x));
     }
-    if (tid < D) a.t.km[(size_t)page * D + tid] = (int8_t)code_i8(mean, code_factor(topm, 127.0f));
     if (tid == 0) {
         // (what is not finite must not get lost: NaN for whoever attends the block)
         a.t.ks[page] = topk < INFINITY ? code_scale(topk, most) : __uint_as_float(0x7FC00000u);
@@ -544,7 +615,8 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void cache8_attn_kernel(Attn
 {
     using T = CacheTile<D>;
     constexpr int KH = D / 64, NX = D / 16, RO = D + 4;
-    __shared__ __attribute__((aligned(16))) unsigned char tiles[4][2 * T::BYTES];   // a wave's keys and values; its result at the end
+    constexpr bool FOUR = FORMAT == FORMAT_E2M1;
+    __shared__ __attribute__((aligned(16))) unsigned char tiles[4][FOUR ? 16 * RO * 4 : 2 * T::BYTES];   // a wave's keys and values; its result at the end
     __shared__ float sm_[4][16], sl[4][16], shares[4 * MAX_UPW + 1][16];
     __shared__ unsigned seen[MAX_CAP / 32];
     static_assert(16 * RO * 4 <= 2 * T::BYTES, "room for a wave's result");
@@ -590,15 +662,17 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void cache8_attn_kernel(Attn
         ks = a.c.t.ks[page];
         vs = a.c.t.vs[page];
     }
-    // Q^T: head col, columns 64 half + 16 grp + 8 sub .., relative to the head's largest value
-    const uint16_t* qr = a.q + (head0 + min(col, live - 1)) * D + 16 * grp;
+    // Q^T: head col, columns 64 half + 16 grp + 8 sub .. (in 4 bits: a lane's are those of one scale or half of one), relative to the head's
+    // largest value
+    constexpr int QG = FOUR ? D / 4 : 16, QH = FOUR ? 16 : 64;
+    const uint16_t* qr = a.q + (head0 + min(col, live - 1)) * D + QG * grp;
     u32x4 qw[KH][2];
     unsigned top = 0;
 #pragma unroll
     for (int h = 0; h < KH; h++)
 #pragma unroll
         for (int s = 0; s < 2; s++) {
-            qw[h][s] = *(const u32x4*)(qr + 64 * h + 8 * s);
+            qw[h][s] = *(const u32x4*)(qr + QH * h + 8 * s);
 #pragma unroll
             for (int e = 0; e < 4; e++) top = max(top, max(qw[h][s][e] << 16 & 0x7FFFFFFFu, qw[h][s][e] & 0x7FFF0000u));
         }
@@ -621,7 +695,100 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void cache8_attn_kernel(Attn
     const bool weighs = a.accumulate && !alone;
     const buffer_t wbuf = buffer_of(weighs ? a.weight + head0 * a.units : nullptr, weighs ? live * a.units * 4 : 0);
     const int wat = grp == 0 && col < live ? col * a.units * 4 : 0x7FFFFF00;
-    if (have) {
+    if (FOUR && have) {
+        using P = Page4<D>;
+        // Keys and values go from memory to the registers in which the products take them; the next block's keys are asked for behind the
+        // last product with this one's, and so are the values.
+        u32x4 kc[D / 32], vc[D / 32];
+        unsigned ke = 0, ve[D / 64];
+        auto load_k = [&](int i) {
+            const size_t page_i = (size_t)__builtin_amdgcn_readlane(page, i);
+            const unsigned char* at = (const unsigned char*)a.c.t.k8 + page_i * P::CODES + 16 * lane;
+#pragma unroll
+            for (int x = 0; x < D / 32; x++) kc[x] = *(const u32x4*)(at + 1024 * x);
+            ke = *(const unsigned*)(a.c.ke + page_i * P::SCALES + 4 * (D == 128 ? lane : 16 * (grp / 2) + col));
+        };
+        auto load_v = [&](int i) {
+            const size_t page_i = (size_t)__builtin_amdgcn_readlane(page, i);
+            const unsigned char* at = (const unsigned char*)a.c.t.v8 + page_i * P::CODES + 16 * lane;
+#pragma unroll
+            for (int x = 0; x < D / 32; x++) vc[x] = *(const u32x4*)(at + 1024 * x);
+#pragma unroll
+            for (int x = 0; x < D / 64; x++) ve[x] = *(const unsigned*)(a.c.ve + page_i * P::SCALES + (16 * (grp / 2) + col) * (D / 16) + 4 * x);
+        };
+        load_k(0);
+        load_v(0);
+        for (int i = 0; i < count; i++) {
+            const Relative krel(readlane_f32(ks, i)), vrel(readlane_f32(vs, i));
+            const float f = krel.unit * c2q;
+            const bool there = have >> i & 1;
+            f32x4m s[4];
+            if (!krel.wide) {
+#pragma unroll
+                for (int t = 0; t < 4; t++) {
+                    s[t] = f32x4m{0, 0, 0, 0};
+                    const float scale = krel.of(ke, t);
+#pragma unroll
+                    for (int x = 0; x < D / 32; x++) {
+                        const unsigned w = D == 128 ? kc[t][x] : kc[t / 2][2 * (t % 2) + x];
+                        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen_e2m1(w, scale), qf[x / 2][x % 2], s[t], 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int r = 0; r < 4; r++) s[t][r] = there ? s[t][r] * f : -INFINITY;
+                }
+            } else {   // 32 channels at a time, whose products are scaled in fp32
+                const unsigned char* scales = a.c.ke + (size_t)__builtin_amdgcn_readlane(page, i) * P::SCALES;
+#pragma unroll
+                for (int t = 0; t < 4; t++) {
+                    s[t] = f32x4m{0, 0, 0, 0};
+                    for (int j = 0; j < D / 32; j++) {
+                        const bool mine = (D == 128 ? grp : grp / 2) == j;
+                        f32x4m y = {0, 0, 0, 0};
+#pragma unroll
+                        for (int x = 0; x < D / 32; x++) {
+                            const unsigned w = D == 128 ? kc[t][x] : kc[t / 2][2 * (t % 2) + x];
+                            y = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen_e2m1(mine ? w : 0u, 1.0f), qf[x / 2][x % 2], y, 0, 0, 0);
+                        }
+#pragma unroll
+                        for (int r = 0; r < 4; r++) s[t][r] += y[r] * (__uint_as_float((unsigned)scales[(j * 16 + 4 * grp + r) * 4 + t] << 23) * c2q);
+                    }
+#pragma unroll
+                    for (int r = 0; r < 4; r++) s[t][r] = there ? s[t][r] : -INFINITY;
+                }
+            }
+            if (i + 1 < count) load_k(i + 1);
+            f16x8 pb[2];
+            float corr;
+            const float share = soft_unit(s, row, corr, [&](int t, int r, float p) { pb[t >> 1][4 * (t & 1) + r] = (_Float16)p; });
+            if (!vrel.wide) {
+#pragma unroll
+                for (int x = 0; x < NX; x++) {
+                    const float scale = vrel.of(ve[x / 4], x % 4);
+                    f32x4m y = {0, 0, 0, 0};
+                    y = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen_e2m1(vc[x / 2][2 * (x % 2)], scale), pb[0], y, 0, 0, 0);
+                    y = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen_e2m1(vc[x / 2][2 * (x % 2) + 1], scale), pb[1], y, 0, 0, 0);
+#pragma unroll
+                    for (int r = 0; r < 4; r++) acc[x][r] = fmaf(acc[x][r], corr, vrel.unit * y[r]);
+                }
+            } else {   // 32 tokens at a time
+                const unsigned char* scales = a.c.ve + (size_t)__builtin_amdgcn_readlane(page, i) * P::SCALES;
+#pragma unroll
+                for (int x = 0; x < NX; x++)
+                    for (int j = 0; j < 2; j++) {
+                        f32x4m y = {0, 0, 0, 0};
+#pragma unroll
+                        for (int z = 0; z < 2; z++)
+                            y = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen_e2m1(grp / 2 == j ? vc[x / 2][2 * (x % 2) + z] : 0u, 1.0f), pb[z], y, 0, 0, 0);
+#pragma unroll
+                        for (int r = 0; r < 4; r++)
+                            acc[x][r] = fmaf(acc[x][r], j ? 1.0f : corr, y[r] * __uint_as_float((unsigned)scales[(j * 16 + 4 * grp + r) * (D / 16) + x] << 23));
+                    }
+            }
+            if (alone) shares[u0 + i][col] = share;
+            else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(share), wbuf, wat + 4 * (u0 + i), 0, 0);
+            if (i + 1 < count) load_v(i + 1);
+        }
+    } else if (!FOUR && have) {
         unsigned char *kt = tiles[wv], *vt = kt + T::BYTES;
         // A whole cache is streamed past the chip's caches (64 sequences of up to 8192: 148 us -> 130).  Blocks that were chosen are likely
         // to be chosen by the next token again (16 sequences, 16 of 1024 blocks, this kernel alone: 14.4 us where the last cache has them,
@@ -713,7 +880,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void cache8_attn_kernel(Attn
             for (int h = 0; h < KH; h++)
 #pragma unroll
                 for (int x = 0; x < 2; x++)
-                    s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8*)(kp + tok * D + 64 * h + 16 * grp + 8 * x), *(const bf16x8*)(qr + 64 * h + 8 * x), s[t], 0, 0, 0);
+                    s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8*)(kp + tok * D + QH * h + QG * grp + 8 * x), *(const bf16x8*)(qr + QH * h + 8 * x), s[t], 0, 0, 0);
 #pragma unroll
             for (int r = 0; r < 4; r++) s[t][r] = 16 * grp + 4 * t + r < ru.tail ? s[t][r] * a.c2 : -INFINITY;
         }
@@ -934,19 +1101,24 @@ __global__ __launch_bounds__(256) void cache8_evict_kernel(CacheArgs a, int budg
 
 static CacheArgs cache_args(const sparsek_cache8_cfg& c, const sparsek_cache8& t, const int32_t* lens)
 {
-    return CacheArgs{t, c.B, c.H, c.Hkv, c.H / c.Hkv, c.cap, c.pages, lens};
+    return CacheArgs{t, c.B, c.H, c.Hkv, c.H / c.Hkv, c.cap, c.pages, lens, nullptr, nullptr};
+}
+static CacheArgs cache_args(const sparsek_cache8_cfg& c, const sparsek_cache4& t, const int32_t* lens)
+{
+    return CacheArgs{sparsek_cache8{t.k4, t.v4, t.ks, t.vs, t.km, t.kms, t.kt, t.vt, t.table, t.mass}, c.B, c.H, c.Hkv, c.H / c.Hkv, c.cap, c.pages, lens,
+                     t.ke, t.ve};
 }
 
 #define BY_FORMAT(c, LAUNCH)                                                          \
-    if (c.d == 128 && c.format == SPARSEK_I8) { LAUNCH(128, SPARSEK_I8); }            \
+    if (c.format == SPARSEK_E2M1 && c.d == 128) { LAUNCH(128, FORMAT_E2M1); }         \
+    else if (c.format == SPARSEK_E2M1) { LAUNCH(64, FORMAT_E2M1); }                   \
+    else if (c.d == 128 && c.format == SPARSEK_I8) { LAUNCH(128, SPARSEK_I8); }            \
     else if (c.d == 128) { LAUNCH(128, SPARSEK_E4M3); }                               \
     else if (c.format == SPARSEK_I8) { LAUNCH(64, SPARSEK_I8); }                      \
     else { LAUNCH(64, SPARSEK_E4M3); }
 
-int launch_cache8_append(const sparsek_cache8_cfg& c, const sparsek_cache8& t, const int32_t* lens, const int32_t* counts, int count,
-                         const void* k, const void* v, hipStream_t st)
+static int append_launch(const sparsek_cache8_cfg& c, const CacheArgs& a, const int32_t* counts, int count, const void* k, const void* v, hipStream_t st)
 {
-    const CacheArgs a = cache_args(c, t, lens);
     const dim3 grid((unsigned)((count + 2 * BT - 2) / BT), c.B * c.Hkv);   // blocks that `count` tokens from any place touch
 #define APPEND(D, F) hipLaunchKernelGGL((cache8_append_kernel<D, F>), grid, dim3(256), 0, st, a, counts, count, (const uint16_t*)k, (const uint16_t*)v)
     BY_FORMAT(c, APPEND)
@@ -954,9 +1126,8 @@ int launch_cache8_append(const sparsek_cache8_cfg& c, const sparsek_cache8& t, c
     return launch_status();
 }
 
-int launch_cache8_select(const sparsek_cache8_cfg& c, const sparsek_cache8& t, const int32_t* lens, const void* q, int top, int32_t* idx, hipStream_t st)
+static int select_launch(const sparsek_cache8_cfg& c, const CacheArgs& a, const void* q, int top, int32_t* idx, hipStream_t st)
 {
-    const CacheArgs a = cache_args(c, t, lens);
     const size_t lds = (size_t)c.cap * 8;
     if (c.d == 128) hipLaunchKernelGGL((cache8_select_kernel<128>), dim3(c.B * c.Hkv), dim3(1024), lds, st, a, (const uint16_t*)q, top, idx);
     else hipLaunchKernelGGL((cache8_select_kernel<64>), dim3(c.B * c.Hkv), dim3(1024), lds, st, a, (const uint16_t*)q, top, idx);
@@ -988,12 +1159,12 @@ static Cache8Layout cache8_layout(const sparsek_cache8_cfg& c, int top)
 }
 size_t cache8_attn_ws_bytes(const sparsek_cache8_cfg& c, int top) { return cache8_layout(c, top).bytes; }
 
-int launch_cache8_attn(const sparsek_cache8_cfg& c, const sparsek_cache8& t, const int32_t* lens, const void* q, const int32_t* idx, int top,
-                       int accumulate, void* o, float* lse, void* ws, hipStream_t st)
+static int attn_launch(const sparsek_cache8_cfg& c, const CacheArgs& cache, const void* q, const int32_t* idx, int top, int accumulate, void* o,
+                       float* lse, void* ws, hipStream_t st)
 {
     const Cache8Layout y = cache8_layout(c, idx ? top : 0);
     AttnArgs a;
-    a.c = cache_args(c, t, lens);
+    a.c = cache;
     a.q = (const uint16_t*)q;
     a.idx = idx;
     a.top = idx ? top : 0;
@@ -1018,12 +1189,36 @@ int launch_cache8_attn(const sparsek_cache8_cfg& c, const sparsek_cache8& t, con
     return launch_status();
 }
 
-int launch_cache8_evict(const sparsek_cache8_cfg& c, const sparsek_cache8& t, const int32_t* lens, int budget, int sink, int recent,
-                        int32_t* table, float* mass, int32_t* lens_out, hipStream_t st)
+static int evict_launch(const sparsek_cache8_cfg& c, const CacheArgs& a, int budget, int sink, int recent, int32_t* table, float* mass, int32_t* lens_out,
+                        hipStream_t st)
 {
-    const CacheArgs a = cache_args(c, t, lens);
-hipLaunchKernelGGL(cache8_evict_kernel, dim3(c.B * c.Hkv), dim3(256), (size_t)c.cap * 8, st, a, budget, sink, recent, table, mass, lens_out);
+    hipLaunchKernelGGL(cache8_evict_kernel, dim3(c.B * c.Hkv), dim3(256), (size_t)c.cap * 8, st, a, budget, sink, recent, table, mass, lens_out);
     return launch_status();
 }
+
+// The entry points of both caches.
+#define OF_CACHE(NAME, CACHE)                                                                                                                        \
+    int launch_##NAME##_append(const sparsek_cache8_cfg& c, const CACHE& t, const int32_t* lens, const int32_t* counts, int count, const void* k,      \
+                               const void* v, hipStream_t st)                                                                                          \
+    {                                                                                                                                                  \
+        return append_launch(c, cache_args(c, t, lens), counts, count, k, v, st);                                                                      \
+    }                                                                                                                                                  \
+    int launch_##NAME##_select(const sparsek_cache8_cfg& c, const CACHE& t, const int32_t* lens, const void* q, int top, int32_t* idx, hipStream_t st) \
+    {                                                                                                                                                  \
+        return select_launch(c, cache_args(c, t, lens), q, top, idx, st);                                                                              \
+    }                                                                                                                                                  \
+    int launch_##NAME##_attn(const sparsek_cache8_cfg& c, const CACHE& t, const int32_t* lens, const void* q, const int32_t* idx, int top,             \
+                             int accumulate, void* o, float* lse, void* ws, hipStream_t st)                                                            \
+    {                                                                                                                                                  \
+        return attn_launch(c, cache_args(c, t, lens), q, idx, top, accumulate, o, lse, ws, st);                                                        \
+    }                                                                                                                                                  \
+    int launch_##NAME##_evict(const sparsek_cache8_cfg& c, const CACHE& t, const int32_t* lens, int budget, int sink, int recent, int32_t* table,      \
+                              float* mass, int32_t* lens_out, hipStream_t st)                                                                          \
+    {                                                                                                                                                  \
+        return evict_launch(c, cache_args(c, t, lens), budget, sink, recent, table, mass, lens_out, st);                                               \
+    }
+OF_CACHE(cache8, sparsek_cache8)
+OF_CACHE(cache4, sparsek_cache4)
+#undef OF_CACHE
 
 }  // namespace spk
