@@ -841,14 +841,35 @@ def _heads_of(name, t, dtype, shape, device):
     return tuple(t.stride(x) if t.shape[x] > 1 else 0 for x in range(3))
 
 
-def _rope_kept(q, k, pos, freq, axis, interleaved, norm, qw, kw, eps, grads=None):
+def _seen(t):
+    """What the checks of a tensor go by."""
+    return (t.dtype, t.shape, t.stride(), t.device) if t is not None else None
+
+
+_ropes = {}   # configurations by what their tensors look like: a call on tensors like an earlier one's needs no more checks
+
+
+def _rope_kept(q, k, pos, freq, axis, interleaved, norm, qw, kw, eps, grads=(None, None)):
+    key = (_seen(q), _seen(k), _seen(pos), _seen(freq), _seen(axis), _seen(qw), _seen(kw), _seen(grads[0]), _seen(grads[1]), interleaved, norm, eps)
+    got = _ropes.get(key)
+    if got is None:
+        got = _rope_checked(q, k, pos, freq, axis, interleaved, norm, qw, kw, eps, grads)
+        if len(_ropes) >= _CFG_KEPT:
+            _ropes.clear()
+        _ropes[key] = got
+    return got
+
+
+def _rope_checked(q, k, pos, freq, axis, interleaved, norm, qw, kw, eps, grads):
     torch = _torch()
     if q.dim() != 4 or (k is not None and k.dim() != 4):
         raise ValueError("q is [B,n,H,d] and k is [B,n,Hkv,d]")
     B, n, H, d = q.shape
     Hkv, dev = k.shape[2] if k is not None else 0, q.device
     dtype = _dtype_code(q)
-    strides = [_heads_of("q", q, q.dtype, (B, n, H, d), dev), _heads_of("k", k, q.dtype, (B, n, Hkv, d), dev) if k is not None else (0, 0, 0)]
+    none = (0, 0, 0)
+    strides = [_heads_of(name, t, q.dtype, (B, n, heads, d), dev) if t is not None else none
+               for name, t, heads in (("q", q, H), ("k", k, Hkv), ("dq", grads[0], H), ("dk", grads[1], Hkv))]
     rot, axes = 2 * freq.shape[0] if freq is not None else 0, 1
     if rot:
         if pos is None or pos.dim() != 3:
@@ -863,10 +884,6 @@ def _rope_kept(q, k, pos, freq, axis, interleaved, norm, qw, kw, eps, grads=None
             if not norm:
                 raise ValueError("%s without norm" % name)
             _same(name, w, torch.float32, (d,), dev)
-    for name, t in (("dq", grads[0]), ("dk", grads[1])) if grads else ():
-        heads = H if name == "dq" else Hkv
-        strides.append(_heads_of(name, t, q.dtype, (B, n, heads, d), dev) if t is not None else (0, 0, 0))
-    strides += [(0, 0, 0)] * (4 - len(strides))
     return _kept("rope", (B, H, Hkv, n, d, rot, axes, int(bool(interleaved)), int(bool(norm)), dtype, float(eps), *strides), _make_rope_cfg)
 
 
@@ -874,12 +891,10 @@ def sparsek_rope_fwd(q, k, pos, freq, axis=None, interleaved=False, norm=False, 
     """Queries q [B,n,H,d] and keys k [B,n,Hkv,d] (any strides of batch, token and head; k None: queries alone) with each head's norm, if
     norm, weighted by qw, kw [d] fp32, if given, and turned by their positions: pair p by pos[axis[p]] * freq[p] (pos [axes,B,n] int32, freq
     [rot/2] fp32 or None, axis [rot/2] int32, None: the first).  Returns qo [B,H,n,d] and ko [B,Hkv,n,d] (None without k), new or those of `out`."""
-    torch = _torch()
     cfg = _rope_kept(q, k, pos, freq, axis, interleaved, norm, qw, kw, eps)
     B, n, H, d = q.shape
     if out is None:
-        qo = torch.empty(B, H, n, d, dtype=q.dtype, device=q.device)
-        ko = torch.empty(B, k.shape[2], n, d, dtype=q.dtype, device=q.device) if k is not None else None
+        qo, ko = q.new_empty((B, H, n, d)), k.new_empty((B, k.shape[2], n, d)) if k is not None else None
     else:
         qo, ko = out
         _same("out q", qo, q.dtype, (B, H, n, d), q.device)
@@ -893,14 +908,13 @@ def sparsek_rope_fwd(q, k, pos, freq, axis=None, interleaved=False, norm=False, 
 def sparsek_rope_bwd(q, k, pos, freq, dqo, dko, axis=None, interleaved=False, norm=False, qw=None, kw=None, eps=1e-6, out=None, ws=None):
     """dq [B,n,H,d], dk [B,n,Hkv,d], dqw, dkw [d] fp32 (None where there is no such weight): gradients of sum(dqo*qo) + sum(dko*ko) for the
     outputs of sparsek_rope_fwd on the same arguments.  out: (dq, dk) to write to, in any strides (slices of a fused gradient)."""
-    torch = _torch()
     B, n, H, d = q.shape
     if out is None:
-        out = (torch.empty(q.shape, dtype=q.dtype, device=q.device), torch.empty(k.shape, dtype=q.dtype, device=q.device) if k is not None else None)
+        out = q.new_empty(q.shape), k.new_empty(k.shape) if k is not None else None
     dq, dk = out
     if (dk is None) != (k is None) or (dko is None) != (k is None):
         raise ValueError("k, dko and dk go together")
-    cfg = _rope_kept(q, k, pos, freq, axis, interleaved, norm, qw, kw, eps, grads=(dq, dk))
+    cfg = _rope_kept(q, k, pos, freq, axis, interleaved, norm, qw, kw, eps, out)
     _same("dqo", dqo, q.dtype, (B, H, n, d), q.device)
     if k is not None:
         _same("dko", dko, q.dtype, (B, k.shape[2], n, d), q.device)

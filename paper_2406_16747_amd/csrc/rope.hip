@@ -24,49 +24,56 @@ struct RopeArgs {
     int tiles;       // of a workgroup's tokens
 };
 
+constexpr int W = 4;   // channels of a lane in either half (eight bf16 values, 16 bytes to a load: 138 us for a document of 32768 too)
+
+// W values of storage type T, as they lie and in fp32.
 template <class T>
-struct Four {   // 4 values of storage type T
-    static __device__ __forceinline__ void load(const T* p, float (&x)[4]);
-    static __device__ __forceinline__ void store(T* p, const float (&x)[4]);
-};
+struct Some;
 template <>
-struct Four<uint16_t> {
-    static __device__ __forceinline__ void load(const uint16_t* p, float (&x)[4])
+struct Some<uint16_t> {
+    typedef u32x2 Raw;
+    static __device__ __forceinline__ void widen(Raw w, float (&x)[W])
     {
-        const u32x2 w = *(const u32x2*)p;
 #pragma unroll
-        for (int e = 0; e < 4; e++) x[e] = __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
+        for (int e = 0; e < W; e++) x[e] = __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
     }
-    static __device__ __forceinline__ void store(uint16_t* p, const float (&x)[4])
+    static __device__ __forceinline__ Raw narrow(const float (&x)[W])
     {
-        u32x2 w;
-#pragma unroll
-        for (int e = 0; e < 2; e++) w[e] = (unsigned)f32_to_bf16(x[2 * e]) | (unsigned)f32_to_bf16(x[2 * e + 1]) << 16;
-        *(u32x2*)p = w;
+        return Raw{(unsigned)f32_to_bf16(x[0]) | (unsigned)f32_to_bf16(x[1]) << 16, (unsigned)f32_to_bf16(x[2]) | (unsigned)f32_to_bf16(x[3]) << 16};
     }
 };
 template <>
-struct Four<float> {
-    static __device__ __forceinline__ void load(const float* p, float (&x)[4])
+struct Some<float> {
+    typedef u32x4 Raw;
+    static __device__ __forceinline__ void widen(Raw w, float (&x)[W])
     {
-        const u32x4 w = *(const u32x4*)p;
 #pragma unroll
-        for (int e = 0; e < 4; e++) x[e] = __uint_as_float(w[e]);
+        for (int e = 0; e < W; e++) x[e] = __uint_as_float(w[e]);
     }
-    static __device__ __forceinline__ void store(float* p, const float (&x)[4])
+    static __device__ __forceinline__ Raw narrow(const float (&x)[W])
     {
-        u32x4 w;
-#pragma unroll
-        for (int e = 0; e < 4; e++) w[e] = __float_as_uint(x[e]);
-        *(u32x4*)p = w;
+        return Raw{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
     }
 };
+// What a call reads and writes goes past the chip's caches where it is more than the last of them holds.
+template <bool STREAM, class Raw>
+__device__ __forceinline__ Raw load(const void* p)
+{
+    if constexpr (STREAM) return __builtin_nontemporal_load((const Raw*)p);
+    else return *(const Raw*)p;
+}
+template <bool STREAM, class Raw>
+__device__ __forceinline__ void store(void* p, Raw x)
+{
+    if constexpr (STREAM) __builtin_nontemporal_store(x, (Raw*)p);
+    else *(Raw*)p = x;
+}
 
 // The sum over LPR neighbouring lanes.
 template <int LPR>
 __device__ __forceinline__ float row_sum(float x)
 {
-    x += dpp_f32(x, 0);
+    if constexpr (LPR > 1) x += dpp_f32(x, 0);
     if constexpr (LPR > 2) x += dpp_f32(x, 1);
     if constexpr (LPR > 4) x += dpp_f32(x, 2);
     if constexpr (LPR > 8) x += dpp_f32(x, 3);
@@ -77,38 +84,42 @@ __device__ __forceinline__ float row_sum(float x)
     return x;
 }
 
-// Which channels a lane has: four from a, four from b.
+// Which channels a lane has: W from a, W from b, and which of the angles turn them.  A row's lanes have neighbouring ones, so each load or
+// store of a row is one of whole lines (eight neighbours of fp32 in two loads to a lane: 82 us instead of 60, 16 x 2000 tokens forward).
 struct Chunk {
-    int a, b, pair;   // pair: of a's first channel (interleaved: b's are two on), -1: they do not turn
+    int a, b, pa, pb;   // the first pair of a's and of b's channels (not interleaved: of both), -1: they do not turn
 };
 __device__ __forceinline__ Chunk chunk_of(const RopeArgs& p, int c)
 {
-    if (8 * c >= p.rot) return Chunk{8 * c, 8 * c + 4, -1};
-    if (p.interleaved) return Chunk{8 * c, 8 * c + 4, 4 * c};
-    return Chunk{4 * c, p.rot / 2 + 4 * c, 4 * c};
+    if (p.interleaved) {
+        const int a = W * c, b = p.d / 2 + W * c;
+        return Chunk{a, b, a < p.rot ? a / 2 : -1, b < p.rot ? b / 2 : -1};
+    }
+    if (2 * W * c < p.rot) return Chunk{W * c, p.rot / 2 + W * c, W * c, W * c};
+    const int a = p.rot / 2 + W * c;   // (rot + W (c - rot / 2W))
+    return Chunk{a, a + (p.d - p.rot) / 2, -1, -1};
 }
 
-// cos and sin of the lane's four pairs.  The angle in turns, pos freq / (2 pi), is made and reduced in 64 bits: at position 2^31 and a
+// cos and sin of the lane's W pairs.  The angle in turns, pos freq / (2 pi), is made and reduced in 64 bits: at position 2^31 and a
 // frequency of 1 it is off by 2^-24 of a turn.
-__device__ __forceinline__ void angles(const RopeArgs& p, const Chunk& ch, unsigned token, float (&co)[4], float (&si)[4])
+__device__ __forceinline__ void angles(const RopeArgs& p, const Chunk& ch, unsigned token, float (&co)[W], float (&si)[W])
 {
 #pragma unroll
-    for (int e = 0; e < 4; e++) {
+    for (int e = 0; e < W; e++) {
+        const bool second = p.interleaved && e >= W / 2;
+        const int first = second ? ch.pb : ch.pa;
         co[e] = 1.0f;
         si[e] = 0.0f;
-    }
-    if (ch.pair < 0) return;
-#pragma unroll
-    for (int e = 0; e < 4; e++) {
-        const int x = ch.pair + e, ax = p.axis ? min(max(p.axis[x], 0), p.axes - 1) : 0;
+        if (first < 0) continue;
+        const int x = first + e - (second ? W / 2 : 0), ax = p.axis ? min(max(p.axis[x], 0), p.axes - 1) : 0;
         const double turns = (double)p.pos[(size_t)ax * p.B * p.n + token] * ((double)p.freq[x] * 0.15915494309189533577);
         const float t = (float)(turns - rint(turns));
         sincospif(2.0f * t, &si[e], &co[e]);
     }
 }
 
-// The four pairs of a lane turn (back: the other way).
-__device__ __forceinline__ void turn(bool interleaved, bool back, const float (&co)[4], const float (&si)[4], float (&a)[4], float (&b)[4])
+// The W pairs of a lane turn (back: the other way).
+__device__ __forceinline__ void turn(bool interleaved, bool back, const Chunk& ch, const float (&co)[W], const float (&si)[W], float (&a)[W], float (&b)[W])
 {
     auto one = [&](float& x, float& y, float c, float s) {
         s = back ? -s : s;
@@ -117,130 +128,161 @@ __device__ __forceinline__ void turn(bool interleaved, bool back, const float (&
         x = z;
     };
     if (interleaved) {
-        one(a[0], a[1], co[0], si[0]);
-        one(a[2], a[3], co[1], si[1]);
-        one(b[0], b[1], co[2], si[2]);
-        one(b[2], b[3], co[3], si[3]);
-    } else {
+        if (ch.pa >= 0)
 #pragma unroll
-        for (int e = 0; e < 4; e++) one(a[e], b[e], co[e], si[e]);
+            for (int e = 0; e < W / 2; e++) one(a[2 * e], a[2 * e + 1], co[e], si[e]);
+        if (ch.pb >= 0)
+#pragma unroll
+            for (int e = 0; e < W / 2; e++) one(b[2 * e], b[2 * e + 1], co[W / 2 + e], si[W / 2 + e]);
+    } else if (ch.pa >= 0) {
+#pragma unroll
+        for (int e = 0; e < W; e++) one(a[e], b[e], co[e], si[e]);
     }
 }
 
+// Rows of a token that are on their way together.  Four where much is streamed in bf16 (a document of 32768, 32 + 8 heads of 128: 138 us, one
+// at a time 140; training on it 300 and 308); one is faster where the caches have it (two prompts of 5003: 19.0 us, four 20.4), and in fp32, whose
+// rows are twice as long (a training pass of 4 x 2000, 24 heads of 64: 55 us, four 63; of 16 x 2000 199 and 198).
+template <class T, bool STREAM>
+constexpr int rows_at_once() { return STREAM && sizeof(T) == 2 ? 4 : 1; }
+
 struct Weights {
-    float a[4], b[4];
+    float a[W], b[W];
     __device__ __forceinline__ void load(const float* w, const Chunk& ch, bool live)
     {
 #pragma unroll
-        for (int e = 0; e < 4; e++) {
+        for (int e = 0; e < W; e++) {
             a[e] = w && live ? w[ch.a + e] : 1.0f;
             b[e] = w && live ? w[ch.b + e] : 1.0f;
         }
     }
 };
 
-template <class T, int LPR>
+template <class T, int LPR, bool STREAM>
 __global__ __launch_bounds__(256) void rope_fwd_kernel(RopeArgs p)
 {
-    constexpr int TOK = 256 / LPR;
+    constexpr int TOK = 256 / LPR, ROWS = rows_at_once<T, STREAM>();
     const int c = threadIdx.x % LPR;
     const unsigned token = blockIdx.x * TOK + threadIdx.x / LPR, all = (unsigned)p.B * p.n;   // (below 2^31)
-    const bool live = token < all && 8 * c < p.d;
+    const bool live = token < all && 2 * W * c < p.d;
     const Chunk ch = chunk_of(p, live ? c : 0);
     const unsigned at = live ? token : 0, b = at / p.n, t = at - b * p.n;
-    float co[4], si[4];
+    float co[W], si[W];
     angles(p, ch, at, co, si);
     const int h0 = blockIdx.y * p.heads, h1 = min(h0 + p.heads, p.H + p.Hkv);
     auto part = [&](const T* x, long long step, T* out, const float* wts, int from, int to) {   // x, out: of head 0
+        typedef typename Some<T>::Raw Raw;
         Weights w;
         w.load(wts, ch, live);
-        for (int h = from; h < to; h++) {
-            float xa[4] = {0, 0, 0, 0}, xb[4] = {0, 0, 0, 0};
-            if (live) {
-                Four<T>::load(x + h * step + ch.a, xa);
-                Four<T>::load(x + h * step + ch.b, xb);
+        for (int hr = from; hr < to; hr += ROWS) {
+            Raw ra[ROWS], rb[ROWS];
+#pragma unroll
+            for (int u = 0; u < ROWS; u++) {   // (on their way together)
+                const T* row = x + min(hr + u, to - 1) * step;
+                ra[u] = load<STREAM, Raw>(row + ch.a);
+                rb[u] = load<STREAM, Raw>(row + ch.b);
             }
-            if (p.norm) {
-                float s = 0.0f;
 #pragma unroll
-                for (int e = 0; e < 4; e++) s = fmaf(xa[e], xa[e], fmaf(xb[e], xb[e], s));
-                const float r = rsqrtf(row_sum<LPR>(s) * p.inv_d + p.eps);
+            for (int u = 0; u < ROWS; u++) {
+                float xa[W], xb[W];
+                Some<T>::widen(ra[u], xa);
+                Some<T>::widen(rb[u], xb);
+                if (p.norm) {
+                    float s = 0.0f;
 #pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    xa[e] *= r * w.a[e];
-                    xb[e] *= r * w.b[e];
+                    for (int e = 0; e < W; e++) s = fmaf(xa[e], xa[e], fmaf(xb[e], xb[e], s));
+                    const float r = rsqrtf(row_sum<LPR>(live ? s : 0.0f) * p.inv_d + p.eps);
+#pragma unroll
+                    for (int e = 0; e < W; e++) {
+                        xa[e] *= r * w.a[e];
+                        xb[e] *= r * w.b[e];
+                    }
                 }
-            }
-            if (ch.pair >= 0) turn(p.interleaved, false, co, si, xa, xb);
-            if (live) {
-                T* o = out + (long long)h * p.n * p.d;
-                Four<T>::store(o + ch.a, xa);
-                Four<T>::store(o + ch.b, xb);
+                turn(p.interleaved, false, ch, co, si, xa, xb);
+                if (live && hr + u < to) {
+                    T* o = out + (size_t)(hr + u) * p.n * p.d;
+                    store<STREAM, Raw>(o + ch.a, Some<T>::narrow(xa));
+                    store<STREAM, Raw>(o + ch.b, Some<T>::narrow(xb));
+                }
             }
         }
     };
-    part((const T*)p.q + b * p.qs.batch + t * p.qs.token, p.qs.head, (T*)p.qo + ((size_t)b * p.H * p.n + t) * p.d, p.qw, h0, min(h1, p.H));
+    if (h0 < p.H) part((const T*)p.q + b * p.qs.batch + t * p.qs.token, p.qs.head, (T*)p.qo + ((size_t)b * p.H * p.n + t) * p.d, p.qw, h0, min(h1, p.H));
     if (h1 > p.H) part((const T*)p.k + b * p.ks.batch + t * p.ks.token, p.ks.head, (T*)p.ko + ((size_t)b * p.Hkv * p.n + t) * p.d, p.kw, max(h0 - p.H, 0), h1 - p.H);
 }
 
 // A workgroup takes `tiles` groups of tokens one after another and all of its heads, and leaves its part of the sums for the weights.
-template <class T, int LPR>
+template <class T, int LPR, bool STREAM>
 __global__ __launch_bounds__(256) void rope_bwd_kernel(RopeArgs p)
 {
-    constexpr int TOK = 256 / LPR;
-    __shared__ float sums[TOK][8 * LPR + 1];
+    constexpr int TOK = 256 / LPR, ROWS = rows_at_once<T, STREAM>();
+    __shared__ float sums[TOK][2 * W * LPR + 1];
     const int c = threadIdx.x % LPR, row = threadIdx.x / LPR;
     const unsigned all = (unsigned)p.B * p.n;
     const int h0 = blockIdx.y * p.heads, h1 = min(h0 + p.heads, p.H + p.Hkv);
-    const Chunk ch = chunk_of(p, 8 * c < p.d ? c : 0);
-    float wsum[2][8];
+    const Chunk ch = chunk_of(p, 2 * W * c < p.d ? c : 0);
+    float wsum[2][2 * W];
 #pragma unroll
-    for (int e = 0; e < 8; e++) wsum[0][e] = wsum[1][e] = 0.0f;
+    for (int e = 0; e < 2 * W; e++) wsum[0][e] = wsum[1][e] = 0.0f;
     for (int tile = 0; tile < p.tiles; tile++) {
         const unsigned token = (blockIdx.x * p.tiles + tile) * TOK + row;   // (below 2^31 and a workgroup's share)
-        const bool live = token < all && 8 * c < p.d;
+        const bool live = token < all && 2 * W * c < p.d;
         const unsigned at = live ? token : 0, b = at / p.n, t = at - b * p.n;
-        float co[4], si[4];
+        float co[W], si[W];
         angles(p, ch, at, co, si);
-        auto part = [&](const T* x, long long step, const T* dout, T* dx, long long dstep, const float* wts, float (&ws)[8], int from, int to) {
+        auto part = [&](const T* x, long long step, const T* dout, T* dx, long long dstep, const float* wts, float (&ws)[2 * W], int from, int to) {
+            typedef typename Some<T>::Raw Raw;
             Weights w;
             w.load(wts, ch, live);
-            for (int h = from; h < to; h++) {
-                float ga[4] = {0, 0, 0, 0}, gb[4] = {0, 0, 0, 0};
-                if (live) {
-                    const T* g = dout + (long long)h * p.n * p.d;
-                    Four<T>::load(g + ch.a, ga);
-                    Four<T>::load(g + ch.b, gb);
-                }
-                if (ch.pair >= 0) turn(p.interleaved, true, co, si, ga, gb);
-                if (p.norm) {
-                    float xa[4] = {0, 0, 0, 0}, xb[4] = {0, 0, 0, 0}, s = 0.0f, m = 0.0f;
-                    if (live) {
-                        Four<T>::load(x + h * step + ch.a, xa);
-                        Four<T>::load(x + h * step + ch.b, xb);
-                    }
+            for (int hr = from; hr < to; hr += ROWS) {
+                Raw rga[ROWS], rgb[ROWS], rxa[ROWS], rxb[ROWS];
 #pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        s = fmaf(xa[e], xa[e], fmaf(xb[e], xb[e], s));
-                        m = fmaf(xa[e] * w.a[e], ga[e], fmaf(xb[e] * w.b[e], gb[e], m));
-                    }
-                    const float r = rsqrtf(row_sum<LPR>(s) * p.inv_d + p.eps);
-                    const float f = r * r * (row_sum<LPR>(m) * p.inv_d);
-#pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        ws[e] = fmaf(xa[e] * r, ga[e], ws[e]);
-                        ws[4 + e] = fmaf(xb[e] * r, gb[e], ws[4 + e]);
-                        ga[e] = r * (w.a[e] * ga[e] - xa[e] * f);
-                        gb[e] = r * (w.b[e] * gb[e] - xb[e] * f);
+                for (int u = 0; u < ROWS; u++) {   // (on their way together)
+                    const int h = min(hr + u, to - 1);
+                    const T *g = dout + (size_t)h * p.n * p.d, *row = x + h * step;
+                    rga[u] = load<STREAM, Raw>(g + ch.a);
+                    rgb[u] = load<STREAM, Raw>(g + ch.b);
+                    if (p.norm) {
+                        rxa[u] = load<STREAM, Raw>(row + ch.a);
+                        rxb[u] = load<STREAM, Raw>(row + ch.b);
                     }
                 }
-                if (live) {
-                    Four<T>::store(dx + h * dstep + ch.a, ga);
-                    Four<T>::store(dx + h * dstep + ch.b, gb);
+#pragma unroll
+                for (int u = 0; u < ROWS; u++) {
+                    const bool real = live && hr + u < to;
+                    float ga[W], gb[W];
+                    Some<T>::widen(rga[u], ga);
+                    Some<T>::widen(rgb[u], gb);
+                    turn(p.interleaved, true, ch, co, si, ga, gb);
+                    if (p.norm) {
+                        float xa[W], xb[W], s = 0.0f, m = 0.0f;
+                        Some<T>::widen(rxa[u], xa);
+                        Some<T>::widen(rxb[u], xb);
+#pragma unroll
+                        for (int e = 0; e < W; e++) {
+                            s = fmaf(xa[e], xa[e], fmaf(xb[e], xb[e], s));
+                            m = fmaf(xa[e] * w.a[e], ga[e], fmaf(xb[e] * w.b[e], gb[e], m));
+                        }
+                        const float r = rsqrtf(row_sum<LPR>(live ? s : 0.0f) * p.inv_d + p.eps);
+                        const float f = r * r * (row_sum<LPR>(live ? m : 0.0f) * p.inv_d);
+#pragma unroll
+                        for (int e = 0; e < W; e++) {
+                            ws[e] += real ? xa[e] * r * ga[e] : 0.0f;
+                            ws[W + e] += real ? xb[e] * r * gb[e] : 0.0f;
+                            ga[e] = r * (w.a[e] * ga[e] - xa[e] * f);
+                            gb[e] = r * (w.b[e] * gb[e] - xb[e] * f);
+                        }
+                    }
+                    if (real) {
+                        T* o = dx + (hr + u) * dstep;
+                        store<STREAM, Raw>(o + ch.a, Some<T>::narrow(ga));
+                        store<STREAM, Raw>(o + ch.b, Some<T>::narrow(gb));
+                    }
                 }
             }
         };
-        part((const T*)p.q + b * p.qs.batch + t * p.qs.token, p.qs.head, (const T*)p.dqo + ((size_t)b * p.H * p.n + t) * p.d,
+        if (h0 < p.H)
+            part((const T*)p.q + b * p.qs.batch + t * p.qs.token, p.qs.head, (const T*)p.dqo + ((size_t)b * p.H * p.n + t) * p.d,
              (T*)p.dq + b * p.dqs.batch + t * p.dqs.token, p.dqs.head, p.qw, wsum[0], h0, min(h1, p.H));
         if (h1 > p.H)
             part((const T*)p.k + b * p.ks.batch + t * p.ks.token, p.ks.head, (const T*)p.dko + ((size_t)b * p.Hkv * p.n + t) * p.d,
@@ -251,11 +293,11 @@ __global__ __launch_bounds__(256) void rope_bwd_kernel(RopeArgs p)
 #pragma unroll
     for (int w = 0; w < 2; w++) {
         if (w) __syncthreads();
-        if (8 * c < p.d)
+        if (2 * W * c < p.d)
 #pragma unroll
-            for (int e = 0; e < 4; e++) {
+            for (int e = 0; e < W; e++) {
                 sums[row][ch.a + e] = wsum[w][e];
-                sums[row][ch.b + e] = wsum[w][4 + e];
+                sums[row][ch.b + e] = wsum[w][W + e];
             }
         __syncthreads();
         for (int x = threadIdx.x; x < p.d; x += 256) {
@@ -267,21 +309,23 @@ __global__ __launch_bounds__(256) void rope_bwd_kernel(RopeArgs p)
 }
 
 // The workgroups' parts are added up in 64 bits, in an order of their own: 8 columns of dqw and dkw to a workgroup.
-__global__ __launch_bounds__(256) void rope_weights_kernel(const float* __restrict__ part, int parts, int d, float* __restrict__ dqw, float* __restrict__ dkw)
+__global__ __launch_bounds__(1024) void rope_weights_kernel(const float* __restrict__ part, int parts, int d, float* __restrict__ dqw, float* __restrict__ dkw)
 {
-    __shared__ double sums[32][8];
-    const int row = threadIdx.x / 8, x = blockIdx.x * 8 + threadIdx.x % 8;
+    __shared__ double sums[128][9];
+    const int row = threadIdx.x / 8, col = threadIdx.x % 8, x = blockIdx.x * 8 + col;
     double y = 0;
 #pragma unroll 8
-    for (int r = row; r < parts; r += 32) y += (double)part[(size_t)r * 2 * d + x];
-    sums[row][threadIdx.x % 8] = y;
+    for (int r = row; r < parts; r += 128) y += (double)part[(size_t)r * 2 * d + x];
+    sums[row][col] = y;
     __syncthreads();
-    if (threadIdx.x >= 8) return;
+    if (row >= 8) return;
     y = 0;
 #pragma unroll
-    for (int r = 0; r < 32; r++) y += sums[r][threadIdx.x];
+    for (int r = 0; r < 16; r++) y += sums[row + 8 * r][col];
+#pragma unroll
+    for (int z = 8; z < 64; z *= 2) y += __shfl_xor(y, z, 64);   // (the first wave)
     float* out = x < d ? dqw : dkw;
-    if (out) out[x % d] = (float)y;
+    if (row == 0 && out) out[x % d] = (float)y;
 }
 
 // ---- launches ----
@@ -293,11 +337,18 @@ struct RopeShape {
 static RopeShape rope_shape(const sparsek_rope_cfg& c)
 {
     RopeShape s;
-    s.lpr = 2;
-    while (8 * s.lpr < c.d) s.lpr *= 2;
+    s.lpr = 1;
+    while (2 * W * s.lpr < c.d) s.lpr *= 2;
     s.tok = 256 / s.lpr;
     s.groups = ((long long)c.B * c.n + s.tok - 1) / s.tok;
     return s;
+}
+// Whether a call that reads or writes every value `passes` times does not fit the last cache, of 256 MB (streamed and not: a document of 32768, 671
+// MB, 138 and 148 us; forward of 16 x 2000 tokens in fp32, 393 MB, 76 and 82; two prompts of 5003, 92 MB, 27 and 19; forward of 4 x 2000 in fp32, 98
+// MB, 20 and 17).
+static bool rope_streams(const sparsek_rope_cfg& c, int passes)
+{
+    return (double)passes * c.B * c.n * (c.H + c.Hkv) * c.d * (c.dtype == SPARSEK_BF16 ? 2 : 4) > 256e6;
 }
 static RopeArgs rope_args(const sparsek_rope_cfg& c, const void* q, const void* k, const int32_t* pos, const float* freq, const int32_t* axis,
                           const float* qw, const float* kw)
@@ -311,20 +362,16 @@ static RopeArgs rope_args(const sparsek_rope_cfg& c, const void* q, const void* 
     return a;
 }
 
-#define BY_ROW(c, lpr, LAUNCH)                                       \
-    if (c.dtype == SPARSEK_BF16) {                                   \
-        if (lpr == 2) { LAUNCH(uint16_t, 2); }                       \
-        else if (lpr == 4) { LAUNCH(uint16_t, 4); }                  \
-        else if (lpr == 8) { LAUNCH(uint16_t, 8); }                  \
-        else if (lpr == 16) { LAUNCH(uint16_t, 16); }                \
-        else { LAUNCH(uint16_t, 32); }                               \
-    } else {                                                         \
-        if (lpr == 2) { LAUNCH(float, 2); }                          \
-        else if (lpr == 4) { LAUNCH(float, 4); }                     \
-        else if (lpr == 8) { LAUNCH(float, 8); }                     \
-        else if (lpr == 16) { LAUNCH(float, 16); }                   \
-        else { LAUNCH(float, 32); }                                  \
-    }
+#define BY_LANES(T, lpr, stream, LAUNCH)                                                      \
+    if (lpr == 1) { if (stream) { LAUNCH(T, 1, true); } else { LAUNCH(T, 1, false); } }        \
+    else if (lpr == 2) { if (stream) { LAUNCH(T, 2, true); } else { LAUNCH(T, 2, false); } }   \
+    else if (lpr == 4) { if (stream) { LAUNCH(T, 4, true); } else { LAUNCH(T, 4, false); } }   \
+    else if (lpr == 8) { if (stream) { LAUNCH(T, 8, true); } else { LAUNCH(T, 8, false); } }   \
+    else if (lpr == 16) { if (stream) { LAUNCH(T, 16, true); } else { LAUNCH(T, 16, false); } } \
+    else { if (stream) { LAUNCH(T, 32, true); } else { LAUNCH(T, 32, false); } }
+#define BY_ROW(c, lpr, stream, LAUNCH)                                     \
+    if (c.dtype == SPARSEK_F32) { BY_LANES(float, lpr, stream, LAUNCH) }   \
+    else { BY_LANES(uint16_t, lpr, stream, LAUNCH) }
 
 // Workgroups that share a token's heads: as many as leave 2048 in all.
 static int head_shares(long long groups, int heads) { return (int)std::max<long long>(1, std::min<long long>(heads, 2048 / std::max<long long>(groups, 1))); }
@@ -338,8 +385,9 @@ int launch_rope_fwd(const sparsek_rope_cfg& c, const void* q, const void* k, con
     const int heads = c.H + c.Hkv, shares = head_shares(s.groups, heads);
     a.heads = (heads + shares - 1) / shares;
     const dim3 grid((unsigned)s.groups, (heads + a.heads - 1) / a.heads);
-#define FWD(T, L) hipLaunchKernelGGL((rope_fwd_kernel<T, L>), grid, dim3(256), 0, st, a)
-    BY_ROW(c, s.lpr, FWD)
+    const bool stream = rope_streams(c, 2);
+#define FWD(T, L, S) hipLaunchKernelGGL((rope_fwd_kernel<T, L, S>), grid, dim3(256), 0, st, a)
+    BY_ROW(c, s.lpr, stream, FWD)
 #undef FWD
     return launch_status();
 }
@@ -376,10 +424,11 @@ int launch_rope_bwd(const sparsek_rope_cfg& c, const void* q, const void* k, con
     a.heads = y.heads;
     a.tiles = y.tiles;
     a.part = dqw || dkw ? (float*)ws : nullptr;
-#define BWD(T, L) hipLaunchKernelGGL((rope_bwd_kernel<T, L>), dim3(y.gx, y.gy), dim3(256), 0, st, a)
-    BY_ROW(c, y.s.lpr, BWD)
+    const bool stream = rope_streams(c, c.norm ? 3 : 2);
+#define BWD(T, L, S) hipLaunchKernelGGL((rope_bwd_kernel<T, L, S>), dim3(y.gx, y.gy), dim3(256), 0, st, a)
+    BY_ROW(c, y.s.lpr, stream, BWD)
 #undef BWD
-    if (a.part) hipLaunchKernelGGL(rope_weights_kernel, dim3(c.d / 4), dim3(256), 0, st, a.part, (int)(y.gx * y.gy), c.d, dqw, dkw);
+    if (a.part) hipLaunchKernelGGL(rope_weights_kernel, dim3(c.d / 4), dim3(1024), 0, st, a.part, (int)(y.gx * y.gy), c.d, dqw, dkw);
     return launch_status();
 }
 
