@@ -67,18 +67,20 @@ __device__ __forceinline__ float page_scale(float top, int lowest)
 // In fp16 a page's values stand relative to its largest scale, which becomes 2^13 (6 times that is below fp16's largest number): all of them are
 // exact unless the page is wide, whose products are scaled in fp32 instead.
 struct Relative {
-    int add;      // to a scale's biased exponent
+    int low;      // what a scale's biased exponent counts as at least (that of a group of zeros: 0)
+    unsigned add; // to the exponent, in its place in a float
     float unit;   // what 1 stands for in the products; NaN of a page with a value that is not finite
     bool wide;
     __device__ __forceinline__ explicit Relative(float largest)
     {
         const unsigned b = __float_as_uint(largest);
         const int e = (int)(b >> 23) & 255;
-        add = 127 + 13 - e;
+        low = max(e - 139, 0);
+        add = (unsigned)(127 + 13 - e) << 23;
         wide = (b & 0x7FFFFFu) && e < 255;
         unit = largest * 0x1p-13f;
     }
-    __device__ __forceinline__ float of(unsigned scales, int byte) const { return __uint_as_float((unsigned)max((int)(scales >> 8 * byte & 255) + add, 1) << 23); }
+    __device__ __forceinline__ float of(unsigned scales, int byte) const { return __uint_as_float(((unsigned)max((int)(scales >> 8 * byte & 255), low) << 23) + add); }
 };
 
 }  // namespace spk

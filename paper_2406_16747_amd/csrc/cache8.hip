@@ -457,7 +457,7 @@ __global__ __launch_bounds__(1024) void cache8_select_kernel(CacheArgs a, const 
 // bits are exact in fp16; so is q relative to its largest value (what fp16 drops lies 2^-27 below it), and weights lose 2^-11
 // where bf16 would lose 2^-8.  What bounds it is memory: a wave has the keys of one block or the values of another on
 // their way while it computes.
-constexpr int MAX_UPW = 5, MAX_CAP = 8192;   // units of a wave, blocks of a row at most
+constexpr int MAX_UPW = 10, MAX_CAP = 8192;   // units of a wave, blocks of a row at most
 struct AttnArgs {
     CacheArgs c;
     const uint16_t* q;
@@ -611,18 +611,23 @@ struct CacheTile {
 };
 
 template <int D, int FORMAT>
-__global__ __launch_bounds__(256, D == 128 ? 2 : 4) void cache8_attn_kernel(AttnArgs a)
+__global__ __launch_bounds__(256, FORMAT == FORMAT_E2M1 ? 3 : D == 128 ? 2 : 4) void cache8_attn_kernel(AttnArgs a)
 {
     using T = CacheTile<D>;
     constexpr int KH = D / 64, NX = D / 16, RO = D + 4;
     constexpr bool FOUR = FORMAT == FORMAT_E2M1;
-    __shared__ __attribute__((aligned(16))) unsigned char tiles[4][FOUR ? 16 * RO * 4 : 2 * T::BYTES];   // a wave's keys and values; its result at the end
+    constexpr int T4 = BT * D + 512;   // a page's codes, and its scales in two times 256 bytes
+    static_assert(16 * RO * 4 <= T4 && 1024 * (NX < 4 ? 4 : NX) <= T4, "room for a wave's result, and for the products of a wide page");
+    __shared__ __attribute__((aligned(16))) unsigned char tiles[4][FOUR ? T4 : 2 * T::BYTES];   // a wave's keys and values; its result at the end
     __shared__ float sm_[4][16], sl[4][16], shares[4 * MAX_UPW + 1][16];
     __shared__ unsigned seen[MAX_CAP / 32];
     static_assert(16 * RO * 4 <= 2 * T::BYTES, "room for a wave's result");
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, grp = lane >> 4;
     const int groups = (a.c.G + 15) / 16;
-    const int split = blockIdx.x, g = blockIdx.y / groups, rg = blockIdx.y % groups, b = blockIdx.z;
+    // Workgroups go to the chip's 8 partitions in turn.  The heads of a sequence, all of one length, come first, and sequences begin with parts of
+    // their own: were it the parts, the last ones, which are empty where a sequence is shorter than the longest, would be some partitions'
+    // alone (64 sequences of up to 4000 in 4 bits, four parts each: 59 us).
+    const int g = blockIdx.x / groups, rg = blockIdx.x % groups, b = blockIdx.z, split = (blockIdx.y + b) % a.splits;
     const size_t bg = (size_t)b * a.c.Hkv + g;
     const int u0 = split * 4 * a.upw + wv * a.upw;
     // (the pages are asked for ahead of the length, of which they depend in number only)
@@ -696,97 +701,146 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void cache8_attn_kernel(Attn
     const buffer_t wbuf = buffer_of(weighs ? a.weight + head0 * a.units : nullptr, weighs ? live * a.units * 4 : 0);
     const int wat = grp == 0 && col < live ? col * a.units * 4 : 0x7FFFFF00;
     if (FOUR && have) {
+        // As in 8 bits, but codes lie in LDS as they lie in memory: a lane reads what it loaded, 16 bytes at a time.
         using P = Page4<D>;
-        // Keys and values go from memory to the registers in which the products take them; the next block's keys are asked for behind the
-        // last product with this one's, and so are the values.
-        u32x4 kc[D / 32], vc[D / 32];
-        unsigned ke = 0, ve[D / 64];
-        auto load_k = [&](int i) {
-            const size_t page_i = (size_t)__builtin_amdgcn_readlane(page, i);
-            const unsigned char* at = (const unsigned char*)a.c.t.k8 + page_i * P::CODES + 16 * lane;
+        constexpr int LOADS = P::CODES / 1024 + 1;
+        unsigned char *kt = tiles[wv], *vt = kt + P::CODES, *kx = vt + P::CODES, *vx = kx + 256;
+        const bool stream = !a.idx && a.c.G <= 16;
+        const uint32_t at16 = 16 * lane, at4 = min(4 * lane, P::SCALES - 4);
+        auto load = [&](const void* codes, const uint8_t* scales, int i, unsigned char* to, unsigned char* scales_to) {
+            const size_t pg = (size_t)__builtin_amdgcn_readlane(page, i);
+            const unsigned char* from = (const unsigned char*)codes + pg * P::CODES;
+            if (stream) {
 #pragma unroll
-            for (int x = 0; x < D / 32; x++) kc[x] = *(const u32x4*)(at + 1024 * x);
-            ke = *(const unsigned*)(a.c.ke + page_i * P::SCALES + 4 * (D == 128 ? lane : 16 * (grp / 2) + col));
+                for (int x = 0; x < P::CODES / 1024; x++) async_stream_lds16(from + 1024 * x, at16, to + 1024 * x);
+            } else {
+#pragma unroll
+                for (int x = 0; x < P::CODES / 1024; x++) async_load_lds16(from + 1024 * x, at16, to + 1024 * x);
+            }
+            async_load_lds4(scales + pg * P::SCALES, at4, scales_to);
         };
-        auto load_v = [&](int i) {
-            const size_t page_i = (size_t)__builtin_amdgcn_readlane(page, i);
-            const unsigned char* at = (const unsigned char*)a.c.t.v8 + page_i * P::CODES + 16 * lane;
-#pragma unroll
-            for (int x = 0; x < D / 32; x++) vc[x] = *(const u32x4*)(at + 1024 * x);
-#pragma unroll
-            for (int x = 0; x < D / 64; x++) ve[x] = *(const unsigned*)(a.c.ve + page_i * P::SCALES + (16 * (grp / 2) + col) * (D / 16) + 4 * x);
-        };
+        auto load_k = [&](int i) { load(a.c.t.k8, a.c.ke, i, kt, kx); };
+        auto load_v = [&](int i) { load(a.c.t.v8, a.c.ve, i, vt, vx); };
         load_k(0);
         load_v(0);
         for (int i = 0; i < count; i++) {
-            const Relative krel(readlane_f32(ks, i)), vrel(readlane_f32(vs, i));
-            const float f = krel.unit * c2q;
+            const float kl = readlane_f32(ks, i), vl = readlane_f32(vs, i);
+            const Relative krel(kl), vrel(vl);
             const bool there = have >> i & 1;
             f32x4m s[4];
-            if (!krel.wide) {
+            f16x8 pb[2];
+            float corr, share;
+            auto weigh = [&] { return soft_unit(s, row, corr, [&](int t, int r, float p) { pb[t >> 1][4 * (t & 1) + r] = (_Float16)p; }); };
+            if (!krel.wide && !vrel.wide) {
+                const float f = krel.unit * c2q;
+                // the keys are there when no more than the values' loads are under way (memory operations end in order)
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
+                const unsigned ke = *(const unsigned*)(kx + 4 * (D == 128 ? lane : 16 * (grp / 2) + col));
 #pragma unroll
-                for (int t = 0; t < 4; t++) {
-                    s[t] = f32x4m{0, 0, 0, 0};
-                    const float scale = krel.of(ke, t);
+                for (int z = 0; z < D / 32; z++) {
+                    const u32x4 w = *(const u32x4*)(kt + 1024 * z + 16 * lane);
 #pragma unroll
-                    for (int x = 0; x < D / 32; x++) {
-                        const unsigned w = D == 128 ? kc[t][x] : kc[t / 2][2 * (t % 2) + x];
-                        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen_e2m1(w, scale), qf[x / 2][x % 2], s[t], 0, 0, 0);
+                    for (int u = 0; u < 128 / D; u++) {
+                        const int t = 128 / D * z + u;
+                        s[t] = f32x4m{0, 0, 0, 0};
+                        const float scale = krel.of(ke, t);
+#pragma unroll
+                        for (int x = 0; x < D / 32; x++)
+                            s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen_e2m1(w[2 * u + x], scale), qf[x / 2][x % 2], s[t], 0, 0, 0);
+#pragma unroll
+                        for (int r = 0; r < 4; r++) s[t][r] = there ? s[t][r] * f : -INFINITY;
                     }
-#pragma unroll
-                    for (int r = 0; r < 4; r++) s[t][r] = there ? s[t][r] * f : -INFINITY;
                 }
-            } else {   // 32 channels at a time, whose products are scaled in fp32
-                const unsigned char* scales = a.c.ke + (size_t)__builtin_amdgcn_readlane(page, i) * P::SCALES;
+                // the next keys; the values are there when no more than those are under way
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                if (i + 1 < count) {
+                    load_k(i + 1);
+                    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
+                } else {
+                    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                }
+                share = weigh();
+                unsigned ve[D / 64];
 #pragma unroll
+                for (int z = 0; z < D / 64; z++) ve[z] = *(const unsigned*)(vx + (16 * (grp / 2) + col) * (D / 16) + 4 * z);
+#pragma unroll
+                for (int z = 0; z < NX / 2; z++) {
+                    const u32x4 w = *(const u32x4*)(vt + 1024 * z + 16 * lane);
+#pragma unroll
+                    for (int u = 0; u < 2; u++) {
+                        const int x = 2 * z + u;
+                        const float scale = vrel.of(ve[x / 4], x % 4);
+                        f32x4m y = {0, 0, 0, 0};
+                        y = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen_e2m1(w[2 * u], scale), pb[0], y, 0, 0, 0);
+                        y = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen_e2m1(w[2 * u + 1], scale), pb[1], y, 0, 0, 0);
+#pragma unroll
+                        for (int r = 0; r < 4; r++) acc[x][r] = fmaf(acc[x][r], corr, vrel.unit * y[r]);
+                    }
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                if (i + 1 < count) load_v(i + 1);
+            } else {
+                // The products of 32 channels, or tokens, at a time are scaled in fp32.  Rare: small loops that read the page from memory, around a
+                // lane's own places in LDS, which cost the others no registers.
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (what is on its way there has arrived)
+                const size_t pg = (size_t)__builtin_amdgcn_readlane(page, i);
+                const unsigned char *kp = (const unsigned char*)a.c.t.k8 + pg * P::CODES + 16 * lane, *vp = (const unsigned char*)a.c.t.v8 + pg * P::CODES + 16 * lane;
+                const unsigned char *kscale = a.c.ke + pg * P::SCALES + 16 * grp, *vscale = a.c.ve + pg * P::SCALES + 4 * grp * (D / 16);
+                const float kn = kl == kl ? c2q : kl, vn = vl == vl ? 1.0f : vl;   // (one of the two may have a value that is not finite)
+                f32x4m* mine = (f32x4m*)tiles[wv] + lane;
+#pragma unroll 1
                 for (int t = 0; t < 4; t++) {
-                    s[t] = f32x4m{0, 0, 0, 0};
+                    f32x4m sum = {0, 0, 0, 0};
+#pragma unroll 1
                     for (int j = 0; j < D / 32; j++) {
-                        const bool mine = (D == 128 ? grp : grp / 2) == j;
                         f32x4m y = {0, 0, 0, 0};
 #pragma unroll
                         for (int x = 0; x < D / 32; x++) {
-                            const unsigned w = D == 128 ? kc[t][x] : kc[t / 2][2 * (t % 2) + x];
-                            y = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen_e2m1(mine ? w : 0u, 1.0f), qf[x / 2][x % 2], y, 0, 0, 0);
+                            const unsigned w = *(const unsigned*)(kp + (D == 128 ? 1024 * t : 1024 * (t / 2) + 8 * (t % 2)) + 4 * x);
+                            y = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen_e2m1((D == 128 ? grp : grp / 2) == j ? w : 0u, 1.0f), qf[x / 2][x % 2], y, 0, 0, 0);
                         }
 #pragma unroll
-                        for (int r = 0; r < 4; r++) s[t][r] += y[r] * (__uint_as_float((unsigned)scales[(j * 16 + 4 * grp + r) * 4 + t] << 23) * c2q);
+                        for (int r = 0; r < 4; r++) sum[r] = fmaf(y[r], __uint_as_float((unsigned)kscale[64 * j + 4 * r + t] << 23) * kn, sum[r]);
                     }
+                    mine[64 * t] = sum;
+                }
+#pragma unroll
+                for (int t = 0; t < 4; t++) {
+                    s[t] = mine[64 * t];
 #pragma unroll
                     for (int r = 0; r < 4; r++) s[t][r] = there ? s[t][r] : -INFINITY;
                 }
-            }
-            if (i + 1 < count) load_k(i + 1);
-            f16x8 pb[2];
-            float corr;
-            const float share = soft_unit(s, row, corr, [&](int t, int r, float p) { pb[t >> 1][4 * (t & 1) + r] = (_Float16)p; });
-            if (!vrel.wide) {
-#pragma unroll
+                share = weigh();
+#pragma unroll 1
                 for (int x = 0; x < NX; x++) {
-                    const float scale = vrel.of(ve[x / 4], x % 4);
-                    f32x4m y = {0, 0, 0, 0};
-                    y = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen_e2m1(vc[x / 2][2 * (x % 2)], scale), pb[0], y, 0, 0, 0);
-                    y = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen_e2m1(vc[x / 2][2 * (x % 2) + 1], scale), pb[1], y, 0, 0, 0);
-#pragma unroll
-                    for (int r = 0; r < 4; r++) acc[x][r] = fmaf(acc[x][r], corr, vrel.unit * y[r]);
-                }
-            } else {   // 32 tokens at a time
-                const unsigned char* scales = a.c.ve + (size_t)__builtin_amdgcn_readlane(page, i) * P::SCALES;
-#pragma unroll
-                for (int x = 0; x < NX; x++)
+                    f32x4m sum = {0, 0, 0, 0};
+#pragma unroll 1
                     for (int j = 0; j < 2; j++) {
                         f32x4m y = {0, 0, 0, 0};
 #pragma unroll
-                        for (int z = 0; z < 2; z++)
-                            y = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen_e2m1(grp / 2 == j ? vc[x / 2][2 * (x % 2) + z] : 0u, 1.0f), pb[z], y, 0, 0, 0);
+                        for (int z = 0; z < 2; z++) {
+                            const unsigned w = *(const unsigned*)(vp + 1024 * (x / 2) + 8 * (x % 2) + 4 * z);
+                            y = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen_e2m1(grp / 2 == j ? w : 0u, 1.0f), pb[z], y, 0, 0, 0);
+                        }
 #pragma unroll
-                        for (int r = 0; r < 4; r++)
-                            acc[x][r] = fmaf(acc[x][r], j ? 1.0f : corr, y[r] * __uint_as_float((unsigned)scales[(j * 16 + 4 * grp + r) * (D / 16) + x] << 23));
+                        for (int r = 0; r < 4; r++) sum[r] = fmaf(y[r], __uint_as_float((unsigned)vscale[(16 * j + r) * (D / 16) + x] << 23) * vn, sum[r]);
                     }
+                    mine[64 * x] = sum;
+                }
+#pragma unroll
+                for (int x = 0; x < NX; x++) {
+                    const f32x4m y = mine[64 * x];
+#pragma unroll
+                    for (int r = 0; r < 4; r++) acc[x][r] = fmaf(acc[x][r], corr, y[r]);
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                if (i + 1 < count) {
+                    load_k(i + 1);
+                    load_v(i + 1);
+                }
             }
             if (alone) shares[u0 + i][col] = share;
             else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(share), wbuf, wat + 4 * (u0 + i), 0, 0);
-            if (i + 1 < count) load_v(i + 1);
         }
     } else if (!FOUR && have) {
         unsigned char *kt = tiles[wv], *vt = kt + T::BYTES;
@@ -1146,9 +1200,13 @@ static Cache8Layout cache8_layout(const sparsek_cache8_cfg& c, int top)
     // Units per wave.  Up to 20 units and 16 heads of a group are one workgroup's, which needs no second launch.  Beyond that
     // as many as leave 8 waves for each of 256 compute units, 5 at most (sequences are shorter than the longest, and the waves that
     // they leave idle weigh less the fewer units each has: 64 sequences of up to 8192 127.5 us with 5, 128.3 with 4, 130 with 3, 136 with 2).
-    const long long all = (long long)c.B * c.Hkv * y.groups * y.units;
-    if (y.units <= 4 * MAX_UPW && y.groups == 1) y.upw = (y.units + 3) / 4;
-    else y.upw = (int)std::max<long long>(1, std::min<long long>(MAX_UPW, all / 2048));
+    const long long rows = (long long)c.B * c.Hkv * y.groups, all = rows * y.units;
+    // In 4 bits a unit is half as long and the second launch weighs more: one workgroup for up to 28, or 40 where there is one for every compute unit
+    // (sequences of up to 2400, 38 units: 64 of them 31.6 us in one and 39.1 in two, 32 of them 22.7 and 25.3, 8 of them 20.8 and 19.4; of up to 1400, 22
+    // units: 23.2 and 37.6 for 64, 15.4 and 19.5 for 4).
+    const int most = 5, alone = c.format != SPARSEK_E2M1 ? most : rows >= 256 ? MAX_UPW : 7;
+    if (y.units <= 4 * alone && y.groups == 1) y.upw = (y.units + 3) / 4;
+    else y.upw = (int)std::max<long long>(1, std::min<long long>(most, all / 2048));
     y.splits = (y.units + 4 * y.upw - 1) / (4 * y.upw);
     const size_t parts = (size_t)c.B * c.H * y.splits;
     y.part_o = 0;
@@ -1179,7 +1237,7 @@ static int attn_launch(const sparsek_cache8_cfg& c, const CacheArgs& cache, cons
     a.o = (uint16_t*)o;
     a.lse = lse;
     const int mass_wgs = accumulate ? (y.units + 255) / 256 : 0;
-#define ATTN(D, F) hipLaunchKernelGGL((cache8_attn_kernel<D, F>), dim3(y.splits, c.Hkv * y.groups, c.B), dim3(256), 0, st, a)
+#define ATTN(D, F) hipLaunchKernelGGL((cache8_attn_kernel<D, F>), dim3(c.Hkv * y.groups, y.splits, c.B), dim3(256), 0, st, a)
     BY_FORMAT(c, ATTN)
 #undef ATTN
     if (y.splits == 1 && y.groups == 1) return launch_status();
