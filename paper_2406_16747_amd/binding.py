@@ -742,13 +742,14 @@ def _cache_attn(f, need, cache, lens, q, idx, accumulate, ws):
         nbytes = cache.bytes.get(top)
         if nbytes is None:
             nbytes = cache.bytes[top] = max(need(cache.ref, top), 256)
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=cache.device)
+        if nbytes > 256 or type(cache) is Cache8:   # (in 4 bits that is no workspace at all)
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=cache.device)
     else:
         if ws.device != cache.device or not ws.is_contiguous():
             raise ValueError("ws must be contiguous and on %s" % cache.device)
         nbytes = ws.numel() * ws.element_size()
     _on(cache.device, f, cache.ref, cache.cref, lens.data_ptr(), q.data_ptr(), _ptr(idx), top, 1 if accumulate else 0,
-        o.data_ptr(), lse.data_ptr(), ws.data_ptr(), nbytes)
+        o.data_ptr(), lse.data_ptr(), _ptr(ws), nbytes)
     return o, lse
 
 

@@ -1,5 +1,6 @@
 // C-ABI entry points of libsparsek: argument validation, then the launch wrappers.
 #include "common.hpp"
+#include "block_parts.hpp"
 #include "mask_ranges.hpp"
 
 #include <initializer_list>
@@ -551,10 +552,13 @@ int cache_attn(const sparsek_cache8_cfg* cfg, const typename Of::Cache* cache, c
     if (!cache) return SPARSEK_ERR_INVALID_ARG;
     int rc = check_cache<Of>(cfg, cache);
     if (rc) return rc;
-    if (!lens || !q || !o || !lse || !ws || (idx ? top < 1 : top != 0)) return SPARSEK_ERR_INVALID_ARG;
+    if (!lens || !q || !o || !lse || (idx ? top < 1 : top != 0)) return SPARSEK_ERR_INVALID_ARG;
     if (!Of::wide(*cache) || !aligned({q, o, ws})) return SPARSEK_ERR_INVALID_ARG;
-    if (top > MAX_CACHE_BLOCKS) return SPARSEK_ERR_UNSUPPORTED;
-    if (ws_bytes < spk::cache8_attn_ws_bytes(*cfg, top)) return SPARSEK_ERR_WORKSPACE;
+    if (top > MAX_CACHE_BLOCKS) return ws ? SPARSEK_ERR_UNSUPPORTED : SPARSEK_ERR_INVALID_ARG;
+    const size_t need = spk::cache8_attn_ws_bytes(*cfg, top);
+    const bool none = cfg->format == SPARSEK_E2M1 && need == spk::NO_WORKSPACE;
+    if (!ws && !none) return SPARSEK_ERR_INVALID_ARG;
+    if (ws && ws_bytes < need) return SPARSEK_ERR_WORKSPACE;
     return Of::attn(*cfg, *cache, lens, q, idx, top, accumulate != 0, o, lse, ws, (hipStream_t)stream);
 }
 

@@ -10,6 +10,9 @@ static_assert(BT == KT, "a block is one key tile");
 // A block whose largest magnitude is below this is held as zeros with scale 0: 127 / max (or 448 / max) stays finite.
 constexpr float TINY_MAX = 0x1p-100f;
 
+// What the size query of the attention over a cache in 4 bits answers where it needs no workspace.
+constexpr size_t NO_WORKSPACE = 256;
+
 inline int block_count(int n) { return (n + BT - 1) / BT; }
 
 // The lists that the attention kernels walk: for every key block the queries that attend it -- its own ones first, then those that

@@ -11,8 +11,10 @@ struct ReadArgs {
     uint16_t *k, *v;   // [B,Hkv,n,D]
 };
 
-// One workgroup of 256 per (block that the range touches, batch and head).  What bounds it is writing.
-template <int D>
+// One workgroup of 256 per (block that the range touches, batch and head).  What bounds it is writing: STREAM leaves the chip's caches out where
+// they do not hold what is written (a prefix of 4096 for 16 sequences, 8 heads of 128, 268 MB: 52 us, 6.0 TB/s, and 62 through them; for 8 of them
+// 27 and 25).
+template <int D, bool STREAM>
 __global__ __launch_bounds__(256) void cache4_read_kernel(ReadArgs a)
 {
     using P = Page4<D>;
@@ -24,7 +26,10 @@ __global__ __launch_bounds__(256) void cache4_read_kernel(ReadArgs a)
     uint16_t *ko = a.k + (size_t)bg * a.n * D, *vo = a.v + (size_t)bg * a.n * D;
     auto out_row = [&](int s) { return first + s >= 0 && first + s < a.n; };
     auto put = [&](uint16_t* o, int s, int c8, u32x4 w) {
-        if (out_row(s)) *(u32x4*)(o + (size_t)(first + s) * D + 8 * c8) = w;
+        u32x4* at = (u32x4*)(o + (size_t)(first + s) * D + 8 * c8);
+        if (!out_row(s)) return;
+        if constexpr (STREAM) __builtin_nontemporal_store(w, at);
+        else *at = w;
     };
     const int live = min(len - j * BT, BT);                  // tokens of the block that are there
     const int page = live == BT && j < a.cap ? a.t.table[(size_t)bg * a.cap + j] : -1;
@@ -103,8 +108,16 @@ int launch_cache4_read(const sparsek_cache8_cfg& c, const sparsek_cache4& t, con
 {
     const ReadArgs a = {t, c.Hkv, c.cap, c.pages, begin, n, lens, (uint16_t*)k, (uint16_t*)v};
     const dim3 grid((unsigned)((begin + n - 1) / BT - begin / BT + 1), c.B * c.Hkv);
-    if (c.d == 128) hipLaunchKernelGGL((cache4_read_kernel<128>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((cache4_read_kernel<64>), grid, dim3(256), 0, st, a);
+    const bool stream = 4.0 * c.B * c.Hkv * n * c.d > 256e6;   // (the last cache has 256 MB)
+#define READ(D, S) hipLaunchKernelGGL((cache4_read_kernel<D, S>), grid, dim3(256), 0, st, a)
+    if (c.d == 128) {
+        if (stream) READ(128, true);
+        else READ(128, false);
+    } else {
+        if (stream) READ(64, true);
+        else READ(64, false);
+    }
+#undef READ
     return launch_status();
 }
 

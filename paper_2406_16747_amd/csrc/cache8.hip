@@ -1015,28 +1015,28 @@ __global__ __launch_bounds__(256, FORMAT == FORMAT_E2M1 ? 3 : D == 128 ? 2 : 4) 
     }
 }
 
-// The parts of a head are joined (workgroups 0 .. H-1 of a sequence), and the shares of its blocks join the masses (the others).
-template <int D>
-__global__ __launch_bounds__(256) void cache8_join_kernel(AttnArgs a, int mass_wgs)
+// The parts of a head are joined (workgroups 0 .. H-1 of a sequence), and the shares of its blocks join the masses (the others).  NW waves.
+template <int D, int NW>
+__global__ __launch_bounds__(64 * NW) void cache8_join_kernel(AttnArgs a, int mass_wgs)
 {
     constexpr int EPL = D / 64, UNR = 8;   // columns per lane
-    __shared__ float red[4][D], ms[4], ls[4], logs[4];
+    __shared__ float red[NW][D], ms[NW], ls[NW], logs[NW];
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, b = blockIdx.y, G = a.c.G;
     const RowUnits ru = row_units(a, b);
     const int nu = ru.nsel + (ru.tail ? 1 : 0), splits = (nu + 4 * a.upw - 1) / (4 * a.upw);
-    if ((int)blockIdx.x < a.c.H) {   // a wave takes every fourth part, 8 of them under way together
+    if ((int)blockIdx.x < a.c.H) {   // a wave takes every NW-th part, 8 of them under way together
         const size_t row = (size_t)b * a.c.H + blockIdx.x;
         const float2* ml = a.part_ml + row * a.splits;
         const float* po = a.part_o + row * a.splits * D + EPL * lane;
         float M = -INFINITY, L = 0.0f, sum[EPL];
 #pragma unroll
         for (int e = 0; e < EPL; e++) sum[e] = 0.0f;
-        for (int s0 = wv; s0 < splits; s0 += 4 * UNR) {
+        for (int s0 = wv; s0 < splits; s0 += NW * UNR) {
             float2 p[UNR];
             float x[UNR][EPL];
 #pragma unroll
             for (int u = 0; u < UNR; u++) {
-                const int s = min(s0 + 4 * u, splits - 1);
+                const int s = min(s0 + NW * u, splits - 1);
                 p[u] = ml[s];
 #pragma unroll
                 for (int e = 0; e < EPL; e++) x[u][e] = po[(size_t)s * D + e];
@@ -1044,7 +1044,7 @@ __global__ __launch_bounds__(256) void cache8_join_kernel(AttnArgs a, int mass_w
             float top = M;
 #pragma unroll
             for (int u = 0; u < UNR; u++) {
-                if (s0 + 4 * u >= splits) p[u].x = -INFINITY;
+                if (s0 + NW * u >= splits) p[u].x = -INFINITY;
                 top = fmaxf(top, p[u].x);
             }
             if (top == -INFINITY) continue;
@@ -1066,17 +1066,21 @@ __global__ __launch_bounds__(256) void cache8_join_kernel(AttnArgs a, int mass_w
 #pragma unroll
         for (int e = 0; e < EPL; e++) red[wv][EPL * lane + e] = sum[e];
         __syncthreads();
-        const float top = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3]));
-        float all = 0.0f, y = 0.0f;
-        if (top > -INFINITY)
+        float top = ms[0];
 #pragma unroll
-            for (int w = 0; w < 4; w++) {
-                const float f = __builtin_amdgcn_exp2f(ms[w] - top);
-                all = fmaf(f, ls[w], all);
-                if (tid < D) y = fmaf(f, red[w][tid], y);
-            }
-        if (tid < D) a.o[row * D + tid] = f32_to_bf16(top > -INFINITY ? y / all : 0.0f);
-        if (tid == 0) a.lse[row] = log_of(top, all);
+        for (int w = 1; w < NW; w++) top = fmaxf(top, ms[w]);
+        for (int x = tid; x < D; x += 64 * NW) {
+            float all = 0.0f, y = 0.0f;
+            if (top > -INFINITY)
+#pragma unroll
+                for (int w = 0; w < NW; w++) {
+                    const float f = __builtin_amdgcn_exp2f(ms[w] - top);
+                    all = fmaf(f, ls[w], all);
+                    y = fmaf(f, red[w][x], y);
+                }
+            a.o[row * D + x] = f32_to_bf16(top > -INFINITY ? y / all : 0.0f);
+            if (x == 0) a.lse[row] = log_of(top, all);
+        }
         return;
     }
     auto total = [&](int h) {   // log2 of head h's sum, by a wave
@@ -1093,21 +1097,21 @@ __global__ __launch_bounds__(256) void cache8_join_kernel(AttnArgs a, int mass_w
         return top + log2f(L * 0x1p-15f);
     };
     const int g = (blockIdx.x - a.c.H) / mass_wgs, part = (blockIdx.x - a.c.H) % mass_wgs;
-    if (part * 256 >= nu) return;
+    if (part * 64 * NW >= nu) return;
     const size_t bg = (size_t)b * a.c.Hkv + g;
-    const int u = part * 256 + tid;
+    const int u = part * 64 * NW + tid;
     float sum = 0.0f;
-    for (int r0 = 0; r0 < G; r0 += 4) {   // a wave per head
-        float w[4];
+    for (int r0 = 0; r0 < G; r0 += NW) {   // a wave per head
+        float w[NW];
 #pragma unroll
-        for (int x = 0; x < 4; x++) w[x] = u < nu && r0 + x < G ? a.weight[((size_t)b * a.c.H + g * G + r0 + x) * a.units + u] : -INFINITY;
+        for (int x = 0; x < NW; x++) w[x] = u < nu && r0 + x < G ? a.weight[((size_t)b * a.c.H + g * G + r0 + x) * a.units + u] : -INFINITY;
         if (r0 + wv < G) {
             const float all = total(g * G + r0 + wv);
             if (lane == 0) logs[wv] = all;
         }
         __syncthreads();
 #pragma unroll
-        for (int x = 0; x < 4; x++)
+        for (int x = 0; x < NW; x++)
             if (w[x] != -INFINITY) sum += __builtin_amdgcn_exp2f(w[x] - logs[x]);
         __syncthreads();
     }
@@ -1213,6 +1217,7 @@ static Cache8Layout cache8_layout(const sparsek_cache8_cfg& c, int top)
     y.part_ml = align_up(parts * c.d * 4, 256);
     y.weight = y.part_ml + align_up(parts * 8, 256);
     y.bytes = y.weight + align_up((size_t)c.B * c.H * y.units * 4, 256);
+    if (c.format == SPARSEK_E2M1 && y.splits == 1 && y.groups == 1) y.bytes = NO_WORKSPACE;   // (one workgroup has all of it: nothing is kept there)
     return y;
 }
 size_t cache8_attn_ws_bytes(const sparsek_cache8_cfg& c, int top) { return cache8_layout(c, top).bytes; }
@@ -1236,14 +1241,21 @@ static int attn_launch(const sparsek_cache8_cfg& c, const CacheArgs& cache, cons
     a.units = y.units;
     a.o = (uint16_t*)o;
     a.lse = lse;
-    const int mass_wgs = accumulate ? (y.units + 255) / 256 : 0;
 #define ATTN(D, F) hipLaunchKernelGGL((cache8_attn_kernel<D, F>), dim3(c.Hkv * y.groups, y.splits, c.B), dim3(256), 0, st, a)
     BY_FORMAT(c, ATTN)
 #undef ATTN
     if (y.splits == 1 && y.groups == 1) return launch_status();
+    // In 4 bits up to 8 parts are one wave's, on their way together (64 sequences of up to 8192, 7 parts each: 5.0 us, with 4 waves 7.0; of 65 parts,
+    // one sequence of 32768: 16 waves 4.4, 4 waves 4.3).
+    const int nw = c.format == SPARSEK_E2M1 && y.splits <= 8 ? 1 : 4;
+    const int mass_wgs = accumulate ? (y.units + 64 * nw - 1) / (64 * nw) : 0;
     const dim3 join(c.H + c.Hkv * mass_wgs, c.B);
-    if (c.d == 128) hipLaunchKernelGGL((cache8_join_kernel<128>), join, dim3(256), 0, st, a, std::max(mass_wgs, 1));
-    else hipLaunchKernelGGL((cache8_join_kernel<64>), join, dim3(256), 0, st, a, std::max(mass_wgs, 1));
+#define JOIN(D, NW) hipLaunchKernelGGL((cache8_join_kernel<D, NW>), join, dim3(64 * NW), 0, st, a, std::max(mass_wgs, 1))
+    if (c.d == 128 && nw == 1) JOIN(128, 1);
+    else if (c.d == 128) JOIN(128, 4);
+    else if (nw == 1) JOIN(64, 1);
+    else JOIN(64, 4);
+#undef JOIN
     return launch_status();
 }
 

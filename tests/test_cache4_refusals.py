@@ -65,6 +65,8 @@ def test_pointers():
     assert need > 0 and L.sparsek_cache4_attn_workspace_bytes(c, -1) == 0
     assert L.sparsek_cache4_attn(c, t, ONE, ONE, ONE, 4, 0, ONE, ONE, ONE, need - 1, NULL) == -3
     assert L.sparsek_cache4_attn(c, t, ONE, ONE, NULL, 4, 0, ONE, ONE, ONE, BIG, NULL) == -1
+    assert need == 256 and L.sparsek_cache4_attn_workspace_bytes(ccfg(cap=200), 0) > 256
+    assert L.sparsek_cache4_attn(ccfg(cap=200), t, ONE, ONE, NULL, 0, 0, ONE, ONE, NULL, BIG, NULL) == -1
     far = [ctypes.c_void_p(x << 20) for x in (1, 2, 3)]
     for budget, sink, recent in ((-1, 0, 0), (4, 3, 2), (4, -1, 0), (4, 0, -1)):
         assert L.sparsek_cache4_evict(c, t, ONE, budget, sink, recent, *far, NULL) == -1
