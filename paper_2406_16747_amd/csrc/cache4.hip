@@ -12,8 +12,8 @@ struct ReadArgs {
 };
 
 // One workgroup of 256 per (block that the range touches, batch and head).  What bounds it is writing: STREAM leaves the chip's caches out where
-// they do not hold what is written (a prefix of 4096 for 16 sequences, 8 heads of 128, 268 MB: 52 us, 6.0 TB/s, and 62 through them; for 8 of them
-// 27 and 25).
+// much is written (a prefix of 4096 for 16 sequences, 8 heads of 128, 268 MB: 52 us, 6.0 TB/s, and 70 through them; for 8 of them 27 and 38, for 4 of
+// them, 67 MB, 14.3 and 13.1).
 template <int D, bool STREAM>
 __global__ __launch_bounds__(256) void cache4_read_kernel(ReadArgs a)
 {
@@ -108,7 +108,7 @@ int launch_cache4_read(const sparsek_cache8_cfg& c, const sparsek_cache4& t, con
 {
     const ReadArgs a = {t, c.Hkv, c.cap, c.pages, begin, n, lens, (uint16_t*)k, (uint16_t*)v};
     const dim3 grid((unsigned)((begin + n - 1) / BT - begin / BT + 1), c.B * c.Hkv);
-    const bool stream = 4.0 * c.B * c.Hkv * n * c.d > 256e6;   // (the last cache has 256 MB)
+    const bool stream = 4.0 * c.B * c.Hkv * n * c.d > 100e6;
 #define READ(D, S) hipLaunchKernelGGL((cache4_read_kernel<D, S>), grid, dim3(256), 0, st, a)
     if (c.d == 128) {
         if (stream) READ(128, true);

@@ -343,12 +343,12 @@ static RopeShape rope_shape(const sparsek_rope_cfg& c)
     s.groups = ((long long)c.B * c.n + s.tok - 1) / s.tok;
     return s;
 }
-// Whether a call that reads or writes every value `passes` times does not fit the last cache, of 256 MB (streamed and not: a document of 32768, 671
-// MB, 138 and 148 us; forward of 16 x 2000 tokens in fp32, 393 MB, 76 and 82; two prompts of 5003, 92 MB, 27 and 19; forward of 4 x 2000 in fp32, 98
-// MB, 20 and 17).
+// Whether a call that reads or writes every value `passes` times goes past the last cache, of 256 MB (streamed and not: a document of 32768, 671 MB,
+// 138 and 148 us; of 12000, 246 MB, 53.7 and 60.1; of 8192, 168 MB, 39.0 both; two prompts of 5003, 92 MB, 31 and 19; forward of 16 x 2000 tokens in
+// fp32, 393 MB, 76 and 82).
 static bool rope_streams(const sparsek_rope_cfg& c, int passes)
 {
-    return (double)passes * c.B * c.n * (c.H + c.Hkv) * c.d * (c.dtype == SPARSEK_BF16 ? 2 : 4) > 256e6;
+    return (double)passes * c.B * c.n * (c.H + c.Hkv) * c.d * (c.dtype == SPARSEK_BF16 ? 2 : 4) > 200e6;
 }
 static RopeArgs rope_args(const sparsek_rope_cfg& c, const void* q, const void* k, const int32_t* pos, const float* freq, const int32_t* axis,
                           const float* qw, const float* kw)
