@@ -424,7 +424,7 @@ int sparsek_cache4_evict(const sparsek_cache8_cfg *cfg, const sparsek_cache4 *ca
  * bwd: for L = sum(dqo * qo) + sum(dko * ko), dqo, dko contiguous as qo, ko: dq, dk in the strides cfg->dq, cfg->dk (places of one tensor must not
  * coincide: INVALID_ARG), and dqw, dkw [d] fp32, NULL: not wanted (norm == 0: they must be NULL).  q and k are not read where norm == 0 and may be NULL.
  * The sums behind dqw and dkw have an order of their own that does not depend on timing.
- * SPARSEK_BF16 or SPARSEK_F32; d a multiple of 8, 8 .. 256; rot a multiple of 8, 0 .. d; axes 1 .. 4; H + Hkv <= 65535, B n < 2^31 (UNSUPPORTED
+ * SPARSEK_BF16 or SPARSEK_F32; d a multiple of 8, 8 .. 256; rot a multiple of 8, 0 .. d; axes 1 .. 4; H + Hkv <= 65535, B n < 2^27 (UNSUPPORTED
  * otherwise).  Strides are in elements, not negative, multiples of 4, and the last row begins below 2^46; tensors and ws begin at multiples of 16 bytes; outputs overlap no
  * inputs (INVALID_ARG otherwise). */
 typedef struct {
@@ -434,7 +434,7 @@ typedef struct {
     int32_t B, H, Hkv, n, d;
     int32_t rot, axes, interleaved, norm;
     int32_t dtype;                /* of q, k, qo, ko and their gradients */
-    float eps;                    /* finite and > 0 where norm != 0 */
+    float eps;                    /* finite and at least 2^-126 where norm != 0 */
     sparsek_rope_strides q, k;
     sparsek_rope_strides dq, dk;  /* of the backward's outputs (not read by the forward) */
 } sparsek_rope_cfg;

@@ -164,17 +164,22 @@ def check(rc):
 # kept, pointers are passed as plain integers, and the stream is asked for without building a Stream object.
 torch = None
 _raw_stream = None
+_here = None      # the current device; the stream of a device, as an integer
 _CFG_KEPT = 256   # configurations kept per kind
 _cfgs = {}
 
 
 def _torch():
-    global torch, _raw_stream
+    global torch, _raw_stream, _here
     if torch is None:
         import torch as t
 
         get, dev = getattr(t._C, "_cuda_getCurrentRawStream", None), getattr(t._C, "_cuda_getDevice", None)
         _raw_stream = (lambda: get(dev())) if get and dev else (lambda: t.cuda.current_stream().cuda_stream)
+        if get and dev:
+            _here = dev, get
+        else:
+            _here = t.cuda.current_device, lambda device: t.cuda.current_stream(device).cuda_stream
         torch = t
     return torch
 
@@ -519,8 +524,9 @@ def _on(device, f, *args):
     """f(*args, stream) for the device that the tensors are on, on its current stream."""
     if device.type != "cuda":
         raise ValueError("the tensors must be on the GPU, got %s" % device)
-    if device.index == torch.cuda.current_device():
-        rc = f(*args, _raw_stream())
+    here = _here[0]()
+    if device.index == here:
+        rc = f(*args, _here[1](here))
     else:
         with torch.cuda.device(device):
             rc = f(*args, _raw_stream())
@@ -816,7 +822,7 @@ def sparsek_cache4_read(cache, lens, begin, n, out=None):
     _same("lens", lens, torch.int32, cache.lens_shape, cache.device)
     shape = (cache.B, cache.Hkv, int(n), cache.d)
     if out is None:
-        out = tuple(torch.empty(cache.B, cache.Hkv, max(int(n), 0), cache.d, dtype=torch.bfloat16, device=cache.device) for _ in range(2))
+        out = cache.kt.new_empty((2, cache.B, cache.Hkv, max(int(n), 0), cache.d)).unbind()
     else:
         for name, t in zip(("out k", "out v"), out):
             _same(name, t, torch.bfloat16, shape, cache.device)

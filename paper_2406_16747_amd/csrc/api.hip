@@ -753,10 +753,10 @@ bool apart(const sparsek_rope_cfg& c, const sparsek_rope_strides& s, int heads)
 int check_rope(const sparsek_rope_cfg* c)
 {
     if (!c || c->B < 1 || c->H < 1 || c->Hkv < 0 || c->n < 1 || c->d < 1 || c->rot < 0 || c->rot > c->d || c->axes < 1) return SPARSEK_ERR_INVALID_ARG;
-    if (c->norm && (!(c->eps > 0.0f) || !(c->eps < INFINITY))) return SPARSEK_ERR_INVALID_ARG;
+    if (c->norm && (!(c->eps >= 0x1p-126f) || !(c->eps < INFINITY))) return SPARSEK_ERR_INVALID_ARG;
     if (c->dtype != SPARSEK_BF16 && c->dtype != SPARSEK_F32) return SPARSEK_ERR_UNSUPPORTED;
     if (c->d % 8 || c->d > 256 || c->rot % 8 || c->axes > 4) return SPARSEK_ERR_UNSUPPORTED;
-    if ((long long)c->H + c->Hkv > 65535 || (long long)c->B * c->n >= (1ll << 31)) return SPARSEK_ERR_UNSUPPORTED;
+    if ((long long)c->H + c->Hkv > 65535 || (long long)c->B * c->n >= (1ll << 27)) return SPARSEK_ERR_UNSUPPORTED;
     if (!good(*c, c->q, c->H) || (c->Hkv && !good(*c, c->k, c->Hkv))) return SPARSEK_ERR_INVALID_ARG;
     return SPARSEK_OK;
 }

@@ -543,3 +543,55 @@ def test_decode_step_replays_as_a_graph():
     for _, cache, lens, _, _ in graphs:
         assert torch.equal(cache.mass, ec.mass) and torch.equal(lens, el)
         assert torch.equal(cache.k4, ec.k4) and torch.equal(cache.ve, ec.ve) and torch.equal(cache.kt, ec.kt)
+
+
+def test_pages_beyond_32_bits():
+    """A pool of more than 2^32 bytes: its last pages hold what its first ones would."""
+    require_gpu()
+    say("cache4, pages beyond 2^32 bytes")
+    B, H, Hkv, d, cap, n = 1, 4, 2, 128, 8, 400
+    g = gen(101)
+    k, v, q = rand(g, B, Hkv, n, d), rand(g, B, Hkv, n, d), rand(g, B, H, d)
+    runs = []
+    for pages in (16, 2 ** 20 + 40):
+        cache = spk.Cache4.empty(B, H, Hkv, d, cap, pages=pages)
+        cache.table.copy_(torch.arange(pages - 16, pages, dtype=torch.int32).view(B, Hkv, cap))
+        L = ints([n])
+        spk.sparsek_cache4_append(cache, torch.zeros_like(L), k, v)
+        idx = spk.sparsek_cache4_select(cache, L, q, 3)
+        runs.append(spk.sparsek_cache4_attn(cache, L, q, accumulate=True) + spk.sparsek_cache4_attn(cache, L, q, idx) + spk.sparsek_cache4_read(cache, L, 0, n))
+        runs[-1] += (idx, cache.mass.clone(), cache.ke[-16:].clone())
+        torch.cuda.synchronize()
+        assert pages == 16 or (cache.k4[:64] == 0).all() and cache.k4.numel() > 2 ** 32
+        del cache
+    assert all(torch.equal(a, b) for a, b in zip(*runs))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("H,Hkv,B,n", [(40, 2, 2, 700), (16, 16, 20, 2400), (8, 8, 40, 2400), (8, 8, 1, 1900), (4, 4, 1, 9000), (6, 2, 3, 20000)])
+def test_one_workgroup_or_many(H, Hkv, B, n, d):
+    """Every way in which a sequence is shared out: more heads than a product has columns, one workgroup for few blocks, for up to 40 of them where
+    there are many sequences, few parts and many parts of a sequence; all with the masses of all blocks."""
+    require_gpu()
+    say("cache4, shared out", H, Hkv, B, n, d)
+    g = gen(111)
+    base = rand(g, 1, Hkv, n, d), rand(g, 1, Hkv, n, d)
+    cache = spk.Cache4.empty(B, H, Hkv, d, n // 64 + 1, pages=Hkv * (n // 64 + 1))
+    cache.table.copy_(torch.arange(Hkv * (n // 64 + 1), dtype=torch.int32).view(1, Hkv, -1).expand_as(cache.table))   # (all sequences have the same pages)
+    one = spk.Cache4(cache.k4, cache.v4, cache.ke, cache.ve, cache.ks, cache.vs, cache.km, cache.kms, cache.kt[:1].clone(), cache.vt[:1].clone(),
+                     cache.table[:1].clone(), cache.mass[:1].clone(), H, d ** -0.5)
+    spk.sparsek_cache4_append(one, ints([0]), *base)
+    cache.kt.copy_(one.kt.expand_as(cache.kt))
+    cache.vt.copy_(one.vt.expand_as(cache.vt))
+    whole = n // 64 * 64
+    lens = [n if b == 0 else whole - 64 * (b % (n // 64)) for b in range(B)]   # (others end with a block, so that the unfinished one is nobody's)
+    q = rand(g, B, H, d)
+    o, lse = spk.sparsek_cache4_attn(cache, ints(lens), q, accumulate=True)
+    torch.cuda.synchronize()
+    for b in sorted({0, B // 2, B - 1}):
+        cut = type("C", (), dict(B=1, H=H, Hkv=Hkv, d=d, cap=cache.cap, cfg=cache.cfg, k4=cache.k4, v4=cache.v4, ke=cache.ke, ve=cache.ve, ks=cache.ks,
+                                 vs=cache.vs, kt=cache.kt[b:b + 1], vt=cache.vt[b:b + 1], table=cache.table[b:b + 1]))
+        ro, rl, rm, ob = ref.cache_attn(cut, lens[b:b + 1], q[b:b + 1])
+        assert ((ref.f64(o[b:b + 1]) - ro).abs() <= ob).all()
+        assert ((lse[b:b + 1].cpu().double() - rl).abs() <= 2e-4).all()
+        assert ((ref.f64(cache.mass[b:b + 1]) - rm).abs() <= 2 ** -12 * rm).all()

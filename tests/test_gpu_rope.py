@@ -191,3 +191,73 @@ def test_ahead_of_attention_over_blocks_and_behind_its_backward():
         rx, rw, bx, bw = ref.bwd(x, pos, freq, None, False, True, wt, 1e-6, do)
         held(dx, rx, bx)
         held(dw, rw, bw)
+
+
+def test_offsets_beyond_32_bits():
+    """Inputs, outputs and gradients of more than 2^31 elements: as the same tokens and heads give alone."""
+    require_gpu()
+    say("rope beyond 2^31 elements")
+    B, n, H, d = 1, 131072, 136, 128
+    q = torch.empty(B, n, H, d, dtype=BF16, device="cuda")
+    q.view(-1, 1 << 20).copy_(torch.randn(1 << 20, generator=gen(71)).bfloat16().cuda())
+    assert q.numel() > 2 ** 31
+    pos, freq, _ = ladder(gen(72), B, n, d, 1, far=200000)
+    w = (1 + 0.2 * torch.randn(d, generator=gen(73))).cuda()
+    qo, _ = spk.sparsek_rope_fwd(q, None, pos, freq, norm=True, qw=w)
+    dq = spk.sparsek_rope_bwd(q, None, pos, freq, qo, None, norm=True, qw=w)[0]
+    for rows, heads in ((slice(0, 3), slice(0, 2)), (slice(n - 70, n), slice(H - 3, H)), (slice(n // 2, n // 2 + 5), slice(64, 66))):
+        x, p = q[:, rows, heads], pos[:, :, rows].contiguous()
+        o, _ = spk.sparsek_rope_fwd(x, None, p, freq, norm=True, qw=w)
+        back = spk.sparsek_rope_bwd(x, None, p, freq, o, None, norm=True, qw=w)[0]
+        torch.cuda.synchronize()
+        assert torch.equal(o, qo[:, heads, rows]) and torch.equal(back, dq[:, rows, heads])
+
+
+def test_single_tokens_are_rows_of_prompts():
+    """A step's token, of several sequences at positions of their own, has the bits that a prompt gives it."""
+    require_gpu()
+    say("rope, steps and prompts")
+    g = gen(81)
+    q, k = fused(g, 3, 40, 6, 2, 80, BF16)
+    pos, freq, axis = ladder(g, 3, 40, 64, 2, far=50000)
+    w = (1 + 0.2 * torch.randn(2, 80, generator=g)).cuda()
+    args = dict(axis=axis, norm=True, qw=w[0], kw=w[1])
+    qo, ko = spk.sparsek_rope_fwd(q, k, pos, freq, **args)
+    out = torch.empty(3, 6, 1, 80, dtype=BF16, device="cuda"), torch.empty(3, 2, 1, 80, dtype=BF16, device="cuda")
+    for t in (0, 17, 39):
+        got = spk.sparsek_rope_fwd(q[:, t:t + 1], k[:, t:t + 1], pos[:, :, t:t + 1].contiguous(), freq, out=out, **args)
+        torch.cuda.synchronize()
+        assert got[0] is out[0] and torch.equal(out[0], qo[:, :, t:t + 1]) and torch.equal(out[1], ko[:, :, t:t + 1])
+
+
+@pytest.mark.parametrize("dtype,n", [(BF16, 90000), (F32, 45000)])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_calls_that_are_streamed(dtype, n, interleaved):
+    """More than the chip's last cache holds, heads in no multiple of what is on its way together: stretches of tokens have the bits that they have
+    alone, and the weights' gradients are the definition's."""
+    require_gpu()
+    say("rope streamed", dtype, interleaved)
+    g = gen(91)
+    B, H, Hkv, d, rot = 1, 6, 1, 112, 96
+    x = torch.randn(B, 3000, (H + 2 * Hkv) * d, generator=g).to(dtype).cuda().repeat(1, n // 3000, 1)
+    q, k = x[..., :H * d].unflatten(-1, (H, d)), x[..., H * d:(H + Hkv) * d].unflatten(-1, (Hkv, d))
+    pos, freq, axis = ladder(g, B, n, rot, 3, far=100000)
+    w = (1 + 0.2 * torch.randn(2, d, generator=g)).cuda()
+    args = dict(axis=axis, interleaved=interleaved, norm=True, qw=w[0], kw=w[1])
+    qo, ko = spk.sparsek_rope_fwd(q, k, pos, freq, **args)
+    dqo, dko = qo.flip(2).contiguous(), ko.flip(2).contiguous()
+    dq, dk, dqw, dkw = spk.sparsek_rope_bwd(q, k, pos, freq, dqo, dko, **args)
+    for a in (0, 777, n - 500):
+        rows = slice(a, a + 500)
+        got = check(q[:, rows], k[:, rows], pos[:, :, rows].contiguous(), freq, **args) if a == 777 else spk.sparsek_rope_fwd(
+            q[:, rows], k[:, rows], pos[:, :, rows].contiguous(), freq, **args)
+        back = spk.sparsek_rope_bwd(q[:, rows], k[:, rows], pos[:, :, rows].contiguous(), freq, dqo[:, :, rows].contiguous(), dko[:, :, rows].contiguous(), **args)
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], qo[:, :, rows]) and torch.equal(got[1], ko[:, :, rows])
+        assert torch.equal(back[0], dq[:, rows]) and torch.equal(back[1], dk[:, rows])
+    for y, do, dw, heads in ((q, dqo, dqw, H), (k, dko, dkw, Hkv)):
+        want, size = torch.zeros(d).double(), torch.zeros(d).double()
+        for a in range(0, n, 15000):
+            _, p, _, m = ref.bwd(y[:, a:a + 15000], pos[:, :, a:a + 15000], freq, axis, interleaved, True, w[0], 1e-6, do[:, :, a:a + 15000])
+            want, size = want + p, size + m
+        held(dw, want, 2 * size)   # (a lane adds up three groups of tokens here, and one in a stretch: 3 heads + 128 steps, below twice heads + 128)

@@ -34,9 +34,9 @@ def calls(c, L=None):
 
 
 @pytest.mark.parametrize("kw,rc", [(x, -1) for x in (
-    dict(B=0), dict(H=0), dict(Hkv=-1), dict(n=0), dict(d=0), dict(rot=-8), dict(rot=72), dict(axes=0), dict(eps=0.0), dict(eps=-1.0), dict(eps=float("nan")),
+    dict(B=0), dict(H=0), dict(Hkv=-1), dict(n=0), dict(d=0), dict(rot=-8), dict(rot=72), dict(axes=0), dict(eps=0.0), dict(eps=1e-39), dict(eps=-1.0), dict(eps=float("nan")),
     dict(eps=float("inf")), dict(q=strides(-4, 512, 64)), dict(q=strides(5120, 510, 64)), dict(k=strides(2 ** 46, 512, 64)), dict(k=strides(5120, 2 ** 45, 64)))] +
-    [(x, -2) for x in (dict(dtype=spk.I8), dict(d=60, rot=0), dict(d=264), dict(rot=12), dict(axes=5), dict(H=65535, Hkv=1), dict(B=65536, n=32768))])
+    [(x, -2) for x in (dict(dtype=spk.I8), dict(d=60, rot=0), dict(d=264), dict(rot=12), dict(axes=5), dict(H=65535, Hkv=1), dict(B=65536, n=2048))])
 def test_configurations(kw, rc):
     c = cfg(**kw)
     assert spk.lib().sparsek_rope_bwd_workspace_bytes(c) == 0
