@@ -5,8 +5,9 @@
 // Backward, of dout: g = the rotation by -a of dout, dw = sum over rows of x r g, dx = r (w g - x r^2 mean(x w g)).
 //
 // A row is one head of one token.  Its lanes have 8 channels each, four and the four that they turn with (pairs half a rotation apart), or
-// eight neighbours, so a pair never leaves a lane; a token's lanes go through the heads, and the angles, which depend on the token
-// alone, are made once.
+// four of either half (neighbours), so a pair never leaves a lane; a token's lanes go through the heads, and the angles, which depend on the
+// token alone, are made once.  What bounds it is memory: a document of 32768, 32 + 8 heads of 128, is normed and turned in 136 us, at 4.9 TB/s
+// (a copy of 1 GiB reaches 5.1), its vector instructions beside that for 60 % of the time; backward 4 x 8192 tokens of 32 heads take 168 us (4.8).
 #include "block_parts.hpp"
 
 namespace spk {
@@ -24,7 +25,7 @@ struct RopeArgs {
     int tiles;       // of a workgroup's tokens
 };
 
-constexpr int W = 4;   // channels of a lane in either half (eight bf16 values, 16 bytes to a load: 138 us for a document of 32768 too)
+constexpr int W = 4;   // channels of a lane in either half (eight bf16 values, 16 bytes to a load, are no faster)
 
 // W values of storage type T, as they lie and in fp32.
 template <class T>
@@ -39,7 +40,8 @@ struct Some<uint16_t> {
     }
     static __device__ __forceinline__ Raw narrow(const float (&x)[W])
     {
-        return Raw{(unsigned)f32_to_bf16(x[0]) | (unsigned)f32_to_bf16(x[1]) << 16, (unsigned)f32_to_bf16(x[2]) | (unsigned)f32_to_bf16(x[3]) << 16};
+        typedef __bf16 Four __attribute__((ext_vector_type(4)));   // (to the nearest, even on ties, two to an instruction)
+        return __builtin_bit_cast(Raw, Four{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]});
     }
 };
 template <>
@@ -140,9 +142,9 @@ __device__ __forceinline__ void turn(bool interleaved, bool back, const Chunk& c
     }
 }
 
-// Rows of a token that are on their way together.  Four where much is streamed in bf16 (a document of 32768, 32 + 8 heads of 128: 138 us, one
-// at a time 140; training on it 300 and 308); one is faster where the caches have it (two prompts of 5003: 19.0 us, four 20.4), and in fp32, whose
-// rows are twice as long (a training pass of 4 x 2000, 24 heads of 64: 55 us, four 63; of 16 x 2000 199 and 198).
+// Rows of a token that are on their way together.  Four where much is streamed in bf16 (a document of 32768, 32 + 8 heads of 128: 136 us, one
+// at a time 138; training on video, 4 x 8192 tokens, 286 and 303); one where the caches have it (a document of 8192 38.5 us, four 41.4) and in fp32,
+// whose rows are twice as long (a training pass of 4 x 2000, 24 heads of 64: 57 us, four 70; of 16 x 2000 198 and 199).
 template <class T, bool STREAM>
 constexpr int rows_at_once() { return STREAM && sizeof(T) == 2 ? 4 : 1; }
 
@@ -213,7 +215,7 @@ __global__ __launch_bounds__(256) void rope_fwd_kernel(RopeArgs p)
 
 // A workgroup takes `tiles` groups of tokens one after another and all of its heads, and leaves its part of the sums for the weights.
 template <class T, int LPR, bool STREAM>
-__global__ __launch_bounds__(256) void rope_bwd_kernel(RopeArgs p)
+__global__ __launch_bounds__(256, 3) void rope_bwd_kernel(RopeArgs p)
 {
     constexpr int TOK = 256 / LPR, ROWS = rows_at_once<T, STREAM>();
     __shared__ float sums[TOK][2 * W * LPR + 1];
@@ -344,8 +346,8 @@ static RopeShape rope_shape(const sparsek_rope_cfg& c)
     return s;
 }
 // Whether a call that reads or writes every value `passes` times goes past the last cache, of 256 MB (streamed and not: a document of 32768, 671 MB,
-// 138 and 148 us; of 12000, 246 MB, 53.7 and 60.1; of 8192, 168 MB, 39.0 both; two prompts of 5003, 92 MB, 31 and 19; forward of 16 x 2000 tokens in
-// fp32, 393 MB, 76 and 82).
+// 136 and 149 us; of 12000, 246 MB, 51.6 and 58.4; of 8192, 168 MB, 37.7 and 38.5; two prompts of 5003, 92 MB, 28 and 17; forward of 16 x 2000 tokens
+// in fp32, 393 MB, 75 and 81; of 4 x 2000, 98 MB, 20.6 and 19.3).
 static bool rope_streams(const sparsek_rope_cfg& c, int passes)
 {
     return (double)passes * c.B * c.n * (c.H + c.Hkv) * c.d * (c.dtype == SPARSEK_BF16 ? 2 : 4) > 200e6;
@@ -373,8 +375,9 @@ static RopeArgs rope_args(const sparsek_rope_cfg& c, const void* q, const void* 
     if (c.dtype == SPARSEK_F32) { BY_LANES(float, lpr, stream, LAUNCH) }   \
     else { BY_LANES(uint16_t, lpr, stream, LAUNCH) }
 
-// Workgroups that share a token's heads: as many as leave 2048 in all.
-static int head_shares(long long groups, int heads) { return (int)std::max<long long>(1, std::min<long long>(heads, 2048 / std::max<long long>(groups, 1))); }
+// Workgroups that share a token's heads: as many as leave 1024 in all (training on 4 x 500 tokens, 16 + 16 heads of 128: 30.4 us, with 512 28.4, with
+// 2048 39.1; on 4 x 2000: 79, 91 and 87; each share makes the angles anew).
+static int head_shares(long long groups, int heads) { return (int)std::max<long long>(1, std::min<long long>(heads, 1024 / std::max<long long>(groups, 1))); }
 
 int launch_rope_fwd(const sparsek_rope_cfg& c, const void* q, const void* k, const int32_t* pos, const float* freq, const int32_t* axis,
                     const float* qw, const float* kw, void* qo, void* ko, hipStream_t st)

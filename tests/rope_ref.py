@@ -78,9 +78,10 @@ def bwd(x, pos, freq, axis, interleaved, norm, w, eps, grad):
     dx = r * (w * g) - xd * r ** 3 * (xd * w * g).mean(-1, keepdim=True)
     bound = half * dx.abs() + r * w.abs() * lost + xd.abs() * r ** 3 * (xd.abs() * w.abs() * (lost + 2 ** -18 * m)).mean(-1, keepdim=True) + 1e-37
     dw = (xd * r * g).sum((0, 1, 2))
-    # sums of fp32: a lane's rows one after another (every head of its tokens, 2048 groups of tokens at once), the tokens of a group (128 at most)
+    # sums of fp32: a lane's rows one after another (every head of its tokens, 2048 groups of tokens at once), then the tokens of a group (256 lanes,
+    # of which a row has one for 8 channels, a power of two of them)
     B, n, heads, d = x.shape
-    lanes = 2 ** max(1, math.ceil(math.log2(d / 8)))
-    steps = heads * -(-(-(-B * n // (256 // lanes))) // 2048) + 128
+    group = 256 // 2 ** math.ceil(math.log2(d / 8))
+    steps = heads * -(-(-(-B * n // group)) // 2048) + group + 4
     wb = 2 ** -24 * steps * (xd.abs() * r * m).sum((0, 1, 2)) + (xd.abs() * r * lost).sum((0, 1, 2)) + 2 ** -24 * dw.abs() + 1e-37
     return dx, dw, bound, wb
