@@ -5,9 +5,10 @@
 // block at the end of a sequence is kept in bf16, values transposed as well.  Page numbers outside the pool are never
 // followed: such a page is neither written nor attended.
 //
-// What bounds the kernels is memory where there is much to move (four prompts of 8192 go in at 5.2 TB/s, 64 sequences of up to 8192 are
-// attended at 5.4 TB/s of the kernel's time) and the length of a chain of dependent steps where there is little: a token's append takes
-// 3 us, 6 to 8 where it ends a block; the choice among 1024 blocks 12; the attention of 200 tokens 8; an eviction from 129 blocks 6.
+// What bounds the kernels is memory where there is much to move (four prompts of 8192 go in at 5.6 TB/s, 64 sequences of up to 8192 are
+// attended at 5.4 TB/s of the kernel's time, in 4 bits at 5.2) and the length of a chain of dependent steps where there is little: a token's
+// append takes 3 us, 6 to 8 where it ends a block; the choice among 1024 blocks 12; the attention of 200 tokens 6 to 8; an eviction from
+// 129 blocks 6.
 #include "cache4_parts.hpp"
 
 namespace spk {
@@ -711,7 +712,10 @@ __global__ __launch_bounds__(256, FORMAT == FORMAT_E2M1 ? 3 : D == 128 ? 2 : 4) 
     const buffer_t wbuf = buffer_of(weighs ? a.weight + head0 * a.units : nullptr, weighs ? live * a.units * 4 : 0);
     const int wat = grp == 0 && col < live ? col * a.units * 4 : 0x7FFFFF00;
     if (FOUR && have) {
-        // As in 8 bits, but codes lie in LDS as they lie in memory: a lane reads what it loaded, 16 bytes at a time.
+        // As in 8 bits, but codes lie in LDS as they lie in memory: a lane reads what it loaded, 16 bytes at a time, and widens it with its group's
+        // scale (four instructions for eight codes).  What bounds it is memory: the vector units are busy 56 % of the time, the products 13 %.
+        // 64 sequences of up to 8192 take 66 us, 5.2 TB/s, with three waves to a SIMD; from memory straight to the lanes' registers, which leaves
+        // two, 75; with four, whose registers spill, 73; with two blocks ahead and two waves 71.
         using P = Page4<D>;
         constexpr int LOADS = P::CODES / 1024 + 1;
         unsigned char *kt = tiles[wv], *vt = kt + P::CODES, *kx = vt + P::CODES, *vx = kx + 256;

@@ -7,7 +7,7 @@
 // A row is one head of one token.  Its lanes have 8 channels each, four and the four that they turn with (pairs half a rotation apart), or
 // four of either half (neighbours), so a pair never leaves a lane; a token's lanes go through the heads, and the angles, which depend on the
 // token alone, are made once.  What bounds it is memory: a document of 32768, 32 + 8 heads of 128, is normed and turned in 136 us, at 4.9 TB/s
-// (a copy of 1 GiB reaches 5.1), its vector instructions beside that for 60 % of the time; backward 4 x 8192 tokens of 32 heads take 168 us (4.8).
+// (a copy of 1 GiB reaches 5.1), its vector instructions beside that for 60 % of the time; backward 4 x 8192 tokens of 32 heads take 170 us (4.7).
 #include "block_parts.hpp"
 
 namespace spk {
