@@ -756,7 +756,7 @@ int check_rope(const sparsek_rope_cfg* c)
     if (c->norm && (!(c->eps >= 0x1p-126f) || !(c->eps < INFINITY))) return SPARSEK_ERR_INVALID_ARG;
     if (c->dtype != SPARSEK_BF16 && c->dtype != SPARSEK_F32) return SPARSEK_ERR_UNSUPPORTED;
     if (c->d % 8 || c->d > 256 || c->rot % 8 || c->axes > 4) return SPARSEK_ERR_UNSUPPORTED;
-    if ((long long)c->H + c->Hkv > 65535 || (long long)c->B * c->n >= (1ll << 27)) return SPARSEK_ERR_UNSUPPORTED;
+    if ((long long)c->H + c->Hkv > 65535 || (long long)c->B * c->n > (1ll << 26)) return SPARSEK_ERR_UNSUPPORTED;
     if (!good(*c, c->q, c->H) || (c->Hkv && !good(*c, c->k, c->Hkv))) return SPARSEK_ERR_INVALID_ARG;
     return SPARSEK_OK;
 }
@@ -806,7 +806,7 @@ int sparsek_rope_bwd(const sparsek_rope_cfg* cfg, const void* q, const void* k, 
     if ((rc = check_rope_inputs(c, c.norm, q, k, pos, freq))) return rc;
     if (!dqo || !dq || (c.Hkv && (!dko || !dk)) || !aligned({dqo, dko, dq, dk, ws})) return SPARSEK_ERR_INVALID_ARG;
     if ((dqw && !c.norm) || (dkw && (!c.norm || !c.Hkv)) || ((dqw || dkw) && !ws)) return SPARSEK_ERR_INVALID_ARG;
-    if (!good(c, c.dq, c.H) || !apart(c, c.dq, c.H) || (c.Hkv && (!good(c, c.dk, c.Hkv) || !apart(c, c.dk, c.Hkv)))) return SPARSEK_ERR_INVALID_ARG;
+    if (dq == dk || !good(c, c.dq, c.H) || !apart(c, c.dq, c.H) || (c.Hkv && (!good(c, c.dk, c.Hkv) || !apart(c, c.dk, c.Hkv)))) return SPARSEK_ERR_INVALID_ARG;
     const size_t row = (size_t)c.B * c.n * c.d * (c.dtype == SPARSEK_BF16 ? 2 : 4);
     const void* in[] = {c.norm ? q : nullptr, dqo, c.norm && c.Hkv ? k : nullptr, c.Hkv ? dko : nullptr};
     const size_t nin[] = {span(c, c.q, c.H), row * c.H, c.Hkv ? span(c, c.k, c.Hkv) : 0, row * c.Hkv};

@@ -165,7 +165,7 @@ __global__ __launch_bounds__(256) void rope_fwd_kernel(RopeArgs p)
 {
     constexpr int TOK = 256 / LPR, ROWS = rows_at_once<T, STREAM>();
     const int c = threadIdx.x % LPR;
-    const unsigned token = blockIdx.x * TOK + threadIdx.x / LPR, all = (unsigned)p.B * p.n;   // (below 2^27)
+    const unsigned token = blockIdx.x * TOK + threadIdx.x / LPR, all = (unsigned)p.B * p.n;   // (at most 2^26)
     const bool live = token < all && 2 * W * c < p.d;
     const Chunk ch = chunk_of(p, live ? c : 0);
     const unsigned at = live ? token : 0, b = at / p.n, t = at - b * p.n;
@@ -227,7 +227,7 @@ __global__ __launch_bounds__(256, 3) void rope_bwd_kernel(RopeArgs p)
 #pragma unroll
     for (int e = 0; e < 2 * W; e++) wsum[0][e] = wsum[1][e] = 0.0f;
     for (int tile = 0; tile < p.tiles; tile++) {
-        const unsigned token = (blockIdx.x * p.tiles + tile) * TOK + row;   // (below 2^27 and a workgroup's share)
+        const unsigned token = (blockIdx.x * p.tiles + tile) * TOK + row;   // (at most 2^26 and a workgroup's share)
         const bool live = token < all && 2 * W * c < p.d;
         const unsigned at = live ? token : 0, b = at / p.n, t = at - b * p.n;
         float co[W], si[W];

@@ -36,7 +36,7 @@ def calls(c, L=None):
 @pytest.mark.parametrize("kw,rc", [(x, -1) for x in (
     dict(B=0), dict(H=0), dict(Hkv=-1), dict(n=0), dict(d=0), dict(rot=-8), dict(rot=72), dict(axes=0), dict(eps=0.0), dict(eps=1e-39), dict(eps=-1.0), dict(eps=float("nan")),
     dict(eps=float("inf")), dict(q=strides(-4, 512, 64)), dict(q=strides(5120, 510, 64)), dict(k=strides(2 ** 46, 512, 64)), dict(k=strides(5120, 2 ** 45, 64)))] +
-    [(x, -2) for x in (dict(dtype=spk.I8), dict(d=60, rot=0), dict(d=264), dict(rot=12), dict(axes=5), dict(H=65535, Hkv=1), dict(B=65536, n=2048))])
+    [(x, -2) for x in (dict(dtype=spk.I8), dict(d=60, rot=0), dict(d=264), dict(rot=12), dict(axes=5), dict(H=65535, Hkv=1), dict(B=65536, n=1025))])
 def test_configurations(kw, rc):
     c = cfg(**kw)
     assert spk.lib().sparsek_rope_bwd_workspace_bytes(c) == 0
@@ -83,6 +83,9 @@ def test_outputs_that_lie_over_inputs_or_themselves():
             args = [far(z + 1) for z in range(14)]
             args[y] = ctypes.c_void_p(args[x].value + 16)
             assert L.sparsek_rope_bwd(c, *args, BIG, NULL) == -1
+    args = [far(z + 1) for z in range(14)]
+    args[10] = args[9]
+    assert L.sparsek_rope_bwd(c, *args, BIG, NULL) == -1
     for s in (strides(5120, 512, 0), strides(0, 512, 64), strides(5120, 0, 64), strides(5120, 192, 64), strides(2048, 512, 64), strides(5120, 512, 60),
               strides(640, 64, 640)):
         assert L.sparsek_rope_bwd(cfg(dq=s), *[far(z + 1) for z in range(14)], BIG, NULL) == -1
