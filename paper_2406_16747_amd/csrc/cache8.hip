@@ -233,25 +233,26 @@ __global__ __launch_bounds__(256) void cache8_append_kernel(CacheArgs a, const i
     if (j * BT >= after) return;
     const uint16_t *kn = k + (size_t)bg * c * D, *vn = v + (size_t)bg * c * D;
     uint16_t *kt = (uint16_t*)a.t.kt + (size_t)bg * BT * D, *vt = (uint16_t*)a.t.vt + (size_t)bg * BT * D;
-    const int page = (j + 1) * BT <= after ? a.t.table[(size_t)bg * a.cap + j] : -1;
-    if (page >= 0 && page < a.pages) {
-        u32x4 kr[R::NT];
+    if ((j + 1) * BT <= after) {
+        const int page = a.t.table[(size_t)bg * a.cap + j];   // (not waited for before the tokens are asked for)
+        u32x4 kr[R::NT], vr[R::NT];
         unsigned tv = 0;
         const int old = max(0, len - j * BT);   // tokens of the block that are there already (in the first one only)
         const int tok0 = tid / R::CPR, col = 8 * (tid % R::CPR);
 #pragma unroll
+        for (int t = 0; t < R::NT; t++) {   // (all of them on their way together, old tokens' values as new ones' that nobody looks at)
+            const int x = tok0 + R::RG * t;
+            const size_t at = (size_t)(j * BT + max(x, old) - len) * D + col;
+            kr[t] = __builtin_nontemporal_load((const u32x4*)(x < old ? kt + x * D + col : kn + at));
+            vr[t] = __builtin_nontemporal_load((const u32x4*)(vn + at));
+        }
+#pragma unroll
         for (int t = 0; t < R::NT; t++) {
             const int x = tok0 + R::RG * t;
-            const size_t at = (size_t)(j * BT + x - len) * D + col;
-            if (x < old) {
-                kr[t] = *(const u32x4*)(kt + x * D + col);
-                continue;
-            }
-            kr[t] = __builtin_nontemporal_load((const u32x4*)(kn + at));
-            const u32x4 vr = __builtin_nontemporal_load((const u32x4*)(vn + at));
-            tv = max(tv, top_of_8(vr));
+            if (x < old) continue;
+            tv = max(tv, top_of_8(vr[t]));
 #pragma unroll
-            for (int e = 0; e < 8; e++) sm.vt[AppendSmem<D>::at(col + e, x)] = (uint16_t)(e & 1 ? vr[e / 2] >> 16 : vr[e / 2] & 0xFFFFu);
+            for (int e = 0; e < 8; e++) sm.vt[AppendSmem<D>::at(col + e, x)] = (uint16_t)(e & 1 ? vr[t][e / 2] >> 16 : vr[t][e / 2] & 0xFFFFu);
         }
         if (old) {   // (8 tokens of a column at a time, the last of them perhaps in part)
             u32x4 vo[D * 8 / 256];
@@ -275,7 +276,7 @@ __global__ __launch_bounds__(256) void cache8_append_kernel(CacheArgs a, const i
                 }
             }
         }
-        store_block<D, FORMAT>(sm, a, page, kr, tv, tid);
+        if (page >= 0 && page < a.pages) store_block<D, FORMAT>(sm, a, page, kr, tv, tid);
     }
     const int whole = after / BT;   // the block that stays unfinished, if it has tokens
     if (len % BT && whole > first ? blockIdx.x != 0 : j != whole) return;
