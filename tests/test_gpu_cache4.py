@@ -180,17 +180,18 @@ def test_blocks_of_all_kinds(kind, d):
 
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("where", ["key", "value"])
-def test_what_a_query_does_not_weigh_does_not_move_it(where, d):
-    """A key of 1e30 in a channel where the query is 0, or a value of 1e30 whose weight is 0: the others of its block keep all their bits."""
+@pytest.mark.parametrize("e", [10, 20, 27, 30, 33, 35, 36, 37, 38, 39, 100])
+def test_what_a_query_does_not_weigh_does_not_move_it(where, e, d):
+    """A key of 2^e in a channel where the query is 0, or a value of 2^e whose weight is 0: the others of its block keep all their bits."""
     require_gpu()
-    say("cache4, an outlier beside ordinary", where, d)
+    say("cache4, an outlier beside ordinary", where, e, d)
     g = gen(14)
     k, v, q = rand(g, 1, 1, 64, d), rand(g, 1, 1, 64, d), rand(g, 1, 2, d)
     q[..., 40] = 0.0
     if where == "key":
-        k[0, 0, 9, 40] = 1e30
+        k[0, 0, 9, 40] = 2.0 ** e
     else:
-        v[0, 0, 9, 40] = 1e30
+        v[0, 0, 9, 40] = 2.0 ** e
         k[0, 0, 9] = (-1e4 * q[0, 0].float().sign()).bfloat16()
         q[0, 1] = q[0, 0]
     cache, L = given(k, v, 2, 3)
@@ -595,3 +596,44 @@ def test_one_workgroup_or_many(H, Hkv, B, n, d):
         assert ((ref.f64(o[b:b + 1]) - ro).abs() <= ob).all()
         assert ((lse[b:b + 1].cpu().double() - rl).abs() <= 2e-4).all()
         assert ((ref.f64(cache.mass[b:b + 1]) - rm).abs() <= 2 ** -12 * rm).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("H,Hkv", [(4, 2), (40, 2)])
+def test_wide_pages_among_others(H, Hkv, d):
+    """Pages whose scales lie far apart in keys, in values or in both, beside ordinary ones, ones with a value that is not finite, and ones outside the
+    pool: over all tokens and over chosen blocks, with the masses."""
+    require_gpu()
+    say("cache4, wide pages among others", H, Hkv, d)
+    B, n = 2, 700
+    g = gen(121)
+    k, v, q = rand(g, B, Hkv, n, d), rand(g, B, Hkv, n, d), rand(g, B, H, d)
+    far, off = (torch.exp2(torch.randint(-60, 1, s, generator=g).float()).cuda().bfloat16() for s in ((B, Hkv, n, 1), (B, Hkv, 1, d)))   # (32 share a scale)
+    block = torch.arange(n).cuda() // 64
+    k = torch.where((block % 3 == 1).view(1, 1, n, 1), k * far, k)
+    v = torch.where((block % 4 >= 2).view(1, 1, n, 1), v * off, v)
+    cap = n // 64 + 1
+    cache, L = given(k, v, H, cap)
+    cache.table[1, 0, 4] = -1
+    wide = (cache.ks.view(torch.int32) & 0x7FFFFF) != 0, (cache.vs.view(torch.int32) & 0x7FFFFF) != 0
+    assert all(x.any() and not x.all() for x in wide)
+    idx = ints([1, 2, 4, 7]).expand(B, Hkv, 4).contiguous()
+    for x in (None, idx):
+        cache.mass.zero_()
+        o, lse = spk.sparsek_cache4_attn(cache, L, q, x, accumulate=True)
+        torch.cuda.synchronize()
+        ro, rl, rm, ob = ref.cache_attn(cache, [n] * B, q, None if x is None else x.cpu())
+        assert ((ref.f64(o) - ro).abs() <= ob).all(), float(((ref.f64(o) - ro).abs() / ob).max())
+        assert ((lse.cpu().double() - rl).abs() <= 2e-4).all()
+        assert ((ref.f64(cache.mass) - rm).abs() <= 2 ** -12 * rm).all()
+    # a key that is not finite in a block whose values are wide, and a value in one whose keys are
+    for x, b, at in ((k, 0, 64 * 3 + 5), (v, 1, 64 * 1 + 9)):
+        x[b, 1, at, 11] = float("nan")
+    cache, L = given(k, v, H, cap)
+    o, lse = spk.sparsek_cache4_attn(cache, L, q)
+    torch.cuda.synchronize()
+    ro, rl, _, ob = ref.cache_attn(cache, [n] * B, q)
+    bad = torch.zeros(B, H, dtype=torch.bool)
+    bad[0, H // 2:] = bad[1, H // 2:] = True
+    assert torch.isnan(o[bad.cuda()]).all() and torch.isnan(lse[0, H // 2:]).all() and torch.isfinite(lse[1]).all()
+    assert ((ref.f64(o) - ro).abs() <= ob)[~bad].all()
