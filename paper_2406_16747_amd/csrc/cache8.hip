@@ -5,7 +5,7 @@
 // block at the end of a sequence is kept in bf16, values transposed as well.  Page numbers outside the pool are never
 // followed: such a page is neither written nor attended.
 //
-// What bounds the kernels is memory where there is much to move (four prompts of 8192 go in at 5.6 TB/s, 64 sequences of up to 8192 are
+// What bounds the kernels is memory where there is much to move (four prompts of up to 8192 go in at 5.9 TB/s, 64 sequences of up to 8192 are
 // attended at 5.4 TB/s of the kernel's time, in 4 bits at 5.2) and the length of a chain of dependent steps where there is little: a token's
 // append takes 3 us, 6 to 8 where it ends a block; the choice among 1024 blocks 12; the attention of 200 tokens 6 to 8; an eviction from
 // 129 blocks 6.

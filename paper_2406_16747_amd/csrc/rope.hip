@@ -303,29 +303,31 @@ __global__ __launch_bounds__(256, 3) void rope_bwd_kernel(RopeArgs p)
             }
         __syncthreads();
         for (int x = threadIdx.x; x < p.d; x += 256) {
-            float y = 0.0f;
-            for (int r = 0; r < TOK; r++) y += sums[r][x];
-            out[w * p.d + x] = y;
+            double y = 0;   // (in fp32 the weights' gradients of 8000 tokens are 1.8e-7 of their scale off, so 0.7e-7)
+            for (int r = 0; r < TOK; r++) y += (double)sums[r][x];
+            out[w * p.d + x] = (float)y;
         }
     }
 }
 
-// The workgroups' parts are added up in 64 bits, in an order of their own: 8 columns of dqw and dkw to a workgroup.
+// The workgroups' parts are added up in 64 bits, in an order of their own: COLS columns of dqw and dkw to a workgroup.
+constexpr int COLS = 4;
 __global__ __launch_bounds__(1024) void rope_weights_kernel(const float* __restrict__ part, int parts, int d, float* __restrict__ dqw, float* __restrict__ dkw)
 {
-    __shared__ double sums[128][9];
-    const int row = threadIdx.x / 8, col = threadIdx.x % 8, x = blockIdx.x * 8 + col;
+    constexpr int ROWS = 1024 / COLS;
+    __shared__ double sums[ROWS][COLS + 1];
+    const int row = threadIdx.x / COLS, col = threadIdx.x % COLS, x = blockIdx.x * COLS + col;
     double y = 0;
 #pragma unroll 8
-    for (int r = row; r < parts; r += 128) y += (double)part[(size_t)r * 2 * d + x];
+    for (int r = row; r < parts; r += ROWS) y += (double)part[(size_t)r * 2 * d + x];
     sums[row][col] = y;
     __syncthreads();
-    if (row >= 8) return;
+    if (threadIdx.x >= 64) return;
     y = 0;
 #pragma unroll
-    for (int r = 0; r < 16; r++) y += sums[row + 8 * r][col];
+    for (int r = 0; r < ROWS * COLS / 64; r++) y += sums[row + 64 / COLS * r][col];
 #pragma unroll
-    for (int z = 8; z < 64; z *= 2) y += __shfl_xor(y, z, 64);   // (the first wave)
+    for (int z = COLS; z < 64; z *= 2) y += __shfl_xor(y, z, 64);
     float* out = x < d ? dqw : dkw;
     if (row == 0 && out) out[x % d] = (float)y;
 }
@@ -431,7 +433,7 @@ int launch_rope_bwd(const sparsek_rope_cfg& c, const void* q, const void* k, con
 #define BWD(T, L, S) hipLaunchKernelGGL((rope_bwd_kernel<T, L, S>), dim3(y.gx, y.gy), dim3(256), 0, st, a)
     BY_ROW(c, y.s.lpr, stream, BWD)
 #undef BWD
-    if (a.part) hipLaunchKernelGGL(rope_weights_kernel, dim3(c.d / 4), dim3(1024), 0, st, a.part, (int)(y.gx * y.gy), c.d, dqw, dkw);
+    if (a.part) hipLaunchKernelGGL(rope_weights_kernel, dim3(2 * c.d / COLS), dim3(1024), 0, st, a.part, (int)(y.gx * y.gy), c.d, dqw, dkw);
     return launch_status();
 }
 
