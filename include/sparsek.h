@@ -425,8 +425,8 @@ int sparsek_cache4_evict(const sparsek_cache8_cfg *cfg, const sparsek_cache4 *ca
  * place may coincide with another: INVALID_ARG within a tensor), and dqw, dkw [d] fp32, NULL: not wanted (norm == 0: they must be NULL).  q and k are not read where norm == 0 and may be NULL.
  * The sums behind dqw and dkw have an order of their own that does not depend on timing.
  * SPARSEK_BF16 or SPARSEK_F32; d a multiple of 8, 8 .. 256; rot a multiple of 8, 0 .. d; axes 1 .. 4; H + Hkv <= 65535, B n <= 2^26 (UNSUPPORTED
- * otherwise).  Strides are in elements, not negative, multiples of 4, and the last row begins below 2^46; tensors and ws begin at multiples of 16 bytes; outputs overlap no
- * inputs (INVALID_ARG otherwise). */
+ * otherwise).  Strides are in elements, not negative, multiples of 4, and the last row begins below 2^46; q, k, qo, ko, their gradients and ws begin at
+ * multiples of 16 bytes; outputs and ws overlap no inputs and each other only as dq and dk may, row beside row (INVALID_ARG otherwise). */
 typedef struct {
     int64_t batch, token, head;   /* elements between neighbours; channels are contiguous */
 } sparsek_rope_strides;

@@ -736,6 +736,8 @@ size_t span(const sparsek_rope_cfg& c, const sparsek_rope_strides& s, int heads)
     return (size_t)last * (c.dtype == SPARSEK_BF16 ? 2 : 4);
 }
 
+size_t positions(const sparsek_rope_cfg& c) { return c.rot ? (size_t)c.axes * c.B * c.n * 4 : 0; }
+
 // Whether every place of a strided output has an address of its own: each stride steps over all that the smaller ones reach.
 bool apart(const sparsek_rope_cfg& c, const sparsek_rope_strides& s, int heads)
 {
@@ -761,6 +763,25 @@ int check_rope(const sparsek_rope_cfg* c)
     return SPARSEK_OK;
 }
 
+struct Place {
+    const void* p;
+    size_t n;
+    bool on(const Place& x) const { return p && x.p && n && x.n && overlap(p, n, x.p, x.n); }
+};
+
+// Whether an output lies over an input or over another output.
+template <int IN, int OUT>
+bool any_overlap(const Place (&in)[IN], const Place (&out)[OUT])
+{
+    for (int x = 0; x < OUT; x++) {
+        for (const Place& y : in)
+            if (out[x].on(y)) return true;
+        for (int y = 0; y < x; y++)
+            if (out[x].on(out[y])) return true;
+    }
+    return false;
+}
+
 // Arguments that both directions share.  (x_read: q and k are read.)
 int check_rope_inputs(const sparsek_rope_cfg& c, bool x_read, const void* q, const void* k, const int32_t* pos, const float* freq)
 {
@@ -781,12 +802,11 @@ int sparsek_rope_fwd(const sparsek_rope_cfg* cfg, const void* q, const void* k, 
     const sparsek_rope_cfg& c = *cfg;
     if ((rc = check_rope_inputs(c, true, q, k, pos, freq))) return rc;
     if (!qo || (c.Hkv && !ko) || !aligned({qo, ko})) return SPARSEK_ERR_INVALID_ARG;
-    const size_t row = (size_t)c.B * c.n * c.d * (c.dtype == SPARSEK_BF16 ? 2 : 4), nq = span(c, c.q, c.H), nqo = row * c.H, nko = row * c.Hkv;
-    if (overlap(q, nq, qo, nqo)) return SPARSEK_ERR_INVALID_ARG;
-    if (c.Hkv) {
-        const size_t nk = span(c, c.k, c.Hkv);
-        if (overlap(q, nq, ko, nko) || overlap(k, nk, qo, nqo) || overlap(k, nk, ko, nko) || overlap(qo, nqo, ko, nko)) return SPARSEK_ERR_INVALID_ARG;
-    }
+    const size_t row = (size_t)c.B * c.n * c.d * (c.dtype == SPARSEK_BF16 ? 2 : 4), nw = (size_t)c.d * 4;
+    const Place in[] = {{q, span(c, c.q, c.H)}, {k, c.Hkv ? span(c, c.k, c.Hkv) : 0}, {pos, positions(c)}, {freq, c.rot * 2u}, {axis, c.rot * 2u},
+                        {qw, nw}, {kw, nw}};
+    const Place out[] = {{qo, row * c.H}, {ko, row * c.Hkv}};
+    if (any_overlap(in, out)) return SPARSEK_ERR_INVALID_ARG;
     return spk::launch_rope_fwd(c, q, k, pos, freq, axis, qw, kw, qo, ko, (hipStream_t)stream);
 }
 
@@ -807,15 +827,17 @@ int sparsek_rope_bwd(const sparsek_rope_cfg* cfg, const void* q, const void* k, 
     if (!dqo || !dq || (c.Hkv && (!dko || !dk)) || !aligned({dqo, dko, dq, dk, ws})) return SPARSEK_ERR_INVALID_ARG;
     if ((dqw && !c.norm) || (dkw && (!c.norm || !c.Hkv)) || ((dqw || dkw) && !ws)) return SPARSEK_ERR_INVALID_ARG;
     if (dq == dk || !good(c, c.dq, c.H) || !apart(c, c.dq, c.H) || (c.Hkv && (!good(c, c.dk, c.Hkv) || !apart(c, c.dk, c.Hkv)))) return SPARSEK_ERR_INVALID_ARG;
-    const size_t row = (size_t)c.B * c.n * c.d * (c.dtype == SPARSEK_BF16 ? 2 : 4);
-    const void* in[] = {c.norm ? q : nullptr, dqo, c.norm && c.Hkv ? k : nullptr, c.Hkv ? dko : nullptr};
-    const size_t nin[] = {span(c, c.q, c.H), row * c.H, c.Hkv ? span(c, c.k, c.Hkv) : 0, row * c.Hkv};
-    for (int x = 0; x < 4; x++) {
-        if (!in[x]) continue;
-        if (overlap(in[x], nin[x], dq, span(c, c.dq, c.H))) return SPARSEK_ERR_INVALID_ARG;
-        if (c.Hkv && overlap(in[x], nin[x], dk, span(c, c.dk, c.Hkv))) return SPARSEK_ERR_INVALID_ARG;
+    const size_t row = (size_t)c.B * c.n * c.d * (c.dtype == SPARSEK_BF16 ? 2 : 4), nw = (size_t)c.d * 4, need = spk::rope_bwd_ws_bytes(c);
+    const bool sums = dqw || dkw;
+    const Place in[] = {{q, c.norm ? span(c, c.q, c.H) : 0}, {k, c.norm && c.Hkv ? span(c, c.k, c.Hkv) : 0}, {dqo, row * c.H}, {dko, row * c.Hkv},
+                        {pos, positions(c)}, {freq, c.rot * 2u}, {axis, c.rot * 2u}, {qw, c.norm ? nw : 0}, {kw, c.norm ? nw : 0}};
+    const Place dx[] = {{dq, span(c, c.dq, c.H)}, {dk, c.Hkv ? span(c, c.dk, c.Hkv) : 0}}, other[] = {{dqw, nw}, {dkw, nw}, {ws, sums ? need : 0}};
+    for (const Place& x : dx) {   // (which may be slices of one gradient)
+        const Place one[] = {x};
+        if (any_overlap(in, one) || any_overlap(one, other)) return SPARSEK_ERR_INVALID_ARG;
     }
-    if ((dqw || dkw) && ws_bytes < spk::rope_bwd_ws_bytes(c)) return SPARSEK_ERR_WORKSPACE;
+    if (any_overlap(in, other)) return SPARSEK_ERR_INVALID_ARG;
+    if (sums && ws_bytes < need) return SPARSEK_ERR_WORKSPACE;
     return spk::launch_rope_bwd(c, q, k, pos, freq, axis, qw, kw, dqo, dko, dq, dk, dqw, dkw, ws, (hipStream_t)stream);
 }
 

@@ -91,6 +91,25 @@ def test_outputs_that_lie_over_inputs_or_themselves():
         assert L.sparsek_rope_bwd(cfg(dq=s), *[far(z + 1) for z in range(14)], BIG, NULL) == -1
 
 
+def test_outputs_that_lie_over_what_goes_with_the_inputs():
+    L, c = spk.lib(), cfg()
+    for x in range(2, 7):
+        for y in (7, 8):
+            args = [far(z + 1) for z in range(9)]
+            args[y] = ctypes.c_void_p(args[x].value + 16)
+            assert L.sparsek_rope_fwd(c, *args, NULL) == -1, (x, y)
+    for x in range(9):
+        for y in range(9, 14):
+            args = [far(z + 1) for z in range(14)]
+            args[y] = args[x]
+            assert L.sparsek_rope_bwd(c, *args, BIG, NULL) == -1, (x, y)
+    for x in range(9, 14):
+        for y in range(max(x + 1, 11), 14):
+            args = [far(z + 1) for z in range(14)]
+            args[y] = args[x]
+            assert L.sparsek_rope_bwd(c, *args, BIG, NULL) == -1, (x, y)
+
+
 def test_the_binding_refuses_tensors_of_another_kind():
     q, k = torch.zeros(1, 10, 4, 64, dtype=torch.bfloat16), torch.zeros(1, 10, 2, 64, dtype=torch.bfloat16)
     pos, freq, w = torch.zeros(1, 1, 10, dtype=torch.int32), torch.ones(32), torch.ones(64)
