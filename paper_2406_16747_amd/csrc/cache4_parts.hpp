@@ -1,9 +1,9 @@
 // The cache in 4 bits: what its append, its attention and its reading back share.
 //
 // A value is an e2m1 code (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign) times a power of two that 32 values share: of keys 32 channels of a token, of
-// values 32 tokens of a channel.  The power is the smallest with which none of the 32 passes 6, so a value is off by a sixth of the
-// largest at most, and scaling loses nothing.  Inside a page codes and scales lie as the lanes of the matrix instructions take them, 16
-// bytes of codes to a lane at a time: the attention's loads are whole lines, straight into registers.
+// values 32 tokens of a channel.  The power is the smallest with which none of the 32 passes 6, so a value is off by a fifth of the
+// largest at most (where that is 5 times the power, 4 stands for it), and scaling loses nothing.  Inside a page codes and scales lie as the
+// lanes of the matrix instructions take them, 16 bytes of codes to a lane at a time: the attention's loads are whole lines, straight into LDS.
 #pragma once
 #include "block_parts.hpp"
 
