@@ -160,30 +160,118 @@ struct Weights {
     }
 };
 
-template <class T, int LPR, bool STREAM>
+// Where a lane loads and stores: two pieces of W channels.  They are those that it turns, a and b; or, LINES, those that stand at its place
+// among all of its wave's, token after token, and change hands in LDS, so that whole lines come and go where a's and b's are less.
+struct Piece {
+    unsigned b, t;
+    int ch;
+    bool live;
+};
+template <int LPR, bool LINES>
+struct Pieces {
+    Piece at[2];
+    int a, b;   // LINES: where those that it turns lie among the wave's
+    __device__ __forceinline__ Pieces(const RopeArgs& p, const Chunk& ch, unsigned token, unsigned all)
+    {
+        const int lane = threadIdx.x % 64, c = lane % LPR;
+        if constexpr (LINES) {
+            const int row = p.d / W, first = lane / LPR * row;
+            a = first + ch.a / W;
+            b = first + ch.b / W;
+#pragma unroll
+            for (int x = 0; x < 2; x++) {
+                const int m = lane + 64 * x, of = m / row;
+                const unsigned tk = token - lane / LPR + of;
+                at[x].live = of < 64 / LPR && tk < all;
+                at[x].ch = W * (m - of * row);
+                at[x].b = at[x].live ? tk / p.n : 0;
+                at[x].t = at[x].live ? tk - at[x].b * p.n : 0;
+            }
+        } else {
+            at[0].live = token < all && 2 * W * c < p.d;
+            at[0].b = at[0].live ? token / p.n : 0;
+            at[0].t = at[0].live ? token - at[0].b * p.n : 0;
+            at[1] = at[0];
+            at[0].ch = ch.a;
+            at[1].ch = ch.b;
+        }
+    }
+    // From the pieces that were loaded to those that are turned, ROWS heads at once, and back (mine: the lane has some to turn).
+    template <int ROWS, class Raw>
+    __device__ __forceinline__ void take(Raw (*lds)[128], Raw (&x)[ROWS], Raw (&y)[ROWS]) const
+    {
+        if constexpr (LINES) {
+            const int lane = threadIdx.x % 64;
+            wave_lds_order();
+#pragma unroll
+            for (int u = 0; u < ROWS; u++) {
+                lds[u][lane] = x[u];
+                lds[u][lane + 64] = y[u];
+            }
+            wave_lds_order();
+#pragma unroll
+            for (int u = 0; u < ROWS; u++) {
+                x[u] = lds[u][a];
+                y[u] = lds[u][b];
+            }
+        }
+    }
+    template <int ROWS, class Raw>
+    __device__ __forceinline__ void give(Raw (*lds)[128], bool mine, Raw (&x)[ROWS], Raw (&y)[ROWS]) const
+    {
+        if constexpr (LINES) {
+            const int lane = threadIdx.x % 64;
+            wave_lds_order();
+            if (mine)
+#pragma unroll
+                for (int u = 0; u < ROWS; u++) {
+                    lds[u][a] = x[u];
+                    lds[u][b] = y[u];
+                }
+            wave_lds_order();
+#pragma unroll
+            for (int u = 0; u < ROWS; u++) {
+                x[u] = lds[u][lane];
+                y[u] = lds[u][lane + 64];
+            }
+        }
+    }
+};
+
+template <class T, int LPR, bool STREAM, bool LINES>
 __global__ __launch_bounds__(256) void rope_fwd_kernel(RopeArgs p)
 {
+    typedef typename Some<T>::Raw Raw;
     constexpr int TOK = 256 / LPR, ROWS = rows_at_once<T, STREAM>();
+    __shared__ Raw pieces[LINES ? 4 * ROWS : 1][128];
+    Raw(*lds)[128] = &pieces[LINES ? threadIdx.x / 64 * ROWS : 0];
     const int c = threadIdx.x % LPR;
     const unsigned token = blockIdx.x * TOK + threadIdx.x / LPR, all = (unsigned)p.B * p.n;   // (at most 2^26)
-    const bool live = token < all && 2 * W * c < p.d;
-    const Chunk ch = chunk_of(p, live ? c : 0);
-    const unsigned at = live ? token : 0, b = at / p.n, t = at - b * p.n;
+    const bool mine = 2 * W * c < p.d, live = token < all && mine;
+    const Chunk ch = chunk_of(p, mine ? c : 0);
     float co[W], si[W];
-    angles(p, ch, at, co, si);
+    angles(p, ch, live ? token : 0, co, si);
+    const Pieces<LPR, LINES> at(p, ch, token, all);
     const int h0 = blockIdx.y * p.heads, h1 = min(h0 + p.heads, p.H + p.Hkv);
-    auto part = [&](const T* x, long long step, T* out, const float* wts, int from, int to) {   // x, out: of head 0
-        typedef typename Some<T>::Raw Raw;
+    auto part = [&](const T* x, const sparsek_rope_strides& step, T* out, int heads, const float* wts, int from, int to) {
+        const T* xs[2];
+        T* os[2];
+#pragma unroll
+        for (int y = 0; y < 2; y++) {
+            xs[y] = x + at.at[y].b * step.batch + at.at[y].t * step.token + at.at[y].ch;
+            os[y] = out + ((size_t)at.at[y].b * heads * p.n + at.at[y].t) * p.d + at.at[y].ch;
+        }
         Weights w;
         w.load(wts, ch, live);
         for (int hr = from; hr < to; hr += ROWS) {
             Raw ra[ROWS], rb[ROWS];
 #pragma unroll
             for (int u = 0; u < ROWS; u++) {   // (on their way together)
-                const T* row = x + min(hr + u, to - 1) * step;
-                ra[u] = load<STREAM, Raw>(row + ch.a);
-                rb[u] = load<STREAM, Raw>(row + ch.b);
+                const long long h = min(hr + u, to - 1) * step.head;
+                ra[u] = load<STREAM, Raw>(xs[0] + h);
+                rb[u] = load<STREAM, Raw>(xs[1] + h);
             }
+            at.take(lds, ra, rb);
 #pragma unroll
             for (int u = 0; u < ROWS; u++) {
                 float xa[W], xb[W];
@@ -201,39 +289,57 @@ __global__ __launch_bounds__(256) void rope_fwd_kernel(RopeArgs p)
                     }
                 }
                 turn(p.interleaved, false, ch, co, si, xa, xb);
-                if (live && hr + u < to) {
-                    T* o = out + (size_t)(hr + u) * p.n * p.d;
-                    store<STREAM, Raw>(o + ch.a, Some<T>::narrow(xa));
-                    store<STREAM, Raw>(o + ch.b, Some<T>::narrow(xb));
-                }
+                ra[u] = Some<T>::narrow(xa);
+                rb[u] = Some<T>::narrow(xb);
+            }
+            at.give(lds, mine, ra, rb);
+#pragma unroll
+            for (int u = 0; u < ROWS; u++) {
+                const size_t o = (size_t)(hr + u) * p.n * p.d;
+                if (at.at[0].live && hr + u < to) store<STREAM, Raw>(os[0] + o, ra[u]);
+                if (at.at[1].live && hr + u < to) store<STREAM, Raw>(os[1] + o, rb[u]);
             }
         }
     };
-    if (h0 < p.H) part((const T*)p.q + b * p.qs.batch + t * p.qs.token, p.qs.head, (T*)p.qo + ((size_t)b * p.H * p.n + t) * p.d, p.qw, h0, min(h1, p.H));
-    if (h1 > p.H) part((const T*)p.k + b * p.ks.batch + t * p.ks.token, p.ks.head, (T*)p.ko + ((size_t)b * p.Hkv * p.n + t) * p.d, p.kw, max(h0 - p.H, 0), h1 - p.H);
+    if (h0 < p.H) part((const T*)p.q, p.qs, (T*)p.qo, p.H, p.qw, h0, min(h1, p.H));
+    if (h1 > p.H) part((const T*)p.k, p.ks, (T*)p.ko, p.Hkv, p.kw, max(h0 - p.H, 0), h1 - p.H);
 }
 
 // A workgroup takes `tiles` groups of tokens one after another and all of its heads, and leaves its part of the sums for the weights.
-template <class T, int LPR, bool STREAM>
+template <class T, int LPR, bool STREAM, bool LINES>
 __global__ __launch_bounds__(256, 3) void rope_bwd_kernel(RopeArgs p)
 {
+    typedef typename Some<T>::Raw Raw;
     constexpr int TOK = 256 / LPR, ROWS = rows_at_once<T, STREAM>();
     __shared__ float sums[TOK][2 * W * LPR + 1];
+    __shared__ Raw pieces[LINES ? 4 * ROWS : 1][128];
+    Raw(*lds)[128] = &pieces[LINES ? threadIdx.x / 64 * ROWS : 0];
     const int c = threadIdx.x % LPR, row = threadIdx.x / LPR;
     const unsigned all = (unsigned)p.B * p.n;
     const int h0 = blockIdx.y * p.heads, h1 = min(h0 + p.heads, p.H + p.Hkv);
-    const Chunk ch = chunk_of(p, 2 * W * c < p.d ? c : 0);
+    const bool mine = 2 * W * c < p.d;
+    const Chunk ch = chunk_of(p, mine ? c : 0);
     float wsum[2][2 * W];
 #pragma unroll
     for (int e = 0; e < 2 * W; e++) wsum[0][e] = wsum[1][e] = 0.0f;
     for (int tile = 0; tile < p.tiles; tile++) {
         const unsigned token = (blockIdx.x * p.tiles + tile) * TOK + row;   // (at most 2^26 and a workgroup's share)
-        const bool live = token < all && 2 * W * c < p.d;
-        const unsigned at = live ? token : 0, b = at / p.n, t = at - b * p.n;
+        const bool live = token < all && mine;
         float co[W], si[W];
-        angles(p, ch, at, co, si);
-        auto part = [&](const T* x, long long step, const T* dout, T* dx, long long dstep, const float* wts, float (&ws)[2 * W], int from, int to) {
-            typedef typename Some<T>::Raw Raw;
+        angles(p, ch, live ? token : 0, co, si);
+        const Pieces<LPR, LINES> at(p, ch, token, all);
+        auto part = [&](const T* x, const sparsek_rope_strides& step, const T* dout, T* dx, const sparsek_rope_strides& dstep, int heads, const float* wts,
+                        float (&ws)[2 * W], int from, int to) {
+            const T *xs[2], *gs[2];
+            T* os[2];
+#pragma unroll
+            for (int y = 0; y < 2; y++) {
+                const Piece& l = at.at[y];
+                xs[y] = x + l.b * step.batch + l.t * step.token + l.ch;
+                gs[y] = dout + ((size_t)l.b * heads * p.n + l.t) * p.d + l.ch;
+                os[y] = dx + l.b * dstep.batch + l.t * dstep.token + l.ch;
+            }
+            const long long between = os[1] - os[0];
             Weights w;
             w.load(wts, ch, live);
             for (int hr = from; hr < to; hr += ROWS) {
@@ -241,14 +347,21 @@ __global__ __launch_bounds__(256, 3) void rope_bwd_kernel(RopeArgs p)
 #pragma unroll
                 for (int u = 0; u < ROWS; u++) {   // (on their way together)
                     const int h = min(hr + u, to - 1);
-                    const T *g = dout + (size_t)h * p.n * p.d, *row = x + h * step;
-                    rga[u] = load<STREAM, Raw>(g + ch.a);
-                    rgb[u] = load<STREAM, Raw>(g + ch.b);
+                    const size_t g = (size_t)h * p.n * p.d;
+                    rga[u] = load<STREAM, Raw>(gs[0] + g);
+                    rgb[u] = load<STREAM, Raw>(gs[1] + g);
                     if (p.norm) {
-                        rxa[u] = load<STREAM, Raw>(row + ch.a);
-                        rxb[u] = load<STREAM, Raw>(row + ch.b);
+                        rxa[u] = load<STREAM, Raw>(xs[0] + h * step.head);
+                        rxb[u] = load<STREAM, Raw>(xs[1] + h * step.head);
                     }
                 }
+                auto put = [&](int u) {
+                    T* o = os[0] + (hr + u) * dstep.head;
+                    if (at.at[0].live && hr + u < to) store<STREAM, Raw>(o, rga[u]);
+                    if (at.at[1].live && hr + u < to) store<STREAM, Raw>(o + between, rgb[u]);
+                };
+                at.take(lds, rga, rgb);
+                if (p.norm) at.take(lds, rxa, rxb);
 #pragma unroll
                 for (int u = 0; u < ROWS; u++) {
                     const bool real = live && hr + u < to;
@@ -275,20 +388,21 @@ __global__ __launch_bounds__(256, 3) void rope_bwd_kernel(RopeArgs p)
                             gb[e] = r * (w.b[e] * gb[e] - xb[e] * f);
                         }
                     }
-                    if (real) {
-                        T* o = dx + (hr + u) * dstep;
-                        store<STREAM, Raw>(o + ch.a, Some<T>::narrow(ga));
-                        store<STREAM, Raw>(o + ch.b, Some<T>::narrow(gb));
-                    }
+                    rga[u] = Some<T>::narrow(ga);
+                    rgb[u] = Some<T>::narrow(gb);
+                    if (!LINES) put(u);
+                }
+                if (LINES) {
+                    at.give(lds, mine, rga, rgb);
+#pragma unroll
+                    for (int u = 0; u < ROWS; u++) put(u);
                 }
             }
         };
         if (h0 < p.H)
-            part((const T*)p.q + b * p.qs.batch + t * p.qs.token, p.qs.head, (const T*)p.dqo + ((size_t)b * p.H * p.n + t) * p.d,
-             (T*)p.dq + b * p.dqs.batch + t * p.dqs.token, p.dqs.head, p.qw, wsum[0], h0, min(h1, p.H));
+            part((const T*)p.q, p.qs, (const T*)p.dqo, (T*)p.dq, p.dqs, p.H, p.qw, wsum[0], h0, min(h1, p.H));
         if (h1 > p.H)
-            part((const T*)p.k + b * p.ks.batch + t * p.ks.token, p.ks.head, (const T*)p.dko + ((size_t)b * p.Hkv * p.n + t) * p.d,
-                 (T*)p.dk + b * p.dks.batch + t * p.dks.token, p.dks.head, p.kw, wsum[1], max(h0 - p.H, 0), h1 - p.H);
+            part((const T*)p.k, p.ks, (const T*)p.dko, (T*)p.dk, p.dks, p.Hkv, p.kw, wsum[1], max(h0 - p.H, 0), h1 - p.H);
     }
     if (!p.part) return;
     float* out = p.part + ((size_t)blockIdx.y * gridDim.x + blockIdx.x) * 2 * p.d;
@@ -366,16 +480,30 @@ static RopeArgs rope_args(const sparsek_rope_cfg& c, const void* q, const void* 
     return a;
 }
 
-#define BY_LANES(T, lpr, stream, LAUNCH)                                                      \
-    if (lpr == 1) { if (stream) { LAUNCH(T, 1, true); } else { LAUNCH(T, 1, false); } }        \
-    else if (lpr == 2) { if (stream) { LAUNCH(T, 2, true); } else { LAUNCH(T, 2, false); } }   \
-    else if (lpr == 4) { if (stream) { LAUNCH(T, 4, true); } else { LAUNCH(T, 4, false); } }   \
-    else if (lpr == 8) { if (stream) { LAUNCH(T, 8, true); } else { LAUNCH(T, 8, false); } }   \
-    else if (lpr == 16) { if (stream) { LAUNCH(T, 16, true); } else { LAUNCH(T, 16, false); } } \
-    else { if (stream) { LAUNCH(T, 32, true); } else { LAUNCH(T, 32, false); } }
-#define BY_ROW(c, lpr, stream, LAUNCH)                                     \
-    if (c.dtype == SPARSEK_F32) { BY_LANES(float, lpr, stream, LAUNCH) }   \
-    else { BY_LANES(uint16_t, lpr, stream, LAUNCH) }
+// Whether what a row's lanes load and store at once ends inside a line of 128 bytes, in a call that is streamed: then LINES (without, every line
+// goes twice: 22592 tokens, 64 heads of 64, forward 79 us, 96 otherwise, with the backward 213 and 236; 32 heads of 128 of which 64 turn 77 and 95, 203 and
+// 229; 36 heads of 112 of which 96 turn 83 and 116, 222 and 290; whole lines anyway, 32 heads of 128: 77.5 and 76.5, 203 and 200).  Through the caches
+// LDS costs more than it brings: two prompts of 5003, 18.4 us and 17.2.
+static bool part_lines(const sparsek_rope_cfg& c)
+{
+    const int size = c.dtype == SPARSEK_BF16 ? 2 : 4;
+    return c.interleaved ? c.d / 2 * size % 128 : c.rot / 2 * size % 128 || (c.d - c.rot) / 2 * size % 128;
+}
+
+#define BY_CACHES(T, lpr, c, stream, LAUNCH)           \
+    if (!stream) { LAUNCH(T, lpr, false, false); }      \
+    else if (part_lines(c)) { LAUNCH(T, lpr, true, true); } \
+    else { LAUNCH(T, lpr, true, false); }
+#define BY_LANES(T, lpr, c, stream, LAUNCH)                    \
+    if (lpr == 1) { BY_CACHES(T, 1, c, stream, LAUNCH) }        \
+    else if (lpr == 2) { BY_CACHES(T, 2, c, stream, LAUNCH) }   \
+    else if (lpr == 4) { BY_CACHES(T, 4, c, stream, LAUNCH) }   \
+    else if (lpr == 8) { BY_CACHES(T, 8, c, stream, LAUNCH) }   \
+    else if (lpr == 16) { BY_CACHES(T, 16, c, stream, LAUNCH) } \
+    else { BY_CACHES(T, 32, c, stream, LAUNCH) }
+#define BY_ROW(c, lpr, stream, LAUNCH)                                        \
+    if (c.dtype == SPARSEK_F32) { BY_LANES(float, lpr, c, stream, LAUNCH) }   \
+    else { BY_LANES(uint16_t, lpr, c, stream, LAUNCH) }
 
 // Workgroups that share a token's heads: as many as leave 1024 in all (training on 4 x 500 tokens, 16 + 16 heads of 128: 30.4 us, with 512 28.4, with
 // 2048 39.1; on 4 x 2000: 79, 91 and 87; each share makes the angles anew).
@@ -391,7 +519,7 @@ int launch_rope_fwd(const sparsek_rope_cfg& c, const void* q, const void* k, con
     a.heads = (heads + shares - 1) / shares;
     const dim3 grid((unsigned)s.groups, (heads + a.heads - 1) / a.heads);
     const bool stream = rope_streams(c, 2);
-#define FWD(T, L, S) hipLaunchKernelGGL((rope_fwd_kernel<T, L, S>), grid, dim3(256), 0, st, a)
+#define FWD(T, L, S, N) hipLaunchKernelGGL((rope_fwd_kernel<T, L, S, N>), grid, dim3(256), 0, st, a)
     BY_ROW(c, s.lpr, stream, FWD)
 #undef FWD
     return launch_status();
@@ -430,7 +558,7 @@ int launch_rope_bwd(const sparsek_rope_cfg& c, const void* q, const void* k, con
     a.tiles = y.tiles;
     a.part = dqw || dkw ? (float*)ws : nullptr;
     const bool stream = rope_streams(c, c.norm ? 3 : 2);
-#define BWD(T, L, S) hipLaunchKernelGGL((rope_bwd_kernel<T, L, S>), dim3(y.gx, y.gy), dim3(256), 0, st, a)
+#define BWD(T, L, S, N) hipLaunchKernelGGL((rope_bwd_kernel<T, L, S, N>), dim3(y.gx, y.gy), dim3(256), 0, st, a)
     BY_ROW(c, y.s.lpr, stream, BWD)
 #undef BWD
     if (a.part) hipLaunchKernelGGL(rope_weights_kernel, dim3(2 * c.d / COLS), dim3(1024), 0, st, a.part, (int)(y.gx * y.gy), c.d, dqw, dkw);

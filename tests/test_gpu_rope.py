@@ -261,3 +261,41 @@ def test_calls_that_are_streamed(dtype, n, interleaved):
             _, p, _, m = ref.bwd(y[:, a:a + 15000], pos[:, :, a:a + 15000], freq, axis, interleaved, True, w[0], 1e-6, do[:, :, a:a + 15000])
             want, size = want + p, size + m
         held(dw, want, 3 * size)   # (a lane adds up three groups of tokens here, and one in a stretch)
+
+
+@pytest.mark.parametrize("dtype,d,rot,interleaved", [
+    (BF16, 8, 8, False), (BF16, 24, 8, False), (BF16, 32, 32, True), (BF16, 64, 64, False), (BF16, 64, 32, False), (BF16, 80, 64, True), (BF16, 128, 64, False),
+    (BF16, 128, 32, False), (BF16, 128, 128, False), (BF16, 256, 96, False), (F32, 16, 16, False), (F32, 64, 64, False), (F32, 128, 32, False), (F32, 200, 104, True)])
+def test_streamed_rows_of_all_kinds(dtype, d, rot, interleaved):
+    """Rows that are whole lines and that are not, three sequences that end inside a wave's tokens, gradients into one fused one: what the tokens have
+    in calls that the caches hold, and the definition's."""
+    require_gpu()
+    say("rope streamed rows", dtype, d, rot, interleaved)
+    g = gen(95)
+    B, H, Hkv = 3, 5, 2
+    n = 220_000_000 // (2 * B * (H + Hkv) * d * (2 if dtype is BF16 else 4)) | 1
+    x = torch.randn(B, 1000, (H + 2 * Hkv) * d, generator=g).to(dtype).cuda()
+    x = x[:, torch.arange(n, device="cuda") % 1000]
+    q, k = x[..., :H * d].unflatten(-1, (H, d)), x[..., H * d:(H + Hkv) * d].unflatten(-1, (Hkv, d))
+    pos, freq, axis = ladder(g, B, n, rot, 2, far=100000)
+    w = (1 + 0.2 * torch.randn(2, d, generator=g)).cuda()
+    args = dict(axis=axis, interleaved=interleaved, norm=True, qw=w[0], kw=w[1])
+    qo, ko = spk.sparsek_rope_fwd(q, k, pos, freq, **args)
+    dqo, dko = qo.flip(2).contiguous(), ko.flip(2).contiguous()
+    dx = torch.full_like(x, 7)
+    dq, dk = dx[..., :H * d].unflatten(-1, (H, d)), dx[..., H * d:(H + Hkv) * d].unflatten(-1, (Hkv, d))
+    spk.sparsek_rope_bwd(q, k, pos, freq, dqo, dko, out=(dq, dk), **args)
+    torch.cuda.synchronize()
+    assert (dx[..., (H + Hkv) * d:] == 7).all()
+    for b, rows in ((0, slice(0, 300)), (0, slice(n - 77, n)), (1, slice(0, 77)), (1, slice(n // 2, n // 2 + 100)), (2, slice(n - 300, n))):
+        one = slice(b, b + 1)
+        y, z, at = q[one, rows], k[one, rows], pos[:, one, rows].contiguous()
+        got = spk.sparsek_rope_fwd(y, z, at, freq, **args)
+        back = spk.sparsek_rope_bwd(y, z, at, freq, dqo[one, :, rows].contiguous(), dko[one, :, rows].contiguous(), **args)
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], qo[one, :, rows]) and torch.equal(got[1], ko[one, :, rows])
+        assert torch.equal(back[0], dq[one, rows]) and torch.equal(back[1], dk[one, rows])
+        for t, wt, o, do, dt in ((y, w[0], qo, dqo, dq), (z, w[1], ko, dko, dk)):
+            held(o[one, :, rows], *ref.fwd(t, at, freq, axis, interleaved, True, wt, 1e-6))
+            rx, _, bx, _ = ref.bwd(t, at, freq, axis, interleaved, True, wt, 1e-6, do[one, :, rows])
+            held(dt[one, rows], rx, bx)
