@@ -463,12 +463,13 @@ static RopeShape rope_shape(const sparsek_rope_cfg& c)
     s.groups = ((long long)c.B * c.n + s.tok - 1) / s.tok;
     return s;
 }
-// Whether a call that reads or writes every value `passes` times goes past the last cache, of 256 MB (streamed and not: a document of 32768, 671 MB,
-// 136 and 149 us; of 12000, 246 MB, 51.6 and 58.4; of 8192, 168 MB, 37.7 and 38.5; two prompts of 5003, 92 MB, 28 and 17; forward of 16 x 2000 tokens
-// in fp32, 393 MB, 75 and 81; of 4 x 2000, 98 MB, 20.6 and 19.3).
+// Whether a call that reads or writes every value `passes` times goes past the last cache, of 256 MB.  Forward, streamed and not: a document of
+// 32768, 671 MB, 135 and 149 us; of 9500, 195 MB, 43 and 52; of 8192, 168 MB, 35 and 39; 16 x 2000 tokens in fp32, 393 MB, 75 and 81; 8000 tokens of
+// 32 heads of 128, 131 MB, with their backward, which finds less in the cache then, 80 and 77; 5003 of 64 heads of 64, 82 MB, 21.5 and 16.6.
+// Backward, behind a forward that was not: 4 x 2000 in fp32, 147 MB, 50 and 55; 5500 tokens of 32 heads, 135 MB, 55 and 59; 5000, 123 MB, 54 and 51.
 static bool rope_streams(const sparsek_rope_cfg& c, int passes)
 {
-    return (double)passes * c.B * c.n * (c.H + c.Hkv) * c.d * (c.dtype == SPARSEK_BF16 ? 2 : 4) > 200e6;
+    return (double)passes * c.B * c.n * (c.H + c.Hkv) * c.d * (c.dtype == SPARSEK_BF16 ? 2 : 4) > (passes == 3 ? 130e6 : 150e6);
 }
 static RopeArgs rope_args(const sparsek_rope_cfg& c, const void* q, const void* k, const int32_t* pos, const float* freq, const int32_t* axis,
                           const float* qw, const float* kw)
