@@ -1225,9 +1225,12 @@ static Cache8Layout cache8_layout(const sparsek_cache8_cfg& c, int top)
     // In 4 bits a unit is half as long and the second launch weighs more: one workgroup for up to 28, or 40 where there is one for every compute unit
     // (sequences of up to 2400, 38 units: 64 of them 31.6 us in one and 39.1 in two, 32 of them 22.7 and 25.3, 8 of them 20.8 and 19.4; of up to 1400, 22
     // units: 23.2 and 37.6 for 64, 15.4 and 19.5 for 4).
-    const int most = 5, alone = c.format != SPARSEK_E2M1 ? most : rows >= 256 ? MAX_UPW : 7;
+    // In 4 bits, whose waves are 12 to a compute unit, what 2048 waves leave over is rounded up where it is more than a 32nd: 544 workgroups of two units
+    // to a wave take as long as 768 (attention and join of one sequence with 8 heads: of 34000 19.7 us, with three units 17.4; of 28000 19.9 with one unit,
+    // 16.5 with two), but 520 do not (of 32768: 17.1 with two, 17.4 with three; of 65536 22.1 with four, 22.9 with five).
+    const int most = 5, alone = c.format != SPARSEK_E2M1 ? most : rows >= 256 ? MAX_UPW : 7, over = c.format != SPARSEK_E2M1 ? 0 : 2048 - 2048 / 32;
     if (y.units <= 4 * alone && y.groups == 1) y.upw = (y.units + 3) / 4;
-    else y.upw = (int)std::max<long long>(1, std::min<long long>(most, all / 2048));
+    else y.upw = (int)std::max<long long>(1, std::min<long long>(most, (all + over) / 2048));
     y.splits = (y.units + 4 * y.upw - 1) / (4 * y.upw);
     const size_t parts = (size_t)c.B * c.H * y.splits;
     y.part_o = 0;
