@@ -422,7 +422,8 @@ int sparsek_cache4_evict(const sparsek_cache8_cfg *cfg, const sparsek_cache4 *ca
  * [rot/2] int32, which position turns the pair (values outside 0 .. axes-1 count as the nearest), NULL: 0.  pos, freq may be NULL where rot == 0.
  * Angles are made in 64 bits, sums in fp32; the outputs are rounded once.  Squares that pass fp32's range overflow (values beyond 2^60).
  * bwd: for L = sum(dqo * qo) + sum(dko * ko), dqo, dko contiguous as qo, ko: dq, dk in the strides cfg->dq, cfg->dk (slices of one gradient, say; no
- * place may coincide with another: INVALID_ARG within a tensor), and dqw, dkw [d] fp32, NULL: not wanted (norm == 0: they must be NULL).  q and k are not read where norm == 0 and may be NULL.
+ * place may coincide with another, of the same tensor or of the other: INVALID_ARG, also for strides of dq and dk so far from each other's that 2^18
+ * comparisons do not tell), and dqw, dkw [d] fp32, NULL: not wanted (norm == 0: they must be NULL).  q and k are not read where norm == 0 and may be NULL.
  * The sums behind dqw and dkw have an order of their own that does not depend on timing.
  * SPARSEK_BF16 or SPARSEK_F32; d a multiple of 8, 8 .. 256; rot a multiple of 8, 0 .. d; axes 1 .. 4; H + Hkv <= 65535, B n <= 2^26 (UNSUPPORTED
  * otherwise).  Strides are in elements, not negative, multiples of 4, and the last row begins below 2^46; q, k, qo, ko, their gradients and ws begin at

@@ -752,6 +752,42 @@ bool apart(const sparsek_rope_cfg& c, const sparsek_rope_strides& s, int heads)
     return true;
 }
 
+// Places of a strided output: rows of `row` bytes, and the steps between them, the largest first.
+struct Rows {
+    int64_t row, step[3], count[3], reach[4];   // reach[i]: what the steps from i on span
+    int n = 0;
+    Rows(const sparsek_rope_cfg& c, const sparsek_rope_strides& s, int heads)
+    {
+        const int64_t size = c.dtype == SPARSEK_BF16 ? 2 : 4;
+        std::pair<int64_t, int64_t> dims[3] = {{s.batch, c.B}, {s.token, c.n}, {s.head, heads}};
+        std::sort(dims, dims + 3);
+        for (int x = 2; x >= 0; x--)
+            if (dims[x].second > 1) {
+                step[n] = dims[x].first * size;
+                count[n++] = dims[x].second;
+            }
+        reach[n] = row = c.d * size;
+        for (int x = n - 1; x >= 0; x--) reach[x] = reach[x + 1] + (count[x] - 1) * step[x];
+    }
+};
+
+// Whether a row of b, which begins `off` bytes behind a, lies over one of a; both are apart() in themselves, from steps i and j on.  Equal steps leave three
+// pairs of neighbours at most to look at; others are gone through one by one, and what is not through after `left` pairs counts as meeting (a
+// fused gradient has the same steps for both but for the heads, of which there are 65535).
+bool meet(const Rows& a, int i, const Rows& b, int j, int64_t off, int& left)
+{
+    if (off >= a.reach[i] || -off >= b.reach[j]) return false;
+    if ((i == a.n && j == b.n) || --left < 0) return true;
+    const int64_t sa = i < a.n ? a.step[i] : 0, sb = j < b.n ? b.step[j] : 0;
+    const bool in_a = sa >= sb, in_b = sb >= sa;
+    const int64_t step = std::max(sa, sb), ra = a.reach[i + in_a], rb = b.reach[j + in_b];
+    // parts x of a and y of b that are off + (y - x) step apart, more than -rb and less than ra
+    const int64_t x1 = in_a ? a.count[i] - 1 : 0, y1 = in_b ? b.count[j] - 1 : 0;
+    for (int64_t m = std::max(-x1, -((off + rb - 1) / step)); m <= y1 && off + m * step < ra; m++)
+        if (meet(a, i + in_a, b, j + in_b, off + m * step, left)) return true;
+    return false;
+}
+
 int check_rope(const sparsek_rope_cfg* c)
 {
     if (!c || c->B < 1 || c->H < 1 || c->Hkv < 0 || c->n < 1 || c->d < 1 || c->rot < 0 || c->rot > c->d || c->axes < 1) return SPARSEK_ERR_INVALID_ARG;
@@ -826,13 +862,15 @@ int sparsek_rope_bwd(const sparsek_rope_cfg* cfg, const void* q, const void* k, 
     if ((rc = check_rope_inputs(c, c.norm, q, k, pos, freq))) return rc;
     if (!dqo || !dq || (c.Hkv && (!dko || !dk)) || !aligned({dqo, dko, dq, dk, ws})) return SPARSEK_ERR_INVALID_ARG;
     if ((dqw && !c.norm) || (dkw && (!c.norm || !c.Hkv)) || ((dqw || dkw) && !ws)) return SPARSEK_ERR_INVALID_ARG;
-    if (dq == dk || !good(c, c.dq, c.H) || !apart(c, c.dq, c.H) || (c.Hkv && (!good(c, c.dk, c.Hkv) || !apart(c, c.dk, c.Hkv)))) return SPARSEK_ERR_INVALID_ARG;
+    if (!good(c, c.dq, c.H) || !apart(c, c.dq, c.H) || (c.Hkv && (!good(c, c.dk, c.Hkv) || !apart(c, c.dk, c.Hkv)))) return SPARSEK_ERR_INVALID_ARG;
+    int pairs = 1 << 18;
+    if (c.Hkv && meet(Rows(c, c.dq, c.H), 0, Rows(c, c.dk, c.Hkv), 0, (const char*)dk - (const char*)dq, pairs)) return SPARSEK_ERR_INVALID_ARG;
     const size_t row = (size_t)c.B * c.n * c.d * (c.dtype == SPARSEK_BF16 ? 2 : 4), nw = (size_t)c.d * 4, need = spk::rope_bwd_ws_bytes(c);
     const bool sums = dqw || dkw;
     const Place in[] = {{q, c.norm ? span(c, c.q, c.H) : 0}, {k, c.norm && c.Hkv ? span(c, c.k, c.Hkv) : 0}, {dqo, row * c.H}, {dko, row * c.Hkv},
                         {pos, positions(c)}, {freq, c.rot * 2u}, {axis, c.rot * 2u}, {qw, c.norm ? nw : 0}, {kw, c.norm ? nw : 0}};
     const Place dx[] = {{dq, span(c, c.dq, c.H)}, {dk, c.Hkv ? span(c, c.dk, c.Hkv) : 0}}, other[] = {{dqw, nw}, {dkw, nw}, {ws, sums ? need : 0}};
-    for (const Place& x : dx) {   // (which may be slices of one gradient)
+    for (const Place& x : dx) {   // (which may be slices of one gradient, row beside row)
         const Place one[] = {x};
         if (any_overlap(in, one) || any_overlap(one, other)) return SPARSEK_ERR_INVALID_ARG;
     }

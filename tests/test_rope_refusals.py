@@ -151,3 +151,103 @@ def test_every_entry_point_of_the_header_is_there():
     assert len(names) == 3
     for name in names:
         assert getattr(spk.lib(), name), name
+
+
+def gradients(c, dk):
+    """What a backward call says whose dk lies `dk` bytes behind dq; nothing is launched (the workspace is too small, which is looked at last)."""
+    L = spk.lib()
+    args = [far(z + 1) for z in range(14)]
+    args[10] = ctypes.c_void_p(args[9].value + dk)
+    return L.sparsek_rope_bwd(c, *args, L.sparsek_rope_bwd_workspace_bytes(c) - 1, NULL)
+
+
+def beside(token, head_q, head_k, batch=None, **kw):
+    return cfg(dq=strides(10 * token if batch is None else batch, token, head_q), dk=strides(10 * token if batch is None else batch, token, head_k), **kw)
+
+
+@pytest.mark.parametrize("dtype,size", [(spk.BF16, 2), (spk.F32, 4)])
+def test_gradients_of_queries_and_keys_in_one_tensor(dtype, size):
+    """(2 sequences of 10 tokens, 4 + 2 heads of 64.)  Row beside row is allowed, rows over rows are not."""
+    kw = dict(dtype=dtype)
+    # slices of a fused gradient: 4 heads, 2 heads, 2 heads that belong to neither
+    fused = beside(512, 64, 64, **kw)
+    for at in (256, 320, 384):
+        assert gradients(fused, at * size) == -3, at
+    for at in (8, 56, 64, 192, 248, 392, 448, 504, 512, 512 + 64, 512 * 9 + 448, 512 * 9 + 504, 512 * 10 + 64, 512 * 19 + 192):
+        assert gradients(fused, at * size) == -1, at
+    for at in (512 + 256, 512 * 9 + 256, 512 * 10 + 384):     # (a row further on: the last rows lie behind the others)
+        assert gradients(fused, at * size) == -3, at
+    for at in (-128, -512 + 256, -512 * 10 + 384, -512 * 19 - 256, -512 * 19 + 256):
+        assert gradients(fused, at * size) == -3, at
+    for at in (-64, -120, -512 + 64, -512 * 10, -512 * 19 + 192):
+        assert gradients(fused, at * size) == -1, at
+    # a head's query, key and value beside each other
+    three = beside(4 * 192, 192, 192, **kw)
+    for at in (64, 72, 128, 192 + 64, 3 * 192 + 128):
+        assert gradients(three, at * size) == -3, at
+    for at in (8, 56, 136, 184, 192, 384):
+        assert gradients(three, at * size) == -1, at
+    # keys and values in turns behind the queries
+    turns = beside(512, 64, 128, **kw)
+    for at in (256, 320):
+        assert gradients(turns, at * size) == -3, at
+    for at in (0 + 8, 64, 128, 192, 248, 384, 392):
+        assert gradients(turns, at * size) == -1, at
+    # keys between the queries' groups
+    groups = cfg(H=2, dq=strides(5120, 512, 256), dk=strides(5120, 512, 128), **kw)
+    for at in (64, 448):
+        assert gradients(groups, at * size) == -3, at
+    for at in (128, 192 + 8, 384):
+        assert gradients(groups, at * size) == -1, at
+    # heads first, one block a sequence; and all of a tensor's tokens one sequence behind the other
+    first = cfg(dq=strides(6 * 640, 64, 640), dk=strides(6 * 640, 64, 640), **kw)
+    assert gradients(first, 4 * 640 * size) == -3 and gradients(first, (6 + 4) * 640 * size) == -3
+    for at in (640, 3 * 640, 4 * 640 - 64, 4 * 640 - 8, 4 * 640 + 8, 5 * 640, 6 * 640):
+        assert gradients(first, at * size) == -1, at
+    # tokens first and heads first of one block a sequence
+    mixed = cfg(dq=strides(6 * 640, 256, 64), dk=strides(6 * 640, 64, 640), **kw)
+    assert gradients(mixed, 4 * 640 * size) == -3
+    for at in (640, 4 * 640 - 8, 4 * 640 + 64):
+        assert gradients(mixed, at * size) == -1, at
+    # tensors of their own, and one sequence of one token
+    assert gradients(cfg(dq=strides(2560, 256, 64), dk=strides(1280, 128, 64), **kw), 2 * 2560 * size) == -3
+    one = cfg(B=1, n=1, dq=strides(0, 0, 64), dk=strides(0, 0, 64), **kw)
+    assert gradients(one, 256 * size) == -3 and gradients(one, -128 * size) == -3
+    for at in (8, 64, 192, 248, -64, -120):
+        assert gradients(one, at * size) == -1, at
+
+
+def test_gradients_in_one_tensor_against_every_place():
+    """Small layouts, their places counted one by one: none is taken whose rows meet, and none refused whose strides are the same and whose rows do not."""
+    g = torch.Generator().manual_seed(17)
+    draw = lambda a, b: int(torch.randint(a, b + 1, (1,), generator=g))   # noqa: E731
+    seen = {-1: 0, -3: 0}
+    for case in range(3000):
+        B, n, H, Hkv, d = draw(1, 3), draw(1, 5), draw(1, 4), draw(1, 4), 8 * draw(1, 3)
+
+        def layout(heads):
+            order = torch.randperm(3, generator=g).tolist()
+            s, reach = [0, 0, 0], d
+            for x in order:
+                s[x] = reach + 4 * draw(0, 3) * draw(0, 12)
+                reach = s[x] * ((B, n, heads)[x] - 1) + reach
+            return s
+
+        sq = layout(max(H, Hkv))
+        sk = list(sq) if case % 3 else layout(Hkv)
+        if case % 3 == 2 and sk[2] < min(sk[:2]):   # (heads nearer to each other, in the same tokens)
+            sk[2] = draw(d, sk[2]) // 4 * 4
+        c = cfg(B=B, n=n, H=H, Hkv=Hkv, d=d, rot=0, dtype=spk.F32, dq=strides(*sq), dk=strides(*sk))
+        rows = lambda s, heads: [b * s[0] + t * s[1] + h * s[2] for b in range(B) for t in range(n) for h in range(heads)]   # noqa: E731
+        q, k = sorted(rows(sq, H)), sorted(rows(sk, Hkv))
+        if any(y - x < d for x, y in zip(k, k[1:])):
+            continue
+        at = 4 * draw(-(k[-1] + d) // 4, (q[-1] + d) // 4)
+        places = torch.zeros(max(q[-1], k[-1]) + abs(at) + d + 1, dtype=torch.int8)
+        for x in q:
+            places[x + max(-at, 0):x + max(-at, 0) + d] = 1
+        meet = any(bool(places[x + max(at, 0):x + max(at, 0) + d].any()) for x in k)
+        rc = gradients(c, 4 * at)
+        seen[rc] += 1
+        assert rc == (-1 if meet else -3), (B, n, H, Hkv, d, sq, sk, at)
+    assert min(seen.values()) > 300
