@@ -47,15 +47,19 @@ __device__ __forceinline__ unsigned codes_e2m1(u32x4 x, unsigned e)
     return e ? w : 0u;
 }
 
-// 8 codes as fp16, times 2^(e - 127).
-__device__ __forceinline__ f16x8 widen_e2m1(unsigned w, float scale)
+// 8 codes times their scale, which bf16 holds exactly whatever it is; scale: its float's bits, 0 for a group of zeros.
+__device__ __forceinline__ bf16x8 widen_e2m1(unsigned w, unsigned scale)
 {
-    const f16x2v a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 1);
-    const f16x2v c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 3);
-    return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+    const float f = __uint_as_float(scale);
+    const bf16x2v a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, f, 1);
+    const bf16x2v c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, f, 3);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
+// Byte x of four scales as such bits.
+__device__ __forceinline__ unsigned scale_bits(unsigned scales, int x) { return (scales >> 8 * x & 255) << 23; }
 
-// A page's largest scale, which ks and vs hold: times 1.5 where its scales are `wide`, where one that is not 0 is less than 2^-36 of it.
+// What ks and vs hold: a page's largest scale, times 1.5 where one that is not 0 is less than 2^-36 of it (a reader that widens to fp16 cannot hold both),
+// NaN where a value is not finite, which is what the attention and reading back look for.
 constexpr int WIDE = 36;
 __device__ __forceinline__ float page_scale(float top, int lowest)
 {
@@ -63,24 +67,5 @@ __device__ __forceinline__ float page_scale(float top, int lowest)
     const int e = (int)scale_of_top(__float_as_uint(top));
     return __uint_as_float((unsigned)e << 23 | (lowest < e - WIDE ? 0x400000u : 0u));
 }
-
-// In fp16 a page's values stand relative to its largest scale, which becomes 2^13 (6 times that is below fp16's largest number): all of them are
-// exact unless the page is wide, whose products are scaled in fp32 instead.
-struct Relative {
-    int low;      // what a scale's biased exponent counts as at least (that of a group of zeros: 0)
-    unsigned add; // to the exponent, in its place in a float
-    float unit;   // what 1 stands for in the products; NaN of a page with a value that is not finite
-    bool wide;
-    __device__ __forceinline__ explicit Relative(float largest)
-    {
-        const unsigned b = __float_as_uint(largest);
-        const int e = (int)(b >> 23) & 255;
-        low = max(e - 139, 0);
-        add = (unsigned)(127 + 13 - e) << 23;
-        wide = (b & 0x7FFFFFu) && e < 255;
-        unit = largest * 0x1p-13f;
-    }
-    __device__ __forceinline__ float of(unsigned scales, int byte) const { return __uint_as_float(((unsigned)max((int)(scales >> 8 * byte & 255), low) << 23) + add); }
-};
 
 }  // namespace spk

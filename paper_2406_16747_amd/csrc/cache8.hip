@@ -478,6 +478,7 @@ struct AttnArgs {
     float c2;
     float* part_o;         // [B,H,splits][D]
     float2* part_ml;       // [B,H,splits]: the largest logit (times log2 e), the sum
+    float one;             // Weight::ONE of part_o and of these sums
     float* weight;         // [B,H,units]: log2 of a unit's share before the division
     int units;             // units per row at most
     bool accumulate;
@@ -557,11 +558,18 @@ __device__ __forceinline__ void add_mass(const AttnArgs& a, const RowUnits& ru, 
     if (j >= 0 && j < a.c.cap && sum != 0.0f) a.c.t.mass[bg * a.c.cap + j] += sum;
 }
 
-// The running softmax over a unit's logits (in s, times log2 e); put(t, r, p) takes the weight of s[t][r], times 2^15.
+// Weights times 2^UP: in fp16 2^15, so that small ones keep their bits; in bf16, which has fp32's range, as they are.
+template <int UP>
+struct Weight {
+    static constexpr float ONE = UP ? 0x1p-15f : 1.0f;   // brings a sum of weights back
+    static_assert(UP == 0 || UP == 15, "2^-UP");
+};
+
+// The running softmax over a unit's logits (in s, times log2 e); put(t, r, p) takes the weight of s[t][r], times 2^UP.
 struct SoftRow {
     float m, l;
 };
-template <class Put>
+template <int UP, class Put>
 __device__ __forceinline__ float soft_unit(const f32x4m (&s)[4], SoftRow& row, float& corr, Put put)
 {
     float top = -INFINITY;
@@ -581,7 +589,7 @@ __device__ __forceinline__ float soft_unit(const f32x4m (&s)[4], SoftRow& row, f
     for (int t = 0; t < 4; t++)
 #pragma unroll
         for (int r = 0; r < 4; r++) {
-            const float p = __builtin_amdgcn_exp2f(s[t][r] - ref + 15.0f);   // (ref - 15 would be rounded where it is large, past fp16's range)
+            const float p = __builtin_amdgcn_exp2f(s[t][r] - ref + (float)UP);   // (ref - UP would be rounded where it is large, past fp16's range)
             sum += p;
             put(t, r, p);
         }
@@ -590,16 +598,16 @@ __device__ __forceinline__ float soft_unit(const f32x4m (&s)[4], SoftRow& row, f
     const auto e = __builtin_amdgcn_permlane16_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
     sum = __uint_as_float(e[0]) + __uint_as_float(e[1]);
     row.l = fmaf(row.l, corr, sum);
-    return ref + log2f(sum * 0x1p-15f);   // log2 of the unit's share
+    return ref + log2f(sum * Weight<UP>::ONE);   // log2 of the unit's share
 }
 
 // The largest logit of keys that were attended but have none above -inf: they are infinite themselves, or their query is, or their scale
 // is NaN.  No finite logit is below it, and still it is not the -inf of no keys at all: what remains of such a row alone is 0 / 0.
 constexpr float NO_LOGIT = -__FLT_MAX__;
-__device__ __forceinline__ float log_of(float top, float sum)   // a row's lse; sum: times 2^15
+__device__ __forceinline__ float log_of(float top, float sum)   // a row's lse
 {
     if (top == -INFINITY) return -INFINITY;
-    return sum == 0.0f ? __uint_as_float(0x7FC00000u) : (top + log2f(sum * 0x1p-15f)) * 0.6931471805599453f;
+    return sum == 0.0f ? __uint_as_float(0x7FC00000u) : (top + log2f(sum)) * 0.6931471805599453f;
 }
 
 // A wave's block in LDS: 64 rows of D bytes of keys, D rows of 64 bytes of values.  The pieces (16 bytes) of a row change places so that the
@@ -629,11 +637,12 @@ __global__ __launch_bounds__(256, FORMAT == FORMAT_E2M1 ? 3 : D == 128 ? 2 : 4) 
     constexpr int KH = D / 64, NX = D / 16, RO = D + 4;
     constexpr bool FOUR = FORMAT == FORMAT_E2M1;
     constexpr int T4 = BT * D + 512;   // a page's codes, and its scales in two times 256 bytes
-    static_assert(16 * RO * 4 <= T4 && 1024 * (NX < 4 ? 4 : NX) <= T4, "room for a wave's result, and for the products of a wide page");
+    constexpr int UP = FOUR ? 0 : 15;
+    constexpr float ONE = Weight<UP>::ONE;
+    static_assert(16 * RO * 4 <= (FOUR ? T4 : 2 * T::BYTES), "room for a wave's result");
     __shared__ __attribute__((aligned(16))) unsigned char tiles[4][FOUR ? T4 : 2 * T::BYTES];   // a wave's keys and values; its result at the end
     __shared__ float sm_[4][16], sl[4][16], shares[4 * MAX_UPW + 1][16];
     __shared__ unsigned seen[MAX_CAP / 32];
-    static_assert(16 * RO * 4 <= 2 * T::BYTES, "room for a wave's result");
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, grp = lane >> 4;
     const int groups = (a.c.G + 15) / 16;
     // Workgroups go to the chip's 8 partitions in turn.  The heads of a sequence, all of one length, come first, and sequences begin with parts of
@@ -679,31 +688,37 @@ __global__ __launch_bounds__(256, FORMAT == FORMAT_E2M1 ? 3 : D == 128 ? 2 : 4) 
         ks = a.c.t.ks[page];
         vs = a.c.t.vs[page];
     }
-    // Q^T: head col, columns 64 half + 16 grp + 8 sub .. (in 4 bits: a lane's are those of one scale or half of one), relative to the head's
-    // largest value
+    // Q^T: head col, columns 64 half + 16 grp + 8 sub .. (in 4 bits: a lane's are those of one scale or half of one).  In 8 bits relative to the
+    // head's largest value, in 4 as they are.
     constexpr int QG = FOUR ? D / 4 : 16, QH = FOUR ? 16 : 64;
     const uint16_t* qr = a.q + (head0 + min(col, live - 1)) * D + QG * grp;
     u32x4 qw[KH][2];
-    unsigned top = 0;
 #pragma unroll
     for (int h = 0; h < KH; h++)
 #pragma unroll
-        for (int s = 0; s < 2; s++) {
-            qw[h][s] = *(const u32x4*)(qr + QH * h + 8 * s);
-#pragma unroll
-            for (int e = 0; e < 4; e++) top = max(top, max(qw[h][s][e] << 16 & 0x7FFFFFFFu, qw[h][s][e] & 0x7FFF0000u));
-        }
-    top = max(top, (unsigned)__shfl_xor((int)top, 16, 64));
-    top = max(top, (unsigned)__shfl_xor((int)top, 32, 64));
-    const int E = scale_exp(top);
-    const float down = scale_down(E), c2q = a.c2 * scale_up(E);
+        for (int s = 0; s < 2; s++) qw[h][s] = *(const u32x4*)(qr + QH * h + 8 * s);
     f16x8 qf[KH][2];
+    float c2q = a.c2;
+    if constexpr (!FOUR) {
+        unsigned top = 0;
 #pragma unroll
-    for (int h = 0; h < KH; h++)
+        for (int h = 0; h < KH; h++)
 #pragma unroll
-        for (int s = 0; s < 2; s++)
+            for (int s = 0; s < 2; s++)
 #pragma unroll
-            for (int e = 0; e < 8; e++) qf[h][s][e] = (_Float16)(half_of(qw[h][s], e) * down);
+                for (int e = 0; e < 4; e++) top = max(top, max(qw[h][s][e] << 16 & 0x7FFFFFFFu, qw[h][s][e] & 0x7FFF0000u));
+        top = max(top, (unsigned)__shfl_xor((int)top, 16, 64));
+        top = max(top, (unsigned)__shfl_xor((int)top, 32, 64));
+        const int E = scale_exp(top);
+        const float down = scale_down(E);
+        c2q = a.c2 * scale_up(E);
+#pragma unroll
+        for (int h = 0; h < KH; h++)
+#pragma unroll
+            for (int s = 0; s < 2; s++)
+#pragma unroll
+                for (int e = 0; e < 8; e++) qf[h][s][e] = (_Float16)(half_of(qw[h][s], e) * down);
+    }
     f32x4m acc[NX];
 #pragma unroll
     for (int x = 0; x < NX; x++) acc[x] = f32x4m{0, 0, 0, 0};
@@ -712,11 +727,18 @@ __global__ __launch_bounds__(256, FORMAT == FORMAT_E2M1 ? 3 : D == 128 ? 2 : 4) 
     const bool weighs = a.accumulate && !alone;
     const buffer_t wbuf = buffer_of(weighs ? a.weight + head0 * a.units : nullptr, weighs ? live * a.units * 4 : 0);
     const int wat = grp == 0 && col < live ? col * a.units * 4 : 0x7FFFFF00;
+    // Weights as the sum of two bf16 numbers (2^-16).
+    bf16x8 ph[2], pl[2];
+    auto split_weight = [&](int t, int r, float p) {
+        const __bf16 hi = (__bf16)p;
+        ph[t >> 1][4 * (t & 1) + r] = hi;
+        pl[t >> 1][4 * (t & 1) + r] = (__bf16)(p - (float)hi);
+    };
     if (FOUR && have) {
         // As in 8 bits, but codes lie in LDS as they lie in memory: a lane reads what it loaded, 16 bytes at a time, and widens it with its group's
-        // scale (four instructions for eight codes).  What bounds it is memory: the vector units are busy 56 % of the time, the products 13 %.
-        // 64 sequences of up to 8192 take 66 us, 5.2 TB/s, with three waves to a SIMD; from memory straight to the lanes' registers, which leaves
-        // two, 75; with four, whose registers spill, 73; with two blocks ahead and two waves 71.
+        // scale (four instructions for eight codes) to bf16, which holds every value as it is: how large others of the page are does not matter, and
+        // what a weight of 2^-100 brings of a value of 2^120 is counted.  (Weights below 2^-126 are 0.)  What bounds it is memory: 64 sequences of up to
+        // 8192 take 68 to 73 us, 5.1 TB/s, with 126 registers; the second products in accumulators of their own 70 to 75, with 145.
         using P = Page4<D>;
         constexpr int LOADS = P::CODES / 1024 + 1;
         unsigned char *kt = tiles[wv], *vt = kt + P::CODES, *kx = vt + P::CODES, *vx = kx + 256;
@@ -740,120 +762,60 @@ __global__ __launch_bounds__(256, FORMAT == FORMAT_E2M1 ? 3 : D == 128 ? 2 : 4) 
         load_v(0);
         for (int i = 0; i < count; i++) {
             const float kl = readlane_f32(ks, i), vl = readlane_f32(vs, i);
-            const Relative krel(kl), vrel(vl);
+            const float f = kl == kl ? a.c2 : kl;   // (NaN: the page has a value that is not finite)
             const bool there = have >> i & 1;
             f32x4m s[4];
-            f16x8 pb[2];
-            float corr, share;
-            auto weigh = [&] { return soft_unit(s, row, corr, [&](int t, int r, float p) { pb[t >> 1][4 * (t & 1) + r] = (_Float16)p; }); };
-            if (!krel.wide && !vrel.wide) {
-                const float f = krel.unit * c2q;
-                // the keys are there when no more than the values' loads are under way (memory operations end in order)
-                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
-                const unsigned ke = *(const unsigned*)(kx + 4 * (D == 128 ? lane : 16 * (grp / 2) + col));
+            // the keys are there when no more than the values' loads are under way (memory operations end in order)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
+            const unsigned ke = *(const unsigned*)(kx + 4 * (D == 128 ? lane : 16 * (grp / 2) + col));
 #pragma unroll
-                for (int z = 0; z < D / 32; z++) {
-                    const u32x4 w = *(const u32x4*)(kt + 1024 * z + 16 * lane);
+            for (int z = 0; z < D / 32; z++) {
+                const u32x4 w = *(const u32x4*)(kt + 1024 * z + 16 * lane);
 #pragma unroll
-                    for (int u = 0; u < 128 / D; u++) {
-                        const int t = 128 / D * z + u;
-                        s[t] = f32x4m{0, 0, 0, 0};
-                        const float scale = krel.of(ke, t);
+                for (int u = 0; u < 128 / D; u++) {
+                    const int t = 128 / D * z + u;
+                    s[t] = f32x4m{0, 0, 0, 0};
 #pragma unroll
-                        for (int x = 0; x < D / 32; x++)
-                            s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen_e2m1(w[2 * u + x], scale), qf[x / 2][x % 2], s[t], 0, 0, 0);
+                    for (int x = 0; x < D / 32; x++)
+                        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen_e2m1(w[2 * u + x], scale_bits(ke, t)), __builtin_bit_cast(bf16x8, qw[x / 2][x % 2]),
+                                                                       s[t], 0, 0, 0);
 #pragma unroll
-                        for (int r = 0; r < 4; r++) s[t][r] = there ? s[t][r] * f : -INFINITY;
-                    }
-                }
-                // the next keys; the values are there when no more than those are under way
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                if (i + 1 < count) {
-                    load_k(i + 1);
-                    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
-                } else {
-                    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-                }
-                share = weigh();
-                unsigned ve[D / 64];
-#pragma unroll
-                for (int z = 0; z < D / 64; z++) ve[z] = *(const unsigned*)(vx + (16 * (grp / 2) + col) * (D / 16) + 4 * z);
-#pragma unroll
-                for (int z = 0; z < NX / 2; z++) {
-                    const u32x4 w = *(const u32x4*)(vt + 1024 * z + 16 * lane);
-#pragma unroll
-                    for (int u = 0; u < 2; u++) {
-                        const int x = 2 * z + u;
-                        const float scale = vrel.of(ve[x / 4], x % 4);
-                        f32x4m y = {0, 0, 0, 0};
-                        y = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen_e2m1(w[2 * u], scale), pb[0], y, 0, 0, 0);
-                        y = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen_e2m1(w[2 * u + 1], scale), pb[1], y, 0, 0, 0);
-#pragma unroll
-                        for (int r = 0; r < 4; r++) acc[x][r] = fmaf(acc[x][r], corr, vrel.unit * y[r]);
-                    }
-                }
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                if (i + 1 < count) load_v(i + 1);
-            } else {
-                // The products of 32 channels, or tokens, at a time are scaled in fp32.  Rare: small loops that read the page from memory, around a
-                // lane's own places in LDS, which cost the others no registers.
-                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (what is on its way there has arrived)
-                const size_t pg = (size_t)__builtin_amdgcn_readlane(page, i);
-                const unsigned char *kp = (const unsigned char*)a.c.t.k8 + pg * P::CODES + 16 * lane, *vp = (const unsigned char*)a.c.t.v8 + pg * P::CODES + 16 * lane;
-                const unsigned char *kscale = a.c.ke + pg * P::SCALES + 16 * grp, *vscale = a.c.ve + pg * P::SCALES + 4 * grp * (D / 16);
-                const float kn = kl == kl ? c2q : kl, vn = vl == vl ? 1.0f : vl;   // (one of the two may have a value that is not finite)
-                f32x4m* mine = (f32x4m*)tiles[wv] + lane;
-#pragma unroll 1
-                for (int t = 0; t < 4; t++) {
-                    f32x4m sum = {0, 0, 0, 0};
-#pragma unroll 1
-                    for (int j = 0; j < D / 32; j++) {
-                        f32x4m y = {0, 0, 0, 0};
-#pragma unroll
-                        for (int x = 0; x < D / 32; x++) {
-                            const unsigned w = *(const unsigned*)(kp + (D == 128 ? 1024 * t : 1024 * (t / 2) + 8 * (t % 2)) + 4 * x);
-                            y = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen_e2m1((D == 128 ? grp : grp / 2) == j ? w : 0u, 1.0f), qf[x / 2][x % 2], y, 0, 0, 0);
-                        }
-#pragma unroll
-                        for (int r = 0; r < 4; r++) sum[r] = fmaf(y[r], __uint_as_float((unsigned)kscale[64 * j + 4 * r + t] << 23) * kn, sum[r]);
-                    }
-                    mine[64 * t] = sum;
-                }
-#pragma unroll
-                for (int t = 0; t < 4; t++) {
-                    s[t] = mine[64 * t];
-#pragma unroll
-                    for (int r = 0; r < 4; r++) s[t][r] = there ? s[t][r] : -INFINITY;
-                }
-                share = weigh();
-#pragma unroll 1
-                for (int x = 0; x < NX; x++) {
-                    f32x4m sum = {0, 0, 0, 0};
-#pragma unroll 1
-                    for (int j = 0; j < 2; j++) {
-                        f32x4m y = {0, 0, 0, 0};
-#pragma unroll
-                        for (int z = 0; z < 2; z++) {
-                            const unsigned w = *(const unsigned*)(vp + 1024 * (x / 2) + 8 * (x % 2) + 4 * z);
-                            y = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen_e2m1(grp / 2 == j ? w : 0u, 1.0f), pb[z], y, 0, 0, 0);
-                        }
-#pragma unroll
-                        for (int r = 0; r < 4; r++) sum[r] = fmaf(y[r], __uint_as_float((unsigned)vscale[(16 * j + r) * (D / 16) + x] << 23) * vn, sum[r]);
-                    }
-                    mine[64 * x] = sum;
-                }
-#pragma unroll
-                for (int x = 0; x < NX; x++) {
-                    const f32x4m y = mine[64 * x];
-#pragma unroll
-                    for (int r = 0; r < 4; r++) acc[x][r] = fmaf(acc[x][r], corr, y[r]);
-                }
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                if (i + 1 < count) {
-                    load_k(i + 1);
-                    load_v(i + 1);
+                    for (int r = 0; r < 4; r++) s[t][r] = there ? s[t][r] * f : -INFINITY;
                 }
             }
+            // the next keys; the values are there when no more than those are under way
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (i + 1 < count) {
+                load_k(i + 1);
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
+            } else {
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            }
+            float corr;
+            const float share = soft_unit<UP>(s, row, corr, split_weight);
+            const float keep = vl == vl ? corr : vl;
+            unsigned ve[D / 64];
+#pragma unroll
+            for (int z = 0; z < D / 64; z++) ve[z] = *(const unsigned*)(vx + (16 * (grp / 2) + col) * (D / 16) + 4 * z);
+#pragma unroll
+            for (int z = 0; z < NX / 2; z++) {
+                const u32x4 w = *(const u32x4*)(vt + 1024 * z + 16 * lane);
+#pragma unroll
+                for (int u = 0; u < 2; u++) {
+                    const int x = 2 * z + u;
+                    const unsigned scale = scale_bits(ve[x / 4], x % 4);
+#pragma unroll
+                    for (int r = 0; r < 4; r++) acc[x][r] *= keep;
+#pragma unroll
+                    for (int y = 0; y < 2; y++) {
+                        const bf16x8 v = widen_e2m1(w[2 * u + y], scale);
+                        acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, ph[y], acc[x], 0, 0, 0);
+                        acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pl[y], acc[x], 0, 0, 0);
+                    }
+                }
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (i + 1 < count) load_v(i + 1);
             if (alone) shares[u0 + i][col] = share;
             else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(share), wbuf, wat + 4 * (u0 + i), 0, 0);
         }
@@ -916,7 +878,7 @@ __global__ __launch_bounds__(256, FORMAT == FORMAT_E2M1 ? 3 : D == 128 ? 2 : 4) 
             }
             f16x8 pb[2];
             float corr;
-            const float share = soft_unit(s, row, corr, [&](int t, int r, float p) { pb[t >> 1][4 * (t & 1) + r] = (_Float16)p; });
+            const float share = soft_unit<UP>(s, row, corr, [&](int t, int r, float p) { pb[t >> 1][4 * (t & 1) + r] = (_Float16)p; });
 #pragma unroll
             for (int x = 0; x < NX; x++) {
                 const int vr = 16 * x + col;
@@ -965,13 +927,8 @@ __global__ __launch_bounds__(256, FORMAT == FORMAT_E2M1 ? 3 : D == 128 ? 2 : 4) 
             }
             return w;
         };
-        bf16x8 ph[2], pl[2];
         float corr;
-        const float share = soft_unit(s, row, corr, [&](int t, int r, float p) {
-            const __bf16 hi = (__bf16)p;
-            ph[t >> 1][4 * (t & 1) + r] = hi;
-            pl[t >> 1][4 * (t & 1) + r] = (__bf16)(p - (float)hi);
-        });
+        const float share = soft_unit<UP>(s, row, corr, split_weight);
         if (alone) shares[ru.nsel][col] = share;
         else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(share), wbuf, wat + 4 * ru.nsel, 0, 0);
 #pragma unroll
@@ -1009,7 +966,7 @@ __global__ __launch_bounds__(256, FORMAT == FORMAT_E2M1 ? 3 : D == 128 ? 2 : 4) 
         if (alone) {
             const bool some_key = M > -INFINITY;
             a.o[(head0 + h) * D + d] = f32_to_bf16(some_key ? sum / den : 0.0f);
-            if (d == 0) a.lse[head0 + h] = log_of(M, den);
+            if (d == 0) a.lse[head0 + h] = log_of(M, den * ONE);
             continue;
         }
         const size_t at = (head0 + h) * a.splits + split;
@@ -1024,7 +981,7 @@ __global__ __launch_bounds__(256, FORMAT == FORMAT_E2M1 ? 3 : D == 128 ? 2 : 4) 
             float den = 0.0f;
 #pragma unroll
             for (int w = 0; w < 4; w++) den += sm_[w][h] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm_[w][h] - M) * sl[w][h];
-            if (shares[tid][h] != -INFINITY) sum += __builtin_amdgcn_exp2f(shares[tid][h] - (M + log2f(den * 0x1p-15f)));
+            if (shares[tid][h] != -INFINITY) sum += __builtin_amdgcn_exp2f(shares[tid][h] - (M + log2f(den * ONE)));
         }
         add_mass(a, ru, bg, tid, sum);
     }
@@ -1094,7 +1051,7 @@ __global__ __launch_bounds__(64 * NW) void cache8_join_kernel(AttnArgs a, int ma
                     y = fmaf(f, red[w][x], y);
                 }
             a.o[row * D + x] = f32_to_bf16(top > -INFINITY ? y / all : 0.0f);
-            if (x == 0) a.lse[row] = log_of(top, all);
+            if (x == 0) a.lse[row] = log_of(top, all * a.one);
         }
         return;
     }
@@ -1109,7 +1066,7 @@ __global__ __launch_bounds__(64 * NW) void cache8_join_kernel(AttnArgs a, int ma
         }
         const float top = wave_max_f32(M);
         L = wave_sum_f32(M > -INFINITY ? L * __builtin_amdgcn_exp2f(M - top) : 0.0f);
-        return top + log2f(L * 0x1p-15f);
+        return top + log2f(L * a.one);
     };
     const int g = (blockIdx.x - a.c.H) / mass_wgs, part = (blockIdx.x - a.c.H) % mass_wgs;
     if (part * 64 * NW >= nu) return;
@@ -1258,6 +1215,7 @@ static int attn_launch(const sparsek_cache8_cfg& c, const CacheArgs& cache, cons
     a.part_o = (float*)(w + y.part_o); a.part_ml = (float2*)(w + y.part_ml);
     a.weight = (float*)(w + y.weight);
     a.accumulate = accumulate;
+    a.one = c.format == SPARSEK_E2M1 ? Weight<0>::ONE : Weight<15>::ONE;
     a.units = y.units;
     a.o = (uint16_t*)o;
     a.lse = lse;

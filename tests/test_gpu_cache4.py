@@ -637,3 +637,64 @@ def test_wide_pages_among_others(H, Hkv, d):
     bad[0, H // 2:] = bad[1, H // 2:] = True
     assert torch.isnan(o[bad.cuda()]).all() and torch.isnan(lse[0, H // 2:]).all() and torch.isfinite(lse[1]).all()
     assert ((ref.f64(o) - ro).abs() <= ob)[~bad].all()
+
+
+def close(cache, lens, q, o, lse):
+    """Bounds of the attention with weights as two bf16 numbers: 2^-8 of what is rounded to bf16, 2^-16 of a weight (each of the two roundings 2^-8), and 2^-14
+    for sums in fp32 and exponentials (exponents up to 93 of two, of products rounded twice to fp32: 93 * 2^-23 * ln 2 = 2^-17)."""
+    torch.cuda.synchronize()
+    B, H, d = q.shape
+    G = H // cache.Hkv
+    for b in range(B):
+        for h in range(H):
+            K, V, _, _, _ = ref.row_tokens(cache, lens, b, h // G)
+            s = K @ ref.f64(q[b, h]) * cache.cfg.softmax_scale
+            p = torch.softmax(s, 0)
+            want, bound = p @ V, 2 ** -8 * (p @ V).abs() + (2 ** -16 + 2 ** -14) * (p @ V.abs())
+            e = (ref.f64(o[b, h]) - want).abs()
+            assert (e <= bound).all(), float((e / bound).max())
+            assert abs(float(lse[b, h]) - float(torch.logsumexp(s, 0))) <= 2e-4
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("at,n", [(9, 64), (9, 200), (70, 200), (194, 200), (9, 2000), (1500, 2000)])
+@pytest.mark.parametrize("key,e", [(-16, 20), (-16, 27), (-16, 40), (-24, 30), (-24, 36), (-32, 45), (-32, 60), (-64, 100)])
+def test_large_values_of_small_weights(key, e, at, n, d):
+    """A value of 2^e whose weight is exp(key) of the others', in their block, in another and in the unfinished one: what it adds is its product."""
+    require_gpu()
+    say("cache4, large values of small weights", key, e, at, n, d)
+    g = gen(131)
+    k, v, q = torch.zeros(1, 1, n, d).bfloat16().cuda(), rand(g, 1, 1, n, d), torch.zeros(1, 2, d).bfloat16().cuda()
+    q[:, 0, 0], q[:, 1, 0] = 1.0, 0.5
+    k[0, 0, at, 0] = key
+    v[0, 0, at, ::3] = 2.0 ** e
+    cache, L = given(k, v, 2, 40, scale=1.0)
+    close(cache, [n], q, *spk.sparsek_cache4_attn(cache, L, q))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("cap,n", [(3, 150), (40, 150), (40, 128)])
+@pytest.mark.parametrize("e", [60, 105, 112, 114, 118])
+def test_values_of_all_sizes(e, cap, n, d):
+    """Outputs of up to 2^e are finite, whether a block is whole or not.  (150 of them, four standard deviations each, sum up to less than 2^(e+10).)"""
+    require_gpu()
+    say("cache4, values of 2^%d" % e, cap, n, d)
+    g = gen(141)
+    k, v, q = rand(g, 1, 2, n, d), rand(g, 1, 2, n, d) * 2.0 ** e, rand(g, 1, 4, d)
+    cache, L = given(k, v, 4, cap)
+    close(cache, [n], q, *spk.sparsek_cache4_attn(cache, L, q))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("e", [10, 17, 20, 24, 30, 36, 60])
+def test_small_channels_of_queries_and_large_ones_of_keys(e, d):
+    """A query's channel of 2^-e meets keys of 2^e there: logits are as with 1 and 1."""
+    require_gpu()
+    say("cache4, small channels of queries", e, d)
+    g = gen(151)
+    n = 200
+    k, v, q = rand(g, 1, 1, n, d), rand(g, 1, 1, n, d), rand(g, 1, 2, d)
+    k[..., 3] = torch.tensor([-4.0, -2.0, 0.5, 1.0, 3.0, 6.0]).bfloat16().cuda()[torch.randint(0, 6, (n,), generator=g).cuda()] * 2.0 ** e
+    q[..., 3] = torch.tensor([3.0, -5.0]).cuda() * 2.0 ** -e
+    cache, L = given(k, v, 2, 4)
+    close(cache, [n], q, *spk.sparsek_cache4_attn(cache, L, q))
