@@ -299,3 +299,33 @@ def test_streamed_rows_of_all_kinds(dtype, d, rot, interleaved):
             held(o[one, :, rows], *ref.fwd(t, at, freq, axis, interleaved, True, wt, 1e-6))
             rx, _, bx, _ = ref.bwd(t, at, freq, axis, interleaved, True, wt, 1e-6, do[one, :, rows])
             held(dt[one, rows], rx, bx)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("kind", ["ladder", "quarters of a turn", "halves of a turn", "far"])
+def test_cosines_and_sines_in_fp32(kind, interleaved):
+    """Pairs (1, 0) become (cos a, sin a), and their gradients (cos a, -sin a), with the relative accuracy of fp32 where they are small too: 4 of the
+    function's last places (2^-23 of the value each) and the last rounding; 2^-51 of the angle for its two roundings to 64 bits and the
+    reference's; 2^-45 for what the angle's second part leaves out (the square of 2^-23.5)."""
+    require_gpu()
+    say("rope cosines", kind, interleaved)
+    g = gen(101)
+    B, n, d = 1, 3000, 64
+    pos, freq, _ = ladder(g, B, n, d, 1, far=2 ** 20 if kind == "far" else 4000)
+    if kind in ("quarters of a turn", "halves of a turn"):   # (next to them: as far as pi in fp32 is from pi, for each position)
+        freq = torch.full((d // 2,), 3.141592653589793 / (2 if kind == "quarters of a turn" else 1)).cuda()
+        freq[d // 4:] *= 1 + 2.0 ** -20 * torch.arange(d // 4).cuda()
+    elif kind == "far":
+        freq = (6.28 * torch.rand(d // 2, generator=g)).cuda()
+    x = torch.zeros(B, n, 2, d, device="cuda")
+    first = slice(0, None, 2) if interleaved else slice(0, d // 2)
+    second = slice(1, None, 2) if interleaved else slice(d // 2, None)
+    x[..., first] = 1.0
+    qo, ko = spk.sparsek_rope_fwd(x, x[:, :, :1], pos, freq, interleaved=interleaved)
+    heads = x.transpose(1, 2).contiguous()
+    dq, dk, _, _ = spk.sparsek_rope_bwd(x, x[:, :, :1], pos, freq, heads, heads[:, :1].contiguous(), interleaved=interleaved)
+    torch.cuda.synchronize()
+    a = ref.angles(pos, freq, None).transpose(1, 2)
+    for got, sign in ((qo, 1), (ko, 1), (dq.transpose(1, 2), -1), (dk.transpose(1, 2), -1)):
+        for part, want in ((first, torch.cos(a)), (second, sign * torch.sin(a))):
+            held(got[..., part], want.expand(-1, got.shape[1], -1, -1), (5 * 2 ** -23 * want.abs() + 2 ** -51 * a.abs() + 2 ** -45).expand(-1, got.shape[1], -1, -1))
