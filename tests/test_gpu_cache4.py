@@ -698,3 +698,55 @@ def test_small_channels_of_queries_and_large_ones_of_keys(e, d):
     q[..., 3] = torch.tensor([3.0, -5.0]).cuda() * 2.0 ** -e
     cache, L = given(k, v, 2, 4)
     close(cache, [n], q, *spk.sparsek_cache4_attn(cache, L, q))
+
+
+@pytest.mark.parametrize("d,n,begin", [(64, 33001, 37), (128, 17001, 130)])
+def test_long_ranges_that_are_read(d, n, begin):
+    """Outputs of more than 100 MB, which go past the caches: every stretch has the bits that it has in a short read, over lengths inside and outside the range,
+    a page with a value that is not finite and pages outside the pool; what was not asked for is not written."""
+    require_gpu()
+    say("cache4 long read", d, n, begin)
+    lens, Hkv = [begin + n + 200, 9017, 0], 4
+    assert 4 * len(lens) * Hkv * n * d > 100e6
+    cap = (begin + n) // 64 + 5
+    cache, g = shuffled(spk.Cache4.empty(len(lens), Hkv, Hkv, d, cap), 161), gen(162)
+    k, v = (torch.randn(Hkv, 4000, d, generator=g).bfloat16().cuda()[:, torch.arange(max(lens), device="cuda") % 4000].expand(len(lens), -1, -1, -1).contiguous()
+            for _ in range(2))
+    k[0, 1, 700, 3], v[1, 2, 5000, 9] = float("nan"), float("inf")
+    L = ints(lens)
+    spk.sparsek_cache4_append(cache, torch.zeros_like(L), k, v, counts=L)
+    cache.table[0, 3, 40], cache.table[1, 0, 30] = -1, cache.cfg.pages
+    room = torch.full((2, len(lens) * Hkv * n * d + 256), 5.0, dtype=torch.bfloat16, device="cuda")
+    out = tuple(x[128:-128].view(len(lens), Hkv, n, d) for x in room)
+    rk, rv = spk.sparsek_cache4_read(cache, L, begin, n, out=out)
+    torch.cuda.synchronize()
+    assert (room[:, :128] == 5).all() and (room[:, -128:] == 5).all()
+    for a in range(0, n, 4001):
+        c = min(4001, n - a)
+        for got, want in zip((rk, rv), spk.sparsek_cache4_read(cache, L, begin + a, c)):
+            assert torch.equal(got[:, :, a:a + c].contiguous().view(torch.int16), want.view(torch.int16)), a
+    assert rk[0, 1].isnan().any() and rv[1, 2].isnan().any() and not rk[1].isnan().any()
+    assert (rk[1, :, 9017 - begin:] == 0).all() and (rv[2] == 0).all() and (rk[0, 3, 40 * 64 - begin:41 * 64 - begin] == 0).all()
+    clean = slice(10 * 64, 20 * 64)
+    for got, given_, dim in ((rk, k, -1), (rv, v, -2)):
+        want = ref.rounded(given_[0, 0, clean].unflatten(0, (-1, 64)), dim).flatten(0, 1)
+        assert torch.equal(ref.f64(got[0, 0, 10 * 64 - begin:20 * 64 - begin]), want)
+
+
+def test_reading_more_than_2_31_values():
+    require_gpu()
+    say("cache4 read of more than 2^31 values")
+    B, Hkv, d, cap, n = 8, 4, 128, 8192, 530000
+    assert B * Hkv * n * d > 2 ** 31
+    cache, g = spk.Cache4.empty(B, Hkv, Hkv, d, cap, pages=64 * B * Hkv), gen(171)
+    spk.sparsek_cache4_append(cache, torch.zeros(B, dtype=torch.int32).cuda(), rand(g, B, Hkv, 4096, d), rand(g, B, Hkv, 4096, d))
+    cache.table.copy_(torch.randint(0, 64 * B * Hkv, cache.table.shape, generator=g, dtype=torch.int32))
+    cache.kt.copy_(rand(g, *cache.kt.shape))
+    cache.vt.copy_(rand(g, *cache.vt.shape))
+    lens = ints([cap * 64 + 63, 500, 100000, 0, 1, 300000, 64 * 8000, cap * 64 + 63])
+    rk, rv = spk.sparsek_cache4_read(cache, lens, 0, n)
+    for a in (0, 99900, 299900, cap * 64 - 100):
+        for got, want in zip((rk, rv), spk.sparsek_cache4_read(cache, lens, a, 300)):
+            assert torch.equal(got[:, :, a:a + 300], want), a
+    torch.cuda.synchronize()
+    assert (rk[7, 3, cap * 64 + 63:] == 0).all() and (rk[7, 3, :cap * 64 + 63].abs().amax(-1) > 0).all()

@@ -329,3 +329,39 @@ def test_cosines_and_sines_in_fp32(kind, interleaved):
     for got, sign in ((qo, 1), (ko, 1), (dq.transpose(1, 2), -1), (dk.transpose(1, 2), -1)):
         for part, want in ((first, torch.cos(a)), (second, sign * torch.sin(a))):
             held(got[..., part], want.expand(-1, got.shape[1], -1, -1), (5 * 2 ** -23 * want.abs() + 2 ** -51 * a.abs() + 2 ** -45).expand(-1, got.shape[1], -1, -1))
+
+
+@pytest.mark.parametrize("norm,keys", [(False, True), (False, False), (True, False)])
+@pytest.mark.parametrize("dtype,d,rot", [(BF16, 128, 128), (BF16, 64, 64), (BF16, 112, 96), (F32, 64, 64), (F32, 40, 24)])
+def test_streamed_calls_without_norms_or_keys(dtype, d, rot, norm, keys):
+    """Forward and backward past the caches (a backward without norms reads no inputs): stretches of tokens as they are alone, and the definition's."""
+    require_gpu()
+    say("rope streamed", "norm" if norm else "no norm", "keys" if keys else "no keys", dtype, d, rot)
+    g = gen(111)
+    B, H, Hkv = 2, 5, 2 if keys else 0
+    n = 230_000_000 // (2 * B * (H + Hkv) * d * (2 if dtype is BF16 else 4)) | 1
+    x = torch.randn(B, 1000, (H + 2 * Hkv) * d, generator=g).to(dtype).cuda()
+    x = x[:, torch.arange(n, device="cuda") % 1000]
+    parts = [x[..., :H * d].unflatten(-1, (H, d)), x[..., H * d:(H + Hkv) * d].unflatten(-1, (Hkv, d)) if keys else None]
+    pos, freq, axis = ladder(g, B, n, rot, 2, far=100000)
+    w = (1 + 0.2 * torch.randn(2, d, generator=g)).cuda()
+    args = dict(axis=axis, norm=norm, qw=w[0] if norm else None, kw=w[1] if norm and keys else None)
+    outs = spk.sparsek_rope_fwd(*parts, pos, freq, **args)
+    grads = [o.flip(2).contiguous() if o is not None else None for o in outs]
+    back = spk.sparsek_rope_bwd(*parts, pos, freq, *grads, **args)
+    torch.cuda.synchronize()
+    for b, rows in ((0, slice(0, 300)), (0, slice(n - 77, n)), (1, slice(0, 77)), (1, slice(n // 2, n // 2 + 100)), (1, slice(n - 300, n))):
+        one = slice(b, b + 1)
+        cut = lambda t, heads_first: None if t is None else t[one, :, rows].contiguous() if heads_first else t[one, rows]   # noqa: E731
+        at = pos[:, one, rows].contiguous()
+        got = spk.sparsek_rope_fwd(*(cut(t, False) for t in parts), at, freq, **args)
+        short = spk.sparsek_rope_bwd(*(cut(t, False) for t in parts), at, freq, *(cut(t, True) for t in grads), **args)
+        torch.cuda.synchronize()
+        for t, o, do, dt, a, c, wt in zip(parts, outs, grads, back, got, short, w if norm else (None, None)):
+            if t is None:
+                assert o is None and dt is None
+                continue
+            assert torch.equal(a, o[one, :, rows]) and torch.equal(c, dt[one, rows])
+            held(a, *ref.fwd(t[one, rows], at, freq, axis, False, norm, wt, 1e-6))
+            rx, _, bx, _ = ref.bwd(t[one, rows], at, freq, axis, False, norm, wt, 1e-6, do[one, :, rows])
+            held(c, rx, bx)
