@@ -388,7 +388,7 @@ int sparsek_cache8_evict(const sparsek_cache8_cfg *cfg, const sparsek_cache8 *ca
  * read: k, v [B,Hkv,n,d] out of `dtype`: tokens begin .. begin+n-1 of every sequence as they are attended (the unfinished block's as they were
  *     given), NaN for all of a page that holds one which is not finite; zeros behind a sequence's end and for blocks whose page is outside the pool.
  * begin >= 0, n >= 1 (INVALID_ARG), begin + n <= 2^28 (UNSUPPORTED).  k4, v4, ke, ve, km, kt, vt and all tensors of q, k, v, o and ws begin at multiples of 16
- * bytes; outputs overlap no inputs. */
+ * bytes; outputs overlap no inputs, nor each other (read: INVALID_ARG). */
 #define SPARSEK_E2M1 4
 typedef struct {
     void *k4, *v4;

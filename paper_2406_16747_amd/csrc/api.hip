@@ -479,6 +479,25 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb)
     return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
 }
 
+struct Place {
+    const void* p;
+    size_t n;
+    bool on(const Place& x) const { return p && x.p && n && x.n && overlap(p, n, x.p, x.n); }
+};
+
+// Whether an output lies over an input or over another output.
+template <int IN, int OUT>
+bool any_overlap(const Place (&in)[IN], const Place (&out)[OUT])
+{
+    for (int x = 0; x < OUT; x++) {
+        for (const Place& y : in)
+            if (out[x].on(y)) return true;
+        for (int y = 0; y < x; y++)
+            if (out[x].on(out[y])) return true;
+    }
+    return false;
+}
+
 // Both caches: the same checks, and the same launches.
 struct Of8 {
     typedef sparsek_cache8 Cache;
@@ -704,6 +723,11 @@ int sparsek_cache4_read(const sparsek_cache8_cfg* cfg, const sparsek_cache4* cac
     if (rc) return rc;
     if (!lens || !k || !v || begin < 0 || n < 1 || !Of4::wide(*cache) || !aligned({k, v})) return SPARSEK_ERR_INVALID_ARG;
     if ((long long)begin + n > (1 << 28)) return SPARSEK_ERR_UNSUPPORTED;
+    const size_t pages = cfg->pages, rows = (size_t)cfg->B * cfg->Hkv, d = cfg->d, tail = rows * 64 * d * 2;
+    const Place in[] = {{cache->k4, pages * 32 * d}, {cache->v4, pages * 32 * d}, {cache->ke, pages * 2 * d}, {cache->ve, pages * 2 * d}, {cache->ks, pages * 4},
+                        {cache->vs, pages * 4}, {cache->kt, tail}, {cache->vt, tail}, {cache->table, rows * cfg->cap * 4}, {lens, cfg->B * 4u}};
+    const Place out[] = {{k, rows * n * d * 2}, {v, rows * n * d * 2}};
+    if (any_overlap(in, out)) return SPARSEK_ERR_INVALID_ARG;
     return spk::launch_cache4_read(*cfg, *cache, lens, begin, n, k, v, (hipStream_t)stream);
 }
 
@@ -797,25 +821,6 @@ int check_rope(const sparsek_rope_cfg* c)
     if ((long long)c->H + c->Hkv > 65535 || (long long)c->B * c->n > (1ll << 26)) return SPARSEK_ERR_UNSUPPORTED;
     if (!good(*c, c->q, c->H) || (c->Hkv && !good(*c, c->k, c->Hkv))) return SPARSEK_ERR_INVALID_ARG;
     return SPARSEK_OK;
-}
-
-struct Place {
-    const void* p;
-    size_t n;
-    bool on(const Place& x) const { return p && x.p && n && x.n && overlap(p, n, x.p, x.n); }
-};
-
-// Whether an output lies over an input or over another output.
-template <int IN, int OUT>
-bool any_overlap(const Place (&in)[IN], const Place (&out)[OUT])
-{
-    for (int x = 0; x < OUT; x++) {
-        for (const Place& y : in)
-            if (out[x].on(y)) return true;
-        for (int y = 0; y < x; y++)
-            if (out[x].on(out[y])) return true;
-    }
-    return false;
 }
 
 // Arguments that both directions share.  (x_read: q and k are read.)

@@ -109,3 +109,22 @@ def test_every_entry_point_of_the_header_is_there():
     assert len(names) == 6
     for name in names:
         assert getattr(spk.lib(), name), name
+
+
+def test_reading_over_the_cache_or_itself():
+    """(2 heads of 40 tokens of 64: 10240 bytes each.)  Outputs that lie over each other, or over what is read."""
+    L, c = spk.lib(), ccfg()
+    far = lambda x, more=0: ctypes.c_void_p((x << 32) + more)   # noqa: E731
+    names = [n for n, _ in spk.SparsekCache4._fields_]
+    t = spk.SparsekCache4(**{n: (x + 1) << 32 for x, n in enumerate(names)})
+    k, v, lens = far(20), far(21), far(22)
+    for more in (0, 16, 10224):
+        assert L.sparsek_cache4_read(c, t, lens, 0, 40, k, far(20, more), NULL) == -1
+        assert L.sparsek_cache4_read(c, t, lens, 0, 40, far(20, more), k, NULL) == -1
+    for n in names:
+        if n not in ("km", "kms", "mass"):   # (which reading does not look at)
+            for more in (0, -10224):
+                at = far(names.index(n) + 1, more)
+                assert L.sparsek_cache4_read(c, t, lens, 0, 40, at, v, NULL) == -1, n
+                assert L.sparsek_cache4_read(c, t, lens, 0, 40, k, at, NULL) == -1, n
+    assert L.sparsek_cache4_read(c, t, lens, 0, 40, lens, v, NULL) == -1
