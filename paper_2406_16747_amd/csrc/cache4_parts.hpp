@@ -2,7 +2,8 @@
 //
 // A value is an e2m1 code (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign) times a power of two that 32 values share: of keys 32 channels of a token, of
 // values 32 tokens of a channel.  The power is the smallest with which none of the 32 passes 6, so a value is off by a fifth of the
-// largest at most (where that is 5 times the power, 4 stands for it), and scaling loses nothing.  Inside a page codes and scales lie as the
+// largest at most (where that is 5 times the power, 4 stands for it), and scaling loses nothing.  Two exceptions: where the largest is above 6 * 2^125 the
+// power stays 2^125 and 6 of them stand for it (off by a quarter of bf16's largest number, at most), and where it is below 2^-100 zeros do.  Inside a page codes and scales lie as the
 // lanes of the matrix instructions take them, 16 bytes of codes to a lane at a time: the attention's loads are whole lines, straight into LDS.
 #pragma once
 #include "block_parts.hpp"

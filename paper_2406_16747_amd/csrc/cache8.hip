@@ -6,7 +6,7 @@
 // followed: such a page is neither written nor attended.
 //
 // What bounds the kernels is memory where there is much to move (four prompts of up to 8192 go in at 5.9 TB/s, 64 sequences of up to 8192 are
-// attended at 5.4 TB/s of the kernel's time, in 4 bits at 5.2) and the length of a chain of dependent steps where there is little: a token's
+// attended at 5.4 TB/s of the kernel's time, in 4 bits at 5.1) and the length of a chain of dependent steps where there is little: a token's
 // append takes 3 us, 6 to 8 where it ends a block; the choice among 1024 blocks 12; the attention of 200 tokens 6 to 8; an eviction from
 // 129 blocks 6.
 #include "cache4_parts.hpp"
@@ -1180,11 +1180,12 @@ static Cache8Layout cache8_layout(const sparsek_cache8_cfg& c, int top)
     // they leave idle weigh less the fewer units each has: 64 sequences of up to 8192 127.5 us with 5, 128.3 with 4, 130 with 3, 136 with 2).
     const long long rows = (long long)c.B * c.Hkv * y.groups, all = rows * y.units;
     // In 4 bits a unit is half as long and the second launch weighs more: one workgroup for up to 28, or 40 where there is one for every compute unit
-    // (sequences of up to 2400, 38 units: 64 of them 31.6 us in one and 39.1 in two, 32 of them 22.7 and 25.3, 8 of them 20.8 and 19.4; of up to 1400, 22
-    // units: 23.2 and 37.6 for 64, 15.4 and 19.5 for 4).
-    // In 4 bits, whose waves are 12 to a compute unit, what 2048 waves leave over is rounded up where it is more than a 32nd: 544 workgroups of two units
-    // to a wave take as long as 768 (attention and join of one sequence with 8 heads: of 34000 19.7 us, with three units 17.4; of 28000 19.9 with one unit,
-    // 16.5 with two), but 520 do not (of 32768: 17.1 with two, 17.4 with three; of 65536 22.1 with four, 22.9 with five).
+    // (a token of 8 key/value heads, append and attention, sequences of up to 2400, 38 units: 64 of them 33.1 us in one and 38.3 in two, 32 of them 24.0 and
+    // 26.4, 8 of them 21.6 and 17.2; of up to 1400, 22 units: 24.5 and 35.8 for 64, 16.3 and 18.1 for 4).  Whole sequences, that is: selections go by the
+    // same rule, which was not measured on them.
+    // In 4 bits, what 2048 waves leave over is rounded up where it is more than a 32nd: 544 workgroups of two units to a wave take as long as 768
+    // (attention and join of one sequence with 8 heads: of 34000 20.1 us, with three units 18.5; of 28000 19.2 with one unit, 17.0 with two), but 520 do
+    // not (of 32768: 17.7 with two, 18.7 with three; of 65536 23.3 with four, 24.2 with five).
     const int most = 5, alone = c.format != SPARSEK_E2M1 ? most : rows >= 256 ? MAX_UPW : 7, over = c.format != SPARSEK_E2M1 ? 0 : 2048 - 2048 / 32;
     if (y.units <= 4 * alone && y.groups == 1) y.upw = (y.units + 3) / 4;
     else y.upw = (int)std::max<long long>(1, std::min<long long>(most, (all + over) / 2048));
@@ -1223,8 +1224,8 @@ static int attn_launch(const sparsek_cache8_cfg& c, const CacheArgs& cache, cons
     BY_FORMAT(c, ATTN)
 #undef ATTN
     if (y.splits == 1 && y.groups == 1) return launch_status();
-    // In 4 bits up to 8 parts are one wave's, on their way together (64 sequences of up to 8192, 7 parts each: 5.0 us, with 4 waves 7.0; of 65 parts,
-    // one sequence of 32768: 16 waves 4.4, 4 waves 4.3).
+    // In 4 bits up to 8 parts are one wave's, on their way together (64 sequences of up to 8192, 7 parts each: 4.9 us, with 4 waves 6.9; of 65 parts,
+    // one sequence of 32768: 16 waves 4.4, 4 waves 4.3).  The masses, which that wave makes a head at a time, were not measured either way.
     const int nw = c.format == SPARSEK_E2M1 && y.splits <= 8 ? 1 : 4;
     const int mass_wgs = accumulate ? (y.units + 64 * nw - 1) / (64 * nw) : 0;
     const dim3 join(c.H + c.Hkv * mass_wgs, c.B);

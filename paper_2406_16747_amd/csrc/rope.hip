@@ -7,7 +7,7 @@
 // A row is one head of one token.  Its lanes have 8 channels each, four and the four that they turn with (pairs half a rotation apart), or
 // four of either half (neighbours), so a pair never leaves a lane; a token's lanes go through the heads, and the angles, which depend on the
 // token alone, are made once.  What bounds it is memory: a document of 32768, 32 + 8 heads of 128, is normed and turned in 135 us, at 5.0 TB/s
-// (a copy of 1 GiB reaches 5.1), its vector instructions beside that for 60 % of the time; backward 4 x 8192 tokens of 32 heads take 170 us (4.7).
+// (a copy of 1 GiB reaches 5.1), its vector instructions beside that for 43 % of the time; backward 4 x 8192 tokens of 32 heads take 170 us (4.7).
 // In a call that is streamed every load and store takes whole lines: where a row's halves end inside one, its wave's lanes load what lies side by side
 // and hand it over in LDS.
 #include "block_parts.hpp"
@@ -149,9 +149,10 @@ __device__ __forceinline__ void turn(bool interleaved, bool back, const Chunk& c
     }
 }
 
-// Rows of a token that are on their way together.  Four where much is streamed in bf16 (a document of 32768, 32 + 8 heads of 128: 135 us, one
-// at a time 140; training on video, 4 x 8192 tokens, 281 and 307); one where the caches have it (a document of 8192 38.5 us, four 41.4) and in fp32,
-// whose rows are twice as long (a training pass of 4 x 2000, 24 heads of 64: 57 us, four 70; of 16 x 2000 198 and 199).
+// Rows of a token that are on their way together.  Four where much is streamed in bf16 (a document of 32768, 32 + 8 heads of 128: 132 us, one
+// at a time 139; training on video, 4 x 8192 tokens of 16 + 16 heads, 280 and 305); one where the caches have it (training on 4 x 1250 of those tokens 53.9 us,
+// four 59.7; on 4 x 500 29 and 31; forward two prompts of 5003, 16 + 2 heads, 17.3 and 17.8, but a document of 5000 24.0 and 22.1) and in fp32, whose rows are
+// twice as long (a training pass of 4 x 2000, 24 heads of 64, its backward streamed: 50 us, four 62.5).
 template <class T, bool STREAM>
 constexpr int rows_at_once() { return STREAM && sizeof(T) == 2 ? 4 : 1; }
 
