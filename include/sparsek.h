@@ -383,8 +383,8 @@ int sparsek_cache8_evict(const sparsek_cache8_cfg *cfg, const sparsek_cache8 *ca
  *                                 NaN: it holds a value that is not finite, and NaN is what a query gets that attends it
  * The other tensors, lens, and what holds of pages are those of sparsek_cache8, and so are append, select, attn and evict; cfg.format is
  * SPARSEK_E2M1.  Where sparsek_cache4_attn_workspace_bytes answers 256, attn's ws may be NULL.
- * attn: weights are held to 2^-16 (below 2^-126 of the row's largest: 0), values and queries as they are, sums in fp32: outputs are finite where the sum of
- * the attended values' magnitudes is.
+ * attn: weights are held to 2^-16 (below 2^-126 of the row's largest: 0), values and keys as they are, queries but for channels below 2^-62, sums in fp32:
+ * outputs are finite where the sum of the attended values' magnitudes is, for logits below 2^64.
  * read: k, v [B,Hkv,n,d] out of `dtype`: tokens begin .. begin+n-1 of every sequence as they are attended (the unfinished block's as they were
  *     given), NaN for all of a page that holds one which is not finite; zeros behind a sequence's end and for blocks whose page is outside the pool.
  * begin >= 0, n >= 1 (INVALID_ARG), begin + n <= 2^28 (UNSUPPORTED).  k4, v4, ke, ve, km, kt, vt and all tensors of q, k, v, o and ws begin at multiples of 16

@@ -475,7 +475,7 @@ struct AttnArgs {
     const uint16_t* q;
     const int32_t* idx;    // [B,Hkv,top] or null: all blocks
     int top, splits, upw;  // parts of a row, units per wave
-    float c2;
+    float c2, q_scale;     // log2 e times the softmax's scale is their product; q_scale: a power of two, 1 in 8 bits
     float* part_o;         // [B,H,splits][D]
     float2* part_ml;       // [B,H,splits]: the largest logit (times log2 e), the sum
     float one;             // Weight::ONE of part_o and of these sums
@@ -689,7 +689,7 @@ __global__ __launch_bounds__(256, FORMAT == FORMAT_E2M1 ? 3 : D == 128 ? 2 : 4) 
         vs = a.c.t.vs[page];
     }
     // Q^T: head col, columns 64 half + 16 grp + 8 sub .. (in 4 bits: a lane's are those of one scale or half of one).  In 8 bits relative to the
-    // head's largest value, in 4 as they are.
+    // head's largest value, in 4 times q_scale.
     constexpr int QG = FOUR ? D / 4 : 16, QH = FOUR ? 16 : 64;
     const uint16_t* qr = a.q + (head0 + min(col, live - 1)) * D + QG * grp;
     u32x4 qw[KH][2];
@@ -718,6 +718,16 @@ __global__ __launch_bounds__(256, FORMAT == FORMAT_E2M1 ? 3 : D == 128 ? 2 : 4) 
             for (int s = 0; s < 2; s++)
 #pragma unroll
                 for (int e = 0; e < 8; e++) qf[h][s][e] = (_Float16)(half_of(qw[h][s], e) * down);
+    } else {
+#pragma unroll
+        for (int h = 0; h < KH; h++)
+#pragma unroll
+            for (int s = 0; s < 2; s++) {
+                bf16x8 x;
+#pragma unroll
+                for (int e = 0; e < 8; e++) x[e] = (__bf16)(half_of(qw[h][s], e) * a.q_scale);
+                qw[h][s] = __builtin_bit_cast(u32x4, x);
+            }
     }
     f32x4m acc[NX];
 #pragma unroll
@@ -910,8 +920,10 @@ __global__ __launch_bounds__(256, FORMAT == FORMAT_E2M1 ? 3 : D == 128 ? 2 : 4) 
 #pragma unroll
             for (int h = 0; h < KH; h++)
 #pragma unroll
-                for (int x = 0; x < 2; x++)
-                    s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8*)(kp + tok * D + QH * h + QG * grp + 8 * x), *(const bf16x8*)(qr + QH * h + 8 * x), s[t], 0, 0, 0);
+                for (int x = 0; x < 2; x++) {
+                    const bf16x8 qx = FOUR ? __builtin_bit_cast(bf16x8, qw[h][x]) : *(const bf16x8*)(qr + QH * h + 8 * x);
+                    s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8*)(kp + tok * D + QH * h + QG * grp + 8 * x), qx, s[t], 0, 0, 0);
+                }
 #pragma unroll
             for (int r = 0; r < 4; r++) s[t][r] = 16 * grp + 4 * t + r < ru.tail ? s[t][r] * a.c2 : -INFINITY;
         }
@@ -1212,6 +1224,14 @@ static int attn_launch(const sparsek_cache8_cfg& c, const CacheArgs& cache, cons
     a.splits = y.splits;
     a.upw = y.upw;
     a.c2 = c.softmax_scale * 1.4426950408889634f;
+    a.q_scale = 1.0f;
+    if (c.format == SPARSEK_E2M1 && a.c2 < 1.0f) {
+        // Half of it goes to the queries: products then overflow only where logits pass 2^64, and bits are lost only by channels of queries below
+        // 2^-124 at ordinary scales, 2^-62 at one of 2^-126 (with all of it there, those of 1 would lose some).
+        const int e = std::ilogb(a.c2) / 2;
+        a.q_scale = std::ldexp(1.0f, e);
+        a.c2 = std::ldexp(a.c2, -e);
+    }
     char* w = (char*)ws;
     a.part_o = (float*)(w + y.part_o); a.part_ml = (float2*)(w + y.part_ml);
     a.weight = (float*)(w + y.weight);

@@ -750,3 +750,16 @@ def test_reading_more_than_2_31_values():
             assert torch.equal(got[:, :, a:a + 300], want), a
     torch.cuda.synchronize()
     assert (rk[7, 3, cap * 64 + 63:] == 0).all() and (rk[7, 3, :cap * 64 + 63].abs().amax(-1) > 0).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [128, 150, 2000])
+@pytest.mark.parametrize("eq,ek", [(0, 100), (0, 123), (60, 60), (100, 20), (0, -95), (-60, -30), (-100, 100), (-20, 120)])
+def test_queries_and_keys_of_all_sizes(eq, ek, n, d):
+    """Queries of 2^eq and keys of 2^ek whose scale makes ordinary logits of them: products beyond fp32's range are no logits beyond it."""
+    require_gpu()
+    say("cache4, queries and keys of all sizes", eq, ek, n, d)
+    g = gen(181)
+    k, v, q = rand(g, 1, 2, n, d) * 2.0 ** ek, rand(g, 1, 2, n, d), rand(g, 1, 4, d) * 2.0 ** eq
+    cache, L = given(k, v, 4, 40, scale=d ** -0.5 * 2.0 ** (-eq - ek))
+    close(cache, [n], q, *spk.sparsek_cache4_attn(cache, L, q))
